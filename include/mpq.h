@@ -306,6 +306,102 @@ int mpq_linear_host_prepared(const float* x_host, const uint32_t* w_planes, cons
                              int32_t* out_i32_host, float* out_f32_host,
                              void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ==== Operators of an encoded decoder block ====================================================
+ * The method's quantizer and level product (Eq. 15-18) where a transformer serves tokens: one
+ * range per TOKEN instead of one per tensor, operands as level bytes for the 8-bit tensor cores,
+ * and keys and values held on levels in a paged cache.  (The paper sets no such layers; the
+ * quantizer, the levels and the scale rule are its own, see mpq_encode and mpq_gemm.)
+ *
+ * Level bytes: an operand [rows x k] holds the level index u (0..2^bits-1) of each element in one
+ * byte, rows mpq_level_row_bytes(k) = k rounded up to 16 bytes apart, the bytes behind element k-1
+ * are 0.  Beside them: scale[rows] (range of the row) and sums[rows] = sum over the row of u, which
+ * the product needs to turn sum u_a u_w into sum q_a q_w.  An element stands for (2u - L) * (s / L),
+ * L = 2^bits - 1.
+ * dtype arguments are mpq_dtype; row, token and head strides are in elements; the elements of a row
+ * (or of one head) are adjacent.  Strides and addresses need no alignment beyond the type's own
+ * (16-byte aligned ones run faster) unless stated. */
+typedef enum { MPQ_F32 = 0, MPQ_F16 = 1, MPQ_BF16 = 2 } mpq_dtype;
+/* Activation of a product's epilogue: none, max(y,0), y Phi(y) (erf form), the tanh form of the same, y / (1 + e^-y). */
+typedef enum { MPQ_GLUE_NONE = 0, MPQ_GLUE_RELU = 1, MPQ_GLUE_GELU = 2, MPQ_GLUE_GELU_TANH = 3, MPQ_GLUE_SILU = 4 } mpq_glue;
+
+int64_t mpq_level_row_bytes(int64_t k);
+
+/* Root-mean-square norm with the residual's addition and level output.  Per row, in fp32:
+ *   h = x (+ residual);  y = (h * gain) * (1 / sqrt(mean(h^2) + eps));  s = max |y|;
+ *   u = quantizer of mpq_encode (HTanh, `bits`) of y with range s.
+ * x, residual, residual_out: [rows x k] of `dtype`, row strides ldx, ldr, ldo.  residual may be NULL;
+ * residual_out (h rounded once to dtype; may be NULL) may be the same tensor as x or residual.
+ * gain: k floats or NULL (ones).  levels / scale / sums as above, all required.  values (optional,
+ * [rows x k] of values_dtype, row stride ldv): the numbers the levels stand for, rounded once, for
+ * consumers that stay in full precision.  A row with a NaN or an infinity gets a NaN range.
+ * rows = 0 is allowed and does nothing.  k < 2^23. */
+int mpq_rmsnorm_levels(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype,
+                       const float* gain, float eps, int64_t rows, int64_t k, int bits,
+                       void* residual_out, int64_t ldo,
+                       uint8_t* levels, float* scale, int32_t* sums,
+                       void* values, int values_dtype, int64_t ldv, void* stream);
+
+/* The same without the norm: range (as mpq_absmax with one range per row gives it) and level bytes
+ * (as mpq_encode decides them) of each row -- weights, once, and activations inside a block. */
+int mpq_encode_levels(const void* x, int64_t ldx, int dtype, int64_t rows, int64_t k, int act, int bits,
+                      uint8_t* levels, float* scale, int32_t* sums,
+                      void* values, int values_dtype, int64_t ldv, void* stream);
+
+/* Product of level bytes with bias, activation and residual in its epilogue:
+ *   acc = sum_t q_a[r][t] q_w[c][t]   (exact, = mpq_gemm's c_i32 for the same levels)
+ *   f   = float(acc) * ((a_scale[r] / L_a) * (w_scale[c] / L_w));  f += bias[c] (optional);
+ *   f   = glue(f);  f += residual[r][c] (optional, of `dtype`, row stride ldr);  out = f rounded once.
+ * a [m] rows and w [n] rows of level bytes over k elements, both 16-byte aligned, with their scales
+ * and level sums.  out [m x n] of `dtype`, row stride ldo; it may be the residual's own tensor.
+ * k (2^a_bits - 1)(2^w_bits - 1) < 2^31.  m = 0 is allowed and does nothing. */
+int mpq_linear_levels(const uint8_t* a, const float* a_scale, const int32_t* a_sums, int a_bits,
+                      const uint8_t* w, const float* w_scale, const int32_t* w_sums, int w_bits,
+                      int64_t m, int64_t n, int64_t k,
+                      const float* bias, int glue, const void* residual, int64_t ldr,
+                      void* out, int dtype, int64_t ldo, void* stream);
+
+/* Paged cache of keys and values on levels of 8 or 4 bits, one range per (token, head):
+ *   levels [pages][heads][page_size][dim * bits / 8] bytes, 16-byte aligned, scale [pages][heads][page_size],
+ * once for the keys, once for the values.  With 4 bits byte i holds element 2i in its low half and
+ * element 2i+1 in its high half.  dim is a multiple of 32, at most 256.  A slot is
+ * page * page_size + position in the page.
+ * mpq_cache_write quantizes `tokens` keys and values [token][head][dim] and puts token t at slots[t];
+ * a slot outside the cache (-1 by convention) writes nothing.  Slots of one call are distinct.
+ * mpq_cache_read is the way back: the values that the levels at slots[t] stand for, rounded once to
+ * dtype; zeros for a slot outside the cache. */
+int mpq_cache_write(const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                    const void* v, int64_t v_token_stride, int64_t v_head_stride, int dtype,
+                    const int64_t* slots, int64_t tokens, int heads, int dim, int bits,
+                    uint8_t* k_levels, float* k_scale, uint8_t* v_levels, float* v_scale,
+                    int64_t pages, int page_size, void* stream);
+int mpq_cache_read(const uint8_t* k_levels, const float* k_scale, const uint8_t* v_levels, const float* v_scale,
+                   int64_t pages, int page_size, const int64_t* slots, int64_t tokens, int heads, int dim, int bits,
+                   void* k, int64_t k_token_stride, int64_t k_head_stride,
+                   void* v, int64_t v_token_stride, int64_t v_head_stride, int dtype, void* stream);
+
+/* Attention of new tokens over the paged cache (their own keys and values written to it before).
+ * Sequence b has the new tokens q_starts[b] .. q_starts[b+1]-1 of q [tokens][heads][dim] and a context
+ * of kv_lens[b] tokens, the new ones last; its token j lies in page table[b][j / page_size] (row stride
+ * table_stride; kv_lens beyond table_stride * page_size are cut).  New token i of n sees
+ *   pos = kv_lens[b] - n + i:   j <= pos if causal, j > pos - window if window > 0, j < kv_lens[b];
+ * a token of the context whose page number lies outside the cache is not seen.
+ *   out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j);  lse = log sum_j p_j (optional, [tokens][heads]).
+ * A row that sees nothing gets out = 0 and lse = -infinity.  heads is a multiple of kv_heads; query
+ * head h reads key head h / (heads / kv_heads).  dim is 64 or 128; dtype (q and out) MPQ_F16 or MPQ_BF16.
+ * max_q and max_kv are the caller's upper bounds on a sequence's new tokens and context; they choose
+ * the launch (how rows are tiled, how far a context is split), any value gives the same sums.
+ * workspace: mpq_cache_attention_workspace() bytes for the same sizes, 16-byte aligned (NULL if 0). */
+int64_t mpq_cache_attention_workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim,
+                                      int64_t max_q, int64_t max_kv);
+int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, int dtype,
+                        const int32_t* q_starts, const int32_t* kv_lens, const int32_t* table, int64_t table_stride,
+                        int64_t tokens, int batch, int heads, int kv_heads, int dim, int64_t max_q, int64_t max_kv,
+                        const uint8_t* k_levels, const float* k_scale, const uint8_t* v_levels, const float* v_scale,
+                        int bits, int64_t pages, int page_size,
+                        int causal, int64_t window, float scale,
+                        void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                        void* workspace, int64_t workspace_bytes, void* stream);
+
 /* ---- Roofline denominator: measures this GPU's 32-bit population-count issue rate with a
  * register-only loop (no memory traffic) and the SM clock it ran at.  Synchronous.
  * popc_per_s: lane-level POPC results per second over the whole chip; sm_mhz: SM clock

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -86,6 +86,21 @@ def lib() -> ctypes.CDLL:
         L.mpq_measure_b1_mma_peak.argtypes = [i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double),
                                               ctypes.POINTER(ctypes.c_int), P]
         L.mpq_measure_b1_mma_peak.restype = i32
+        f32 = ctypes.c_float
+        L.mpq_level_row_bytes.argtypes = [i64]
+        L.mpq_level_row_bytes.restype = i64
+        L.mpq_rmsnorm_levels.argtypes = [P, i64, P, i64, i32, P, f32, i64, i64, i32, P, i64, P, P, P, P, i32, i64, P]
+        L.mpq_encode_levels.argtypes = [P, i64, i32, i64, i64, i32, i32, P, P, P, P, i32, i64, P]
+        L.mpq_linear_levels.argtypes = [P, P, P, i32, P, P, P, i32, i64, i64, i64, P, i32, P, i64, P, i32, i64, P]
+        L.mpq_cache_write.argtypes = [P, i64, i64, P, i64, i64, i32, P, i64, i32, i32, i32, P, P, P, P, i64, i32, P]
+        L.mpq_cache_read.argtypes = [P, P, P, P, i64, i32, P, i64, i32, i32, i32, P, i64, i64, P, i64, i64, i32, P]
+        L.mpq_cache_attention_workspace.argtypes = [i64, i32, i32, i32, i32, i64, i64]
+        L.mpq_cache_attention_workspace.restype = i64
+        L.mpq_cache_attention.argtypes = [P, i64, i64, i32, P, P, P, i64, i64, i32, i32, i32, i32, i64, i64, P, P, P, P,
+                                          i32, i64, i32, i32, i64, f32, P, i64, i64, P, P, i64, P]
+        for name in ("mpq_rmsnorm_levels", "mpq_encode_levels", "mpq_linear_levels", "mpq_cache_write", "mpq_cache_read",
+                     "mpq_cache_attention"):
+            getattr(L, name).restype = i32
         for name in ("mpq_absmax", "mpq_encode", "mpq_encode_nchw", "mpq_encode_oihw", "mpq_gemm", "mpq_conv",
                      "mpq_add_relu", "mpq_stem_conv7x7", "mpq_maxpool3x3s2", "mpq_conv_fused", "mpq_zero", "mpq_linear", "mpq_linear_static", "mpq_linear_host", "mpq_measure_popc_peak",
                      "mpq_encode_with", "mpq_encode_ranged", "mpq_gemm_fused", "mpq_conv_encoded", "mpq_linear_host_prepared",
@@ -426,6 +441,196 @@ def linear_host_prepared(x_host: torch.Tensor, w_planes: torch.Tensor, w_scale: 
                                           m, n, k, a_bits, w_bits, a_act, w_mode, hp(out_i32_host), hp(out_f32_host),
                                           workspace.data_ptr(), workspace.numel(), _stream()), "mpq_linear_host_prepared")
     return out_i32_host, out_f32_host
+
+
+# ---- operators of an encoded decoder block ------------------------------------------------------
+F32, F16, BF16 = 0, 1, 2
+GLUE = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+_DTYPE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+
+
+def _dtype(t: torch.dtype) -> int:
+    if t not in _DTYPE:
+        raise ValueError("expected float32, float16 or bfloat16, got %s" % t)
+    return _DTYPE[t]
+
+
+class Levels(NamedTuple):
+    """An operand on level bytes: bytes uint8 [rows][level_row_bytes(k)], scale and sums [rows], its width and k."""
+    bytes: torch.Tensor
+    scale: torch.Tensor
+    sums: torch.Tensor
+    bits: int
+    k: int
+
+
+class LevelCache(NamedTuple):
+    """A paged cache on levels: k and v uint8 [pages][heads][page_size][dim * bits / 8], their ranges [pages][heads][page_size]."""
+    k: torch.Tensor
+    k_scale: torch.Tensor
+    v: torch.Tensor
+    v_scale: torch.Tensor
+    bits: int
+
+
+def level_row_bytes(k: int) -> int:
+    return int(lib().mpq_level_row_bytes(k))
+
+
+def _rows(t: Optional[torch.Tensor], shape, dtype=None):
+    """(pointer, row stride) of a matrix whose rows are contiguous; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or tuple(t.shape) != tuple(shape) or (dtype is not None and t.dtype != dtype):
+        raise ValueError("expected a CUDA tensor of shape %s%s, got %s %s" % (
+            tuple(shape), "" if dtype is None else " and dtype %s" % dtype, t.dtype, tuple(t.shape)))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("the elements of a row have to be adjacent")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _vector(t: Optional[torch.Tensor], n: int, dtype) -> Optional[int]:
+    if t is not None and t.numel() != n:
+        raise ValueError("expected %d values, got %d" % (n, t.numel()))
+    return _ptr(t, dtype)
+
+
+def _level_outputs(rows: int, k: int, bits: int, device, out: Optional[Levels]) -> Levels:
+    if out is None:
+        return Levels(torch.empty((rows, -(-k // 16) * 16), dtype=torch.uint8, device=device),
+                      torch.empty(rows, dtype=torch.float32, device=device),
+                      torch.empty(rows, dtype=torch.int32, device=device), bits, k)
+    if tuple(out.bytes.shape) != (rows, -(-k // 16) * 16) or out.bits != bits or out.k != k:
+        raise ValueError("the output levels are of another shape or width")
+    return out
+
+
+def rmsnorm_levels(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float, bits: int = 8,
+                   residual: Optional[torch.Tensor] = None, residual_out: Optional[torch.Tensor] = None,
+                   values: Optional[torch.Tensor] = None, out: Optional[Levels] = None) -> Levels:
+    """Root-mean-square norm of x (+ residual) [rows x k], quantized with one range per row.  residual_out receives
+    x + residual (it may be x or residual), values the numbers that the levels stand for."""
+    rows, k = x.shape
+    px, ldx = _rows(x, x.shape)
+    pr, ldr = _rows(residual, x.shape, x.dtype)
+    po, ldo = _rows(residual_out, x.shape, x.dtype)
+    pv, ldv = _rows(values, x.shape)
+    out = _level_outputs(rows, k, bits, x.device, out)
+    _check(lib().mpq_rmsnorm_levels(px, ldx, pr, ldr, _dtype(x.dtype), _vector(gain, k, torch.float32), eps, rows, k, bits,
+                                    po, ldo, _ptr(out.bytes, torch.uint8), _vector(out.scale, rows, torch.float32),
+                                    _vector(out.sums, rows, torch.int32), pv, 0 if pv is None else _dtype(values.dtype), ldv,
+                                    _stream()), "mpq_rmsnorm_levels")
+    return out
+
+
+def encode_levels(x: torch.Tensor, bits: int = 8, act: int = ACT_HTANH, values: Optional[torch.Tensor] = None,
+                  out: Optional[Levels] = None) -> Levels:
+    """[rows x k] -> level bytes with one range per row (weights, once; activations inside a block)."""
+    rows, k = x.shape
+    px, ldx = _rows(x, x.shape)
+    pv, ldv = _rows(values, x.shape)
+    out = _level_outputs(rows, k, bits, x.device, out)
+    _check(lib().mpq_encode_levels(px, ldx, _dtype(x.dtype), rows, k, act, bits, _ptr(out.bytes, torch.uint8),
+                                   _vector(out.scale, rows, torch.float32), _vector(out.sums, rows, torch.int32),
+                                   pv, 0 if pv is None else _dtype(values.dtype), ldv, _stream()), "mpq_encode_levels")
+    return out
+
+
+def linear_levels(a: Levels, w: Levels, bias: Optional[torch.Tensor] = None, act: str = "none",
+                  residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """act(a w^T + bias) + residual on level operands: a [m x k], w [n x k] -> [m x n] of ``dtype`` (or of ``out``)."""
+    m, n = a.bytes.shape[0], w.bytes.shape[0]
+    if a.k != w.k or a.bytes.shape[1] != w.bytes.shape[1] or a.bytes.shape[1] != -(-a.k // 16) * 16:
+        raise ValueError("the operands' rows differ: %d and %d elements" % (a.k, w.k))
+    if act not in GLUE:
+        raise ValueError("unknown activation %r: expected one of %s" % (act, ", ".join(GLUE)))
+    if out is None:
+        out = torch.empty((m, n), dtype=dtype, device=a.bytes.device)
+    po, ldo = _rows(out, (m, n))
+    pr, ldr = _rows(residual, (m, n), out.dtype)
+    _check(lib().mpq_linear_levels(_ptr(a.bytes, torch.uint8), _vector(a.scale, m, torch.float32), _vector(a.sums, m, torch.int32), a.bits,
+                                   _ptr(w.bytes, torch.uint8), _vector(w.scale, n, torch.float32), _vector(w.sums, n, torch.int32), w.bits,
+                                   m, n, a.k, _vector(bias, n, torch.float32), GLUE[act], pr, ldr, po, _dtype(out.dtype), ldo,
+                                   _stream()), "mpq_linear_levels")
+    return out
+
+
+def level_cache(pages: int, heads: int, page_size: int, dim: int, bits: int, device="cuda") -> LevelCache:
+    """An empty paged cache (pages * heads * page_size * (dim * bits / 8 + 4) bytes for the keys, and the same for the values)."""
+    rows = [torch.zeros((pages, heads, page_size, dim * bits // 8), dtype=torch.uint8, device=device) for _ in range(2)]
+    ranges = [torch.zeros((pages, heads, page_size), dtype=torch.float32, device=device) for _ in range(2)]
+    return LevelCache(rows[0], ranges[0], rows[1], ranges[1], bits)
+
+
+def _cache(c: LevelCache):
+    pages, heads, page_size, row = c.k.shape
+    if c.v.shape != c.k.shape or c.k_scale.shape != c.k.shape[:3] or c.v_scale.shape != c.k.shape[:3]:
+        raise ValueError("the cache's keys, values and ranges differ in shape")
+    return (pages, heads, page_size, row * 8 // c.bits if c.bits else 0,
+            _ptr(c.k, torch.uint8), _ptr(c.k_scale, torch.float32), _ptr(c.v, torch.uint8), _ptr(c.v_scale, torch.float32))
+
+
+def _heads(t: torch.Tensor, shape, dtype=None):
+    """(pointer, token stride, head stride) of a [tokens][heads][dim] tensor whose head rows are contiguous."""
+    if not t.is_cuda or tuple(t.shape) != tuple(shape) or (dtype is not None and t.dtype != dtype):
+        raise ValueError("expected a CUDA tensor of shape %s%s, got %s %s" % (
+            tuple(shape), "" if dtype is None else " and dtype %s" % dtype, t.dtype, tuple(t.shape)))
+    if t.stride(2) != 1:
+        raise ValueError("the elements of a head have to be adjacent")
+    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1] * shape[2]), (t.stride(1) if shape[1] > 1 else shape[2])
+
+
+def cache_write(cache: LevelCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> LevelCache:
+    """Quantizes keys and values [tokens][heads][dim] into the cache at ``slots`` (int64; -1: not written)."""
+    pages, heads, page_size, dim, pk, pks, pv, pvs = _cache(cache)
+    shape = (k.shape[0], heads, dim)
+    _check(lib().mpq_cache_write(*_heads(k, shape), *_heads(v, shape, k.dtype), _dtype(k.dtype), _vector(slots, k.shape[0], torch.int64),
+                                 k.shape[0], heads, dim, cache.bits, pk, pks, pv, pvs, pages, page_size, _stream()), "mpq_cache_write")
+    return cache
+
+
+def cache_read(cache: LevelCache, slots: torch.Tensor, dtype: torch.dtype, k: Optional[torch.Tensor] = None,
+               v: Optional[torch.Tensor] = None):
+    """The keys and values at ``slots`` as [tokens][heads][dim] of ``dtype`` (zeros for a slot of -1)."""
+    pages, heads, page_size, dim, pk, pks, pv, pvs = _cache(cache)
+    shape = (slots.numel(), heads, dim)
+    k = torch.empty(shape, dtype=dtype, device=slots.device) if k is None else k
+    v = torch.empty(shape, dtype=dtype, device=slots.device) if v is None else v
+    _check(lib().mpq_cache_read(pk, pks, pv, pvs, pages, page_size, _ptr(slots, torch.int64), shape[0], heads, dim, cache.bits,
+                                *_heads(k, shape, dtype), *_heads(v, shape, dtype), _dtype(dtype), _stream()), "mpq_cache_read")
+    return k, v
+
+
+def cache_attention_workspace(tokens: int, batch: int, heads: int, kv_heads: int, dim: int, max_q: int, max_kv: int) -> int:
+    return int(lib().mpq_cache_attention_workspace(tokens, batch, heads, kv_heads, dim, max_q, max_kv))
+
+
+def cache_attention(q: torch.Tensor, cache: LevelCache, q_starts: torch.Tensor, kv_lens: torch.Tensor, table: torch.Tensor,
+                    max_q: int, max_kv: int, causal: bool = True, window: int = 0, scale: Optional[float] = None,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens q [tokens][heads][dim] of ``batch`` sequences (token ranges q_starts [batch + 1]) over
+    their contexts of kv_lens [batch] tokens in the pages table [batch][..] names.  scale defaults to dim ** -0.5."""
+    pages, kv_heads, page_size, dim, pk, pks, pv, pvs = _cache(cache)
+    tokens, heads = q.shape[0], q.shape[1]
+    batch = kv_lens.numel()
+    pq, qt, qh = _heads(q, (tokens, heads, dim))
+    if out is None:
+        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
+    po, ot, oh = _heads(out, (tokens, heads, dim), q.dtype)
+    if table.dim() != 2 or table.shape[0] != batch:
+        raise ValueError("expected a page table of %d rows" % batch)
+    if workspace is None:
+        need = lib().mpq_cache_attention_workspace(tokens, batch, heads, kv_heads, dim, max_q, max_kv)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _check(lib().mpq_cache_attention(pq, qt, qh, _dtype(q.dtype), _vector(q_starts, batch + 1, torch.int32), _vector(kv_lens, batch, torch.int32),
+                                     _ptr(table, torch.int32), table.shape[1], tokens, batch, heads, kv_heads, dim, max_q, max_kv, pk, pks, pv, pvs,
+                                     cache.bits, pages, page_size, int(causal), window, dim ** -0.5 if scale is None else scale,
+                                     po, ot, oh, _vector(lse, tokens * heads, torch.float32),
+                                     None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
+                                     _stream()), "mpq_cache_attention")
+    return out
 
 
 def measure_popc_peak():

@@ -20,7 +20,11 @@ ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 # IEEE arithmetic is part of the contract (bit-exact codes): never --use_fast_math / -ftz.
 
-PLAIN = ["mpq_api.cu", "mpq_encode.cu", "mpq_encode_trig.cu", "mpq_gemm.cu", "mpq_glue.cu", "mpq_probe.cu"]
+PLAIN = ["mpq_api.cu", "mpq_encode.cu", "mpq_encode_trig.cu", "mpq_gemm.cu", "mpq_glue.cu", "mpq_probe.cu",
+         "mpq_levels.cu", "mpq_linear_levels.cu", "mpq_cache.cu", "mpq_attention.cu"]
+# headers of the decoder-block operators only: the other sources are not rebuilt for them
+BLOCK_HEADERS = ["mpq_levels.cuh", "mpq_attention.cuh"]
+BLOCK_SOURCES = {"mpq_levels.cu", "mpq_linear_levels.cu", "mpq_cache.cu", "mpq_attention.cu"}
 HEADERS = ["mpq_common.cuh", "mpq_branch_kernel.cuh", "mpq_branch_launch.cuh", "mpq_pointwise_kernel.cuh", os.path.join(INCLUDE, "mpq.h")]
 
 
@@ -32,8 +36,9 @@ def _jobs():
     return jobs
 
 
-def _newest_header():
-    paths = [h if os.path.isabs(h) else os.path.join(CSRC, h) for h in HEADERS]
+def _newest_header(src):
+    names = HEADERS + (BLOCK_HEADERS if os.path.basename(src) in BLOCK_SOURCES else [])
+    paths = [h if os.path.isabs(h) else os.path.join(CSRC, h) for h in names]
     return max(os.path.getmtime(p) for p in paths)
 
 
@@ -48,11 +53,10 @@ def _compile(job, verbose):
 
 def build(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(OBJ_DIR, exist_ok=True)
-    hdr = _newest_header()
     todo = []
     for job in _jobs():
         src, obj, _ = job
-        if force or not os.path.exists(obj) or os.path.getmtime(obj) < max(os.path.getmtime(src), hdr):
+        if force or not os.path.exists(obj) or os.path.getmtime(obj) < max(os.path.getmtime(src), _newest_header(src)):
             todo.append(job)
     if todo:
         with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as ex:

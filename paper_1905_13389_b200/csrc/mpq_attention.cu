@@ -1,0 +1,446 @@
+// Attention over a paged cache of levels for few query rows (mpq_cache_attention): tiles of 16 rows.
+//
+// A CTA of four warps takes 16 query rows (tokens x heads of one key head) and a stretch of the context;
+// each warp runs an online softmax of its own over every fourth chunk of 32 tokens and the four are merged
+// at the end.  Level bytes go from global memory straight into the operand registers of
+// mma.sync.m16n8k16: the element order inside a dot product is free, so the 16 bytes that a lane loads ARE
+// its operand fragment, for the keys (lane = token, bytes along dim) and for the values (lane = 16 dims of
+// a token pair).  With 16 rows the work is bound by reading the cache, not by the matrix pipe (which is why
+// the 128-row tcgen05 tile, seven eighths of it empty here, is not used), and nothing is staged in shared
+// memory.  The keys of the next chunk are loaded while the softmax and the value product of this one run.
+#include "mpq_attention.cuh"
+
+namespace mpq {
+
+constexpr int kRows = 16, kChunk = 32, kWarps = 4;
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Two 16-bit lanes 1024 + u (u in the low bits, 0x6400 above) -> fp16 2u - (L + 1), exact: the even
+// neighbour below the level 2u - L.  The missing 1 is added back per row (sum of q, sum of w).
+template <int BITS>
+__device__ __forceinline__ uint32_t even_level(uint32_t x) {
+    constexpr float c = BITS == 8 ? -2304.0f : -2064.0f;
+    const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), __float2half2_rn(2.0f), __float2half2_rn(c));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Word of level bytes -> operand register `pair` (0, 1: BITS = 8; 0..3: BITS = 4): elements pair*2, pair*2+1
+// of the word for 8 bits, pair and pair + 4 for 4 bits.
+template <int BITS>
+__device__ __forceinline__ uint32_t key_pair(uint32_t w, int pair) {
+    if (BITS == 8) return even_level<8>(__byte_perm(w, 0x64646464u, pair ? 0x4342 : 0x4140));
+    return even_level<4>(((w >> (4 * pair)) & 0x000f000fu) | 0x64006400u);
+}
+// Element i (0..3 for 8 bits, 0..7 for 4 bits) of the words of two tokens, side by side.
+template <int BITS>
+__device__ __forceinline__ uint32_t value_pair(uint32_t a, uint32_t b, int i) {
+    if (BITS == 8) return even_level<8>((__byte_perm(a, b, 0x0400 + 0x0101 * i) & 0x00ff00ffu) | 0x64006400u);
+    return even_level<4>(((__byte_perm(a, b, i < 4 ? 0x5410 : 0x7632) >> (4 * (i & 3))) & 0x000f000fu) | 0x64006400u);
+}
+// Position inside a row of the element that operand register `pair` of word `word` holds in its low half
+// (the high half holds + 1 for 8 bits, + 4 for 4 bits), for lane column t.
+template <int D, int BITS>
+__device__ __forceinline__ int key_element(int word, int pair, int t) {
+    constexpr int kPerLane = D / 4;                       // elements of a lane
+    constexpr int kPerWord = 32 / BITS, kWords = kPerLane / kPerWord;
+    if (BITS == 8) {
+        if (kWords <= 4) return t * kPerLane + word * 4 + pair * 2;
+        return (word >> 2) * (D / 2) + t * 16 + (word & 3) * 4 + pair * 2;      // two 16-byte loads, half a row apart
+    }
+    return t * kPerLane + word * 8 + pair;
+}
+
+// Words of `bytes` level bytes loaded by a lane.
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
+    if constexpr (N == 4) { const uint4 v = __ldg(reinterpret_cast<const uint4*>(p)); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+    else if constexpr (N == 2) { const uint2 v = __ldg(reinterpret_cast<const uint2*>(p)); w[0] = v.x; w[1] = v.y; }
+    else { w[0] = __ldg(reinterpret_cast<const uint32_t*>(p)); }
+}
+
+template <typename T, int D, int BITS>
+__global__ void __launch_bounds__(kWarps * 32)
+attn_rows_kernel(const AttnArgs g) {
+    constexpr int kRowBytes = D * BITS / 8;
+    constexpr int kKeyWords = D / 4 * BITS / 32;          // words of a key row per lane (4 lanes share a row)
+    constexpr int kKeyLoads = kKeyWords > 4 ? 2 : 1;      // ... in loads of at most 16 bytes
+    constexpr int kKeyStep = kKeyWords / kKeyLoads;
+    constexpr int kValWords = D / 8 * BITS / 32;          // words of a value row per lane (8 lanes share a row)
+    constexpr int kPairs = 16 / BITS;                     // operand registers per word (keys)
+    constexpr int kSteps = D / 16;                        // k-steps of the score product
+    constexpr int kTiles = D / 8;                         // 8-wide output tiles of the value product
+    __shared__ float sh_ml[kWarps][kRows][2];
+    __shared__ float sh_o[kWarps][kRows][D / 2 + 4];      // half of the dims at a time
+
+    chain_entry();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int gr = lane >> 2, t4 = lane & 3;
+    const int kv_head = blockIdx.y;
+    AttnTile t;
+    if (!find_tile<kRows>(g, blockIdx.x, t)) return;
+    tile_range<kRows, kChunk>(g, t);
+    const int used = tile_splits(g, t);
+    if ((int)blockIdx.z >= used) return;
+    int begin, end;
+    split_range(g, t, blockIdx.z, used, begin, end);
+    const int32_t* pages_of = g.table + (int64_t)t.b * g.table_stride;
+
+    // ---- queries: rows gr and gr + 8 as operand fragments
+    uint32_t qf[kSteps][4];
+    float row_scale[2], qsum[2];
+    int first[2], last[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int r = t.row0 + gr + 8 * half;
+        const bool live = r < t.rows;
+        const int token = live ? r / g.group : 0, head = kv_head * g.group + (live ? r % g.group : 0);
+        const T* q = static_cast<const T*>(g.q) + (int64_t)(t.q0 + token) * g.q_ts + (int64_t)head * g.q_hs;
+        float amax = 0.0f;
+        float lo[kSteps][2], hi[kSteps][2];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int reg = s * 2 + i;                              // operand register counted along the row
+                const int e = key_element<D, BITS>(reg / kPairs, reg % kPairs, t4);
+                lo[s][i] = live ? to_f32(q[e]) : 0.0f;
+                hi[s][i] = live ? to_f32(q[e + (BITS == 8 ? 1 : 4)]) : 0.0f;
+                amax = fmaxf(amax, fmaxf(fabsf(lo[s][i]), fabsf(hi[s][i])));
+            }
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        float down, up, sum = 0.0f;
+        row_power(amax, down, up);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const __half2 h = __floats2half2_rn(lo[s][i] * down, hi[s][i] * down);
+                qf[s][i * 2 + half] = *reinterpret_cast<const uint32_t*>(&h);
+                sum += __low2float(h) + __high2float(h);
+            }
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        qsum[half] = sum;
+        row_scale[half] = up * g.scale_log2;
+        row_range(g, t, token, first[half], last[half]);
+        if (!live) { first[half] = 0; last[half] = 0x7fffffff; }   // computed with q = 0, never stored: no masks on its account
+    }
+
+    float o[kTiles][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, wsum[2] = {0.0f, 0.0f};
+
+    // ---- context: this warp's chunks
+    // lane's token of a chunk: row number in the cache and the token's ranges (0 where there is no token)
+    auto chunk_rows = [&](int c0, uint32_t& row, float& ks, float& vs) {
+        const int j = c0 + lane;
+        row = j < end ? context_row(g, pages_of, j, kv_head) : 0xffffffffu;
+        ks = vs = 0.0f;
+        if (row != 0xffffffffu) { ks = __ldg(g.k_scale + row); vs = __ldg(g.v_scale + row); }
+    };
+    uint32_t kw[4][kKeyWords];
+    auto load_keys = [&](uint32_t row) {
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+            const uint32_t r = __shfl_sync(0xffffffffu, row, nt * 8 + gr);
+            const uint8_t* p = g.k_levels + (uint64_t)(r == 0xffffffffu ? 0 : r) * kRowBytes + t4 * (kKeyStep * 4);
+#pragma unroll
+            for (int i = 0; i < kKeyLoads; ++i) load_words<kKeyStep>(p + i * (kRowBytes / 2), kw[nt] + i * kKeyStep);
+        }
+    };
+    uint32_t row, next_row = 0xffffffffu;
+    float ks, vs, next_ks = 0.0f, next_vs = 0.0f;
+    int c0 = begin + warp * kChunk;
+    if (c0 < end) {
+        chunk_rows(c0, row, ks, vs);
+        load_keys(row);
+    }
+    for (; c0 < end; c0 += kWarps * kChunk) {
+        const int cn = c0 + kWarps * kChunk;
+        // values of this chunk, and where the next chunk lies
+        uint32_t vw[2][4][kValWords];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = __shfl_sync(0xffffffffu, row, kt * 16 + t4 * 2 + (i & 1) + (i >> 1) * 8);
+                load_words<kValWords>(g.v_levels + (uint64_t)(r == 0xffffffffu ? 0 : r) * kRowBytes + gr * (kValWords * 4), vw[kt][i]);
+            }
+        if (cn < end) chunk_rows(cn, next_row, next_ks, next_vs);
+        // scores
+        float s[4][4];
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                const int reg = k * 2;
+                mma_f16(s[nt], qf[k], key_pair<BITS>(kw[nt][reg / kPairs], reg % kPairs), key_pair<BITS>(kw[nt][(reg + 1) / kPairs], (reg + 1) % kPairs));
+            }
+        }
+        if (cn < end) load_keys(next_row);
+        // y = x + log2 of the value's range; masks only where the chunk needs them
+        float lg, inv;
+        range_exponent(vs, lg, inv);
+        const float kf = ks * (1.0f / (float)((1 << BITS) - 1));
+        const uint32_t here = __ballot_sync(0xffffffffu, row != 0xffffffffu);
+        const bool whole = here == 0xffffffffu && __all_sync(0xffffffffu, c0 >= max(first[0], first[1]) && c0 + kChunk - 1 <= min(last[0], last[1]));
+        float ivs[4][2], mx[2] = {m[0], m[1]};
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int src = nt * 8 + t4 * 2 + e;
+                const float kj = __shfl_sync(0xffffffffu, kf, src), lj = __shfl_sync(0xffffffffu, lg, src);
+                ivs[nt][e] = __shfl_sync(0xffffffffu, inv, src);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float y = fmaf((s[nt][half * 2 + e] + qsum[half]) * kj, row_scale[half], lj);
+                    if (!whole) {
+                        const int j = c0 + src;
+                        if (!((here >> src) & 1) || j < first[half] || j > last[half]) y = -INFINITY;
+                    }
+                    s[nt][half * 2 + e] = y;
+                    mx[half] = fmaxf(mx[half], y);
+                }
+            }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            mx[half] = fmaxf(mx[half], __shfl_xor_sync(0xffffffffu, mx[half], 1));
+            mx[half] = fmaxf(mx[half], __shfl_xor_sync(0xffffffffu, mx[half], 2));
+        }
+        if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const float f = mx[half] == m[half] ? 1.0f : fast_exp2(m[half] - mx[half]);       // m = -inf: 0
+                m[half] = mx[half];
+                l[half] *= f; wsum[half] *= f;
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i) { o[i][half * 2] *= f; o[i][half * 2 + 1] *= f; }
+            }
+        }
+        const float ref[2] = {m[0] == -INFINITY ? 0.0f : m[0] - kBoost, m[1] == -INFINITY ? 0.0f : m[1] - kBoost};
+        uint32_t pf[2][4];
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float w[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float y = s[nt][half * 2 + e];
+                    w[e] = fast_exp2(y - ref[half]);
+                    // a token that is not seen may have any range: its reciprocal must not meet the 0
+                    l[half] = whole || y != -INFINITY ? fmaf(w[e], ivs[nt][e], l[half]) : l[half];
+                }
+                const __half2 h = __floats2half2_rn(w[0], w[1]);
+                wsum[half] += __low2float(h) + __high2float(h);
+                pf[nt >> 1][(nt & 1) * 2 + half] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+        }
+        // values
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) {
+                constexpr int kPer = 32 / BITS;
+                const int word = i / kPer, e = i % kPer;
+                mma_f16(o[i], pf[kt], value_pair<BITS>(vw[kt][0][word], vw[kt][1][word], e), value_pair<BITS>(vw[kt][2][word], vw[kt][3][word], e));
+            }
+        row = next_row; ks = next_ks; vs = next_vs;
+    }
+
+    // ---- merge: rows of the four warps, then the splits (by attn_merge_kernel) or the result
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int d = 1; d <= 2; d <<= 1) {
+            l[half] += __shfl_xor_sync(0xffffffffu, l[half], d);
+            wsum[half] += __shfl_xor_sync(0xffffffffu, wsum[half], d);
+        }
+        if (t4 == 0) { sh_ml[warp][gr + 8 * half][0] = m[half]; sh_ml[warp][gr + 8 * half][1] = l[half]; }
+    }
+    __syncthreads();
+    constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);
+    float factor[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh_ml[w][gr + 8 * half][0]);
+        factor[half] = (m[half] == -INFINITY ? 0.0f : fast_exp2(m[half] - top)) * kInvL;
+    }
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {                  // lanes gr < 4 hold the first half of the dims, gr >= 4 the second
+        if (part) __syncthreads();
+        // column of output tile i for this lane's columns 2 t4, 2 t4 + 1 (as lane index of the value operand): dim = lane * D/8 + i
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int owner = t4 * 2 + e;                   // which eighth of the row
+            if (owner / 4 == part) {
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        sh_o[warp][gr + 8 * half][(owner & 3) * kTiles + i] = (o[i][half * 2 + e] + wsum[half]) * factor[half];
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < kRows * (D / 2); i += kWarps * 32) {
+            const int r = i / (D / 2), d = i % (D / 2);
+            if (t.row0 + r >= t.rows) continue;
+            float top = -INFINITY, den = 0.0f, num = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh_ml[w][r][0]);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float mw = sh_ml[w][r][0];
+                if (mw != -INFINITY) den += sh_ml[w][r][1] * fast_exp2(mw - top);
+                num += sh_o[w][r][d];
+            }
+            const int token = (t.row0 + r) / g.group, head = kv_head * g.group + (t.row0 + r) % g.group;
+            const int64_t at = (int64_t)(t.q0 + token) * g.heads + head;
+            if (used > 1) {
+                const int64_t slot = at * g.splits + blockIdx.z;
+                g.part_o[slot * D + part * (D / 2) + d] = num;
+                if (part == 0 && d == 0) g.part_ml[slot] = make_float2(top, den);
+            } else {
+                const float v = top == -INFINITY ? 0.0f : final_value(num / den);
+                static_cast<T*>(g.out)[(int64_t)(t.q0 + token) * g.o_ts + (int64_t)head * g.o_hs + part * (D / 2) + d] = from_f32<T>(v);
+                if (g.lse && part == 0 && d == 0)
+                    g.lse[at] = top == -INFINITY ? -INFINITY : (top - kBoost + log2f(den)) * 0.6931471805599453f;
+            }
+        }
+    }
+}
+
+// Splits of a context -> result: one warp per (token, head).
+template <typename T, int D, int R, int CHUNK>
+__global__ void __launch_bounds__(128) attn_merge_kernel(const AttnArgs g) {
+    chain_entry();
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (at >= g.tokens * g.heads) return;
+    const int token = (int)(at / g.heads), head = (int)(at % g.heads);
+    // the sequence that holds the token: the last one that starts at or before it and is not empty there
+    int lo = 0, hi = g.batch;                                // q_starts[lo] <= token < q_starts[hi] is kept
+    if (g.q_starts[0] > token || g.q_starts[g.batch] <= token) return;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (g.q_starts[mid] <= token) lo = mid; else hi = mid;
+    }
+    AttnTile t;
+    t.b = lo; t.q0 = g.q_starts[lo];
+    t.n_q = (int)min((int64_t)g.q_starts[lo + 1], g.tokens) - t.q0;
+    t.rows = t.n_q * g.group;
+    t.row0 = ((token - t.q0) * g.group + head % g.group) / R * R;
+    tile_range<R, CHUNK>(g, t);
+    const int used = tile_splits(g, t);
+    if (used <= 1) return;                                   // stored by the split itself
+    float top = -INFINITY, den = 0.0f;
+    for (int s = 0; s < used; ++s) top = fmaxf(top, g.part_ml[at * g.splits + s].x);
+    float acc[D / 32] = {};
+    for (int s = 0; s < used; ++s) {
+        const float2 ml = g.part_ml[at * g.splits + s];
+        const float f = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
+        den = ml.x == -INFINITY ? den : fmaf(ml.y, f, den);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(g.part_o[(at * g.splits + s) * D + i * 32 + lane], f, acc[i]);
+    }
+    T* out = static_cast<T*>(g.out) + (int64_t)token * g.o_ts + (int64_t)head * g.o_hs;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) out[i * 32 + lane] = from_f32<T>(top == -INFINITY ? 0.0f : final_value(acc[i] / den));
+    if (g.lse && lane == 0) g.lse[at] = top == -INFINITY ? -INFINITY : (top - kBoost + log2f(den)) * 0.6931471805599453f;
+}
+
+// Tiles of `rows` query rows that `tokens` new tokens in at most `batch` sequences can fill.
+inline int64_t tile_bound(int64_t tokens, int batch, int group, int rows) {
+    return tokens * group / rows + (tokens < batch ? tokens : batch);
+}
+
+struct AttnPlan { int64_t tiles; int splits, split_tokens; };
+
+// How far a context is split: enough CTAs for about three rounds of four per multiprocessor, at least one
+// chunk per warp in each.
+AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_kv) {
+    AttnPlan p;
+    p.tiles = tile_bound(tokens, batch, group, kRows);
+    const int64_t want = 148 * 4 * 3;
+    int64_t per = ceil_div(max_kv * p.tiles * kv_heads, want);
+    per = ceil_div(per < 1 ? 1 : per, kChunk * kWarps) * (kChunk * kWarps);
+    int64_t splits = ceil_div(max_kv < 1 ? 1 : max_kv, per);
+    if (splits > 256) { splits = 256; per = ceil_div(ceil_div(max_kv, splits), kChunk * kWarps) * (kChunk * kWarps); }
+    p.splits = (int)splits;
+    p.split_tokens = (int)per;
+    return p;
+}
+
+inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
+
+template <typename T, int D, int BITS>
+int launch_attention(const AttnArgs& g, const AttnPlan& p, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)p.tiles, (unsigned)g.kv_heads, (unsigned)p.splits);
+    cfg.blockDim = dim3(kWarps * 32, 1, 1);
+    cfg.stream = st;
+    if (cudaLaunchKernelEx(&cfg, attn_rows_kernel<T, D, BITS>, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
+    if (p.splits > 1) {
+        const int64_t blocks = ceil_div(g.tokens * g.heads, 4);
+        return launch_chained_as(true, attn_merge_kernel<T, D, kRows, kChunk>, (unsigned)blocks, 128u, 0, st, g);
+    }
+    return launch_status();
+}
+
+}  // namespace mpq
+
+using namespace mpq;
+
+extern "C" int64_t mpq_cache_attention_workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim,
+                                                 int64_t max_q, int64_t max_kv) {
+    if (tokens <= 0 || batch <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || dim <= 0 || max_q < 0 || max_kv < 0) return 0;
+    const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_kv);
+    if (p.splits <= 1) return 0;
+    return up16(tokens * heads * p.splits * dim * 4) + up16(tokens * heads * p.splits * 8);
+}
+
+extern "C" int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_t q_head_stride, int dtype,
+                                   const int32_t* q_starts, const int32_t* kv_lens, const int32_t* table, int64_t table_stride,
+                                   int64_t tokens, int batch, int heads, int kv_heads, int dim, int64_t max_q, int64_t max_kv,
+                                   const uint8_t* k_levels, const float* k_scale, const uint8_t* v_levels, const float* v_scale,
+                                   int bits, int64_t pages, int page_size,
+                                   int causal, int64_t window, float scale,
+                                   void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                                   void* workspace, int64_t workspace_bytes, void* stream) {
+    if (tokens != 0 && (!q || !q_starts || !kv_lens || !table || !k_levels || !k_scale || !v_levels || !v_scale || !out)) return MPQ_ERR_NULL;
+    if (tokens < 0 || batch <= 0 || heads <= 0 || heads > 65536 || tokens > 0x7fffffff / heads || kv_heads <= 0 || heads % kv_heads || kv_heads > 65535 ||
+        table_stride <= 0 || pages <= 0 || pages > 0x7fffffff || page_size <= 0 || max_q < 0 || max_kv < 0 || window < 0 ||
+        (heads > 1 && out_head_stride < dim) || (tokens > 1 && out_token_stride < dim)) return MPQ_ERR_BAD_SHAPE;
+    if ((dtype != MPQ_F16 && dtype != MPQ_BF16) || (bits != 8 && bits != 4) || (dim != 64 && dim != 128)) return MPQ_ERR_UNSUPPORTED;
+    if (!(scale == scale) || scale - scale != 0.0f) return MPQ_ERR_UNSUPPORTED;
+    if (!aligned16(k_levels) || !aligned16(v_levels) || !aligned_to(k_scale, 4) || !aligned_to(v_scale, 4) || !aligned_to(q, 2) ||
+        !aligned_to(out, 2) || !aligned_to(lse, 4) || !aligned_to(q_starts, 4) || !aligned_to(kv_lens, 4) || !aligned_to(table, 4)) return MPQ_ERR_ALIGN;
+    if (tokens == 0) return MPQ_OK;
+    const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_kv);
+    if (p.tiles > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
+    AttnArgs g = {q, q_token_stride, q_head_stride, q_starts, kv_lens, table, table_stride, tokens, batch, heads, kv_heads, heads / kv_heads,
+                  k_levels, k_scale, v_levels, v_scale, pages, page_size, causal != 0, window, scale * 1.4426950408889634f,
+                  out, out_token_stride, out_head_stride, lse, nullptr, nullptr, p.splits, p.split_tokens};
+    if (p.splits > 1) {
+        if (!workspace) return MPQ_ERR_NULL;
+        if (!aligned16(workspace)) return MPQ_ERR_ALIGN;
+        if (workspace_bytes < mpq_cache_attention_workspace(tokens, batch, heads, kv_heads, dim, max_q, max_kv)) return MPQ_ERR_WORKSPACE;
+        g.part_o = static_cast<float*>(workspace);
+        g.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + up16(tokens * heads * p.splits * dim * 4));
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    const bool bf = dtype == MPQ_BF16;
+    if (dim == 128) {
+        if (bits == 8) return bf ? launch_attention<__nv_bfloat16, 128, 8>(g, p, st) : launch_attention<__half, 128, 8>(g, p, st);
+        return bf ? launch_attention<__nv_bfloat16, 128, 4>(g, p, st) : launch_attention<__half, 128, 4>(g, p, st);
+    }
+    if (bits == 8) return bf ? launch_attention<__nv_bfloat16, 64, 8>(g, p, st) : launch_attention<__half, 64, 8>(g, p, st);
+    return bf ? launch_attention<__nv_bfloat16, 64, 4>(g, p, st) : launch_attention<__half, 64, 4>(g, p, st);
+}

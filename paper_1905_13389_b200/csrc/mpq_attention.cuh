@@ -1,0 +1,143 @@
+// Attention of new tokens over a paged cache of levels: what its kernels share.
+//
+// Mathematics.  A key or value of the cache is (2u - L) s / L with one range s per (token, head).  For a
+// query row (token, head) with scores x_j = scale log2(e) q . k_j,
+//   out = sum_j 2^x_j v_j / sum_j 2^x_j.
+// The ranges never touch the level bytes: levels are small integers, exact in fp16, so both products run
+// on the fp16 tensor pipes over the bare levels, and
+//   x_j = (q . levels_j) (s^k_j / L) scale log2(e)          one fp32 multiply per score,
+//   2^x_j v_j = 2^(x_j + log2 s^v_j) levels_j / L           the value's range moves into the exponent.
+// With y_j = x_j + log2 s^v_j and the running maximum m of y, the weights w_j = 2^(y_j - m + 15) lie in
+// [0, 2^15] whatever the ranges are: that is what makes fp16 weights safe (what is lost is a weight below
+// 2^-39 of the row's largest CONTRIBUTION, never a token whose score alone is small).  The denominator is
+// kept in fp32:
+//   l = sum_j w_j / s^v_j = 2^(15 - m) sum_j 2^x_j,
+// where a token drops out only if its contribution lies 2^141 below the row's largest one.
+// Queries are scaled by a power of two per row before they become fp16, so nothing overflows or is lost
+// beside the row's largest element.  Ranges below 2^-90 (all-zero values among them) count as 2^-90
+// in the exponent, and a result below 2^-89 in magnitude is stored as 0.
+#pragma once
+#include "mpq_levels.cuh"
+
+namespace mpq {
+
+struct AttnArgs {
+    const void* q; int64_t q_ts, q_hs;
+    const int32_t* q_starts; const int32_t* kv_lens; const int32_t* table; int64_t table_stride;
+    int64_t tokens; int batch, heads, kv_heads, group;
+    const uint8_t* k_levels; const float* k_scale; const uint8_t* v_levels; const float* v_scale;
+    int64_t pages; int page_size;
+    int causal; int64_t window;
+    float scale_log2;                       // scale * log2(e)
+    void* out; int64_t o_ts, o_hs; float* lse;
+    float* part_o; float2* part_ml;         // [tokens][heads][splits](dim), (m, l) of each split; used where a tile has more than one split
+    int splits, split_tokens;               // launch grid's splits; context tokens of one split
+};
+
+// One tile of query rows of one sequence: row r is token r / group, head kv_head * group + r % group.
+struct AttnTile {
+    int b, q0, n_q, rows, row0;             // sequence, its first token, tokens, n_q * group, first row of the tile
+    int kv_len;
+    int lo, hi;                             // context tokens that some row of the tile may see, lo a multiple of the chunk
+};
+
+// Visible range of row r: [first, last].
+__device__ __forceinline__ void row_range(const AttnArgs& g, const AttnTile& t, int token, int& first, int& last) {
+    const int pos = t.kv_len - t.n_q + token;
+    last = g.causal ? min(pos, t.kv_len - 1) : t.kv_len - 1;
+    first = g.window > 0 ? (int)max((int64_t)0, (int64_t)pos - g.window + 1) : 0;
+}
+
+// The sequence and rows of tile number `index` of R rows each, tiles counted over the sequences in order
+// (all 32 lanes call; the result is the same in every lane).  False: no such tile.
+template <int R>
+__device__ __forceinline__ bool find_tile(const AttnArgs& g, int index, AttnTile& t) {
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int base = 0; base < g.batch; base += 32) {
+        const int b = base + lane;
+        int q0 = 0, n = 0;
+        if (b < g.batch) {
+            q0 = (int)min((int64_t)max(g.q_starts[b], 0), g.tokens);
+            n = (int)min((int64_t)max(g.q_starts[b + 1], q0), g.tokens) - q0;
+        }
+        const int tiles = (int)(((int64_t)n * g.group + R - 1) / R);
+        int upto = tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, before + upto > index);
+        if (past) {
+            const int src = __ffs(past) - 1;
+            t.b = base + src;
+            t.q0 = __shfl_sync(0xffffffffu, q0, src);
+            t.n_q = __shfl_sync(0xffffffffu, n, src);
+            t.row0 = (index - before - __shfl_sync(0xffffffffu, upto - tiles, src)) * R;
+            t.rows = t.n_q * g.group;
+            return true;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return false;
+}
+
+// Context range of a tile of R rows, its start rounded down to a multiple of CHUNK.
+template <int R, int CHUNK>
+__device__ __forceinline__ void tile_range(const AttnArgs& g, AttnTile& t) {
+    t.kv_len = (int)max((int64_t)0, min((int64_t)g.kv_lens[t.b], min(g.table_stride * g.page_size, (int64_t)0x7fffff00)));
+    int first, last, unused;
+    row_range(g, t, t.row0 / g.group, first, unused);
+    row_range(g, t, (min(t.row0 + R, t.rows) - 1) / g.group, unused, last);
+    t.hi = max(last + 1, 0);
+    t.lo = min(first, t.hi) / CHUNK * CHUNK;
+}
+
+// Splits that a tile with context range [lo, hi) really uses, and the tokens of split s.
+__device__ __forceinline__ int tile_splits(const AttnArgs& g, const AttnTile& t) {
+    return max(1, min(g.splits, (t.hi - t.lo + g.split_tokens - 1) / g.split_tokens));
+}
+// The last split of the grid takes whatever is left, so any split count covers the whole context.
+__device__ __forceinline__ void split_range(const AttnArgs& g, const AttnTile& t, int s, int used, int& begin, int& end) {
+    begin = t.lo + s * g.split_tokens;
+    end = s == used - 1 ? t.hi : min(t.hi, begin + g.split_tokens);
+}
+
+// Row number in the cache (in tokens) of context token j, or 0xffffffff when its page number lies outside
+// the cache.  Cache rows are counted in 32 bits: 2^32 rows of 32 bytes are more than the device holds.
+__device__ __forceinline__ uint32_t context_row(const AttnArgs& g, const int32_t* pages_of, int j, int kv_head) {
+    const int p = j / g.page_size;
+    const int32_t page = __ldg(pages_of + p);
+    if (page < 0 || page >= g.pages) return 0xffffffffu;
+    return ((uint32_t)page * (uint32_t)g.kv_heads + (uint32_t)kv_head) * (uint32_t)g.page_size + (uint32_t)(j - p * g.page_size);
+}
+
+constexpr float kTinyRange = 8.077935669463161e-28f;        // 2^-90
+constexpr float kBoost = 15.0f;                             // weights are scaled by 2^15: up to half of fp16's largest number
+
+// 2^x to 2 units in the last place or so; 2^-infinity = 0.
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// log2 of a value's range and the reciprocal that belongs to it (2^-that, so that rounding the logarithm
+// cancels in the denominator).
+__device__ __forceinline__ void range_exponent(float s, float& lg, float& inv) {
+    lg = __log2f(s < kTinyRange ? kTinyRange : s);           // NaN passes through
+    inv = fast_exp2(-lg);
+}
+
+__device__ __forceinline__ float final_value(float o) { return fabsf(o) < 2.0f * kTinyRange ? 0.0f : o; }
+
+// Power of two that brings a row's largest magnitude into [1, 2), and its inverse.
+__device__ __forceinline__ void row_power(float amax, float& down, float& up) {
+    int e = amax > 0.0f ? (int)((__float_as_uint(amax) >> 23) & 0xff) - 127 : 0;
+    e = min(max(e, -100), 126);
+    down = __uint_as_float((uint32_t)(127 - e) << 23);
+    up = __uint_as_float((uint32_t)(127 + e) << 23);
+}
+
+}  // namespace mpq

@@ -1,0 +1,302 @@
+// Level bytes with one range per row: the root-mean-square norm with the residual's addition
+// (mpq_rmsnorm_levels) and the plain row encoder (mpq_encode_levels).
+#include "mpq_levels.cuh"
+
+namespace mpq {
+
+struct RowArgs {
+    const void* x; int64_t ldx;
+    const void* res; int64_t ldr;
+    const float* gain;
+    float eps;
+    int64_t rows, k, row_bytes;
+    LevelRule rule;
+    void* res_out; int64_t ldo;
+    uint8_t* levels; float* scale; int32_t* sums;
+    void* values; int64_t ldv;
+    int values_dtype;
+};
+
+// One row of partial results: sum of squares and the largest |h gain|.
+// y = (h gain) r with one r > 0 per row, and a rounded product by r is monotone, so
+// max |y| = r max |h gain| to the last bit: both statistics come out of ONE pass and one barrier.
+__device__ __forceinline__ void block_stats(float& ss, float& mx, float2* sh) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    }
+    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    if (warps == 1) return;
+    if (lane == 0) sh[threadIdx.x >> 5] = make_float2(ss, mx);
+    __syncthreads();
+    const float2 v = lane < warps ? sh[lane] : make_float2(0.0f, 0.0f);
+    ss = v.x; mx = v.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    }
+}
+__device__ __forceinline__ void block_level_sum(int u, int32_t* dst, int* sh) {
+    u = __reduce_add_sync(0xffffffffu, u);
+    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    if (warps > 1) {
+        if (lane == 0) sh[threadIdx.x >> 5] = u;
+        __syncthreads();
+        if (threadIdx.x >= 32) return;
+        u = __reduce_add_sync(0xffffffffu, lane < warps ? sh[lane] : 0);
+    }
+    if (lane == 0) *dst = u;
+}
+
+template <int ACT_HR>
+__device__ __forceinline__ int row_level(float y, float inv, const LevelRule& r) {
+    return level_index<ACT_HR>(y, inv, r.half_L, r.lo, r.hi, r.H);
+}
+
+// N adjacent elements at once where addresses and strides allow it (VECTOR), one by one otherwise, `count` of
+// them (the tail of a row).  Threads own the same N elements either way, so a row's sums do not depend on how
+// it lies in memory.
+template <typename T, int N, bool VECTOR>
+__device__ __forceinline__ void load_part(const T* p, float (&f)[N], int count) {
+    if constexpr (VECTOR) {
+        load_vec<T, N>(p, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = i < count ? to_f32(p[i]) : 0.0f;
+    }
+}
+template <typename T, int N, bool VECTOR>
+__device__ __forceinline__ void store_part(T* p, const float (&f)[N], int count) {
+    if constexpr (VECTOR) {
+        store_vec<T, N>(p, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) if (i < count) p[i] = from_f32<T>(f[i]);
+    }
+}
+// Level rows are 16-byte aligned and padded: whole words always fit (u past the row's end is 0).
+template <int N>
+__device__ __forceinline__ void store_levels(uint8_t* p, const int (&u)[N]) {
+#pragma unroll
+    for (int c = 0; c < N / 4; ++c)
+        reinterpret_cast<uint32_t*>(p)[c] = (uint32_t)u[4 * c] | ((uint32_t)u[4 * c + 1] << 8) |
+                                            ((uint32_t)u[4 * c + 2] << 16) | ((uint32_t)u[4 * c + 3] << 24);
+}
+template <int N, bool VECTOR>
+__device__ __forceinline__ void store_values(const RowArgs& g, int64_t row, int64_t at, const int (&u)[N], float alpha, int count) {
+    float f[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = (float)(2 * u[i] - g.rule.L) * alpha;
+    const int64_t o = row * g.ldv + at;
+    if (g.values_dtype == MPQ_BF16) store_part<__nv_bfloat16, N, VECTOR>(static_cast<__nv_bfloat16*>(g.values) + o, f, count);
+    else if (g.values_dtype == MPQ_F16) store_part<__half, N, VECTOR>(static_cast<__half*>(g.values) + o, f, count);
+    else store_part<float, N, VECTOR>(static_cast<float*>(g.values) + o, f, count);
+}
+
+// One CTA per row; the row stays in registers between the statistics and the quantizer (NV vectors of
+// VEC elements per thread), so memory is read once and written once.
+template <typename T, int VEC, int NV, bool VECTOR, bool NORM, int ACT>
+__global__ void __launch_bounds__(1024)
+level_rows_kernel(const RowArgs g) {
+    __shared__ float2 sh_stats[32];
+    __shared__ int sh_sum[32];
+    chain_entry();
+    const int64_t row = blockIdx.x;
+    const T* x = static_cast<const T*>(g.x) + row * g.ldx;
+    const T* res = NORM && g.res ? static_cast<const T*>(g.res) + row * g.ldr : nullptr;
+    const int k = (int)g.k, nvec = (k + VEC - 1) / VEC;
+    float h[NV][VEC];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = threadIdx.x + j * blockDim.x;
+        if (i < nvec) load_part<T, VEC, VECTOR>(x + (int64_t)i * VEC, h[j], k - i * VEC);
+    }
+    if (NORM && res) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = threadIdx.x + j * blockDim.x;
+            if (i < nvec) {
+                float f[VEC];
+                load_part<T, VEC, VECTOR>(res + (int64_t)i * VEC, f, k - i * VEC);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) h[j][e] += f[e];
+            }
+        }
+    }
+    float ss = 0.0f, mx = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = threadIdx.x + j * blockDim.x;
+        if (i < nvec) {
+            if (NORM) {
+                if (g.res_out) store_part<T, VEC, VECTOR>(static_cast<T*>(g.res_out) + row * g.ldo + (int64_t)i * VEC, h[j], k - i * VEC);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) ss = fmaf(h[j][e], h[j][e], ss);
+                if (g.gain) {
+                    // read-only loads: the compiler may move them above the stores of residual_out
+                    if constexpr (VECTOR) {
+#pragma unroll
+                        for (int c = 0; c < VEC / 4; ++c) {
+                            const float4 gn = __ldg(reinterpret_cast<const float4*>(g.gain + (int64_t)i * VEC) + c);
+                            h[j][4 * c] *= gn.x; h[j][4 * c + 1] *= gn.y; h[j][4 * c + 2] *= gn.z; h[j][4 * c + 3] *= gn.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) if (i * VEC + e < k) h[j][e] *= __ldg(g.gain + i * VEC + e);
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, ACT == MPQ_ACT_HRELU ? h[j][e] : fabsf(h[j][e]));
+        }
+    }
+    block_stats(ss, mx, sh_stats);
+    const float r = NORM ? __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)g.k), g.eps))) : 1.0f;
+    const float s = NORM ? mx * r : mx;
+    const float inv = inverse_scale(s);
+    const float alpha = __fdiv_rn(s, (float)g.rule.L);
+    uint8_t* out = g.levels + row * g.row_bytes;
+    int total = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int i = threadIdx.x + j * blockDim.x;
+        if (i < nvec) {
+            int u[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                u[e] = row_level<ACT>(NORM ? h[j][e] * r : h[j][e], inv, g.rule);
+                if (!VECTOR && i * VEC + e >= k) u[e] = 0;
+                total += u[e];
+            }
+            store_levels<VEC>(out + (int64_t)i * VEC, u);
+            if (g.values) store_values<VEC, VECTOR>(g, row, (int64_t)i * VEC, u, alpha, k - i * VEC);
+        }
+    }
+    // padding words behind the last vector
+    for (int i = nvec * VEC + threadIdx.x * 4; i < (int)g.row_bytes; i += blockDim.x * 4) *reinterpret_cast<uint32_t*>(out + i) = 0u;
+    block_level_sum(total, g.sums + row, sh_sum);
+    if (threadIdx.x == 0) g.scale[row] = s;
+}
+
+// Rows that do not fit the registers of one CTA: the row is read twice (statistics, quantizer), the
+// residual sum formed both times.  residual_out is written in the second pass, element by element after
+// the thread's own reads of the same element, so it may be x or the residual.
+template <typename T, bool NORM, int ACT>
+__global__ void __launch_bounds__(1024)
+level_wide_rows_kernel(const RowArgs g) {
+    __shared__ float2 sh_stats[32];
+    __shared__ int sh_sum[32];
+    chain_entry();
+    const int64_t row = blockIdx.x;
+    const T* x = static_cast<const T*>(g.x) + row * g.ldx;
+    const T* res = NORM && g.res ? static_cast<const T*>(g.res) + row * g.ldr : nullptr;
+    float ss = 0.0f, mx = 0.0f;
+    for (int64_t i = threadIdx.x; i < g.k; i += blockDim.x) {
+        float h = to_f32(x[i]);
+        if (NORM) {
+            if (res) h += to_f32(res[i]);
+            ss = fmaf(h, h, ss);
+            if (g.gain) h *= g.gain[i];
+        }
+        mx = fmaxf(mx, ACT == MPQ_ACT_HRELU ? h : fabsf(h));
+    }
+    block_stats(ss, mx, sh_stats);
+    const float r = NORM ? __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)g.k), g.eps))) : 1.0f;
+    const float s = NORM ? mx * r : mx;
+    const float inv = inverse_scale(s);
+    const float alpha = __fdiv_rn(s, (float)g.rule.L);
+    uint8_t* out = g.levels + row * g.row_bytes;
+    int total = 0;
+    for (int64_t i = threadIdx.x; i < g.row_bytes; i += blockDim.x) {
+        if (i >= g.k) { out[i] = 0; continue; }
+        float h = to_f32(x[i]);
+        if (NORM) {
+            if (res) h += to_f32(res[i]);
+            if (g.res_out) static_cast<T*>(g.res_out)[row * g.ldo + i] = from_f32<T>(h);
+            if (g.gain) h *= g.gain[i];
+            h *= r;
+        }
+        const int u[1] = {row_level<ACT>(h, inv, g.rule)};
+        total += u[0];
+        out[i] = (uint8_t)u[0];
+        if (g.values) store_values<1, false>(g, row, i, u, alpha, 1);
+    }
+    block_level_sum(total, g.sums + row, sh_sum);
+    if (threadIdx.x == 0) g.scale[row] = s;
+}
+
+// Threads and vectors per thread: two vectors per thread while the row is short (many loads in flight,
+// few warps to reduce over), more once 1024 threads are not enough.
+template <typename T, int VEC, bool VECTOR, bool NORM, int ACT>
+int launch_level_rows(const RowArgs& g, cudaStream_t st) {
+    const int64_t nvec = ceil_div(g.k, VEC);
+    auto threads_for = [&](int nv) { return (unsigned)(ceil_div(ceil_div(nvec, nv), 32) * 32); };
+    if (threads_for(1) <= 128) return launch_chained(level_rows_kernel<T, VEC, 1, VECTOR, NORM, ACT>, (unsigned)g.rows, threads_for(1), 0, st, g);
+    if (threads_for(2) <= 1024) return launch_chained(level_rows_kernel<T, VEC, 2, VECTOR, NORM, ACT>, (unsigned)g.rows, threads_for(2), 0, st, g);
+    if (threads_for(4) <= 1024) return launch_chained(level_rows_kernel<T, VEC, 4, VECTOR, NORM, ACT>, (unsigned)g.rows, threads_for(4), 0, st, g);
+    return launch_chained(level_wide_rows_kernel<T, NORM, ACT>, (unsigned)g.rows, 1024u, 0, st, g);
+}
+
+template <typename T, bool NORM, int ACT>
+int launch_level_rows_of(const RowArgs& g, cudaStream_t st) {
+    constexpr int VEC = 16 / (int)sizeof(T);
+    auto fits = [&](const void* p, int64_t ld, int size) { return !p || (aligned_to(p, VEC * size > 16 ? 16 : VEC * size) && (ld % VEC == 0 || g.rows == 1)); };
+    const bool vec = g.k % VEC == 0 && fits(g.x, g.ldx, sizeof(T)) && fits(g.res, g.ldr, sizeof(T)) && fits(g.res_out, g.ldo, sizeof(T)) &&
+                     fits(g.gain, 0, 4) && (!g.values || fits(g.values, g.ldv, dtype_size(g.values_dtype)));
+    return vec ? launch_level_rows<T, VEC, true, NORM, ACT>(g, st) : launch_level_rows<T, VEC, false, NORM, ACT>(g, st);
+}
+template <bool NORM, int ACT>
+int launch_level_rows_dtype(int dtype, const RowArgs& g, cudaStream_t st) {
+    if (dtype == MPQ_F32) return launch_level_rows_of<float, NORM, ACT>(g, st);
+    if (dtype == MPQ_F16) return launch_level_rows_of<__half, NORM, ACT>(g, st);
+    return launch_level_rows_of<__nv_bfloat16, NORM, ACT>(g, st);
+}
+
+int check_level_rows(const RowArgs& g, int dtype, int bits) {
+    if (!dtype_ok(dtype) || (g.values && !dtype_ok(g.values_dtype)) || !bits_ok(bits)) return MPQ_ERR_UNSUPPORTED;
+    if (g.rows < 0 || g.rows > 0x7fffffff || g.k <= 0 || g.k >= (1 << 23)) return MPQ_ERR_BAD_SHAPE;
+    if (g.rows > 1 && (g.ldx < g.k || (g.res && g.ldr < g.k) || (g.res_out && g.ldo < g.k) || (g.values && g.ldv < g.k)))
+        return MPQ_ERR_BAD_SHAPE;
+    const int e = dtype_size(dtype);
+    if (!aligned16(g.levels) || !aligned_to(g.x, e) || !aligned_to(g.res, e) || !aligned_to(g.res_out, e) || !aligned_to(g.gain, 4) ||
+        !aligned_to(g.scale, 4) || !aligned_to(g.sums, 4) || (g.values && !aligned_to(g.values, dtype_size(g.values_dtype))))
+        return MPQ_ERR_ALIGN;
+    return MPQ_OK;
+}
+
+}  // namespace mpq
+
+using namespace mpq;
+
+extern "C" int64_t mpq_level_row_bytes(int64_t k) { return k > 0 ? level_row_bytes(k) : 0; }
+
+extern "C" int mpq_rmsnorm_levels(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype,
+                                  const float* gain, float eps, int64_t rows, int64_t k, int bits,
+                                  void* residual_out, int64_t ldo,
+                                  uint8_t* levels, float* scale, int32_t* sums,
+                                  void* values, int values_dtype, int64_t ldv, void* stream) {
+    if (rows != 0 && (!x || !levels || !scale || !sums)) return MPQ_ERR_NULL;
+    RowArgs g = {x, ldx, residual, ldr, gain, eps, rows, k, level_row_bytes(k), {}, residual_out, ldo, levels, scale, sums,
+                 values, ldv, values_dtype};
+    const int rc = check_level_rows(g, dtype, bits);
+    if (rc != MPQ_OK || rows == 0) return rc;
+    if (!(eps >= 0.0f)) return MPQ_ERR_UNSUPPORTED;
+    g.rule = level_rule(bits);
+    return launch_level_rows_dtype<true, MPQ_ACT_HTANH>(dtype, g, (cudaStream_t)stream);
+}
+
+extern "C" int mpq_encode_levels(const void* x, int64_t ldx, int dtype, int64_t rows, int64_t k, int act, int bits,
+                                 uint8_t* levels, float* scale, int32_t* sums,
+                                 void* values, int values_dtype, int64_t ldv, void* stream) {
+    if (rows != 0 && (!x || !levels || !scale || !sums)) return MPQ_ERR_NULL;
+    if (act != MPQ_ACT_HTANH && act != MPQ_ACT_HRELU) return MPQ_ERR_UNSUPPORTED;
+    RowArgs g = {x, ldx, nullptr, 0, nullptr, 0.0f, rows, k, level_row_bytes(k), {}, nullptr, 0, levels, scale, sums,
+                 values, ldv, values_dtype};
+    const int rc = check_level_rows(g, dtype, bits);
+    if (rc != MPQ_OK || rows == 0) return rc;
+    g.rule = level_rule(bits);
+    return act == MPQ_ACT_HTANH ? launch_level_rows_dtype<false, MPQ_ACT_HTANH>(dtype, g, (cudaStream_t)stream)
+                                : launch_level_rows_dtype<false, MPQ_ACT_HRELU>(dtype, g, (cudaStream_t)stream);
+}

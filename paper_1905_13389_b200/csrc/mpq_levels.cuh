@@ -1,0 +1,87 @@
+// Element types and level decoding shared by the operators of an encoded decoder block.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "mpq_common.cuh"
+
+namespace mpq {
+
+inline bool dtype_ok(int d) { return d == MPQ_F32 || d == MPQ_F16 || d == MPQ_BF16; }
+inline int dtype_size(int d) { return d == MPQ_F32 ? 4 : 2; }
+inline bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+__host__ __device__ inline int64_t level_row_bytes(int64_t k) { return ceil_div(k, 16) * 16; }
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// N elements that start at an N * sizeof(T)-byte (at most 16-byte) aligned address.
+template <typename T, int N>
+__device__ __forceinline__ void load_vec(const T* p, float (&f)[N]) {
+    constexpr int kBytes = N * (int)sizeof(T);
+    if constexpr (N == 1) {
+        f[0] = to_f32(*p);
+    } else if constexpr (kBytes == 8) {
+        const uint2 r = *reinterpret_cast<const uint2*>(p);
+        const T* e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = to_f32(e[i]);
+    } else {
+        static_assert(kBytes % 16 == 0, "vectors of 16 bytes");
+        constexpr int kPer = 16 / (int)sizeof(T);
+#pragma unroll
+        for (int c = 0; c < kBytes / 16; ++c) {
+            const uint4 r = reinterpret_cast<const uint4*>(p)[c];
+            const T* e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) f[c * kPer + i] = to_f32(e[i]);
+        }
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_vec(T* p, const float (&f)[N]) {
+    constexpr int kBytes = N * (int)sizeof(T);
+    if constexpr (N == 1) {
+        *p = from_f32<T>(f[0]);
+    } else if constexpr (kBytes == 8) {
+        uint2 r;
+        T* e = reinterpret_cast<T*>(&r);
+#pragma unroll
+        for (int i = 0; i < N; ++i) e[i] = from_f32<T>(f[i]);
+        *reinterpret_cast<uint2*>(p) = r;
+    } else {
+        static_assert(kBytes % 16 == 0, "vectors of 16 bytes");
+        constexpr int kPer = 16 / (int)sizeof(T);
+#pragma unroll
+        for (int c = 0; c < kBytes / 16; ++c) {
+            uint4 r;
+            T* e = reinterpret_cast<T*>(&r);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) e[i] = from_f32<T>(f[c * kPer + i]);
+            reinterpret_cast<uint4*>(p)[c] = r;
+        }
+    }
+}
+
+// Quantizer constants of a width (see mpq_encode).
+struct LevelRule {
+    float half_L, lo, hi;
+    int H, L;
+};
+__host__ __device__ inline LevelRule level_rule(int bits) {
+    LevelRule r;
+    r.H = 1 << (bits - 1);
+    r.L = (1 << bits) - 1;
+    r.half_L = 0.5f * (float)r.L;
+    r.lo = -(float)r.H;
+    r.hi = (float)r.H - 0.5f;
+    return r;
+}
+
+}  // namespace mpq
