@@ -415,10 +415,10 @@ extern "C" int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_
                                    void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
                                    void* workspace, int64_t workspace_bytes, void* stream) {
     if (tokens != 0 && (!q || !q_starts || !kv_lens || !table || !k_levels || !k_scale || !v_levels || !v_scale || !out)) return MPQ_ERR_NULL;
+    if ((dtype != MPQ_F16 && dtype != MPQ_BF16) || (bits != 8 && bits != 4) || (dim != 64 && dim != 128)) return MPQ_ERR_UNSUPPORTED;
     if (tokens < 0 || batch <= 0 || heads <= 0 || heads > 65536 || tokens > 0x7fffffff / heads || kv_heads <= 0 || heads % kv_heads || kv_heads > 65535 ||
         table_stride <= 0 || pages <= 0 || pages > 0x7fffffff || page_size <= 0 || max_q < 0 || max_kv < 0 || window < 0 ||
         (heads > 1 && out_head_stride < dim) || (tokens > 1 && out_token_stride < dim)) return MPQ_ERR_BAD_SHAPE;
-    if ((dtype != MPQ_F16 && dtype != MPQ_BF16) || (bits != 8 && bits != 4) || (dim != 64 && dim != 128)) return MPQ_ERR_UNSUPPORTED;
     if (!(scale == scale) || scale - scale != 0.0f) return MPQ_ERR_UNSUPPORTED;
     if (!aligned16(k_levels) || !aligned16(v_levels) || !aligned_to(k_scale, 4) || !aligned_to(v_scale, 4) || !aligned_to(q, 2) ||
         !aligned_to(out, 2) || !aligned_to(lse, 4) || !aligned_to(q_starts, 4) || !aligned_to(kv_lens, 4) || !aligned_to(table, 4)) return MPQ_ERR_ALIGN;
