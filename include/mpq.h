@@ -402,6 +402,11 @@ int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
                         void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
                         void* workspace, int64_t workspace_bytes, void* stream);
 
+/* How many CTAs of the tensor-core kernels have given up a wait since the library was loaded on the
+ * current device (0 unless the device or the driver misbehaves; the results of such a call are not
+ * valid).  Synchronizes the stream. */
+int mpq_wait_failures(unsigned int* count_host, void* stream);
+
 /* ---- Roofline denominator: measures this GPU's 32-bit population-count issue rate with a
  * register-only loop (no memory traffic) and the SM clock it ran at.  Synchronous.
  * popc_per_s: lane-level POPC results per second over the whole chip; sm_mhz: SM clock

@@ -98,7 +98,8 @@ def lib() -> ctypes.CDLL:
         L.mpq_cache_attention_workspace.restype = i64
         L.mpq_cache_attention.argtypes = [P, i64, i64, i32, P, P, P, i64, i64, i32, i32, i32, i32, i64, i64, P, P, P, P,
                                           i32, i64, i32, i32, i64, f32, P, i64, i64, P, P, i64, P]
-        for name in ("mpq_rmsnorm_levels", "mpq_encode_levels", "mpq_linear_levels", "mpq_cache_write", "mpq_cache_read",
+        L.mpq_wait_failures.argtypes = [ctypes.POINTER(ctypes.c_uint), P]
+        for name in ("mpq_wait_failures", "mpq_rmsnorm_levels", "mpq_encode_levels", "mpq_linear_levels", "mpq_cache_write", "mpq_cache_read",
                      "mpq_cache_attention"):
             getattr(L, name).restype = i32
         for name in ("mpq_absmax", "mpq_encode", "mpq_encode_nchw", "mpq_encode_oihw", "mpq_gemm", "mpq_conv",
@@ -631,6 +632,13 @@ def cache_attention(q: torch.Tensor, cache: LevelCache, q_starts: torch.Tensor, 
                                      None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
                                      _stream()), "mpq_cache_attention")
     return out
+
+
+def wait_failures() -> int:
+    """CTAs of the tensor-core kernels that gave up a wait since the library was loaded (0 in a healthy process)."""
+    n = ctypes.c_uint()
+    _check(lib().mpq_wait_failures(ctypes.byref(n), _stream()), "mpq_wait_failures")
+    return n.value
 
 
 def measure_popc_peak():

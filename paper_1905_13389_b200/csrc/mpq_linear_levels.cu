@@ -5,6 +5,7 @@
 // so the inner loop multiplies unsigned bytes and the level sums that lie beside the operands do the rest.
 // The result fits int32 (checked on the host), hence the terms may be combined modulo 2^32.
 #include "mpq_levels.cuh"
+#include "mpq_tensor.cuh"
 
 namespace mpq {
 
@@ -34,60 +35,423 @@ __device__ __forceinline__ float glue_value(float f, int glue) {
     }
 }
 
-constexpr int kTile = 64, kStep = 64;      // 64 x 64 outputs, 64 bytes of k at a time
-
-template <typename T>
-__global__ void __launch_bounds__(256) linear_levels_kernel(const LinearArgs g) {
-    __shared__ uint32_t sa[kTile][kStep / 4 + 1], sw[kTile][kStep / 4 + 1];
-    chain_entry();
-    const int64_t m0 = (int64_t)blockIdx.y * kTile, n0 = (int64_t)blockIdx.x * kTile;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    uint32_t acc[4][4] = {};
-    for (int64_t k0 = 0; k0 < g.row_bytes; k0 += kStep) {
-        for (int i = threadIdx.x; i < kTile * (kStep / 16); i += 256) {
-            const int r = i / (kStep / 16), c = i % (kStep / 16);
-            const int64_t at = k0 + c * 16;
-            uint4 va = make_uint4(0, 0, 0, 0), vw = va;
-            if (at < g.row_bytes) {
-                if (m0 + r < g.m) va = *reinterpret_cast<const uint4*>(g.a + (m0 + r) * g.row_bytes + at);
-                if (n0 + r < g.n) vw = *reinterpret_cast<const uint4*>(g.w + (n0 + r) * g.row_bytes + at);
-            }
-            sa[r][4 * c] = va.x; sa[r][4 * c + 1] = va.y; sa[r][4 * c + 2] = va.z; sa[r][4 * c + 3] = va.w;
-            sw[r][4 * c] = vw.x; sw[r][4 * c + 1] = vw.y; sw[r][4 * c + 2] = vw.z; sw[r][4 * c + 3] = vw.w;
-        }
-        __syncthreads();
-#pragma unroll 4
-        for (int t = 0; t < kStep / 4; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a(sa[ty * 4 + i][t], sw[tx + 16 * j][t], acc[i][j]);
-        __syncthreads();
-    }
-    for (int i = 0; i < 4; ++i) {
-        const int64_t r = m0 + ty * 4 + i;
-        if (r >= g.m) break;
-        const float ra = __fdiv_rn(g.a_scale[r], (float)g.La);
-        const uint32_t row_term = (uint32_t)g.k * (uint32_t)g.La * (uint32_t)g.Lw - 2u * (uint32_t)g.Lw * (uint32_t)g.a_sums[r];
-        for (int j = 0; j < 4; ++j) {
-            const int64_t c = n0 + tx + 16 * j;
-            if (c >= g.n) continue;
-            const int32_t q = (int32_t)(4u * acc[i][j] + row_term - 2u * (uint32_t)g.La * (uint32_t)g.w_sums[c]);
-            float f = (float)q * (ra * __fdiv_rn(g.w_scale[c], (float)g.Lw));
-            if (g.bias) f += g.bias[c];
-            f = glue_value(f, g.glue);
-            if (g.res) f += to_f32(static_cast<const T*>(g.res)[r * g.ldr + c]);
-            static_cast<T*>(g.out)[r * g.ldo + c] = from_f32<T>(f);
-        }
-    }
+// acc (levels u, unsigned) -> one output, in the header's order of operations
+struct RowTerm { float scale; uint32_t term; };          // a_scale / L_a;  k L_a L_w - 2 L_w sums_a
+struct ColTerm { float scale; uint32_t term; float bias; };   // w_scale / L_w;  2 L_a sums_w;  bias
+__device__ __forceinline__ RowTerm row_term(const LinearArgs& g, int64_t r) {
+    RowTerm t;
+    t.scale = __fdiv_rn(__ldg(g.a_scale + r), (float)g.La);
+    t.term = (uint32_t)g.k * (uint32_t)g.La * (uint32_t)g.Lw - 2u * (uint32_t)g.Lw * (uint32_t)__ldg(g.a_sums + r);
+    return t;
+}
+__device__ __forceinline__ ColTerm col_term(const LinearArgs& g, int64_t c) {
+    ColTerm t;
+    t.scale = __fdiv_rn(__ldg(g.w_scale + c), (float)g.Lw);
+    t.term = 2u * (uint32_t)g.La * (uint32_t)__ldg(g.w_sums + c);
+    t.bias = g.bias ? __ldg(g.bias + c) : 0.0f;
+    return t;
+}
+__device__ __forceinline__ float linear_value(const LinearArgs& g, uint32_t acc, const RowTerm& r, const ColTerm& c) {
+    const float f = (float)(int32_t)(4u * acc + r.term - c.term) * (r.scale * c.scale);
+    return glue_value(g.bias ? f + c.bias : f, g.glue);
 }
 
+constexpr int kBlock = 128;                               // bytes of k per stage: one swizzled row
+constexpr int kThreads = 192;                             // warp 0 loads, warp 1 issues the products, warps 2-5 store
+
+__device__ unsigned int g_wait_failures;                  // waits that ran out, over the life of the process
+
+// ---- few rows: C^T = W A^T.  The 128 rows of a tile are weight rows (output columns), its BN columns are
+// activation rows, so a handful of tokens wastes nothing of the 128 TMEM lanes and the weights are read once.
+// These products are bound by reading the weights; with one CTA per multiprocessor and a ring of 130-180 KB
+// the loads of a whole multiprocessor stay in flight.  Too few tiles for all multiprocessors: the k range of a
+// tile is split over a cluster of S CTAs, which exchange their integer partial sums through distributed
+// shared memory (exact, so any order gives the same result) -- CTA i finishes rows i BN/S .. of the tile.
+template <int BN> struct SmallShape {
+    static constexpr int stages = BN == 16 ? 10 : BN == 32 ? 8 : BN == 64 ? 6 : 4;
+    static constexpr int stage_bytes = (128 + BN) * kBlock;
+    static constexpr int exchange_bytes = BN * 128 * 4;   // [S source CTAs][BN / S rows][128 columns] int32
+    static constexpr int smem = stages * stage_bytes + exchange_bytes + 1024;
+};
+
+template <typename T, int BN>
+__global__ void __launch_bounds__(kThreads, 1)
+linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const LinearArgs g,
+                    int tiles_w, int splits) {
+    using Shape = SmallShape<BN>;
+    constexpr int kStages = Shape::stages;
+    constexpr uint32_t kCols = BN < 32 ? 32 : BN;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 1];
+    __shared__ uint32_t tmem_holder;
+    __shared__ int failed;
+    __shared__ float row_scale[BN];
+    __shared__ uint32_t row_terms[BN];
+    const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    const uint32_t exchange = ring + kStages * Shape::stage_bytes;
+    uint32_t* exchange_ptr = reinterpret_cast<uint32_t*>(smem_raw + (exchange - smem_addr(smem_raw)));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto full = [&](int s) { return smem_addr(&bars[s]); };
+    auto empty = [&](int s) { return smem_addr(&bars[kStages + s]); };
+    const uint32_t done = smem_addr(&bars[2 * kStages]);
+    auto has_failed = [&]() { return *(volatile int*)&failed != 0; };
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2 * kStages + 1; ++i) mbar_init(smem_addr(&bars[i]), 1);
+        failed = 0;
+        mbar_init_fence();
+        tma_prefetch(&map_w);
+        tma_prefetch(&map_a);
+    }
+    if (warp == 0) tmem_alloc<1>(&tmem_holder, kCols);
+    tmem_fence_before();
+    if (splits > 1) cluster_sync_all();                   // the other CTAs' shared memory is there
+    else __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = tmem_holder;
+    chain_entry();
+
+    const int split = splits > 1 ? (int)cluster_rank() : 0;
+    const int tile = (int)blockIdx.x / splits;
+    const int n0 = tile % tiles_w * 128, m0 = tile / tiles_w * BN;
+    const int blocks = (int)((g.row_bytes + kBlock - 1) / kBlock);
+    const int kb0 = (int)((int64_t)blocks * split / splits), kb1 = (int)((int64_t)blocks * (split + 1) / splits);
+
+    if (warp == 0 && lane == 0) {
+        int i = 0;
+        for (int kb = kb0; kb < kb1; ++kb, ++i) {
+            const int s = i % kStages;
+            if (i >= kStages && !mbar_wait(empty(s), (i / kStages - 1) & 1)) { atomicExch(&failed, 1); break; }
+            if (has_failed()) break;
+            const uint32_t dst = ring + s * Shape::stage_bytes;
+            mbar_expect_tx(full(s), Shape::stage_bytes);
+            tma_load_2d(dst, &map_w, kb * kBlock, n0, full(s));
+            tma_load_2d(dst + 128 * kBlock, &map_a, kb * kBlock, m0, full(s));
+        }
+        if (has_failed())
+            for (int q = i > kStages ? i - kStages : 0; q < i; ++q) mbar_wait(full(q % kStages), (q / kStages) & 1);
+    } else if (warp == 1 && lane == 0) {
+        constexpr uint32_t idesc = umma_idesc_u8(128, BN);
+        int i = 0;
+        for (int kb = kb0; kb < kb1; ++kb, ++i) {
+            const int s = i % kStages;
+            if (!mbar_wait(full(s), (i / kStages) & 1)) { atomicExch(&failed, 1); break; }
+            if (has_failed()) break;
+            tmem_fence_after();
+            const uint32_t at = ring + s * Shape::stage_bytes;
+            const uint64_t da = umma_desc(at), db = umma_desc(at + 128 * kBlock);
+#pragma unroll
+            for (int j = 0; j < kBlock / 32; ++j) umma_u8<1>(tmem, da + 2 * j, db + 2 * j, idesc, i > 0 || j > 0);
+            umma_commit<1>(empty(s));
+        }
+        umma_commit<1>(done);
+    } else if (warp >= 2) {
+        // constants of the tile's rows while the products run
+        const int t = threadIdx.x - 64;
+        for (int r = t; r < BN; r += 128) {
+            RowTerm rt = {0.0f, 0u};
+            if (m0 + r < g.m) rt = row_term(g, m0 + r);
+            row_scale[r] = rt.scale;
+            row_terms[r] = rt.term;
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const int quarter = warp & 3;
+        const int col = quarter * 32 + lane;              // TMEM lane = weight row = output column
+        const int64_t c = (int64_t)n0 + col;
+        ColTerm ct = {0.0f, 0u, 0.0f};
+        if (c < g.n) ct = col_term(g, c);
+        bool ok = mbar_wait(done, 0);
+        if (!ok) atomicExch(&failed, 1);
+        ok = __all_sync(0xffffffffu, ok && !has_failed());
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+        const int own = BN / splits;
+        if (ok) {
+            tmem_fence_after();
+#pragma unroll 1
+            for (int r0 = 0; r0 < BN; r0 += 16) {
+                uint32_t v[16];
+                tmem_load16(lanes + r0, v);
+                tmem_wait_ld();
+                if (splits == 1) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int64_t r = m0 + r0 + j;
+                        if (r >= g.m || c >= g.n) continue;
+                        float f = linear_value(g, v[j], RowTerm{row_scale[r0 + j], row_terms[r0 + j]}, ct);
+                        if (g.res) f += to_f32(static_cast<const T*>(g.res)[r * g.ldr + c]);
+                        static_cast<T*>(g.out)[r * g.ldo + c] = from_f32<T>(f);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int r = r0 + j, owner = r / own;
+                        st_cluster(map_to_cta(exchange + (uint32_t)(((split * own + r % own) * 128 + col) * 4), (uint32_t)owner), v[j]);
+                    }
+                }
+            }
+        }
+        tmem_fence_before();
+    }
+    __syncwarp();
+    if (splits > 1) {
+        cluster_sync_all();                                // every CTA's partial sums have arrived
+        if (warp >= 2 && !has_failed()) {
+            const int col = (warp & 3) * 32 + lane, own = BN / splits;
+            const int64_t c = (int64_t)n0 + col;
+            if (c < g.n) {
+                const ColTerm ct = col_term(g, c);
+                for (int j = 0; j < own; ++j) {
+                    const int rr = split * own + j;
+                    const int64_t r = m0 + rr;
+                    if (r >= g.m) break;
+                    uint32_t acc = 0;
+                    for (int s = 0; s < splits; ++s) acc += exchange_ptr[(s * own + j) * 128 + col];
+                    float f = linear_value(g, acc, RowTerm{row_scale[rr], row_terms[rr]}, ct);
+                    if (g.res) f += to_f32(static_cast<const T*>(g.res)[r * g.ldr + c]);
+                    static_cast<T*>(g.out)[r * g.ldo + c] = from_f32<T>(f);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    tmem_fence_after();
+    if (warp == 0) tmem_free<1>(tmem, kCols);
+    if (threadIdx.x == 0 && failed) atomicAdd(&g_wait_failures, 1u);
+}
+
+// ---- many rows: 256 x BN tiles on CTA pairs.  One CTA alone cannot feed kind::i8: a 128 x 256 x 32 product
+// takes 128 cycles and reads 12 KB of operands while 12 KB of new ones arrive, 1.5 times the 128 bytes a cycle
+// of shared memory.  The pair (cta_group::2) shares the BN operand rows, each CTA holds half of them: 8 + 8 KB
+// per 128 cycles for BN = 256.  Persistent: pair p takes tiles p, p + pairs, ...; two accumulators in TMEM,
+// so a tile is stored while the next one is multiplied.  The store goes through a padded shared-memory
+// transpose, after which a lane owns two adjacent columns (their constants in registers) and a warp writes
+// whole row pieces whatever the row stride is.
+template <int BN> struct PairShape {
+    static constexpr int stage_bytes = (128 + BN / 2) * kBlock;     // per CTA
+    static constexpr int stages = BN == 256 ? 6 : 7;
+    static constexpr int row_words = 66;                            // 64 columns + 2: conflict-free 8-byte accesses both ways
+    static constexpr int transpose_bytes = 4 * 32 * row_words * 4;
+    static constexpr int smem = stages * stage_bytes + transpose_bytes + 1024;
+};
+
+template <typename T, int BN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const LinearArgs g,
+                   int tiles_m, int tiles) {
+    using Shape = PairShape<BN>;
+    constexpr int kStages = Shape::stages, kAccs = 2;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kAccs];
+    __shared__ uint32_t tmem_holder;
+    __shared__ int failed;
+    const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    uint32_t* transpose = reinterpret_cast<uint32_t*>(smem_raw + (ring - smem_addr(smem_raw)) + kStages * Shape::stage_bytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    auto full = [&](int s) { return smem_addr(&bars[s]); };                        // used in the leader (rank 0)
+    auto empty = [&](int s) { return smem_addr(&bars[kStages + s]); };             // one in each CTA
+    auto acc_full = [&](int a) { return smem_addr(&bars[2 * kStages + a]); };      // one in each CTA
+    auto acc_empty = [&](int a) { return smem_addr(&bars[2 * kStages + kAccs + a]); };   // leader: 8 storing warps
+    auto has_failed = [&]() { return *(volatile int*)&failed != 0; };
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2 * kStages + kAccs; ++i) mbar_init(smem_addr(&bars[i]), 1);
+        for (int a = 0; a < kAccs; ++a) mbar_init(acc_empty(a), 8);
+        failed = 0;
+        mbar_init_fence();
+        tma_prefetch(&map_a);
+        tma_prefetch(&map_w);
+    }
+    if (warp == 0) tmem_alloc<2>(&tmem_holder, kAccs * BN);
+    tmem_fence_before();
+    cluster_sync_all();                                    // both CTAs' barriers exist
+    tmem_fence_after();
+    const uint32_t tmem = tmem_holder;
+    chain_entry();
+
+    const int pair = (int)blockIdx.x / 2, pairs = (int)gridDim.x / 2;
+    const int my_tiles = tiles > pair ? (tiles - pair + pairs - 1) / pairs : 0;
+    const int blocks = (int)((g.row_bytes + kBlock - 1) / kBlock);
+    // consecutive tiles share their weight rows: what a round of pairs reads of them stays in L2
+    auto origin = [&](int i, int& m0, int& n0) {
+        const int t = pair + i * pairs;
+        m0 = t % tiles_m * 256;
+        n0 = t / tiles_m * BN;
+    };
+
+    if (warp == 0 && lane == 0) {
+        int issued = 0;
+        for (int i = 0; i < my_tiles && !has_failed(); ++i) {
+            int m0, n0;
+            origin(i, m0, n0);
+            for (int kb = 0; kb < blocks; ++kb, ++issued) {
+                const int s = issued % kStages;
+                if (issued >= kStages && !mbar_wait(empty(s), (issued / kStages - 1) & 1)) { atomicExch(&failed, 1); break; }
+                if (has_failed()) break;
+                const uint32_t dst = ring + s * Shape::stage_bytes, bar = map_to_cta(full(s), 0);
+                if (rank == 0) mbar_expect_tx(full(s), 2 * Shape::stage_bytes);
+                tma_load_2d_pair(dst, &map_a, kb * kBlock, m0 + (int)rank * 128, bar);
+                tma_load_2d_pair(dst + 128 * kBlock, &map_w, kb * kBlock, n0 + (int)rank * (BN / 2), bar);
+            }
+        }
+        // after a failure copies may still be on their way into this CTA; their barrier may be the other CTA's
+        if (has_failed()) for (int q = 0; q < 100; ++q) __nanosleep(100000);
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        constexpr uint32_t idesc = umma_idesc_u8(256, BN);
+        int consumed = 0;
+        for (int i = 0; i < my_tiles && !has_failed(); ++i) {
+            const int acc = i & 1;
+            if (i >= kAccs && !mbar_wait(acc_empty(acc), ((i >> 1) - 1) & 1)) { atomicExch(&failed, 1); break; }
+            tmem_fence_after();
+            const uint32_t d = tmem + (uint32_t)(acc * BN);
+            for (int kb = 0; kb < blocks; ++kb, ++consumed) {
+                const int s = consumed % kStages;
+                if (!mbar_wait(full(s), (consumed / kStages) & 1)) { atomicExch(&failed, 1); break; }
+                if (has_failed()) break;
+                tmem_fence_after();
+                const uint32_t at = ring + s * Shape::stage_bytes;
+                const uint64_t da = umma_desc(at), db = umma_desc(at + 128 * kBlock);
+#pragma unroll
+                for (int j = 0; j < kBlock / 32; ++j) umma_u8<2>(d, da + 2 * j, db + 2 * j, idesc, kb > 0 || j > 0);
+                umma_commit<2>(empty(s));
+            }
+            umma_commit<2>(acc_full(acc));
+        }
+    } else if (warp >= 2) {
+        const int quarter = warp & 3;
+        uint32_t* sh = transpose + quarter * 32 * Shape::row_words;
+        const T* res = static_cast<const T*>(g.res);
+        T* out = static_cast<T*>(g.out);
+        // two adjacent columns at once where rows start on a multiple of two elements
+        const bool twos = (reinterpret_cast<uintptr_t>(out) % (2 * sizeof(T))) == 0 && g.ldo % 2 == 0 &&
+                          (!res || ((reinterpret_cast<uintptr_t>(res) % (2 * sizeof(T))) == 0 && g.ldr % 2 == 0));
+        for (int i = 0; i < my_tiles; ++i) {
+            const int acc = i & 1;
+            int m0, n0;
+            origin(i, m0, n0);
+            const int64_t row0 = (int64_t)m0 + (int)rank * 128 + quarter * 32;     // this warp's 32 rows
+            RowTerm mine = {0.0f, 0u};                                             // lane's row; handed round by shuffles
+            if (row0 + lane < g.m) mine = row_term(g, row0 + lane);
+            bool ok = mbar_wait(acc_full(acc), (i >> 1) & 1);
+            if (!ok) atomicExch(&failed, 1);
+            ok = __all_sync(0xffffffffu, ok && !has_failed());
+            if (!ok) break;
+            tmem_fence_after();
+            const int rows = (int)min((int64_t)32, g.m - row0);
+#pragma unroll 1
+            for (int c0 = 0; c0 < BN; c0 += 64) {
+                const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + c0);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t v[32];
+                    tmem_load32(from + h * 32, v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2)
+                        *reinterpret_cast<uint2*>(sh + lane * Shape::row_words + h * 32 + j) = make_uint2(v[j], v[j + 1]);
+                }
+                __syncwarp();
+                if (c0 + 64 >= BN) {                       // this warp's quarter of the accumulator is read
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(acc), 0));
+                }
+                const int64_t c = (int64_t)n0 + c0 + 2 * lane;
+                ColTerm ct[2] = {{0.0f, 0u, 0.0f}, {0.0f, 0u, 0.0f}};
+                if (c < g.n) ct[0] = col_term(g, c);
+                if (c + 1 < g.n) ct[1] = col_term(g, c + 1);
+#pragma unroll 4
+                for (int r = 0; r < rows; ++r) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(sh + r * Shape::row_words + 2 * lane);
+                    const RowTerm rt = {__shfl_sync(0xffffffffu, mine.scale, r), __shfl_sync(0xffffffffu, mine.term, r)};
+                    float f[2] = {linear_value(g, v.x, rt, ct[0]), linear_value(g, v.y, rt, ct[1])};
+                    T* o = out + (row0 + r) * g.ldo + c;
+                    const T* q = res + (row0 + r) * g.ldr + c;
+                    if (twos && c + 1 < g.n) {
+                        struct alignas(2 * sizeof(T)) Two { T x, y; };
+                        if (res) {
+                            const Two w = *reinterpret_cast<const Two*>(q);
+                            f[0] += to_f32(w.x);
+                            f[1] += to_f32(w.y);
+                        }
+                        *reinterpret_cast<Two*>(o) = Two{from_f32<T>(f[0]), from_f32<T>(f[1])};
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (c + e < g.n) {
+                                if (res) f[e] += to_f32(q[e]);
+                                o[e] = from_f32<T>(f[e]);
+                            }
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    __syncwarp();
+    tmem_fence_before();
+    cluster_sync_all();
+    tmem_fence_after();
+    if (warp == 0) tmem_free<2>(tmem, kAccs * BN);
+    if (threadIdx.x == 0 && failed) atomicAdd(&g_wait_failures, 1u);
+}
+
+template <typename T, int BN>
+int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
+    using Shape = SmallShape<BN>;
+    static PerDeviceOnce once;
+    auto* kernel = linear_small_kernel<T, BN>;
+    int rc = once.raise_smem_limit(kernel, Shape::smem);
+    if (rc != MPQ_OK) return rc;
+    CUtensorMap map_w, map_a;
+    if (!byte_tensor_map(&map_w, g.w, g.n, g.row_bytes, 128) || !byte_tensor_map(&map_a, g.a, g.m, g.row_bytes, BN)) return MPQ_ERR_CUDA;
+    const int sms = sm_count();
+    if (sms == 0) return MPQ_ERR_CUDA;
+    const int64_t tiles_w = ceil_div(g.n, 128), tiles = tiles_w * ceil_div(g.m, BN), blocks = ceil_div(g.row_bytes, kBlock);
+    if (tiles > (1 << 28)) return MPQ_ERR_BAD_SHAPE;
+    int splits = 1;                                       // as many as still fit the device at once, two blocks of k each at least
+    while (splits < 8 && splits * 2 <= BN && tiles * splits * 2 <= sms && blocks >= splits * 4) splits *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * splits), 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = Shape::smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)splits;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, map_w, map_a, g, (int)tiles_w, splits) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
+    return launch_status();
+}
+
+template <typename T, int BN>
+int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
+    using Shape = PairShape<BN>;
+    static PerDeviceOnce once;
+    auto* kernel = linear_pair_kernel<T, BN>;
+    int rc = once.raise_smem_limit(kernel, Shape::smem);
+    if (rc != MPQ_OK) return rc;
+    CUtensorMap map_w, map_a;
+    if (!byte_tensor_map(&map_w, g.w, g.n, g.row_bytes, BN / 2) || !byte_tensor_map(&map_a, g.a, g.m, g.row_bytes, 128)) return MPQ_ERR_CUDA;
+    const int pairs = sm_count() / 2;
+    if (pairs == 0) return MPQ_ERR_CUDA;
+    const int64_t tiles_m = ceil_div(g.m, 256), tiles = tiles_m * ceil_div(g.n, BN);
+    if (tiles > (1 << 28)) return MPQ_ERR_BAD_SHAPE;
+    const unsigned ctas = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
+    kernel<<<ctas, kThreads, Shape::smem, st>>>(map_a, map_w, g, (int)tiles_m, (int)tiles);
+    return launch_status();
+}
+
+// Up to 128 rows the weights' own traffic decides: the small form, its tile just wide enough.  Above, CTA pairs.
 template <typename T>
 int launch_linear_levels(const LinearArgs& g, cudaStream_t st) {
-    const int64_t tiles_m = ceil_div(g.m, kTile);
-    if (tiles_m > 65535) return MPQ_ERR_BAD_SHAPE;
-    linear_levels_kernel<T><<<dim3((unsigned)ceil_div(g.n, kTile), (unsigned)tiles_m), 256, 0, st>>>(g);
-    return launch_status();
+    if (g.m <= 16) return launch_linear_small<T, 16>(g, st);
+    if (g.m <= 32) return launch_linear_small<T, 32>(g, st);
+    if (g.m <= 64) return launch_linear_small<T, 64>(g, st);
+    if (g.m <= 128) return launch_linear_small<T, 128>(g, st);
+    return launch_linear_pair<T, 256>(g, st);
 }
 
 }  // namespace mpq
@@ -112,4 +476,11 @@ extern "C" int mpq_linear_levels(const uint8_t* a, const float* a_scale, const i
     if (dtype == MPQ_F32) return launch_linear_levels<float>(g, (cudaStream_t)stream);
     if (dtype == MPQ_F16) return launch_linear_levels<__half>(g, (cudaStream_t)stream);
     return launch_linear_levels<__nv_bfloat16>(g, (cudaStream_t)stream);
+}
+
+extern "C" int mpq_wait_failures(unsigned int* count_host, void* stream) {
+    if (!count_host) return MPQ_ERR_NULL;
+    if (cudaMemcpyFromSymbolAsync(count_host, g_wait_failures, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess ||
+        cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
+    return MPQ_OK;
 }

@@ -146,3 +146,8 @@ def test_no_rows_and_another_stream(mpq, cuda):
             got = mpq.linear_levels(part, w)
         st.synchronize()
         assert torch.equal(got, ref)
+
+
+def test_no_wait_ran_out(mpq, cuda):
+    """After every product above: no CTA gave up waiting for its copies or its partner."""
+    assert mpq.wait_failures() == 0
