@@ -20,21 +20,6 @@ struct LinearArgs {
     void* out; int64_t ldo;
 };
 
-// Epilogue constants of one row and one column, and the order of its fp32 operations (see the header).
-__device__ __forceinline__ float glue_value(float f, int glue) {
-    switch (glue) {
-        case MPQ_GLUE_RELU: return fmaxf(f, 0.0f);
-        case MPQ_GLUE_GELU: return 0.5f * f * (1.0f + erff(f * 0.70710678118654752f));
-        case MPQ_GLUE_GELU_TANH: {
-            // 0.5 f (1 + tanh z) = f / (1 + e^(-2z)); the exponential saturates to 0 or infinity, the quotient to f or 0
-            const float z2 = 1.5957691216057308f * (f + 0.044715f * f * f * f);
-            return __fdividef(f, 1.0f + __expf(-z2));
-        }
-        case MPQ_GLUE_SILU: return __fdividef(f, 1.0f + __expf(-f));
-        default: return f;
-    }
-}
-
 // acc (levels u, unsigned) -> one output, in the header's order of operations
 struct RowTerm { float scale; uint32_t term; };          // a_scale / L_a;  k L_a L_w - 2 L_w sums_a
 struct ColTerm { float scale; uint32_t term; float bias; };   // w_scale / L_w;  2 L_a sums_w;  bias
@@ -53,7 +38,28 @@ __device__ __forceinline__ ColTerm col_term(const LinearArgs& g, int64_t c) {
 }
 __device__ __forceinline__ float linear_value(const LinearArgs& g, uint32_t acc, const RowTerm& r, const ColTerm& c) {
     const float f = (float)(int32_t)(4u * acc + r.term - c.term) * (r.scale * c.scale);
-    return glue_value(g.bias ? f + c.bias : f, g.glue);
+    return g.bias ? f + c.bias : f;
+}
+// The activation of N values at once: one (uniform) branch for all of them, so their chains overlap.
+template <int N>
+__device__ __forceinline__ void glue_values(float (&f)[N], int glue) {
+    if (glue == MPQ_GLUE_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = fmaxf(f[i], 0.0f);
+    } else if (glue == MPQ_GLUE_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = 0.5f * f[i] * (1.0f + erff(f[i] * 0.70710678118654752f));
+    } else if (glue == MPQ_GLUE_GELU_TANH) {
+        // 0.5 f (1 + tanh z) = f / (1 + e^(-2z)); the exponential saturates to 0 or infinity, the quotient to f or 0
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float z2 = 1.5957691216057308f * (f[i] + 0.044715f * f[i] * f[i] * f[i]);
+            f[i] = __fdividef(f[i], 1.0f + __expf(-z2));
+        }
+    } else if (glue == MPQ_GLUE_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = __fdividef(f[i], 1.0f + __expf(-f[i]));
+    }
 }
 
 constexpr int kBlock = 128;                               // bytes of k per stage: one swizzled row
@@ -73,6 +79,24 @@ template <int BN> struct SmallShape {
     static constexpr int exchange_bytes = BN * 128 * 4;   // [S source CTAs][BN / S rows][128 columns] int32
     static constexpr int smem = stages * stage_bytes + exchange_bytes + 1024;
 };
+
+// `count` of N results of one column, rows r .. : the residuals are all read before the first result is written
+// (they may be the same tensor, so the compiler cannot move a load over a store).
+template <typename T, int N>
+__device__ __forceinline__ void store_column(const LinearArgs& g, float (&f)[N], int64_t r, int64_t c, int count) {
+    if (c >= g.n) return;
+    if (g.res) {
+        const T* res = static_cast<const T*>(g.res) + r * g.ldr + c;
+        T v[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) if (j < count) v[j] = res[j * g.ldr];
+#pragma unroll
+        for (int j = 0; j < N; ++j) if (j < count) f[j] += to_f32(v[j]);
+    }
+    T* out = static_cast<T*>(g.out) + r * g.ldo + c;
+#pragma unroll
+    for (int j = 0; j < N; ++j) if (j < count) out[j * g.ldo] = from_f32<T>(f[j]);
+}
 
 template <typename T, int BN>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -173,14 +197,11 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                 tmem_load16(lanes + r0, v);
                 tmem_wait_ld();
                 if (splits == 1) {
+                    float f[16];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const int64_t r = m0 + r0 + j;
-                        if (r >= g.m || c >= g.n) continue;
-                        float f = linear_value(g, v[j], RowTerm{row_scale[r0 + j], row_terms[r0 + j]}, ct);
-                        if (g.res) f += to_f32(static_cast<const T*>(g.res)[r * g.ldr + c]);
-                        static_cast<T*>(g.out)[r * g.ldo + c] = from_f32<T>(f);
-                    }
+                    for (int j = 0; j < 16; ++j) f[j] = linear_value(g, v[j], RowTerm{row_scale[r0 + j], row_terms[r0 + j]}, ct);
+                    glue_values(f, g.glue);
+                    store_column<T, 16>(g, f, (int64_t)m0 + r0, c, (int)min((int64_t)16, g.m - m0 - r0));
                 } else {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
@@ -200,15 +221,18 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             const int64_t c = (int64_t)n0 + col;
             if (c < g.n) {
                 const ColTerm ct = col_term(g, c);
-                for (int j = 0; j < own; ++j) {
-                    const int rr = split * own + j;
-                    const int64_t r = m0 + rr;
-                    if (r >= g.m) break;
-                    uint32_t acc = 0;
-                    for (int s = 0; s < splits; ++s) acc += exchange_ptr[(s * own + j) * 128 + col];
-                    float f = linear_value(g, acc, RowTerm{row_scale[rr], row_terms[rr]}, ct);
-                    if (g.res) f += to_f32(static_cast<const T*>(g.res)[r * g.ldr + c]);
-                    static_cast<T*>(g.out)[r * g.ldo + c] = from_f32<T>(f);
+                for (int j0 = 0; j0 < own; j0 += 2) {     // own is 2 or more
+                    const int rr = split * own + j0;
+                    if (m0 + rr >= g.m) break;
+                    float f[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t acc = 0;
+                        for (int s = 0; s < splits; ++s) acc += exchange_ptr[(s * own + j0 + j) * 128 + col];
+                        f[j] = linear_value(g, acc, RowTerm{row_scale[rr + j], row_terms[rr + j]}, ct);
+                    }
+                    glue_values(f, g.glue);
+                    store_column<T, 2>(g, f, (int64_t)m0 + rr, c, (int)min((int64_t)2, g.m - m0 - rr));
                 }
             }
         }
@@ -223,19 +247,21 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 // takes 128 cycles and reads 12 KB of operands while 12 KB of new ones arrive, 1.5 times the 128 bytes a cycle
 // of shared memory.  The pair (cta_group::2) shares the BN operand rows, each CTA holds half of them: 8 + 8 KB
 // per 128 cycles for BN = 256.  Persistent: pair p takes tiles p, p + pairs, ...; two accumulators in TMEM,
-// so a tile is stored while the next one is multiplied.  The store goes through a padded shared-memory
+// so a tile is stored while the next one is multiplied.  The store goes through a shared-memory
 // transpose, after which a lane owns two adjacent columns (their constants in registers) and a warp writes
 // whole row pieces whatever the row stride is.
+constexpr int kPairStoreWarps = 8;                        // two per quarter of the TMEM lanes, each with half of the columns
+constexpr int kPairThreads = 64 + 32 * kPairStoreWarps;
 template <int BN> struct PairShape {
     static constexpr int stage_bytes = (128 + BN / 2) * kBlock;     // per CTA
-    static constexpr int stages = BN == 256 ? 6 : 7;
-    static constexpr int row_words = 66;                            // 64 columns + 2: conflict-free 8-byte accesses both ways
-    static constexpr int transpose_bytes = 4 * 32 * row_words * 4;
+    static constexpr int stages = BN == 256 ? 5 : 6;
+    static constexpr int row_words = 64;                            // column pair p of row r lies at pair p ^ r: no bank conflicts either way
+    static constexpr int transpose_bytes = kPairStoreWarps * 32 * row_words * 4;
     static constexpr int smem = stages * stage_bytes + transpose_bytes + 1024;
 };
 
 template <typename T, int BN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const LinearArgs g,
                    int tiles_m, int tiles) {
     using Shape = PairShape<BN>;
@@ -251,12 +277,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     auto full = [&](int s) { return smem_addr(&bars[s]); };                        // used in the leader (rank 0)
     auto empty = [&](int s) { return smem_addr(&bars[kStages + s]); };             // one in each CTA
     auto acc_full = [&](int a) { return smem_addr(&bars[2 * kStages + a]); };      // one in each CTA
-    auto acc_empty = [&](int a) { return smem_addr(&bars[2 * kStages + kAccs + a]); };   // leader: 8 storing warps
+    auto acc_empty = [&](int a) { return smem_addr(&bars[2 * kStages + kAccs + a]); };   // leader: the storing warps of both
     auto has_failed = [&]() { return *(volatile int*)&failed != 0; };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2 * kStages + kAccs; ++i) mbar_init(smem_addr(&bars[i]), 1);
-        for (int a = 0; a < kAccs; ++a) mbar_init(acc_empty(a), 8);
+        for (int a = 0; a < kAccs; ++a) mbar_init(acc_empty(a), 2 * kPairStoreWarps);
         failed = 0;
         mbar_init_fence();
         tma_prefetch(&map_a);
@@ -318,28 +344,33 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             umma_commit<2>(acc_full(acc));
         }
     } else if (warp >= 2) {
-        const int quarter = warp & 3;
-        uint32_t* sh = transpose + quarter * 32 * Shape::row_words;
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        uint32_t* sh = transpose + (warp - 2) * 32 * Shape::row_words;
         const T* res = static_cast<const T*>(g.res);
         T* out = static_cast<T*>(g.out);
         // two adjacent columns at once where rows start on a multiple of two elements
         const bool twos = (reinterpret_cast<uintptr_t>(out) % (2 * sizeof(T))) == 0 && g.ldo % 2 == 0 &&
                           (!res || ((reinterpret_cast<uintptr_t>(res) % (2 * sizeof(T))) == 0 && g.ldr % 2 == 0));
+        struct alignas(2 * sizeof(T)) Two { T x, y; };
         for (int i = 0; i < my_tiles; ++i) {
             const int acc = i & 1;
             int m0, n0;
             origin(i, m0, n0);
             const int64_t row0 = (int64_t)m0 + (int)rank * 128 + quarter * 32;     // this warp's 32 rows
+            const int rows = (int)min((int64_t)32, g.m - row0);                    // 0 or less: none of them exists
             RowTerm mine = {0.0f, 0u};                                             // lane's row; handed round by shuffles
-            if (row0 + lane < g.m) mine = row_term(g, row0 + lane);
+            if (lane < rows) mine = row_term(g, row0 + lane);
             bool ok = mbar_wait(acc_full(acc), (i >> 1) & 1);
             if (!ok) atomicExch(&failed, 1);
             ok = __all_sync(0xffffffffu, ok && !has_failed());
             if (!ok) break;
             tmem_fence_after();
-            const int rows = (int)min((int64_t)32, g.m - row0);
 #pragma unroll 1
-            for (int c0 = 0; c0 < BN; c0 += 64) {
+            for (int c0 = half * (BN / 2); c0 < (half + 1) * (BN / 2); c0 += 64) {
+                const int64_t c = (int64_t)n0 + c0 + 2 * lane;
+                ColTerm ct[2] = {{0.0f, 0u, 0.0f}, {0.0f, 0u, 0.0f}};
+                if (c < g.n) ct[0] = col_term(g, c);
+                if (c + 1 < g.n) ct[1] = col_term(g, c + 1);
                 const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + c0);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -348,40 +379,45 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     tmem_wait_ld();
 #pragma unroll
                     for (int j = 0; j < 32; j += 2)
-                        *reinterpret_cast<uint2*>(sh + lane * Shape::row_words + h * 32 + j) = make_uint2(v[j], v[j + 1]);
+                        *reinterpret_cast<uint2*>(sh + lane * Shape::row_words + 2 * ((h * 16 + j / 2) ^ lane)) = make_uint2(v[j], v[j + 1]);
                 }
                 __syncwarp();
-                if (c0 + 64 >= BN) {                       // this warp's quarter of the accumulator is read
+                if (c0 + 64 >= (half + 1) * (BN / 2)) {    // this warp's part of the accumulator is read
                     tmem_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(acc), 0));
                 }
-                const int64_t c = (int64_t)n0 + c0 + 2 * lane;
-                ColTerm ct[2] = {{0.0f, 0u, 0.0f}, {0.0f, 0u, 0.0f}};
-                if (c < g.n) ct[0] = col_term(g, c);
-                if (c + 1 < g.n) ct[1] = col_term(g, c + 1);
-#pragma unroll 4
-                for (int r = 0; r < rows; ++r) {
-                    const uint2 v = *reinterpret_cast<const uint2*>(sh + r * Shape::row_words + 2 * lane);
-                    const RowTerm rt = {__shfl_sync(0xffffffffu, mine.scale, r), __shfl_sync(0xffffffffu, mine.term, r)};
-                    float f[2] = {linear_value(g, v.x, rt, ct[0]), linear_value(g, v.y, rt, ct[1])};
-                    T* o = out + (row0 + r) * g.ldo + c;
-                    const T* q = res + (row0 + r) * g.ldr + c;
-                    if (twos && c + 1 < g.n) {
-                        struct alignas(2 * sizeof(T)) Two { T x, y; };
-                        if (res) {
-                            const Two w = *reinterpret_cast<const Two*>(q);
-                            f[0] += to_f32(w.x);
-                            f[1] += to_f32(w.y);
-                        }
-                        *reinterpret_cast<Two*>(o) = Two{from_f32<T>(f[0]), from_f32<T>(f[1])};
-                    } else {
+                const bool both = c + 1 < g.n;
+                // kRowsAtOnce rows at a time: all residuals are read before the first result of the group is written
+                constexpr int kRowsAtOnce = 8;
+#pragma unroll 1
+                for (int r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
+                    T w[kRowsAtOnce][2];
+                    if (res && c < g.n) {
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            if (c + e < g.n) {
-                                if (res) f[e] += to_f32(q[e]);
-                                o[e] = from_f32<T>(f[e]);
-                            }
+                        for (int j = 0; j < kRowsAtOnce; ++j) {
+                            if (r0 + j >= rows) continue;
+                            const T* q = res + (row0 + r0 + j) * g.ldr + c;
+                            if (twos && both) { const Two t = *reinterpret_cast<const Two*>(q); w[j][0] = t.x; w[j][1] = t.y; }
+                            else { w[j][0] = q[0]; if (both) w[j][1] = q[1]; }
+                        }
+                    }
+                    float f[2 * kRowsAtOnce];
+#pragma unroll
+                    for (int j = 0; j < kRowsAtOnce; ++j) {
+                        const uint2 v = *reinterpret_cast<const uint2*>(sh + (r0 + j) * Shape::row_words + 2 * (lane ^ (r0 + j)));
+                        const RowTerm rt = {__shfl_sync(0xffffffffu, mine.scale, r0 + j), __shfl_sync(0xffffffffu, mine.term, r0 + j)};
+                        f[2 * j] = linear_value(g, v.x, rt, ct[0]);
+                        f[2 * j + 1] = linear_value(g, v.y, rt, ct[1]);
+                    }
+                    glue_values(f, g.glue);
+#pragma unroll
+                    for (int j = 0; j < kRowsAtOnce; ++j) {
+                        if (r0 + j >= rows || c >= g.n) continue;
+                        if (res) { f[2 * j] += to_f32(w[j][0]); if (both) f[2 * j + 1] += to_f32(w[j][1]); }
+                        T* o = out + (row0 + r0 + j) * g.ldo + c;
+                        if (twos && both) *reinterpret_cast<Two*>(o) = Two{from_f32<T>(f[2 * j]), from_f32<T>(f[2 * j + 1])};
+                        else { o[0] = from_f32<T>(f[2 * j]); if (both) o[1] = from_f32<T>(f[2 * j + 1]); }
                     }
                 }
                 __syncwarp();
@@ -410,7 +446,7 @@ int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
     const int64_t tiles_w = ceil_div(g.n, 128), tiles = tiles_w * ceil_div(g.m, BN), blocks = ceil_div(g.row_bytes, kBlock);
     if (tiles > (1 << 28)) return MPQ_ERR_BAD_SHAPE;
     int splits = 1;                                       // as many as still fit the device at once, two blocks of k each at least
-    while (splits < 8 && splits * 2 <= BN && tiles * splits * 2 <= sms && blocks >= splits * 4) splits *= 2;
+    while (splits < 8 && splits * 4 <= BN && tiles * splits * 2 <= sms && blocks >= splits * 4) splits *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * splits), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -440,7 +476,7 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     const int64_t tiles_m = ceil_div(g.m, 256), tiles = tiles_m * ceil_div(g.n, BN);
     if (tiles > (1 << 28)) return MPQ_ERR_BAD_SHAPE;
     const unsigned ctas = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
-    kernel<<<ctas, kThreads, Shape::smem, st>>>(map_a, map_w, g, (int)tiles_m, (int)tiles);
+    kernel<<<ctas, kPairThreads, Shape::smem, st>>>(map_a, map_w, g, (int)tiles_m, (int)tiles);
     return launch_status();
 }
 
