@@ -361,37 +361,63 @@ inline int64_t tile_bound(int64_t tokens, int batch, int group, int rows) {
     return tokens * group / rows + (tokens < batch ? tokens : batch);
 }
 
-struct AttnPlan { int64_t tiles; int splits, split_tokens; };
+struct AttnPlan { bool many; int64_t tiles; int splits, split_tokens; };
 
-// How far a context is split: enough CTAs for about three rounds of four per multiprocessor, at least one
+// Which kernel, and how far a context is split.
+//   More than 32 rows per sequence and key head: 256-row tiles on the tensor cores.  A context is split only
+// while the tiles do not fill the multiprocessors, in stretches of 512 tokens at least (each split writes and
+// re-reads a row of fp32 results).
+//   Otherwise: tiles of 16 rows; enough CTAs for about three rounds of four per multiprocessor, at least one
 // chunk per warp in each.
-AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_kv) {
+AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_q, int64_t max_kv) {
     AttnPlan p;
-    p.tiles = tile_bound(tokens, batch, group, kRows);
-    const int64_t want = 148 * 4 * 3;
-    int64_t per = ceil_div(max_kv * p.tiles * kv_heads, want);
-    per = ceil_div(per < 1 ? 1 : per, kChunk * kWarps) * (kChunk * kWarps);
-    int64_t splits = ceil_div(max_kv < 1 ? 1 : max_kv, per);
-    if (splits > 256) { splits = 256; per = ceil_div(ceil_div(max_kv, splits), kChunk * kWarps) * (kChunk * kWarps); }
-    p.splits = (int)splits;
-    p.split_tokens = (int)per;
+    p.many = max_q * group > 32;
+    const int64_t context = max_kv < 1 ? 1 : max_kv;
+    int64_t per, unit;
+    if (p.many) {
+        p.tiles = tile_bound(tokens, batch, group, kTileRows);
+        unit = kStepTokens;
+        int64_t likely = batch * ceil_div(max_q * group, kTileRows);
+        if (likely > p.tiles) likely = p.tiles;
+        int64_t splits = 148 / (likely * kv_heads);
+        if (splits > ceil_div(context, 512)) splits = ceil_div(context, 512);
+        per = ceil_div(context, splits < 1 ? 1 : splits);
+    } else {
+        p.tiles = tile_bound(tokens, batch, group, kRows);
+        unit = kChunk * kWarps;
+        per = ceil_div(context * p.tiles * kv_heads, 148 * 4 * 3);
+    }
+    per = ceil_div(per, unit) * unit;
+    if (ceil_div(context, per) > 256) per = ceil_div(ceil_div(context, 256), unit) * unit;
+    p.splits = (int)ceil_div(context, per);
+    p.split_tokens = (int)(per > 0x40000000 ? 0x40000000 : per);
     return p;
 }
 
 inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 
+template <typename T, int D>
+int launch_merge(const AttnArgs& g, bool many, cudaStream_t st) {
+    const unsigned blocks = (unsigned)ceil_div(g.tokens * g.heads, 4);
+    return many ? launch_chained_as(true, attn_merge_kernel<T, D, kTileRows, kStepTokens>, blocks, 128u, 0, st, g)
+                : launch_chained_as(true, attn_merge_kernel<T, D, kRows, kChunk>, blocks, 128u, 0, st, g);
+}
+
 template <typename T, int D, int BITS>
-int launch_attention(const AttnArgs& g, const AttnPlan& p, cudaStream_t st) {
+int launch_rows(const AttnArgs& g, const AttnPlan& p, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.tiles, (unsigned)g.kv_heads, (unsigned)p.splits);
     cfg.blockDim = dim3(kWarps * 32, 1, 1);
     cfg.stream = st;
     if (cudaLaunchKernelEx(&cfg, attn_rows_kernel<T, D, BITS>, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
-    if (p.splits > 1) {
-        const int64_t blocks = ceil_div(g.tokens * g.heads, 4);
-        return launch_chained_as(true, attn_merge_kernel<T, D, kRows, kChunk>, (unsigned)blocks, 128u, 0, st, g);
-    }
     return launch_status();
+}
+
+template <typename T, int D>
+int launch_attention(const AttnArgs& g, const AttnPlan& p, int dtype, int bits, cudaStream_t st) {
+    const int rc = p.many ? attention_tiles(g, dtype, D, bits, p.tiles, st)
+                          : bits == 8 ? launch_rows<T, D, 8>(g, p, st) : launch_rows<T, D, 4>(g, p, st);
+    return rc != MPQ_OK || p.splits == 1 ? rc : launch_merge<T, D>(g, p.many, st);
 }
 
 }  // namespace mpq
@@ -401,7 +427,7 @@ using namespace mpq;
 extern "C" int64_t mpq_cache_attention_workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim,
                                                  int64_t max_q, int64_t max_kv) {
     if (tokens <= 0 || batch <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || dim <= 0 || max_q < 0 || max_kv < 0) return 0;
-    const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_kv);
+    const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_q, max_kv);
     if (p.splits <= 1) return 0;
     return up16(tokens * heads * p.splits * dim * 4) + up16(tokens * heads * p.splits * 8);
 }
@@ -423,7 +449,7 @@ extern "C" int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_
     if (!aligned16(k_levels) || !aligned16(v_levels) || !aligned_to(k_scale, 4) || !aligned_to(v_scale, 4) || !aligned_to(q, 2) ||
         !aligned_to(out, 2) || !aligned_to(lse, 4) || !aligned_to(q_starts, 4) || !aligned_to(kv_lens, 4) || !aligned_to(table, 4)) return MPQ_ERR_ALIGN;
     if (tokens == 0) return MPQ_OK;
-    const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_kv);
+    const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_q, max_kv);
     if (p.tiles > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
     AttnArgs g = {q, q_token_stride, q_head_stride, q_starts, kv_lens, table, table_stride, tokens, batch, heads, kv_heads, heads / kv_heads,
                   k_levels, k_scale, v_levels, v_scale, pages, page_size, causal != 0, window, scale * 1.4426950408889634f,
@@ -437,10 +463,6 @@ extern "C" int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_
     }
     cudaStream_t st = (cudaStream_t)stream;
     const bool bf = dtype == MPQ_BF16;
-    if (dim == 128) {
-        if (bits == 8) return bf ? launch_attention<__nv_bfloat16, 128, 8>(g, p, st) : launch_attention<__half, 128, 8>(g, p, st);
-        return bf ? launch_attention<__nv_bfloat16, 128, 4>(g, p, st) : launch_attention<__half, 128, 4>(g, p, st);
-    }
-    if (bits == 8) return bf ? launch_attention<__nv_bfloat16, 64, 8>(g, p, st) : launch_attention<__half, 64, 8>(g, p, st);
-    return bf ? launch_attention<__nv_bfloat16, 64, 4>(g, p, st) : launch_attention<__half, 64, 4>(g, p, st);
+    if (dim == 128) return bf ? launch_attention<__nv_bfloat16, 128>(g, p, dtype, bits, st) : launch_attention<__half, 128>(g, p, dtype, bits, st);
+    return bf ? launch_attention<__nv_bfloat16, 64>(g, p, dtype, bits, st) : launch_attention<__half, 64>(g, p, dtype, bits, st);
 }

@@ -127,7 +127,7 @@ __device__ __forceinline__ float fast_exp2(float x) {
 // cancels in the denominator).
 __device__ __forceinline__ void range_exponent(float s, float& lg, float& inv) {
     lg = __log2f(s < kTinyRange ? kTinyRange : s);           // NaN passes through
-    inv = fast_exp2(-lg);
+    inv = exp2f(-lg);                                       // may be subnormal
 }
 
 __device__ __forceinline__ float final_value(float o) { return fabsf(o) < 2.0f * kTinyRange ? 0.0f : o; }
@@ -139,5 +139,10 @@ __device__ __forceinline__ void row_power(float amax, float& down, float& up) {
     down = __uint_as_float((uint32_t)(127 - e) << 23);
     up = __uint_as_float((uint32_t)(127 + e) << 23);
 }
+
+// The tensor-core form for many query rows (mpq_attention_tiles.cu).
+constexpr int kTileRows = 256, kStepTokens = 128;         // rows of a CTA, context tokens of a step
+int attention_tiles(const AttnArgs& g, int dtype, int dim, int bits, int64_t tiles, cudaStream_t st);
+int attention_wait_failures(unsigned int* count_host, cudaStream_t st);
 
 }  // namespace mpq

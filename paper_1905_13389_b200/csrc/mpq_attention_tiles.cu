@@ -1,0 +1,509 @@
+// Attention over a paged cache of levels for many query rows (mpq_cache_attention): tiles of 256 rows on the
+// 5th-generation tensor cores.
+//
+// A CTA takes 256 query rows (tokens x heads of one key head, two tiles of 128) and a stretch of the context
+// in steps of 128 tokens.  Warps 8-11 turn level bytes into fp16 levels: keys as rows [token][dim], values
+// transposed, [dim][token], both in the 128-byte swizzled K-major layout that tcgen05.mma reads; they load a
+// step ahead into registers, so pages of any size cost nothing but the address arithmetic.  Warp 12 issues
+//     S_h = Q_h K^T  (fp16, fp32 accumulator in TMEM),    O_h += W_h V  (W_h in TMEM, where S_h was)
+// for the two tiles in turn, so that the tensor cores work on one tile while the other one's softmax runs in
+// warps 0-3 and 4-7, one thread per row: no reductions across lanes.  W_h overwrites S_h, and the commit of
+// S_h's next product also says that O_h is complete: a row whose maximum has grown by more than 2^3 rescales
+// its part of O_h then, before it hands over its weights (the accumulators are otherwise left alone).
+//
+// What bounds it: per step and tile the score and value products take 512 cycles each at the fp16 rate for
+// dim 128, the 128 exponentials of a row 1024 cycles of the special-function units; the three constants per
+// token that every row needs (range factor of the key, exponent and reciprocal of the value's range) come
+// from shared memory at 128 bytes a cycle, 1536 cycles.
+#include "mpq_attention.cuh"
+#include "mpq_tensor.cuh"
+
+namespace mpq {
+
+constexpr int kTileThreads = 512;
+constexpr float kLag = 3.0f;                              // the reference may lie this far (log2) below a row's maximum
+constexpr float kTileBoost = kBoost - kLag;               // so that weights still end at 2^15
+
+__device__ unsigned int g_attention_wait_failures;
+
+template <int D> struct TileSmem {
+    static constexpr int q_half = 128 * 128;              // 128 rows x 64 elements
+    static constexpr int q_tile = q_half * (D / 64);
+    static constexpr int k_stage = 128 * 128 * (D / 64);  // [D / 64][128 tokens][64 dims]
+    static constexpr int v_stage = D * 128 * 2;           // [2][D dims][64 tokens]
+    static constexpr int q = 0, k = 2 * q_tile, v = k + 2 * k_stage, consts = v + 2 * v_stage;
+    static constexpr int const_stage = 3 * kStepTokens * 4;   // key factor, value exponent, value reciprocal
+    static constexpr int rows = consts + 2 * const_stage;     // cache row numbers, two steps
+    static constexpr int total = rows + 2 * kStepTokens * 4 + 1024;
+};
+
+template <int REGS> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
+template <int REGS> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS)); }
+
+__device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// Two 16-bit lanes holding 2u + 1 + 1024 (as fp16 bits 0x6401 + 2u) -> fp16 level 2u - L
+template <int BITS>
+__device__ __forceinline__ uint32_t exact_level(uint32_t x) {
+    constexpr float c = BITS == 8 ? -1280.0f : -1040.0f;
+    const __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&x), __float2half2_rn(c));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Bytes sel and sel' of (a, b), zero-extended to 16 bits each by the caller's masks -> levels
+__device__ __forceinline__ uint32_t level8(uint32_t spread) { return exact_level<8>(spread * 2u + 0x64016401u); }
+// Nibble i (0..3) of each half word of x -> levels
+__device__ __forceinline__ uint32_t level4(uint32_t x, int i) {
+    return exact_level<4>(((i == 0 ? x << 1 : x >> (4 * i - 1)) & 0x001e001eu) | 0x64016401u);
+}
+// Eight key elements as one 16-byte chunk: in order for 8 bits; 0 4 1 5 2 6 3 7 for 4 bits (the queries are
+// staged in the same order).
+__device__ __forceinline__ void key_chunk8(uint32_t w0, uint32_t w1, uint32_t addr) {
+    st_shared16(addr, level8(__byte_perm(w0, 0, 0x4140)), level8(__byte_perm(w0, 0, 0x4342)),
+                level8(__byte_perm(w1, 0, 0x4140)), level8(__byte_perm(w1, 0, 0x4342)));
+}
+__device__ __forceinline__ void key_chunk4(uint32_t w, uint32_t addr) {
+    st_shared16(addr, level4(w, 0), level4(w, 1), level4(w, 2), level4(w, 3));
+}
+// 16-byte chunk `c` of row r in a [rows][128 bytes] tile with the 128-byte swizzle
+__device__ __forceinline__ uint32_t swizzled(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
+
+template <typename T, int D, int BITS>
+__global__ void __launch_bounds__(kTileThreads, 1)
+attn_tiles_kernel(const AttnArgs g) {
+    using Smem = TileSmem<D>;
+    constexpr int kRowBytes = D * BITS / 8;
+    constexpr uint32_t kTmemS = 0, kTmemO = 256;          // S_0, S_1: 128 columns each; O_0, O_1: D columns each, 128 apart
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[16];
+    __shared__ uint32_t tmem_holder;
+    __shared__ int failed;
+    const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    unsigned char* base_ptr = smem_raw + (base - smem_addr(smem_raw));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t q_ready = smem_addr(&bars[0]), o_full = smem_addr(&bars[1]);
+    auto k_full = [&](int s) { return smem_addr(&bars[2 + s]); };
+    auto k_empty = [&](int s) { return smem_addr(&bars[4 + s]); };
+    auto v_full = [&](int s) { return smem_addr(&bars[6 + s]); };
+    auto v_empty = [&](int s) { return smem_addr(&bars[8 + s]); };
+    auto c_empty = [&](int s) { return smem_addr(&bars[10 + s]); };      // constants of a step: read by the softmax warps
+    auto s_full = [&](int h) { return smem_addr(&bars[12 + h]); };
+    auto p_ready = [&](int h) { return smem_addr(&bars[14 + h]); };
+    auto has_failed = [&]() { return *(volatile int*)&failed != 0; };
+
+    chain_entry();
+    // ---- which rows, which part of the context (the same in every warp)
+    AttnTile t;
+    const int tile_index = (int)gridDim.x - 1 - (int)blockIdx.x;         // later tiles see more: they go first
+    const int kv_head = blockIdx.y;
+    if (!find_tile<kTileRows>(g, tile_index, t)) return;
+    tile_range<kTileRows, kStepTokens>(g, t);
+    const int used = tile_splits(g, t);
+    if ((int)blockIdx.z >= used) return;
+    int begin, end;
+    split_range(g, t, blockIdx.z, used, begin, end);
+    const int steps = (end - begin + kStepTokens - 1) / kStepTokens;
+    const int tiles = t.rows - t.row0 > 128 ? 2 : 1;
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_ready, 4 * tiles);
+        mbar_init(o_full, 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(k_full(s), 4); mbar_init(k_empty(s), 1);
+            mbar_init(v_full(s), 4); mbar_init(v_empty(s), 1);
+            mbar_init(c_empty(s), 4 * tiles);
+            mbar_init(s_full(s), 1); mbar_init(p_ready(s), 4);
+        }
+        failed = 0;
+        mbar_init_fence();
+    }
+    if (warp == 12) tmem_alloc<1>(&tmem_holder, 512);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = tmem_holder;
+
+    if (warp < 8) {
+        // ================= softmax: one thread per query row
+        regs_up<192>();
+        const int h = warp >> 2;
+        if (h < tiles) {
+            const int in_tile = threadIdx.x & 127, r = t.row0 + h * 128 + in_tile;
+            const bool live = r < t.rows;
+            const int token = live ? r / g.group : t.n_q - 1, head = kv_head * g.group + (live ? r % g.group : 0);
+            float row_scale;
+            int first, last;
+            {
+                // the row as fp16, scaled by a power of two
+                const T* q = static_cast<const T*>(g.q) + (int64_t)(t.q0 + token) * g.q_ts + (int64_t)head * g.q_hs;
+                uint4 raw[D / 8];
+                if (live && (reinterpret_cast<uintptr_t>(q) & 15u) == 0) {
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c) raw[c] = __ldg(reinterpret_cast<const uint4*>(q) + c);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c) {
+                        T e[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) e[i] = live ? q[c * 8 + i] : from_f32<T>(0.0f);
+                        raw[c] = *reinterpret_cast<const uint4*>(e);
+                    }
+                }
+                float amax = 0.0f;
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    const T* e = reinterpret_cast<const T*>(&raw[c]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(to_f32(e[i])));
+                }
+                float down, up;
+                row_power(amax, down, up);
+                row_scale = up * g.scale_log2;
+                const uint32_t tile = base + Smem::q + h * Smem::q_tile;
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    const T* e = reinterpret_cast<const T*>(&raw[c]);
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int a = BITS == 8 ? 2 * i : i, b = BITS == 8 ? 2 * i + 1 : i + 4;
+                        const __half2 v = __floats2half2_rn(to_f32(e[a]) * down, to_f32(e[b]) * down);
+                        w[i] = *reinterpret_cast<const uint32_t*>(&v);
+                    }
+                    st_shared16(tile + (c >> 3) * Smem::q_half + swizzled(in_tile, c & 7), w[0], w[1], w[2], w[3]);
+                }
+                row_range(g, t, token, first, last);
+                if (!live) { first = 0; last = 0x7fffffff; }             // computed with q = 0, never stored
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_ready);
+            }
+            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+            const uint32_t ts = lanes + kTmemS + h * 128, to = lanes + kTmemO + h * 128;
+            float top = -INFINITY, ref = 0.0f, l0 = 0.0f, l1 = 0.0f;     // ref: what is subtracted, top - kTileBoost when it was set
+            float set = -INFINITY;                                       // the maximum that ref belongs to
+            bool ok = true;
+            for (int i = 0; i < steps; ++i) {
+                const int st = i & 1, j0 = begin + i * kStepTokens;
+                // the constants were written before the keys that S is made of
+                ok = mbar_wait_or(s_full(h), i & 1, &failed) && mbar_wait_or(k_full(st), (i >> 1) & 1, &failed);
+                ok = __all_sync(0xffffffffu, ok && !has_failed());
+                if (!ok) break;
+                tmem_fence_after();
+                uint32_t v[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_load32(ts + c * 32, v[c]);
+                tmem_wait_ld();
+                const float4* kf = reinterpret_cast<const float4*>(base_ptr + Smem::consts + st * Smem::const_stage);
+                const float4* lf = kf + kStepTokens / 4;
+                const float4* inv = lf + kStepTokens / 4;
+                const bool whole = __all_sync(0xffffffffu, j0 >= first && j0 + kStepTokens - 1 <= last);
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 k4 = kf[c * 8 + e], l4 = lf[c * 8 + e];
+                        const float ks[4] = {k4.x, k4.y, k4.z, k4.w}, ls[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const float y = fmaf(__uint_as_float(v[c][e * 4 + x]) * ks[x], row_scale, ls[x]);
+                            v[c][e * 4 + x] = __float_as_uint(y);
+                        }
+                    }
+                if (!whole) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const int j = j0 + c * 32 + e;
+                            if (j < first || j > last) v[c][e] = 0xff800000u;        // -infinity
+                        }
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(v[c][e]));
+                top = fmaxf(top, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+                const bool grow = top > set + kLag;                                   // also the first finite maximum
+                if (__any_sync(0xffffffffu, grow)) {
+                    const float f = grow ? fast_exp2(set - top) : 1.0f;               // set = -infinity: 0
+                    if (grow) { set = top; ref = top - kTileBoost; l0 *= f; l1 *= f; }
+                    if (i > 0) {
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t o[32];
+                            tmem_load32(to + c * 32, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_store32(to + c * 32, o);
+                        }
+                        tmem_wait_st();
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 i4 = inv[c * 8 + e];
+                        const float is[4] = {i4.x, i4.y, i4.z, i4.w};
+                        float w[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) w[x] = fast_exp2(__uint_as_float(v[c][e * 4 + x]) - ref);
+                        if (whole) {
+                            l0 = fmaf(w[0], is[0], l0); l1 = fmaf(w[1], is[1], l1);
+                            l0 = fmaf(w[2], is[2], l0); l1 = fmaf(w[3], is[3], l1);
+                        } else {
+                            // a token that is not seen may have any range: its reciprocal must not meet the 0
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                if (v[c][e * 4 + x] != 0xff800000u) l0 = fmaf(w[x], is[x], l0);
+                        }
+                        const __half2 a = __floats2half2_rn(w[0], w[1]), b = __floats2half2_rn(w[2], w[3]);
+                        p[e * 2] = *reinterpret_cast<const uint32_t*>(&a);
+                        p[e * 2 + 1] = *reinterpret_cast<const uint32_t*>(&b);
+                    }
+                    tmem_store16(ts + c * 16, p);
+                }
+                tmem_wait_st();
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) { mbar_arrive(p_ready(h)); mbar_arrive(c_empty(st)); }
+            }
+            // ---- result
+            ok = mbar_wait_or(o_full, 0, &failed);
+            ok = __all_sync(0xffffffffu, ok && !has_failed());
+            if (ok) {
+                tmem_fence_after();
+                const float l = l0 + l1;
+                const bool empty = set == -INFINITY;
+                constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);
+                const int64_t at = (int64_t)(t.q0 + token) * g.heads + head;
+                const float den = used > 1 ? kInvL : __fdiv_rn(kInvL, l);
+                T* out = static_cast<T*>(g.out) + (int64_t)(t.q0 + token) * g.o_ts + (int64_t)head * g.o_hs;
+                const int64_t slot = at * g.splits + blockIdx.z;
+                const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
+#pragma unroll 1
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    if (steps > 0) { tmem_load32(to + c * 32, o); tmem_wait_ld(); }
+                    if (!live) continue;
+                    float f[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) f[e] = empty ? 0.0f : __uint_as_float(o[e]) * den;
+                    if (used > 1) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            *reinterpret_cast<float4*>(g.part_o + slot * D + c * 32 + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) f[e] = final_value(f[e]);
+                        if (aligned) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8) {
+                                const float part[8] = {f[e], f[e + 1], f[e + 2], f[e + 3], f[e + 4], f[e + 5], f[e + 6], f[e + 7]};
+                                store_vec<T, 8>(out + c * 32 + e, part);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) out[c * 32 + e] = from_f32<T>(f[e]);
+                        }
+                    }
+                }
+                if (live) {
+                    // the merge counts in units of 2^kBoost above the maximum it is told
+                    if (used > 1) g.part_ml[slot] = make_float2(empty ? -INFINITY : ref + kBoost, l);
+                    else if (g.lse) g.lse[at] = empty ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+                }
+                tmem_fence_before();
+            }
+        }
+    } else if (warp < 12) {
+        // ================= levels: bytes of the cache -> fp16 operands
+        regs_down<104>();
+        const int th = threadIdx.x - 256;
+        const int32_t* pages_of = g.table + (int64_t)t.b * g.table_stride;
+        uint32_t* row_of = reinterpret_cast<uint32_t*>(base_ptr + Smem::rows);
+        // keys: kKeyLanes lanes share a row, 16 bytes each
+        constexpr int kKeyLanes = kRowBytes / 16, kKeyLoads = kKeyLanes;
+        const int key_row = th / kKeyLanes, key_part = th % kKeyLanes;
+        // values: eight tokens and an eighth of the dims per thread; neighbouring lanes take neighbouring token groups
+        constexpr int kValBytes = kRowBytes / 8, kDims = D / 8;
+        const int group8 = th & 15, eighth = th >> 4;
+        auto rows_of_step = [&](int i, float& ks, float& vs) {           // this thread's token of step i
+            const int j = begin + i * kStepTokens + th;
+            const uint32_t row = j < end ? context_row(g, pages_of, j, kv_head) : 0xffffffffu;
+            row_of[(i & 1) * kStepTokens + th] = row == 0xffffffffu ? 0u : row;       // a row that can be read; weight 0
+            ks = row == 0xffffffffu ? -1.0f : __ldg(g.k_scale + row);
+            vs = row == 0xffffffffu ? 0.0f : __ldg(g.v_scale + row);
+            return row != 0xffffffffu;
+        };
+        uint4 kw[kKeyLoads];
+        auto load_keys = [&](int i) {
+#pragma unroll
+            for (int x = 0; x < kKeyLoads; ++x) {
+                const uint32_t row = row_of[(i & 1) * kStepTokens + key_row + x * (128 / kKeyLanes)];
+                kw[x] = __ldg(reinterpret_cast<const uint4*>(g.k_levels + (uint64_t)row * kRowBytes + key_part * 16));
+            }
+        };
+        float ks = 0.0f, vs = 0.0f, next_ks = 0.0f, next_vs = 0.0f;
+        bool here = false, next_here = false;
+        if (steps > 0) here = rows_of_step(0, ks, vs);
+        asm volatile("bar.sync 2, 128;" ::: "memory");
+        if (steps > 0) load_keys(0);
+        for (int i = 0; i < steps; ++i) {
+            const int st = i & 1;
+            // values of this step into registers, rows of the next one
+            uint32_t vw[8][kValBytes / 4];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const uint32_t row = row_of[st * kStepTokens + group8 * 8 + x];
+                const uint8_t* p = g.v_levels + (uint64_t)row * kRowBytes + eighth * kValBytes;
+                if constexpr (kValBytes == 16) { const uint4 r = __ldg(reinterpret_cast<const uint4*>(p)); vw[x][0] = r.x; vw[x][1] = r.y; vw[x][2] = r.z; vw[x][3] = r.w; }
+                else if constexpr (kValBytes == 8) { const uint2 r = __ldg(reinterpret_cast<const uint2*>(p)); vw[x][0] = r.x; vw[x][1] = r.y; }
+                else vw[x][0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+            }
+            if (i + 1 < steps) next_here = rows_of_step(i + 1, next_ks, next_vs);
+            bool ok = true;
+            if (i >= 2) ok = mbar_wait_or(k_empty(st), ((i >> 1) - 1) & 1, &failed) && mbar_wait_or(c_empty(st), ((i >> 1) - 1) & 1, &failed);
+            ok = __all_sync(0xffffffffu, ok && !has_failed());
+            if (ok) {
+                float* consts = reinterpret_cast<float*>(base_ptr + Smem::consts + st * Smem::const_stage);
+                float lg, inv;
+                range_exponent(vs, lg, inv);
+                consts[th] = here ? ks * (1.0f / (float)((1 << BITS) - 1)) : 0.0f;
+                consts[kStepTokens + th] = here ? lg : -INFINITY;        // a token that is not there: weight 0
+                consts[2 * kStepTokens + th] = here ? inv : 0.0f;
+                const uint32_t tile = base + Smem::k + st * Smem::k_stage;
+#pragma unroll
+                for (int x = 0; x < kKeyLoads; ++x) {
+                    const int r = key_row + x * (128 / kKeyLanes);
+                    const uint32_t w[4] = {kw[x].x, kw[x].y, kw[x].z, kw[x].w};
+                    if constexpr (BITS == 8) {
+                        // the two 8-element chunks; lanes of the two halves of a row start with different ones (banks)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const int z = (key_part * 2 >= 8) ^ y, c = key_part * 2 + z;
+                            key_chunk8(z ? w[2] : w[0], z ? w[3] : w[1], tile + (c >> 3) * 16384 + swizzled(r, c & 7));
+                        }
+                    } else {
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const int c = key_part * 4 + y;
+                            key_chunk4(w[y], tile + (c >> 3) * 16384 + swizzled(r, c & 7));
+                        }
+                    }
+                }
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(k_full(st));
+            }
+            asm volatile("bar.sync 2, 128;" ::: "memory");               // rows of the next step are there
+            if (i + 1 < steps) load_keys(i + 1);
+            ok = true;
+            if (i >= 2) ok = mbar_wait_or(v_empty(st), ((i >> 1) - 1) & 1, &failed);
+            ok = __all_sync(0xffffffffu, ok && !has_failed());
+            if (ok) {
+                const uint32_t tile = base + Smem::v + st * Smem::v_stage + (group8 >> 3) * (D * 128);
+                constexpr int kPer = 32 / BITS;                          // dims per word
+#pragma unroll
+                for (int w = 0; w < kValBytes / 4; ++w)
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) {
+                        uint32_t p[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const uint32_t a = vw[2 * x][w], b = vw[2 * x + 1][w];
+                            if constexpr (BITS == 8) p[x] = level8(__byte_perm(a, b, 0x0400 + 0x0101 * e) & 0x00ff00ffu);
+                            else p[x] = level4(__byte_perm(a, b, e < 4 ? 0x5410 : 0x7632), e & 3);
+                        }
+                        const int d = eighth * kDims + w * kPer + e;
+                        st_shared16(tile + swizzled(d, group8 & 7), p[0], p[1], p[2], p[3]);
+                    }
+                proxy_fence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(v_full(st));
+            }
+            ks = next_ks; vs = next_vs; here = next_here;
+        }
+    } else {
+        // ================= tensor-core issue
+        regs_down<24>();
+        if (warp == 12 && lane == 0) {
+            constexpr uint32_t idesc_s = umma_idesc_f16(128, kStepTokens), idesc_o = umma_idesc_f16(128, D);
+            bool ok = mbar_wait_or(q_ready, 0, &failed);
+            auto scores = [&](int h, int st) {
+                const uint64_t a = umma_desc(base + Smem::q + h * Smem::q_tile), b = umma_desc(base + Smem::k + st * Smem::k_stage);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)                         // 16 elements = 32 bytes; 64 elements per half
+                    umma_f16_ss(tmem + kTmemS + h * 128, a + (uint64_t)((k >> 2) * (16384 >> 4) + (k & 3) * 2),
+                                b + (uint64_t)((k >> 2) * (16384 >> 4) + (k & 3) * 2), idesc_s, k > 0);
+                umma_commit<1>(s_full(h));
+            };
+            if (ok && steps > 0) {
+                ok = mbar_wait_or(k_full(0), 0, &failed);
+                tmem_fence_after();
+                if (ok) {
+                    for (int h = 0; h < tiles; ++h) scores(h, 0);
+                    umma_commit<1>(k_empty(0));
+                }
+            }
+            for (int i = 0; i < steps && ok && !has_failed(); ++i) {
+                const int st = i & 1, nx = st ^ 1;
+                ok = mbar_wait_or(v_full(st), (i >> 1) & 1, &failed);
+                if (ok && i + 1 < steps) ok = mbar_wait_or(k_full(nx), ((i + 1) >> 1) & 1, &failed);
+                for (int h = 0; h < tiles && ok; ++h) {
+                    ok = mbar_wait_or(p_ready(h), i & 1, &failed);
+                    if (!ok || has_failed()) { ok = false; break; }
+                    tmem_fence_after();
+                    const uint64_t b = umma_desc(base + Smem::v + st * Smem::v_stage);
+#pragma unroll
+                    for (int k = 0; k < kStepTokens / 16; ++k)
+                        umma_f16_ts(tmem + kTmemO + h * 128, tmem + kTmemS + h * 128 + k * 8,
+                                    b + (uint64_t)((k >> 2) * ((D * 128) >> 4) + (k & 3) * 2), idesc_o, i > 0 || k > 0);
+                    if (h == tiles - 1) umma_commit<1>(v_empty(st));
+                    if (i + 1 < steps) {
+                        scores(h, nx);
+                        if (h == tiles - 1) umma_commit<1>(k_empty(nx));
+                    }
+                }
+            }
+            umma_commit<1>(o_full);
+            if (!mbar_wait(o_full, 0)) atomicExch(&failed, 1);
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    tmem_fence_after();
+    if (warp == 12) tmem_free<1>(tmem, 512);
+    if (threadIdx.x == 0 && failed) atomicAdd(&g_attention_wait_failures, 1u);
+}
+
+template <typename T, int D, int BITS>
+int launch_tiles(const AttnArgs& g, int64_t tiles, cudaStream_t st) {
+    static PerDeviceOnce once;
+    auto* kernel = attn_tiles_kernel<T, D, BITS>;
+    const int rc = once.raise_smem_limit(kernel, TileSmem<D>::total);
+    if (rc != MPQ_OK) return rc;
+    kernel<<<dim3((unsigned)tiles, (unsigned)g.kv_heads, (unsigned)g.splits), kTileThreads, TileSmem<D>::total, st>>>(g);
+    return launch_status();
+}
+
+int attention_tiles(const AttnArgs& g, int dtype, int dim, int bits, int64_t tiles, cudaStream_t st) {
+    const bool bf = dtype == MPQ_BF16;
+    if (dim == 128) {
+        if (bits == 8) return bf ? launch_tiles<__nv_bfloat16, 128, 8>(g, tiles, st) : launch_tiles<__half, 128, 8>(g, tiles, st);
+        return bf ? launch_tiles<__nv_bfloat16, 128, 4>(g, tiles, st) : launch_tiles<__half, 128, 4>(g, tiles, st);
+    }
+    if (bits == 8) return bf ? launch_tiles<__nv_bfloat16, 64, 8>(g, tiles, st) : launch_tiles<__half, 64, 8>(g, tiles, st);
+    return bf ? launch_tiles<__nv_bfloat16, 64, 4>(g, tiles, st) : launch_tiles<__half, 64, 4>(g, tiles, st);
+}
+
+int attention_wait_failures(unsigned int* count_host, cudaStream_t st) {
+    return cudaMemcpyFromSymbolAsync(count_host, g_attention_wait_failures, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, st) == cudaSuccess &&
+                   cudaStreamSynchronize(st) == cudaSuccess ? MPQ_OK : MPQ_ERR_CUDA;
+}
+
+}  // namespace mpq

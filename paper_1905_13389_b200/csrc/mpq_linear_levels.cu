@@ -4,7 +4,7 @@
 //   sum q_a q_w = 4 sum u_a u_w - 2 L_w sum u_a - 2 L_a sum u_w + k L_a L_w,
 // so the inner loop multiplies unsigned bytes and the level sums that lie beside the operands do the rest.
 // The result fits int32 (checked on the host), hence the terms may be combined modulo 2^32.
-#include "mpq_levels.cuh"
+#include "mpq_attention.cuh"
 #include "mpq_tensor.cuh"
 
 namespace mpq {
@@ -516,7 +516,11 @@ extern "C" int mpq_linear_levels(const uint8_t* a, const float* a_scale, const i
 
 extern "C" int mpq_wait_failures(unsigned int* count_host, void* stream) {
     if (!count_host) return MPQ_ERR_NULL;
-    if (cudaMemcpyFromSymbolAsync(count_host, g_wait_failures, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess ||
-        cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
+    unsigned int attention = 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (attention_wait_failures(&attention, st) != MPQ_OK ||
+        cudaMemcpyFromSymbolAsync(count_host, g_wait_failures, sizeof(unsigned int), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
+    *count_host += attention;
     return MPQ_OK;
 }
