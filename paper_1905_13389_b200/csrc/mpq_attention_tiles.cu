@@ -125,7 +125,7 @@ attn_tiles_kernel(const AttnArgs g) {
 
     if (warp < 8) {
         // ================= softmax: one thread per query row
-        regs_up<192>();
+        regs_up<184>();
         const int h = warp >> 2;
         if (h < tiles) {
             const int in_tile = threadIdx.x & 127, r = t.row0 + h * 128 + in_tile;
@@ -332,15 +332,21 @@ attn_tiles_kernel(const AttnArgs g) {
         // values: eight tokens and an eighth of the dims per thread; neighbouring lanes take neighbouring token groups
         constexpr int kValBytes = kRowBytes / 8, kDims = D / 8;
         const int group8 = th & 15, eighth = th >> 4;
-        auto rows_of_step = [&](int i, float& ks, float& vs) {           // this thread's token of step i
+        // Everything is loaded a step before it is needed: the page numbers two steps ahead, then the ranges, keys
+        // and values of the next step while this one is converted.  row_of holds the rows of two steps; the barrier
+        // at the end of step i publishes those of step i + 2 (over those of step i, whose loads are all issued).
+        auto find_row = [&](int i) {                                     // this thread's token of step i
             const int j = begin + i * kStepTokens + th;
-            const uint32_t row = j < end ? context_row(g, pages_of, j, kv_head) : 0xffffffffu;
+            return j < end ? context_row(g, pages_of, j, kv_head) : 0xffffffffu;
+        };
+        auto publish = [&](int i, uint32_t row, float& ks, float& vs) {
             row_of[(i & 1) * kStepTokens + th] = row == 0xffffffffu ? 0u : row;       // a row that can be read; weight 0
-            ks = row == 0xffffffffu ? -1.0f : __ldg(g.k_scale + row);
-            vs = row == 0xffffffffu ? 0.0f : __ldg(g.v_scale + row);
-            return row != 0xffffffffu;
+            ks = 0.0f;
+            vs = -1.0f;                                                  // no token
+            if (row != 0xffffffffu) { ks = __ldg(g.k_scale + row); vs = __ldg(g.v_scale + row); }
         };
         uint4 kw[kKeyLoads];
+        uint32_t vw[8][kValBytes / 4];
         auto load_keys = [&](int i) {
 #pragma unroll
             for (int x = 0; x < kKeyLoads; ++x) {
@@ -348,61 +354,68 @@ attn_tiles_kernel(const AttnArgs g) {
                 kw[x] = __ldg(reinterpret_cast<const uint4*>(g.k_levels + (uint64_t)row * kRowBytes + key_part * 16));
             }
         };
-        float ks = 0.0f, vs = 0.0f, next_ks = 0.0f, next_vs = 0.0f;
-        bool here = false, next_here = false;
-        if (steps > 0) here = rows_of_step(0, ks, vs);
-        asm volatile("bar.sync 2, 128;" ::: "memory");
-        if (steps > 0) load_keys(0);
-        for (int i = 0; i < steps; ++i) {
-            const int st = i & 1;
-            // values of this step into registers, rows of the next one
-            uint32_t vw[8][kValBytes / 4];
+        auto load_values = [&](int i) {
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-                const uint32_t row = row_of[st * kStepTokens + group8 * 8 + x];
+                const uint32_t row = row_of[(i & 1) * kStepTokens + group8 * 8 + x];
                 const uint8_t* p = g.v_levels + (uint64_t)row * kRowBytes + eighth * kValBytes;
                 if constexpr (kValBytes == 16) { const uint4 r = __ldg(reinterpret_cast<const uint4*>(p)); vw[x][0] = r.x; vw[x][1] = r.y; vw[x][2] = r.z; vw[x][3] = r.w; }
                 else if constexpr (kValBytes == 8) { const uint2 r = __ldg(reinterpret_cast<const uint2*>(p)); vw[x][0] = r.x; vw[x][1] = r.y; }
                 else vw[x][0] = __ldg(reinterpret_cast<const uint32_t*>(p));
             }
-            if (i + 1 < steps) next_here = rows_of_step(i + 1, next_ks, next_vs);
+        };
+        float ks, vs, next_ks, next_vs;
+        {
+            const uint32_t r0 = find_row(0), r1 = find_row(1);
+            publish(0, r0, ks, vs);
+            publish(1, r1, next_ks, next_vs);
+        }
+        asm volatile("bar.sync 2, 128;" ::: "memory");
+        load_keys(0);
+        load_values(0);
+        asm volatile("bar.sync 2, 128;" ::: "memory");
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i) {
+            const int st = i & 1;
+            const uint32_t row2 = find_row(i + 2);
             bool ok = true;
             if (i >= 2) ok = mbar_wait_or(k_empty(st), ((i >> 1) - 1) & 1, &failed) && mbar_wait_or(c_empty(st), ((i >> 1) - 1) & 1, &failed);
             ok = __all_sync(0xffffffffu, ok && !has_failed());
-            if (ok) {
+            if (ok) {                                                    // after a failure only the barriers are kept up
                 float* consts = reinterpret_cast<float*>(base_ptr + Smem::consts + st * Smem::const_stage);
                 float lg, inv;
                 range_exponent(vs, lg, inv);
-                consts[th] = here ? ks * (1.0f / (float)((1 << BITS) - 1)) : 0.0f;
-                consts[kStepTokens + th] = here ? lg : -INFINITY;        // a token that is not there: weight 0
+                const bool here = vs != -1.0f;
+                consts[th] = ks * (1.0f / (float)((1 << BITS) - 1));
+                consts[kStepTokens + th] = here ? lg : -INFINITY;            // a token that is not there: weight 0
                 consts[2 * kStepTokens + th] = here ? inv : 0.0f;
-                const uint32_t tile = base + Smem::k + st * Smem::k_stage;
+                {
+                    const uint32_t tile = base + Smem::k + st * Smem::k_stage;
 #pragma unroll
-                for (int x = 0; x < kKeyLoads; ++x) {
-                    const int r = key_row + x * (128 / kKeyLanes);
-                    const uint32_t w[4] = {kw[x].x, kw[x].y, kw[x].z, kw[x].w};
-                    if constexpr (BITS == 8) {
-                        // the two 8-element chunks; lanes of the two halves of a row start with different ones (banks)
+                    for (int x = 0; x < kKeyLoads; ++x) {
+                        const int r = key_row + x * (128 / kKeyLanes);
+                        const uint32_t w[4] = {kw[x].x, kw[x].y, kw[x].z, kw[x].w};
+                        if constexpr (BITS == 8) {
+                            // the two 8-element chunks; lanes of the two halves of a row start with different ones (banks)
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const int z = (key_part * 2 >= 8) ^ y, c = key_part * 2 + z;
-                            key_chunk8(z ? w[2] : w[0], z ? w[3] : w[1], tile + (c >> 3) * 16384 + swizzled(r, c & 7));
-                        }
-                    } else {
+                            for (int y = 0; y < 2; ++y) {
+                                const int z = (key_part * 2 >= 8) ^ y, c = key_part * 2 + z;
+                                key_chunk8(z ? w[2] : w[0], z ? w[3] : w[1], tile + (c >> 3) * 16384 + swizzled(r, c & 7));
+                            }
+                        } else {
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const int c = key_part * 4 + y;
-                            key_chunk4(w[y], tile + (c >> 3) * 16384 + swizzled(r, c & 7));
+                            for (int y = 0; y < 4; ++y) {
+                                const int c = key_part * 4 + y;
+                                key_chunk4(w[y], tile + (c >> 3) * 16384 + swizzled(r, c & 7));
+                            }
                         }
                     }
                 }
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(k_full(st));
+                load_keys(i + 1);
             }
-            asm volatile("bar.sync 2, 128;" ::: "memory");               // rows of the next step are there
-            if (i + 1 < steps) load_keys(i + 1);
-            ok = true;
             if (i >= 2) ok = mbar_wait_or(v_empty(st), ((i >> 1) - 1) & 1, &failed);
             ok = __all_sync(0xffffffffu, ok && !has_failed());
             if (ok) {
@@ -425,21 +438,25 @@ attn_tiles_kernel(const AttnArgs g) {
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(v_full(st));
+                load_values(i + 1);
             }
-            ks = next_ks; vs = next_vs; here = next_here;
+            ks = next_ks; vs = next_vs;
+            // every warp has issued its loads of step i + 1 when it comes here, none still reads rows of step i
+            publish(i + 2, row2, next_ks, next_vs);
+            asm volatile("bar.sync 2, 128;" ::: "memory");
         }
     } else {
         // ================= tensor-core issue
-        regs_down<24>();
+        regs_down<40>();
         if (warp == 12 && lane == 0) {
             constexpr uint32_t idesc_s = umma_idesc_f16(128, kStepTokens), idesc_o = umma_idesc_f16(128, D);
             bool ok = mbar_wait_or(q_ready, 0, &failed);
             auto scores = [&](int h, int st) {
-                const uint64_t a = umma_desc(base + Smem::q + h * Smem::q_tile), b = umma_desc(base + Smem::k + st * Smem::k_stage);
+                const uint32_t a = umma_desc_low(base + Smem::q + h * Smem::q_tile), b = umma_desc_low(base + Smem::k + st * Smem::k_stage);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)                         // 16 elements = 32 bytes; 64 elements per half
-                    umma_f16_ss(tmem + kTmemS + h * 128, a + (uint64_t)((k >> 2) * (16384 >> 4) + (k & 3) * 2),
-                                b + (uint64_t)((k >> 2) * (16384 >> 4) + (k & 3) * 2), idesc_s, k > 0);
+                    umma_f16_ss(tmem + kTmemS + h * 128, a + (uint32_t)((k >> 2) * (16384 >> 4) + (k & 3) * 2),
+                                b + (uint32_t)((k >> 2) * (16384 >> 4) + (k & 3) * 2), idesc_s, k > 0);
                 umma_commit<1>(s_full(h));
             };
             if (ok && steps > 0) {
@@ -458,11 +475,11 @@ attn_tiles_kernel(const AttnArgs g) {
                     ok = mbar_wait_or(p_ready(h), i & 1, &failed);
                     if (!ok || has_failed()) { ok = false; break; }
                     tmem_fence_after();
-                    const uint64_t b = umma_desc(base + Smem::v + st * Smem::v_stage);
+                    const uint32_t b = umma_desc_low(base + Smem::v + st * Smem::v_stage);
 #pragma unroll
                     for (int k = 0; k < kStepTokens / 16; ++k)
                         umma_f16_ts(tmem + kTmemO + h * 128, tmem + kTmemS + h * 128 + k * 8,
-                                    b + (uint64_t)((k >> 2) * ((D * 128) >> 4) + (k & 3) * 2), idesc_o, i > 0 || k > 0);
+                                    b + (uint32_t)((k >> 2) * ((D * 128) >> 4) + (k & 3) * 2), idesc_o, i > 0 || k > 0);
                     if (h == tiles - 1) umma_commit<1>(v_empty(st));
                     if (i + 1 < steps) {
                         scores(h, nx);
