@@ -233,8 +233,7 @@ attn_rows_kernel(const AttnArgs g) {
                 for (int e = 0; e < 2; ++e) {
                     const float y = s[nt][half * 2 + e];
                     w[e] = fast_exp2(y - ref[half]);
-                    // a token that is not seen may have any range: its reciprocal must not meet the 0
-                    l[half] = whole || y != -INFINITY ? fmaf(w[e], ivs[nt][e], l[half]) : l[half];
+                    l[half] = fmaf(w[e], ivs[nt][e], l[half]);
                 }
                 const __half2 h = __floats2half2_rn(w[0], w[1]);
                 wsum[half] += __low2float(h) + __high2float(h);

@@ -124,10 +124,11 @@ __device__ __forceinline__ float fast_exp2(float x) {
 }
 
 // log2 of a value's range and the reciprocal that belongs to it (2^-that, so that rounding the logarithm
-// cancels in the denominator).
+// cancels in the denominator).  The reciprocal is always finite (a NaN range gives 0): a masked token's weight
+// of 0 may be multiplied by it; a row that does see such a token gets its NaN from the exponent.
 __device__ __forceinline__ void range_exponent(float s, float& lg, float& inv) {
     lg = __log2f(s < kTinyRange ? kTinyRange : s);           // NaN passes through
-    inv = exp2f(-lg);                                       // may be subnormal
+    inv = lg == lg ? exp2f(-lg) : 0.0f;                      // may be subnormal
 }
 
 __device__ __forceinline__ float final_value(float o) { return fabsf(o) < 2.0f * kTinyRange ? 0.0f : o; }

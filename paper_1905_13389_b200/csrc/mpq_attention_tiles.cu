@@ -32,9 +32,10 @@ template <int D> struct TileSmem {
     static constexpr int k_stage = 128 * 128 * (D / 64);  // [D / 64][128 tokens][64 dims]
     static constexpr int v_stage = D * 128 * 2;           // [2][D dims][64 tokens]
     static constexpr int q = 0, k = 2 * q_tile, v = k + 2 * k_stage, consts = v + 2 * v_stage;
-    static constexpr int const_stage = 3 * kStepTokens * 4;   // key factor, value exponent, value reciprocal
+    static constexpr int const_stage = 3 * kStepTokens * 4;   // [64 token pairs](key factors, value exponents), [128] value reciprocals
     static constexpr int rows = consts + 2 * const_stage;     // cache row numbers, two steps
-    static constexpr int total = rows + 2 * kStepTokens * 4 + 1024;
+    static constexpr int ranges = rows + 2 * kStepTokens * 4; // first and last visible token of each row
+    static constexpr int total = ranges + kTileRows * 8 + 1024;
 };
 
 template <int REGS> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
@@ -68,27 +69,56 @@ __device__ __forceinline__ void key_chunk4(uint32_t w, uint32_t addr) {
 // 16-byte chunk `c` of row r in a [rows][128 bytes] tile with the 128-byte swizzle
 __device__ __forceinline__ uint32_t swizzled(int r, int c) { return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4)); }
 
+// Two fp32 operations in one instruction (sm_100's f32x2 forms).
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(kTileThreads, 1)
 attn_tiles_kernel(const AttnArgs g) {
     using Smem = TileSmem<D>;
     constexpr int kRowBytes = D * BITS / 8;
-    constexpr uint32_t kTmemS = 0, kTmemO = 256;          // S_0, S_1: 128 columns each; O_0, O_1: D columns each, 128 apart
+    constexpr uint32_t kTmemS = 0, kTmemO = 256;          // S_0, S_1: two half steps of 64 columns each; O_0, O_1: D columns each, 128 apart
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[16];
+    __shared__ __align__(8) uint64_t bars[22];
     __shared__ uint32_t tmem_holder;
     __shared__ int failed;
     const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
     unsigned char* base_ptr = smem_raw + (base - smem_addr(smem_raw));
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t q_ready = smem_addr(&bars[0]), o_full = smem_addr(&bars[1]);
     auto k_full = [&](int s) { return smem_addr(&bars[2 + s]); };
     auto k_empty = [&](int s) { return smem_addr(&bars[4 + s]); };
     auto v_full = [&](int s) { return smem_addr(&bars[6 + s]); };
     auto v_empty = [&](int s) { return smem_addr(&bars[8 + s]); };
     auto c_empty = [&](int s) { return smem_addr(&bars[10 + s]); };      // constants of a step: read by the softmax warps
-    auto s_full = [&](int h) { return smem_addr(&bars[12 + h]); };
-    auto p_ready = [&](int h) { return smem_addr(&bars[14 + h]); };
+    auto s_full = [&](int h, int half) { return smem_addr(&bars[12 + 2 * h + half]); };
+    auto p_ready = [&](int h, int half) { return smem_addr(&bars[16 + 2 * h + half]); };
+    auto o_done = [&](int h) { return smem_addr(&bars[20 + h]); };       // W V of a half step is in O
     auto has_failed = [&]() { return *(volatile int*)&failed != 0; };
 
     chain_entry();
@@ -112,7 +142,8 @@ attn_tiles_kernel(const AttnArgs g) {
             mbar_init(k_full(s), 4); mbar_init(k_empty(s), 1);
             mbar_init(v_full(s), 4); mbar_init(v_empty(s), 1);
             mbar_init(c_empty(s), 4 * tiles);
-            mbar_init(s_full(s), 1); mbar_init(p_ready(s), 4);
+            for (int half = 0; half < 2; ++half) { mbar_init(s_full(s, half), 1); mbar_init(p_ready(s, half), 4); }
+            mbar_init(o_done(s), 1);
         }
         failed = 0;
         mbar_init_fence();
@@ -125,14 +156,14 @@ attn_tiles_kernel(const AttnArgs g) {
 
     if (warp < 8) {
         // ================= softmax: one thread per query row
-        regs_up<184>();
+        regs_up<176>();
         const int h = warp >> 2;
         if (h < tiles) {
             const int in_tile = threadIdx.x & 127, r = t.row0 + h * 128 + in_tile;
             const bool live = r < t.rows;
             const int token = live ? r / g.group : t.n_q - 1, head = kv_head * g.group + (live ? r % g.group : 0);
             float row_scale;
-            int first, last;
+            int my_first, my_last;
             {
                 // the row as fp16, scaled by a power of two
                 const T* q = static_cast<const T*>(g.q) + (int64_t)(t.q0 + token) * g.q_ts + (int64_t)head * g.q_hs;
@@ -172,116 +203,170 @@ attn_tiles_kernel(const AttnArgs g) {
                     }
                     st_shared16(tile + (c >> 3) * Smem::q_half + swizzled(in_tile, c & 7), w[0], w[1], w[2], w[3]);
                 }
-                row_range(g, t, token, first, last);
-                if (!live) { first = 0; last = 0x7fffffff; }             // computed with q = 0, never stored
+                row_range(g, t, token, my_first, my_last);
+                if (!live) { my_first = 0; my_last = 0x7fffffff; }             // computed with q = 0, never stored
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_ready);
             }
+            // In the loop a thread holds a quarter of the columns of four rows (the matrix-fragment shape), so a token's
+            // constants serve four rows: they come from shared memory at 128 bytes a cycle, and with one row per thread
+            // they alone took 3072 cycles a step.  Row k of the thread is row (lane / 4) + 8 k of the warp's 32.
             const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
             const uint32_t ts = lanes + kTmemS + h * 128, to = lanes + kTmemO + h * 128;
-            float top = -INFINITY, ref = 0.0f, l0 = 0.0f, l1 = 0.0f;     // ref: what is subtracted, top - kTileBoost when it was set
-            float set = -INFINITY;                                       // the maximum that ref belongs to
+            float set[4];                                 // the maximum that the weights' reference belongs to
+            uint64_t rs[4], l[4];                         // the row's scale, twice; two partial sums
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float x = __shfl_sync(0xffffffffu, row_scale, (lane >> 2) + 8 * k);
+                rs[k] = pack2(x, x);
+                set[k] = -INFINITY;
+                l[k] = 0;
+            }
+            const int first_of_all = __reduce_max_sync(0xffffffffu, my_first), last_of_all = __reduce_min_sync(0xffffffffu, my_last);
+            int2* ranges = reinterpret_cast<int2*>(base_ptr + Smem::ranges) + warp * 32;      // this warp's rows
+            ranges[lane] = make_int2(my_first, my_last);
+            __syncwarp();
             bool ok = true;
-            for (int i = 0; i < steps; ++i) {
-                const int st = i & 1, j0 = begin + i * kStepTokens;
-                // the constants were written before the keys that S is made of
-                ok = mbar_wait_or(s_full(h), i & 1, &failed) && mbar_wait_or(k_full(st), (i >> 1) & 1, &failed);
-                ok = __all_sync(0xffffffffu, ok && !has_failed());
-                if (!ok) break;
-                tmem_fence_after();
-                uint32_t v[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_load32(ts + c * 32, v[c]);
-                tmem_wait_ld();
-                const float4* kf = reinterpret_cast<const float4*>(base_ptr + Smem::consts + st * Smem::const_stage);
-                const float4* lf = kf + kStepTokens / 4;
-                const float4* inv = lf + kStepTokens / 4;
-                const bool whole = __all_sync(0xffffffffu, j0 >= first && j0 + kStepTokens - 1 <= last);
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float4 k4 = kf[c * 8 + e], l4 = lf[c * 8 + e];
-                        const float ks[4] = {k4.x, k4.y, k4.z, k4.w}, ls[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const float y = fmaf(__uint_as_float(v[c][e * 4 + x]) * ks[x], row_scale, ls[x]);
-                            v[c][e * 4 + x] = __float_as_uint(y);
-                        }
-                    }
-                if (!whole) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const int j = j0 + c * 32 + e;
-                            if (j < first || j > last) v[c][e] = 0xff800000u;        // -infinity
-                        }
-                }
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(v[c][e]));
-                top = fmaxf(top, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
-                const bool grow = top > set + kLag;                                   // also the first finite maximum
-                if (__any_sync(0xffffffffu, grow)) {
-                    const float f = grow ? fast_exp2(set - top) : 1.0f;               // set = -infinity: 0
-                    if (grow) { set = top; ref = top - kTileBoost; l0 *= f; l1 *= f; }
-                    if (i > 0) {
 #pragma unroll 1
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t o[32];
-                            tmem_load32(to + c * 32, o);
-                            tmem_wait_ld();
+            for (int i = 0; i < 2 * steps; ++i) {         // half steps of 64 tokens
+                const int half = i & 1, st = (i >> 1) & 1, j0 = begin + i * 64;
+                ok = mbar_wait_or(s_full(h, half), (i >> 1) & 1, &failed);
+                // the constants were written before the keys that S is made of
+                if (half == 0) ok = ok && mbar_wait_or(k_full(st), (i >> 2) & 1, &failed);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                tmem_fence_after();
+                const uint32_t from_s = ts + half * 64;
+                const float4* consts = reinterpret_cast<const float4*>(base_ptr + Smem::consts + st * Smem::const_stage) + half * 32 + (lane & 3);
+                const float2* inv = reinterpret_cast<const float2*>(base_ptr + Smem::consts + st * Smem::const_stage + 2 * kStepTokens * 4) + half * 32 + (lane & 3);
+                uint32_t p[2][16];                        // weights: [16-row half]
+                uint64_t ls[4];
+                // The weights are made with the reference of the half step before, in one pass over S; only when a row's
+                // maximum has outgrown it (always in the first one, rarely later) is the pass repeated with a new one.
+                while (true) {
+                    uint64_t less[4];                     // minus the reference: set - kTileBoost, 0 while nothing was seen
+                    float top[4];
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            tmem_store32(to + c * 32, o);
-                        }
-                        tmem_wait_st();
+                    for (int k = 0; k < 4; ++k) {
+                        const float x = set[k] == -INFINITY ? 0.0f : kTileBoost - set[k];
+                        less[k] = pack2(x, x);
+                        top[k] = -INFINITY;
+                        ls[k] = 0;
                     }
-                }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t p[16];
+                    uint32_t v[2][32];
+                    tmem_load_frag(from_s, v[0]);
+                    tmem_load_frag(from_s + (16u << 16), v[1]);
+                    tmem_wait_ld();
+                    uint64_t y[8][4];                     // [8-column group][row]: two neighbouring tokens each
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float4 i4 = inv[c * 8 + e];
-                        const float is[4] = {i4.x, i4.y, i4.z, i4.w};
-                        float w[4];
+                        const float4 kl = consts[e * 4];
+                        const uint64_t kf = pack2(kl.x, kl.y), lg = pack2(kl.z, kl.w);
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) w[x] = fast_exp2(__uint_as_float(v[c][e * 4 + x]) - ref);
-                        if (whole) {
-                            l0 = fmaf(w[0], is[0], l0); l1 = fmaf(w[1], is[1], l1);
-                            l0 = fmaf(w[2], is[2], l0); l1 = fmaf(w[3], is[3], l1);
-                        } else {
-                            // a token that is not seen may have any range: its reciprocal must not meet the 0
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)
-                                if (v[c][e * 4 + x] != 0xff800000u) l0 = fmaf(w[x], is[x], l0);
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t* sc = &v[k >> 1][e * 4 + (k & 1) * 2];
+                            y[e][k] = fma2(mul2(pack2(__uint_as_float(sc[0]), __uint_as_float(sc[1])), kf), rs[k], lg);
                         }
-                        const __half2 a = __floats2half2_rn(w[0], w[1]), b = __floats2half2_rn(w[2], w[3]);
-                        p[e * 2] = *reinterpret_cast<const uint32_t*>(&a);
-                        p[e * 2 + 1] = *reinterpret_cast<const uint32_t*>(&b);
                     }
-                    tmem_store16(ts + c * 16, p);
+                    if (j0 < first_of_all || j0 + 63 > last_of_all) {                 // some row of the warp sees only a part
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int2 seen = ranges[(lane >> 2) + 8 * k];
+                            const int at = j0 + 2 * (lane & 3), from = seen.x - at, upto = seen.y - at;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                float u, w;
+                                unpack2(y[e][k], u, w);
+                                y[e][k] = pack2(e * 8 < from || e * 8 > upto ? -INFINITY : u, e * 8 + 1 < from || e * 8 + 1 > upto ? -INFINITY : w);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 i2 = inv[e * 4];
+                        const uint64_t iv = pack2(i2.x, i2.y);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            float w0, w1;
+                            unpack2(y[e][k], w0, w1);
+                            top[k] = max3(top[k], w0, w1);
+                            unpack2(add2(y[e][k], less[k]), w0, w1);
+                            w0 = fast_exp2(w0);
+                            w1 = fast_exp2(w1);
+                            ls[k] = fma2(pack2(w0, w1), iv, ls[k]);
+                            const __half2 w = __floats2half2_rn(w0, w1);
+                            p[k >> 1][e * 2 + (k & 1)] = *reinterpret_cast<const uint32_t*>(&w);
+                        }
+                    }
+                    // a thread's own quarter of the columns decides whether to look at the others': nearly always it does not
+                    bool grow = false;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) grow = grow || top[k] > set[k] + kLag;
+                    if (!__any_sync(0xffffffffu, grow)) break;
+                    float f[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
+                        top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
+                        f[k] = 1.0f;
+                        if (top[k] > set[k] + kLag) {
+                            f[k] = fast_exp2(set[k] - top[k]);                        // set = -infinity: 0
+                            set[k] = top[k];
+                            l[k] = mul2(l[k], pack2(f[k], f[k]));
+                        }
+                    }
+                    if (i > 0) {
+                        ok = mbar_wait_or(o_done(h), (i - 1) & 1, &failed);           // O is complete up to the half step before
+                        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                        tmem_fence_after();
+#pragma unroll
+                        for (int a = 0; a < 2; ++a)
+#pragma unroll 1
+                            for (int c = 0; c < D / 64; ++c) {
+                                uint32_t o[32];
+                                tmem_load_frag(to + ((uint32_t)(16 * a) << 16) + c * 64, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f[a * 2 + ((e >> 1) & 1)]);
+                                tmem_store_frag(to + ((uint32_t)(16 * a) << 16) + c * 64, o);
+                            }
+                    }
                 }
+                if (!ok) break;
+                tmem_store_frag_half(from_s, p[0]);
+                tmem_store_frag_half(from_s + (16u << 16), p[1]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) l[k] = add2(l[k], ls[k]);
                 tmem_wait_st();
                 tmem_fence_before();
                 __syncwarp();
-                if (lane == 0) { mbar_arrive(p_ready(h)); mbar_arrive(c_empty(st)); }
+                if (lane == 0) {
+                    mbar_arrive(p_ready(h, half));
+                    if (half) mbar_arrive(c_empty(st));
+                }
             }
             // ---- result
             ok = mbar_wait_or(o_full, 0, &failed);
             ok = __all_sync(0xffffffffu, ok && !has_failed());
             if (ok) {
                 tmem_fence_after();
-                const float l = l0 + l1;
-                const bool empty = set == -INFINITY;
+                // back to one row per thread
+                float l_row = 0.0f, set_row = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float sum, odd;
+                    unpack2(l[k], sum, odd);
+                    sum += odd;
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                    const int from = (lane & 7) * 4;
+                    const float a = __shfl_sync(0xffffffffu, sum, from), b = __shfl_sync(0xffffffffu, set[k], from);
+                    if ((lane >> 3) == k) { l_row = a; set_row = b; }
+                }
+                const bool empty = set_row == -INFINITY;
                 constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);
                 const int64_t at = (int64_t)(t.q0 + token) * g.heads + head;
-                const float den = used > 1 ? kInvL : __fdiv_rn(kInvL, l);
+                const float den = used > 1 ? kInvL : __fdiv_rn(kInvL, l_row);
                 T* out = static_cast<T*>(g.out) + (int64_t)(t.q0 + token) * g.o_ts + (int64_t)head * g.o_hs;
                 const int64_t slot = at * g.splits + blockIdx.z;
                 const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
@@ -314,15 +399,15 @@ attn_tiles_kernel(const AttnArgs g) {
                 }
                 if (live) {
                     // the merge counts in units of 2^kBoost above the maximum it is told
-                    if (used > 1) g.part_ml[slot] = make_float2(empty ? -INFINITY : ref + kBoost, l);
-                    else if (g.lse) g.lse[at] = empty ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+                    if (used > 1) g.part_ml[slot] = make_float2(empty ? -INFINITY : set_row - kTileBoost + kBoost, l_row);
+                    else if (g.lse) g.lse[at] = empty ? -INFINITY : (set_row - kTileBoost + log2f(l_row)) * 0.6931471805599453f;
                 }
                 tmem_fence_before();
             }
         }
     } else if (warp < 12) {
         // ================= levels: bytes of the cache -> fp16 operands
-        regs_down<104>();
+        regs_down<120>();
         const int th = threadIdx.x - 256;
         const int32_t* pages_of = g.table + (int64_t)t.b * g.table_stride;
         uint32_t* row_of = reinterpret_cast<uint32_t*>(base_ptr + Smem::rows);
@@ -386,8 +471,8 @@ attn_tiles_kernel(const AttnArgs g) {
                 float lg, inv;
                 range_exponent(vs, lg, inv);
                 const bool here = vs != -1.0f;
-                consts[th] = ks * (1.0f / (float)((1 << BITS) - 1));
-                consts[kStepTokens + th] = here ? lg : -INFINITY;            // a token that is not there: weight 0
+                consts[(th >> 1) * 4 + (th & 1)] = ks * (1.0f / (float)((1 << BITS) - 1));
+                consts[(th >> 1) * 4 + 2 + (th & 1)] = here ? lg : -INFINITY;    // a token that is not there: weight 0
                 consts[2 * kStepTokens + th] = here ? inv : 0.0f;
                 {
                     const uint32_t tile = base + Smem::k + st * Smem::k_stage;
@@ -448,47 +533,64 @@ attn_tiles_kernel(const AttnArgs g) {
     } else {
         // ================= tensor-core issue
         regs_down<40>();
-        if (warp == 12 && lane == 0) {
-            constexpr uint32_t idesc_s = umma_idesc_f16(128, kStepTokens), idesc_o = umma_idesc_f16(128, D);
-            bool ok = mbar_wait_or(q_ready, 0, &failed);
-            auto scores = [&](int h, int st) {
-                const uint32_t a = umma_desc_low(base + Smem::q + h * Smem::q_tile), b = umma_desc_low(base + Smem::k + st * Smem::k_stage);
+        if (warp == 12) {
+            constexpr uint32_t idesc_s = umma_idesc_f16(128, 64), idesc_o = umma_idesc_f16(128, D);
+            const uint32_t acc = __shfl_sync(0xffffffffu, tmem, 0);
+            const bool leader = elect_one();
+            bool ok = mbar_wait_warp(q_ready, 0, &failed);
+            // scores of half step i (64 tokens) of tile h; the keys of a step lie in one stage
+            auto scores = [&](int h, int i) {
+                const int half = i & 1, st = (i >> 1) & 1;
+                const uint32_t a = umma_desc_low(base + Smem::q + h * Smem::q_tile);
+                const uint32_t b = umma_desc_low(base + Smem::k + st * Smem::k_stage + half * (64 * 128));
+                const uint32_t d = acc + kTmemS + h * 128 + half * 64;
+                if (leader) {
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k)                         // 16 elements = 32 bytes; 64 elements per half
-                    umma_f16_ss(tmem + kTmemS + h * 128, a + (uint32_t)((k >> 2) * (16384 >> 4) + (k & 3) * 2),
-                                b + (uint32_t)((k >> 2) * (16384 >> 4) + (k & 3) * 2), idesc_s, k > 0);
-                umma_commit<1>(s_full(h));
+                    for (int k = 0; k < D / 16; ++k) {                   // 16 elements = 32 bytes, 64 elements per part
+                        const uint32_t at = (uint32_t)((k >> 2) * (16384 >> 4) + (k & 3) * 2);
+                        umma_f16_ss(d, a + at, b + at, idesc_s, k > 0);
+                    }
+                    umma_commit<1>(s_full(h, half));
+                }
             };
+            const int halves = 2 * steps;
             if (ok && steps > 0) {
-                ok = mbar_wait_or(k_full(0), 0, &failed);
+                ok = mbar_wait_warp(k_full(0), 0, &failed);
                 tmem_fence_after();
                 if (ok) {
-                    for (int h = 0; h < tiles; ++h) scores(h, 0);
-                    umma_commit<1>(k_empty(0));
+                    for (int half = 0; half < 2; ++half)
+                        for (int h = 0; h < tiles; ++h) scores(h, half);
+                    if (leader) umma_commit<1>(k_empty(0));
                 }
             }
-            for (int i = 0; i < steps && ok && !has_failed(); ++i) {
-                const int st = i & 1, nx = st ^ 1;
-                ok = mbar_wait_or(v_full(st), (i >> 1) & 1, &failed);
-                if (ok && i + 1 < steps) ok = mbar_wait_or(k_full(nx), ((i + 1) >> 1) & 1, &failed);
+#pragma unroll 1
+            for (int i = 0; i < halves && ok; ++i) {
+                const int half = i & 1, st = (i >> 1) & 1;
+                if (half == 0) {
+                    ok = mbar_wait_warp(v_full(st), (i >> 2) & 1, &failed);
+                    if (ok && i + 2 < halves) ok = mbar_wait_warp(k_full(st ^ 1), ((i + 2) >> 2) & 1, &failed);
+                }
+#pragma unroll 1
                 for (int h = 0; h < tiles && ok; ++h) {
-                    ok = mbar_wait_or(p_ready(h), i & 1, &failed);
-                    if (!ok || has_failed()) { ok = false; break; }
+                    ok = mbar_wait_warp(p_ready(h, half), (i >> 1) & 1, &failed);
+                    if (!ok) break;
                     tmem_fence_after();
-                    const uint32_t b = umma_desc_low(base + Smem::v + st * Smem::v_stage);
+                    const uint32_t d = acc + kTmemO + h * 128, w = acc + kTmemS + h * 128 + half * 64;
+                    const uint32_t b = umma_desc_low(base + Smem::v + st * Smem::v_stage + half * (D * 128));
+                    if (leader) {
 #pragma unroll
-                    for (int k = 0; k < kStepTokens / 16; ++k)
-                        umma_f16_ts(tmem + kTmemO + h * 128, tmem + kTmemS + h * 128 + k * 8,
-                                    b + (uint32_t)((k >> 2) * ((D * 128) >> 4) + (k & 3) * 2), idesc_o, i > 0 || k > 0);
-                    if (h == tiles - 1) umma_commit<1>(v_empty(st));
-                    if (i + 1 < steps) {
-                        scores(h, nx);
-                        if (h == tiles - 1) umma_commit<1>(k_empty(nx));
+                        for (int k = 0; k < 4; ++k) umma_f16_ts(d, w + k * 8, b + k * 2, idesc_o, i > 0 || k > 0);
+                        umma_commit<1>(o_done(h));
+                        if (half && h == tiles - 1) umma_commit<1>(v_empty(st));
+                    }
+                    if (i + 2 < halves) {                                // S of this half step is free now
+                        scores(h, i + 2);
+                        if (half && h == tiles - 1 && leader) umma_commit<1>(k_empty(st ^ 1));
                     }
                 }
             }
-            umma_commit<1>(o_full);
-            if (!mbar_wait(o_full, 0)) atomicExch(&failed, 1);
+            if (leader) umma_commit<1>(o_full);
+            mbar_wait_warp(o_full, 0, &failed);
         }
     }
     __syncwarp();
