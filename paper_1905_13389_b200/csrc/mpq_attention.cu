@@ -1,23 +1,30 @@
-// Attention over a paged cache of levels for few query rows (mpq_cache_attention): tiles of 16 rows.
+// Attention over a paged cache of levels for few query rows (mpq_cache_attention): tiles of 8 or 16 rows.
 //
-// A CTA of four warps takes 16 query rows (tokens x heads of one key head) and a stretch of the context;
+// A CTA of four warps takes 8 NQ query rows (tokens x heads of one key head) and a stretch of the context;
 // each warp runs an online softmax of its own over every fourth chunk of 32 tokens and the four are merged
-// at the end.  Level bytes go from global memory straight into the operand registers of
-// mma.sync.m16n8k16: the element order inside a dot product is free, so the 16 bytes that a lane loads ARE
-// its operand fragment, for the keys (lane = token, bytes along dim) and for the values (lane = 16 dims of
-// a token pair).  With 16 rows the work is bound by reading the cache, not by the matrix pipe (which is why
-// the 128-row tcgen05 tile, seven eighths of it empty here, is not used), and nothing is staged in shared
-// memory.  The keys of the next chunk are loaded while the softmax and the value product of this one run.
+// at the end.  The products are transposed, S^T = K Q^T and O^T = V^T W^T with mma.sync.m16n8k16: tokens and
+// dims fill the 16-wide side, eight query rows the other one, so a single token of a few heads wastes little.
+// Level bytes go from global memory straight into the operand registers: the element order inside a dot
+// product is free, so the 16 bytes that a lane loads ARE its operand fragment, for the keys (lane = token,
+// bytes along dim) and for the values (lane = 16 dims of a token pair); only W^T changes hands, by one
+// 8 x 8 register transpose per 8 tokens.  With so few rows the work is bound by reading the cache, not by the
+// matrix pipe (which is why the 128-row tcgen05 tile, mostly empty here, is not used), and nothing is staged
+// in shared memory.  The keys of the next chunk are loaded while the softmax and the value product run.
 #include "mpq_attention.cuh"
 
 namespace mpq {
 
-constexpr int kRows = 16, kChunk = 32, kWarps = 4;
+constexpr int kChunk = 32, kWarps = 4;
 
-__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 // Two 16-bit lanes 1024 + u (u in the low bits, 0x6400 above) -> fp16 2u - (L + 1), exact: the even
 // neighbour below the level 2u - L.  The missing 1 is added back per row (sum of q, sum of w).
@@ -61,19 +68,19 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
     else { w[0] = __ldg(reinterpret_cast<const uint32_t*>(p)); }
 }
 
-template <typename T, int D, int BITS>
-__global__ void __launch_bounds__(kWarps * 32)
+template <typename T, int D, int BITS, int NQ>
+__global__ void __launch_bounds__(kWarps * 32, NQ == 1 ? 3 : 2)
 attn_rows_kernel(const AttnArgs g) {
+    constexpr int kRows = 8 * NQ;
     constexpr int kRowBytes = D * BITS / 8;
     constexpr int kKeyWords = D / 4 * BITS / 32;          // words of a key row per lane (4 lanes share a row)
     constexpr int kKeyLoads = kKeyWords > 4 ? 2 : 1;      // ... in loads of at most 16 bytes
     constexpr int kKeyStep = kKeyWords / kKeyLoads;
     constexpr int kValWords = D / 8 * BITS / 32;          // words of a value row per lane (8 lanes share a row)
     constexpr int kPairs = 16 / BITS;                     // operand registers per word (keys)
-    constexpr int kSteps = D / 16;                        // k-steps of the score product
-    constexpr int kTiles = D / 8;                         // 8-wide output tiles of the value product
+    constexpr int kSteps = D / 16;                        // k-steps of the score product, 16-dim tiles of the value product
     __shared__ float sh_ml[kWarps][kRows][2];
-    __shared__ float sh_o[kWarps][kRows][D / 2 + 4];      // half of the dims at a time
+    __shared__ __align__(16) float sh_o[kWarps][kRows][D + 4];
 
     chain_entry();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -88,13 +95,40 @@ attn_rows_kernel(const AttnArgs g) {
     split_range(g, t, blockIdx.z, used, begin, end);
     const int32_t* pages_of = g.table + (int64_t)t.b * g.table_stride;
 
-    // ---- queries: rows gr and gr + 8 as operand fragments
-    uint32_t qf[kSteps][4];
-    float row_scale[2], qsum[2];
-    int first[2], last[2];
+    // ---- context: this warp's chunks
+    // lane's token of a chunk: row number in the cache and the token's ranges (-1: there is no token)
+    auto chunk_rows = [&](int c0, uint32_t& row, float& ks, float& vs) {
+        const int j = c0 + lane;
+        row = j < end ? context_row(g, pages_of, j, kv_head) : 0xffffffffu;
+        ks = 0.0f; vs = -1.0f;
+        if (row != 0xffffffffu) { ks = __ldg(g.k_scale + row); vs = __ldg(g.v_scale + row); }
+        else row = 0u;                                    // a row that can be read; weight 0
+    };
+    uint32_t kw[4][kKeyWords];                            // tokens 8 n + gr of the chunk
+    auto load_keys = [&](uint32_t row) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int r = t.row0 + gr + 8 * half;
+        for (int n = 0; n < 4; ++n) {
+            const uint32_t r = __shfl_sync(0xffffffffu, row, n * 8 + gr);
+            const uint8_t* p = g.k_levels + (uint64_t)r * kRowBytes + t4 * (kKeyStep * 4);
+#pragma unroll
+            for (int i = 0; i < kKeyLoads; ++i) load_words<kKeyStep>(p + i * (kRowBytes / 2), kw[n] + i * kKeyStep);
+        }
+    };
+    uint32_t row = 0u, next_row = 0u;
+    float ks = 0.0f, vs = -1.0f, next_ks = 0.0f, next_vs = -1.0f;
+    int c0 = begin + warp * kChunk;
+    if (c0 < end) {
+        chunk_rows(c0, row, ks, vs);
+        load_keys(row);
+    }
+
+    // ---- queries: row gr (+ 8) of the tile as operand fragments
+    uint32_t qf[NQ][kSteps][2];
+    float row_scale[NQ][2], qsum[NQ][2];                  // of rows 2 t4 + e (+ 8): the columns of this lane's scores
+    int first[NQ][2], last[NQ][2];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int r = t.row0 + gr + 8 * n;
         const bool live = r < t.rows;
         const int token = live ? r / g.group : 0, head = kv_head * g.group + (live ? r % g.group : 0);
         const T* q = static_cast<const T*>(g.q) + (int64_t)(t.q0 + token) * g.q_ts + (int64_t)head * g.q_hs;
@@ -119,199 +153,195 @@ attn_rows_kernel(const AttnArgs g) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const __half2 h = __floats2half2_rn(lo[s][i] * down, hi[s][i] * down);
-                qf[s][i * 2 + half] = *reinterpret_cast<const uint32_t*>(&h);
+                qf[n][s][i] = *reinterpret_cast<const uint32_t*>(&h);
                 sum += __low2float(h) + __high2float(h);
             }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        qsum[half] = sum;
-        row_scale[half] = up * g.scale_log2;
-        row_range(g, t, token, first[half], last[half]);
-        if (!live) { first[half] = 0; last[half] = 0x7fffffff; }   // computed with q = 0, never stored: no masks on its account
-    }
-
-    float o[kTiles][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, wsum[2] = {0.0f, 0.0f};
-
-    // ---- context: this warp's chunks
-    // lane's token of a chunk: row number in the cache and the token's ranges (0 where there is no token)
-    auto chunk_rows = [&](int c0, uint32_t& row, float& ks, float& vs) {
-        const int j = c0 + lane;
-        row = j < end ? context_row(g, pages_of, j, kv_head) : 0xffffffffu;
-        ks = vs = 0.0f;
-        if (row != 0xffffffffu) { ks = __ldg(g.k_scale + row); vs = __ldg(g.v_scale + row); }
-    };
-    uint32_t kw[4][kKeyWords];
-    auto load_keys = [&](uint32_t row) {
+        int from, upto;
+        row_range(g, t, token, from, upto);
+        if (!live) { from = 0; upto = 0x7fffffff; }       // computed with q = 0, never stored: no masks on its account
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt) {
-            const uint32_t r = __shfl_sync(0xffffffffu, row, nt * 8 + gr);
-            const uint8_t* p = g.k_levels + (uint64_t)(r == 0xffffffffu ? 0 : r) * kRowBytes + t4 * (kKeyStep * 4);
-#pragma unroll
-            for (int i = 0; i < kKeyLoads; ++i) load_words<kKeyStep>(p + i * (kRowBytes / 2), kw[nt] + i * kKeyStep);
+        for (int e = 0; e < 2; ++e) {
+            const int src = (t4 * 2 + e) * 4;
+            row_scale[n][e] = __shfl_sync(0xffffffffu, up, src) * g.scale_log2;
+            qsum[n][e] = __shfl_sync(0xffffffffu, sum, src);
+            first[n][e] = __shfl_sync(0xffffffffu, from, src);
+            last[n][e] = __shfl_sync(0xffffffffu, upto, src);
         }
-    };
-    uint32_t row, next_row = 0xffffffffu;
-    float ks, vs, next_ks = 0.0f, next_vs = 0.0f;
-    int c0 = begin + warp * kChunk;
-    if (c0 < end) {
-        chunk_rows(c0, row, ks, vs);
-        load_keys(row);
     }
+    int first_of_all = first[0][0], last_of_all = last[0][0];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { first_of_all = max(first_of_all, first[n][e]); last_of_all = min(last_of_all, last[n][e]); }
+    first_of_all = __reduce_max_sync(0xffffffffu, first_of_all);
+    last_of_all = __reduce_min_sync(0xffffffffu, last_of_all);
+
+    float o[kSteps][NQ][4] = {}, m[NQ][2], l[NQ][2], wsum[NQ][2];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.0f; wsum[n][e] = 0.0f; }
+
     for (; c0 < end; c0 += kWarps * kChunk) {
         const int cn = c0 + kWarps * kChunk;
         // values of this chunk, and where the next chunk lies
-        uint32_t vw[2][4][kValWords];
+        uint32_t vw[2][4][kValWords];                     // tokens 16 k + 2 t4 + {0, 1, 8, 9}
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t r = __shfl_sync(0xffffffffu, row, kt * 16 + t4 * 2 + (i & 1) + (i >> 1) * 8);
-                load_words<kValWords>(g.v_levels + (uint64_t)(r == 0xffffffffu ? 0 : r) * kRowBytes + gr * (kValWords * 4), vw[kt][i]);
+                const uint32_t r = __shfl_sync(0xffffffffu, row, k * 16 + t4 * 2 + (i & 1) + (i >> 1) * 8);
+                load_words<kValWords>(g.v_levels + (uint64_t)r * kRowBytes + gr * (kValWords * 4), vw[k][i]);
             }
         if (cn < end) chunk_rows(cn, next_row, next_ks, next_vs);
-        // scores
-        float s[4][4];
+        // scores of tokens 16 k + gr + 8 h (h: register pair) against rows 2 t4 + e
+        float s[2][NQ][4] = {};
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt) {
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[nt][i] = 0.0f;
+            for (int x = 0; x < kSteps; ++x) {
+                const int reg = x * 2;
+                const uint32_t a[4] = {key_pair<BITS>(kw[2 * k][reg / kPairs], reg % kPairs), key_pair<BITS>(kw[2 * k + 1][reg / kPairs], reg % kPairs),
+                                       key_pair<BITS>(kw[2 * k][(reg + 1) / kPairs], (reg + 1) % kPairs),
+                                       key_pair<BITS>(kw[2 * k + 1][(reg + 1) / kPairs], (reg + 1) % kPairs)};
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k) {
-                const int reg = k * 2;
-                mma_f16(s[nt], qf[k], key_pair<BITS>(kw[nt][reg / kPairs], reg % kPairs), key_pair<BITS>(kw[nt][(reg + 1) / kPairs], (reg + 1) % kPairs));
+                for (int n = 0; n < NQ; ++n) mma_f16(s[k][n], a, qf[n][x]);
             }
-        }
         if (cn < end) load_keys(next_row);
         // y = x + log2 of the value's range; masks only where the chunk needs them
         float lg, inv;
         range_exponent(vs, lg, inv);
+        const bool here = vs != -1.0f;
         const float kf = ks * (1.0f / (float)((1 << BITS) - 1));
-        const uint32_t here = __ballot_sync(0xffffffffu, row != 0xffffffffu);
-        const bool whole = here == 0xffffffffu && __all_sync(0xffffffffu, c0 >= max(first[0], first[1]) && c0 + kChunk - 1 <= min(last[0], last[1]));
-        float ivs[4][2], mx[2] = {m[0], m[1]};
+        lg = here ? lg : -INFINITY;                       // a token that is not there: weight 0
+        inv = here ? inv : 0.0f;
+        const bool partial = c0 < first_of_all || c0 + kChunk - 1 > last_of_all;
+        float iv[2][2], mx[NQ][2];
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) mx[n][e] = m[n][e];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int src = k * 16 + h * 8 + gr;
+                const float kj = __shfl_sync(0xffffffffu, kf, src), lj = __shfl_sync(0xffffffffu, lg, src);
+                iv[k][h] = __shfl_sync(0xffffffffu, inv, src);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float y = fmaf((s[k][n][h * 2 + e] + qsum[n][e]) * kj, row_scale[n][e], lj);
+                        if (partial && (c0 + src < first[n][e] || c0 + src > last[n][e])) y = -INFINITY;
+                        s[k][n][h * 2 + e] = y;
+                        mx[n][e] = fmaxf(mx[n][e], y);
+                    }
+            }
+        bool grow = false;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int src = nt * 8 + t4 * 2 + e;
-                const float kj = __shfl_sync(0xffffffffu, kf, src), lj = __shfl_sync(0xffffffffu, lg, src);
-                ivs[nt][e] = __shfl_sync(0xffffffffu, inv, src);
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float y = fmaf((s[nt][half * 2 + e] + qsum[half]) * kj, row_scale[half], lj);
-                    if (!whole) {
-                        const int j = c0 + src;
-                        if (!((here >> src) & 1) || j < first[half] || j > last[half]) y = -INFINITY;
-                    }
-                    s[nt][half * 2 + e] = y;
-                    mx[half] = fmaxf(mx[half], y);
-                }
+                for (int d = 4; d <= 16; d <<= 1) mx[n][e] = fmaxf(mx[n][e], __shfl_xor_sync(0xffffffffu, mx[n][e], d));
+                grow = grow || mx[n][e] > m[n][e];
             }
+        if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            mx[half] = fmaxf(mx[half], __shfl_xor_sync(0xffffffffu, mx[half], 1));
-            mx[half] = fmaxf(mx[half], __shfl_xor_sync(0xffffffffu, mx[half], 2));
-        }
-        if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const float f = mx[half] == m[half] ? 1.0f : fast_exp2(m[half] - mx[half]);       // m = -inf: 0
-                m[half] = mx[half];
-                l[half] *= f; wsum[half] *= f;
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i) { o[i][half * 2] *= f; o[i][half * 2 + 1] *= f; }
-            }
-        }
-        const float ref[2] = {m[0] == -INFINITY ? 0.0f : m[0] - kBoost, m[1] == -INFINITY ? 0.0f : m[1] - kBoost};
-        uint32_t pf[2][4];
-#pragma unroll
-        for (int nt = 0; nt < 4; ++nt) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float w[2];
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float y = s[nt][half * 2 + e];
-                    w[e] = fast_exp2(y - ref[half]);
-                    l[half] = fmaf(w[e], ivs[nt][e], l[half]);
+                    const float f = mx[n][e] == m[n][e] ? 1.0f : fast_exp2(m[n][e] - mx[n][e]);      // m = -inf: 0
+                    m[n][e] = mx[n][e];
+                    l[n][e] *= f; wsum[n][e] *= f;
+#pragma unroll
+                    for (int i = 0; i < kSteps; ++i) { o[i][n][e] *= f; o[i][n][2 + e] *= f; }
                 }
-                const __half2 h = __floats2half2_rn(w[0], w[1]);
-                wsum[half] += __low2float(h) + __high2float(h);
-                pf[nt >> 1][(nt & 1) * 2 + half] = *reinterpret_cast<const uint32_t*>(&h);
-            }
         }
-        // values
+        uint32_t wt[2][NQ][2];                            // weights as the second operand: [token half][row group][8 tokens]
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int n = 0; n < NQ; ++n) {
+            const float ref[2] = {m[n][0] == -INFINITY ? 0.0f : m[n][0] - kBoost, m[n][1] == -INFINITY ? 0.0f : m[n][1] - kBoost};
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) {
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float w[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        w[e] = fast_exp2(s[k][n][h * 2 + e] - ref[e]);
+                        l[n][e] = fmaf(w[e], iv[k][h], l[n][e]);
+                    }
+                    const __half2 p = __floats2half2_rn(w[0], w[1]);
+                    wsum[n][0] += __low2float(p);
+                    wsum[n][1] += __high2float(p);
+                    wt[k][n][h] = transpose_8x8(*reinterpret_cast<const uint32_t*>(&p));
+                }
+        }
+        // values: dims gr D/8 + 2 i (+ 1) of the 16-dim tile i
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
                 constexpr int kPer = 32 / BITS;
-                const int word = i / kPer, e = i % kPer;
-                mma_f16(o[i], pf[kt], value_pair<BITS>(vw[kt][0][word], vw[kt][1][word], e), value_pair<BITS>(vw[kt][2][word], vw[kt][3][word], e));
+                const int word = 2 * i / kPer, e = 2 * i % kPer;
+                const uint32_t a[4] = {value_pair<BITS>(vw[k][0][word], vw[k][1][word], e), value_pair<BITS>(vw[k][0][word], vw[k][1][word], e + 1),
+                                       value_pair<BITS>(vw[k][2][word], vw[k][3][word], e), value_pair<BITS>(vw[k][2][word], vw[k][3][word], e + 1)};
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) mma_f16(o[i][n], a, wt[k][n]);
             }
         row = next_row; ks = next_ks; vs = next_vs;
     }
 
     // ---- merge: rows of the four warps, then the splits (by attn_merge_kernel) or the result
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-#pragma unroll
-        for (int d = 1; d <= 2; d <<= 1) {
-            l[half] += __shfl_xor_sync(0xffffffffu, l[half], d);
-            wsum[half] += __shfl_xor_sync(0xffffffffu, wsum[half], d);
-        }
-        if (t4 == 0) { sh_ml[warp][gr + 8 * half][0] = m[half]; sh_ml[warp][gr + 8 * half][1] = l[half]; }
-    }
-    __syncthreads();
-    constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);
-    float factor[2];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh_ml[w][gr + 8 * half][0]);
-        factor[half] = (m[half] == -INFINITY ? 0.0f : fast_exp2(m[half] - top)) * kInvL;
-    }
-#pragma unroll
-    for (int part = 0; part < 2; ++part) {                  // lanes gr < 4 hold the first half of the dims, gr >= 4 the second
-        if (part) __syncthreads();
-        // column of output tile i for this lane's columns 2 t4, 2 t4 + 1 (as lane index of the value operand): dim = lane * D/8 + i
+    for (int n = 0; n < NQ; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int owner = t4 * 2 + e;                   // which eighth of the row
-            if (owner / 4 == part) {
 #pragma unroll
-                for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half)
-                        sh_o[warp][gr + 8 * half][(owner & 3) * kTiles + i] = (o[i][half * 2 + e] + wsum[half]) * factor[half];
+            for (int d = 4; d <= 16; d <<= 1) {
+                l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
+                wsum[n][e] += __shfl_xor_sync(0xffffffffu, wsum[n][e], d);
             }
+            const int r = n * 8 + t4 * 2 + e;
+            if (gr == 0) { sh_ml[warp][r][0] = m[n][e]; sh_ml[warp][r][1] = l[n][e]; }
+            // the missing 1 of every level (even_level) is one weight sum per row
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+                *reinterpret_cast<float2*>(&sh_o[warp][r][gr * (D / 8) + 2 * i]) = make_float2(o[i][n][e] + wsum[n][e], o[i][n][2 + e] + wsum[n][e]);
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < kRows * (D / 2); i += kWarps * 32) {
-            const int r = i / (D / 2), d = i % (D / 2);
-            if (t.row0 + r >= t.rows) continue;
-            float top = -INFINITY, den = 0.0f, num = 0.0f;
+    __syncthreads();
+    constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);
+    // one warp per row: 32 lanes along the dims
+    for (int r = warp; r < kRows; r += kWarps) {
+        if (t.row0 + r >= t.rows) break;
+        float top = -INFINITY, den = 0.0f, f[kWarps];
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh_ml[w][r][0]);
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh_ml[w][r][0]);
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float mw = sh_ml[w][r][0];
-                if (mw != -INFINITY) den += sh_ml[w][r][1] * fast_exp2(mw - top);
-                num += sh_o[w][r][d];
-            }
-            const int token = (t.row0 + r) / g.group, head = kv_head * g.group + (t.row0 + r) % g.group;
-            const int64_t at = (int64_t)(t.q0 + token) * g.heads + head;
-            if (used > 1) {
-                const int64_t slot = at * g.splits + blockIdx.z;
-                g.part_o[slot * D + part * (D / 2) + d] = num;
-                if (part == 0 && d == 0) g.part_ml[slot] = make_float2(top, den);
-            } else {
-                const float v = top == -INFINITY ? 0.0f : final_value(num / den);
-                static_cast<T*>(g.out)[(int64_t)(t.q0 + token) * g.o_ts + (int64_t)head * g.o_hs + part * (D / 2) + d] = from_f32<T>(v);
-                if (g.lse && part == 0 && d == 0)
-                    g.lse[at] = top == -INFINITY ? -INFINITY : (top - kBoost + log2f(den)) * 0.6931471805599453f;
-            }
+        for (int w = 0; w < kWarps; ++w) {
+            const float mw = sh_ml[w][r][0];
+            f[w] = mw == -INFINITY ? 0.0f : fast_exp2(mw - top);
+            den = mw == -INFINITY ? den : fmaf(sh_ml[w][r][1], f[w], den);
+        }
+        const int token = (t.row0 + r) / g.group, head = kv_head * g.group + (t.row0 + r) % g.group;
+        const int64_t at = (int64_t)(t.q0 + token) * g.heads + head, slot = at * g.splits + blockIdx.z;
+        T* out = static_cast<T*>(g.out) + (int64_t)(t.q0 + token) * g.o_ts + (int64_t)head * g.o_hs;
+#pragma unroll
+        for (int d = lane; d < D; d += 32) {
+            float num = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) num = fmaf(sh_o[w][r][d], f[w], num);
+            num *= kInvL;
+            if (used > 1) g.part_o[slot * D + d] = num;
+            else out[d] = from_f32<T>(top == -INFINITY ? 0.0f : final_value(num / den));
+        }
+        if (lane == 0) {
+            if (used > 1) g.part_ml[slot] = make_float2(top, den);
+            else if (g.lse) g.lse[at] = top == -INFINITY ? -INFINITY : (top - kBoost + log2f(den)) * 0.6931471805599453f;
         }
     }
 }
@@ -360,21 +390,21 @@ inline int64_t tile_bound(int64_t tokens, int batch, int group, int rows) {
     return tokens * group / rows + (tokens < batch ? tokens : batch);
 }
 
-struct AttnPlan { bool many; int64_t tiles; int splits, split_tokens; };
+struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; };   // rows of a tile: 8, 16 or kTileRows
 
 // Which kernel, and how far a context is split.
 //   More than 32 rows per sequence and key head: 256-row tiles on the tensor cores.  A context is split only
 // while the tiles do not fill the multiprocessors, in stretches of 512 tokens at least (each split writes and
 // re-reads a row of fp32 results).
-//   Otherwise: tiles of 16 rows; enough CTAs for about three rounds of four per multiprocessor, at least one
+//   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; enough CTAs for about three rounds of four per multiprocessor, at least one
 // chunk per warp in each.
 AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_q, int64_t max_kv) {
     AttnPlan p;
-    p.many = max_q * group > 32;
+    p.rows = max_q * group > 32 ? kTileRows : max_q * group > 8 ? 16 : 8;
     const int64_t context = max_kv < 1 ? 1 : max_kv;
     int64_t per, unit;
-    if (p.many) {
-        p.tiles = tile_bound(tokens, batch, group, kTileRows);
+    p.tiles = tile_bound(tokens, batch, group, p.rows);
+    if (p.rows == kTileRows) {
         unit = kStepTokens;
         int64_t likely = batch * ceil_div(max_q * group, kTileRows);
         if (likely > p.tiles) likely = p.tiles;
@@ -382,7 +412,6 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
         if (splits > ceil_div(context, 512)) splits = ceil_div(context, 512);
         per = ceil_div(context, splits < 1 ? 1 : splits);
     } else {
-        p.tiles = tile_bound(tokens, batch, group, kRows);
         unit = kChunk * kWarps;
         per = ceil_div(context * p.tiles * kv_heads, 148 * 4 * 3);
     }
@@ -396,10 +425,11 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
 inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 
 template <typename T, int D>
-int launch_merge(const AttnArgs& g, bool many, cudaStream_t st) {
+int launch_merge(const AttnArgs& g, int rows, cudaStream_t st) {
     const unsigned blocks = (unsigned)ceil_div(g.tokens * g.heads, 4);
-    return many ? launch_chained_as(true, attn_merge_kernel<T, D, kTileRows, kStepTokens>, blocks, 128u, 0, st, g)
-                : launch_chained_as(true, attn_merge_kernel<T, D, kRows, kChunk>, blocks, 128u, 0, st, g);
+    auto* kernel = rows == kTileRows ? attn_merge_kernel<T, D, kTileRows, kStepTokens>
+                   : rows == 16      ? attn_merge_kernel<T, D, 16, kChunk> : attn_merge_kernel<T, D, 8, kChunk>;
+    return launch_chained_as(true, kernel, blocks, 128u, 0, st, g);
 }
 
 template <typename T, int D, int BITS>
@@ -408,15 +438,16 @@ int launch_rows(const AttnArgs& g, const AttnPlan& p, cudaStream_t st) {
     cfg.gridDim = dim3((unsigned)p.tiles, (unsigned)g.kv_heads, (unsigned)p.splits);
     cfg.blockDim = dim3(kWarps * 32, 1, 1);
     cfg.stream = st;
-    if (cudaLaunchKernelEx(&cfg, attn_rows_kernel<T, D, BITS>, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
+    auto* kernel = p.rows == 8 ? attn_rows_kernel<T, D, BITS, 1> : attn_rows_kernel<T, D, BITS, 2>;
+    if (cudaLaunchKernelEx(&cfg, kernel, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
     return launch_status();
 }
 
 template <typename T, int D>
 int launch_attention(const AttnArgs& g, const AttnPlan& p, int dtype, int bits, cudaStream_t st) {
-    const int rc = p.many ? attention_tiles(g, dtype, D, bits, p.tiles, st)
+    const int rc = p.rows == kTileRows ? attention_tiles(g, dtype, D, bits, p.tiles, st)
                           : bits == 8 ? launch_rows<T, D, 8>(g, p, st) : launch_rows<T, D, 4>(g, p, st);
-    return rc != MPQ_OK || p.splits == 1 ? rc : launch_merge<T, D>(g, p.many, st);
+    return rc != MPQ_OK || p.splits == 1 ? rc : launch_merge<T, D>(g, p.rows, st);
 }
 
 }  // namespace mpq
