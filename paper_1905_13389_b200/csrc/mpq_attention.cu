@@ -2,14 +2,13 @@
 //
 // A CTA of four warps takes 8 NQ query rows (tokens x heads of one key head) and a stretch of the context;
 // each warp runs an online softmax of its own over every fourth chunk of 32 tokens and the four are merged
-// at the end.  The products are transposed, S^T = K Q^T and O^T = V^T W^T with mma.sync.m16n8k16: tokens and
+// at the end.  A warp copies its chunks asynchronously into a ring of its own in shared memory, the next one
+// under way while it works on this one, so 12 warps a multiprocessor keep some 100 KB in flight.  The products are transposed, S^T = K Q^T and O^T = V^T W^T with mma.sync.m16n8k16: tokens and
 // dims fill the 16-wide side, eight query rows the other one, so a single token of a few heads wastes little.
-// Level bytes go from global memory straight into the operand registers: the element order inside a dot
-// product is free, so the 16 bytes that a lane loads ARE its operand fragment, for the keys (lane = token,
-// bytes along dim) and for the values (lane = 16 dims of a token pair); only W^T changes hands, by one
-// 8 x 8 register transpose per 8 tokens.  With so few rows the work is bound by reading the cache, not by the
-// matrix pipe (which is why the 128-row tcgen05 tile, mostly empty here, is not used), and nothing is staged
-// in shared memory.  The keys of the next chunk are loaded while the softmax and the value product run.
+// The element order inside a dot product is free, so the 16 level bytes that a lane reads ARE its operand
+// fragment, for the keys (lane = token, bytes along dim) and for the values (lane = 16 dims of a token pair);
+// only W^T changes hands, by one 8 x 8 register transpose per 8 tokens.  With so few rows the work is bound by
+// reading the cache, not by the matrix pipe, which is why the 128-row tcgen05 tile, mostly empty here, is not used.
 #include "mpq_attention.cuh"
 
 namespace mpq {
@@ -60,12 +59,24 @@ __device__ __forceinline__ int key_element(int word, int pair, int t) {
     return t * kPerLane + word * 8 + pair;
 }
 
-// Words of `bytes` level bytes loaded by a lane.
+// N words of level bytes of a lane, from shared memory.
 template <int N>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
-    if constexpr (N == 4) { const uint4 v = __ldg(reinterpret_cast<const uint4*>(p)); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
-    else if constexpr (N == 2) { const uint2 v = __ldg(reinterpret_cast<const uint2*>(p)); w[0] = v.x; w[1] = v.y; }
-    else { w[0] = __ldg(reinterpret_cast<const uint32_t*>(p)); }
+    if constexpr (N == 4) { const uint4 v = *reinterpret_cast<const uint4*>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+    else if constexpr (N == 2) { const uint2 v = *reinterpret_cast<const uint2*>(p); w[0] = v.x; w[1] = v.y; }
+    else { w[0] = *reinterpret_cast<const uint32_t*>(p); }
+}
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// Where byte `at` of token `row`'s keys and values lies in a chunk's tile: 16-byte pieces are exchanged inside a row so
+// that the 8 lanes of one shared-memory access meet different banks (keys: two rows x four pieces for rows of 128 bytes;
+// values: rows 2 t of four token pairs).
+template <int ROW_BYTES>
+__device__ __forceinline__ int key_place(int row, int at) { return row * ROW_BYTES + (ROW_BYTES == 128 ? at ^ ((row & 1) << 6) : at); }
+template <int ROW_BYTES>
+__device__ __forceinline__ int value_place(int row, int at) {
+    return row * ROW_BYTES + (ROW_BYTES == 128 ? at ^ ((row & 7) << 4) : ROW_BYTES == 64 ? at ^ (((row >> 1) & 3) << 4) : at);
 }
 
 template <typename T, int D, int BITS, int NQ>
@@ -79,8 +90,10 @@ attn_rows_kernel(const AttnArgs g) {
     constexpr int kValWords = D / 8 * BITS / 32;          // words of a value row per lane (8 lanes share a row)
     constexpr int kPairs = 16 / BITS;                     // operand registers per word (keys)
     constexpr int kSteps = D / 16;                        // k-steps of the score product, 16-dim tiles of the value product
+    constexpr int kTile = kChunk * kRowBytes;             // bytes of a chunk's keys (or values)
+    extern __shared__ __align__(128) unsigned char ring_raw[];            // [warps][2 stages][keys, values]; the merge's rows afterwards
     __shared__ float sh_ml[kWarps][kRows][2];
-    __shared__ __align__(16) float sh_o[kWarps][kRows][D + 4];
+    float (*sh_o)[kRows][D + 4] = reinterpret_cast<float (*)[kRows][D + 4]>(ring_raw);
 
     chain_entry();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -96,31 +109,37 @@ attn_rows_kernel(const AttnArgs g) {
     const int32_t* pages_of = g.table + (int64_t)t.b * g.table_stride;
 
     // ---- context: this warp's chunks
-    // lane's token of a chunk: row number in the cache and the token's ranges (-1: there is no token)
-    auto chunk_rows = [&](int c0, uint32_t& row, float& ks, float& vs) {
-        const int j = c0 + lane;
-        row = j < end ? context_row(g, pages_of, j, kv_head) : 0xffffffffu;
+    // lane's token of a chunk: its row number in the cache (all ones: there is no token), then its ranges (-1: none).
+    // Rows are looked up three chunks ahead, ranges and bytes requested two chunks ahead: no load waits for another.
+    auto find_row = [&](int c) { return c + lane < end ? context_row(g, pages_of, c + lane, kv_head) : 0xffffffffu; };
+    unsigned char* ring = ring_raw + warp * (4 * kTile);
+    auto request = [&](int stage, uint32_t row, float& ks, float& vs) {
         ks = 0.0f; vs = -1.0f;
         if (row != 0xffffffffu) { ks = __ldg(g.k_scale + row); vs = __ldg(g.v_scale + row); }
         else row = 0u;                                    // a row that can be read; weight 0
-    };
-    uint32_t kw[4][kKeyWords];                            // tokens 8 n + gr of the chunk
-    auto load_keys = [&](uint32_t row) {
+        constexpr int kPieces = kRowBytes / 16;
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring + stage * (2 * kTile));
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const uint32_t r = __shfl_sync(0xffffffffu, row, n * 8 + gr);
-            const uint8_t* p = g.k_levels + (uint64_t)r * kRowBytes + t4 * (kKeyStep * 4);
-#pragma unroll
-            for (int i = 0; i < kKeyLoads; ++i) load_words<kKeyStep>(p + i * (kRowBytes / 2), kw[n] + i * kKeyStep);
+        for (int x = 0; x < kPieces; ++x) {
+            const int r = (x * 32 + lane) / kPieces, at = (x * 32 + lane) % kPieces * 16;
+            const int64_t from = (int64_t)__shfl_sync(0xffffffffu, row, r) * kRowBytes + at;
+            copy_async16(dst + key_place<kRowBytes>(r, at), g.k_levels + from);
+            copy_async16(dst + kTile + value_place<kRowBytes>(r, at), g.v_levels + from);
         }
     };
-    uint32_t row = 0u, next_row = 0u;
+    auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+    constexpr int kStride = kWarps * kChunk;
     float ks = 0.0f, vs = -1.0f, next_ks = 0.0f, next_vs = -1.0f;
+    uint32_t row2 = 0xffffffffu;
     int c0 = begin + warp * kChunk;
     if (c0 < end) {
-        chunk_rows(c0, row, ks, vs);
-        load_keys(row);
+        const uint32_t r0 = find_row(c0), r1 = find_row(c0 + kStride);
+        row2 = find_row(c0 + 2 * kStride);
+        request(0, r0, ks, vs);
+        commit();
+        if (c0 + kStride < end) request(1, r1, next_ks, next_vs);
     }
+    commit();
 
     // ---- queries: row gr (+ 8) of the tile as operand fragments
     uint32_t qf[NQ][kSteps][2];
@@ -184,32 +203,32 @@ attn_rows_kernel(const AttnArgs g) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.0f; wsum[n][e] = 0.0f; }
 
-    for (; c0 < end; c0 += kWarps * kChunk) {
-        const int cn = c0 + kWarps * kChunk;
-        // values of this chunk, and where the next chunk lies
-        uint32_t vw[2][4][kValWords];                     // tokens 16 k + 2 t4 + {0, 1, 8, 9}
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t r = __shfl_sync(0xffffffffu, row, k * 16 + t4 * 2 + (i & 1) + (i >> 1) * 8);
-                load_words<kValWords>(g.v_levels + (uint64_t)r * kRowBytes + gr * (kValWords * 4), vw[k][i]);
-            }
-        if (cn < end) chunk_rows(cn, next_row, next_ks, next_vs);
+    for (int stage = 0; c0 < end; c0 += kStride, stage ^= 1) {
+        const uint32_t row3 = find_row(c0 + 3 * kStride);
+        const unsigned char* keys = ring + stage * (2 * kTile);
+        const unsigned char* values = keys + kTile;
+        asm volatile("cp.async.wait_group 1;" ::: "memory");             // this chunk's copies, not the next one's
+        __syncwarp();
         // scores of tokens 16 k + gr + 8 h (h: register pair) against rows 2 t4 + e
         float s[2][NQ][4] = {};
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < 2; ++k) {
+            uint32_t kw[2][kKeyWords];                    // tokens 16 k + gr, + 8
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < kKeyLoads; ++i)
+                    load_words<kKeyStep>(keys + key_place<kRowBytes>(k * 16 + h * 8 + gr, t4 * (kKeyStep * 4) + i * (kRowBytes / 2)), kw[h] + i * kKeyStep);
 #pragma unroll
             for (int x = 0; x < kSteps; ++x) {
                 const int reg = x * 2;
-                const uint32_t a[4] = {key_pair<BITS>(kw[2 * k][reg / kPairs], reg % kPairs), key_pair<BITS>(kw[2 * k + 1][reg / kPairs], reg % kPairs),
-                                       key_pair<BITS>(kw[2 * k][(reg + 1) / kPairs], (reg + 1) % kPairs),
-                                       key_pair<BITS>(kw[2 * k + 1][(reg + 1) / kPairs], (reg + 1) % kPairs)};
+                const uint32_t a[4] = {key_pair<BITS>(kw[0][reg / kPairs], reg % kPairs), key_pair<BITS>(kw[1][reg / kPairs], reg % kPairs),
+                                       key_pair<BITS>(kw[0][(reg + 1) / kPairs], (reg + 1) % kPairs),
+                                       key_pair<BITS>(kw[1][(reg + 1) / kPairs], (reg + 1) % kPairs)};
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) mma_f16(s[k][n], a, qf[n][x]);
             }
-        if (cn < end) load_keys(next_row);
+        }
         // y = x + log2 of the value's range; masks only where the chunk needs them
         float lg, inv;
         range_exponent(vs, lg, inv);
@@ -283,18 +302,29 @@ attn_rows_kernel(const AttnArgs g) {
         }
         // values: dims gr D/8 + 2 i (+ 1) of the 16-dim tile i
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < 2; ++k) {
+            uint32_t vw[4][kValWords];                    // tokens 16 k + 2 t4 + {0, 1, 8, 9}
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                load_words<kValWords>(values + value_place<kRowBytes>(k * 16 + t4 * 2 + (i & 1) + (i >> 1) * 8, gr * (kValWords * 4)), vw[i]);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 constexpr int kPer = 32 / BITS;
                 const int word = 2 * i / kPer, e = 2 * i % kPer;
-                const uint32_t a[4] = {value_pair<BITS>(vw[k][0][word], vw[k][1][word], e), value_pair<BITS>(vw[k][0][word], vw[k][1][word], e + 1),
-                                       value_pair<BITS>(vw[k][2][word], vw[k][3][word], e), value_pair<BITS>(vw[k][2][word], vw[k][3][word], e + 1)};
+                const uint32_t a[4] = {value_pair<BITS>(vw[0][word], vw[1][word], e), value_pair<BITS>(vw[0][word], vw[1][word], e + 1),
+                                       value_pair<BITS>(vw[2][word], vw[3][word], e), value_pair<BITS>(vw[2][word], vw[3][word], e + 1)};
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) mma_f16(o[i][n], a, wt[k][n]);
             }
-        row = next_row; ks = next_ks; vs = next_vs;
+        }
+        __syncwarp();                                     // every lane has read this stage
+        ks = next_ks; vs = next_vs;
+        if (c0 + 2 * kStride < end) request(stage, row2, next_ks, next_vs);
+        commit();
+        row2 = row3;
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();                                      // the ring becomes the merge's buffer
 
     // ---- merge: rows of the four warps, then the splits (by attn_merge_kernel) or the result
 #pragma unroll
@@ -362,23 +392,35 @@ __global__ void __launch_bounds__(128) attn_merge_kernel(const AttnArgs g) {
         if (g.q_starts[mid] <= token) lo = mid; else hi = mid;
     }
     AttnTile t;
-    t.b = lo; t.q0 = g.q_starts[lo];
+    t.b = lo; t.q0 = g.q_starts[lo]; t.kv_len = g.kv_lens[lo];
     t.n_q = (int)min((int64_t)g.q_starts[lo + 1], g.tokens) - t.q0;
     t.rows = t.n_q * g.group;
     t.row0 = ((token - t.q0) * g.group + head % g.group) / R * R;
     tile_range<R, CHUNK>(g, t);
     const int used = tile_splits(g, t);
     if (used <= 1) return;                                   // stored by the split itself
+    // lane s (and s + 32, ...) weighs split s; the rows are then summed with the loads of four splits in flight
+    const float2* ml = g.part_ml + at * g.splits;
     float top = -INFINITY, den = 0.0f;
-    for (int s = 0; s < used; ++s) top = fmaxf(top, g.part_ml[at * g.splits + s].x);
-    float acc[D / 32] = {};
-    for (int s = 0; s < used; ++s) {
-        const float2 ml = g.part_ml[at * g.splits + s];
-        const float f = ml.x == -INFINITY ? 0.0f : fast_exp2(ml.x - top);
-        den = ml.x == -INFINITY ? den : fmaf(ml.y, f, den);
+    for (int s = lane; s < used; s += 32) top = fmaxf(top, ml[s].x);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(g.part_o[(at * g.splits + s) * D + i * 32 + lane], f, acc[i]);
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float acc[D / 32] = {};
+    for (int s0 = 0; s0 < used; s0 += 32) {
+        const float2 mine = s0 + lane < used ? ml[s0 + lane] : make_float2(-INFINITY, 0.0f);
+        const float f = mine.x == -INFINITY ? 0.0f : fast_exp2(mine.x - top);
+        if (mine.x != -INFINITY) den = fmaf(mine.y, f, den);
+        const int n = min(32, used - s0);
+        const float* part = g.part_o + (at * g.splits + s0) * D + lane;
+#pragma unroll 4
+        for (int s = 0; s < n; ++s) {
+            const float fs = __shfl_sync(0xffffffffu, f, s);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(__ldg(part + (int64_t)s * D + i * 32), fs, acc[i]);
+        }
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
     T* out = static_cast<T*>(g.out) + (int64_t)token * g.o_ts + (int64_t)head * g.o_hs;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) out[i * 32 + lane] = from_f32<T>(top == -INFINITY ? 0.0f : final_value(acc[i] / den));
@@ -396,7 +438,7 @@ struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; };   // row
 //   More than 32 rows per sequence and key head: 256-row tiles on the tensor cores.  A context is split only
 // while the tiles do not fill the multiprocessors, in stretches of 512 tokens at least (each split writes and
 // re-reads a row of fp32 results).
-//   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; enough CTAs for about three rounds of four per multiprocessor, at least one
+//   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; enough CTAs for about eight rounds of three per multiprocessor, at least one
 // chunk per warp in each.
 AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_q, int64_t max_kv) {
     AttnPlan p;
@@ -413,7 +455,7 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
         per = ceil_div(context, splits < 1 ? 1 : splits);
     } else {
         unit = kChunk * kWarps;
-        per = ceil_div(context * p.tiles * kv_heads, 148 * 4 * 3);
+        per = ceil_div(context * p.tiles * kv_heads, 148 * 4 * 6);
     }
     per = ceil_div(per, unit) * unit;
     if (ceil_div(context, per) > 256) per = ceil_div(ceil_div(context, 256), unit) * unit;
@@ -438,7 +480,12 @@ int launch_rows(const AttnArgs& g, const AttnPlan& p, cudaStream_t st) {
     cfg.gridDim = dim3((unsigned)p.tiles, (unsigned)g.kv_heads, (unsigned)p.splits);
     cfg.blockDim = dim3(kWarps * 32, 1, 1);
     cfg.stream = st;
+    const size_t ring = (size_t)kWarps * 4 * kChunk * (D * BITS / 8), merge = (size_t)kWarps * p.rows * (D + 4) * 4;
+    cfg.dynamicSmemBytes = ring > merge ? ring : merge;
+    static PerDeviceOnce once8, once16;
     auto* kernel = p.rows == 8 ? attn_rows_kernel<T, D, BITS, 1> : attn_rows_kernel<T, D, BITS, 2>;
+    const int rc = (p.rows == 8 ? once8 : once16).raise_smem_limit(kernel, cfg.dynamicSmemBytes);
+    if (rc != MPQ_OK) return rc;
     if (cudaLaunchKernelEx(&cfg, kernel, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
     return launch_status();
 }

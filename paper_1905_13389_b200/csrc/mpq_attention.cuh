@@ -56,8 +56,9 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& g, int index, AttnTile
     int before = 0;
     for (int base = 0; base < g.batch; base += 32) {
         const int b = base + lane;
-        int q0 = 0, n = 0;
+        int q0 = 0, n = 0, kv = 0;
         if (b < g.batch) {
+            kv = g.kv_lens[b];
             q0 = (int)min((int64_t)max(g.q_starts[b], 0), g.tokens);
             n = (int)min((int64_t)max(g.q_starts[b + 1], q0), g.tokens) - q0;
         }
@@ -74,6 +75,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& g, int index, AttnTile
             t.b = base + src;
             t.q0 = __shfl_sync(0xffffffffu, q0, src);
             t.n_q = __shfl_sync(0xffffffffu, n, src);
+            t.kv_len = __shfl_sync(0xffffffffu, kv, src);
             t.row0 = (index - before - __shfl_sync(0xffffffffu, upto - tiles, src)) * R;
             t.rows = t.n_q * g.group;
             return true;
@@ -83,10 +85,10 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& g, int index, AttnTile
     return false;
 }
 
-// Context range of a tile of R rows, its start rounded down to a multiple of CHUNK.
+// Context range of a tile of R rows (t.kv_len as the caller gave it), its start rounded down to a multiple of CHUNK.
 template <int R, int CHUNK>
 __device__ __forceinline__ void tile_range(const AttnArgs& g, AttnTile& t) {
-    t.kv_len = (int)max((int64_t)0, min((int64_t)g.kv_lens[t.b], min(g.table_stride * g.page_size, (int64_t)0x7fffff00)));
+    t.kv_len = (int)max((int64_t)0, min((int64_t)t.kv_len, min(g.table_stride * g.page_size, (int64_t)0x7fff0000)));
     int first, last, unused;
     row_range(g, t, t.row0 / g.group, first, unused);
     row_range(g, t, (min(t.row0 + R, t.rows) - 1) / g.group, unused, last);
