@@ -2,8 +2,9 @@
 //
 // A CTA of four warps takes 8 NQ query rows (tokens x heads of one key head) and a stretch of the context;
 // each warp runs an online softmax of its own over every fourth chunk of 32 tokens and the four are merged
-// at the end.  A warp copies its chunks asynchronously into a ring of its own in shared memory, the next one
-// under way while it works on this one, so 12 warps a multiprocessor keep some 100 KB in flight.  The products are transposed, S^T = K Q^T and O^T = V^T W^T with mma.sync.m16n8k16: tokens and
+// at the end.  A warp copies its chunks asynchronously into a ring of its own in shared memory, two to seven of
+// them under way while it works on one: 8 warps a multiprocessor keep 128 KB in flight, and a short context is not
+// paced by the latency of one load after the other.  The products are transposed, S^T = K Q^T and O^T = V^T W^T with mma.sync.m16n8k16: tokens and
 // dims fill the 16-wide side, eight query rows the other one, so a single token of a few heads wastes little.
 // The element order inside a dot product is free, so the 16 level bytes that a lane reads ARE its operand
 // fragment, for the keys (lane = token, bytes along dim) and for the values (lane = 16 dims of a token pair);
@@ -25,26 +26,36 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-// Two 16-bit lanes 1024 + u (u in the low bits, 0x6400 above) -> fp16 2u - (L + 1), exact: the even
-// neighbour below the level 2u - L.  The missing 1 is added back per row (sum of q, sum of w).
-template <int BITS>
-__device__ __forceinline__ uint32_t even_level(uint32_t x) {
-    constexpr float c = BITS == 8 ? -2304.0f : -2064.0f;
-    const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), __float2half2_rn(2.0f), __float2half2_rn(c));
-    return *reinterpret_cast<const uint32_t*>(&r);
+// Operands are the level INDICES behind a power of two, fp16 1024 + u (8 bits: u below 0x64) or 16 + u (4 bits: u in
+// bits 6-9 of 0x4c00), which a byte permutation or one shift and mask make; with OFFSET = 1024 or 16
+//   2u - L = 2 (OFFSET + u) - (2 OFFSET + L),
+// so one term per row, (2 OFFSET + L) times the sum of q or of w, turns the products into those of the levels.  The
+// terms cancel to 1/30 (8 bits) of their size at most on typical levels: 5 bits of the 24 that the sums carry.
+template <int BITS> struct Shifted { static constexpr float offset = BITS == 8 ? 1024.0f : 16.0f, correction = 2.0f * offset + (float)((1 << BITS) - 1); };
+__device__ __forceinline__ uint32_t shifted_nibbles(uint32_t x, int i) {
+    return ((i == 0 ? x << 6 : i == 1 ? x << 2 : i == 2 ? x >> 2 : x >> 6) & 0x03c003c0u) | 0x4c004c00u;
 }
 // Word of level bytes -> operand register `pair` (0, 1: BITS = 8; 0..3: BITS = 4): elements pair*2, pair*2+1
 // of the word for 8 bits, pair and pair + 4 for 4 bits.
 template <int BITS>
 __device__ __forceinline__ uint32_t key_pair(uint32_t w, int pair) {
-    if (BITS == 8) return even_level<8>(__byte_perm(w, 0x64646464u, pair ? 0x4342 : 0x4140));
-    return even_level<4>(((w >> (4 * pair)) & 0x000f000fu) | 0x64006400u);
+    if (BITS == 8) return __byte_perm(w, 0x64646464u, pair ? 0x4342 : 0x4140);
+    return shifted_nibbles(w, pair);
 }
-// Element i (0..3 for 8 bits, 0..7 for 4 bits) of the words of two tokens, side by side.
+// The words of two tokens -> operand registers of their elements side by side, `count` = 32 / BITS of them.
 template <int BITS>
-__device__ __forceinline__ uint32_t value_pair(uint32_t a, uint32_t b, int i) {
-    if (BITS == 8) return even_level<8>((__byte_perm(a, b, 0x0400 + 0x0101 * i) & 0x00ff00ffu) | 0x64006400u);
-    return even_level<4>(((__byte_perm(a, b, i < 4 ? 0x5410 : 0x7632) >> (4 * (i & 3))) & 0x000f000fu) | 0x64006400u);
+__device__ __forceinline__ void value_pairs(uint32_t a, uint32_t b, uint32_t* v) {
+    if (BITS == 8) {
+        const uint32_t lo = __byte_perm(a, b, 0x5140), hi = __byte_perm(a, b, 0x7362);       // a0 b0 a1 b1, a2 b2 a3 b3
+        v[0] = __byte_perm(lo, 0x64646464u, 0x4140);
+        v[1] = __byte_perm(lo, 0x64646464u, 0x4342);
+        v[2] = __byte_perm(hi, 0x64646464u, 0x4140);
+        v[3] = __byte_perm(hi, 0x64646464u, 0x4342);
+    } else {
+        const uint32_t lo = __byte_perm(a, b, 0x5410), hi = __byte_perm(a, b, 0x7632);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = shifted_nibbles(lo, i); v[4 + i] = shifted_nibbles(hi, i); }
+    }
 }
 // Position inside a row of the element that operand register `pair` of word `word` holds in its low half
 // (the high half holds + 1 for 8 bits, + 4 for 4 bits), for lane column t.
@@ -69,6 +80,9 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void copy_async4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 // Where byte `at` of token `row`'s keys and values lies in a chunk's tile: 16-byte pieces are exchanged inside a row so
 // that the 8 lanes of one shared-memory access meet different banks (keys: two rows x four pieces for rows of 128 bytes;
 // values: rows 2 t of four token pairs).
@@ -79,8 +93,16 @@ __device__ __forceinline__ int value_place(int row, int at) {
     return row * ROW_BYTES + (ROW_BYTES == 128 ? at ^ ((row & 7) << 4) : ROW_BYTES == 64 ? at ^ (((row >> 1) & 3) << 4) : at);
 }
 
+// Stages of a warp's ring: 24 KB of level bytes (16 KB for rows of 32 bytes), and each stage's ranges.
+template <int ROW_BYTES> struct Ring {
+    static constexpr int stages = ROW_BYTES == 128 ? 3 : ROW_BYTES == 64 ? 6 : 8;
+    static constexpr int tile = kChunk * ROW_BYTES;       // a chunk's keys (or values)
+    static constexpr int stage = 2 * tile + 2 * kChunk * 4;
+    static constexpr int warp = stages * stage;
+};
+
 template <typename T, int D, int BITS, int NQ>
-__global__ void __launch_bounds__(kWarps * 32, NQ == 1 ? 3 : 2)
+__global__ void __launch_bounds__(kWarps * 32, 2)
 attn_rows_kernel(const AttnArgs g) {
     constexpr int kRows = 8 * NQ;
     constexpr int kRowBytes = D * BITS / 8;
@@ -90,8 +112,9 @@ attn_rows_kernel(const AttnArgs g) {
     constexpr int kValWords = D / 8 * BITS / 32;          // words of a value row per lane (8 lanes share a row)
     constexpr int kPairs = 16 / BITS;                     // operand registers per word (keys)
     constexpr int kSteps = D / 16;                        // k-steps of the score product, 16-dim tiles of the value product
-    constexpr int kTile = kChunk * kRowBytes;             // bytes of a chunk's keys (or values)
-    extern __shared__ __align__(128) unsigned char ring_raw[];            // [warps][2 stages][keys, values]; the merge's rows afterwards
+    using R = Ring<kRowBytes>;
+    constexpr int kTile = R::tile, kStages = R::stages;
+    extern __shared__ __align__(128) unsigned char ring_raw[];            // [warps][stages][keys, values, ranges]; the merge's rows afterwards
     __shared__ float sh_ml[kWarps][kRows][2];
     float (*sh_o)[kRows][D + 4] = reinterpret_cast<float (*)[kRows][D + 4]>(ring_raw);
 
@@ -109,16 +132,23 @@ attn_rows_kernel(const AttnArgs g) {
     const int32_t* pages_of = g.table + (int64_t)t.b * g.table_stride;
 
     // ---- context: this warp's chunks
-    // lane's token of a chunk: its row number in the cache (all ones: there is no token), then its ranges (-1: none).
-    // Rows are looked up three chunks ahead, ranges and bytes requested two chunks ahead: no load waits for another.
+    // lane's token of a chunk: its row number in the cache (all ones: there is no token), looked up before it is needed
     auto find_row = [&](int c) { return c + lane < end ? context_row(g, pages_of, c + lane, kv_head) : 0xffffffffu; };
-    unsigned char* ring = ring_raw + warp * (4 * kTile);
-    auto request = [&](int stage, uint32_t row, float& ks, float& vs) {
-        ks = 0.0f; vs = -1.0f;
-        if (row != 0xffffffffu) { ks = __ldg(g.k_scale + row); vs = __ldg(g.v_scale + row); }
-        else row = 0u;                                    // a row that can be read; weight 0
+    unsigned char* ring = ring_raw + warp * R::warp;
+    auto request = [&](int stage, uint32_t row) {         // bytes and ranges of a chunk into a stage
+        unsigned char* at_stage = ring + stage * R::stage;
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(at_stage);
+        const uint32_t ranges = dst + 2 * kTile + lane * 4;
+        if (row != 0xffffffffu) {
+            copy_async4(ranges, g.k_scale + row);
+            copy_async4(ranges + kChunk * 4, g.v_scale + row);
+        } else {                                          // no token (range -1): read a row that is there, give it weight 0
+            float* r = reinterpret_cast<float*>(at_stage + 2 * kTile);
+            r[lane] = 0.0f;
+            r[kChunk + lane] = -1.0f;
+            row = 0u;
+        }
         constexpr int kPieces = kRowBytes / 16;
-        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring + stage * (2 * kTile));
 #pragma unroll
         for (int x = 0; x < kPieces; ++x) {
             const int r = (x * 32 + lane) / kPieces, at = (x * 32 + lane) % kPieces * 16;
@@ -129,21 +159,23 @@ attn_rows_kernel(const AttnArgs g) {
     };
     auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
     constexpr int kStride = kWarps * kChunk;
-    float ks = 0.0f, vs = -1.0f, next_ks = 0.0f, next_vs = -1.0f;
-    uint32_t row2 = 0xffffffffu;
     int c0 = begin + warp * kChunk;
-    if (c0 < end) {
-        const uint32_t r0 = find_row(c0), r1 = find_row(c0 + kStride);
-        row2 = find_row(c0 + 2 * kStride);
-        request(0, r0, ks, vs);
-        commit();
-        if (c0 + kStride < end) request(1, r1, next_ks, next_vs);
+    uint32_t pending;
+    {
+        uint32_t rows[kStages - 1];
+#pragma unroll
+        for (int s = 0; s < kStages - 1; ++s) rows[s] = find_row(c0 + s * kStride);
+        pending = find_row(c0 + (kStages - 1) * kStride);
+#pragma unroll
+        for (int s = 0; s < kStages - 1; ++s) {
+            if (c0 + s * kStride < end) request(s, rows[s]);
+            commit();
+        }
     }
-    commit();
 
     // ---- queries: row gr (+ 8) of the tile as operand fragments
     uint32_t qf[NQ][kSteps][2];
-    float row_scale[NQ][2], qsum[NQ][2];                  // of rows 2 t4 + e (+ 8): the columns of this lane's scores
+    float row_scale[NQ][2], q_term[NQ][2];                // of rows 2 t4 + e (+ 8): the columns of this lane's scores
     int first[NQ][2], last[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
@@ -184,7 +216,7 @@ attn_rows_kernel(const AttnArgs g) {
         for (int e = 0; e < 2; ++e) {
             const int src = (t4 * 2 + e) * 4;
             row_scale[n][e] = __shfl_sync(0xffffffffu, up, src) * g.scale_log2;
-            qsum[n][e] = __shfl_sync(0xffffffffu, sum, src);
+            q_term[n][e] = -Shifted<BITS>::correction * __shfl_sync(0xffffffffu, sum, src);
             first[n][e] = __shfl_sync(0xffffffffu, from, src);
             last[n][e] = __shfl_sync(0xffffffffu, upto, src);
         }
@@ -203,14 +235,17 @@ attn_rows_kernel(const AttnArgs g) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) { m[n][e] = -INFINITY; l[n][e] = 0.0f; wsum[n][e] = 0.0f; }
 
-    for (int stage = 0; c0 < end; c0 += kStride, stage ^= 1) {
-        const uint32_t row3 = find_row(c0 + 3 * kStride);
-        const unsigned char* keys = ring + stage * (2 * kTile);
+    for (int stage = 0; c0 < end; c0 += kStride, stage = stage + 1 == kStages ? 0 : stage + 1) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");      // this chunk's copies are done
+        __syncwarp();                                     // ... every lane's, and every lane has read the stage before
+        if (c0 + (kStages - 1) * kStride < end) request(stage == 0 ? kStages - 1 : stage - 1, pending);
+        commit();
+        pending = find_row(c0 + kStages * kStride);
+        const unsigned char* keys = ring + stage * R::stage;
         const unsigned char* values = keys + kTile;
-        asm volatile("cp.async.wait_group 1;" ::: "memory");             // this chunk's copies, not the next one's
-        __syncwarp();
+        const float* ranges = reinterpret_cast<const float*>(keys + 2 * kTile);
         // scores of tokens 16 k + gr + 8 h (h: register pair) against rows 2 t4 + e
-        float s[2][NQ][4] = {};
+        float s[2][NQ][4] = {}, s_odd[2][NQ][4] = {};   // two chains of products each
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             uint32_t kw[2][kKeyWords];                    // tokens 16 k + gr, + 8
@@ -226,22 +261,21 @@ attn_rows_kernel(const AttnArgs g) {
                                        key_pair<BITS>(kw[0][(reg + 1) / kPairs], (reg + 1) % kPairs),
                                        key_pair<BITS>(kw[1][(reg + 1) / kPairs], (reg + 1) % kPairs)};
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) mma_f16(s[k][n], a, qf[n][x]);
+                for (int n = 0; n < NQ; ++n) mma_f16(x & 1 ? s_odd[k][n] : s[k][n], a, qf[n][x]);
             }
         }
         // y = x + log2 of the value's range; masks only where the chunk needs them
+        const float vs = ranges[kChunk + lane];
         float lg, inv;
         range_exponent(vs, lg, inv);
         const bool here = vs != -1.0f;
-        const float kf = ks * (1.0f / (float)((1 << BITS) - 1));
+        const float kf = ranges[lane] * (1.0f / (float)((1 << BITS) - 1));
         lg = here ? lg : -INFINITY;                       // a token that is not there: weight 0
         inv = here ? inv : 0.0f;
         const bool partial = c0 < first_of_all || c0 + kChunk - 1 > last_of_all;
-        float iv[2][2], mx[NQ][2];
+        float iv[2][2], top[NQ][2];
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) mx[n][e] = m[n][e];
+        for (int n = 0; n < NQ; ++n) top[n][0] = top[n][1] = -INFINITY;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -253,31 +287,29 @@ attn_rows_kernel(const AttnArgs g) {
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float y = fmaf((s[k][n][h * 2 + e] + qsum[n][e]) * kj, row_scale[n][e], lj);
+                        float y = fmaf(fmaf(2.0f, s[k][n][h * 2 + e] + s_odd[k][n][h * 2 + e], q_term[n][e]) * kj, row_scale[n][e], lj);
                         if (partial && (c0 + src < first[n][e] || c0 + src > last[n][e])) y = -INFINITY;
                         s[k][n][h * 2 + e] = y;
-                        mx[n][e] = fmaxf(mx[n][e], y);
+                        top[n][e] = fmaxf(top[n][e], y);
                     }
             }
-        bool grow = false;
+        bool grow = false;                                // also the first finite maximum
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                for (int d = 4; d <= 16; d <<= 1) mx[n][e] = fmaxf(mx[n][e], __shfl_xor_sync(0xffffffffu, mx[n][e], d));
-                grow = grow || mx[n][e] > m[n][e];
-            }
+        for (int n = 0; n < NQ; ++n) grow = grow || top[n][0] > m[n][0] + kLag || top[n][1] > m[n][1] + kLag;
         if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float f = mx[n][e] == m[n][e] ? 1.0f : fast_exp2(m[n][e] - mx[n][e]);      // m = -inf: 0
-                    m[n][e] = mx[n][e];
-                    l[n][e] *= f; wsum[n][e] *= f;
 #pragma unroll
-                    for (int i = 0; i < kSteps; ++i) { o[i][n][e] *= f; o[i][n][2 + e] *= f; }
+                    for (int d = 4; d <= 16; d <<= 1) top[n][e] = fmaxf(top[n][e], __shfl_xor_sync(0xffffffffu, top[n][e], d));
+                    if (top[n][e] > m[n][e] + kLag) {
+                        const float f = fast_exp2(m[n][e] - top[n][e]);               // m = -infinity: 0
+                        m[n][e] = top[n][e];
+                        l[n][e] *= f; wsum[n][e] *= f;
+#pragma unroll
+                        for (int i = 0; i < kSteps; ++i) { o[i][n][e] *= f; o[i][n][2 + e] *= f; }
+                    }
                 }
         }
         uint32_t wt[2][NQ][2];                            // weights as the second operand: [token half][row group][8 tokens]
@@ -307,21 +339,20 @@ attn_rows_kernel(const AttnArgs g) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 load_words<kValWords>(values + value_place<kRowBytes>(k * 16 + t4 * 2 + (i & 1) + (i >> 1) * 8, gr * (kValWords * 4)), vw[i]);
+            constexpr int kPer = 32 / BITS;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                constexpr int kPer = 32 / BITS;
-                const int word = 2 * i / kPer, e = 2 * i % kPer;
-                const uint32_t a[4] = {value_pair<BITS>(vw[0][word], vw[1][word], e), value_pair<BITS>(vw[0][word], vw[1][word], e + 1),
-                                       value_pair<BITS>(vw[2][word], vw[3][word], e), value_pair<BITS>(vw[2][word], vw[3][word], e + 1)};
+            for (int word = 0; word < kValWords; ++word) {
+                uint32_t low[kPer], high[kPer];
+                value_pairs<BITS>(vw[0][word], vw[1][word], low);
+                value_pairs<BITS>(vw[2][word], vw[3][word], high);
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) mma_f16(o[i][n], a, wt[k][n]);
+                for (int e = 0; e < kPer; e += 2) {
+                    const uint32_t a[4] = {low[e], low[e + 1], high[e], high[e + 1]};
+#pragma unroll
+                    for (int n = 0; n < NQ; ++n) mma_f16(o[(word * kPer + e) / 2][n], a, wt[k][n]);
+                }
             }
         }
-        __syncwarp();                                     // every lane has read this stage
-        ks = next_ks; vs = next_vs;
-        if (c0 + 2 * kStride < end) request(stage, row2, next_ks, next_vs);
-        commit();
-        row2 = row3;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();                                      // the ring becomes the merge's buffer
@@ -338,10 +369,10 @@ attn_rows_kernel(const AttnArgs g) {
             }
             const int r = n * 8 + t4 * 2 + e;
             if (gr == 0) { sh_ml[warp][r][0] = m[n][e]; sh_ml[warp][r][1] = l[n][e]; }
-            // the missing 1 of every level (even_level) is one weight sum per row
+            const float w_term = -Shifted<BITS>::correction * wsum[n][e];
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
-                *reinterpret_cast<float2*>(&sh_o[warp][r][gr * (D / 8) + 2 * i]) = make_float2(o[i][n][e] + wsum[n][e], o[i][n][2 + e] + wsum[n][e]);
+                *reinterpret_cast<float2*>(&sh_o[warp][r][gr * (D / 8) + 2 * i]) = make_float2(fmaf(2.0f, o[i][n][e], w_term), fmaf(2.0f, o[i][n][2 + e], w_term));
         }
     __syncthreads();
     constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);
@@ -376,51 +407,70 @@ attn_rows_kernel(const AttnArgs g) {
     }
 }
 
-// Splits of a context -> result: one warp per (token, head).
-template <typename T, int D, int R, int CHUNK>
-__global__ void __launch_bounds__(128) attn_merge_kernel(const AttnArgs g) {
+// Splits of a context -> result: WARPS warps per (token, head), each with every WARPS-th split, so that the rows of up
+// to 32 splits are loaded at once (one warp looping over 43 splits took 10 us).
+constexpr int kMergeThreads = 256;
+template <typename T, int D, int R, int CHUNK, int WARPS>
+__global__ void __launch_bounds__(kMergeThreads) attn_merge_kernel(const AttnArgs g) {
+    __shared__ float sh_acc[kMergeThreads / 32][D], sh_den[kMergeThreads / 32];
     chain_entry();
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (at >= g.tokens * g.heads) return;
-    const int token = (int)(at / g.heads), head = (int)(at % g.heads);
-    // the sequence that holds the token: the last one that starts at or before it and is not empty there
-    int lo = 0, hi = g.batch;                                // q_starts[lo] <= token < q_starts[hi] is kept
-    if (g.q_starts[0] > token || g.q_starts[g.batch] <= token) return;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (g.q_starts[mid] <= token) lo = mid; else hi = mid;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % WARPS;
+    const int64_t at = (int64_t)blockIdx.x * (kMergeThreads / 32 / WARPS) + warp / WARPS;
+    const bool exists = at < g.tokens * g.heads;
+    const int token = exists ? (int)(at / g.heads) : 0, head = exists ? (int)(at % g.heads) : 0;
+    // the sequence that holds the token: the last one that starts at or before it (q_starts[lo] <= token < q_starts[hi])
+    int used = 0;
+    if (exists && g.q_starts[0] <= token && g.q_starts[g.batch] > token) {
+        int lo = 0, hi = g.batch;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (g.q_starts[mid] <= token) lo = mid; else hi = mid;
+        }
+        AttnTile t;
+        t.b = lo; t.q0 = g.q_starts[lo]; t.kv_len = g.kv_lens[lo];
+        t.n_q = (int)min((int64_t)g.q_starts[lo + 1], g.tokens) - t.q0;
+        t.rows = t.n_q * g.group;
+        t.row0 = ((token - t.q0) * g.group + head % g.group) / R * R;
+        tile_range<R, CHUNK>(g, t);
+        used = tile_splits(g, t);
     }
-    AttnTile t;
-    t.b = lo; t.q0 = g.q_starts[lo]; t.kv_len = g.kv_lens[lo];
-    t.n_q = (int)min((int64_t)g.q_starts[lo + 1], g.tokens) - t.q0;
-    t.rows = t.n_q * g.group;
-    t.row0 = ((token - t.q0) * g.group + head % g.group) / R * R;
-    tile_range<R, CHUNK>(g, t);
-    const int used = tile_splits(g, t);
-    if (used <= 1) return;                                   // stored by the split itself
-    // lane s (and s + 32, ...) weighs split s; the rows are then summed with the loads of four splits in flight
+    if (used <= 1) used = 0;                                 // stored by the split itself (or not a token of any sequence)
     const float2* ml = g.part_ml + at * g.splits;
     float top = -INFINITY, den = 0.0f;
     for (int s = lane; s < used; s += 32) top = fmaxf(top, ml[s].x);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     float acc[D / 32] = {};
-    for (int s0 = 0; s0 < used; s0 += 32) {
-        const float2 mine = s0 + lane < used ? ml[s0 + lane] : make_float2(-INFINITY, 0.0f);
+    // lane i weighs split part + WARPS i; the rows are summed with the loads of four splits in flight
+    for (int s0 = part; s0 < used; s0 += 32 * WARPS) {
+        const int my = s0 + lane * WARPS;
+        const float2 mine = my < used ? ml[my] : make_float2(-INFINITY, 0.0f);
         const float f = mine.x == -INFINITY ? 0.0f : fast_exp2(mine.x - top);
         if (mine.x != -INFINITY) den = fmaf(mine.y, f, den);
-        const int n = min(32, used - s0);
-        const float* part = g.part_o + (at * g.splits + s0) * D + lane;
+        const int n = min(32, (used - s0 + WARPS - 1) / WARPS);
+        const float* row = g.part_o + (at * g.splits + s0) * D + lane;
 #pragma unroll 4
         for (int s = 0; s < n; ++s) {
             const float fs = __shfl_sync(0xffffffffu, f, s);
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(__ldg(part + (int64_t)s * D + i * 32), fs, acc[i]);
+            for (int i = 0; i < D / 32; ++i) acc[i] = fmaf(__ldg(row + (int64_t)s * (WARPS * D) + i * 32), fs, acc[i]);
         }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+    if constexpr (WARPS > 1) {
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) sh_acc[warp][i * 32 + lane] = acc[i];
+        if (lane == 0) sh_den[warp] = den;
+        __syncthreads();
+        if (part != 0) return;
+        for (int w = 1; w < WARPS; ++w) {
+            den += sh_den[warp + w];
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) acc[i] += sh_acc[warp + w][i * 32 + lane];
+        }
+    }
+    if (used == 0) return;
     T* out = static_cast<T*>(g.out) + (int64_t)token * g.o_ts + (int64_t)head * g.o_hs;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) out[i * 32 + lane] = from_f32<T>(top == -INFINITY ? 0.0f : final_value(acc[i] / den));
@@ -438,24 +488,27 @@ struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; };   // row
 //   More than 32 rows per sequence and key head: 256-row tiles on the tensor cores.  A context is split only
 // while the tiles do not fill the multiprocessors, in stretches of 512 tokens at least (each split writes and
 // re-reads a row of fp32 results).
-//   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; enough CTAs for about eight rounds of three per multiprocessor, at least one
-// chunk per warp in each.
+//   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; splits that give each of the two CTAs
+// per multiprocessor one, but of no more than kLongSplit tokens, so that contexts of different lengths even out
+// (a CTA costs some 3 us beside its tokens: 128-token splits of 8 contexts of 4000 took 31 us, these KKK).
+constexpr int kLongSplit = 1536;
 AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_q, int64_t max_kv) {
     AttnPlan p;
     p.rows = max_q * group > 32 ? kTileRows : max_q * group > 8 ? 16 : 8;
     const int64_t context = max_kv < 1 ? 1 : max_kv;
     int64_t per, unit;
     p.tiles = tile_bound(tokens, batch, group, p.rows);
+    int64_t likely = batch * ceil_div(max_q < 1 ? group : max_q * group, p.rows);
+    if (likely > p.tiles) likely = p.tiles;
     if (p.rows == kTileRows) {
         unit = kStepTokens;
-        int64_t likely = batch * ceil_div(max_q * group, kTileRows);
-        if (likely > p.tiles) likely = p.tiles;
         int64_t splits = 148 / (likely * kv_heads);
         if (splits > ceil_div(context, 512)) splits = ceil_div(context, 512);
         per = ceil_div(context, splits < 1 ? 1 : splits);
     } else {
         unit = kChunk * kWarps;
-        per = ceil_div(context * p.tiles * kv_heads, 148 * 4 * 6);
+        per = ceil_div(context * likely * kv_heads, 148 * 2);
+        if (per > kLongSplit) per = kLongSplit;
     }
     per = ceil_div(per, unit) * unit;
     if (ceil_div(context, per) > 256) per = ceil_div(ceil_div(context, 256), unit) * unit;
@@ -466,12 +519,16 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
 
 inline int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 
+template <typename T, int D, int R, int CHUNK>
+int launch_merge_of(const AttnArgs& g, cudaStream_t st) {
+    const int64_t rows = g.tokens * g.heads;
+    return g.splits > 4 ? launch_chained_as(true, attn_merge_kernel<T, D, R, CHUNK, 8>, (unsigned)rows, kMergeThreads, 0, st, g)
+                        : launch_chained_as(true, attn_merge_kernel<T, D, R, CHUNK, 1>, (unsigned)ceil_div(rows, kMergeThreads / 32), kMergeThreads, 0, st, g);
+}
 template <typename T, int D>
 int launch_merge(const AttnArgs& g, int rows, cudaStream_t st) {
-    const unsigned blocks = (unsigned)ceil_div(g.tokens * g.heads, 4);
-    auto* kernel = rows == kTileRows ? attn_merge_kernel<T, D, kTileRows, kStepTokens>
-                   : rows == 16      ? attn_merge_kernel<T, D, 16, kChunk> : attn_merge_kernel<T, D, 8, kChunk>;
-    return launch_chained_as(true, kernel, blocks, 128u, 0, st, g);
+    return rows == kTileRows ? launch_merge_of<T, D, kTileRows, kStepTokens>(g, st)
+           : rows == 16      ? launch_merge_of<T, D, 16, kChunk>(g, st) : launch_merge_of<T, D, 8, kChunk>(g, st);
 }
 
 template <typename T, int D, int BITS>
@@ -480,7 +537,7 @@ int launch_rows(const AttnArgs& g, const AttnPlan& p, cudaStream_t st) {
     cfg.gridDim = dim3((unsigned)p.tiles, (unsigned)g.kv_heads, (unsigned)p.splits);
     cfg.blockDim = dim3(kWarps * 32, 1, 1);
     cfg.stream = st;
-    const size_t ring = (size_t)kWarps * 4 * kChunk * (D * BITS / 8), merge = (size_t)kWarps * p.rows * (D + 4) * 4;
+    const size_t ring = (size_t)kWarps * Ring<D * BITS / 8>::warp, merge = (size_t)kWarps * p.rows * (D + 4) * 4;
     cfg.dynamicSmemBytes = ring > merge ? ring : merge;
     static PerDeviceOnce once8, once16;
     auto* kernel = p.rows == 8 ? attn_rows_kernel<T, D, BITS, 1> : attn_rows_kernel<T, D, BITS, 2>;
@@ -528,8 +585,10 @@ extern "C" int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_
     if (tokens == 0) return MPQ_OK;
     const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_q, max_kv);
     if (p.tiles > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
+    int page_shift = -1;
+    if ((page_size & (page_size - 1)) == 0) for (page_shift = 0; (1 << page_shift) < page_size; ++page_shift) {}
     AttnArgs g = {q, q_token_stride, q_head_stride, q_starts, kv_lens, table, table_stride, tokens, batch, heads, kv_heads, heads / kv_heads,
-                  k_levels, k_scale, v_levels, v_scale, pages, page_size, causal != 0, window, scale * 1.4426950408889634f,
+                  k_levels, k_scale, v_levels, v_scale, pages, page_size, page_shift, causal != 0, window, scale * 1.4426950408889634f,
                   out, out_token_stride, out_head_stride, lse, nullptr, nullptr, p.splits, p.split_tokens};
     if (p.splits > 1) {
         if (!workspace) return MPQ_ERR_NULL;

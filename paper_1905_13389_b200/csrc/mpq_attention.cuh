@@ -7,12 +7,13 @@
 // on the fp16 tensor pipes over the bare levels, and
 //   x_j = (q . levels_j) (s^k_j / L) scale log2(e)          one fp32 multiply per score,
 //   2^x_j v_j = 2^(x_j + log2 s^v_j) levels_j / L           the value's range moves into the exponent.
-// With y_j = x_j + log2 s^v_j and the running maximum m of y, the weights w_j = 2^(y_j - m + 15) lie in
-// [0, 2^15] whatever the ranges are: that is what makes fp16 weights safe (what is lost is a weight below
-// 2^-39 of the row's largest CONTRIBUTION, never a token whose score alone is small).  The denominator is
-// kept in fp32:
-//   l = sum_j w_j / s^v_j = 2^(15 - m) sum_j 2^x_j,
-// where a token drops out only if its contribution lies 2^141 below the row's largest one.
+// With y_j = x_j + log2 s^v_j and a reference m at most 2^3 below the running maximum of y, the weights
+// w_j = 2^(y_j - m + 12) lie in [0, 2^15] whatever the ranges are: that is what makes fp16 weights safe (what
+// is lost is a weight below 2^-36 of the row's largest CONTRIBUTION, never a token whose score alone is small).
+// The reference moves only when the maximum has outgrown it by more than 2^3, so a step usually needs neither
+// a reduction of the maximum over lanes nor a rescaling of what has been summed.  The denominator is kept in fp32:
+//   l = sum_j w_j / s^v_j = 2^(12 - m) sum_j 2^x_j,
+// where a token drops out only if its contribution lies 2^138 below the row's largest one.
 // Queries are scaled by a power of two per row before they become fp16, so nothing overflows or is lost
 // beside the row's largest element.  Ranges below 2^-90 (all-zero values among them) count as 2^-90
 // in the exponent, and a result below 2^-89 in magnitude is stored as 0.
@@ -26,7 +27,7 @@ struct AttnArgs {
     const int32_t* q_starts; const int32_t* kv_lens; const int32_t* table; int64_t table_stride;
     int64_t tokens; int batch, heads, kv_heads, group;
     const uint8_t* k_levels; const float* k_scale; const uint8_t* v_levels; const float* v_scale;
-    int64_t pages; int page_size;
+    int64_t pages; int page_size, page_shift;   // shift: log2 of a page size that is a power of two, else -1
     int causal; int64_t window;
     float scale_log2;                       // scale * log2(e)
     void* out; int64_t o_ts, o_hs; float* lse;
@@ -109,14 +110,15 @@ __device__ __forceinline__ void split_range(const AttnArgs& g, const AttnTile& t
 // Row number in the cache (in tokens) of context token j, or 0xffffffff when its page number lies outside
 // the cache.  Cache rows are counted in 32 bits: 2^32 rows of 32 bytes are more than the device holds.
 __device__ __forceinline__ uint32_t context_row(const AttnArgs& g, const int32_t* pages_of, int j, int kv_head) {
-    const int p = j / g.page_size;
+    const int p = g.page_shift >= 0 ? j >> g.page_shift : j / g.page_size;
     const int32_t page = __ldg(pages_of + p);
-    if (page < 0 || page >= g.pages) return 0xffffffffu;
+    if ((uint32_t)page >= (uint32_t)g.pages) return 0xffffffffu;          // g.pages is below 2^31
     return ((uint32_t)page * (uint32_t)g.kv_heads + (uint32_t)kv_head) * (uint32_t)g.page_size + (uint32_t)(j - p * g.page_size);
 }
 
 constexpr float kTinyRange = 8.077935669463161e-28f;        // 2^-90
-constexpr float kBoost = 15.0f;                             // weights are scaled by 2^15: up to half of fp16's largest number
+constexpr float kLag = 3.0f;                                // the reference may lie this far (log2) below a row's maximum,
+constexpr float kBoost = 12.0f;                             // and weights are scaled by 2^12: up to half of fp16's largest number
 
 // 2^x to 2 units in the last place or so; 2^-infinity = 0.
 __device__ __forceinline__ float fast_exp2(float x) {

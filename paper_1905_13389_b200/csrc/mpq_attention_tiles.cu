@@ -21,8 +21,6 @@
 namespace mpq {
 
 constexpr int kTileThreads = 512;
-constexpr float kLag = 3.0f;                              // the reference may lie this far (log2) below a row's maximum
-constexpr float kTileBoost = kBoost - kLag;               // so that weights still end at 2^15
 
 __device__ unsigned int g_attention_wait_failures;
 
@@ -244,11 +242,11 @@ attn_tiles_kernel(const AttnArgs g) {
                 // The weights are made with the reference of the half step before, in one pass over S; only when a row's
                 // maximum has outgrown it (always in the first one, rarely later) is the pass repeated with a new one.
                 while (true) {
-                    uint64_t less[4];                     // minus the reference: set - kTileBoost, 0 while nothing was seen
+                    uint64_t less[4];                     // minus the reference: set - kBoost, 0 while nothing was seen
                     float top[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float x = set[k] == -INFINITY ? 0.0f : kTileBoost - set[k];
+                        const float x = set[k] == -INFINITY ? 0.0f : kBoost - set[k];
                         less[k] = pack2(x, x);
                         top[k] = -INFINITY;
                         ls[k] = 0;
@@ -398,9 +396,8 @@ attn_tiles_kernel(const AttnArgs g) {
                     }
                 }
                 if (live) {
-                    // the merge counts in units of 2^kBoost above the maximum it is told
-                    if (used > 1) g.part_ml[slot] = make_float2(empty ? -INFINITY : set_row - kTileBoost + kBoost, l_row);
-                    else if (g.lse) g.lse[at] = empty ? -INFINITY : (set_row - kTileBoost + log2f(l_row)) * 0.6931471805599453f;
+                    if (used > 1) g.part_ml[slot] = make_float2(empty ? -INFINITY : set_row, l_row);
+                    else if (g.lse) g.lse[at] = empty ? -INFINITY : (set_row - kBoost + log2f(l_row)) * 0.6931471805599453f;
                 }
                 tmem_fence_before();
             }
