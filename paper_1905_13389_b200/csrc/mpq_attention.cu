@@ -2,9 +2,8 @@
 //
 // A CTA of four warps takes 8 NQ query rows (tokens x heads of one key head) and a stretch of the context;
 // each warp runs an online softmax of its own over every fourth chunk of 32 tokens and the four are merged
-// at the end.  A warp copies its chunks asynchronously into a ring of its own in shared memory, two to seven of
-// them under way while it works on one: 8 warps a multiprocessor keep 128 KB in flight, and a short context is not
-// paced by the latency of one load after the other.  The products are transposed, S^T = K Q^T and O^T = V^T W^T with mma.sync.m16n8k16: tokens and
+// at the end.  A warp copies its chunks asynchronously into a ring of its own in shared memory, one to seven of
+// them under way while it works on one: 12 warps a multiprocessor keep some 100 KB in flight.  The products are transposed, S^T = K Q^T and O^T = V^T W^T with mma.sync.m16n8k16: tokens and
 // dims fill the 16-wide side, eight query rows the other one, so a single token of a few heads wastes little.
 // The element order inside a dot product is free, so the 16 level bytes that a lane reads ARE its operand
 // fragment, for the keys (lane = token, bytes along dim) and for the values (lane = 16 dims of a token pair);
@@ -93,16 +92,18 @@ __device__ __forceinline__ int value_place(int row, int at) {
     return row * ROW_BYTES + (ROW_BYTES == 128 ? at ^ ((row & 7) << 4) : ROW_BYTES == 64 ? at ^ (((row >> 1) & 3) << 4) : at);
 }
 
-// Stages of a warp's ring: 24 KB of level bytes (16 KB for rows of 32 bytes), and each stage's ranges.
-template <int ROW_BYTES> struct Ring {
-    static constexpr int stages = ROW_BYTES == 128 ? 3 : ROW_BYTES == 64 ? 6 : 8;
+// Stages of a warp's ring.  Eight rows: three CTAs share a multiprocessor and 16 KB of level bytes a warp are enough;
+// sixteen rows need more registers, two CTAs with 24 KB (1 context of 16384, 4 tokens of 32 heads: 24 us, with the
+// smaller ring 31; 32 contexts, 1 token each: 127 us with the larger ring and two CTAs, 110 with the smaller and three).
+template <int ROW_BYTES, int NQ> struct Ring {
+    static constexpr int stages = (ROW_BYTES == 128 ? 2 : ROW_BYTES == 64 ? 4 : 8) * (NQ == 1 || ROW_BYTES == 32 ? 2 : 3) / 2;
     static constexpr int tile = kChunk * ROW_BYTES;       // a chunk's keys (or values)
     static constexpr int stage = 2 * tile + 2 * kChunk * 4;
     static constexpr int warp = stages * stage;
 };
 
 template <typename T, int D, int BITS, int NQ>
-__global__ void __launch_bounds__(kWarps * 32, 2)
+__global__ void __launch_bounds__(kWarps * 32, NQ == 1 ? 3 : 2)
 attn_rows_kernel(const AttnArgs g) {
     constexpr int kRows = 8 * NQ;
     constexpr int kRowBytes = D * BITS / 8;
@@ -112,7 +113,7 @@ attn_rows_kernel(const AttnArgs g) {
     constexpr int kValWords = D / 8 * BITS / 32;          // words of a value row per lane (8 lanes share a row)
     constexpr int kPairs = 16 / BITS;                     // operand registers per word (keys)
     constexpr int kSteps = D / 16;                        // k-steps of the score product, 16-dim tiles of the value product
-    using R = Ring<kRowBytes>;
+    using R = Ring<kRowBytes, NQ>;
     constexpr int kTile = R::tile, kStages = R::stages;
     extern __shared__ __align__(128) unsigned char ring_raw[];            // [warps][stages][keys, values, ranges]; the merge's rows afterwards
     __shared__ float sh_ml[kWarps][kRows][2];
@@ -161,16 +162,38 @@ attn_rows_kernel(const AttnArgs g) {
     constexpr int kStride = kWarps * kChunk;
     int c0 = begin + warp * kChunk;
     uint32_t pending;
-    {
-        uint32_t rows[kStages - 1];
+    // the page numbers and the query rows are requested together, the copies as soon as the pages are known
+    uint32_t rows[kStages - 1];
 #pragma unroll
-        for (int s = 0; s < kStages - 1; ++s) rows[s] = find_row(c0 + s * kStride);
-        pending = find_row(c0 + (kStages - 1) * kStride);
+    for (int s = 0; s < kStages - 1; ++s) rows[s] = find_row(c0 + s * kStride);
+    pending = find_row(c0 + (kStages - 1) * kStride);
+    // elements of a lane's share of a query row: 32 / BITS adjacent ones per operand word
+    constexpr int kPerWord = 32 / BITS;
+    T raw[NQ][kKeyWords * kPerWord];
+    int q_token[NQ];
 #pragma unroll
-        for (int s = 0; s < kStages - 1; ++s) {
-            if (c0 + s * kStride < end) request(s, rows[s]);
-            commit();
+    for (int n = 0; n < NQ; ++n) {
+        const int r = t.row0 + gr + 8 * n;
+        const bool live = r < t.rows;
+        const int head = kv_head * g.group + (live ? r % g.group : 0);
+        q_token[n] = live ? r / g.group : -1;
+        const T* q = static_cast<const T*>(g.q) + (int64_t)(t.q0 + max(q_token[n], 0)) * g.q_ts + (int64_t)head * g.q_hs;
+        const bool aligned = (reinterpret_cast<uintptr_t>(q) & 15u) == 0;
+#pragma unroll
+        for (int c = 0; c < kKeyWords * kPerWord; c += 8) {              // 8 adjacent elements
+            const T* p = q + key_element<D, BITS>(c / kPerWord, 0, t4) + c % kPerWord;
+            if (live && aligned) {
+                *reinterpret_cast<uint4*>(&raw[n][c]) = __ldg(reinterpret_cast<const uint4*>(p));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) raw[n][c + i] = live ? p[i] : from_f32<T>(0.0f);
+            }
         }
+    }
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) {
+        if (c0 + s * kStride < end) request(s, rows[s]);
+        commit();
     }
 
     // ---- queries: row gr (+ 8) of the tile as operand fragments
@@ -179,22 +202,9 @@ attn_rows_kernel(const AttnArgs g) {
     int first[NQ][2], last[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        const int r = t.row0 + gr + 8 * n;
-        const bool live = r < t.rows;
-        const int token = live ? r / g.group : 0, head = kv_head * g.group + (live ? r % g.group : 0);
-        const T* q = static_cast<const T*>(g.q) + (int64_t)(t.q0 + token) * g.q_ts + (int64_t)head * g.q_hs;
         float amax = 0.0f;
-        float lo[kSteps][2], hi[kSteps][2];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int reg = s * 2 + i;                              // operand register counted along the row
-                const int e = key_element<D, BITS>(reg / kPairs, reg % kPairs, t4);
-                lo[s][i] = live ? to_f32(q[e]) : 0.0f;
-                hi[s][i] = live ? to_f32(q[e + (BITS == 8 ? 1 : 4)]) : 0.0f;
-                amax = fmaxf(amax, fmaxf(fabsf(lo[s][i]), fabsf(hi[s][i])));
-            }
+        for (int i = 0; i < kKeyWords * kPerWord; ++i) amax = fmaxf(amax, fabsf(to_f32(raw[n][i])));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
         float down, up, sum = 0.0f;
@@ -203,15 +213,16 @@ attn_rows_kernel(const AttnArgs g) {
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const __half2 h = __floats2half2_rn(lo[s][i] * down, hi[s][i] * down);
+                const int reg = s * 2 + i, low = reg / kPairs * kPerWord + (BITS == 8 ? 2 : 1) * (reg % kPairs);   // as key_pair pairs them
+                const __half2 h = __floats2half2_rn(to_f32(raw[n][low]) * down, to_f32(raw[n][low + (BITS == 8 ? 1 : 4)]) * down);
                 qf[n][s][i] = *reinterpret_cast<const uint32_t*>(&h);
                 sum += __low2float(h) + __high2float(h);
             }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
         int from, upto;
-        row_range(g, t, token, from, upto);
-        if (!live) { from = 0; upto = 0x7fffffff; }       // computed with q = 0, never stored: no masks on its account
+        row_range(g, t, q_token[n], from, upto);
+        if (q_token[n] < 0) { from = 0; upto = 0x7fffffff; }   // computed with q = 0, never stored: no masks on its account
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int src = (t4 * 2 + e) * 4;
@@ -488,10 +499,11 @@ struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; };   // row
 //   More than 32 rows per sequence and key head: 256-row tiles on the tensor cores.  A context is split only
 // while the tiles do not fill the multiprocessors, in stretches of 512 tokens at least (each split writes and
 // re-reads a row of fp32 results).
-//   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; splits that give each of the two CTAs
+//   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; splits that give each of the three (two) CTAs
 // per multiprocessor one, but of no more than kLongSplit tokens, so that contexts of different lengths even out
-// (a CTA costs some 3 us beside its tokens: 128-token splits of 8 contexts of 4000 took 31 us, these KKK).
-constexpr int kLongSplit = 1536;
+// (32 contexts of up to 16384: 117, 110 and 127 us with 1536, 3072 and 4096; a CTA costs some 3 us beside its
+// tokens: 128-token splits of 8 contexts of 4000 took 31 us, these 22).
+constexpr int kLongSplit = 3072;
 AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_q, int64_t max_kv) {
     AttnPlan p;
     p.rows = max_q * group > 32 ? kTileRows : max_q * group > 8 ? 16 : 8;
@@ -507,7 +519,7 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
         per = ceil_div(context, splits < 1 ? 1 : splits);
     } else {
         unit = kChunk * kWarps;
-        per = ceil_div(context * likely * kv_heads, 148 * 2);
+        per = ceil_div(context * likely * kv_heads, 148 * (p.rows == 8 ? 3 : 2));
         if (per > kLongSplit) per = kLongSplit;
     }
     per = ceil_div(per, unit) * unit;
@@ -537,7 +549,7 @@ int launch_rows(const AttnArgs& g, const AttnPlan& p, cudaStream_t st) {
     cfg.gridDim = dim3((unsigned)p.tiles, (unsigned)g.kv_heads, (unsigned)p.splits);
     cfg.blockDim = dim3(kWarps * 32, 1, 1);
     cfg.stream = st;
-    const size_t ring = (size_t)kWarps * Ring<D * BITS / 8>::warp, merge = (size_t)kWarps * p.rows * (D + 4) * 4;
+    const size_t ring = (size_t)kWarps * (p.rows == 8 ? Ring<D * BITS / 8, 1>::warp : Ring<D * BITS / 8, 2>::warp), merge = (size_t)kWarps * p.rows * (D + 4) * 4;
     cfg.dynamicSmemBytes = ring > merge ? ring : merge;
     static PerDeviceOnce once8, once16;
     auto* kernel = p.rows == 8 ? attn_rows_kernel<T, D, BITS, 1> : attn_rows_kernel<T, D, BITS, 2>;
