@@ -7,6 +7,8 @@
 #include "mpq_attention.cuh"
 #include "mpq_tensor.cuh"
 
+#include <type_traits>
+
 namespace mpq {
 
 struct LinearArgs {
@@ -114,7 +116,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t exchange = ring + kStages * Shape::stage_bytes;
     uint32_t* exchange_ptr = reinterpret_cast<uint32_t*>(smem_raw + (exchange - smem_addr(smem_raw)));
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     auto full = [&](int s) { return smem_addr(&bars[s]); };
     auto empty = [&](int s) { return smem_addr(&bars[kStages + s]); };
     const uint32_t done = smem_addr(&bars[2 * kStages]);
@@ -141,34 +143,39 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     const int blocks = (int)((g.row_bytes + kBlock - 1) / kBlock);
     const int kb0 = (int)((int64_t)blocks * split / splits), kb1 = (int)((int64_t)blocks * (split + 1) / splits);
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+        const bool leader = elect_one();
         int i = 0;
         for (int kb = kb0; kb < kb1; ++kb, ++i) {
             const int s = i % kStages;
-            if (i >= kStages && !mbar_wait(empty(s), (i / kStages - 1) & 1)) { atomicExch(&failed, 1); break; }
-            if (has_failed()) break;
-            const uint32_t dst = ring + s * Shape::stage_bytes;
-            mbar_expect_tx(full(s), Shape::stage_bytes);
-            tma_load_2d(dst, &map_w, kb * kBlock, n0, full(s));
-            tma_load_2d(dst + 128 * kBlock, &map_a, kb * kBlock, m0, full(s));
+            if (i >= kStages && !mbar_wait_warp(empty(s), (i / kStages - 1) & 1, &failed)) break;
+            if (leader) {
+                const uint32_t dst = ring + s * Shape::stage_bytes;
+                mbar_expect_tx(full(s), Shape::stage_bytes);
+                tma_load_2d(dst, &map_w, kb * kBlock, n0, full(s));
+                tma_load_2d(dst + 128 * kBlock, &map_a, kb * kBlock, m0, full(s));
+            }
         }
         if (has_failed())
             for (int q = i > kStages ? i - kStages : 0; q < i; ++q) mbar_wait(full(q % kStages), (q / kStages) & 1);
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         constexpr uint32_t idesc = umma_idesc_u8(128, BN);
+        const bool leader = elect_one();
+        const uint32_t d = __shfl_sync(0xffffffffu, tmem, 0);
         int i = 0;
         for (int kb = kb0; kb < kb1; ++kb, ++i) {
             const int s = i % kStages;
-            if (!mbar_wait(full(s), (i / kStages) & 1)) { atomicExch(&failed, 1); break; }
-            if (has_failed()) break;
+            if (!mbar_wait_warp(full(s), (i / kStages) & 1, &failed)) break;
             tmem_fence_after();
             const uint32_t at = ring + s * Shape::stage_bytes;
-            const uint64_t da = umma_desc(at), db = umma_desc(at + 128 * kBlock);
+            if (leader) {
+                const uint64_t da = umma_desc(at), db = umma_desc(at + 128 * kBlock);
 #pragma unroll
-            for (int j = 0; j < kBlock / 32; ++j) umma_u8<1>(tmem, da + 2 * j, db + 2 * j, idesc, i > 0 || j > 0);
-            umma_commit<1>(empty(s));
+                for (int j = 0; j < kBlock / 32; ++j) umma_u8<1>(d, da + 2 * j, db + 2 * j, idesc, i > 0 || j > 0);
+                umma_commit<1>(empty(s));
+            }
         }
-        umma_commit<1>(done);
+        if (leader) umma_commit<1>(done);
     } else if (warp >= 2) {
         // constants of the tile's rows while the products run
         const int t = threadIdx.x - 64;
@@ -184,9 +191,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         const int64_t c = (int64_t)n0 + col;
         ColTerm ct = {0.0f, 0u, 0.0f};
         if (c < g.n) ct = col_term(g, c);
-        bool ok = mbar_wait(done, 0);
-        if (!ok) atomicExch(&failed, 1);
-        ok = __all_sync(0xffffffffu, ok && !has_failed());
+        const bool ok = mbar_wait_warp(done, 0, &failed) && !__any_sync(0xffffffffu, has_failed());
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
         const int own = BN / splits;
         if (ok) {
@@ -221,19 +226,24 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             const int64_t c = (int64_t)n0 + col;
             if (c < g.n) {
                 const ColTerm ct = col_term(g, c);
-                for (int j0 = 0; j0 < own; j0 += 2) {     // own is 2 or more
+                auto finish = [&](auto count, int j0) {    // `count` rows of this CTA's share at once
+                    constexpr int N = decltype(count)::value;
                     const int rr = split * own + j0;
-                    if (m0 + rr >= g.m) break;
-                    float f[2];
+                    if (m0 + rr >= g.m) return;
+                    float f[N];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
+                    for (int j = 0; j < N; ++j) {
                         uint32_t acc = 0;
                         for (int s = 0; s < splits; ++s) acc += exchange_ptr[(s * own + j0 + j) * 128 + col];
                         f[j] = linear_value(g, acc, RowTerm{row_scale[rr + j], row_terms[rr + j]}, ct);
                     }
                     glue_values(f, g.glue);
-                    store_column<T, 2>(g, f, (int64_t)m0 + rr, c, (int)min((int64_t)2, g.m - m0 - rr));
-                }
+                    store_column<T, N>(g, f, (int64_t)m0 + rr, c, (int)min((int64_t)N, g.m - m0 - rr));
+                };
+                // own is a power of two, 2 or more: every batch lies inside this CTA's share
+                if (own >= 16) for (int j0 = 0; j0 < own; j0 += 16) finish(std::integral_constant<int, 16>(), j0);
+                else if (own >= 4) for (int j0 = 0; j0 < own; j0 += 4) finish(std::integral_constant<int, 4>(), j0);
+                else finish(std::integral_constant<int, 2>(), 0);
             }
         }
     }
@@ -272,7 +282,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     __shared__ int failed;
     const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
     uint32_t* transpose = reinterpret_cast<uint32_t*>(smem_raw + (ring - smem_addr(smem_raw)) + kStages * Shape::stage_bytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
     auto full = [&](int s) { return smem_addr(&bars[s]); };                        // used in the leader (rank 0)
     auto empty = [&](int s) { return smem_addr(&bars[kStages + s]); };             // one in each CTA
@@ -305,52 +315,63 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         n0 = t / tiles_m * BN;
     };
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+        const bool leader = elect_one();
         int issued = 0;
-        for (int i = 0; i < my_tiles && !has_failed(); ++i) {
+        bool ok = true;
+        for (int i = 0; i < my_tiles && ok; ++i) {
             int m0, n0;
             origin(i, m0, n0);
             for (int kb = 0; kb < blocks; ++kb, ++issued) {
                 const int s = issued % kStages;
-                if (issued >= kStages && !mbar_wait(empty(s), (issued / kStages - 1) & 1)) { atomicExch(&failed, 1); break; }
-                if (has_failed()) break;
-                const uint32_t dst = ring + s * Shape::stage_bytes, bar = map_to_cta(full(s), 0);
-                if (rank == 0) mbar_expect_tx(full(s), 2 * Shape::stage_bytes);
-                tma_load_2d_pair(dst, &map_a, kb * kBlock, m0 + (int)rank * 128, bar);
-                tma_load_2d_pair(dst + 128 * kBlock, &map_w, kb * kBlock, n0 + (int)rank * (BN / 2), bar);
+                if (issued >= kStages && !mbar_wait_warp(empty(s), (issued / kStages - 1) & 1, &failed)) { ok = false; break; }
+                if (leader) {
+                    const uint32_t dst = ring + s * Shape::stage_bytes, bar = map_to_cta(full(s), 0);
+                    if (rank == 0) mbar_expect_tx(full(s), 2 * Shape::stage_bytes);
+                    tma_load_2d_pair(dst, &map_a, kb * kBlock, m0 + (int)rank * 128, bar);
+                    tma_load_2d_pair(dst + 128 * kBlock, &map_w, kb * kBlock, n0 + (int)rank * (BN / 2), bar);
+                }
             }
         }
         // after a failure copies may still be on their way into this CTA; their barrier may be the other CTA's
         if (has_failed()) for (int q = 0; q < 100; ++q) __nanosleep(100000);
-    } else if (warp == 1 && lane == 0 && rank == 0) {
-        constexpr uint32_t idesc = umma_idesc_u8(256, BN);
-        int consumed = 0;
-        for (int i = 0; i < my_tiles && !has_failed(); ++i) {
-            const int acc = i & 1;
-            if (i >= kAccs && !mbar_wait(acc_empty(acc), ((i >> 1) - 1) & 1)) { atomicExch(&failed, 1); break; }
-            tmem_fence_after();
-            const uint32_t d = tmem + (uint32_t)(acc * BN);
-            for (int kb = 0; kb < blocks; ++kb, ++consumed) {
-                const int s = consumed % kStages;
-                if (!mbar_wait(full(s), (consumed / kStages) & 1)) { atomicExch(&failed, 1); break; }
-                if (has_failed()) break;
+    } else if (warp == 1) {
+        if (rank == 0) {
+            constexpr uint32_t idesc = umma_idesc_u8(256, BN);
+            const bool leader = elect_one();
+            const uint32_t acc_base = __shfl_sync(0xffffffffu, tmem, 0);
+            int consumed = 0;
+            bool ok = true;
+            for (int i = 0; i < my_tiles && ok; ++i) {
+                const int acc = i & 1;
+                if (i >= kAccs && !mbar_wait_warp(acc_empty(acc), ((i >> 1) - 1) & 1, &failed)) break;
                 tmem_fence_after();
-                const uint32_t at = ring + s * Shape::stage_bytes;
-                const uint64_t da = umma_desc(at), db = umma_desc(at + 128 * kBlock);
+                const uint32_t d = acc_base + (uint32_t)(acc * BN);
+                for (int kb = 0; kb < blocks; ++kb, ++consumed) {
+                    const int s = consumed % kStages;
+                    if (!mbar_wait_warp(full(s), (consumed / kStages) & 1, &failed)) { ok = false; break; }
+                    tmem_fence_after();
+                    const uint32_t at = ring + s * Shape::stage_bytes;
+                    if (leader) {
+                        const uint64_t da = umma_desc(at), db = umma_desc(at + 128 * kBlock);
 #pragma unroll
-                for (int j = 0; j < kBlock / 32; ++j) umma_u8<2>(d, da + 2 * j, db + 2 * j, idesc, kb > 0 || j > 0);
-                umma_commit<2>(empty(s));
+                        for (int j = 0; j < kBlock / 32; ++j) umma_u8<2>(d, da + 2 * j, db + 2 * j, idesc, kb > 0 || j > 0);
+                        umma_commit<2>(empty(s));
+                    }
+                }
+                if (leader) umma_commit<2>(acc_full(acc));
             }
-            umma_commit<2>(acc_full(acc));
         }
     } else if (warp >= 2) {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         uint32_t* sh = transpose + (warp - 2) * 32 * Shape::row_words;
         const T* res = static_cast<const T*>(g.res);
         T* out = static_cast<T*>(g.out);
-        // two adjacent columns at once where rows start on a multiple of two elements
+        // Where rows start on a multiple of two elements a lane owns two adjacent columns, elsewhere columns 32 apart
+        // (its accesses are then single elements, side by side across the warp).
         const bool twos = (reinterpret_cast<uintptr_t>(out) % (2 * sizeof(T))) == 0 && g.ldo % 2 == 0 &&
                           (!res || ((reinterpret_cast<uintptr_t>(res) % (2 * sizeof(T))) == 0 && g.ldr % 2 == 0));
+        const int ca = twos ? 2 * lane : lane, cb = twos ? 2 * lane + 1 : lane + 32;
         struct alignas(2 * sizeof(T)) Two { T x, y; };
         for (int i = 0; i < my_tiles; ++i) {
             const int acc = i & 1;
@@ -360,17 +381,16 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             const int rows = (int)min((int64_t)32, g.m - row0);                    // 0 or less: none of them exists
             RowTerm mine = {0.0f, 0u};                                             // lane's row; handed round by shuffles
             if (lane < rows) mine = row_term(g, row0 + lane);
-            bool ok = mbar_wait(acc_full(acc), (i >> 1) & 1);
-            if (!ok) atomicExch(&failed, 1);
-            ok = __all_sync(0xffffffffu, ok && !has_failed());
-            if (!ok) break;
+            if (!mbar_wait_warp(acc_full(acc), (i >> 1) & 1, &failed) || __any_sync(0xffffffffu, has_failed())) break;
             tmem_fence_after();
 #pragma unroll 1
             for (int c0 = half * (BN / 2); c0 < (half + 1) * (BN / 2); c0 += 64) {
-                const int64_t c = (int64_t)n0 + c0 + 2 * lane;
+                const int64_t cx = (int64_t)n0 + c0 + ca, cy = (int64_t)n0 + c0 + cb;
+                const bool in_x = cx < g.n, in_y = cy < g.n;
                 ColTerm ct[2] = {{0.0f, 0u, 0.0f}, {0.0f, 0u, 0.0f}};
-                if (c < g.n) ct[0] = col_term(g, c);
-                if (c + 1 < g.n) ct[1] = col_term(g, c + 1);
+                if (in_x) ct[0] = col_term(g, cx);
+                if (in_y) ct[1] = col_term(g, cy);
+                const bool fast = twos && n0 + c0 + 64 <= g.n;
                 const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + c0);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -387,37 +407,56 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(acc), 0));
                 }
-                const bool both = c + 1 < g.n;
-                // kRowsAtOnce rows at a time: all residuals are read before the first result of the group is written
+                // kRowsAtOnce rows at a time.  All residuals of a group are requested before any is used or any result is
+                // written: they may lie in the result's own tensor, so the compiler could not move a load up by itself, and
+                // one load after the other took 45 us of a tile's 51.  (All 32 rows at once spill: 61 -> 78 us at 4096^3.)
                 constexpr int kRowsAtOnce = 8;
 #pragma unroll 1
                 for (int r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
-                    T w[kRowsAtOnce][2];
-                    if (res && c < g.n) {
+                    const bool all_rows = r0 + kRowsAtOnce <= rows;
+                    T* o = out + (row0 + r0) * g.ldo;
+                    const T* q = res + (row0 + r0) * g.ldr;
+                    Two w[kRowsAtOnce];
+                    if (res && fast && all_rows) {
+#pragma unroll
+                        for (int j = 0; j < kRowsAtOnce; ++j) w[j] = *reinterpret_cast<const Two*>(q + j * g.ldr + cx);
+                    } else if (res) {
 #pragma unroll
                         for (int j = 0; j < kRowsAtOnce; ++j) {
-                            if (r0 + j >= rows) continue;
-                            const T* q = res + (row0 + r0 + j) * g.ldr + c;
-                            if (twos && both) { const Two t = *reinterpret_cast<const Two*>(q); w[j][0] = t.x; w[j][1] = t.y; }
-                            else { w[j][0] = q[0]; if (both) w[j][1] = q[1]; }
+                            const int64_t at = min(j, rows - 1 - r0) * g.ldr;      // a row that exists: no branch between the loads
+                            w[j].x = q[at + min(cx, g.n - 1)];
+                            w[j].y = q[at + min(cy, g.n - 1)];
                         }
                     }
                     float f[2 * kRowsAtOnce];
 #pragma unroll
                     for (int j = 0; j < kRowsAtOnce; ++j) {
-                        const uint2 v = *reinterpret_cast<const uint2*>(sh + (r0 + j) * Shape::row_words + 2 * (lane ^ (r0 + j)));
-                        const RowTerm rt = {__shfl_sync(0xffffffffu, mine.scale, r0 + j), __shfl_sync(0xffffffffu, mine.term, r0 + j)};
+                        const int r = r0 + j;
+                        uint2 v;
+                        if (twos) {
+                            v = *reinterpret_cast<const uint2*>(sh + r * Shape::row_words + 2 * (lane ^ r));
+                        } else {
+                            v.x = sh[r * Shape::row_words + 2 * ((ca >> 1) ^ r) + (ca & 1)];
+                            v.y = sh[r * Shape::row_words + 2 * ((cb >> 1) ^ r) + (cb & 1)];
+                        }
+                        const RowTerm rt = {__shfl_sync(0xffffffffu, mine.scale, r), __shfl_sync(0xffffffffu, mine.term, r)};
                         f[2 * j] = linear_value(g, v.x, rt, ct[0]);
                         f[2 * j + 1] = linear_value(g, v.y, rt, ct[1]);
                     }
                     glue_values(f, g.glue);
+                    if (res) {
 #pragma unroll
-                    for (int j = 0; j < kRowsAtOnce; ++j) {
-                        if (r0 + j >= rows || c >= g.n) continue;
-                        if (res) { f[2 * j] += to_f32(w[j][0]); if (both) f[2 * j + 1] += to_f32(w[j][1]); }
-                        T* o = out + (row0 + r0 + j) * g.ldo + c;
-                        if (twos && both) *reinterpret_cast<Two*>(o) = Two{from_f32<T>(f[2 * j]), from_f32<T>(f[2 * j + 1])};
-                        else { o[0] = from_f32<T>(f[2 * j]); if (both) o[1] = from_f32<T>(f[2 * j + 1]); }
+                        for (int j = 0; j < kRowsAtOnce; ++j) { f[2 * j] += to_f32(w[j].x); f[2 * j + 1] += to_f32(w[j].y); }
+                    }
+                    if (fast && all_rows) {
+#pragma unroll
+                        for (int j = 0; j < kRowsAtOnce; ++j) *reinterpret_cast<Two*>(o + j * g.ldo + cx) = Two{from_f32<T>(f[2 * j]), from_f32<T>(f[2 * j + 1])};
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kRowsAtOnce; ++j) {
+                            if (r0 + j < rows && in_x) o[j * g.ldo + cx] = from_f32<T>(f[2 * j]);
+                            if (r0 + j < rows && in_y) o[j * g.ldo + cy] = from_f32<T>(f[2 * j + 1]);
+                        }
                     }
                 }
                 __syncwarp();
@@ -430,6 +469,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     tmem_fence_after();
     if (warp == 0) tmem_free<2>(tmem, kAccs * BN);
     if (threadIdx.x == 0 && failed) atomicAdd(&g_wait_failures, 1u);
+}
+
+// Splits of k: as many as still fit the device at once, with two blocks each and two rows of the tile each at least.
+inline int small_splits(int64_t tiles, int64_t blocks, int bn, int64_t sms) {
+    int splits = 1;
+    while (splits < 8 && splits * 4 <= bn && tiles * splits * 2 <= sms && blocks >= splits * 4) splits *= 2;
+    return splits;
 }
 
 template <typename T, int BN>
@@ -445,8 +491,7 @@ int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
     if (sms == 0) return MPQ_ERR_CUDA;
     const int64_t tiles_w = ceil_div(g.n, 128), tiles = tiles_w * ceil_div(g.m, BN), blocks = ceil_div(g.row_bytes, kBlock);
     if (tiles > (1 << 28)) return MPQ_ERR_BAD_SHAPE;
-    int splits = 1;                                       // as many as still fit the device at once, two blocks of k each at least
-    while (splits < 8 && splits * 4 <= BN && tiles * splits * 2 <= sms && blocks >= splits * 4) splits *= 2;
+    const int splits = small_splits(tiles, blocks, BN, sms);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * splits), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -480,14 +525,25 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     return launch_status();
 }
 
-// Up to 128 rows the weights' own traffic decides: the small form, its tile just wide enough.  Above, CTA pairs.
+// Which form, by estimated cycles per multiprocessor: a k block of 128 bytes takes a pair 2 BN cycles (the 8-bit rate)
+// and an unpaired 128 x BN tile 2 (128 + BN) (its shared memory), a tile's store some 16 BN, and starting up,
+// exchanging partial sums and draining about 5000 in the small form.
 template <typename T>
 int launch_linear_levels(const LinearArgs& g, cudaStream_t st) {
     if (g.m <= 16) return launch_linear_small<T, 16>(g, st);
     if (g.m <= 32) return launch_linear_small<T, 32>(g, st);
     if (g.m <= 64) return launch_linear_small<T, 64>(g, st);
-    if (g.m <= 128) return launch_linear_small<T, 128>(g, st);
-    return launch_linear_pair<T, 256>(g, st);
+    const int64_t sms = sm_count(), blocks = ceil_div(g.row_bytes, kBlock);
+    if (sms < 2) return MPQ_ERR_CUDA;
+    auto pair_cost = [&](int64_t bn) {
+        return ceil_div(ceil_div(g.m, 256) * ceil_div(g.n, bn), sms / 2) * (blocks * 2 * bn + 16 * bn);
+    };
+    const int64_t small_tiles = ceil_div(g.m, 128) * ceil_div(g.n, 128);
+    const int64_t splits = small_splits(small_tiles, blocks, 128, sms);
+    const int64_t small_cost = ceil_div(small_tiles * splits, sms) * (blocks / splits * 512 + 16 * 128) + 5000;
+    const int64_t wide = pair_cost(256), narrow = pair_cost(128);
+    if (g.m <= 128 || small_cost < (wide < narrow ? wide : narrow)) return launch_linear_small<T, 128>(g, st);
+    return wide <= narrow ? launch_linear_pair<T, 256>(g, st) : launch_linear_pair<T, 128>(g, st);
 }
 
 }  // namespace mpq
