@@ -551,6 +551,11 @@ int launch_rows(const AttnArgs& g, const AttnPlan& p, cudaStream_t st) {
     cfg.stream = st;
     const size_t ring = (size_t)kWarps * (p.rows == 8 ? Ring<D * BITS / 8, 1>::warp : Ring<D * BITS / 8, 2>::warp), merge = (size_t)kWarps * p.rows * (D + 4) * 4;
     cfg.dynamicSmemBytes = ring > merge ? ring : merge;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
     static PerDeviceOnce once8, once16;
     auto* kernel = p.rows == 8 ? attn_rows_kernel<T, D, BITS, 1> : attn_rows_kernel<T, D, BITS, 2>;
     const int rc = (p.rows == 8 ? once8 : once16).raise_smem_limit(kernel, cfg.dynamicSmemBytes);

@@ -603,7 +603,17 @@ int launch_tiles(const AttnArgs& g, int64_t tiles, cudaStream_t st) {
     auto* kernel = attn_tiles_kernel<T, D, BITS>;
     const int rc = once.raise_smem_limit(kernel, TileSmem<D>::total);
     if (rc != MPQ_OK) return rc;
-    kernel<<<dim3((unsigned)tiles, (unsigned)g.kv_heads, (unsigned)g.splits), kTileThreads, TileSmem<D>::total, st>>>(g);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)tiles, (unsigned)g.kv_heads, (unsigned)g.splits);
+    cfg.blockDim = dim3(kTileThreads, 1, 1);
+    cfg.dynamicSmemBytes = TileSmem<D>::total;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
     return launch_status();
 }
 

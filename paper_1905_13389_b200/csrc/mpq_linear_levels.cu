@@ -264,7 +264,7 @@ constexpr int kPairStoreWarps = 8;                        // two per quarter of 
 constexpr int kPairThreads = 64 + 32 * kPairStoreWarps;
 template <int BN> struct PairShape {
     static constexpr int stage_bytes = (128 + BN / 2) * kBlock;     // per CTA
-    static constexpr int stages = BN == 256 ? 5 : 6;
+    static constexpr int stages = BN == 256 ? 5 : BN == 128 ? 6 : 7;
     static constexpr int row_words = 64;                            // column pair p of row r lies at pair p ^ r: no bank conflicts either way
     static constexpr int transpose_bytes = kPairStoreWarps * 32 * row_words * 4;
     static constexpr int smem = stages * stage_bytes + transpose_bytes + 1024;
@@ -497,12 +497,14 @@ int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = Shape::smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)splits;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;      // barriers and TMEM are set up before the wait
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     if (cudaLaunchKernelEx(&cfg, kernel, map_w, map_a, g, (int)tiles_w, splits) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
     return launch_status();
 }
@@ -521,8 +523,7 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     const int64_t tiles_m = ceil_div(g.m, 256), tiles = tiles_m * ceil_div(g.n, BN);
     if (tiles > (1 << 28)) return MPQ_ERR_BAD_SHAPE;
     const unsigned ctas = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
-    kernel<<<ctas, kPairThreads, Shape::smem, st>>>(map_a, map_w, g, (int)tiles_m, (int)tiles);
-    return launch_status();
+    return launch_chained_as(true, kernel, ctas, (unsigned)kPairThreads, Shape::smem, st, map_a, map_w, g, (int)tiles_m, (int)tiles);
 }
 
 // Which form, by estimated cycles per multiprocessor: a k block of 128 bytes takes a pair 2 BN cycles (the 8-bit rate)
