@@ -129,7 +129,8 @@ def _check(status: int, where: str):
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    """The current stream of the current device (asked for by number: a torch.cuda.Stream object costs as much as a small kernel)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _ptr(t: Optional[torch.Tensor], dtype=None) -> Optional[int]:
@@ -478,32 +479,59 @@ def level_row_bytes(k: int) -> int:
     return int(lib().mpq_level_row_bytes(k))
 
 
-def _rows(t: Optional[torch.Tensor], shape, dtype=None):
-    """(pointer, row stride) of a matrix whose rows are contiguous; (None, 0) for None."""
+# The calls below serve single tokens, where this binding's own time is what a user waits for: sizes are compared once per
+# tensor, and results come from empty_strided, the cheapest allocation call.
+
+def _expected(t, shape, dtype):
+    raise ValueError("expected a CUDA tensor of shape %s%s whose rows are contiguous, got %s %s with strides %s on %s" % (
+        tuple(shape), "" if dtype is None else " and dtype %s" % dtype, t.dtype, tuple(t.shape), tuple(t.stride()), t.device))
+
+
+def _rows(t: Optional[torch.Tensor], rows: int, k: int, dtype=None):
+    """(pointer, row stride) of a [rows x k] matrix whose rows are contiguous; (None, 0) for None."""
     if t is None:
         return None, 0
-    if not t.is_cuda or tuple(t.shape) != tuple(shape) or (dtype is not None and t.dtype != dtype):
-        raise ValueError("expected a CUDA tensor of shape %s%s, got %s %s" % (
-            tuple(shape), "" if dtype is None else " and dtype %s" % dtype, t.dtype, tuple(t.shape)))
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError("the elements of a row have to be adjacent")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    if not t.is_cuda or t.shape != (rows, k) or (dtype is not None and t.dtype != dtype):
+        _expected(t, (rows, k), dtype)
+    stride, step = t.stride()
+    if step != 1 and k > 1:
+        _expected(t, (rows, k), dtype)
+    return t.data_ptr(), stride if rows > 1 else k
+
+
+def _heads(t: torch.Tensor, tokens: int, heads: int, dim: int, dtype=None):
+    """(pointer, token stride, head stride) of a [tokens][heads][dim] tensor whose head rows are contiguous."""
+    if not t.is_cuda or t.shape != (tokens, heads, dim) or (dtype is not None and t.dtype != dtype):
+        _expected(t, (tokens, heads, dim), dtype)
+    st, sh, step = t.stride()
+    if step != 1:
+        _expected(t, (tokens, heads, dim), dtype)
+    return t.data_ptr(), st if tokens > 1 else heads * dim, sh if heads > 1 else dim
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype) -> Optional[int]:
-    if t is not None and t.numel() != n:
-        raise ValueError("expected %d values, got %d" % (n, t.numel()))
-    return _ptr(t, dtype)
+    """Pointer of n contiguous values; None for None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError("expected %d contiguous %s values on a CUDA device, got %d of %s on %s" % (n, dtype, t.numel(), t.dtype, t.device))
+    return t.data_ptr()
 
 
-def _level_outputs(rows: int, k: int, bits: int, device, out: Optional[Levels]) -> Levels:
-    if out is None:
-        return Levels(torch.empty((rows, -(-k // 16) * 16), dtype=torch.uint8, device=device),
-                      torch.empty(rows, dtype=torch.float32, device=device),
-                      torch.empty(rows, dtype=torch.int32, device=device), bits, k)
-    if tuple(out.bytes.shape) != (rows, -(-k // 16) * 16) or out.bits != bits or out.k != k:
-        raise ValueError("the output levels are of another shape or width")
-    return out
+def _held(lv: Levels, rows: int, k: int):
+    """Pointers of level bytes, ranges and sums, after comparing their sizes."""
+    row = -(-k // 16) * 16
+    if lv.k != k or lv.bytes.shape != (rows, row):
+        raise ValueError("expected levels of %d rows of %d elements (%d bytes apart), got k = %d and bytes %s" % (
+            rows, k, row, lv.k, tuple(lv.bytes.shape)))
+    return _vector(lv.bytes, rows * row, torch.uint8), _vector(lv.scale, rows, torch.float32), _vector(lv.sums, rows, torch.int32)
+
+
+def _new_levels(rows: int, k: int, bits: int, device) -> Levels:
+    row = -(-k // 16) * 16
+    return Levels(torch.empty_strided((rows, row), (row, 1), dtype=torch.uint8, device=device),
+                  torch.empty_strided((rows,), (1,), dtype=torch.float32, device=device),
+                  torch.empty_strided((rows,), (1,), dtype=torch.int32, device=device), bits, k)
 
 
 def rmsnorm_levels(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float, bits: int = 8,
@@ -512,28 +540,35 @@ def rmsnorm_levels(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float, bi
     """Root-mean-square norm of x (+ residual) [rows x k], quantized with one range per row.  residual_out receives
     x + residual (it may be x or residual), values the numbers that the levels stand for."""
     rows, k = x.shape
-    px, ldx = _rows(x, x.shape)
-    pr, ldr = _rows(residual, x.shape, x.dtype)
-    po, ldo = _rows(residual_out, x.shape, x.dtype)
-    pv, ldv = _rows(values, x.shape)
-    out = _level_outputs(rows, k, bits, x.device, out)
-    _check(lib().mpq_rmsnorm_levels(px, ldx, pr, ldr, _dtype(x.dtype), _vector(gain, k, torch.float32), eps, rows, k, bits,
-                                    po, ldo, _ptr(out.bytes, torch.uint8), _vector(out.scale, rows, torch.float32),
-                                    _vector(out.sums, rows, torch.int32), pv, 0 if pv is None else _dtype(values.dtype), ldv,
-                                    _stream()), "mpq_rmsnorm_levels")
+    dtype = x.dtype
+    if out is None:
+        out = _new_levels(rows, k, bits, x.device)
+    elif out.bits != bits:
+        raise ValueError("the output levels are of another width")
+    _check(lib().mpq_rmsnorm_levels(*_rows(x, rows, k), *_rows(residual, rows, k, dtype), _dtype(dtype), _vector(gain, k, torch.float32),
+                                    eps, rows, k, bits, *_rows(residual_out, rows, k, dtype), *_held(out, rows, k),
+                                    *_values(values, rows, k), _stream()), "mpq_rmsnorm_levels")
     return out
+
+
+def _values(values: Optional[torch.Tensor], rows: int, k: int):
+    """(pointer, dtype, row stride) of the optional decoded output."""
+    if values is None:
+        return None, 0, 0
+    p, stride = _rows(values, rows, k)
+    return p, _dtype(values.dtype), stride
 
 
 def encode_levels(x: torch.Tensor, bits: int = 8, act: int = ACT_HTANH, values: Optional[torch.Tensor] = None,
                   out: Optional[Levels] = None) -> Levels:
     """[rows x k] -> level bytes with one range per row (weights, once; activations inside a block)."""
     rows, k = x.shape
-    px, ldx = _rows(x, x.shape)
-    pv, ldv = _rows(values, x.shape)
-    out = _level_outputs(rows, k, bits, x.device, out)
-    _check(lib().mpq_encode_levels(px, ldx, _dtype(x.dtype), rows, k, act, bits, _ptr(out.bytes, torch.uint8),
-                                   _vector(out.scale, rows, torch.float32), _vector(out.sums, rows, torch.int32),
-                                   pv, 0 if pv is None else _dtype(values.dtype), ldv, _stream()), "mpq_encode_levels")
+    if out is None:
+        out = _new_levels(rows, k, bits, x.device)
+    elif out.bits != bits:
+        raise ValueError("the output levels are of another width")
+    _check(lib().mpq_encode_levels(*_rows(x, rows, k), _dtype(x.dtype), rows, k, act, bits, *_held(out, rows, k),
+                                   *_values(values, rows, k), _stream()), "mpq_encode_levels")
     return out
 
 
@@ -541,20 +576,22 @@ def linear_levels(a: Levels, w: Levels, bias: Optional[torch.Tensor] = None, act
                   residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                   dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """act(a w^T + bias) + residual on level operands: a [m x k], w [n x k] -> [m x n] of ``dtype`` (or of ``out``)."""
-    m, n = a.bytes.shape[0], w.bytes.shape[0]
-    if a.k != w.k or a.bytes.shape[1] != w.bytes.shape[1] or a.bytes.shape[1] != -(-a.k // 16) * 16:
-        raise ValueError("the operands' rows differ: %d and %d elements" % (a.k, w.k))
+    m, n, k = a.bytes.shape[0], w.bytes.shape[0], a.k
     if act not in GLUE:
         raise ValueError("unknown activation %r: expected one of %s" % (act, ", ".join(GLUE)))
+    pa, pw = _held(a, m, k), _held(w, n, k)
     if out is None:
-        out = torch.empty((m, n), dtype=dtype, device=a.bytes.device)
-    po, ldo = _rows(out, (m, n))
-    pr, ldr = _rows(residual, (m, n), out.dtype)
-    _check(lib().mpq_linear_levels(_ptr(a.bytes, torch.uint8), _vector(a.scale, m, torch.float32), _vector(a.sums, m, torch.int32), a.bits,
-                                   _ptr(w.bytes, torch.uint8), _vector(w.scale, n, torch.float32), _vector(w.sums, n, torch.int32), w.bits,
-                                   m, n, a.k, _vector(bias, n, torch.float32), GLUE[act], pr, ldr, po, _dtype(out.dtype), ldo,
-                                   _stream()), "mpq_linear_levels")
+        out = torch.empty_strided((m, n), (n, 1), dtype=dtype, device=a.bytes.device)
+    else:
+        dtype = out.dtype
+    _check(lib().mpq_linear_levels(*pa, a.bits, *pw, w.bits, m, n, k, _vector(bias, n, torch.float32), GLUE[act],
+                                   *_rows(residual, m, n, dtype), *_out(out, m, n, dtype), _stream()), "mpq_linear_levels")
     return out
+
+
+def _out(out: torch.Tensor, m: int, n: int, dtype):
+    p, stride = _rows(out, m, n)
+    return p, _dtype(dtype), stride
 
 
 def level_cache(pages: int, heads: int, page_size: int, dim: int, bits: int, device="cuda") -> LevelCache:
@@ -565,41 +602,38 @@ def level_cache(pages: int, heads: int, page_size: int, dim: int, bits: int, dev
 
 
 def _cache(c: LevelCache):
-    pages, heads, page_size, row = c.k.shape
-    if c.v.shape != c.k.shape or c.k_scale.shape != c.k.shape[:3] or c.v_scale.shape != c.k.shape[:3]:
-        raise ValueError("the cache's keys, values and ranges differ in shape")
-    return (pages, heads, page_size, row * 8 // c.bits if c.bits else 0,
-            _ptr(c.k, torch.uint8), _ptr(c.k_scale, torch.float32), _ptr(c.v, torch.uint8), _ptr(c.v_scale, torch.float32))
-
-
-def _heads(t: torch.Tensor, shape, dtype=None):
-    """(pointer, token stride, head stride) of a [tokens][heads][dim] tensor whose head rows are contiguous."""
-    if not t.is_cuda or tuple(t.shape) != tuple(shape) or (dtype is not None and t.dtype != dtype):
-        raise ValueError("expected a CUDA tensor of shape %s%s, got %s %s" % (
-            tuple(shape), "" if dtype is None else " and dtype %s" % dtype, t.dtype, tuple(t.shape)))
-    if t.stride(2) != 1:
-        raise ValueError("the elements of a head have to be adjacent")
-    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1] * shape[2]), (t.stride(1) if shape[1] > 1 else shape[2])
+    """(pages, heads, page size, dim) and the four pointers of a cache."""
+    shape = c.k.shape
+    pages, heads, page_size, row = shape
+    n = pages * heads * page_size
+    if c.v.shape != shape:
+        raise ValueError("the cache's keys and values differ in shape: %s and %s" % (tuple(shape), tuple(c.v.shape)))
+    return (pages, heads, page_size, row * 8 // c.bits if c.bits else 0), (
+        _vector(c.k, n * row, torch.uint8), _vector(c.k_scale, n, torch.float32), _vector(c.v, n * row, torch.uint8), _vector(c.v_scale, n, torch.float32))
 
 
 def cache_write(cache: LevelCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> LevelCache:
     """Quantizes keys and values [tokens][heads][dim] into the cache at ``slots`` (int64; -1: not written)."""
-    pages, heads, page_size, dim, pk, pks, pv, pvs = _cache(cache)
-    shape = (k.shape[0], heads, dim)
-    _check(lib().mpq_cache_write(*_heads(k, shape), *_heads(v, shape, k.dtype), _dtype(k.dtype), _vector(slots, k.shape[0], torch.int64),
-                                 k.shape[0], heads, dim, cache.bits, pk, pks, pv, pvs, pages, page_size, _stream()), "mpq_cache_write")
+    (pages, heads, page_size, dim), held = _cache(cache)
+    tokens, dtype = k.shape[0], k.dtype
+    _check(lib().mpq_cache_write(*_heads(k, tokens, heads, dim), *_heads(v, tokens, heads, dim, dtype), _dtype(dtype),
+                                 _vector(slots, tokens, torch.int64), tokens, heads, dim, cache.bits, *held, pages, page_size, _stream()),
+           "mpq_cache_write")
     return cache
 
 
 def cache_read(cache: LevelCache, slots: torch.Tensor, dtype: torch.dtype, k: Optional[torch.Tensor] = None,
                v: Optional[torch.Tensor] = None):
     """The keys and values at ``slots`` as [tokens][heads][dim] of ``dtype`` (zeros for a slot of -1)."""
-    pages, heads, page_size, dim, pk, pks, pv, pvs = _cache(cache)
-    shape = (slots.numel(), heads, dim)
-    k = torch.empty(shape, dtype=dtype, device=slots.device) if k is None else k
-    v = torch.empty(shape, dtype=dtype, device=slots.device) if v is None else v
-    _check(lib().mpq_cache_read(pk, pks, pv, pvs, pages, page_size, _ptr(slots, torch.int64), shape[0], heads, dim, cache.bits,
-                                *_heads(k, shape, dtype), *_heads(v, shape, dtype), _dtype(dtype), _stream()), "mpq_cache_read")
+    (pages, heads, page_size, dim), held = _cache(cache)
+    tokens = slots.numel()
+    if k is None:
+        k = torch.empty_strided((tokens, heads, dim), (heads * dim, dim, 1), dtype=dtype, device=slots.device)
+    if v is None:
+        v = torch.empty_strided((tokens, heads, dim), (heads * dim, dim, 1), dtype=dtype, device=slots.device)
+    _check(lib().mpq_cache_read(*held, pages, page_size, _vector(slots, tokens, torch.int64), tokens, heads, dim, cache.bits,
+                                *_heads(k, tokens, heads, dim, dtype), *_heads(v, tokens, heads, dim, dtype), _dtype(dtype), _stream()),
+           "mpq_cache_read")
     return k, v
 
 
@@ -613,24 +647,23 @@ def cache_attention(q: torch.Tensor, cache: LevelCache, q_starts: torch.Tensor, 
                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the new tokens q [tokens][heads][dim] of ``batch`` sequences (token ranges q_starts [batch + 1]) over
     their contexts of kv_lens [batch] tokens in the pages table [batch][..] names.  scale defaults to dim ** -0.5."""
-    pages, kv_heads, page_size, dim, pk, pks, pv, pvs = _cache(cache)
-    tokens, heads = q.shape[0], q.shape[1]
-    batch = kv_lens.numel()
-    pq, qt, qh = _heads(q, (tokens, heads, dim))
+    (pages, kv_heads, page_size, dim), held = _cache(cache)
+    tokens, heads, _ = q.shape
+    batch, dtype = kv_lens.numel(), q.dtype
+    per = table.shape[-1]
     if out is None:
-        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
-    po, ot, oh = _heads(out, (tokens, heads, dim), q.dtype)
-    if table.dim() != 2 or table.shape[0] != batch:
-        raise ValueError("expected a page table of %d rows" % batch)
+        out = torch.empty_strided((tokens, heads, dim), (heads * dim, dim, 1), dtype=dtype, device=q.device)
+    L = lib()
     if workspace is None:
-        need = lib().mpq_cache_attention_workspace(tokens, batch, heads, kv_heads, dim, max_q, max_kv)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    _check(lib().mpq_cache_attention(pq, qt, qh, _dtype(q.dtype), _vector(q_starts, batch + 1, torch.int32), _vector(kv_lens, batch, torch.int32),
-                                     _ptr(table, torch.int32), table.shape[1], tokens, batch, heads, kv_heads, dim, max_q, max_kv, pk, pks, pv, pvs,
-                                     cache.bits, pages, page_size, int(causal), window, dim ** -0.5 if scale is None else scale,
-                                     po, ot, oh, _vector(lse, tokens * heads, torch.float32),
-                                     None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
-                                     _stream()), "mpq_cache_attention")
+        need = L.mpq_cache_attention_workspace(tokens, batch, heads, kv_heads, dim, max_q, max_kv)
+        if need:
+            workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=q.device)
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    _check(L.mpq_cache_attention(*_heads(q, tokens, heads, dim), _dtype(dtype), _vector(q_starts, batch + 1, torch.int32),
+                                 _vector(kv_lens, batch, torch.int32), _vector(table, batch * per, torch.int32), per,
+                                 tokens, batch, heads, kv_heads, dim, max_q, max_kv, *held, cache.bits, pages, page_size,
+                                 causal, window, dim ** -0.5 if scale is None else scale, *_heads(out, tokens, heads, dim, dtype),
+                                 _vector(lse, tokens * heads, torch.float32), ws, ws_bytes, _stream()), "mpq_cache_attention")
     return out
 
 
