@@ -63,7 +63,7 @@ __device__ __forceinline__ void encode_lane(const float (&f)[kLaneElems], float 
     uint32_t w[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < kLaneElems; ++i)
-        w[i * BITS / 32] |= (uint32_t)level_index<MPQ_ACT_HTANH>(f[i], inv, r.half_L, r.lo, r.hi, r.H) << (i * BITS % 32);
+        w[i * BITS / 32] |= level_bits(shifted_level<MPQ_ACT_HTANH>(f[i], inv, r)) << (i * BITS % 32);
     if (BITS == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(dst) = w[0];
 }
@@ -75,7 +75,10 @@ __device__ __forceinline__ void decode_lane(const uint8_t* src, float s, float (
     if (BITS == 8) { const uint2 r = *reinterpret_cast<const uint2*>(src); w[0] = r.x; w[1] = r.y; }
     else w[0] = *reinterpret_cast<const uint32_t*>(src);
 #pragma unroll
-    for (int i = 0; i < kLaneElems; ++i) f[i] = (float)(2 * (int)((w[i * BITS / 32] >> (i * BITS % 32)) & L) - L) * alpha;
+    for (int i = 0; i < kLaneElems; ++i) {                 // u into the mantissa of 2^23: no conversion instruction
+        const float shifted = __uint_as_float(((w[i * BITS / 32] >> (i * BITS % 32)) & L) | 0x4b000000u);
+        f[i] = fmaf(2.0f, shifted - kLevelMagic, -(float)L) * alpha;
+    }
 }
 
 template <typename T, int BITS, bool VEC>

@@ -19,24 +19,43 @@ struct RowArgs {
 
 // One row of partial results: sum of squares and the largest |h gain|.
 // y = (h gain) r with one r > 0 per row, and a rounded product by r is monotone, so
-// max |y| = r max |h gain| to the last bit: both statistics come out of ONE pass and one barrier.
-__device__ __forceinline__ void block_stats(float& ss, float& mx, float2* sh) {
+// max |y| = r max |h gain| to the last bit: both statistics come out of ONE pass.
+// The row's constants follow from them in the first warp alone: a root and four exact divisions in every thread were
+// a third of the kernel's instructions, and it is bound by issuing them (0.78 of the issue slots).
+struct RowScalars { float r, s, inv, alpha; };
+template <bool NORM>
+__device__ __forceinline__ RowScalars row_scalars(float ss, float mx, const RowArgs& g) {
+    RowScalars c;
+    c.r = NORM ? __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)g.k), g.eps))) : 1.0f;
+    c.s = NORM ? mx * c.r : mx;
+    c.inv = inverse_scale(c.s);
+    c.alpha = __fdiv_rn(c.s, (float)g.rule.L);
+    return c;
+}
+template <bool NORM>
+__device__ __forceinline__ RowScalars block_scalars(float ss, float mx, const RowArgs& g, float2* sh, RowScalars* sh_scalars) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        if (NORM) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     }
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    if (warps == 1) return;
+    if (warps == 1) return row_scalars<NORM>(ss, mx, g);
     if (lane == 0) sh[threadIdx.x >> 5] = make_float2(ss, mx);
     __syncthreads();
-    const float2 v = lane < warps ? sh[lane] : make_float2(0.0f, 0.0f);
-    ss = v.x; mx = v.y;
+    if (threadIdx.x < 32) {
+        const float2 v = lane < warps ? sh[lane] : make_float2(0.0f, 0.0f);
+        ss = v.x; mx = v.y;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        for (int o = 16; o > 0; o >>= 1) {
+            if (NORM) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        }
+        const RowScalars c = row_scalars<NORM>(ss, mx, g);
+        if (lane == 0) *sh_scalars = c;
     }
+    __syncthreads();
+    return *sh_scalars;
 }
 __device__ __forceinline__ void block_level_sum(int u, int32_t* dst, int* sh) {
     u = __reduce_add_sync(0xffffffffu, u);
@@ -48,11 +67,6 @@ __device__ __forceinline__ void block_level_sum(int u, int32_t* dst, int* sh) {
         u = __reduce_add_sync(0xffffffffu, lane < warps ? sh[lane] : 0);
     }
     if (lane == 0) *dst = u;
-}
-
-template <int ACT_HR>
-__device__ __forceinline__ int row_level(float y, float inv, const LevelRule& r) {
-    return level_index<ACT_HR>(y, inv, r.half_L, r.lo, r.hi, r.H);
 }
 
 // N adjacent elements at once where addresses and strides allow it (VECTOR), one by one otherwise, `count` of
@@ -78,17 +92,16 @@ __device__ __forceinline__ void store_part(T* p, const float (&f)[N], int count)
 }
 // Level rows are 16-byte aligned and padded: whole words always fit (u past the row's end is 0).
 template <int N>
-__device__ __forceinline__ void store_levels(uint8_t* p, const int (&u)[N]) {
+__device__ __forceinline__ void store_levels(uint8_t* p, const uint32_t (&u)[N]) {
 #pragma unroll
     for (int c = 0; c < N / 4; ++c)
-        reinterpret_cast<uint32_t*>(p)[c] = (uint32_t)u[4 * c] | ((uint32_t)u[4 * c + 1] << 8) |
-                                            ((uint32_t)u[4 * c + 2] << 16) | ((uint32_t)u[4 * c + 3] << 24);
+        reinterpret_cast<uint32_t*>(p)[c] = __byte_perm(__byte_perm(u[4 * c], u[4 * c + 1], 0x0040), __byte_perm(u[4 * c + 2], u[4 * c + 3], 0x0040), 0x5410);
 }
 template <int N, bool VECTOR>
-__device__ __forceinline__ void store_values(const RowArgs& g, int64_t row, int64_t at, const int (&u)[N], float alpha, int count) {
+__device__ __forceinline__ void store_values(const RowArgs& g, int64_t row, int64_t at, const float (&shifted)[N], float alpha, int count) {
     float f[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = (float)(2 * u[i] - g.rule.L) * alpha;
+    for (int i = 0; i < N; ++i) f[i] = level_number(shifted[i], g.rule) * alpha;
     const int64_t o = row * g.ldv + at;
     if (g.values_dtype == MPQ_BF16) store_part<__nv_bfloat16, N, VECTOR>(static_cast<__nv_bfloat16*>(g.values) + o, f, count);
     else if (g.values_dtype == MPQ_F16) store_part<__half, N, VECTOR>(static_cast<__half*>(g.values) + o, f, count);
@@ -101,6 +114,7 @@ template <typename T, int VEC, int NV, bool VECTOR, bool NORM, int ACT>
 __global__ void __launch_bounds__(1024)
 level_rows_kernel(const RowArgs g) {
     __shared__ float2 sh_stats[32];
+    __shared__ RowScalars sh_scalars;
     __shared__ int sh_sum[32];
     chain_entry();
     const int64_t row = blockIdx.x;
@@ -152,26 +166,23 @@ level_rows_kernel(const RowArgs g) {
             for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, ACT == MPQ_ACT_HRELU ? h[j][e] : fabsf(h[j][e]));
         }
     }
-    block_stats(ss, mx, sh_stats);
-    const float r = NORM ? __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)g.k), g.eps))) : 1.0f;
-    const float s = NORM ? mx * r : mx;
-    const float inv = inverse_scale(s);
-    const float alpha = __fdiv_rn(s, (float)g.rule.L);
+    const RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
+    const float r = c.r, s = c.s, inv = c.inv, alpha = c.alpha;
     uint8_t* out = g.levels + row * g.row_bytes;
     int total = 0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int i = threadIdx.x + j * blockDim.x;
         if (i < nvec) {
-            int u[VEC];
+            uint32_t u[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                u[e] = row_level<ACT>(NORM ? h[j][e] * r : h[j][e], inv, g.rule);
-                if (!VECTOR && i * VEC + e >= k) u[e] = 0;
-                total += u[e];
+                h[j][e] = shifted_level<ACT>(NORM ? h[j][e] * r : h[j][e], inv, g.rule);
+                u[e] = !VECTOR && i * VEC + e >= k ? 0u : level_bits(h[j][e]);
+                total += (int)u[e];
             }
             store_levels<VEC>(out + (int64_t)i * VEC, u);
-            if (g.values) store_values<VEC, VECTOR>(g, row, (int64_t)i * VEC, u, alpha, k - i * VEC);
+            if (g.values) store_values<VEC, VECTOR>(g, row, (int64_t)i * VEC, h[j], alpha, k - i * VEC);
         }
     }
     // padding words behind the last vector
@@ -187,6 +198,7 @@ template <typename T, bool NORM, int ACT>
 __global__ void __launch_bounds__(1024)
 level_wide_rows_kernel(const RowArgs g) {
     __shared__ float2 sh_stats[32];
+    __shared__ RowScalars sh_scalars;
     __shared__ int sh_sum[32];
     chain_entry();
     const int64_t row = blockIdx.x;
@@ -202,11 +214,8 @@ level_wide_rows_kernel(const RowArgs g) {
         }
         mx = fmaxf(mx, ACT == MPQ_ACT_HRELU ? h : fabsf(h));
     }
-    block_stats(ss, mx, sh_stats);
-    const float r = NORM ? __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)g.k), g.eps))) : 1.0f;
-    const float s = NORM ? mx * r : mx;
-    const float inv = inverse_scale(s);
-    const float alpha = __fdiv_rn(s, (float)g.rule.L);
+    const RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
+    const float r = c.r, s = c.s, inv = c.inv, alpha = c.alpha;
     uint8_t* out = g.levels + row * g.row_bytes;
     int total = 0;
     for (int64_t i = threadIdx.x; i < g.row_bytes; i += blockDim.x) {
@@ -218,22 +227,22 @@ level_wide_rows_kernel(const RowArgs g) {
             if (g.gain) h *= g.gain[i];
             h *= r;
         }
-        const int u[1] = {row_level<ACT>(h, inv, g.rule)};
-        total += u[0];
-        out[i] = (uint8_t)u[0];
-        if (g.values) store_values<1, false>(g, row, i, u, alpha, 1);
+        const float shifted[1] = {shifted_level<ACT>(h, inv, g.rule)};
+        total += (int)level_bits(shifted[0]);
+        out[i] = (uint8_t)level_bits(shifted[0]);
+        if (g.values) store_values<1, false>(g, row, i, shifted, alpha, 1);
     }
     block_level_sum(total, g.sums + row, sh_sum);
     if (threadIdx.x == 0) g.scale[row] = s;
 }
 
-// Threads and vectors per thread: two vectors per thread while the row is short (many loads in flight,
-// few warps to reduce over), more once 1024 threads are not enough.
+// Threads and vectors per thread: one vector each up to 1024 threads (a single row of 4096: 2.7 us, with two 3.6, with
+// four 6.2; 4096 rows 33, 33 and 39 us), then more.
 template <typename T, int VEC, bool VECTOR, bool NORM, int ACT>
 int launch_level_rows(const RowArgs& g, cudaStream_t st) {
     const int64_t nvec = ceil_div(g.k, VEC);
     auto threads_for = [&](int nv) { return (unsigned)(ceil_div(ceil_div(nvec, nv), 32) * 32); };
-    if (threads_for(1) <= 128) return launch_chained(level_rows_kernel<T, VEC, 1, VECTOR, NORM, ACT>, (unsigned)g.rows, threads_for(1), 0, st, g);
+    if (threads_for(1) <= 1024) return launch_chained(level_rows_kernel<T, VEC, 1, VECTOR, NORM, ACT>, (unsigned)g.rows, threads_for(1), 0, st, g);
     if (threads_for(2) <= 1024) return launch_chained(level_rows_kernel<T, VEC, 2, VECTOR, NORM, ACT>, (unsigned)g.rows, threads_for(2), 0, st, g);
     if (threads_for(4) <= 1024) return launch_chained(level_rows_kernel<T, VEC, 4, VECTOR, NORM, ACT>, (unsigned)g.rows, threads_for(4), 0, st, g);
     return launch_chained(level_wide_rows_kernel<T, NORM, ACT>, (unsigned)g.rows, 1024u, 0, st, g);

@@ -71,7 +71,7 @@ __device__ __forceinline__ void store_vec(T* p, const float (&f)[N]) {
 
 // Quantizer constants of a width (see mpq_encode).
 struct LevelRule {
-    float half_L, lo, hi;
+    float half_L, lo, hi, magic;
     int H, L;
 };
 __host__ __device__ inline LevelRule level_rule(int bits) {
@@ -81,7 +81,23 @@ __host__ __device__ inline LevelRule level_rule(int bits) {
     r.half_L = 0.5f * (float)r.L;
     r.lo = -(float)r.H;
     r.hi = (float)r.H - 0.5f;
+    r.magic = 8388608.0f + (float)r.H;
     return r;
+}
+
+// level_index() without a conversion instruction (those run at an eighth of the rate): the clamped quotient plus
+// 2^23 + H, rounded down, holds floor(y) + H in its low mantissa bits, and float(u) is one subtraction away.
+constexpr float kLevelMagic = 8388608.0f;                  // 2^23, bits 0x4b000000
+template <int ACT>
+__device__ __forceinline__ float shifted_level(float x, float inv_s, const LevelRule& r) {
+    float y = __fmul_rn(__fmul_rn(x, inv_s), r.half_L);
+    if (!(y == y)) y = 0.0f;                               // NaN -> level just above zero
+    if (ACT == MPQ_ACT_HRELU) y = fmaxf(y, 0.0f);
+    return __fadd_rd(fminf(fmaxf(y, r.lo), r.hi), r.magic);
+}
+__device__ __forceinline__ uint32_t level_bits(float shifted) { return __float_as_uint(shifted) & 0xffu; }       // u
+__device__ __forceinline__ float level_number(float shifted, const LevelRule& r) {                              // 2u - L, exact
+    return fmaf(2.0f, shifted - kLevelMagic, -(float)r.L);
 }
 
 }  // namespace mpq
