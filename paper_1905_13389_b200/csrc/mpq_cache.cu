@@ -1,9 +1,10 @@
 // Paged cache of keys and values on levels of 8 or 4 bits: quantised as it is written, and read back.
 //
-// A group of dim / 8 lanes (rounded up to a power of two) owns one (token, head), eight elements of the
-// key and of the value per lane: one 16-byte load each for 16-bit types, the range by shuffles inside the
-// group, one 8-byte (or 4-byte) store of level bytes each.  Nothing is staged or read twice; the kernels
-// are bound by memory, and below a few thousand tokens by the latency of that one round trip.
+// A group of dim / 16 lanes (rounded up to a power of two) owns one (token, head), sixteen elements of the
+// key and of the value per lane, the range by shuffles inside the group.  Nothing is staged or read twice.
+// Large calls are bound by issuing instructions as much as by memory (with eight elements per lane 0.78 of the
+// issue slots and 18 us for 8192 tokens x 8 heads x 128, 4 bits), hence the share per lane and a quantizer without
+// tests or conversions where no element is out of the ordinary; small ones by the latency of the one round trip.
 #include "mpq_levels.cuh"
 
 namespace mpq {
@@ -17,24 +18,21 @@ struct CacheArgs {
     uint8_t *k_levels, *v_levels;
     float *k_scale, *v_scale;
     int64_t pages;
-    int page_size;
+    int page_size, page_shift;                                // shift: log2 of a page size that is a power of two, else -1
 };
 
 constexpr int kCacheThreads = 256;
-constexpr int kLaneElems = 8;
+constexpr int kLaneElems = 16;
 
 // Row of the cache (in tokens) that slot and head name, or -1.
-__device__ __forceinline__ int64_t cache_row(int64_t slot, int64_t pages, int page_size, int heads, int head) {
-    const uint64_t total = (uint64_t)pages * (uint32_t)page_size;
+__device__ __forceinline__ int64_t cache_row(const CacheArgs& g, int64_t slot, int head) {
+    const uint64_t total = (uint64_t)g.pages * (uint32_t)g.page_size;
     if ((uint64_t)slot >= total) return -1;                    // negative slots are huge unsigned numbers
-    uint64_t page, pos;
-    if (total <= 0xffffffffull) {                              // a 32-bit division where it is enough
-        const uint32_t p = (uint32_t)slot / (uint32_t)page_size;
-        page = p; pos = (uint32_t)slot - p * (uint32_t)page_size;
-    } else {
-        page = (uint64_t)slot / (uint32_t)page_size; pos = (uint64_t)slot - page * (uint32_t)page_size;
-    }
-    return (int64_t)((page * (uint32_t)heads + (uint32_t)head) * (uint32_t)page_size + pos);
+    int64_t page;
+    if (g.page_shift >= 0) page = slot >> g.page_shift;
+    else if (total <= 0xffffffffull) page = (uint32_t)slot / (uint32_t)g.page_size;       // a 32-bit division where it is enough
+    else page = slot / g.page_size;
+    return (page * g.heads + head) * g.page_size + (slot - page * g.page_size);
 }
 
 template <typename T, bool VEC>
@@ -59,21 +57,29 @@ __device__ __forceinline__ void store_lane(T* p, const float (&f)[kLaneElems]) {
 template <int BITS>
 __device__ __forceinline__ void encode_lane(const float (&f)[kLaneElems], float s, uint8_t* dst) {
     const LevelRule r = level_rule(BITS);
-    const float inv = inverse_scale(s);
-    uint32_t w[2] = {0u, 0u};
+    const float inv = s > 0.0f && s < __int_as_float(0x7f800000) ? __frcp_rn(s) : 0.0f;      // = inverse_scale(s)
+    float t[kLaneElems];
+    shifted_levels<MPQ_ACT_HTANH>(f, inv, r, ordinary(inv) && finite_sum(f) == 0.0f, t);
+    if (BITS == 4) {
+        // two levels a byte, joined as numbers: (2^23 + u) + 16 u' is exact and keeps both in its low byte
 #pragma unroll
-    for (int i = 0; i < kLaneElems; ++i)
-        w[i * BITS / 32] |= level_bits(shifted_level<MPQ_ACT_HTANH>(f[i], inv, r)) << (i * BITS % 32);
-    if (BITS == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint32_t*>(dst) = w[0];
+        for (int i = 0; i < kLaneElems; i += 2) t[i / 2] = fmaf(16.0f, t[i + 1] - kLevelMagic, t[i]);
+    }
+    constexpr int kWords = kLaneElems * BITS / 32;
+    uint32_t w[kWords];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = level_word(t[4 * i], t[4 * i + 1], t[4 * i + 2], t[4 * i + 3]);
+    if constexpr (kWords == 4) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
 }
 template <int BITS>
 __device__ __forceinline__ void decode_lane(const uint8_t* src, float s, float (&f)[kLaneElems]) {
     constexpr int L = (1 << BITS) - 1;
     const float alpha = __fdiv_rn(s, (float)L);
-    uint32_t w[2];
-    if (BITS == 8) { const uint2 r = *reinterpret_cast<const uint2*>(src); w[0] = r.x; w[1] = r.y; }
-    else w[0] = *reinterpret_cast<const uint32_t*>(src);
+    constexpr int kWords = kLaneElems * BITS / 32;
+    uint32_t w[kWords];
+    if constexpr (kWords == 4) { const uint4 v = *reinterpret_cast<const uint4*>(src); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+    else { const uint2 v = *reinterpret_cast<const uint2*>(src); w[0] = v.x; w[1] = v.y; }
 #pragma unroll
     for (int i = 0; i < kLaneElems; ++i) {                 // u into the mantissa of 2^23: no conversion instruction
         const float shifted = __uint_as_float(((w[i * BITS / 32] >> (i * BITS % 32)) & L) | 0x4b000000u);
@@ -81,22 +87,27 @@ __device__ __forceinline__ void decode_lane(const uint8_t* src, float s, float (
     }
 }
 
+// max(m, |a|, |b|), NaNs ignored
+__device__ __forceinline__ float max_abs(float m, float a, float b) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+
 template <typename T, int BITS, bool VEC>
 __global__ void __launch_bounds__(kCacheThreads) cache_write_kernel(const CacheArgs g, int group, int group_log2) {
     chain_entry();
-    const int64_t item = ((int64_t)blockIdx.x * kCacheThreads + threadIdx.x) >> group_log2;
-    const int lane = threadIdx.x & (group - 1);
-    const bool live = item < g.tokens * g.heads && lane * kLaneElems < g.dim;
-    const int64_t token = item / g.heads;
-    const int head = (int)(item - token * g.heads);
+    const int64_t token = ((int64_t)blockIdx.x * kCacheThreads + threadIdx.x) >> group_log2;
+    const int lane = threadIdx.x & (group - 1), head = blockIdx.y;
+    const bool live = token < g.tokens && lane * kLaneElems < g.dim;
     float kf[kLaneElems], vf[kLaneElems], km = 0.0f, vm = 0.0f;
     int64_t row = -1;
     if (live) {
         load_lane<T, VEC>(static_cast<const T*>(g.k) + token * g.k_ts + head * g.k_hs + lane * kLaneElems, kf);
         load_lane<T, VEC>(static_cast<const T*>(g.v) + token * g.v_ts + head * g.v_hs + lane * kLaneElems, vf);
-        row = cache_row(g.slots[token], g.pages, g.page_size, g.heads, head);
+        row = cache_row(g, g.slots[token], head);
 #pragma unroll
-        for (int i = 0; i < kLaneElems; ++i) { km = fmaxf(km, fabsf(kf[i])); vm = fmaxf(vm, fabsf(vf[i])); }
+        for (int i = 0; i < kLaneElems; i += 2) { km = max_abs(km, kf[i], kf[i + 1]); vm = max_abs(vm, vf[i], vf[i + 1]); }
     }
     for (int o = group >> 1; o > 0; o >>= 1) {
         km = fmaxf(km, __shfl_xor_sync(0xffffffffu, km, o));
@@ -112,12 +123,10 @@ __global__ void __launch_bounds__(kCacheThreads) cache_write_kernel(const CacheA
 template <typename T, int BITS, bool VEC>
 __global__ void __launch_bounds__(kCacheThreads) cache_read_kernel(const CacheArgs g, int group, int group_log2) {
     chain_entry();
-    const int64_t item = ((int64_t)blockIdx.x * kCacheThreads + threadIdx.x) >> group_log2;
-    const int lane = threadIdx.x & (group - 1);
-    if (item >= g.tokens * g.heads || lane * kLaneElems >= g.dim) return;
-    const int64_t token = item / g.heads;
-    const int head = (int)(item - token * g.heads);
-    const int64_t row = cache_row(g.slots[token], g.pages, g.page_size, g.heads, head);
+    const int64_t token = ((int64_t)blockIdx.x * kCacheThreads + threadIdx.x) >> group_log2;
+    const int lane = threadIdx.x & (group - 1), head = blockIdx.y;
+    if (token >= g.tokens || lane * kLaneElems >= g.dim) return;
+    const int64_t row = cache_row(g, g.slots[token], head);
     float kf[kLaneElems] = {}, vf[kLaneElems] = {};
     if (row >= 0) {
         const int64_t at = row * (g.dim * BITS / 8) + lane * (kLaneElems * BITS / 8);
@@ -132,11 +141,28 @@ template <typename T, int BITS>
 int launch_cache(bool write, bool vec, const CacheArgs& g, cudaStream_t st) {
     int group = 1, log2 = 0;
     while (group * kLaneElems < g.dim) { group *= 2; ++log2; }
-    const int64_t blocks = ceil_div(g.tokens * g.heads * group, kCacheThreads);
-    if (blocks > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
+    const int64_t blocks = ceil_div(g.tokens * group, kCacheThreads);
+    if (blocks > 0x7fffffff || g.heads > 65535) return MPQ_ERR_BAD_SHAPE;
     auto* kernel = write ? (vec ? cache_write_kernel<T, BITS, true> : cache_write_kernel<T, BITS, false>)
                          : (vec ? cache_read_kernel<T, BITS, true> : cache_read_kernel<T, BITS, false>);
-    return launch_chained(kernel, (unsigned)blocks, kCacheThreads, 0, st, g, group, log2);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)g.heads, 1);
+    cfg.blockDim = dim3(kCacheThreads, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, g, group, log2) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
+    return launch_status();
+}
+
+inline int page_shift(int page_size) {
+    if (page_size <= 0 || (page_size & (page_size - 1))) return -1;
+    int s = 0;
+    while ((1 << s) < page_size) ++s;
+    return s;
 }
 
 int cache_call(bool write, int dtype, int bits, const CacheArgs& g, cudaStream_t st) {
@@ -167,7 +193,7 @@ extern "C" int mpq_cache_write(const void* k, int64_t k_token_stride, int64_t k_
                                uint8_t* k_levels, float* k_scale, uint8_t* v_levels, float* v_scale,
                                int64_t pages, int page_size, void* stream) {
     const CacheArgs g = {k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, slots, tokens, heads, dim,
-                         k_levels, v_levels, k_scale, v_scale, pages, page_size};
+                         k_levels, v_levels, k_scale, v_scale, pages, page_size, page_shift(page_size)};
     return cache_call(true, dtype, bits, g, (cudaStream_t)stream);
 }
 
@@ -177,6 +203,6 @@ extern "C" int mpq_cache_read(const uint8_t* k_levels, const float* k_scale, con
                               void* v, int64_t v_token_stride, int64_t v_head_stride, int dtype, void* stream) {
     const CacheArgs g = {k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, slots, tokens, heads, dim,
                          const_cast<uint8_t*>(k_levels), const_cast<uint8_t*>(v_levels), const_cast<float*>(k_scale),
-                         const_cast<float*>(v_scale), pages, page_size};
+                         const_cast<float*>(v_scale), pages, page_size, page_shift(page_size)};
     return cache_call(false, dtype, bits, g, (cudaStream_t)stream);
 }

@@ -90,12 +90,19 @@ __device__ __forceinline__ void store_part(T* p, const float (&f)[N], int count)
         for (int i = 0; i < N; ++i) if (i < count) p[i] = from_f32<T>(f[i]);
     }
 }
-// Level rows are 16-byte aligned and padded: whole words always fit (u past the row's end is 0).
-template <int N>
-__device__ __forceinline__ void store_levels(uint8_t* p, const uint32_t (&u)[N]) {
+// Level bytes of N elements, `count` of them inside the row; returns the sum of the levels.  Level rows are 16-byte
+// aligned and padded, so whole words always fit; bytes past the row's end are 0.
+template <int N, bool VECTOR>
+__device__ __forceinline__ uint32_t store_levels(uint8_t* p, const float (&shifted)[N], int count) {
+    uint32_t total = 0;
 #pragma unroll
-    for (int c = 0; c < N / 4; ++c)
-        reinterpret_cast<uint32_t*>(p)[c] = __byte_perm(__byte_perm(u[4 * c], u[4 * c + 1], 0x0040), __byte_perm(u[4 * c + 2], u[4 * c + 3], 0x0040), 0x5410);
+    for (int c = 0; c < N / 4; ++c) {
+        uint32_t w = level_word(shifted[4 * c], shifted[4 * c + 1], shifted[4 * c + 2], shifted[4 * c + 3]);
+        if (!VECTOR) w &= count >= 4 * c + 4 ? 0xffffffffu : count <= 4 * c ? 0u : 0xffffffffu >> (8 * (4 * c + 4 - count));
+        reinterpret_cast<uint32_t*>(p)[c] = w;
+        total = __dp4a(w, 0x01010101u, total);
+    }
+    return total;
 }
 template <int N, bool VECTOR>
 __device__ __forceinline__ void store_values(const RowArgs& g, int64_t row, int64_t at, const float (&shifted)[N], float alpha, int count) {
@@ -168,21 +175,20 @@ level_rows_kernel(const RowArgs g) {
     }
     const RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
     const float r = c.r, s = c.s, inv = c.inv, alpha = c.alpha;
+    // (a NaN range, after a NaN or an infinity under the norm, has the reciprocal 0 and is not ordinary)
+    const bool plain = ordinary(s) && ordinary(inv);
     uint8_t* out = g.levels + row * g.row_bytes;
     int total = 0;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int i = threadIdx.x + j * blockDim.x;
         if (i < nvec) {
-            uint32_t u[VEC];
+            float y[VEC], shifted[VEC];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                h[j][e] = shifted_level<ACT>(NORM ? h[j][e] * r : h[j][e], inv, g.rule);
-                u[e] = !VECTOR && i * VEC + e >= k ? 0u : level_bits(h[j][e]);
-                total += (int)u[e];
-            }
-            store_levels<VEC>(out + (int64_t)i * VEC, u);
-            if (g.values) store_values<VEC, VECTOR>(g, row, (int64_t)i * VEC, h[j], alpha, k - i * VEC);
+            for (int e = 0; e < VEC; ++e) y[e] = NORM ? h[j][e] * r : h[j][e];
+            shifted_levels<ACT>(y, inv, g.rule, plain && finite_sum(y) == 0.0f, shifted);
+            total += (int)store_levels<VEC, VECTOR>(out + (int64_t)i * VEC, shifted, k - i * VEC);
+            if (g.values) store_values<VEC, VECTOR>(g, row, (int64_t)i * VEC, shifted, alpha, k - i * VEC);
         }
     }
     // padding words behind the last vector
@@ -227,9 +233,12 @@ level_wide_rows_kernel(const RowArgs g) {
             if (g.gain) h *= g.gain[i];
             h *= r;
         }
-        const float shifted[1] = {shifted_level<ACT>(h, inv, g.rule)};
-        total += (int)level_bits(shifted[0]);
-        out[i] = (uint8_t)level_bits(shifted[0]);
+        const float y[1] = {h};
+        float shifted[1];
+        shifted_levels<ACT>(y, inv, g.rule, false, shifted);
+        const uint8_t u = (uint8_t)__float_as_uint(shifted[0]);
+        total += u;
+        out[i] = u;
         if (g.values) store_values<1, false>(g, row, i, shifted, alpha, 1);
     }
     block_level_sum(total, g.sums + row, sh_sum);

@@ -85,17 +85,40 @@ __host__ __device__ inline LevelRule level_rule(int bits) {
     return r;
 }
 
-// level_index() without a conversion instruction (those run at an eighth of the rate): the clamped quotient plus
-// 2^23 + H, rounded down, holds floor(y) + H in its low mantissa bits, and float(u) is one subtraction away.
+// level_index() without a conversion instruction (those run at an eighth of the rate): the quotient plus 2^23 + H,
+// rounded down, holds floor(y) + H in its low mantissa bits, and float(u) is one subtraction away.
+// Where the range is the row's own largest magnitude, finite with a finite reciprocal, and no element is a NaN, the
+// quotient lies in [-L/2, L/2] up to two roundings, inside [-H, H): `plain` leaves the NaN test and both clamps out.
 constexpr float kLevelMagic = 8388608.0f;                  // 2^23, bits 0x4b000000
-template <int ACT>
-__device__ __forceinline__ float shifted_level(float x, float inv_s, const LevelRule& r) {
-    float y = __fmul_rn(__fmul_rn(x, inv_s), r.half_L);
-    if (!(y == y)) y = 0.0f;                               // NaN -> level just above zero
-    if (ACT == MPQ_ACT_HRELU) y = fmaxf(y, 0.0f);
-    return __fadd_rd(fminf(fmaxf(y, r.lo), r.hi), r.magic);
+template <int ACT, int N>
+__device__ __forceinline__ void shifted_levels(const float (&x)[N], float inv_s, const LevelRule& r, bool plain, float (&shifted)[N]) {
+    if (ACT == MPQ_ACT_HTANH && plain) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) shifted[i] = __fadd_rd(__fmul_rn(__fmul_rn(x[i], inv_s), r.half_L), r.magic);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float y = __fmul_rn(__fmul_rn(x[i], inv_s), r.half_L);
+            if (!(y == y)) y = 0.0f;                       // NaN -> level just above zero
+            if (ACT == MPQ_ACT_HRELU) y = fmaxf(y, 0.0f);
+            shifted[i] = __fadd_rd(fminf(fmaxf(y, r.lo), r.hi), r.magic);
+        }
+    }
 }
-__device__ __forceinline__ uint32_t level_bits(float shifted) { return __float_as_uint(shifted) & 0xffu; }       // u
+// Zero, or NaN where an element is not finite: one multiply-add per element instead of a test.
+template <int N>
+__device__ __forceinline__ float finite_sum(const float (&x)[N]) {
+    float z = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) z = fmaf(x[i], 0.0f, z);
+    return z;
+}
+__device__ __forceinline__ bool ordinary(float v) { return fabsf(v) < __int_as_float(0x7f800000); }             // neither NaN nor infinite
+// Level bytes of four shifted levels (a level is below 2^8: the low byte of the float's bits).
+__device__ __forceinline__ uint32_t level_word(float a, float b, float c, float d) {
+    return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040),
+                       __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+}
 __device__ __forceinline__ float level_number(float shifted, const LevelRule& r) {                              // 2u - L, exact
     return fmaf(2.0f, shifted - kLevelMagic, -(float)r.L);
 }
