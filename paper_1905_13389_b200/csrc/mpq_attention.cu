@@ -25,35 +25,40 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-// Operands are the level INDICES behind a power of two, fp16 1024 + u (8 bits: u below 0x64) or 16 + u (4 bits: u in
-// bits 6-9 of 0x4c00), which a byte permutation or one shift and mask make; with OFFSET = 1024 or 16
-//   2u - L = 2 (OFFSET + u) - (2 OFFSET + L),
-// so one term per row, (2 OFFSET + L) times the sum of q or of w, turns the products into those of the levels.  The
-// terms cancel to 1/30 (8 bits) of their size at most on typical levels: 5 bits of the 24 that the sums carry.
-template <int BITS> struct Shifted { static constexpr float offset = BITS == 8 ? 1024.0f : 16.0f, correction = 2.0f * offset + (float)((1 << BITS) - 1); };
-__device__ __forceinline__ uint32_t shifted_nibbles(uint32_t x, int i) {
-    return ((i == 0 ? x << 6 : i == 1 ? x << 2 : i == 2 ? x >> 2 : x >> 6) & 0x03c003c0u) | 0x4c004c00u;
+// Operands are the even neighbours below the levels, 2u - (L + 1), exact in fp16: the level index behind a power of
+// two, 1024 + u (8 bits: u below 0x64) or 16 + u (4 bits: u in bits 6-9 of 0x4c00), is a byte permutation or one shift
+// and mask, and one packed multiply-add takes the power away.  The missing 1 comes back as one term per row, the sum of
+// q or of w.  (The multiply-add cannot be left to such a term as well: over a long context the sum of w (1024 + u) is
+// some 400 times the result, and the tensor cores' truncated sums then cost half of its bits.)
+template <int BITS>
+__device__ __forceinline__ uint32_t even_level(uint32_t x) {
+    constexpr float c = BITS == 8 ? -2304.0f : -48.0f;
+    const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&x), __float2half2_rn(2.0f), __float2half2_rn(c));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t even_nibbles(uint32_t x, int i) {
+    return even_level<4>(((i == 0 ? x << 6 : i == 1 ? x << 2 : i == 2 ? x >> 2 : x >> 6) & 0x03c003c0u) | 0x4c004c00u);
 }
 // Word of level bytes -> operand register `pair` (0, 1: BITS = 8; 0..3: BITS = 4): elements pair*2, pair*2+1
 // of the word for 8 bits, pair and pair + 4 for 4 bits.
 template <int BITS>
 __device__ __forceinline__ uint32_t key_pair(uint32_t w, int pair) {
-    if (BITS == 8) return __byte_perm(w, 0x64646464u, pair ? 0x4342 : 0x4140);
-    return shifted_nibbles(w, pair);
+    if (BITS == 8) return even_level<8>(__byte_perm(w, 0x64646464u, pair ? 0x4342 : 0x4140));
+    return even_nibbles(w, pair);
 }
 // The words of two tokens -> operand registers of their elements side by side, `count` = 32 / BITS of them.
 template <int BITS>
 __device__ __forceinline__ void value_pairs(uint32_t a, uint32_t b, uint32_t* v) {
     if (BITS == 8) {
         const uint32_t lo = __byte_perm(a, b, 0x5140), hi = __byte_perm(a, b, 0x7362);       // a0 b0 a1 b1, a2 b2 a3 b3
-        v[0] = __byte_perm(lo, 0x64646464u, 0x4140);
-        v[1] = __byte_perm(lo, 0x64646464u, 0x4342);
-        v[2] = __byte_perm(hi, 0x64646464u, 0x4140);
-        v[3] = __byte_perm(hi, 0x64646464u, 0x4342);
+        v[0] = even_level<8>(__byte_perm(lo, 0x64646464u, 0x4140));
+        v[1] = even_level<8>(__byte_perm(lo, 0x64646464u, 0x4342));
+        v[2] = even_level<8>(__byte_perm(hi, 0x64646464u, 0x4140));
+        v[3] = even_level<8>(__byte_perm(hi, 0x64646464u, 0x4342));
     } else {
         const uint32_t lo = __byte_perm(a, b, 0x5410), hi = __byte_perm(a, b, 0x7632);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = shifted_nibbles(lo, i); v[4 + i] = shifted_nibbles(hi, i); }
+        for (int i = 0; i < 4; ++i) { v[i] = even_nibbles(lo, i); v[4 + i] = even_nibbles(hi, i); }
     }
 }
 // Position inside a row of the element that operand register `pair` of word `word` holds in its low half
@@ -198,7 +203,7 @@ attn_rows_kernel(const AttnArgs g) {
 
     // ---- queries: row gr (+ 8) of the tile as operand fragments
     uint32_t qf[NQ][kSteps][2];
-    float row_scale[NQ][2], q_term[NQ][2];                // of rows 2 t4 + e (+ 8): the columns of this lane's scores
+    float row_scale[NQ][2], q_sum[NQ][2];                 // of rows 2 t4 + e (+ 8): the columns of this lane's scores
     int first[NQ][2], last[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
@@ -227,7 +232,7 @@ attn_rows_kernel(const AttnArgs g) {
         for (int e = 0; e < 2; ++e) {
             const int src = (t4 * 2 + e) * 4;
             row_scale[n][e] = __shfl_sync(0xffffffffu, up, src) * g.scale_log2;
-            q_term[n][e] = -Shifted<BITS>::correction * __shfl_sync(0xffffffffu, sum, src);
+            q_sum[n][e] = __shfl_sync(0xffffffffu, sum, src);
             first[n][e] = __shfl_sync(0xffffffffu, from, src);
             last[n][e] = __shfl_sync(0xffffffffu, upto, src);
         }
@@ -298,7 +303,7 @@ attn_rows_kernel(const AttnArgs g) {
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float y = fmaf(fmaf(2.0f, s[k][n][h * 2 + e] + s_odd[k][n][h * 2 + e], q_term[n][e]) * kj, row_scale[n][e], lj);
+                        float y = fmaf((s[k][n][h * 2 + e] + s_odd[k][n][h * 2 + e] + q_sum[n][e]) * kj, row_scale[n][e], lj);
                         if (partial && (c0 + src < first[n][e] || c0 + src > last[n][e])) y = -INFINITY;
                         s[k][n][h * 2 + e] = y;
                         top[n][e] = fmaxf(top[n][e], y);
@@ -380,10 +385,9 @@ attn_rows_kernel(const AttnArgs g) {
             }
             const int r = n * 8 + t4 * 2 + e;
             if (gr == 0) { sh_ml[warp][r][0] = m[n][e]; sh_ml[warp][r][1] = l[n][e]; }
-            const float w_term = -Shifted<BITS>::correction * wsum[n][e];
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
-                *reinterpret_cast<float2*>(&sh_o[warp][r][gr * (D / 8) + 2 * i]) = make_float2(fmaf(2.0f, o[i][n][e], w_term), fmaf(2.0f, o[i][n][2 + e], w_term));
+                *reinterpret_cast<float2*>(&sh_o[warp][r][gr * (D / 8) + 2 * i]) = make_float2(o[i][n][e] + wsum[n][e], o[i][n][2 + e] + wsum[n][e]);
         }
     __syncthreads();
     constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);

@@ -265,6 +265,26 @@ def test_split_contexts_and_launch_hints(mpq, cuda, q_lens, kv_lens, bits):
     c.check(window=700)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("q_len", [1, 4, 40])
+def test_long_contexts_keep_their_precision(mpq, cuda, q_len, bits):
+    """Over 16,000 tokens the result is an average some hundred times smaller than the values, and sums that carried more
+    than the levels themselves (an offset, say) would lose it.  fp16: rounding the result moves it by at most 2^-11 of its
+    size, 2^-11 / sqrt(3) = 2.8e-4 of it in the root mean square, and rounding each weight does the same to sums of random
+    sign: 4e-4 together, 6e-4 with the scores' own errors."""
+    c = Case(mpq, cuda, [q_len], [16000], 4, 1, 64, bits, 16, torch.float16)
+    out, _ = c.run(scale=0.01, max_kv=1)                     # nearly equal weights, and no split of the context
+    j = np.arange(16000)
+    p, o, L = c.table[0, j // 16], j % 16, (1 << bits) - 1
+    k, v = ((2 * c.u[i][p, 0, o] - L) * (c.s[i][p, 0, o].astype(np.float64) / L)[:, None] for i in (0, 1))
+    x = np.einsum("ihd,jd->ihj", c.q.double().numpy(), k) * 0.01
+    x = np.where(j[None, None] <= 16000 - q_len + np.arange(q_len)[:, None, None], x, -np.inf)
+    w = np.exp(x - x.max(2, keepdims=True))
+    ref = (w @ v) / w.sum(2, keepdims=True)
+    err = out.double().cpu().numpy() - ref
+    assert np.linalg.norm(err) < 6e-4 * np.linalg.norm(ref)
+
+
 @pytest.mark.parametrize("q_lens", [[1, 1], [3, 2], [150, 140]])
 def test_ranges_of_every_size(mpq, cuda, q_lens):
     """Ranges from 2^-60 to 2^60 among the values, sharp and flat scores, tiny and huge queries, zero ranges."""
