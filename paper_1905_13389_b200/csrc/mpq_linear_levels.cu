@@ -76,7 +76,7 @@ __device__ unsigned int g_wait_failures;                  // waits that ran out,
 // tile is split over a cluster of S CTAs, which exchange their integer partial sums through distributed
 // shared memory (exact, so any order gives the same result) -- CTA i finishes rows i BN/S .. of the tile.
 template <int BN> struct SmallShape {
-    static constexpr int stages = BN == 16 ? 10 : BN == 32 ? 8 : BN == 64 ? 6 : 4;
+    static constexpr int stages = BN == 16 ? 10 : BN == 32 ? 8 : 6;
     static constexpr int stage_bytes = (128 + BN) * kBlock;
     static constexpr int exchange_bytes = BN * 128 * 4;   // [S source CTAs][BN / S rows][128 columns] int32
     static constexpr int smem = stages * stage_bytes + exchange_bytes + 1024;
@@ -253,29 +253,31 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     if (threadIdx.x == 0 && failed) atomicAdd(&g_wait_failures, 1u);
 }
 
-// ---- many rows: 256 x BN tiles on CTA pairs.  One CTA alone cannot feed kind::i8: a 128 x 256 x 32 product
-// takes 128 cycles and reads 12 KB of operands while 12 KB of new ones arrive, 1.5 times the 128 bytes a cycle
-// of shared memory.  The pair (cta_group::2) shares the BN operand rows, each CTA holds half of them: 8 + 8 KB
-// per 128 cycles for BN = 256.  Persistent: pair p takes tiles p, p + pairs, ...; two accumulators in TMEM,
-// so a tile is stored while the next one is multiplied.  The store goes through a shared-memory
-// transpose, after which a lane owns two adjacent columns (their constants in registers) and a warp writes
-// whole row pieces whatever the row stride is.
+// ---- many rows: 256 x 128 tiles on CTA pairs (cta_group::2).  The pair shares the 128 operand rows of the weights,
+// each CTA holds half of them and 128 of the 256 activation rows.  Persistent: pair p takes tiles p, p + pairs, ...;
+// two accumulators in TMEM, so a tile is stored while the next one is multiplied.  The store goes through a
+// shared-memory transpose, after which a lane owns two columns (their constants in registers) and a warp writes whole
+// row pieces whatever the row stride is.
+// What bounds it: the operands' way from L2, 24 KB per CTA and 128 bytes of k, some 45 bytes a cycle and multiprocessor;
+// 4096^3 takes 55 us bare and 61 with bias and GELU, 2.5 and 2.26 POP/s, tensor pipes 57 % active.  256 x 256 tiles read a
+// quarter less but leave the last of their 3.5 rounds half empty: 62 us; 1024 x 4096 x 4096 23.5, these 22.0.
 constexpr int kPairStoreWarps = 8;                        // two per quarter of the TMEM lanes, each with half of the columns
 constexpr int kPairThreads = 64 + 32 * kPairStoreWarps;
-template <int BN> struct PairShape {
-    static constexpr int stage_bytes = (128 + BN / 2) * kBlock;     // per CTA
-    static constexpr int stages = BN == 256 ? 5 : BN == 128 ? 6 : 7;
+constexpr int kPairCols = 128;
+struct PairShape {
+    static constexpr int stage_bytes = (128 + kPairCols / 2) * kBlock;   // per CTA
+    static constexpr int stages = 6;
     static constexpr int row_words = 64;                            // column pair p of row r lies at pair p ^ r: no bank conflicts either way
     static constexpr int transpose_bytes = kPairStoreWarps * 32 * row_words * 4;
     static constexpr int smem = stages * stage_bytes + transpose_bytes + 1024;
 };
 
-template <typename T, int BN>
+template <typename T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const LinearArgs g,
                    int tiles_m, int tiles) {
-    using Shape = PairShape<BN>;
-    constexpr int kStages = Shape::stages, kAccs = 2;
+    using Shape = PairShape;
+    constexpr int BN = kPairCols, kStages = Shape::stages, kAccs = 2;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kAccs];
     __shared__ uint32_t tmem_holder;
@@ -509,11 +511,12 @@ int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
     return launch_status();
 }
 
-template <typename T, int BN>
+template <typename T>
 int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
-    using Shape = PairShape<BN>;
+    using Shape = PairShape;
+    constexpr int BN = kPairCols;
     static PerDeviceOnce once;
-    auto* kernel = linear_pair_kernel<T, BN>;
+    auto* kernel = linear_pair_kernel<T>;
     int rc = once.raise_smem_limit(kernel, Shape::smem);
     if (rc != MPQ_OK) return rc;
     CUtensorMap map_w, map_a;
@@ -526,25 +529,17 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     return launch_chained_as(true, kernel, ctas, (unsigned)kPairThreads, Shape::smem, st, map_a, map_w, g, (int)tiles_m, (int)tiles);
 }
 
-// Which form, by estimated cycles per multiprocessor: a k block of 128 bytes takes a pair 2 BN cycles (the 8-bit rate)
-// and an unpaired 128 x BN tile 2 (128 + BN) (its shared memory), a tile's store some 16 BN, and starting up,
-// exchanging partial sums and draining about 5000 in the small form.
+// Which form.  Up to 64 rows the weights' own traffic decides: the small form, its tile just wide enough.  Above, CTA
+// pairs, unless their 256 x 128 tiles are so few that splitting k pays more than reading the weights once: us for
+// m x n x k, pairs / small with 64 rows --
+//   16 tiles: 300 x 1000 x 9000 29 / 22, 1000 x 500 x 500 10.6 / 11.7;  8 tiles: 256 x 1024 x 1024 10.4 / 9.4;
+//   32 tiles: 200 x 4096 x 4096 17 / 24;  71 tiles: 130 x 9000 x 1000 15 / 27.
 template <typename T>
 int launch_linear_levels(const LinearArgs& g, cudaStream_t st) {
     if (g.m <= 16) return launch_linear_small<T, 16>(g, st);
     if (g.m <= 32) return launch_linear_small<T, 32>(g, st);
-    if (g.m <= 64) return launch_linear_small<T, 64>(g, st);
-    const int64_t sms = sm_count(), blocks = ceil_div(g.row_bytes, kBlock);
-    if (sms < 2) return MPQ_ERR_CUDA;
-    auto pair_cost = [&](int64_t bn) {
-        return ceil_div(ceil_div(g.m, 256) * ceil_div(g.n, bn), sms / 2) * (blocks * 2 * bn + 16 * bn);
-    };
-    const int64_t small_tiles = ceil_div(g.m, 128) * ceil_div(g.n, 128);
-    const int64_t splits = small_splits(small_tiles, blocks, 128, sms);
-    const int64_t small_cost = ceil_div(small_tiles * splits, sms) * (blocks / splits * 512 + 16 * 128) + 5000;
-    const int64_t wide = pair_cost(256), narrow = pair_cost(128);
-    if (g.m <= 128 || small_cost < (wide < narrow ? wide : narrow)) return launch_linear_small<T, 128>(g, st);
-    return wide <= narrow ? launch_linear_pair<T, 256>(g, st) : launch_linear_pair<T, 128>(g, st);
+    if (g.m <= 64 || ceil_div(g.m, 256) * ceil_div(g.n, kPairCols) < 24) return launch_linear_small<T, 64>(g, st);
+    return launch_linear_pair<T>(g, st);
 }
 
 }  // namespace mpq
