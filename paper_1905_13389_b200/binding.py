@@ -23,6 +23,7 @@ ACT_HTANH, ACT_HRELU = 0, 1
 ENC_LEVELS, ENC_TRIG = 0, 1
 
 _lib = None
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 class MpqError(RuntimeError):
@@ -130,7 +131,7 @@ def _check(status: int, where: str):
 
 def _stream() -> int:
     """The current stream of the current device (asked for by number: a torch.cuda.Stream object costs as much as a small kernel)."""
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return _raw_stream(_current_device())
 
 
 def _ptr(t: Optional[torch.Tensor], dtype=None) -> Optional[int]:
@@ -452,9 +453,10 @@ _DTYPE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
 
 def _dtype(t: torch.dtype) -> int:
-    if t not in _DTYPE:
+    d = _DTYPE.get(t)
+    if d is None:
         raise ValueError("expected float32, float16 or bfloat16, got %s" % t)
-    return _DTYPE[t]
+    return d
 
 
 class Levels(NamedTuple):
@@ -487,11 +489,9 @@ def _expected(t, shape, dtype):
         tuple(shape), "" if dtype is None else " and dtype %s" % dtype, t.dtype, tuple(t.shape), tuple(t.stride()), t.device))
 
 
-def _rows(t: Optional[torch.Tensor], rows: int, k: int, dtype=None):
-    """(pointer, row stride) of a [rows x k] matrix whose rows are contiguous; (None, 0) for None."""
-    if t is None:
-        return None, 0
-    if not t.is_cuda or t.shape != (rows, k) or (dtype is not None and t.dtype != dtype):
+def _rows(t: torch.Tensor, rows: int, k: int, dtype):
+    """(pointer, row stride) of a [rows x k] matrix whose rows are contiguous."""
+    if t.shape != (rows, k) or t.dtype is not dtype or not t.is_cuda:
         _expected(t, (rows, k), dtype)
     stride, step = t.stride()
     if step != 1 and k > 1:
@@ -499,9 +499,9 @@ def _rows(t: Optional[torch.Tensor], rows: int, k: int, dtype=None):
     return t.data_ptr(), stride if rows > 1 else k
 
 
-def _heads(t: torch.Tensor, tokens: int, heads: int, dim: int, dtype=None):
+def _heads(t: torch.Tensor, tokens: int, heads: int, dim: int, dtype):
     """(pointer, token stride, head stride) of a [tokens][heads][dim] tensor whose head rows are contiguous."""
-    if not t.is_cuda or t.shape != (tokens, heads, dim) or (dtype is not None and t.dtype != dtype):
+    if t.shape != (tokens, heads, dim) or t.dtype is not dtype or not t.is_cuda:
         _expected(t, (tokens, heads, dim), dtype)
     st, sh, step = t.stride()
     if step != 1:
@@ -509,29 +509,47 @@ def _heads(t: torch.Tensor, tokens: int, heads: int, dim: int, dtype=None):
     return t.data_ptr(), st if tokens > 1 else heads * dim, sh if heads > 1 else dim
 
 
-def _vector(t: Optional[torch.Tensor], n: int, dtype) -> Optional[int]:
-    """Pointer of n contiguous values; None for None."""
-    if t is None:
-        return None
-    if not t.is_cuda or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+def _vector(t: torch.Tensor, n: int, dtype) -> int:
+    """Pointer of n contiguous values."""
+    if t.numel() != n or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise ValueError("expected %d contiguous %s values on a CUDA device, got %d of %s on %s" % (n, dtype, t.numel(), t.dtype, t.device))
     return t.data_ptr()
 
 
+_NO_ROWS, _NO_VALUES = (None, 0), (None, 0, 0)
+
+
 def _held(lv: Levels, rows: int, k: int):
     """Pointers of level bytes, ranges and sums, after comparing their sizes."""
-    row = -(-k // 16) * 16
-    if lv.k != k or lv.bytes.shape != (rows, row):
+    held, scale, sums, _, lk = lv
+    row = (k + 15) // 16 * 16
+    if lk != k or held.shape != (rows, row):
         raise ValueError("expected levels of %d rows of %d elements (%d bytes apart), got k = %d and bytes %s" % (
-            rows, k, row, lv.k, tuple(lv.bytes.shape)))
-    return _vector(lv.bytes, rows * row, torch.uint8), _vector(lv.scale, rows, torch.float32), _vector(lv.sums, rows, torch.int32)
+            rows, k, row, lk, tuple(held.shape)))
+    return _vector(held, rows * row, torch.uint8), _vector(scale, rows, torch.float32), _vector(sums, rows, torch.int32)
 
 
-def _new_levels(rows: int, k: int, bits: int, device) -> Levels:
-    row = -(-k // 16) * 16
-    return Levels(torch.empty_strided((rows, row), (row, 1), dtype=torch.uint8, device=device),
-                  torch.empty_strided((rows,), (1,), dtype=torch.float32, device=device),
-                  torch.empty_strided((rows,), (1,), dtype=torch.int32, device=device), bits, k)
+def _new_levels(rows: int, k: int, bits: int, device):
+    """Level outputs and their pointers."""
+    row = (k + 15) // 16 * 16
+    held = torch.empty_strided((rows, row), (row, 1), dtype=torch.uint8, device=device)
+    scale = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=device)
+    sums = torch.empty_strided((rows,), (1,), dtype=torch.int32, device=device)
+    return Levels(held, scale, sums, bits, k), (held.data_ptr(), scale.data_ptr(), sums.data_ptr())
+
+
+def _level_outputs(out: Optional[Levels], rows: int, k: int, bits: int, device):
+    if out is None:
+        return _new_levels(rows, k, bits, device)
+    if out.bits != bits:
+        raise ValueError("the output levels are of another width")
+    return out, _held(out, rows, k)
+
+
+def _values(values: torch.Tensor, rows: int, k: int):
+    """(pointer, dtype, row stride) of the decoded output."""
+    p, stride = _rows(values, rows, k, values.dtype)
+    return p, _dtype(values.dtype), stride
 
 
 def rmsnorm_levels(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float, bits: int = 8,
@@ -541,34 +559,28 @@ def rmsnorm_levels(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float, bi
     x + residual (it may be x or residual), values the numbers that the levels stand for."""
     rows, k = x.shape
     dtype = x.dtype
-    if out is None:
-        out = _new_levels(rows, k, bits, x.device)
-    elif out.bits != bits:
-        raise ValueError("the output levels are of another width")
-    _check(lib().mpq_rmsnorm_levels(*_rows(x, rows, k), *_rows(residual, rows, k, dtype), _dtype(dtype), _vector(gain, k, torch.float32),
-                                    eps, rows, k, bits, *_rows(residual_out, rows, k, dtype), *_held(out, rows, k),
-                                    *_values(values, rows, k), _stream()), "mpq_rmsnorm_levels")
+    px = _rows(x, rows, k, dtype)
+    out, po = _level_outputs(out, rows, k, bits, x.device)
+    st = (_lib or lib()).mpq_rmsnorm_levels(
+        *px, *(_NO_ROWS if residual is None else _rows(residual, rows, k, dtype)), _dtype(dtype),
+        None if gain is None else _vector(gain, k, torch.float32), eps, rows, k, bits,
+        *(_NO_ROWS if residual_out is None else _rows(residual_out, rows, k, dtype)), *po,
+        *(_NO_VALUES if values is None else _values(values, rows, k)), _raw_stream(_current_device()))
+    if st:
+        raise MpqError(st, "mpq_rmsnorm_levels")
     return out
-
-
-def _values(values: Optional[torch.Tensor], rows: int, k: int):
-    """(pointer, dtype, row stride) of the optional decoded output."""
-    if values is None:
-        return None, 0, 0
-    p, stride = _rows(values, rows, k)
-    return p, _dtype(values.dtype), stride
 
 
 def encode_levels(x: torch.Tensor, bits: int = 8, act: int = ACT_HTANH, values: Optional[torch.Tensor] = None,
                   out: Optional[Levels] = None) -> Levels:
     """[rows x k] -> level bytes with one range per row (weights, once; activations inside a block)."""
     rows, k = x.shape
-    if out is None:
-        out = _new_levels(rows, k, bits, x.device)
-    elif out.bits != bits:
-        raise ValueError("the output levels are of another width")
-    _check(lib().mpq_encode_levels(*_rows(x, rows, k), _dtype(x.dtype), rows, k, act, bits, *_held(out, rows, k),
-                                   *_values(values, rows, k), _stream()), "mpq_encode_levels")
+    px = _rows(x, rows, k, x.dtype)
+    out, po = _level_outputs(out, rows, k, bits, x.device)
+    st = (_lib or lib()).mpq_encode_levels(*px, _dtype(x.dtype), rows, k, act, bits, *po,
+                                           *(_NO_VALUES if values is None else _values(values, rows, k)), _raw_stream(_current_device()))
+    if st:
+        raise MpqError(st, "mpq_encode_levels")
     return out
 
 
@@ -584,14 +596,13 @@ def linear_levels(a: Levels, w: Levels, bias: Optional[torch.Tensor] = None, act
         out = torch.empty_strided((m, n), (n, 1), dtype=dtype, device=a.bytes.device)
     else:
         dtype = out.dtype
-    _check(lib().mpq_linear_levels(*pa, a.bits, *pw, w.bits, m, n, k, _vector(bias, n, torch.float32), GLUE[act],
-                                   *_rows(residual, m, n, dtype), *_out(out, m, n, dtype), _stream()), "mpq_linear_levels")
+    po, ldo = _rows(out, m, n, dtype)
+    st = (_lib or lib()).mpq_linear_levels(
+        *pa, a.bits, *pw, w.bits, m, n, k, None if bias is None else _vector(bias, n, torch.float32), GLUE[act],
+        *(_NO_ROWS if residual is None else _rows(residual, m, n, dtype)), po, _dtype(dtype), ldo, _raw_stream(_current_device()))
+    if st:
+        raise MpqError(st, "mpq_linear_levels")
     return out
-
-
-def _out(out: torch.Tensor, m: int, n: int, dtype):
-    p, stride = _rows(out, m, n)
-    return p, _dtype(dtype), stride
 
 
 def level_cache(pages: int, heads: int, page_size: int, dim: int, bits: int, device="cuda") -> LevelCache:
@@ -603,23 +614,27 @@ def level_cache(pages: int, heads: int, page_size: int, dim: int, bits: int, dev
 
 def _cache(c: LevelCache):
     """(pages, heads, page size, dim) and the four pointers of a cache."""
-    shape = c.k.shape
-    pages, heads, page_size, row = shape
+    k, k_scale, v, v_scale, bits = c
+    pages, heads, page_size, row = k.shape
     n = pages * heads * page_size
-    if c.v.shape != shape:
-        raise ValueError("the cache's keys and values differ in shape: %s and %s" % (tuple(shape), tuple(c.v.shape)))
-    return (pages, heads, page_size, row * 8 // c.bits if c.bits else 0), (
-        _vector(c.k, n * row, torch.uint8), _vector(c.k_scale, n, torch.float32), _vector(c.v, n * row, torch.uint8), _vector(c.v_scale, n, torch.float32))
+    return (pages, heads, page_size, row * 8 // bits if bits else 0), (
+        _vector(k, n * row, torch.uint8), _vector(k_scale, n, torch.float32), _vector(v, n * row, torch.uint8), _vector(v_scale, n, torch.float32))
 
 
 def cache_write(cache: LevelCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> LevelCache:
     """Quantizes keys and values [tokens][heads][dim] into the cache at ``slots`` (int64; -1: not written)."""
     (pages, heads, page_size, dim), held = _cache(cache)
     tokens, dtype = k.shape[0], k.dtype
-    _check(lib().mpq_cache_write(*_heads(k, tokens, heads, dim), *_heads(v, tokens, heads, dim, dtype), _dtype(dtype),
-                                 _vector(slots, tokens, torch.int64), tokens, heads, dim, cache.bits, *held, pages, page_size, _stream()),
-           "mpq_cache_write")
+    st = (_lib or lib()).mpq_cache_write(
+        *_heads(k, tokens, heads, dim, dtype), *_heads(v, tokens, heads, dim, dtype), _dtype(dtype), _vector(slots, tokens, torch.int64),
+        tokens, heads, dim, cache.bits, *held, pages, page_size, _raw_stream(_current_device()))
+    if st:
+        raise MpqError(st, "mpq_cache_write")
     return cache
+
+
+def _new_heads(tokens: int, heads: int, dim: int, dtype, device) -> torch.Tensor:
+    return torch.empty_strided((tokens, heads, dim), (heads * dim, dim, 1), dtype=dtype, device=device)
 
 
 def cache_read(cache: LevelCache, slots: torch.Tensor, dtype: torch.dtype, k: Optional[torch.Tensor] = None,
@@ -628,12 +643,14 @@ def cache_read(cache: LevelCache, slots: torch.Tensor, dtype: torch.dtype, k: Op
     (pages, heads, page_size, dim), held = _cache(cache)
     tokens = slots.numel()
     if k is None:
-        k = torch.empty_strided((tokens, heads, dim), (heads * dim, dim, 1), dtype=dtype, device=slots.device)
+        k = _new_heads(tokens, heads, dim, dtype, slots.device)
     if v is None:
-        v = torch.empty_strided((tokens, heads, dim), (heads * dim, dim, 1), dtype=dtype, device=slots.device)
-    _check(lib().mpq_cache_read(*held, pages, page_size, _vector(slots, tokens, torch.int64), tokens, heads, dim, cache.bits,
-                                *_heads(k, tokens, heads, dim, dtype), *_heads(v, tokens, heads, dim, dtype), _dtype(dtype), _stream()),
-           "mpq_cache_read")
+        v = _new_heads(tokens, heads, dim, dtype, slots.device)
+    st = (_lib or lib()).mpq_cache_read(
+        *held, pages, page_size, _vector(slots, tokens, torch.int64), tokens, heads, dim, cache.bits,
+        *_heads(k, tokens, heads, dim, dtype), *_heads(v, tokens, heads, dim, dtype), _dtype(dtype), _raw_stream(_current_device()))
+    if st:
+        raise MpqError(st, "mpq_cache_read")
     return k, v
 
 
@@ -652,18 +669,21 @@ def cache_attention(q: torch.Tensor, cache: LevelCache, q_starts: torch.Tensor, 
     batch, dtype = kv_lens.numel(), q.dtype
     per = table.shape[-1]
     if out is None:
-        out = torch.empty_strided((tokens, heads, dim), (heads * dim, dim, 1), dtype=dtype, device=q.device)
-    L = lib()
+        out = _new_heads(tokens, heads, dim, dtype, q.device)
+    L = _lib or lib()
     if workspace is None:
         need = L.mpq_cache_attention_workspace(tokens, batch, heads, kv_heads, dim, max_q, max_kv)
         if need:
             workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=q.device)
     ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-    _check(L.mpq_cache_attention(*_heads(q, tokens, heads, dim), _dtype(dtype), _vector(q_starts, batch + 1, torch.int32),
-                                 _vector(kv_lens, batch, torch.int32), _vector(table, batch * per, torch.int32), per,
-                                 tokens, batch, heads, kv_heads, dim, max_q, max_kv, *held, cache.bits, pages, page_size,
-                                 causal, window, dim ** -0.5 if scale is None else scale, *_heads(out, tokens, heads, dim, dtype),
-                                 _vector(lse, tokens * heads, torch.float32), ws, ws_bytes, _stream()), "mpq_cache_attention")
+    st = L.mpq_cache_attention(
+        *_heads(q, tokens, heads, dim, dtype), _dtype(dtype), _vector(q_starts, batch + 1, torch.int32),
+        _vector(kv_lens, batch, torch.int32), _vector(table, batch * per, torch.int32), per,
+        tokens, batch, heads, kv_heads, dim, max_q, max_kv, *held, cache.bits, pages, page_size,
+        causal, window, dim ** -0.5 if scale is None else scale, *_heads(out, tokens, heads, dim, dtype),
+        None if lse is None else _vector(lse, tokens * heads, torch.float32), ws, ws_bytes, _raw_stream(_current_device()))
+    if st:
+        raise MpqError(st, "mpq_cache_attention")
     return out
 
 
