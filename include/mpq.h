@@ -16,7 +16,8 @@
  *     Documented exceptions: mpq_linear_static works on a buffer built into the library image;
  *     mpq_linear_host / mpq_linear_host_prepared keep one helper stream and a few events per
  *     device; and per device the library remembers the multiprocessor count and which kernels
- *     have had their shared-memory limit raised (facts that never change while the process lives).
+ *     have had their shared-memory limit raised (facts that never change while the process lives);
+ *     the tensor-core kernels count waits that ran out (mpq_wait_failures).
  *   - Calls are asynchronous on `stream` (a cudaStream_t passed as void*; NULL = the
  *     default stream) unless stated otherwise.  Outputs are fully overwritten.
  *   - Return value: an mpq_status.  Errors that the host can see (null pointers, bad

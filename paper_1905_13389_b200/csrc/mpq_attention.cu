@@ -505,7 +505,8 @@ struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; };   // row
 // re-reads a row of fp32 results).
 //   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; splits that give each of the three (two) CTAs
 // per multiprocessor one, but of no more than kLongSplit tokens, so that contexts of different lengths even out
-// (32 contexts of up to 16384: 117, 110 and 127 us with 1536, 3072 and 4096; a CTA costs some 3 us beside its
+// (32 contexts of up to 16384: 117, 110 and 127 us with 1536, 3072 and 4096, 115 with 3072 since the operands are
+// exact; a CTA costs some 3 us beside its
 // tokens: 128-token splits of 8 contexts of 4000 took 31 us, these 22).
 constexpr int kLongSplit = 3072;
 AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_q, int64_t max_kv) {

@@ -6,15 +6,18 @@
 // transposed, [dim][token], both in the 128-byte swizzled K-major layout that tcgen05.mma reads; they load a
 // step ahead into registers, so pages of any size cost nothing but the address arithmetic.  Warp 12 issues
 //     S_h = Q_h K^T  (fp16, fp32 accumulator in TMEM),    O_h += W_h V  (W_h in TMEM, where S_h was)
-// for the two tiles in turn, so that the tensor cores work on one tile while the other one's softmax runs in
-// warps 0-3 and 4-7, one thread per row: no reductions across lanes.  W_h overwrites S_h, and the commit of
-// S_h's next product also says that O_h is complete: a row whose maximum has grown by more than 2^3 rescales
-// its part of O_h then, before it hands over its weights (the accumulators are otherwise left alone).
+// in half steps of 64 tokens, two of S_h at a time per tile, so that a tile's softmax (warps 0-3 and 4-7) finds
+// its next scores ready; all 512 TMEM columns are in use.  A row's reference moves only when its maximum has
+// outgrown it by 2^3; the weights are then made again and its part of O_h is rescaled.
 //
-// What bounds it: per step and tile the score and value products take 512 cycles each at the fp16 rate for
-// dim 128, the 128 exponentials of a row 1024 cycles of the special-function units; the three constants per
-// token that every row needs (range factor of the key, exponent and reciprocal of the value's range) come
-// from shared memory at 128 bytes a cycle, 1536 cycles.
+// What bounds it (dim 128, 8 bits; cycles per step of 128 tokens and both tiles, of 6450 measured): the tensor
+// cores 3100 (2048 at the full rate; products 64 wide pay for reading Q again), the exponentials 2048 of the
+// special-function units, shared memory some 3900 at 128 bytes a cycle.  None is full: two softmax warps per
+// scheduler do not cover each other's latencies, and registers (512 x 128) leave no room for more.  2048 tokens
+// over 10240, 32 heads on 8: 518 us, 597 TFLOP/s.  On the way: 1181 us with row-per-thread softmax and loads as
+// they were needed, 715 with everything loaded a step ahead, 690 with constants shared by four rows a thread and
+// half steps, 518 once the issuing warp ran its loop with all lanes (see mbar_wait_warp).  Fetching S before the
+// weights of the half step before are handed over was slower (574-635), as were more registers for the softmax (543).
 #include "mpq_attention.cuh"
 #include "mpq_tensor.cuh"
 
