@@ -23,7 +23,9 @@
 
 namespace mpq {
 
-constexpr int kTileThreads = 512;
+constexpr int kSoftmaxWarps = 16;                         // eight per tile
+constexpr int kTileThreads = (kSoftmaxWarps + 4 + 4) * 32; // ... four that decode levels, one that issues (and three idle: register
+                                                          // shares are handed out by fours): 512 x 80 + 128 x 120 + 128 x 40 = 768 x 80
 
 __device__ unsigned int g_attention_wait_failures;
 
@@ -36,7 +38,8 @@ template <int D> struct TileSmem {
     static constexpr int const_stage = 3 * kStepTokens * 4;   // [64 token pairs](key factors, value exponents), [128] value reciprocals
     static constexpr int rows = consts + 2 * const_stage;     // cache row numbers, two steps
     static constexpr int ranges = rows + 2 * kStepTokens * 4; // first and last visible token of each row
-    static constexpr int total = ranges + kTileRows * 8 + 1024;
+    static constexpr int scales = ranges + kTileRows * 8;     // scale of each row; at the end its (reference, denominator)
+    static constexpr int total = scales + kTileRows * 8 + 1024;
 };
 
 template <int REGS> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
@@ -142,59 +145,57 @@ attn_tiles_kernel(const AttnArgs g) {
         for (int s = 0; s < 2; ++s) {
             mbar_init(k_full(s), 4); mbar_init(k_empty(s), 1);
             mbar_init(v_full(s), 4); mbar_init(v_empty(s), 1);
-            mbar_init(c_empty(s), 4 * tiles);
-            for (int half = 0; half < 2; ++half) { mbar_init(s_full(s, half), 1); mbar_init(p_ready(s, half), 4); }
+            mbar_init(c_empty(s), 8 * tiles);
+            for (int half = 0; half < 2; ++half) { mbar_init(s_full(s, half), 1); mbar_init(p_ready(s, half), 8); }
             mbar_init(o_done(s), 1);
         }
         failed = 0;
         mbar_init_fence();
     }
-    if (warp == 12) tmem_alloc<1>(&tmem_holder, 512);
+    if (warp == kSoftmaxWarps + 4) tmem_alloc<1>(&tmem_holder, 512);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = tmem_holder;
 
-    if (warp < 8) {
-        // ================= softmax: one thread per query row
-        regs_up<176>();
-        const int h = warp >> 2;
+    if (warp < kSoftmaxWarps) {
+        // ================= softmax
+        const int h = warp >> 3, sixteen = (warp >> 2) & 1, quarter = warp & 3;
         if (h < tiles) {
-            const int in_tile = threadIdx.x & 127, r = t.row0 + h * 128 + in_tile;
+            int2* ranges = reinterpret_cast<int2*>(base_ptr + Smem::ranges) + h * 128;       // of the tile's rows
+            float2* scales = reinterpret_cast<float2*>(base_ptr + Smem::scales) + h * 128;
+            auto tile_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(3 + h) : "memory"); };
+            const int in_tile = quarter * 32 + lane, r = t.row0 + h * 128 + in_tile;         // the row this thread stages and stores
             const bool live = r < t.rows;
             const int token = live ? r / g.group : t.n_q - 1, head = kv_head * g.group + (live ? r % g.group : 0);
-            float row_scale;
-            int my_first, my_last;
-            {
+            if (sixteen == 0) {
                 // the row as fp16, scaled by a power of two
                 const T* q = static_cast<const T*>(g.q) + (int64_t)(t.q0 + token) * g.q_ts + (int64_t)head * g.q_hs;
-                uint4 raw[D / 8];
-                if (live && (reinterpret_cast<uintptr_t>(q) & 15u) == 0) {
+                const bool aligned = (reinterpret_cast<uintptr_t>(q) & 15u) == 0;
+                auto eight = [&](int c) {                                // 8 elements of the row, read twice: registers are short here
+                    uint4 raw;
+                    if (live && aligned) return __ldg(reinterpret_cast<const uint4*>(q) + c);
+                    T e[8];
 #pragma unroll
-                    for (int c = 0; c < D / 8; ++c) raw[c] = __ldg(reinterpret_cast<const uint4*>(q) + c);
-                } else {
-#pragma unroll
-                    for (int c = 0; c < D / 8; ++c) {
-                        T e[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) e[i] = live ? q[c * 8 + i] : from_f32<T>(0.0f);
-                        raw[c] = *reinterpret_cast<const uint4*>(e);
-                    }
-                }
+                    for (int i = 0; i < 8; ++i) e[i] = live ? q[c * 8 + i] : from_f32<T>(0.0f);
+                    raw = *reinterpret_cast<const uint4*>(e);
+                    return raw;
+                };
                 float amax = 0.0f;
-#pragma unroll
+#pragma unroll 4
                 for (int c = 0; c < D / 8; ++c) {
-                    const T* e = reinterpret_cast<const T*>(&raw[c]);
+                    const uint4 raw = eight(c);
+                    const T* e = reinterpret_cast<const T*>(&raw);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(to_f32(e[i])));
                 }
                 float down, up;
                 row_power(amax, down, up);
-                row_scale = up * g.scale_log2;
                 const uint32_t tile = base + Smem::q + h * Smem::q_tile;
-#pragma unroll
+#pragma unroll 4
                 for (int c = 0; c < D / 8; ++c) {
-                    const T* e = reinterpret_cast<const T*>(&raw[c]);
+                    const uint4 raw = eight(c);
+                    const T* e = reinterpret_cast<const T*>(&raw);
                     uint32_t w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -204,30 +205,36 @@ attn_tiles_kernel(const AttnArgs g) {
                     }
                     st_shared16(tile + (c >> 3) * Smem::q_half + swizzled(in_tile, c & 7), w[0], w[1], w[2], w[3]);
                 }
-                row_range(g, t, token, my_first, my_last);
-                if (!live) { my_first = 0; my_last = 0x7fffffff; }             // computed with q = 0, never stored
+                int first, last;
+                row_range(g, t, token, first, last);
+                if (!live) { first = 0; last = 0x7fffffff; }             // computed with q = 0, never stored
+                ranges[in_tile] = make_int2(first, last);
+                scales[in_tile] = make_float2(up * g.scale_log2, 0.0f);
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_ready);
             }
-            // In the loop a thread holds a quarter of the columns of four rows (the matrix-fragment shape), so a token's
-            // constants serve four rows: they come from shared memory at 128 bytes a cycle, and with one row per thread
-            // they alone took 3072 cycles a step.  Row k of the thread is row (lane / 4) + 8 k of the warp's 32.
-            const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-            const uint32_t ts = lanes + kTmemS + h * 128, to = lanes + kTmemO + h * 128;
-            float set[4];                                 // the maximum that the weights' reference belongs to
-            uint64_t rs[4], l[4];                         // the row's scale, twice; two partial sums
+            tile_sync();
+            // In the loop a warp has 16 rows, and a thread a quarter of the columns of two of them (the matrix-fragment
+            // shape): row k of the thread is row (lane / 4) + 8 k of the warp's.
+            const int row0 = quarter * 32 + sixteen * 16 + (lane >> 2);
+            const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), mine = lanes + ((uint32_t)(sixteen * 16) << 16);
+            const uint32_t ts = mine + kTmemS + h * 128, to = mine + kTmemO + h * 128;
+            float set[2];                                 // the maximum that the weights' reference belongs to
+            uint64_t rs[2], l[2];                         // the row's scale, twice; two partial sums
+            int first_of_all = 0, last_of_all = 0x7fffffff;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float x = __shfl_sync(0xffffffffu, row_scale, (lane >> 2) + 8 * k);
+            for (int k = 0; k < 2; ++k) {
+                const float x = scales[row0 + 8 * k].x;
                 rs[k] = pack2(x, x);
                 set[k] = -INFINITY;
                 l[k] = 0;
+                const int2 seen = ranges[row0 + 8 * k];
+                first_of_all = max(first_of_all, seen.x);
+                last_of_all = min(last_of_all, seen.y);
             }
-            const int first_of_all = __reduce_max_sync(0xffffffffu, my_first), last_of_all = __reduce_min_sync(0xffffffffu, my_last);
-            int2* ranges = reinterpret_cast<int2*>(base_ptr + Smem::ranges) + warp * 32;      // this warp's rows
-            ranges[lane] = make_int2(my_first, my_last);
-            __syncwarp();
+            first_of_all = __reduce_max_sync(0xffffffffu, first_of_all);
+            last_of_all = __reduce_min_sync(0xffffffffu, last_of_all);
             bool ok = true;
 #pragma unroll 1
             for (int i = 0; i < 2 * steps; ++i) {         // half steps of 64 tokens
@@ -240,39 +247,36 @@ attn_tiles_kernel(const AttnArgs g) {
                 const uint32_t from_s = ts + half * 64;
                 const float4* consts = reinterpret_cast<const float4*>(base_ptr + Smem::consts + st * Smem::const_stage) + half * 32 + (lane & 3);
                 const float2* inv = reinterpret_cast<const float2*>(base_ptr + Smem::consts + st * Smem::const_stage + 2 * kStepTokens * 4) + half * 32 + (lane & 3);
-                uint32_t p[2][16];                        // weights: [16-row half]
-                uint64_t ls[4];
+                uint32_t p[16];                           // weights
+                uint64_t ls[2];
                 // The weights are made with the reference of the half step before, in one pass over S; only when a row's
                 // maximum has outgrown it (always in the first one, rarely later) is the pass repeated with a new one.
                 while (true) {
-                    uint64_t less[4];                     // minus the reference: set - kBoost, 0 while nothing was seen
-                    float top[4];
+                    uint64_t less[2];                     // minus the reference: set - kBoost, 0 while nothing was seen
+                    float top[2];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int k = 0; k < 2; ++k) {
                         const float x = set[k] == -INFINITY ? 0.0f : kBoost - set[k];
                         less[k] = pack2(x, x);
                         top[k] = -INFINITY;
                         ls[k] = 0;
                     }
-                    uint32_t v[2][32];
-                    tmem_load_frag(from_s, v[0]);
-                    tmem_load_frag(from_s + (16u << 16), v[1]);
+                    uint32_t v[32];
+                    tmem_load_frag(from_s, v);
                     tmem_wait_ld();
-                    uint64_t y[8][4];                     // [8-column group][row]: two neighbouring tokens each
+                    uint64_t y[8][2];                     // [8-column group][row]: two neighbouring tokens each
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float4 kl = consts[e * 4];
                         const uint64_t kf = pack2(kl.x, kl.y), lg = pack2(kl.z, kl.w);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t* sc = &v[k >> 1][e * 4 + (k & 1) * 2];
-                            y[e][k] = fma2(mul2(pack2(__uint_as_float(sc[0]), __uint_as_float(sc[1])), kf), rs[k], lg);
-                        }
+                        for (int k = 0; k < 2; ++k)
+                            y[e][k] = fma2(mul2(pack2(__uint_as_float(v[e * 4 + k * 2]), __uint_as_float(v[e * 4 + k * 2 + 1])), kf), rs[k], lg);
                     }
                     if (j0 < first_of_all || j0 + 63 > last_of_all) {                 // some row of the warp sees only a part
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int2 seen = ranges[(lane >> 2) + 8 * k];
+                        for (int k = 0; k < 2; ++k) {
+                            const int2 seen = ranges[row0 + 8 * k];
                             const int at = j0 + 2 * (lane & 3), from = seen.x - at, upto = seen.y - at;
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
@@ -287,7 +291,7 @@ attn_tiles_kernel(const AttnArgs g) {
                         const float2 i2 = inv[e * 4];
                         const uint64_t iv = pack2(i2.x, i2.y);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
+                        for (int k = 0; k < 2; ++k) {
                             float w0, w1;
                             unpack2(y[e][k], w0, w1);
                             top[k] = max3(top[k], w0, w1);
@@ -296,17 +300,14 @@ attn_tiles_kernel(const AttnArgs g) {
                             w1 = fast_exp2(w1);
                             ls[k] = fma2(pack2(w0, w1), iv, ls[k]);
                             const __half2 w = __floats2half2_rn(w0, w1);
-                            p[k >> 1][e * 2 + (k & 1)] = *reinterpret_cast<const uint32_t*>(&w);
+                            p[e * 2 + k] = *reinterpret_cast<const uint32_t*>(&w);
                         }
                     }
                     // a thread's own quarter of the columns decides whether to look at the others': nearly always it does not
-                    bool grow = false;
+                    if (!__any_sync(0xffffffffu, top[0] > set[0] + kLag || top[1] > set[1] + kLag)) break;
+                    float f[2];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) grow = grow || top[k] > set[k] + kLag;
-                    if (!__any_sync(0xffffffffu, grow)) break;
-                    float f[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int k = 0; k < 2; ++k) {
                         top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
                         top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
                         f[k] = 1.0f;
@@ -320,24 +321,21 @@ attn_tiles_kernel(const AttnArgs g) {
                         ok = mbar_wait_or(o_done(h), (i - 1) & 1, &failed);           // O is complete up to the half step before
                         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                         tmem_fence_after();
-#pragma unroll
-                        for (int a = 0; a < 2; ++a)
 #pragma unroll 1
-                            for (int c = 0; c < D / 64; ++c) {
-                                uint32_t o[32];
-                                tmem_load_frag(to + ((uint32_t)(16 * a) << 16) + c * 64, o);
-                                tmem_wait_ld();
+                        for (int c = 0; c < D / 64; ++c) {
+                            uint32_t o[32];
+                            tmem_load_frag(to + c * 64, o);
+                            tmem_wait_ld();
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f[a * 2 + ((e >> 1) & 1)]);
-                                tmem_store_frag(to + ((uint32_t)(16 * a) << 16) + c * 64, o);
-                            }
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f[(e >> 1) & 1]);
+                            tmem_store_frag(to + c * 64, o);
+                        }
                     }
                 }
                 if (!ok) break;
-                tmem_store_frag_half(from_s, p[0]);
-                tmem_store_frag_half(from_s + (16u << 16), p[1]);
+                tmem_store_frag_half(from_s, p);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) l[k] = add2(l[k], ls[k]);
+                for (int k = 0; k < 2; ++k) l[k] = add2(l[k], ls[k]);
                 tmem_wait_st();
                 tmem_fence_before();
                 __syncwarp();
@@ -346,24 +344,22 @@ attn_tiles_kernel(const AttnArgs g) {
                     if (half) mbar_arrive(c_empty(st));
                 }
             }
-            // ---- result
+            // ---- result: back to one row per thread, half of the dims for each of the two warps that share 32 rows
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float sum, odd;
+                unpack2(l[k], sum, odd);
+                sum += odd;
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                if ((lane & 3) == 0) scales[row0 + 8 * k] = make_float2(set[k], sum);
+            }
+            tile_sync();
             ok = mbar_wait_or(o_full, 0, &failed);
             ok = __all_sync(0xffffffffu, ok && !has_failed());
             if (ok) {
                 tmem_fence_after();
-                // back to one row per thread
-                float l_row = 0.0f, set_row = -INFINITY;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float sum, odd;
-                    unpack2(l[k], sum, odd);
-                    sum += odd;
-                    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                    const int from = (lane & 7) * 4;
-                    const float a = __shfl_sync(0xffffffffu, sum, from), b = __shfl_sync(0xffffffffu, set[k], from);
-                    if ((lane >> 3) == k) { l_row = a; set_row = b; }
-                }
+                const float set_row = scales[in_tile].x, l_row = scales[in_tile].y;
                 const bool empty = set_row == -INFINITY;
                 constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);
                 const int64_t at = (int64_t)(t.q0 + token) * g.heads + head;
@@ -372,43 +368,43 @@ attn_tiles_kernel(const AttnArgs g) {
                 const int64_t slot = at * g.splits + blockIdx.z;
                 const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
 #pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[32];
-                    if (steps > 0) { tmem_load32(to + c * 32, o); tmem_wait_ld(); }
+                for (int c = sixteen * (D / 32); c < (sixteen + 1) * (D / 32); ++c) {        // 16 dims at a time
+                    uint32_t o[16];
+                    if (steps > 0) { tmem_load16(lanes + kTmemO + h * 128 + c * 16, o); tmem_wait_ld(); }
                     if (!live) continue;
-                    float f[32];
+                    float f[16];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) f[e] = empty ? 0.0f : __uint_as_float(o[e]) * den;
+                    for (int e = 0; e < 16; ++e) f[e] = empty ? 0.0f : __uint_as_float(o[e]) * den;
                     if (used > 1) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<float4*>(g.part_o + slot * D + c * 32 + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                        for (int e = 0; e < 16; e += 4)
+                            *reinterpret_cast<float4*>(g.part_o + slot * D + c * 16 + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
                     } else {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) f[e] = final_value(f[e]);
+                        for (int e = 0; e < 16; ++e) f[e] = final_value(f[e]);
                         if (aligned) {
 #pragma unroll
-                            for (int e = 0; e < 32; e += 8) {
+                            for (int e = 0; e < 16; e += 8) {
                                 const float part[8] = {f[e], f[e + 1], f[e + 2], f[e + 3], f[e + 4], f[e + 5], f[e + 6], f[e + 7]};
-                                store_vec<T, 8>(out + c * 32 + e, part);
+                                store_vec<T, 8>(out + c * 16 + e, part);
                             }
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) out[c * 32 + e] = from_f32<T>(f[e]);
+                            for (int e = 0; e < 16; ++e) out[c * 16 + e] = from_f32<T>(f[e]);
                         }
                     }
                 }
-                if (live) {
+                if (live && sixteen == 0) {
                     if (used > 1) g.part_ml[slot] = make_float2(empty ? -INFINITY : set_row, l_row);
                     else if (g.lse) g.lse[at] = empty ? -INFINITY : (set_row - kBoost + log2f(l_row)) * 0.6931471805599453f;
                 }
                 tmem_fence_before();
             }
         }
-    } else if (warp < 12) {
+    } else if (warp < kSoftmaxWarps + 4) {
         // ================= levels: bytes of the cache -> fp16 operands
-        regs_down<120>();
-        const int th = threadIdx.x - 256;
+        regs_up<120>();
+        const int th = threadIdx.x - kSoftmaxWarps * 32;
         const int32_t* pages_of = g.table + (int64_t)t.b * g.table_stride;
         uint32_t* row_of = reinterpret_cast<uint32_t*>(base_ptr + Smem::rows);
         // keys: kKeyLanes lanes share a row, 16 bytes each
@@ -533,7 +529,7 @@ attn_tiles_kernel(const AttnArgs g) {
     } else {
         // ================= tensor-core issue
         regs_down<40>();
-        if (warp == 12) {
+        if (warp == kSoftmaxWarps + 4) {
             constexpr uint32_t idesc_s = umma_idesc_f16(128, 64), idesc_o = umma_idesc_f16(128, D);
             const uint32_t acc = __shfl_sync(0xffffffffu, tmem, 0);
             const bool leader = elect_one();
@@ -596,7 +592,7 @@ attn_tiles_kernel(const AttnArgs g) {
     __syncwarp();
     __syncthreads();
     tmem_fence_after();
-    if (warp == 12) tmem_free<1>(tmem, 512);
+    if (warp == kSoftmaxWarps + 4) tmem_free<1>(tmem, 512);
     if (threadIdx.x == 0 && failed) atomicAdd(&g_attention_wait_failures, 1u);
 }
 
