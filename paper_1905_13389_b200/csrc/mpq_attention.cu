@@ -503,19 +503,23 @@ struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; };   // row
 //   More than 32 rows per sequence and key head: 256-row tiles on the tensor cores.  A context is split only
 // while the tiles do not fill the multiprocessors, in stretches of 512 tokens at least (each split writes and
 // re-reads a row of fp32 results).
-//   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; splits that give each of the three (two) CTAs
-// per multiprocessor one, but of no more than kLongSplit tokens, so that contexts of different lengths even out
-// (32 contexts of up to 16384: 117, 110 and 127 us with 1536, 3072 and 4096, 115 with 3072 since the operands are
-// exact; a CTA costs some 3 us beside its
-// tokens: 128-token splits of 8 contexts of 4000 took 31 us, these 22).
+//   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; as many splits as leave every CTA a place at
+// once, three (two) to a multiprocessor: rounded down, since a second round of CTAs costs more than a few empty places
+// (32 contexts of 1024 tokens: 21.9 us in 256 CTAs, 28.5 in 512 for 444 places; 8 contexts of 4000: 25.0 in 384, 24.2
+// in 448).  But of no more than kLongSplit tokens, so that contexts of different lengths even out (32 contexts of up
+// to 16384: 117, 110 and 127 us with 1536, 3072 and 4096, 115 with 3072 since the operands are exact).
 constexpr int kLongSplit = 3072;
 AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_q, int64_t max_kv) {
     AttnPlan p;
+    if (max_q > tokens) max_q = tokens;
     p.rows = max_q * group > 32 ? kTileRows : max_q * group > 8 ? 16 : 8;
-    const int64_t context = max_kv < 1 ? 1 : max_kv;
+    const int64_t context = max_kv < 1 ? 1 : max_kv > 0x7fffffff ? 0x7fffffff : max_kv;
     int64_t per, unit;
     p.tiles = tile_bound(tokens, batch, group, p.rows);
+    // tiles to expect: full ones, and half a tile more per sequence; never more than the caller's bound allows
     int64_t likely = batch * ceil_div(max_q < 1 ? group : max_q * group, p.rows);
+    const int64_t filled = tokens * group / p.rows + (batch + 1) / 2;
+    if (likely > filled && p.rows == kTileRows) likely = filled;
     if (likely > p.tiles) likely = p.tiles;
     if (p.rows == kTileRows) {
         unit = kStepTokens;
@@ -524,7 +528,8 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
         per = ceil_div(context, splits < 1 ? 1 : splits);
     } else {
         unit = kChunk * kWarps;
-        per = ceil_div(context * likely * kv_heads, 148 * (p.rows == 8 ? 3 : 2));
+        const int64_t splits = 148 * (p.rows == 8 ? 3 : 2) / (likely * kv_heads);
+        per = ceil_div(context, splits < 1 ? 1 : splits);
         if (per > kLongSplit) per = kLongSplit;
     }
     per = ceil_div(per, unit) * unit;
@@ -582,7 +587,8 @@ using namespace mpq;
 
 extern "C" int64_t mpq_cache_attention_workspace(int64_t tokens, int batch, int heads, int kv_heads, int dim,
                                                  int64_t max_q, int64_t max_kv) {
-    if (tokens <= 0 || batch <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || dim <= 0 || max_q < 0 || max_kv < 0) return 0;
+    if (tokens <= 0 || batch <= 0 || heads <= 0 || heads > 65536 || tokens > 0x7fffffff / heads || kv_heads <= 0 || heads % kv_heads || dim <= 0 ||
+        max_q < 0 || max_kv < 0) return 0;
     const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_q, max_kv);
     if (p.splits <= 1) return 0;
     return up16(tokens * heads * p.splits * dim * 4) + up16(tokens * heads * p.splits * 8);
@@ -605,8 +611,16 @@ extern "C" int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_
     if (!aligned16(k_levels) || !aligned16(v_levels) || !aligned_to(k_scale, 4) || !aligned_to(v_scale, 4) || !aligned_to(q, 2) ||
         !aligned_to(out, 2) || !aligned_to(lse, 4) || !aligned_to(q_starts, 4) || !aligned_to(kv_lens, 4) || !aligned_to(table, 4)) return MPQ_ERR_ALIGN;
     if (tokens == 0) return MPQ_OK;
-    const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_q, max_kv);
+    const int group = heads / kv_heads;
+    AttnPlan p = attn_plan(tokens, batch, group, kv_heads, max_q, max_kv);
     if (p.tiles > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
+    // A window leaves a tile less of its context than that: plan for what it sees, within the workspace's splits (a
+    // ragged batch of 1 to 511 tokens over 5000 with a window of 1500: 61 us planned for 5000, 47 for what a tile sees).
+    if (window > 0 && window < max_kv && p.splits > 1) {
+        const int64_t seen = window + (causal ? p.rows / group + 1 : max_q < tokens ? max_q : tokens);
+        const AttnPlan w = attn_plan(tokens, batch, group, kv_heads, max_q, seen < max_kv ? seen : max_kv);
+        if (w.splits <= p.splits) { p.splits = w.splits; p.split_tokens = w.split_tokens; }
+    }
     int page_shift = -1;
     if ((page_size & (page_size - 1)) == 0) for (page_shift = 0; (1 << page_shift) < page_size; ++page_shift) {}
     AttnArgs g = {q, q_token_stride, q_head_stride, q_starts, kv_lens, table, table_stride, tokens, batch, heads, kv_heads, heads / kv_heads,
