@@ -140,7 +140,7 @@ attn_tiles_kernel(const AttnArgs g) {
     const int tiles = t.rows - t.row0 > 128 ? 2 : 1;
 
     if (threadIdx.x == 0) {
-        mbar_init(q_ready, 4 * tiles);
+        mbar_init(q_ready, 8 * tiles);
         mbar_init(o_full, 1);
         for (int s = 0; s < 2; ++s) {
             mbar_init(k_full(s), 4); mbar_init(k_empty(s), 1);
@@ -165,37 +165,49 @@ attn_tiles_kernel(const AttnArgs g) {
             int2* ranges = reinterpret_cast<int2*>(base_ptr + Smem::ranges) + h * 128;       // of the tile's rows
             float2* scales = reinterpret_cast<float2*>(base_ptr + Smem::scales) + h * 128;
             auto tile_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(3 + h) : "memory"); };
-            const int in_tile = quarter * 32 + lane, r = t.row0 + h * 128 + in_tile;         // the row this thread stages and stores
-            const bool live = r < t.rows;
-            const int token = live ? r / g.group : t.n_q - 1, head = kv_head * g.group + (live ? r % g.group : 0);
-            if (sixteen == 0) {
-                // the row as fp16, scaled by a power of two
+            auto row_of_tile = [&](int in_tile, bool& live, int& token, int& head) {
+                const int r = t.row0 + h * 128 + in_tile;
+                live = r < t.rows;
+                token = live ? r / g.group : t.n_q - 1;
+                head = kv_head * g.group + (live ? r % g.group : 0);
+            };
+            {
+                // A warp stages the 16 rows that it has in the loop as fp16, each scaled by a power of two: two threads a row,
+                // every second 16 bytes each, all loads at once (a thread per row, in four rounds of loads, took NN us more).
+                const int in_tile = quarter * 32 + sixteen * 16 + (lane >> 1), odd = lane & 1;
+                bool live;
+                int token, head;
+                row_of_tile(in_tile, live, token, head);
                 const T* q = static_cast<const T*>(g.q) + (int64_t)(t.q0 + token) * g.q_ts + (int64_t)head * g.q_hs;
-                const bool aligned = (reinterpret_cast<uintptr_t>(q) & 15u) == 0;
-                auto eight = [&](int c) {                                // 8 elements of the row, read twice: registers are short here
-                    uint4 raw;
-                    if (live && aligned) return __ldg(reinterpret_cast<const uint4*>(q) + c);
-                    T e[8];
+                uint4 raw[D / 16];
+                if (!live) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) e[i] = live ? q[c * 8 + i] : from_f32<T>(0.0f);
-                    raw = *reinterpret_cast<const uint4*>(e);
-                    return raw;
-                };
+                    for (int c = 0; c < D / 16; ++c) raw[c] = make_uint4(0, 0, 0, 0);
+                } else if ((reinterpret_cast<uintptr_t>(q) & 15u) == 0) {
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) raw[c] = __ldg(reinterpret_cast<const uint4*>(q) + 2 * c + odd);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) {
+                        const unsigned short* e = reinterpret_cast<const unsigned short*>(q) + (2 * c + odd) * 8;
+                        raw[c] = make_uint4(__ldg(e) | (uint32_t)__ldg(e + 1) << 16, __ldg(e + 2) | (uint32_t)__ldg(e + 3) << 16,
+                                            __ldg(e + 4) | (uint32_t)__ldg(e + 5) << 16, __ldg(e + 6) | (uint32_t)__ldg(e + 7) << 16);
+                    }
+                }
                 float amax = 0.0f;
-#pragma unroll 4
-                for (int c = 0; c < D / 8; ++c) {
-                    const uint4 raw = eight(c);
-                    const T* e = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    const T* e = reinterpret_cast<const T*>(&raw[c]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(to_f32(e[i])));
                 }
+                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
                 float down, up;
                 row_power(amax, down, up);
                 const uint32_t tile = base + Smem::q + h * Smem::q_tile;
-#pragma unroll 4
-                for (int c = 0; c < D / 8; ++c) {
-                    const uint4 raw = eight(c);
-                    const T* e = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) {
+                    const T* e = reinterpret_cast<const T*>(&raw[c]);
                     uint32_t w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -203,18 +215,20 @@ attn_tiles_kernel(const AttnArgs g) {
                         const __half2 v = __floats2half2_rn(to_f32(e[a]) * down, to_f32(e[b]) * down);
                         w[i] = *reinterpret_cast<const uint32_t*>(&v);
                     }
-                    st_shared16(tile + (c >> 3) * Smem::q_half + swizzled(in_tile, c & 7), w[0], w[1], w[2], w[3]);
+                    const int at = 2 * c + odd;
+                    st_shared16(tile + (at >> 3) * Smem::q_half + swizzled(in_tile, at & 7), w[0], w[1], w[2], w[3]);
                 }
-                int first, last;
-                row_range(g, t, token, first, last);
-                if (!live) { first = 0; last = 0x7fffffff; }             // computed with q = 0, never stored
-                ranges[in_tile] = make_int2(first, last);
-                scales[in_tile] = make_float2(up * g.scale_log2, 0.0f);
+                if (!odd) {
+                    int first, last;
+                    row_range(g, t, token, first, last);
+                    if (!live) { first = 0; last = 0x7fffffff; }         // computed with q = 0, never stored
+                    ranges[in_tile] = make_int2(first, last);
+                    scales[in_tile] = make_float2(up * g.scale_log2, 0.0f);
+                }
                 proxy_fence();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_ready);
             }
-            tile_sync();
             // In the loop a warp has 16 rows, and a thread a quarter of the columns of two of them (the matrix-fragment
             // shape): row k of the thread is row (lane / 4) + 8 k of the warp's.
             const int row0 = quarter * 32 + sixteen * 16 + (lane >> 2);
@@ -359,6 +373,10 @@ attn_tiles_kernel(const AttnArgs g) {
             ok = __all_sync(0xffffffffu, ok && !has_failed());
             if (ok) {
                 tmem_fence_after();
+                const int in_tile = quarter * 32 + lane;
+                bool live;
+                int token, head;
+                row_of_tile(in_tile, live, token, head);
                 const float set_row = scales[in_tile].x, l_row = scales[in_tile].y;
                 const bool empty = set_row == -INFINITY;
                 constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);
