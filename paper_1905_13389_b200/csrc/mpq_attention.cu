@@ -10,10 +10,18 @@
 // only W^T changes hands, by one 8 x 8 register transpose per 8 tokens.  With so few rows the work is bound by
 // reading the cache, not by the matrix pipe, which is why the 128-row tcgen05 tile, mostly empty here, is not used.
 #include "mpq_attention.cuh"
+#include "mpq_tensor.cuh"
 
 namespace mpq {
 
 constexpr int kChunk = 32, kWarps = 4;
+constexpr int kJoined = 8;                                // splits that a cluster of CTAs can hold
+
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -412,14 +420,57 @@ attn_rows_kernel(const AttnArgs g) {
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) num = fmaf(sh_o[w][r][d], f[w], num);
             num *= kInvL;
-            if (used > 1) g.part_o[slot * D + d] = num;
+            if (g.joined && used > 1) sh_o[0][r][d] = num;               // read by this thread alone so far
+            else if (used > 1) g.part_o[slot * D + d] = num;
             else out[d] = from_f32<T>(top == -INFINITY ? 0.0f : final_value(num / den));
         }
+        __syncwarp();
         if (lane == 0) {
-            if (used > 1) g.part_ml[slot] = make_float2(top, den);
+            if (g.joined && used > 1) { sh_ml[0][r][0] = top; sh_ml[0][r][1] = den; }
+            else if (used > 1) g.part_ml[slot] = make_float2(top, den);
             else if (g.lse) g.lse[at] = top == -INFINITY ? -INFINITY : (top - kBoost + log2f(den)) * 0.6931471805599453f;
         }
     }
+    if (!g.joined || used <= 1) return;
+    // The cluster's CTAs hold a split each (those past `used` have exited, which counts as arrived): a warp joins a row
+    // of all of them, read from their shared memory.  The result does not depend on which CTA's warp it is.
+    cluster_sync_all();
+    for (int r = blockIdx.z * kWarps + warp; r < min(kRows, t.rows - t.row0); r += used * kWarps) {
+        const uint32_t of_ml = smem_addr(&sh_ml[0][r][0]), of_o = smem_addr(&sh_o[0][r][lane]);
+        float top = -INFINITY, den = 0.0f, part[kJoined][D / 32];
+        if (lane < used) {
+            const uint32_t at = map_to_cta(of_ml, lane);
+            top = ld_cluster(at);
+            den = ld_cluster(at + 4);
+        }
+#pragma unroll
+        for (int s = 0; s < kJoined; ++s)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) part[s][i] = s < used ? ld_cluster(map_to_cta(of_o + i * 128, s)) : 0.0f;
+        const float mine = top;
+#pragma unroll
+        for (int o = 1; o < kJoined; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        top = __shfl_sync(0xffffffffu, top, 0);
+        const float f = mine == -INFINITY ? 0.0f : fast_exp2(mine - top);
+        den = mine == -INFINITY ? 0.0f : den * f;
+#pragma unroll
+        for (int o = 1; o < kJoined; o <<= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+        den = __shfl_sync(0xffffffffu, den, 0);
+        const int token = (t.row0 + r) / g.group, head = kv_head * g.group + (t.row0 + r) % g.group;
+        T* out = static_cast<T*>(g.out) + (int64_t)(t.q0 + token) * g.o_ts + (int64_t)head * g.o_hs;
+        float acc[D / 32] = {};
+#pragma unroll
+        for (int s = 0; s < kJoined; ++s) {
+            const float fs = __shfl_sync(0xffffffffu, f, s);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) acc[i] = s < used ? fmaf(part[s][i], fs, acc[i]) : acc[i];
+        }
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) out[i * 32 + lane] = from_f32<T>(top == -INFINITY ? 0.0f : final_value(acc[i] / den));
+        if (g.lse && lane == 0)
+            g.lse[(int64_t)(t.q0 + token) * g.heads + head] = top == -INFINITY ? -INFINITY : (top - kBoost + log2f(den)) * 0.6931471805599453f;
+    }
+    cluster_sync_all();                                   // nobody leaves while its shared memory is read
 }
 
 // Splits of a context -> result: WARPS warps per (token, head), each with every WARPS-th split, so that the rows of up
@@ -528,7 +579,7 @@ inline int64_t tile_bound(int64_t tokens, int batch, int group, int rows) {
     return tokens * group / rows + (tokens < batch ? tokens : batch);
 }
 
-struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; };   // rows of a tile: 8, 16 or kTileRows
+struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; bool joined; };   // rows of a tile: 8, 16 or kTileRows
 
 // Which kernel, and how far a context is split.
 //   More than 32 rows per sequence and key head: 256-row tiles on the tensor cores.  A context is split only
@@ -567,6 +618,7 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
     if (ceil_div(context, per) > 256) per = ceil_div(ceil_div(context, 256), unit) * unit;
     p.splits = (int)ceil_div(context, per);
     p.split_tokens = (int)(per > 0x40000000 ? 0x40000000 : per);
+    p.joined = p.rows != kTileRows && p.splits > 1 && p.splits <= kJoined && likely * kv_heads * p.splits <= 148 * (p.rows == 8 ? 3 : 2);
     return p;
 }
 
@@ -592,11 +644,14 @@ int launch_rows(const AttnArgs& g, const AttnPlan& p, cudaStream_t st) {
     cfg.stream = st;
     const size_t ring = (size_t)kWarps * (p.rows == 8 ? Ring<D * BITS / 8, 1>::warp : Ring<D * BITS / 8, 2>::warp), merge = (size_t)kWarps * p.rows * (D + 4) * 4;
     cfg.dynamicSmemBytes = ring > merge ? ring : merge;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = (unsigned)p.splits;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = p.joined ? 2 : 1;
     static PerDeviceOnce once8, once16;
     auto* kernel = p.rows == 8 ? attn_rows_kernel<T, D, BITS, 1> : attn_rows_kernel<T, D, BITS, 2>;
     const int rc = (p.rows == 8 ? once8 : once16).raise_smem_limit(kernel, cfg.dynamicSmemBytes);
@@ -609,7 +664,7 @@ template <typename T, int D>
 int launch_attention(const AttnArgs& g, const AttnPlan& p, int dtype, int bits, cudaStream_t st) {
     const int rc = p.rows == kTileRows ? attention_tiles(g, dtype, D, bits, p.tiles, st)
                           : bits == 8 ? launch_rows<T, D, 8>(g, p, st) : launch_rows<T, D, 4>(g, p, st);
-    return rc != MPQ_OK || p.splits == 1 ? rc : launch_merge<T, D>(g, p.rows, st);
+    return rc != MPQ_OK || p.splits == 1 || p.joined ? rc : launch_merge<T, D>(g, p.rows, st);
 }
 
 }  // namespace mpq
@@ -621,7 +676,7 @@ extern "C" int64_t mpq_cache_attention_workspace(int64_t tokens, int batch, int 
     if (tokens <= 0 || batch <= 0 || heads <= 0 || heads > 65536 || tokens > 0x7fffffff / heads || kv_heads <= 0 || heads % kv_heads || dim <= 0 ||
         max_q < 0 || max_kv < 0) return 0;
     const AttnPlan p = attn_plan(tokens, batch, heads / kv_heads, kv_heads, max_q, max_kv);
-    if (p.splits <= 1) return 0;
+    if (p.splits <= 1 || p.joined) return 0;
     return up16(tokens * heads * p.splits * dim * 4) + up16(tokens * heads * p.splits * 8);
 }
 
@@ -650,14 +705,14 @@ extern "C" int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_
     if (window > 0 && window < max_kv && p.splits > 1) {
         const int64_t seen = window + (causal ? p.rows / group + 1 : max_q < tokens ? max_q : tokens);
         const AttnPlan w = attn_plan(tokens, batch, group, kv_heads, max_q, seen < max_kv ? seen : max_kv);
-        if (w.splits <= p.splits) { p.splits = w.splits; p.split_tokens = w.split_tokens; }
+        if (w.splits <= p.splits) { p.splits = w.splits; p.split_tokens = w.split_tokens; p.joined = w.joined; }
     }
     int page_shift = -1;
     if ((page_size & (page_size - 1)) == 0) for (page_shift = 0; (1 << page_shift) < page_size; ++page_shift) {}
     AttnArgs g = {q, q_token_stride, q_head_stride, q_starts, kv_lens, table, table_stride, tokens, batch, heads, kv_heads, heads / kv_heads,
                   k_levels, k_scale, v_levels, v_scale, pages, page_size, page_shift, causal != 0, window, scale * 1.4426950408889634f,
-                  out, out_token_stride, out_head_stride, lse, nullptr, nullptr, p.splits, p.split_tokens};
-    if (p.splits > 1) {
+                  out, out_token_stride, out_head_stride, lse, nullptr, nullptr, p.splits, p.split_tokens, p.joined};
+    if (p.splits > 1 && !p.joined) {
         if (!workspace) return MPQ_ERR_NULL;
         if (!aligned16(workspace)) return MPQ_ERR_ALIGN;
         if (workspace_bytes < mpq_cache_attention_workspace(tokens, batch, heads, kv_heads, dim, max_q, max_kv)) return MPQ_ERR_WORKSPACE;

@@ -33,6 +33,7 @@ struct AttnArgs {
     void* out; int64_t o_ts, o_hs; float* lse;
     float* part_o; float2* part_ml;         // [tokens][heads][splits](dim), (m, l) of each split; used where a tile has more than one split
     int splits, split_tokens;               // launch grid's splits; context tokens of one split
+    int joined;                             // the splits of a tile are one cluster, which joins them (few rows; no workspace)
 };
 
 // One tile of query rows of one sequence: row r is token r / group, head kv_head * group + r % group.
