@@ -589,7 +589,13 @@ struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; bool joined
 // once, three (two) to a multiprocessor: rounded down, since a second round of CTAs costs more than a few empty places
 // (32 contexts of 1024 tokens: 21.9 us in 256 CTAs, 28.5 in 512 for 444 places; 8 contexts of 4000: 25.0 in 384, 24.2
 // in 448).  But of no more than kLongSplit tokens, so that contexts of different lengths even out (32 contexts of up
-// to 16384: 117, 110 and 127 us with 1536, 3072 and 4096, 115 with 3072 since the operands are exact).
+// to 16384: 117, 110 and 127 us with 1536, 3072 and 4096, 113 with 3072 since the operands are exact).
+//   Up to eight splits of a tile are one cluster and need no second launch, if all CTAs fit at once: a cluster holds its
+// places until its longest split is through (8 contexts of 4000: 23.7 us with the second launch, 20.6 without; the 32
+// contexts of up to 16384: 113 and 150).  Short contexts are split no further than that, up to 512 tokens of a split
+// (batches of 4, 2 and 1 over 4000: 15.6, 13.7 and 11.5 us in 8 splits, 17.5, 14.1 and 10.6 in 13, 27 and 32; and a
+// call of one launch is 4 us shorter on the host; over 8000 20.2 and 18.0 against 17.2 and 13.1; tiles of 16 rows lose
+// from 4000 on, 16.9 against 15.1).
 constexpr int kLongSplit = 3072;
 AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_q, int64_t max_kv) {
     AttnPlan p;
@@ -610,7 +616,8 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
         per = ceil_div(context, splits < 1 ? 1 : splits);
     } else {
         unit = kChunk * kWarps;
-        const int64_t splits = 148 * (p.rows == 8 ? 3 : 2) / (likely * kv_heads);
+        int64_t splits = 148 * (p.rows == 8 ? 3 : 2) / (likely * kv_heads);
+        if (p.rows == 8 && splits > kJoined && context <= kJoined * 512) splits = kJoined;
         per = ceil_div(context, splits < 1 ? 1 : splits);
         if (per > kLongSplit) per = kLongSplit;
     }
