@@ -10,19 +10,10 @@
 // only W^T changes hands, by one 8 x 8 register transpose per 8 tokens.  With so few rows the work is bound by
 // reading the cache, not by the matrix pipe, which is why the 128-row tcgen05 tile, mostly empty here, is not used.
 #include "mpq_attention.cuh"
-#include "mpq_tensor.cuh"
 
 namespace mpq {
 
 constexpr int kChunk = 32, kWarps = 4;
-constexpr int kJoined = 8;                                // splits that a cluster of CTAs can hold
-
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -435,41 +426,8 @@ attn_rows_kernel(const AttnArgs g) {
     // The cluster's CTAs hold a split each (those past `used` have exited, which counts as arrived): a warp joins a row
     // of all of them, read from their shared memory.  The result does not depend on which CTA's warp it is.
     cluster_sync_all();
-    for (int r = blockIdx.z * kWarps + warp; r < min(kRows, t.rows - t.row0); r += used * kWarps) {
-        const uint32_t of_ml = smem_addr(&sh_ml[0][r][0]), of_o = smem_addr(&sh_o[0][r][lane]);
-        float top = -INFINITY, den = 0.0f, part[kJoined][D / 32];
-        if (lane < used) {
-            const uint32_t at = map_to_cta(of_ml, lane);
-            top = ld_cluster(at);
-            den = ld_cluster(at + 4);
-        }
-#pragma unroll
-        for (int s = 0; s < kJoined; ++s)
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) part[s][i] = s < used ? ld_cluster(map_to_cta(of_o + i * 128, s)) : 0.0f;
-        const float mine = top;
-#pragma unroll
-        for (int o = 1; o < kJoined; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        top = __shfl_sync(0xffffffffu, top, 0);
-        const float f = mine == -INFINITY ? 0.0f : fast_exp2(mine - top);
-        den = mine == -INFINITY ? 0.0f : den * f;
-#pragma unroll
-        for (int o = 1; o < kJoined; o <<= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-        den = __shfl_sync(0xffffffffu, den, 0);
-        const int token = (t.row0 + r) / g.group, head = kv_head * g.group + (t.row0 + r) % g.group;
-        T* out = static_cast<T*>(g.out) + (int64_t)(t.q0 + token) * g.o_ts + (int64_t)head * g.o_hs;
-        float acc[D / 32] = {};
-#pragma unroll
-        for (int s = 0; s < kJoined; ++s) {
-            const float fs = __shfl_sync(0xffffffffu, f, s);
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) acc[i] = s < used ? fmaf(part[s][i], fs, acc[i]) : acc[i];
-        }
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) out[i * 32 + lane] = from_f32<T>(top == -INFINITY ? 0.0f : final_value(acc[i] / den));
-        if (g.lse && lane == 0)
-            g.lse[(int64_t)(t.q0 + token) * g.heads + head] = top == -INFINITY ? -INFINITY : (top - kBoost + log2f(den)) * 0.6931471805599453f;
-    }
+    join_rows<T, D, kJoined>(g, t, kv_head, min(kRows, t.rows - t.row0), used, blockIdx.z * kWarps + warp, used * kWarps,
+                             [&](int r) { return smem_addr(&sh_ml[0][r][0]); }, [&](int r, int d) { return smem_addr(&sh_o[0][r][d]); });
     cluster_sync_all();                                   // nobody leaves while its shared memory is read
 }
 
@@ -583,19 +541,21 @@ struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; bool joined
 
 // Which kernel, and how far a context is split.
 //   More than 32 rows per sequence and key head: 256-row tiles on the tensor cores.  A context is split only
-// while the tiles do not fill the multiprocessors, in stretches of 512 tokens at least (each split writes and
-// re-reads a row of fp32 results).
+// while the tiles do not fill the multiprocessors, in stretches of 512 tokens at least (each split hands over a row of
+// fp32 results).
 //   Otherwise: tiles of 8 rows where a sequence has no more, else of 16; as many splits as leave every CTA a place at
 // once, three (two) to a multiprocessor: rounded down, since a second round of CTAs costs more than a few empty places
 // (32 contexts of 1024 tokens: 21.9 us in 256 CTAs, 28.5 in 512 for 444 places; 8 contexts of 4000: 25.0 in 384, 24.2
 // in 448).  But of no more than kLongSplit tokens, so that contexts of different lengths even out (32 contexts of up
 // to 16384: 117, 110 and 127 us with 1536, 3072 and 4096, 113 with 3072 since the operands are exact).
 //   Up to eight splits of a tile are one cluster and need no second launch, if all CTAs fit at once: a cluster holds its
-// places until its longest split is through (8 contexts of 4000: 23.7 us with the second launch, 20.6 without; the 32
-// contexts of up to 16384: 113 and 150).  Short contexts are split no further than that, up to 512 tokens of a split
-// (batches of 4, 2 and 1 over 4000: 15.6, 13.7 and 11.5 us in 8 splits, 17.5, 14.1 and 10.6 in 13, 27 and 32; and a
-// call of one launch is 4 us shorter on the host; over 8000 20.2 and 18.0 against 17.2 and 13.1; tiles of 16 rows lose
-// from 4000 on, 16.9 against 15.1).
+// places until its longest split is through (one token over 8 contexts of 4000: 23.7 us with the second launch, 20.6
+// without; 32 contexts of up to 16384: 113 and 150.  64 and 512 tokens over 4000, 8 and 2 splits: 39.7 and 83.3, 33.1
+// and 72.1).  A GPU processing cluster of 16 to 20 multiprocessors may be unable to place up to splits - 1 CTAs of the
+// form that has a multiprocessor to itself; eight of them are allowed for.
+//   Short contexts are split no further than that, up to 512 tokens of a split (batches of 4, 2 and 1 over 4000: 15.6,
+// 13.7 and 11.5 us in 8 splits, 17.5, 14.1 and 10.6 in 13, 27 and 32; and a call of one launch is 4 us shorter on the
+// host; over 8000 20.2 and 18.0 against 17.2 and 13.1; tiles of 16 rows lose from 4000 on, 16.9 against 15.1).
 constexpr int kLongSplit = 3072;
 AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t max_q, int64_t max_kv) {
     AttnPlan p;
@@ -625,7 +585,9 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
     if (ceil_div(context, per) > 256) per = ceil_div(ceil_div(context, 256), unit) * unit;
     p.splits = (int)ceil_div(context, per);
     p.split_tokens = (int)(per > 0x40000000 ? 0x40000000 : per);
-    p.joined = p.rows != kTileRows && p.splits > 1 && p.splits <= kJoined && likely * kv_heads * p.splits <= 148 * (p.rows == 8 ? 3 : 2);
+    p.joined = p.splits > 1 && p.splits <= kJoined &&
+               (p.rows == kTileRows ? likely * kv_heads * p.splits + 8 * (p.splits - 1) <= 148
+                                    : likely * kv_heads * p.splits <= 148 * (p.rows == 8 ? 3 : 2));
     return p;
 }
 

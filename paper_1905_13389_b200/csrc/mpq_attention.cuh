@@ -19,6 +19,7 @@
 // in the exponent, and a result below 2^-89 in magnitude is stored as 0.
 #pragma once
 #include "mpq_levels.cuh"
+#include "mpq_tensor.cuh"
 
 namespace mpq {
 
@@ -33,7 +34,7 @@ struct AttnArgs {
     void* out; int64_t o_ts, o_hs; float* lse;
     float* part_o; float2* part_ml;         // [tokens][heads][splits](dim), (m, l) of each split; used where a tile has more than one split
     int splits, split_tokens;               // launch grid's splits; context tokens of one split
-    int joined;                             // the splits of a tile are one cluster, which joins them (few rows; no workspace)
+    int joined;                             // the splits of a tile are one cluster, which joins them (no workspace)
 };
 
 // One tile of query rows of one sequence: row r is token r / group, head kv_head * group + r % group.
@@ -144,6 +145,54 @@ __device__ __forceinline__ void row_power(float amax, float& down, float& up) {
     e = min(max(e, -100), 126);
     down = __uint_as_float((uint32_t)(127 - e) << 23);
     up = __uint_as_float((uint32_t)(127 + e) << 23);
+}
+
+constexpr int kJoined = 8;                                // splits that a cluster can hold
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+// Joins the rows of a tile over the splits of a cluster's first `used` CTAs, at most SPLITS: warp `index` of `warps` takes
+// every warps-th row.  ml_at(r) is the shared-memory address of row r's (reference, denominator), o_at(r, d) that of its
+// element d, the same in every CTA.  (Two or four rows at once were slower: their registers spill.)
+template <typename T, int D, int SPLITS, typename MlAt, typename OAt>
+__device__ __forceinline__ void join_rows(const AttnArgs& g, const AttnTile& t, int kv_head, int rows, int used, int index, int warps, MlAt ml_at, OAt o_at) {
+    const int lane = threadIdx.x & 31;
+    for (int r = index; r < rows; r += warps) {
+        float part[SPLITS][D / 32], ref = -INFINITY, den = 0.0f;
+        if (lane < used) {
+            const uint32_t at = map_to_cta(ml_at(r), lane);
+            ref = ld_cluster(at);
+            den = ld_cluster(at + 4);
+        }
+#pragma unroll
+        for (int s = 0; s < SPLITS; ++s)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) part[s][i] = s < used ? ld_cluster(map_to_cta(o_at(r, i * 32 + lane), s)) : 0.0f;
+        float top = ref;
+#pragma unroll
+        for (int o = 1; o < SPLITS; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        top = __shfl_sync(0xffffffffu, top, 0);
+        const float f = ref == -INFINITY ? 0.0f : fast_exp2(ref - top);
+        den = ref == -INFINITY ? 0.0f : den * f;
+#pragma unroll
+        for (int o = 1; o < SPLITS; o <<= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+        den = __shfl_sync(0xffffffffu, den, 0);
+        float acc[D / 32] = {};
+#pragma unroll
+        for (int s = 0; s < SPLITS; ++s) {
+            const float fs = __shfl_sync(0xffffffffu, f, s);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) acc[i] = s < used ? fmaf(part[s][i], fs, acc[i]) : acc[i];
+        }
+        const int row = t.row0 + r, token = t.q0 + row / g.group, head = kv_head * g.group + row % g.group;
+        T* out = static_cast<T*>(g.out) + (int64_t)token * g.o_ts + (int64_t)head * g.o_hs;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) out[i * 32 + lane] = from_f32<T>(top == -INFINITY ? 0.0f : final_value(acc[i] / den));
+        if (g.lse && lane == 0)
+            g.lse[(int64_t)token * g.heads + head] = top == -INFINITY ? -INFINITY : (top - kBoost + log2f(den)) * 0.6931471805599453f;
+    }
 }
 
 // The tensor-core form for many query rows (mpq_attention_tiles.cu).

@@ -19,7 +19,6 @@
 // half steps, 518 once the issuing warp ran its loop with all lanes (see mbar_wait_warp).  Fetching S before the
 // weights of the half step before are handed over was slower (574-635), as were more registers for the softmax (543).
 #include "mpq_attention.cuh"
-#include "mpq_tensor.cuh"
 
 namespace mpq {
 
@@ -123,6 +122,10 @@ attn_tiles_kernel(const AttnArgs g) {
     auto s_full = [&](int h, int half) { return smem_addr(&bars[12 + 2 * h + half]); };
     auto p_ready = [&](int h, int half) { return smem_addr(&bars[16 + 2 * h + half]); };
     auto o_done = [&](int h) { return smem_addr(&bars[20 + h]); };       // W V of a half step is in O
+    // element d of row r of the tile in the buffer that a cluster joins: all of the keys' and values' stages, 16-byte chunks
+    // swizzled, since a thread writes along a row
+    static_assert(2 * Smem::k_stage + 2 * Smem::v_stage >= kTileRows * D * 4, "no room for the rows that a cluster joins");
+    auto joined_at = [](int r, int d) { return (uint32_t)(Smem::k + r * (D * 4) + (((d >> 2) ^ (r & 7)) << 4) + (d & 3) * 4); };
     auto has_failed = [&]() { return *(volatile int*)&failed != 0; };
 
     chain_entry();
@@ -393,7 +396,12 @@ attn_tiles_kernel(const AttnArgs g) {
                     float f[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) f[e] = empty ? 0.0f : __uint_as_float(o[e]) * den;
-                    if (used > 1) {
+                    if (used > 1 && g.joined) {                          // for the cluster, where the keys and values were
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            st_shared16(base + joined_at(h * 128 + in_tile, c * 16 + e * 4), __float_as_uint(f[e * 4]), __float_as_uint(f[e * 4 + 1]),
+                                        __float_as_uint(f[e * 4 + 2]), __float_as_uint(f[e * 4 + 3]));
+                    } else if (used > 1) {
 #pragma unroll
                         for (int e = 0; e < 16; e += 4)
                             *reinterpret_cast<float4*>(g.part_o + slot * D + c * 16 + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
@@ -413,8 +421,8 @@ attn_tiles_kernel(const AttnArgs g) {
                     }
                 }
                 if (live && sixteen == 0) {
-                    if (used > 1) g.part_ml[slot] = make_float2(empty ? -INFINITY : set_row, l_row);
-                    else if (g.lse) g.lse[at] = empty ? -INFINITY : (set_row - kBoost + log2f(l_row)) * 0.6931471805599453f;
+                    if (used > 1 && !g.joined) g.part_ml[slot] = make_float2(empty ? -INFINITY : set_row, l_row);
+                    else if (used == 1 && g.lse) g.lse[at] = empty ? -INFINITY : (set_row - kBoost + log2f(l_row)) * 0.6931471805599453f;
                 }
                 tmem_fence_before();
             }
@@ -611,6 +619,17 @@ attn_tiles_kernel(const AttnArgs g) {
     __syncthreads();
     tmem_fence_after();
     if (warp == kSoftmaxWarps + 4) tmem_free<1>(tmem, 512);
+    if (used > 1 && g.joined) {
+        cluster_sync_all();                                              // (CTAs past `used` have exited, which counts as arrived)
+        if (warp < kSoftmaxWarps) {
+            const int rows = min(kTileRows, t.rows - t.row0), index = blockIdx.z * kSoftmaxWarps + warp, warps = used * kSoftmaxWarps;
+            auto ml_at = [&](int r) { return base + Smem::scales + r * 8; };
+            auto o_at = [&](int r, int d) { return base + joined_at(r, d); };
+            if (used == 2) join_rows<T, D, 2>(g, t, kv_head, rows, used, index, warps, ml_at, o_at);
+            else join_rows<T, D, kJoined>(g, t, kv_head, rows, used, index, warps, ml_at, o_at);
+        }
+        cluster_sync_all();                                              // nobody leaves while its shared memory is read
+    }
     if (threadIdx.x == 0 && failed) atomicAdd(&g_attention_wait_failures, 1u);
 }
 
@@ -625,11 +644,14 @@ int launch_tiles(const AttnArgs& g, int64_t tiles, cudaStream_t st) {
     cfg.blockDim = dim3(kTileThreads, 1, 1);
     cfg.dynamicSmemBytes = TileSmem<D>::total;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = (unsigned)g.splits;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = g.joined ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
     return launch_status();
 }
