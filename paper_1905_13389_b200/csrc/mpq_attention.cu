@@ -2,10 +2,11 @@
 //
 // A CTA of four warps takes 8 NQ query rows (tokens x heads of one key head) and a stretch of the context;
 // each warp runs an online softmax of its own over every fourth chunk of 32 tokens and the four are merged
-// at the end.  A warp copies its chunks asynchronously into a ring of its own in shared memory, one to seven of
-// them under way while it works on one: 12 warps a multiprocessor keep some 100 KB in flight.  The products are transposed, S^T = K Q^T and O^T = V^T W^T with mma.sync.m16n8k16: tokens and
-// dims fill the 16-wide side, eight query rows the other one, so a single token of a few heads wastes little.
-// The element order inside a dot product is free, so the 16 level bytes that a lane reads ARE its operand
+// at the end; splits of a context are joined through distributed shared memory where they are a cluster, else by
+// a second kernel.  A warp copies its chunks asynchronously into a ring of its own in shared memory, one to seven of
+// them under way while it works on one: 12 warps a multiprocessor keep some 100 KB in flight.  The products are
+// transposed, S^T = K Q^T and O^T = V^T W^T with mma.sync.m16n8k16: tokens and dims fill the 16-wide side, eight
+// query rows the other one, so a single token of a few heads wastes little.  The element order inside a dot product is free, so the 16 level bytes that a lane reads ARE its operand
 // fragment, for the keys (lane = token, bytes along dim) and for the values (lane = 16 dims of a token pair);
 // only W^T changes hands, by one 8 x 8 register transpose per 8 tokens.  With so few rows the work is bound by
 // reading the cache, not by the matrix pipe, which is why the 128-row tcgen05 tile, mostly empty here, is not used.
@@ -372,7 +373,7 @@ attn_rows_kernel(const AttnArgs g) {
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();                                      // the ring becomes the merge's buffer
 
-    // ---- merge: rows of the four warps, then the splits (by attn_merge_kernel) or the result
+    // ---- merge: rows of the four warps, then the splits (by the cluster or attn_merge_kernel) or the result
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -443,7 +444,7 @@ __global__ void __launch_bounds__(kMergeThreads) attn_merge_kernel(const AttnArg
     const bool exists = at < g.tokens * g.heads;
     const int token = exists ? (int)(at / g.heads) : 0, head = exists ? (int)(at % g.heads) : 0;
     // What the splits left is asked for before it is known how many there are (slots past them are in the workspace, and
-    // not used): one round of loads instead of four, NN us of a call.
+    // not used): one round of loads instead of four, 1 to 2 us.
     const float2* ml = g.part_ml + at * g.splits;
     const float2 first_ml = exists && lane < g.splits ? ml[lane] : make_float2(-INFINITY, 0.0f);
     constexpr int kEarly = WARPS == 1 ? 4 : 0;               // all the splits that this form is launched for

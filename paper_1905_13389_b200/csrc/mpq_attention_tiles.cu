@@ -2,22 +2,23 @@
 // 5th-generation tensor cores.
 //
 // A CTA takes 256 query rows (tokens x heads of one key head, two tiles of 128) and a stretch of the context
-// in steps of 128 tokens.  Warps 8-11 turn level bytes into fp16 levels: keys as rows [token][dim], values
+// in steps of 128 tokens.  Warps 16-19 turn level bytes into fp16 levels: keys as rows [token][dim], values
 // transposed, [dim][token], both in the 128-byte swizzled K-major layout that tcgen05.mma reads; they load a
-// step ahead into registers, so pages of any size cost nothing but the address arithmetic.  Warp 12 issues
+// step ahead into registers, so pages of any size cost nothing but the address arithmetic.  Warp 20 issues
 //     S_h = Q_h K^T  (fp16, fp32 accumulator in TMEM),    O_h += W_h V  (W_h in TMEM, where S_h was)
-// in half steps of 64 tokens, two of S_h at a time per tile, so that a tile's softmax (warps 0-3 and 4-7) finds
-// its next scores ready; all 512 TMEM columns are in use.  A row's reference moves only when its maximum has
-// outgrown it by 2^3; the weights are then made again and its part of O_h is rescaled.
+// in half steps of 64 tokens, two of S_h at a time per tile, so that a tile's softmax (warps 0-7 and 8-15, 16 rows
+// each) finds its next scores ready; all 512 TMEM columns are in use.  A row's reference moves only when its maximum
+// has outgrown it by 2^3; the weights are then made again and its part of O_h is rescaled.
 //
-// What bounds it (dim 128, 8 bits; cycles per step of 128 tokens and both tiles, of 6450 measured): the tensor
-// cores 3100 (2048 at the full rate; products 64 wide pay for reading Q again), the exponentials 2048 of the
-// special-function units, shared memory some 3900 at 128 bytes a cycle.  None is full: two softmax warps per
-// scheduler do not cover each other's latencies, and registers (512 x 128) leave no room for more.  2048 tokens
-// over 10240, 32 heads on 8: 518 us, 597 TFLOP/s.  On the way: 1181 us with row-per-thread softmax and loads as
-// they were needed, 715 with everything loaded a step ahead, 690 with constants shared by four rows a thread and
-// half steps, 518 once the issuing warp ran its loop with all lanes (see mbar_wait_warp).  Fetching S before the
-// weights of the half step before are handed over was slower (574-635), as were more registers for the softmax (543).
+// What bounds it (dim 128, 8 bits; cycles per step of 128 tokens and both tiles, of 5800 measured): shared memory
+// some 4700 at 128 bytes a cycle (the products' operands 2000 -- those 64 wide read Q again for every half step -- the
+// softmax's constants, which all 16 warps read, 1500, the levels' stores 600), the issue slots 3100, the tensor cores
+// 2000 at their full rate, the exponentials 2048 of the special-function units.  None is full, each phase waits for
+// another one's.  2048 tokens over 10240, 32 heads on 8: 503 us, 615 TFLOP/s.  On the way: 1181 us with row-per-thread
+// softmax and loads as they were needed, 715 with everything loaded a step ahead, 690 with constants shared by four
+// rows a thread and half steps, 518 once the issuing warp ran its loop with all lanes (see mbar_wait_warp), 508 with
+// sixteen softmax warps for eight.  Fetching S before the weights of the half step before are handed over was slower
+// (574-635), as were more registers for eight softmax warps (543); a second issuing warp changed nothing (509).
 #include "mpq_attention.cuh"
 
 namespace mpq {
@@ -176,7 +177,7 @@ attn_tiles_kernel(const AttnArgs g) {
             };
             {
                 // A warp stages the 16 rows that it has in the loop as fp16, each scaled by a power of two: two threads a row,
-                // every second 16 bytes each, all loads at once (a thread per row, in four rounds of loads, took NN us more).
+                // every second 16 bytes each, all loads at once (a thread per row, in four rounds of loads, took 3 us more).
                 const int in_tile = quarter * 32 + sixteen * 16 + (lane >> 1), odd = lane & 1;
                 bool live;
                 int token, head;
