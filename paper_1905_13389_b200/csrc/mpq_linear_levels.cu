@@ -257,18 +257,19 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 // each CTA holds half of them and 128 of the 256 activation rows.  Persistent: pair p takes tiles p, p + pairs, ...;
 // two accumulators in TMEM, so a tile is stored while the next one is multiplied.  The store goes through a
 // shared-memory transpose, after which a lane owns two columns (their constants in registers) and a warp writes whole
-// row pieces whatever the row stride is.
+// row pieces whatever the row stride is.  Sixteen warps store (eight: 60.2 us for 57.7 at 4096^3, 45.9 for 41.5 at
+// 777 x 5001 x 4100 with an unaligned residual and output).
 // What bounds it: the operands' way from L2, 24 KB per CTA and 128 bytes of k, some 45 bytes a cycle and multiprocessor;
-// 4096^3 takes 55 us bare and 61 with bias and GELU, 2.5 and 2.26 POP/s, tensor pipes 57 % active.  256 x 256 tiles read a
+// 4096^3 with bias and GELU takes 57.7 us, 2.38 POP/s.  256 x 256 tiles read a
 // quarter less but leave the last of their 3.5 rounds half empty: 62 us; 1024 x 4096 x 4096 23.5, these 22.0.
-constexpr int kPairStoreWarps = 8;                        // two per quarter of the TMEM lanes, each with half of the columns
+constexpr int kPairStoreWarps = 16;                       // four per quarter of the TMEM lanes: two for each half of the columns
 constexpr int kPairThreads = 64 + 32 * kPairStoreWarps;
 constexpr int kPairCols = 128;
 struct PairShape {
     static constexpr int stage_bytes = (128 + kPairCols / 2) * kBlock;   // per CTA
     static constexpr int stages = 6;
     static constexpr int row_words = 64;                            // column pair p of row r lies at pair p ^ r: no bank conflicts either way
-    static constexpr int transpose_bytes = kPairStoreWarps * 32 * row_words * 4;
+    static constexpr int transpose_bytes = kPairStoreWarps / 2 * 32 * row_words * 4;
     static constexpr int smem = stages * stage_bytes + transpose_bytes + 1024;
 };
 
@@ -365,8 +366,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             }
         }
     } else if (warp >= 2) {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        uint32_t* sh = transpose + (warp - 2) * 32 * Shape::row_words;
+        // two warps share 32 rows of 64 columns: each brings half of the columns into the transpose and stores half of the rows
+        const int quarter = warp & 3, half = (warp - 2) >> 3, part = ((warp - 2) >> 2) & 1;
+        const int block = half * 4 + quarter, c0 = half * (BN / 2);
+        uint32_t* sh = transpose + block * 32 * Shape::row_words;
+        auto block_sync = [&] { asm volatile("bar.sync %0, 64;" ::"r"(1 + block) : "memory"); };
+        bool ok = true;
         const T* res = static_cast<const T*>(g.res);
         T* out = static_cast<T*>(g.out);
         // Where rows start on a multiple of two elements a lane owns two adjacent columns, elsewhere columns 32 apart
@@ -383,38 +388,33 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             const int rows = (int)min((int64_t)32, g.m - row0);                    // 0 or less: none of them exists
             RowTerm mine = {0.0f, 0u};                                             // lane's row; handed round by shuffles
             if (lane < rows) mine = row_term(g, row0 + lane);
-            if (!mbar_wait_warp(acc_full(acc), (i >> 1) & 1, &failed) || __any_sync(0xffffffffu, has_failed())) break;
-            tmem_fence_after();
-#pragma unroll 1
-            for (int c0 = half * (BN / 2); c0 < (half + 1) * (BN / 2); c0 += 64) {
-                const int64_t cx = (int64_t)n0 + c0 + ca, cy = (int64_t)n0 + c0 + cb;
-                const bool in_x = cx < g.n, in_y = cy < g.n;
-                ColTerm ct[2] = {{0.0f, 0u, 0.0f}, {0.0f, 0u, 0.0f}};
-                if (in_x) ct[0] = col_term(g, cx);
-                if (in_y) ct[1] = col_term(g, cy);
-                const bool fast = twos && n0 + c0 + 64 <= g.n;
-                const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + c0);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t v[32];
-                    tmem_load32(from + h * 32, v);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2)
-                        *reinterpret_cast<uint2*>(sh + lane * Shape::row_words + 2 * ((h * 16 + j / 2) ^ lane)) = make_uint2(v[j], v[j + 1]);
-                }
+            ok = ok && mbar_wait_warp(acc_full(acc), (i >> 1) & 1, &failed) && !__any_sync(0xffffffffu, has_failed());
+            const int64_t cx = (int64_t)n0 + c0 + ca, cy = (int64_t)n0 + c0 + cb;
+            const bool in_x = cx < g.n, in_y = cy < g.n;
+            ColTerm ct[2] = {{0.0f, 0u, 0.0f}, {0.0f, 0u, 0.0f}};
+            if (in_x) ct[0] = col_term(g, cx);
+            if (in_y) ct[1] = col_term(g, cy);
+            const bool fast = twos && n0 + c0 + 64 <= g.n;
+            if (ok) {
+                tmem_fence_after();
+                uint32_t v[32];
+                tmem_load32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + c0 + part * 32), v);
+                tmem_wait_ld();
+                tmem_fence_before();
                 __syncwarp();
-                if (c0 + 64 >= (half + 1) * (BN / 2)) {    // this warp's part of the accumulator is read
-                    tmem_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(acc), 0));
-                }
+                if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(acc), 0));       // this warp's part of the accumulator is read
+#pragma unroll
+                for (int j = 0; j < 32; j += 2)
+                    *reinterpret_cast<uint2*>(sh + lane * Shape::row_words + 2 * ((part * 16 + j / 2) ^ lane)) = make_uint2(v[j], v[j + 1]);
+            }
+            block_sync();                                                              // after a failure only the barriers are kept up
+            if (ok) {
                 // kRowsAtOnce rows at a time.  All residuals of a group are requested before any is used or any result is
                 // written: they may lie in the result's own tensor, so the compiler could not move a load up by itself, and
                 // one load after the other took 45 us of a tile's 51.  (All 32 rows at once spill: 61 -> 78 us at 4096^3.)
                 constexpr int kRowsAtOnce = 8;
 #pragma unroll 1
-                for (int r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
+                for (int r0 = part * 16; r0 < min(rows, part * 16 + 16); r0 += kRowsAtOnce) {
                     const bool all_rows = r0 + kRowsAtOnce <= rows;
                     T* o = out + (row0 + r0) * g.ldo;
                     const T* q = res + (row0 + r0) * g.ldr;
@@ -461,8 +461,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         }
                     }
                 }
-                __syncwarp();
             }
+            block_sync();
         }
     }
     __syncwarp();
