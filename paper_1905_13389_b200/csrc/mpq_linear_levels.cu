@@ -260,8 +260,8 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 // row pieces whatever the row stride is.  Sixteen warps store (eight: 60.2 us for 57.7 at 4096^3, 45.9 for 41.5 at
 // 777 x 5001 x 4100 with an unaligned residual and output).
 // What bounds it: the operands' way from L2, 24 KB per CTA and 128 bytes of k, some 45 bytes a cycle and multiprocessor;
-// 4096^3 with bias and GELU takes 57.7 us, 2.38 POP/s.  256 x 256 tiles read a
-// quarter less but leave the last of their 3.5 rounds half empty: 62 us; 1024 x 4096 x 4096 23.5, these 22.0.
+// 4096^3 with bias and GELU takes 57.7 us, 2.38 POP/s.  256 x 256 tiles read a quarter less but leave the last of their
+// 3.5 rounds half empty (62 us for 61 with eight storing warps; 1024 x 4096 x 4096 23.5 for 22.0).
 constexpr int kPairStoreWarps = 16;                       // four per quarter of the TMEM lanes: two for each half of the columns
 constexpr int kPairThreads = 64 + 32 * kPairStoreWarps;
 constexpr int kPairCols = 128;
@@ -529,16 +529,17 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     return launch_chained_as(true, kernel, ctas, (unsigned)kPairThreads, Shape::smem, st, map_a, map_w, g, (int)tiles_m, (int)tiles);
 }
 
-// Which form.  Up to 64 rows the weights' own traffic decides: the small form, its tile just wide enough.  Above, CTA
-// pairs, unless their 256 x 128 tiles are so few that splitting k pays more than reading the weights once: us for
-// m x n x k, pairs / small with 64 rows --
-//   16 tiles: 300 x 1000 x 9000 29 / 22, 1000 x 500 x 500 10.6 / 11.7;  8 tiles: 256 x 1024 x 1024 10.4 / 9.4;
-//   32 tiles: 200 x 4096 x 4096 17 / 24;  71 tiles: 130 x 9000 x 1000 15 / 27.
+// Which form.  Up to 64 rows the weights' own traffic decides: the small form, its tile just wide enough.  Above, the
+// small form too while its 128 x 64 tiles fit the device at once (it may split k then), else CTA pairs: us for
+// m x n x k, small / pairs --
+//   64 tiles: 128 x 4096 x 4096 11.8 / 15.2;  128: 200 x 4096 x 4096 12.5 / 15.2;  142: 100 x 9000 x 1000 9.4 / 11.9;
+//   144: 128 x 9216 x 4096 14.3 / 17.1, 2300 x 512 x 9216 19.5 / 22.4;  150: 128 x 9600 x 4096 23.7 / 22.4;
+//   213: 130 x 9000 x 1000 16.6 / 12.6;  256: 1000 x 2000 x 2000 19.8 / 13.1.
 template <typename T>
 int launch_linear_levels(const LinearArgs& g, cudaStream_t st) {
     if (g.m <= 16) return launch_linear_small<T, 16>(g, st);
     if (g.m <= 32) return launch_linear_small<T, 32>(g, st);
-    if (g.m <= 64 || ceil_div(g.m, 256) * ceil_div(g.n, kPairCols) < 24) return launch_linear_small<T, 64>(g, st);
+    if (g.m <= 64 || ceil_div(g.m, 64) * ceil_div(g.n, 128) <= sm_count()) return launch_linear_small<T, 64>(g, st);
     return launch_linear_pair<T>(g, st);
 }
 

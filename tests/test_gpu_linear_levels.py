@@ -75,6 +75,18 @@ def test_epilogues(mpq, cuda, act, out_type, m):
         check(mpq, cuda, m, 200, 320, 8, 8, act, bias, residual, out_type, 77)
 
 
+# more 128 x 64 tiles than multiprocessors: CTA pairs, with one tile each, with several, with rows and columns left over
+MANY = [(513, 2177, 272), (777, 1601, 100), (2600, 1201, 200), (4097, 1001, 130), (1024, 2560, 512), (130, 9001, 48)]
+
+
+@pytest.mark.parametrize("m,n,k", MANY)
+@pytest.mark.parametrize("out_type", list(TYPES))
+def test_many_tiles(mpq, cuda, m, n, k, out_type):
+    check(mpq, cuda, m, n, k, 8, 8, "none", False, False, out_type, m + n + k)
+    check(mpq, cuda, m, n, k, 8, 8, "silu", True, True, out_type, m + n + k + 5)
+    check(mpq, cuda, m, n, k, 3, 5, "gelu", True, True, out_type, m + n + k + 6)
+
+
 @pytest.mark.parametrize("a_bits,w_bits", [(1, 1), (8, 1), (2, 8), (4, 4), (5, 3)])
 @pytest.mark.parametrize("m", [2, 40, 140])
 def test_widths(mpq, cuda, a_bits, w_bits, m):
