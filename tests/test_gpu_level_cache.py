@@ -265,6 +265,25 @@ def test_split_contexts_and_launch_hints(mpq, cuda, q_lens, kv_lens, bits):
     c.check(window=700)
 
 
+@pytest.mark.parametrize("q_lens,kv_lens,heads,kv_heads", [
+    ([1], [900], 32, 8), ([1, 1, 1], [700, 0, 40], 8, 2), ([1, 0, 1], [1024, 5, 129], 5, 5), ([2, 1], [1000, 200], 16, 2),
+    ([70], [4000], 8, 2), ([300, 1, 2], [1500, 30, 0], 6, 2), ([40, 33], [2100, 33], 20, 1)])
+@pytest.mark.parametrize("dim,bits,dtype", [(128, 8, "bf16"), (64, 4, "f16")])
+def test_splits_of_one_cluster(mpq, cuda, q_lens, kv_lens, heads, kv_heads, dim, bits, dtype):
+    """Few enough splits join without a workspace: contexts that use all of them, some, one and none."""
+    assert mpq.cache_attention_workspace(sum(q_lens), len(q_lens), heads, kv_heads, dim, max(q_lens), max(kv_lens)) == 0
+    c = Case(mpq, cuda, q_lens, kv_lens, heads, kv_heads, dim, bits, 24, TYPES[dtype])
+    c.check()
+    c.check(causal=False)
+    c.check(window=600)
+    c.check(window=50)
+
+
+def test_sizes_past_the_call_need_no_workspace(mpq, cuda):
+    assert mpq.cache_attention_workspace(2 ** 62, 2 ** 30, 8, 2, 128, 2 ** 62, 2 ** 62) == 0
+    assert mpq.cache_attention_workspace(1, 1, 8, 2, 128, 2 ** 62, 2 ** 62) > 0
+
+
 @pytest.mark.parametrize("bits", [8, 4])
 @pytest.mark.parametrize("q_len", [1, 4, 40])
 def test_long_contexts_keep_their_precision(mpq, cuda, q_len, bits):
