@@ -387,7 +387,8 @@ int mpq_cache_read(const uint8_t* k_levels, const float* k_scale, const uint8_t*
  *   pos = kv_lens[b] - n + i:   j <= pos if causal, j > pos - window if window > 0, j < kv_lens[b];
  * a token of the context whose page number lies outside the cache is not seen.
  *   out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j);  lse = log sum_j p_j (optional, [tokens][heads]).
- * A row that sees nothing gets out = 0 and lse = -infinity.  heads is a multiple of kv_heads; query
+ * A row that sees nothing gets out = 0 and lse = -infinity.  A row that sees a token with a NaN range or an infinite
+ * key range, or that is not finite itself and sees anything, gets out = NaN and lse = NaN.  heads is a multiple of kv_heads; query
  * head h reads key head h / (heads / kv_heads).  dim is 64 or 128; dtype (q and out) MPQ_F16 or MPQ_BF16.
  * max_q and max_kv are the caller's upper bounds on a sequence's new tokens and context; they choose
  * the launch (how rows are tiled, how far a context is split), any value gives the same sums.

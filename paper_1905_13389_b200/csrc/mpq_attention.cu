@@ -121,7 +121,7 @@ attn_rows_kernel(const AttnArgs g) {
     using R = Ring<kRowBytes, NQ>;
     constexpr int kTile = R::tile, kStages = R::stages;
     extern __shared__ __align__(128) unsigned char ring_raw[];            // [warps][stages][keys, values, ranges]; the merge's rows afterwards
-    __shared__ float sh_ml[kWarps][kRows][2];
+    __shared__ float sh_ml[kWarps][kRows][2], sh_bad[kRows];              // sh_bad: NaN for a query row that is not finite, else 0
     float (*sh_o)[kRows][D + 4] = reinterpret_cast<float (*)[kRows][D + 4]>(ring_raw);
 
     chain_entry();
@@ -209,17 +209,20 @@ attn_rows_kernel(const AttnArgs g) {
     for (int n = 0; n < NQ; ++n) {
         float amax = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kKeyWords * kPerWord; ++i) amax = fmaxf(amax, fabsf(to_f32(raw[n][i])));
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        for (int i = 0; i < kKeyWords * kPerWord; ++i) amax = max_nan(amax, fabsf(to_f32(raw[n][i])));
+        amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        const bool finite = ordinary(amax);               // otherwise the row is computed with q = 0
+        if (warp == 0 && t4 == 0) sh_bad[gr + 8 * n] = finite ? 0.0f : kNaN;
         float down, up, sum = 0.0f;
-        row_power(amax, down, up);
+        row_power(finite ? amax : 0.0f, down, up);
 #pragma unroll
         for (int s = 0; s < kSteps; ++s)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int reg = s * 2 + i, low = reg / kPairs * kPerWord + (BITS == 8 ? 2 : 1) * (reg % kPairs);   // as key_pair pairs them
-                const __half2 h = __floats2half2_rn(to_f32(raw[n][low]) * down, to_f32(raw[n][low + (BITS == 8 ? 1 : 4)]) * down);
+                const float a = to_f32(raw[n][low]) * down, b = to_f32(raw[n][low + (BITS == 8 ? 1 : 4)]) * down;
+                const __half2 h = __floats2half2_rn(finite ? a : 0.0f, finite ? b : 0.0f);
                 qf[n][s][i] = *reinterpret_cast<const uint32_t*>(&h);
                 sum += __low2float(h) + __high2float(h);
             }
@@ -231,7 +234,7 @@ attn_rows_kernel(const AttnArgs g) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const int src = (t4 * 2 + e) * 4;
-            row_scale[n][e] = __shfl_sync(0xffffffffu, up, src) * g.scale_log2;
+            row_scale[n][e] = row_factor(__shfl_sync(0xffffffffu, up, src), g.scale_log2);
             q_sum[n][e] = __shfl_sync(0xffffffffu, sum, src);
             first[n][e] = __shfl_sync(0xffffffffu, from, src);
             last[n][e] = __shfl_sync(0xffffffffu, upto, src);
@@ -285,7 +288,7 @@ attn_rows_kernel(const AttnArgs g) {
         float lg, inv;
         range_exponent(vs, lg, inv);
         const bool here = vs != -1.0f;
-        const float kf = ranges[lane] * (1.0f / (float)((1 << BITS) - 1));
+        const float kf = key_factor<BITS>(ranges[lane]);
         lg = here ? lg : -INFINITY;                       // a token that is not there: weight 0
         inv = here ? inv : 0.0f;
         const bool partial = c0 < first_of_all || c0 + kChunk - 1 > last_of_all;
@@ -384,7 +387,7 @@ attn_rows_kernel(const AttnArgs g) {
                 wsum[n][e] += __shfl_xor_sync(0xffffffffu, wsum[n][e], d);
             }
             const int r = n * 8 + t4 * 2 + e;
-            if (gr == 0) { sh_ml[warp][r][0] = m[n][e]; sh_ml[warp][r][1] = l[n][e]; }
+            if (gr == 0) { sh_ml[warp][r][0] = part_reference(m[n][e], l[n][e]); sh_ml[warp][r][1] = l[n][e]; }
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
                 *reinterpret_cast<float2*>(&sh_o[warp][r][gr * (D / 8) + 2 * i]) = make_float2(o[i][n][e] + wsum[n][e], o[i][n][2 + e] + wsum[n][e]);
@@ -403,6 +406,7 @@ attn_rows_kernel(const AttnArgs g) {
             f[w] = mw == -INFINITY ? 0.0f : fast_exp2(mw - top);
             den = mw == -INFINITY ? den : fmaf(sh_ml[w][r][1], f[w], den);
         }
+        if (top != -INFINITY) den += sh_bad[r];
         const int token = (t.row0 + r) / g.group, head = kv_head * g.group + (t.row0 + r) % g.group;
         const int64_t at = (int64_t)(t.q0 + token) * g.heads + head, slot = at * g.splits + blockIdx.z;
         T* out = static_cast<T*>(g.out) + (int64_t)(t.q0 + token) * g.o_ts + (int64_t)head * g.o_hs;

@@ -17,6 +17,11 @@
 // Queries are scaled by a power of two per row before they become fp16, so nothing overflows or is lost
 // beside the row's largest element.  Ranges below 2^-90 (all-zero values among them) count as 2^-90
 // in the exponent, and a result below 2^-89 in magnitude is stored as 0.
+// What is not finite comes out where it is seen.  A token's NaN (or a key's infinite) range makes the scores of the
+// rows that see it NaN, and with them l; maxima ignore NaNs, so a part of a row whose scores are ALL NaN has no
+// reference and l = NaN, and hands its sums on with the reference +infinity, which wins every join and turns the row
+// into NaNs (part_reference).  A query row that is not finite takes part as zeros, so that masks and missing tokens
+// need no care, and its denominator becomes NaN at the end if it has seen anything.
 #pragma once
 #include "mpq_levels.cuh"
 #include "mpq_tensor.cuh"
@@ -136,6 +141,14 @@ __device__ __forceinline__ void range_exponent(float s, float& lg, float& inv) {
     lg = __log2f(s < kTinyRange ? kTinyRange : s);           // NaN passes through
     inv = lg == lg ? exp2f(-lg) : 0.0f;                      // may be subnormal
 }
+// Factor of a key's range: range / L, NaN for an infinite range (0 * infinity): a score of minus infinity would hide it.
+template <int BITS>
+__device__ __forceinline__ float key_factor(float s) {
+    const float f = s * (1.0f / (float)((1 << BITS) - 1));
+    return fmaf(s, 0.0f, f);
+}
+// Reference that a part of a row hands on with its denominator l: -infinity where it has seen nothing.
+__device__ __forceinline__ float part_reference(float m, float l) { return m == -INFINITY && l != 0.0f ? INFINITY : m; }
 
 __device__ __forceinline__ float final_value(float o) { return fabsf(o) < 2.0f * kTinyRange ? 0.0f : o; }
 
@@ -146,6 +159,9 @@ __device__ __forceinline__ void row_power(float amax, float& down, float& up) {
     down = __uint_as_float((uint32_t)(127 - e) << 23);
     up = __uint_as_float((uint32_t)(127 + e) << 23);
 }
+// Factor of a query row's scores, finite: times a score of 0 it has to stay 0.
+__device__ __forceinline__ float row_factor(float up, float scale_log2) { return fminf(fmaxf(up * scale_log2, -3.402823466e38f), 3.402823466e38f); }
+constexpr float kNaN = __builtin_nanf("");
 
 constexpr int kJoined = 8;                                // splits that a cluster can hold
 __device__ __forceinline__ float ld_cluster(uint32_t addr) {

@@ -38,7 +38,7 @@ template <int D> struct TileSmem {
     static constexpr int const_stage = 3 * kStepTokens * 4;   // [64 token pairs](key factors, value exponents), [128] value reciprocals
     static constexpr int rows = consts + 2 * const_stage;     // cache row numbers, two steps
     static constexpr int ranges = rows + 2 * kStepTokens * 4; // first and last visible token of each row
-    static constexpr int scales = ranges + kTileRows * 8;     // scale of each row; at the end its (reference, denominator)
+    static constexpr int scales = ranges + kTileRows * 8;     // scale of each row (and NaN if the row is not finite); at the end its (reference, denominator)
     static constexpr int total = scales + kTileRows * 8 + 1024;
 };
 
@@ -203,11 +203,12 @@ attn_tiles_kernel(const AttnArgs g) {
                 for (int c = 0; c < D / 16; ++c) {
                     const T* e = reinterpret_cast<const T*>(&raw[c]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(to_f32(e[i])));
+                    for (int i = 0; i < 8; ++i) amax = max_nan(amax, fabsf(to_f32(e[i])));
                 }
-                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+                amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+                const bool finite = ordinary(amax);                      // otherwise the row is computed with q = 0
                 float down, up;
-                row_power(amax, down, up);
+                row_power(finite ? amax : 0.0f, down, up);
                 const uint32_t tile = base + Smem::q + h * Smem::q_tile;
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) {
@@ -216,7 +217,8 @@ attn_tiles_kernel(const AttnArgs g) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int a = BITS == 8 ? 2 * i : i, b = BITS == 8 ? 2 * i + 1 : i + 4;
-                        const __half2 v = __floats2half2_rn(to_f32(e[a]) * down, to_f32(e[b]) * down);
+                        const float qa = to_f32(e[a]) * down, qb = to_f32(e[b]) * down;
+                        const __half2 v = __floats2half2_rn(finite ? qa : 0.0f, finite ? qb : 0.0f);
                         w[i] = *reinterpret_cast<const uint32_t*>(&v);
                     }
                     const int at = 2 * c + odd;
@@ -227,7 +229,7 @@ attn_tiles_kernel(const AttnArgs g) {
                     row_range(g, t, token, first, last);
                     if (!live) { first = 0; last = 0x7fffffff; }         // computed with q = 0, never stored
                     ranges[in_tile] = make_int2(first, last);
-                    scales[in_tile] = make_float2(up * g.scale_log2, 0.0f);
+                    scales[in_tile] = make_float2(row_factor(up, g.scale_log2), finite ? 0.0f : kNaN);
                 }
                 proxy_fence();
                 __syncwarp();
@@ -370,7 +372,8 @@ attn_tiles_kernel(const AttnArgs g) {
                 sum += odd;
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                if ((lane & 3) == 0) scales[row0 + 8 * k] = make_float2(set[k], sum);
+                const float ref = part_reference(set[k], sum);
+                if ((lane & 3) == 0) scales[row0 + 8 * k] = make_float2(ref, ref == -INFINITY ? sum : sum + scales[row0 + 8 * k].y);
             }
             tile_sync();
             ok = mbar_wait_or(o_full, 0, &failed);
@@ -494,7 +497,7 @@ attn_tiles_kernel(const AttnArgs g) {
                 float lg, inv;
                 range_exponent(vs, lg, inv);
                 const bool here = vs != -1.0f;
-                consts[(th >> 1) * 4 + (th & 1)] = ks * (1.0f / (float)((1 << BITS) - 1));
+                consts[(th >> 1) * 4 + (th & 1)] = key_factor<BITS>(ks);
                 consts[(th >> 1) * 4 + 2 + (th & 1)] = here ? lg : -INFINITY;    // a token that is not there: weight 0
                 consts[2 * kStepTokens + th] = here ? inv : 0.0f;
                 {

@@ -114,6 +114,12 @@ __device__ __forceinline__ float finite_sum(const float (&x)[N]) {
     return z;
 }
 __device__ __forceinline__ bool ordinary(float v) { return fabsf(v) < __int_as_float(0x7f800000); }             // neither NaN nor infinite
+// max(a, b), NaN where either is one (fmaxf would give the other).
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 // Level bytes of four shifted levels (a level is below 2^8: the low byte of the float's bits).
 __device__ __forceinline__ uint32_t level_word(float a, float b, float c, float d) {
     return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040),
