@@ -47,7 +47,7 @@ template <int N>
 __device__ __forceinline__ void glue_values(float (&f)[N], int glue) {
     if (glue == MPQ_GLUE_RELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = fmaxf(f[i], 0.0f);
+        for (int i = 0; i < N; ++i) f[i] = max_nan(f[i], 0.0f);       // a NaN range stays visible, as under the other activations
     } else if (glue == MPQ_GLUE_GELU) {
 #pragma unroll
         for (int i = 0; i < N; ++i) f[i] = 0.5f * f[i] * (1.0f + erff(f[i] * 0.70710678118654752f));
