@@ -22,7 +22,10 @@ struct RowArgs {
 // max |y| = r max |h gain| to the last bit: both statistics come out of ONE pass.
 // The row's constants follow from them in the first warp alone: a root and four exact divisions in every thread were
 // a third of the kernel's instructions, and it is bound by issuing them (0.78 of the issue slots).
+// Under the norm the largest magnitude keeps NaNs: an infinite element gives r = 0, and its product with a gain of 0 or
+// with r is the NaN that the row's range has to be.  Without the norm a NaN takes no part in the range.
 struct RowScalars { float r, s, inv, alpha; };
+template <bool NORM> __device__ __forceinline__ float larger(float a, float b) { return NORM ? max_nan(a, b) : fmaxf(a, b); }
 template <bool NORM>
 __device__ __forceinline__ RowScalars row_scalars(float ss, float mx, const RowArgs& g) {
     RowScalars c;
@@ -37,7 +40,7 @@ __device__ __forceinline__ RowScalars block_scalars(float ss, float mx, const Ro
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         if (NORM) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        mx = larger<NORM>(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     }
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
     if (warps == 1) return row_scalars<NORM>(ss, mx, g);
@@ -49,7 +52,7 @@ __device__ __forceinline__ RowScalars block_scalars(float ss, float mx, const Ro
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             if (NORM) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            mx = larger<NORM>(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         }
         const RowScalars c = row_scalars<NORM>(ss, mx, g);
         if (lane == 0) *sh_scalars = c;
@@ -170,7 +173,7 @@ level_rows_kernel(const RowArgs g) {
                 }
             }
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) mx = fmaxf(mx, ACT == MPQ_ACT_HRELU ? h[j][e] : fabsf(h[j][e]));
+            for (int e = 0; e < VEC; ++e) mx = larger<NORM>(mx, ACT == MPQ_ACT_HRELU ? h[j][e] : fabsf(h[j][e]));
         }
     }
     const RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
@@ -218,7 +221,7 @@ level_wide_rows_kernel(const RowArgs g) {
             ss = fmaf(h, h, ss);
             if (g.gain) h *= g.gain[i];
         }
-        mx = fmaxf(mx, ACT == MPQ_ACT_HRELU ? h : fabsf(h));
+        mx = larger<NORM>(mx, ACT == MPQ_ACT_HRELU ? h : fabsf(h));
     }
     const RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
     const float r = c.r, s = c.s, inv = c.inv, alpha = c.alpha;
