@@ -334,7 +334,8 @@ int64_t mpq_level_row_bytes(int64_t k);
  * residual_out (h rounded once to dtype; may be NULL) may be the same tensor as x or residual.
  * gain: k floats or NULL (ones).  levels / scale / sums as above, all required.  values (optional,
  * [rows x k] of values_dtype, row stride ldv): the numbers the levels stand for, rounded once, for
- * consumers that stay in full precision.  A row with a NaN or an infinity gets a NaN range.
+ * consumers that stay in full precision.  A row with a NaN or an infinity gets a NaN range; a finite row keeps its range
+ * also where its squares overflow fp32 (they are then summed in another scale).
  * rows = 0 is allowed and does nothing.  k < 2^23. */
 int mpq_rmsnorm_levels(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype,
                        const float* gain, float eps, int64_t rows, int64_t k, int bits,

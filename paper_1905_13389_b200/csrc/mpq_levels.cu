@@ -24,26 +24,32 @@ struct RowArgs {
 // a third of the kernel's instructions, and it is bound by issuing them (0.78 of the issue slots).
 // Under the norm the largest magnitude keeps NaNs: an infinite element gives r = 0, and its product with a gain of 0 or
 // with r is the NaN that the row's range has to be.  Without the norm a NaN takes no part in the range.
+// A finite row whose sum of squares overflows fp32 gives r = 0 as well.  Every thread sees that, the row is read again
+// and (2^-80 h)^2 is summed (`scaled`), so it keeps its range.  residual_out, which may lie over the inputs, is therefore
+// stored after the statistics (29.6 -> 30.4 us at 4096 x 4096; a second sum beside the ordinary one: 31.4).
+constexpr float kDown = 8.271806125530277e-25f;                          // 2^-80: 2^23 squares of 2^48 fit
 struct RowScalars { float r, s, inv, alpha; };
 template <bool NORM> __device__ __forceinline__ float larger(float a, float b) { return NORM ? max_nan(a, b) : fmaxf(a, b); }
 template <bool NORM>
-__device__ __forceinline__ RowScalars row_scalars(float ss, float mx, const RowArgs& g) {
+__device__ __forceinline__ RowScalars row_scalars(float ss, float mx, const RowArgs& g, bool scaled) {
     RowScalars c;
-    c.r = NORM ? __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)g.k), g.eps))) : 1.0f;
+    const float eps = scaled ? g.eps * kDown * kDown : g.eps;
+    c.r = NORM ? __fdiv_rn(scaled ? kDown : 1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)g.k), eps))) : 1.0f;
+    if (scaled && !ordinary(ss)) mx = __int_as_float(0x7fffffff);        // NaN: an element is infinite
     c.s = NORM ? mx * c.r : mx;
     c.inv = inverse_scale(c.s);
     c.alpha = __fdiv_rn(c.s, (float)g.rule.L);
     return c;
 }
 template <bool NORM>
-__device__ __forceinline__ RowScalars block_scalars(float ss, float mx, const RowArgs& g, float2* sh, RowScalars* sh_scalars) {
+__device__ __forceinline__ RowScalars block_scalars(float ss, float mx, const RowArgs& g, float2* sh, RowScalars* sh_scalars, bool scaled = false) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         if (NORM) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         mx = larger<NORM>(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     }
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    if (warps == 1) return row_scalars<NORM>(ss, mx, g);
+    if (warps == 1) return row_scalars<NORM>(ss, mx, g, scaled);
     if (lane == 0) sh[threadIdx.x >> 5] = make_float2(ss, mx);
     __syncthreads();
     if (threadIdx.x < 32) {
@@ -54,11 +60,23 @@ __device__ __forceinline__ RowScalars block_scalars(float ss, float mx, const Ro
             if (NORM) ss += __shfl_xor_sync(0xffffffffu, ss, o);
             mx = larger<NORM>(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         }
-        const RowScalars c = row_scalars<NORM>(ss, mx, g);
+        const RowScalars c = row_scalars<NORM>(ss, mx, g, scaled);
         if (lane == 0) *sh_scalars = c;
     }
     __syncthreads();
     return *sh_scalars;
+}
+// This thread's share of the row's squares in that scale.  Not inlined: inside the kernel the loop, which hardly any call
+// reaches, cost 5 us of 30.
+template <typename T>
+__device__ __noinline__ float small_squares(const T* x, const T* res, int k) {
+    float ss = 0.0f;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < k; i += blockDim.x) {
+        const float v = (to_f32(x[i]) + (res ? to_f32(res[i]) : 0.0f)) * kDown;
+        ss = fmaf(v, v, ss);
+    }
+    return ss;
 }
 __device__ __forceinline__ void block_level_sum(int u, int32_t* dst, int* sh) {
     u = __reduce_add_sync(0xffffffffu, u);
@@ -91,6 +109,18 @@ __device__ __forceinline__ void store_part(T* p, const float (&f)[N], int count)
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) if (i < count) p[i] = from_f32<T>(f[i]);
+    }
+}
+// ... the same of values already rounded to T
+template <typename T, int N> struct alignas(N * sizeof(T)) Rounded { T e[N]; };
+template <typename T, int N, bool VECTOR>
+__device__ __forceinline__ void store_rounded(T* p, const Rounded<T, N>& v, int count) {
+    if constexpr (VECTOR) {
+        static_assert(sizeof(v) == 16, "one vector");
+        *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) if (i < count) p[i] = v.e[i];
     }
 }
 // Level bytes of N elements, `count` of them inside the row; returns the sum of the levels.  Level rows are 16-byte
@@ -150,12 +180,16 @@ level_rows_kernel(const RowArgs g) {
         }
     }
     float ss = 0.0f, mx = 0.0f;
+    Rounded<T, VEC> sum[NORM ? NV : 1];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int i = threadIdx.x + j * blockDim.x;
         if (i < nvec) {
             if (NORM) {
-                if (g.res_out) store_part<T, VEC, VECTOR>(static_cast<T*>(g.res_out) + row * g.ldo + (int64_t)i * VEC, h[j], k - i * VEC);
+                if (g.res_out) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[j].e[e] = from_f32<T>(h[j][e]);
+                }
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) ss = fmaf(h[j][e], h[j][e], ss);
                 if (g.gain) {
@@ -176,7 +210,8 @@ level_rows_kernel(const RowArgs g) {
             for (int e = 0; e < VEC; ++e) mx = larger<NORM>(mx, ACT == MPQ_ACT_HRELU ? h[j][e] : fabsf(h[j][e]));
         }
     }
-    const RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
+    RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
+    if (NORM && c.r == 0.0f) c = block_scalars<NORM>(small_squares(x, res, k), mx, g, sh_stats, &sh_scalars, true);
     const float r = c.r, s = c.s, inv = c.inv, alpha = c.alpha;
     // (a NaN range, after a NaN or an infinity under the norm, has the reciprocal 0 and is not ordinary)
     const bool plain = ordinary(s) && ordinary(inv);
@@ -186,6 +221,7 @@ level_rows_kernel(const RowArgs g) {
     for (int j = 0; j < NV; ++j) {
         const int i = threadIdx.x + j * blockDim.x;
         if (i < nvec) {
+            if (NORM && g.res_out) store_rounded<T, VEC, VECTOR>(static_cast<T*>(g.res_out) + row * g.ldo + (int64_t)i * VEC, sum[j], k - i * VEC);
             float y[VEC], shifted[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) y[e] = NORM ? h[j][e] * r : h[j][e];
@@ -223,7 +259,8 @@ level_wide_rows_kernel(const RowArgs g) {
         }
         mx = larger<NORM>(mx, ACT == MPQ_ACT_HRELU ? h : fabsf(h));
     }
-    const RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
+    RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
+    if (NORM && c.r == 0.0f) c = block_scalars<NORM>(small_squares(x, res, (int)g.k), mx, g, sh_stats, &sh_scalars, true);
     const float r = c.r, s = c.s, inv = c.inv, alpha = c.alpha;
     uint8_t* out = g.levels + row * g.row_bytes;
     int total = 0;
