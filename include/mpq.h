@@ -382,7 +382,8 @@ int mpq_cache_read(const uint8_t* k_levels, const float* k_scale, const uint8_t*
                    void* v, int64_t v_token_stride, int64_t v_head_stride, int dtype, void* stream);
 
 /* Attention of new tokens over the paged cache (their own keys and values written to it before).
- * Sequence b has the new tokens q_starts[b] .. q_starts[b+1]-1 of q [tokens][heads][dim] and a context
+ * Sequence b has the new tokens q_starts[b] .. q_starts[b+1]-1 of q [tokens][heads][dim] (q_starts ascends from 0;
+ * tokens from q_starts[batch] on belong to no sequence and see nothing) and a context
  * of kv_lens[b] tokens, the new ones last; its token j lies in page table[b][j / page_size] (row stride
  * table_stride; kv_lens beyond table_stride * page_size are cut).  New token i of n sees
  *   pos = kv_lens[b] - n + i:   j <= pos if causal, j > pos - window if window > 0, j < kv_lens[b];

@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(kMergeThreads) attn_merge_kernel(const AttnArg
     for (int s = 0; s < kEarly; ++s)
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) early[s][i] = exists && s < g.splits ? g.part_o[(at * g.splits + s) * D + i * 32 + lane] : 0.0f;
-    // the sequence that holds the token: the last one that starts at or before it
+    // the sequence that holds the token: the last one that starts at or before it (none: the tile itself has stored it)
     int used = 0;
     for (int base = 0; exists && base < g.batch; base += 32) {
         const int i = base + lane;
@@ -537,9 +537,9 @@ __global__ void __launch_bounds__(kMergeThreads) attn_merge_kernel(const AttnArg
     if (g.lse && lane == 0) g.lse[at] = top == -INFINITY ? -INFINITY : (top - kBoost + log2f(den)) * 0.6931471805599453f;
 }
 
-// Tiles of `rows` query rows that `tokens` new tokens in at most `batch` sequences can fill.
-inline int64_t tile_bound(int64_t tokens, int batch, int group, int rows) {
-    return tokens * group / rows + (tokens < batch ? tokens : batch);
+// Tiles of `rows` query rows that `tokens` new tokens in at most `sequences` sequences can fill.
+inline int64_t tile_bound(int64_t tokens, int64_t sequences, int group, int rows) {
+    return tokens * group / rows + (tokens < sequences ? tokens : sequences);
 }
 
 struct AttnPlan { int rows; int64_t tiles; int splits, split_tokens; bool joined; };   // rows of a tile: 8, 16 or kTileRows
@@ -568,12 +568,13 @@ AttnPlan attn_plan(int64_t tokens, int batch, int group, int kv_heads, int64_t m
     p.rows = max_q * group > 32 ? kTileRows : max_q * group > 8 ? 16 : 8;
     const int64_t context = max_kv < 1 ? 1 : max_kv > 0x7fffffff ? 0x7fffffff : max_kv;
     int64_t per, unit;
-    p.tiles = tile_bound(tokens, batch, group, p.rows);
+    p.tiles = tile_bound(tokens, (int64_t)batch + 1, group, p.rows);      // tokens of no sequence are one more (find_tile)
     // tiles to expect: full ones, and half a tile more per sequence; never more than the caller's bound allows
     int64_t likely = batch * ceil_div(max_q < 1 ? group : max_q * group, p.rows);
     const int64_t filled = tokens * group / p.rows + (batch + 1) / 2;
     if (likely > filled && p.rows == kTileRows) likely = filled;
-    if (likely > p.tiles) likely = p.tiles;
+    const int64_t most = tile_bound(tokens, batch, group, p.rows);
+    if (likely > most) likely = most;
     if (p.rows == kTileRows) {
         unit = kStepTokens;
         int64_t splits = 148 / (likely * kv_heads);

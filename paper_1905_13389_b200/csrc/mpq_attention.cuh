@@ -57,18 +57,20 @@ __device__ __forceinline__ void row_range(const AttnArgs& g, const AttnTile& t, 
 }
 
 // The sequence and rows of tile number `index` of R rows each, tiles counted over the sequences in order
-// (all 32 lanes call; the result is the same in every lane).  False: no such tile.
+// (all 32 lanes call; the result is the same in every lane).  False: no such tile.  Tokens past the last sequence (the
+// padding of a captured step) are one sequence more, without a context: their rows see nothing and are stored as such.
 template <int R>
 __device__ __forceinline__ bool find_tile(const AttnArgs& g, int index, AttnTile& t) {
     const int lane = threadIdx.x & 31;
     int before = 0;
-    for (int base = 0; base < g.batch; base += 32) {
+    for (int base = 0; base <= g.batch; base += 32) {
         const int b = base + lane;
         int q0 = 0, n = 0, kv = 0;
-        if (b < g.batch) {
-            kv = g.kv_lens[b];
+        if (b <= g.batch) {
+            if (b < g.batch) kv = g.kv_lens[b];
             q0 = (int)min((int64_t)max(g.q_starts[b], 0), g.tokens);
-            n = (int)min((int64_t)max(g.q_starts[b + 1], q0), g.tokens) - q0;
+            const int64_t next = b < g.batch ? max(g.q_starts[b + 1], q0) : g.tokens;
+            n = (int)min(next, g.tokens) - q0;
         }
         const int tiles = (int)(((int64_t)n * g.group + R - 1) / R);
         int upto = tiles;

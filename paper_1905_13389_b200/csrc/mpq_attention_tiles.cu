@@ -132,7 +132,8 @@ attn_tiles_kernel(const AttnArgs g) {
     chain_entry();
     // ---- which rows, which part of the context (the same in every warp)
     AttnTile t;
-    const int tile_index = (int)gridDim.x - 1 - (int)blockIdx.x;         // later tiles see more: they go first
+    // later tiles see more: they go first -- but for the last one, which only tokens of no sequence can make use of
+    const int last_tile = (int)gridDim.x - 1, tile_index = (int)blockIdx.x == last_tile ? last_tile : last_tile - 1 - (int)blockIdx.x;
     const int kv_head = blockIdx.y;
     if (!find_tile<kTileRows>(g, tile_index, t)) return;
     tile_range<kTileRows, kStepTokens>(g, t);
