@@ -17,7 +17,8 @@
  *     mpq_linear_host / mpq_linear_host_prepared keep one helper stream and a few events per
  *     device; and per device the library remembers the multiprocessor count and which kernels
  *     have had their shared-memory limit raised (facts that never change while the process lives);
- *     the tensor-core kernels count waits that ran out (mpq_wait_failures).
+ *     the tensor-core kernels count waits that ran out (mpq_wait_failures), and the limit of a wait can be
+ *     set for the process (mpq_wait_limit).
  *   - Calls are asynchronous on `stream` (a cudaStream_t passed as void*; NULL = the
  *     default stream) unless stated otherwise.  Outputs are fully overwritten.
  *   - Return value: an mpq_status.  Errors that the host can see (null pointers, bad
@@ -406,10 +407,14 @@ int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
                         void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
                         void* workspace, int64_t workspace_bytes, void* stream);
 
-/* How many CTAs of the tensor-core kernels have given up a wait since the library was loaded on the
- * current device (0 unless the device or the driver misbehaves; the results of such a call are not
- * valid).  Synchronizes the stream. */
+/* How many CTAs of the tensor-core kernels (mpq_linear_levels, mpq_cache_attention) have given up a wait since
+ * the library was loaded on the current device: 0 unless the device or the driver misbehaves.  The results that
+ * such a CTA would have stored are NaN.  Synchronizes the stream. */
 int mpq_wait_failures(unsigned int* count_host, void* stream);
+/* How many polls of some 4 us those kernels, launched from here on by any thread of the process, make before they
+ * give up a wait.  Negative: the default, 2^20.  A limit of 0 or a few makes waits run out on a healthy device, which
+ * is how their end is tested. */
+void mpq_wait_limit(int polls);
 
 /* ---- Roofline denominator: measures this GPU's 32-bit population-count issue rate with a
  * register-only loop (no memory traffic) and the SM clock it ran at.  Synchronous.

@@ -100,6 +100,8 @@ def lib() -> ctypes.CDLL:
         L.mpq_cache_attention.argtypes = [P, i64, i64, i32, P, P, P, i64, i64, i32, i32, i32, i32, i64, i64, P, P, P, P,
                                           i32, i64, i32, i32, i64, f32, P, i64, i64, P, P, i64, P]
         L.mpq_wait_failures.argtypes = [ctypes.POINTER(ctypes.c_uint), P]
+        L.mpq_wait_limit.argtypes = [i32]
+        L.mpq_wait_limit.restype = None
         for name in ("mpq_wait_failures", "mpq_rmsnorm_levels", "mpq_encode_levels", "mpq_linear_levels", "mpq_cache_write", "mpq_cache_read",
                      "mpq_cache_attention"):
             getattr(L, name).restype = i32
@@ -687,8 +689,14 @@ def cache_attention(q: torch.Tensor, cache: LevelCache, q_starts: torch.Tensor, 
     return out
 
 
+def wait_limit(polls: int = -1) -> None:
+    """How many polls the tensor-core kernels launched from here on make before they give up a wait (-1: the default)."""
+    lib().mpq_wait_limit(polls)
+
+
 def wait_failures() -> int:
-    """CTAs of the tensor-core kernels that gave up a wait since the library was loaded (0 in a healthy process)."""
+    """CTAs of the tensor-core kernels that gave up a wait since the library was loaded (0 in a healthy process); what
+    they would have stored is NaN."""
     n = ctypes.c_uint()
     _check(lib().mpq_wait_failures(ctypes.byref(n), _stream()), "mpq_wait_failures")
     return n.value

@@ -686,7 +686,7 @@ extern "C" int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_
     if ((page_size & (page_size - 1)) == 0) for (page_shift = 0; (1 << page_shift) < page_size; ++page_shift) {}
     AttnArgs g = {q, q_token_stride, q_head_stride, q_starts, kv_lens, table, table_stride, tokens, batch, heads, kv_heads, heads / kv_heads,
                   k_levels, k_scale, v_levels, v_scale, pages, page_size, page_shift, causal != 0, window, scale * 1.4426950408889634f,
-                  out, out_token_stride, out_head_stride, lse, nullptr, nullptr, p.splits, p.split_tokens, p.joined};
+                  out, out_token_stride, out_head_stride, lse, nullptr, nullptr, p.splits, p.split_tokens, p.joined, wait_limit()};
     if (p.splits > 1 && !p.joined) {
         if (!workspace) return MPQ_ERR_NULL;
         if (!aligned16(workspace)) return MPQ_ERR_ALIGN;

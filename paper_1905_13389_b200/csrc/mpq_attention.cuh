@@ -40,6 +40,7 @@ struct AttnArgs {
     float* part_o; float2* part_ml;         // [tokens][heads][splits](dim), (m, l) of each split; used where a tile has more than one split
     int splits, split_tokens;               // launch grid's splits; context tokens of one split
     int joined;                             // the splits of a tile are one cluster, which joins them (no workspace)
+    uint32_t polls;                         // limit of a wait (the tensor-core form)
 };
 
 // One tile of query rows of one sequence: row r is token r / group, head kv_head * group + r % group.
@@ -163,7 +164,6 @@ __device__ __forceinline__ void row_power(float amax, float& down, float& up) {
 }
 // Factor of a query row's scores, finite: times a score of 0 it has to stay 0.
 __device__ __forceinline__ float row_factor(float up, float scale_log2) { return fminf(fmaxf(up * scale_log2, -3.402823466e38f), 3.402823466e38f); }
-constexpr float kNaN = __builtin_nanf("");
 
 constexpr int kJoined = 8;                                // splits that a cluster can hold
 __device__ __forceinline__ float ld_cluster(uint32_t addr) {

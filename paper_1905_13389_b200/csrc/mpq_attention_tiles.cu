@@ -260,9 +260,9 @@ attn_tiles_kernel(const AttnArgs g) {
 #pragma unroll 1
             for (int i = 0; i < 2 * steps; ++i) {         // half steps of 64 tokens
                 const int half = i & 1, st = (i >> 1) & 1, j0 = begin + i * 64;
-                ok = mbar_wait_or(s_full(h, half), (i >> 1) & 1, &failed);
+                ok = mbar_wait_or(s_full(h, half), (i >> 1) & 1, &failed, g.polls);
                 // the constants were written before the keys that S is made of
-                if (half == 0) ok = ok && mbar_wait_or(k_full(st), (i >> 2) & 1, &failed);
+                if (half == 0) ok = ok && mbar_wait_or(k_full(st), (i >> 2) & 1, &failed, g.polls);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tmem_fence_after();
                 const uint32_t from_s = ts + half * 64;
@@ -339,7 +339,7 @@ attn_tiles_kernel(const AttnArgs g) {
                         }
                     }
                     if (i > 0) {
-                        ok = mbar_wait_or(o_done(h), (i - 1) & 1, &failed);           // O is complete up to the half step before
+                        ok = mbar_wait_or(o_done(h), (i - 1) & 1, &failed, g.polls);           // O is complete up to the half step before
                         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                         tmem_fence_after();
 #pragma unroll 1
@@ -377,30 +377,32 @@ attn_tiles_kernel(const AttnArgs g) {
                 if ((lane & 3) == 0) scales[row0 + 8 * k] = make_float2(ref, ref == -INFINITY ? sum : sum + scales[row0 + 8 * k].y);
             }
             tile_sync();
-            ok = mbar_wait_or(o_full, 0, &failed);
+            ok = mbar_wait_or(o_full, 0, &failed, g.polls);
             ok = __all_sync(0xffffffffu, ok && !has_failed());
-            if (ok) {
+            {                                             // after a failure (!ok) the warp's part of the result is NaN
                 tmem_fence_after();
                 const int in_tile = quarter * 32 + lane;
                 bool live;
                 int token, head;
                 row_of_tile(in_tile, live, token, head);
-                const float set_row = scales[in_tile].x, l_row = scales[in_tile].y;
+                if (!ok && live) scales[in_tile] = make_float2(INFINITY, kNaN);           // what a cluster joins
+                const float set_row = ok ? scales[in_tile].x : INFINITY, l_row = ok ? scales[in_tile].y : kNaN;
                 const bool empty = set_row == -INFINITY;
                 constexpr float kInvL = 1.0f / (float)((1 << BITS) - 1);
                 const int64_t at = (int64_t)(t.q0 + token) * g.heads + head;
-                const float den = used > 1 ? kInvL : __fdiv_rn(kInvL, l_row);
+                const float den = used > 1 && ok ? kInvL : __fdiv_rn(kInvL, l_row);
                 T* out = static_cast<T*>(g.out) + (int64_t)(t.q0 + token) * g.o_ts + (int64_t)head * g.o_hs;
                 const int64_t slot = at * g.splits + blockIdx.z;
                 const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
 #pragma unroll 1
                 for (int c = sixteen * (D / 32); c < (sixteen + 1) * (D / 32); ++c) {        // 16 dims at a time
-                    uint32_t o[16];
-                    if (steps > 0) { tmem_load16(lanes + kTmemO + h * 128 + c * 16, o); tmem_wait_ld(); }
+                    uint32_t o[16] = {};
+                    if (ok && steps > 0) { tmem_load16(lanes + kTmemO + h * 128 + c * 16, o); tmem_wait_ld(); }
                     if (!live) continue;
                     float f[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) f[e] = empty ? 0.0f : __uint_as_float(o[e]) * den;
+                    if (used > 1 && g.joined && !ok) continue;           // (products may still read what lies there)
                     if (used > 1 && g.joined) {                          // for the cluster, where the keys and values were
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -491,7 +493,7 @@ attn_tiles_kernel(const AttnArgs g) {
             const int st = i & 1;
             const uint32_t row2 = find_row(i + 2);
             bool ok = true;
-            if (i >= 2) ok = mbar_wait_or(k_empty(st), ((i >> 1) - 1) & 1, &failed) && mbar_wait_or(c_empty(st), ((i >> 1) - 1) & 1, &failed);
+            if (i >= 2) ok = mbar_wait_or(k_empty(st), ((i >> 1) - 1) & 1, &failed, g.polls) && mbar_wait_or(c_empty(st), ((i >> 1) - 1) & 1, &failed, g.polls);
             ok = __all_sync(0xffffffffu, ok && !has_failed());
             if (ok) {                                                    // after a failure only the barriers are kept up
                 float* consts = reinterpret_cast<float*>(base_ptr + Smem::consts + st * Smem::const_stage);
@@ -528,7 +530,7 @@ attn_tiles_kernel(const AttnArgs g) {
                 if (lane == 0) mbar_arrive(k_full(st));
                 load_keys(i + 1);
             }
-            if (i >= 2) ok = mbar_wait_or(v_empty(st), ((i >> 1) - 1) & 1, &failed);
+            if (i >= 2) ok = mbar_wait_or(v_empty(st), ((i >> 1) - 1) & 1, &failed, g.polls);
             ok = __all_sync(0xffffffffu, ok && !has_failed());
             if (ok) {
                 const uint32_t tile = base + Smem::v + st * Smem::v_stage + (group8 >> 3) * (D * 128);
@@ -564,7 +566,7 @@ attn_tiles_kernel(const AttnArgs g) {
             constexpr uint32_t idesc_s = umma_idesc_f16(128, 64), idesc_o = umma_idesc_f16(128, D);
             const uint32_t acc = __shfl_sync(0xffffffffu, tmem, 0);
             const bool leader = elect_one();
-            bool ok = mbar_wait_warp(q_ready, 0, &failed);
+            bool ok = mbar_wait_warp(q_ready, 0, &failed, g.polls);
             // scores of half step i (64 tokens) of tile h; the keys of a step lie in one stage
             auto scores = [&](int h, int i) {
                 const int half = i & 1, st = (i >> 1) & 1;
@@ -582,7 +584,7 @@ attn_tiles_kernel(const AttnArgs g) {
             };
             const int halves = 2 * steps;
             if (ok && steps > 0) {
-                ok = mbar_wait_warp(k_full(0), 0, &failed);
+                ok = mbar_wait_warp(k_full(0), 0, &failed, g.polls);
                 tmem_fence_after();
                 if (ok) {
                     for (int half = 0; half < 2; ++half)
@@ -594,12 +596,12 @@ attn_tiles_kernel(const AttnArgs g) {
             for (int i = 0; i < halves && ok; ++i) {
                 const int half = i & 1, st = (i >> 1) & 1;
                 if (half == 0) {
-                    ok = mbar_wait_warp(v_full(st), (i >> 2) & 1, &failed);
-                    if (ok && i + 2 < halves) ok = mbar_wait_warp(k_full(st ^ 1), ((i + 2) >> 2) & 1, &failed);
+                    ok = mbar_wait_warp(v_full(st), (i >> 2) & 1, &failed, g.polls);
+                    if (ok && i + 2 < halves) ok = mbar_wait_warp(k_full(st ^ 1), ((i + 2) >> 2) & 1, &failed, g.polls);
                 }
 #pragma unroll 1
                 for (int h = 0; h < tiles && ok; ++h) {
-                    ok = mbar_wait_warp(p_ready(h, half), (i >> 1) & 1, &failed);
+                    ok = mbar_wait_warp(p_ready(h, half), (i >> 1) & 1, &failed, g.polls);
                     if (!ok) break;
                     tmem_fence_after();
                     const uint32_t d = acc + kTmemO + h * 128, w = acc + kTmemS + h * 128 + half * 64;
@@ -617,7 +619,7 @@ attn_tiles_kernel(const AttnArgs g) {
                 }
             }
             if (leader) umma_commit<1>(o_full);
-            mbar_wait_warp(o_full, 0, &failed);
+            mbar_wait(o_full, 0);                                        // also after a failure: TMEM is freed next
         }
     }
     __syncwarp();

@@ -114,6 +114,7 @@ __device__ __forceinline__ float finite_sum(const float (&x)[N]) {
     return z;
 }
 __device__ __forceinline__ bool ordinary(float v) { return fabsf(v) < __int_as_float(0x7f800000); }             // neither NaN nor infinite
+constexpr float kNaN = __builtin_nanf("");
 // max(a, b), NaN where either is one (fmaxf would give the other).
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;

@@ -7,6 +7,7 @@
 #include "mpq_attention.cuh"
 #include "mpq_tensor.cuh"
 
+#include <atomic>
 #include <type_traits>
 
 namespace mpq {
@@ -20,6 +21,7 @@ struct LinearArgs {
     int glue;
     const void* res; int64_t ldr;
     void* out; int64_t ldo;
+    uint32_t polls;                                       // limit of a wait
 };
 
 // acc (levels u, unsigned) -> one output, in the header's order of operations
@@ -110,7 +112,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * kStages + 1];
     __shared__ uint32_t tmem_holder;
-    __shared__ int failed;
+    __shared__ int failed, peer_failed;                   // a wait of this CTA, or a store of its cluster, gave up
     __shared__ float row_scale[BN];
     __shared__ uint32_t row_terms[BN];
     const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -124,7 +126,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2 * kStages + 1; ++i) mbar_init(smem_addr(&bars[i]), 1);
-        failed = 0;
+        failed = peer_failed = 0;
         mbar_init_fence();
         tma_prefetch(&map_w);
         tma_prefetch(&map_a);
@@ -148,7 +150,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         int i = 0;
         for (int kb = kb0; kb < kb1; ++kb, ++i) {
             const int s = i % kStages;
-            if (i >= kStages && !mbar_wait_warp(empty(s), (i / kStages - 1) & 1, &failed)) break;
+            if (i >= kStages && !mbar_wait_warp(empty(s), (i / kStages - 1) & 1, &failed, g.polls)) break;
             if (leader) {
                 const uint32_t dst = ring + s * Shape::stage_bytes;
                 mbar_expect_tx(full(s), Shape::stage_bytes);
@@ -156,8 +158,8 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                 tma_load_2d(dst + 128 * kBlock, &map_a, kb * kBlock, m0, full(s));
             }
         }
-        if (has_failed())
-            for (int q = i > kStages ? i - kStages : 0; q < i; ++q) mbar_wait(full(q % kStages), (q / kStages) & 1);
+        // Every copy has landed before the CTA ends, also where the products have given up on them.
+        for (int q = i > kStages ? i - kStages : 0; q < i; ++q) mbar_wait(full(q % kStages), (q / kStages) & 1);
     } else if (warp == 1) {
         constexpr uint32_t idesc = umma_idesc_u8(128, BN);
         const bool leader = elect_one();
@@ -165,7 +167,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         int i = 0;
         for (int kb = kb0; kb < kb1; ++kb, ++i) {
             const int s = i % kStages;
-            if (!mbar_wait_warp(full(s), (i / kStages) & 1, &failed)) break;
+            if (!mbar_wait_warp(full(s), (i / kStages) & 1, &failed, g.polls)) break;
             tmem_fence_after();
             const uint32_t at = ring + s * Shape::stage_bytes;
             if (leader) {
@@ -191,10 +193,16 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         const int64_t c = (int64_t)n0 + col;
         ColTerm ct = {0.0f, 0u, 0.0f};
         if (c < g.n) ct = col_term(g, c);
-        const bool ok = mbar_wait_warp(done, 0, &failed) && !__any_sync(0xffffffffu, has_failed());
+        bool ok = mbar_wait_warp(done, 0, &failed, g.polls);
+        if (!ok) mbar_wait(done, 0);                      // what has been issued must end before TMEM is freed
+        ok = ok && !__any_sync(0xffffffffu, has_failed());
+        if (!ok) {                                        // results are NaN from here on, in all CTAs of the tile
+            ct.scale = kNaN;
+            if (splits > 1 && lane < splits) st_cluster(map_to_cta(smem_addr(&peer_failed), (uint32_t)lane), 1u);
+        }
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
         const int own = BN / splits;
-        if (ok) {
+        {
             tmem_fence_after();
 #pragma unroll 1
             for (int r0 = 0; r0 < BN; r0 += 16) {
@@ -221,11 +229,12 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     __syncwarp();
     if (splits > 1) {
         cluster_sync_all();                                // every CTA's partial sums have arrived
-        if (warp >= 2 && !has_failed()) {
+        if (warp >= 2) {
             const int col = (warp & 3) * 32 + lane, own = BN / splits;
             const int64_t c = (int64_t)n0 + col;
             if (c < g.n) {
-                const ColTerm ct = col_term(g, c);
+                ColTerm ct = col_term(g, c);
+                if (*(volatile int*)&peer_failed) ct.scale = kNaN;
                 auto finish = [&](auto count, int j0) {    // `count` rows of this CTA's share at once
                     constexpr int N = decltype(count)::value;
                     const int rr = split * own + j0;
@@ -280,9 +289,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     using Shape = PairShape;
     constexpr int BN = kPairCols, kStages = Shape::stages, kAccs = 2;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kAccs];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kAccs + 1];
     __shared__ uint32_t tmem_holder;
-    __shared__ int failed;
+    __shared__ int failed, peer_failed;                    // a wait of this CTA, or of the other one, gave up
     const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
     uint32_t* transpose = reinterpret_cast<uint32_t*>(smem_raw + (ring - smem_addr(smem_raw)) + kStages * Shape::stage_bytes);
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -291,12 +300,14 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     auto empty = [&](int s) { return smem_addr(&bars[kStages + s]); };             // one in each CTA
     auto acc_full = [&](int a) { return smem_addr(&bars[2 * kStages + a]); };      // one in each CTA
     auto acc_empty = [&](int a) { return smem_addr(&bars[2 * kStages + kAccs + a]); };   // leader: the storing warps of both
+    const uint32_t drained = smem_addr(&bars[2 * kStages + 2 * kAccs]);            // one in each CTA; used after a failure
     auto has_failed = [&]() { return *(volatile int*)&failed != 0; };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2 * kStages + kAccs; ++i) mbar_init(smem_addr(&bars[i]), 1);
         for (int a = 0; a < kAccs; ++a) mbar_init(acc_empty(a), 2 * kPairStoreWarps);
-        failed = 0;
+        mbar_init(drained, 1);
+        failed = peer_failed = 0;
         mbar_init_fence();
         tma_prefetch(&map_a);
         tma_prefetch(&map_w);
@@ -327,7 +338,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             origin(i, m0, n0);
             for (int kb = 0; kb < blocks; ++kb, ++issued) {
                 const int s = issued % kStages;
-                if (issued >= kStages && !mbar_wait_warp(empty(s), (issued / kStages - 1) & 1, &failed)) { ok = false; break; }
+                if (issued >= kStages && !mbar_wait_warp(empty(s), (issued / kStages - 1) & 1, &failed, g.polls)) { ok = false; break; }
                 if (leader) {
                     const uint32_t dst = ring + s * Shape::stage_bytes, bar = map_to_cta(full(s), 0);
                     if (rank == 0) mbar_expect_tx(full(s), 2 * Shape::stage_bytes);
@@ -336,8 +347,6 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 }
             }
         }
-        // after a failure copies may still be on their way into this CTA; their barrier may be the other CTA's
-        if (has_failed()) for (int q = 0; q < 100; ++q) __nanosleep(100000);
     } else if (warp == 1) {
         if (rank == 0) {
             constexpr uint32_t idesc = umma_idesc_u8(256, BN);
@@ -347,12 +356,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             bool ok = true;
             for (int i = 0; i < my_tiles && ok; ++i) {
                 const int acc = i & 1;
-                if (i >= kAccs && !mbar_wait_warp(acc_empty(acc), ((i >> 1) - 1) & 1, &failed)) break;
+                if (i >= kAccs && !mbar_wait_warp(acc_empty(acc), ((i >> 1) - 1) & 1, &failed, g.polls)) break;
                 tmem_fence_after();
                 const uint32_t d = acc_base + (uint32_t)(acc * BN);
                 for (int kb = 0; kb < blocks; ++kb, ++consumed) {
                     const int s = consumed % kStages;
-                    if (!mbar_wait_warp(full(s), (consumed / kStages) & 1, &failed)) { ok = false; break; }
+                    if (!mbar_wait_warp(full(s), (consumed / kStages) & 1, &failed, g.polls)) { ok = false; break; }
                     tmem_fence_after();
                     const uint32_t at = ring + s * Shape::stage_bytes;
                     if (leader) {
@@ -362,7 +371,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         umma_commit<2>(empty(s));
                     }
                 }
-                if (leader) umma_commit<2>(acc_full(acc));
+                if (leader && ok) umma_commit<2>(acc_full(acc));        // a sum that is not complete is never handed over
             }
         }
     } else if (warp >= 2) {
@@ -388,7 +397,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             const int rows = (int)min((int64_t)32, g.m - row0);                    // 0 or less: none of them exists
             RowTerm mine = {0.0f, 0u};                                             // lane's row; handed round by shuffles
             if (lane < rows) mine = row_term(g, row0 + lane);
-            ok = ok && mbar_wait_warp(acc_full(acc), (i >> 1) & 1, &failed) && !__any_sync(0xffffffffu, has_failed());
+            ok = ok && mbar_wait_warp(acc_full(acc), (i >> 1) & 1, &failed, g.polls) && !__any_sync(0xffffffffu, has_failed());
             const int64_t cx = (int64_t)n0 + c0 + ca, cy = (int64_t)n0 + c0 + cb;
             const bool in_x = cx < g.n, in_y = cy < g.n;
             ColTerm ct[2] = {{0.0f, 0u, 0.0f}, {0.0f, 0u, 0.0f}};
@@ -407,8 +416,10 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 for (int j = 0; j < 32; j += 2)
                     *reinterpret_cast<uint2*>(sh + lane * Shape::row_words + 2 * ((part * 16 + j / 2) ^ lane)) = make_uint2(v[j], v[j + 1]);
             }
-            block_sync();                                                              // after a failure only the barriers are kept up
-            if (ok) {
+            block_sync();
+            // (the other warp of the block may have given up: half of the columns are missing then)
+            if (!ok || __any_sync(0xffffffffu, has_failed())) ct[0].scale = ct[1].scale = kNaN;
+            {
                 // kRowsAtOnce rows at a time.  All residuals of a group are requested before any is used or any result is
                 // written: they may lie in the result's own tensor, so the compiler could not move a load up by itself, and
                 // one load after the other took 45 us of a tile's 51.  (All 32 rows at once spill: 61 -> 78 us at 4096^3.)
@@ -466,9 +477,23 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         }
     }
     __syncwarp();
+    if (has_failed() && lane == 0) st_cluster(map_to_cta(smem_addr(&peer_failed), rank ^ 1u), 1u);
     tmem_fence_before();
     cluster_sync_all();
     tmem_fence_after();
+    if (has_failed() || *(volatile int*)&peer_failed) {
+        // The same in both CTAs, none of which issues anything any more: the products under way end, and the copies that
+        // nobody waited for have 10 ms to land before either CTA gives its memory back.
+        if (warp == 1) {
+            if (rank == 0 && elect_one()) umma_commit<2>(drained);
+            __syncwarp();
+            mbar_wait(drained, 0);
+            for (int q = 0; q < 100; ++q) __nanosleep(100000);
+        }
+        __syncwarp();
+        cluster_sync_all();
+        tmem_fence_after();
+    }
     if (warp == 0) tmem_free<2>(tmem, kAccs * BN);
     if (threadIdx.x == 0 && failed) atomicAdd(&g_wait_failures, 1u);
 }
@@ -561,11 +586,19 @@ extern "C" int mpq_linear_levels(const uint8_t* a, const float* a_scale, const i
     if (!aligned16(a) || !aligned16(w) || !aligned_to(a_scale, 4) || !aligned_to(a_sums, 4) || !aligned_to(w_scale, 4) || !aligned_to(w_sums, 4) ||
         !aligned_to(bias, 4) || !aligned_to(residual, e) || !aligned_to(out, e)) return MPQ_ERR_ALIGN;
     if (m == 0) return MPQ_OK;
-    const LinearArgs g = {a, a_scale, a_sums, w, w_scale, w_sums, m, n, k, level_row_bytes(k), (int)La, (int)Lw, bias, glue, residual, ldr, out, ldo};
+    const LinearArgs g = {a, a_scale, a_sums, w, w_scale, w_sums, m, n, k, level_row_bytes(k), (int)La, (int)Lw, bias, glue, residual, ldr, out, ldo,
+                          wait_limit()};
     if (dtype == MPQ_F32) return launch_linear_levels<float>(g, (cudaStream_t)stream);
     if (dtype == MPQ_F16) return launch_linear_levels<__half>(g, (cudaStream_t)stream);
     return launch_linear_levels<__nv_bfloat16>(g, (cudaStream_t)stream);
 }
+
+namespace {
+std::atomic<uint32_t> g_wait_limit{kSpinLimit};
+}
+uint32_t mpq::wait_limit() { return g_wait_limit.load(std::memory_order_relaxed); }
+
+extern "C" void mpq_wait_limit(int polls) { g_wait_limit.store(polls < 0 ? kSpinLimit : (uint32_t)polls, std::memory_order_relaxed); }
 
 extern "C" int mpq_wait_failures(unsigned int* count_host, void* stream) {
     if (!count_host) return MPQ_ERR_NULL;

@@ -1,7 +1,8 @@
 // Thin wrappers of the sm_100a instructions that the tensor-core kernels issue: mbarriers, tiled TMA loads
 // (no multicast; the tensor maps cover this GPU's own memory), tcgen05 products and TMEM.  Every wait is
-// bounded: it gives up after kSpinLimit polls, the kernel then counts the event in g_wait_failures, stops
-// issuing work, lets its copies in flight land and returns.
+// bounded: it gives up after a number of polls that the host passes (mpq_wait_limit).  The kernel then stops issuing
+// work, stores NaN where its results would have been, waits -- with the default limit, so that a short one can be
+// tested -- for what it has under way (mbar_wait), counts the event and returns.
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -9,6 +10,8 @@
 
 namespace mpq {
 
+// Polls that each last 4 us at most: 4 s.  The longest wait is that for a whole tile of a product, a third of a microsecond
+// per 128 bytes of k: 1 s for a single row of 2^31 elements in four parts, less for any other operands that memory holds.
 constexpr uint32_t kSpinLimit = 1u << 20;
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -27,6 +30,15 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// Asks once; mbar_poll waits up to 4 us (measured; a suspend-time hint changes nothing).
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\t"
+                 "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+                 "selp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
 __device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile("{\n\t.reg .pred p;\n\t"
@@ -35,32 +47,37 @@ __device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity) {
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-// Waits for the phase with the given parity; false when the limit ran out.
+// Waits for the phase with the given parity, whatever has failed before; false when the default limit ran out.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     for (uint32_t spin = 0; spin < kSpinLimit; ++spin)
         if (mbar_poll(bar, parity)) return true;
     return false;
 }
 
-// ... and gives up early once *failed is set; sets it when the limit runs out.
-__device__ __forceinline__ bool mbar_wait_or(uint32_t bar, uint32_t parity, int* failed) {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+// ... one question and at most `limit` polls, fewer once *failed is set; sets it when the limit runs out (and before anything that the
+// thread signals afterwards).
+__device__ __forceinline__ bool mbar_wait_or(uint32_t bar, uint32_t parity, int* failed, uint32_t limit) {
+    if (mbar_test(bar, parity)) return true;
+    for (uint32_t spin = 0; spin < limit; ++spin) {
         if (mbar_poll(bar, parity)) return true;
         if ((spin & 255u) == 255u && *(volatile int*)failed) return false;
     }
     atomicExch(failed, 1);
+    __threadfence_block();
     return false;
 }
 
 // The same by a whole warp, with one answer for all lanes.  The warps that issue tensor-core work run their loops
 // with all lanes and elect one around the instructions: their operands then stay in uniform registers (a loop run
 // by a single lane moved each operand of each product there, some 150 cycles a product).
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, int* failed) {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, int* failed, uint32_t limit) {
+    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
+    for (uint32_t spin = 0; spin < limit; ++spin) {
         if (__all_sync(0xffffffffu, mbar_poll(bar, parity))) return true;
         if ((spin & 255u) == 255u && __any_sync(0xffffffffu, *(volatile int*)failed)) return false;
     }
     atomicExch(failed, 1);
+    __threadfence_block();
     return false;
 }
 __device__ __forceinline__ bool elect_one() {
@@ -216,6 +233,9 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint32_t b, 
 }
 // Generic-proxy writes to shared memory -> visible to the tensor cores' reads that follow.
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// ---- host: the limit of a wait in polls
+uint32_t wait_limit();
 
 // ---- host: tensor maps
 typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
