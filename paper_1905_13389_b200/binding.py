@@ -518,6 +518,13 @@ def _vector(t: torch.Tensor, n: int, dtype) -> int:
     return t.data_ptr()
 
 
+def _workspace(t: torch.Tensor):
+    """(pointer, bytes) of a workspace: any contiguous tensor on a CUDA device."""
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous workspace on a CUDA device, got strides %s on %s" % (tuple(t.stride()), t.device))
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 _NO_ROWS, _NO_VALUES = (None, 0), (None, 0, 0)
 
 
@@ -677,7 +684,7 @@ def cache_attention(q: torch.Tensor, cache: LevelCache, q_starts: torch.Tensor, 
         need = L.mpq_cache_attention_workspace(tokens, batch, heads, kv_heads, dim, max_q, max_kv)
         if need:
             workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=q.device)
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    ws, ws_bytes = (None, 0) if workspace is None else _workspace(workspace)
     st = L.mpq_cache_attention(
         *_heads(q, tokens, heads, dim, dtype), _dtype(dtype), _vector(q_starts, batch + 1, torch.int32),
         _vector(kv_lens, batch, torch.int32), _vector(table, batch * per, torch.int32), per,
