@@ -23,7 +23,9 @@ ACT_HTANH, ACT_HRELU = 0, 1
 ENC_LEVELS, ENC_TRIG = 0, 1
 
 _lib = None
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# A torch without CUDA lacks these two; the public functions, which say so, stand in, and what needs no device still works.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 class MpqError(RuntimeError):
