@@ -493,9 +493,19 @@ def _expected(t, shape, dtype):
         tuple(shape), "" if dtype is None else " and dtype %s" % dtype, t.dtype, tuple(t.shape), tuple(t.stride()), t.device))
 
 
-def _rows(t: torch.Tensor, rows: int, k: int, dtype):
+def _device(t: torch.Tensor) -> int:
+    """Number of the device that a call runs on: that of its first tensor, which has to be the current one."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("expected a CUDA tensor, got one on %s" % t.device)
+    if dev != _current_device():
+        raise ValueError("the call's tensors are on cuda:%d, the current device is cuda:%d" % (dev, _current_device()))
+    return dev
+
+
+def _rows(t: torch.Tensor, rows: int, k: int, dtype, dev: int):
     """(pointer, row stride) of a [rows x k] matrix whose rows are contiguous."""
-    if t.shape != (rows, k) or t.dtype is not dtype or not t.is_cuda:
+    if t.shape != (rows, k) or t.dtype is not dtype or t.get_device() != dev:
         _expected(t, (rows, k), dtype)
     stride, step = t.stride()
     if step != 1 and k > 1:
@@ -503,9 +513,9 @@ def _rows(t: torch.Tensor, rows: int, k: int, dtype):
     return t.data_ptr(), stride if rows > 1 else k
 
 
-def _heads(t: torch.Tensor, tokens: int, heads: int, dim: int, dtype):
+def _heads(t: torch.Tensor, tokens: int, heads: int, dim: int, dtype, dev: int):
     """(pointer, token stride, head stride) of a [tokens][heads][dim] tensor whose head rows are contiguous."""
-    if t.shape != (tokens, heads, dim) or t.dtype is not dtype or not t.is_cuda:
+    if t.shape != (tokens, heads, dim) or t.dtype is not dtype or t.get_device() != dev:
         _expected(t, (tokens, heads, dim), dtype)
     st, sh, step = t.stride()
     if step != 1:
@@ -513,31 +523,31 @@ def _heads(t: torch.Tensor, tokens: int, heads: int, dim: int, dtype):
     return t.data_ptr(), st if tokens > 1 else heads * dim, sh if heads > 1 else dim
 
 
-def _vector(t: torch.Tensor, n: int, dtype) -> int:
+def _vector(t: torch.Tensor, n: int, dtype, dev: int) -> int:
     """Pointer of n contiguous values."""
-    if t.numel() != n or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected %d contiguous %s values on a CUDA device, got %d of %s on %s" % (n, dtype, t.numel(), t.dtype, t.device))
+    if t.numel() != n or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("expected %d contiguous %s values on cuda:%d, got %d of %s on %s" % (n, dtype, dev, t.numel(), t.dtype, t.device))
     return t.data_ptr()
 
 
-def _workspace(t: torch.Tensor):
-    """(pointer, bytes) of a workspace: any contiguous tensor on a CUDA device."""
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected a contiguous workspace on a CUDA device, got strides %s on %s" % (tuple(t.stride()), t.device))
+def _workspace(t: torch.Tensor, dev: int = 0):
+    """(pointer, bytes) of a workspace: any contiguous tensor on the call's device."""
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("expected a contiguous workspace on a CUDA device (that of the call), got strides %s on %s" % (tuple(t.stride()), t.device))
     return t.data_ptr(), t.numel() * t.element_size()
 
 
 _NO_ROWS, _NO_VALUES = (None, 0), (None, 0, 0)
 
 
-def _held(lv: Levels, rows: int, k: int):
+def _held(lv: Levels, rows: int, k: int, dev: int):
     """Pointers of level bytes, ranges and sums, after comparing their sizes."""
     held, scale, sums, _, lk = lv
     row = (k + 15) // 16 * 16
     if lk != k or held.shape != (rows, row):
         raise ValueError("expected levels of %d rows of %d elements (%d bytes apart), got k = %d and bytes %s" % (
             rows, k, row, lk, tuple(held.shape)))
-    return _vector(held, rows * row, torch.uint8), _vector(scale, rows, torch.float32), _vector(sums, rows, torch.int32)
+    return _vector(held, rows * row, torch.uint8, dev), _vector(scale, rows, torch.float32, dev), _vector(sums, rows, torch.int32, dev)
 
 
 def _new_levels(rows: int, k: int, bits: int, device):
@@ -549,17 +559,17 @@ def _new_levels(rows: int, k: int, bits: int, device):
     return Levels(held, scale, sums, bits, k), (held.data_ptr(), scale.data_ptr(), sums.data_ptr())
 
 
-def _level_outputs(out: Optional[Levels], rows: int, k: int, bits: int, device):
+def _level_outputs(out: Optional[Levels], rows: int, k: int, bits: int, device, dev: int):
     if out is None:
         return _new_levels(rows, k, bits, device)
     if out.bits != bits:
         raise ValueError("the output levels are of another width")
-    return out, _held(out, rows, k)
+    return out, _held(out, rows, k, dev)
 
 
-def _values(values: torch.Tensor, rows: int, k: int):
+def _values(values: torch.Tensor, rows: int, k: int, dev: int):
     """(pointer, dtype, row stride) of the decoded output."""
-    p, stride = _rows(values, rows, k, values.dtype)
+    p, stride = _rows(values, rows, k, values.dtype, dev)
     return p, _dtype(values.dtype), stride
 
 
@@ -570,13 +580,14 @@ def rmsnorm_levels(x: torch.Tensor, gain: Optional[torch.Tensor], eps: float, bi
     x + residual (it may be x or residual), values the numbers that the levels stand for."""
     rows, k = x.shape
     dtype = x.dtype
-    px = _rows(x, rows, k, dtype)
-    out, po = _level_outputs(out, rows, k, bits, x.device)
+    dev = _device(x)
+    px = _rows(x, rows, k, dtype, dev)
+    out, po = _level_outputs(out, rows, k, bits, x.device, dev)
     st = (_lib or lib()).mpq_rmsnorm_levels(
-        *px, *(_NO_ROWS if residual is None else _rows(residual, rows, k, dtype)), _dtype(dtype),
-        None if gain is None else _vector(gain, k, torch.float32), eps, rows, k, bits,
-        *(_NO_ROWS if residual_out is None else _rows(residual_out, rows, k, dtype)), *po,
-        *(_NO_VALUES if values is None else _values(values, rows, k)), _raw_stream(_current_device()))
+        *px, *(_NO_ROWS if residual is None else _rows(residual, rows, k, dtype, dev)), _dtype(dtype),
+        None if gain is None else _vector(gain, k, torch.float32, dev), eps, rows, k, bits,
+        *(_NO_ROWS if residual_out is None else _rows(residual_out, rows, k, dtype, dev)), *po,
+        *(_NO_VALUES if values is None else _values(values, rows, k, dev)), _raw_stream(dev))
     if st:
         raise MpqError(st, "mpq_rmsnorm_levels")
     return out
@@ -586,10 +597,11 @@ def encode_levels(x: torch.Tensor, bits: int = 8, act: int = ACT_HTANH, values: 
                   out: Optional[Levels] = None) -> Levels:
     """[rows x k] -> level bytes with one range per row (weights, once; activations inside a block)."""
     rows, k = x.shape
-    px = _rows(x, rows, k, x.dtype)
-    out, po = _level_outputs(out, rows, k, bits, x.device)
+    dev = _device(x)
+    px = _rows(x, rows, k, x.dtype, dev)
+    out, po = _level_outputs(out, rows, k, bits, x.device, dev)
     st = (_lib or lib()).mpq_encode_levels(*px, _dtype(x.dtype), rows, k, act, bits, *po,
-                                           *(_NO_VALUES if values is None else _values(values, rows, k)), _raw_stream(_current_device()))
+                                           *(_NO_VALUES if values is None else _values(values, rows, k, dev)), _raw_stream(dev))
     if st:
         raise MpqError(st, "mpq_encode_levels")
     return out
@@ -602,15 +614,16 @@ def linear_levels(a: Levels, w: Levels, bias: Optional[torch.Tensor] = None, act
     m, n, k = a.bytes.shape[0], w.bytes.shape[0], a.k
     if act not in GLUE:
         raise ValueError("unknown activation %r: expected one of %s" % (act, ", ".join(GLUE)))
-    pa, pw = _held(a, m, k), _held(w, n, k)
+    dev = _device(a.bytes)
+    pa, pw = _held(a, m, k, dev), _held(w, n, k, dev)
     if out is None:
         out = torch.empty_strided((m, n), (n, 1), dtype=dtype, device=a.bytes.device)
     else:
         dtype = out.dtype
-    po, ldo = _rows(out, m, n, dtype)
+    po, ldo = _rows(out, m, n, dtype, dev)
     st = (_lib or lib()).mpq_linear_levels(
-        *pa, a.bits, *pw, w.bits, m, n, k, None if bias is None else _vector(bias, n, torch.float32), GLUE[act],
-        *(_NO_ROWS if residual is None else _rows(residual, m, n, dtype)), po, _dtype(dtype), ldo, _raw_stream(_current_device()))
+        *pa, a.bits, *pw, w.bits, m, n, k, None if bias is None else _vector(bias, n, torch.float32, dev), GLUE[act],
+        *(_NO_ROWS if residual is None else _rows(residual, m, n, dtype, dev)), po, _dtype(dtype), ldo, _raw_stream(dev))
     if st:
         raise MpqError(st, "mpq_linear_levels")
     return out
@@ -623,22 +636,24 @@ def level_cache(pages: int, heads: int, page_size: int, dim: int, bits: int, dev
     return LevelCache(rows[0], ranges[0], rows[1], ranges[1], bits)
 
 
-def _cache(c: LevelCache):
+def _cache(c: LevelCache, dev: int):
     """(pages, heads, page size, dim) and the four pointers of a cache."""
     k, k_scale, v, v_scale, bits = c
     pages, heads, page_size, row = k.shape
     n = pages * heads * page_size
     return (pages, heads, page_size, row * 8 // bits if bits else 0), (
-        _vector(k, n * row, torch.uint8), _vector(k_scale, n, torch.float32), _vector(v, n * row, torch.uint8), _vector(v_scale, n, torch.float32))
+        _vector(k, n * row, torch.uint8, dev), _vector(k_scale, n, torch.float32, dev),
+        _vector(v, n * row, torch.uint8, dev), _vector(v_scale, n, torch.float32, dev))
 
 
 def cache_write(cache: LevelCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> LevelCache:
     """Quantizes keys and values [tokens][heads][dim] into the cache at ``slots`` (int64; -1: not written)."""
-    (pages, heads, page_size, dim), held = _cache(cache)
+    dev = _device(cache.k)
+    (pages, heads, page_size, dim), held = _cache(cache, dev)
     tokens, dtype = k.shape[0], k.dtype
     st = (_lib or lib()).mpq_cache_write(
-        *_heads(k, tokens, heads, dim, dtype), *_heads(v, tokens, heads, dim, dtype), _dtype(dtype), _vector(slots, tokens, torch.int64),
-        tokens, heads, dim, cache.bits, *held, pages, page_size, _raw_stream(_current_device()))
+        *_heads(k, tokens, heads, dim, dtype, dev), *_heads(v, tokens, heads, dim, dtype, dev), _dtype(dtype), _vector(slots, tokens, torch.int64, dev),
+        tokens, heads, dim, cache.bits, *held, pages, page_size, _raw_stream(dev))
     if st:
         raise MpqError(st, "mpq_cache_write")
     return cache
@@ -651,15 +666,16 @@ def _new_heads(tokens: int, heads: int, dim: int, dtype, device) -> torch.Tensor
 def cache_read(cache: LevelCache, slots: torch.Tensor, dtype: torch.dtype, k: Optional[torch.Tensor] = None,
                v: Optional[torch.Tensor] = None):
     """The keys and values at ``slots`` as [tokens][heads][dim] of ``dtype`` (zeros for a slot of -1)."""
-    (pages, heads, page_size, dim), held = _cache(cache)
+    dev = _device(cache.k)
+    (pages, heads, page_size, dim), held = _cache(cache, dev)
     tokens = slots.numel()
     if k is None:
         k = _new_heads(tokens, heads, dim, dtype, slots.device)
     if v is None:
         v = _new_heads(tokens, heads, dim, dtype, slots.device)
     st = (_lib or lib()).mpq_cache_read(
-        *held, pages, page_size, _vector(slots, tokens, torch.int64), tokens, heads, dim, cache.bits,
-        *_heads(k, tokens, heads, dim, dtype), *_heads(v, tokens, heads, dim, dtype), _dtype(dtype), _raw_stream(_current_device()))
+        *held, pages, page_size, _vector(slots, tokens, torch.int64, dev), tokens, heads, dim, cache.bits,
+        *_heads(k, tokens, heads, dim, dtype, dev), *_heads(v, tokens, heads, dim, dtype, dev), _dtype(dtype), _raw_stream(dev))
     if st:
         raise MpqError(st, "mpq_cache_read")
     return k, v
@@ -675,7 +691,8 @@ def cache_attention(q: torch.Tensor, cache: LevelCache, q_starts: torch.Tensor, 
                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the new tokens q [tokens][heads][dim] of ``batch`` sequences (token ranges q_starts [batch + 1]) over
     their contexts of kv_lens [batch] tokens in the pages table [batch][..] names.  scale defaults to dim ** -0.5."""
-    (pages, kv_heads, page_size, dim), held = _cache(cache)
+    dev = _device(cache.k)
+    (pages, kv_heads, page_size, dim), held = _cache(cache, dev)
     tokens, heads, _ = q.shape
     batch, dtype = kv_lens.numel(), q.dtype
     per = table.shape[-1]
@@ -686,13 +703,13 @@ def cache_attention(q: torch.Tensor, cache: LevelCache, q_starts: torch.Tensor, 
         need = L.mpq_cache_attention_workspace(tokens, batch, heads, kv_heads, dim, max_q, max_kv)
         if need:
             workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=q.device)
-    ws, ws_bytes = (None, 0) if workspace is None else _workspace(workspace)
+    ws, ws_bytes = (None, 0) if workspace is None else _workspace(workspace, dev)
     st = L.mpq_cache_attention(
-        *_heads(q, tokens, heads, dim, dtype), _dtype(dtype), _vector(q_starts, batch + 1, torch.int32),
-        _vector(kv_lens, batch, torch.int32), _vector(table, batch * per, torch.int32), per,
+        *_heads(q, tokens, heads, dim, dtype, dev), _dtype(dtype), _vector(q_starts, batch + 1, torch.int32, dev),
+        _vector(kv_lens, batch, torch.int32, dev), _vector(table, batch * per, torch.int32, dev), per,
         tokens, batch, heads, kv_heads, dim, max_q, max_kv, *held, cache.bits, pages, page_size,
-        causal, window, dim ** -0.5 if scale is None else scale, *_heads(out, tokens, heads, dim, dtype),
-        None if lse is None else _vector(lse, tokens * heads, torch.float32), ws, ws_bytes, _raw_stream(_current_device()))
+        causal, window, dim ** -0.5 if scale is None else scale, *_heads(out, tokens, heads, dim, dtype, dev),
+        None if lse is None else _vector(lse, tokens * heads, torch.float32, dev), ws, ws_bytes, _raw_stream(dev))
     if st:
         raise MpqError(st, "mpq_cache_attention")
     return out
