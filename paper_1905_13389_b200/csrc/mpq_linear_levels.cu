@@ -380,6 +380,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         const int block = half * 4 + quarter, c0 = half * (BN / 2);
         uint32_t* sh = transpose + block * 32 * Shape::row_words;
         auto block_sync = [&] { asm volatile("bar.sync %0, 64;" ::"r"(1 + block) : "memory"); };
+        auto block_all = [&](bool mine) {                  // ... and whether it holds in both warps
+            uint32_t all;
+            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbar.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                         : "=r"(all) : "r"(1 + block), "r"((uint32_t)mine) : "memory");
+            return all != 0;
+        };
         bool ok = true;
         const T* res = static_cast<const T*>(g.res);
         T* out = static_cast<T*>(g.out);
@@ -416,9 +422,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 for (int j = 0; j < 32; j += 2)
                     *reinterpret_cast<uint2*>(sh + lane * Shape::row_words + 2 * ((part * 16 + j / 2) ^ lane)) = make_uint2(v[j], v[j + 1]);
             }
-            block_sync();
             // (the other warp of the block may have given up: half of the columns are missing then)
-            if (!ok || __any_sync(0xffffffffu, has_failed())) ct[0].scale = ct[1].scale = kNaN;
+            if (!block_all(ok)) ct[0].scale = ct[1].scale = kNaN;
             {
                 // kRowsAtOnce rows at a time.  All residuals of a group are requested before any is used or any result is
                 // written: they may lie in the result's own tensor, so the compiler could not move a load up by itself, and
