@@ -44,6 +44,24 @@ __device__ __forceinline__ float linear_value(const LinearArgs& g, uint32_t acc,
     const float f = (float)(int32_t)(4u * acc + r.term - c.term) * (r.scale * c.scale);
     return g.bias ? f + c.bias : f;
 }
+// f Phi(f), with Phi(-|f|) = erfc(|f| / sqrt 2) / 2 made as a product, so that negative f keep their relative precision
+// (0.5 f (1 + erf) cancels: it lost several percent of the result at -5 and all of it below -5.6).  erfc(z) e^(z^2) / 2 is
+// a polynomial in t = 1 / (1 + 0.43 z), fitted here to the least largest relative error over z in [0, 10], 1.0e-7; with fp32
+// roundings the relative error is 2.6e-6 for f down to -8, most of it from the rounded exponent.
+// (erfcf: 73.9 us at 4096^3, 61.0 with this; 0.5 f (1 + erff) took 63.3.)
+__device__ __forceinline__ float gelu(float f) {
+    const float t = __fdividef(1.0f, fmaf(fabsf(f), 0.43f * 0.70710678f, 1.0f));
+    float q = 0.036572885f;
+    q = fmaf(q, t, -0.15404773f);
+    q = fmaf(q, t, 0.18994352f);
+    q = fmaf(q, t, -0.041152050f);
+    q = fmaf(q, t, 0.12254029f);
+    q = fmaf(q, t, 0.10273626f);
+    q = fmaf(q, t, 0.12214691f);
+    q = fmaf(q, t, 0.12125991f);
+    const float below = q * t * fast_exp2(f * f * -0.72134752f);         // Phi(-|f|); log2(e) / 2
+    return f * (f >= 0.0f ? 1.0f - below : below);
+}
 // The activation of N values at once: one (uniform) branch for all of them, so their chains overlap.
 template <int N>
 __device__ __forceinline__ void glue_values(float (&f)[N], int glue) {
@@ -52,7 +70,7 @@ __device__ __forceinline__ void glue_values(float (&f)[N], int glue) {
         for (int i = 0; i < N; ++i) f[i] = max_nan(f[i], 0.0f);       // a NaN range stays visible, as under the other activations
     } else if (glue == MPQ_GLUE_GELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = 0.5f * f[i] * (1.0f + erff(f[i] * 0.70710678118654752f));
+        for (int i = 0; i < N; ++i) f[i] = gelu(f[i]);
     } else if (glue == MPQ_GLUE_GELU_TANH) {
         // 0.5 f (1 + tanh z) = f / (1 + e^(-2z)); the exponential saturates to 0 or infinity, the quotient to f or 0
 #pragma unroll
