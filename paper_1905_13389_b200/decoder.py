@@ -13,7 +13,7 @@ A block is the usual one of a decoder-only transformer, with every product on le
 Weights are encoded once, at construction, with one range per output channel; activations get one range per
 token.  Positions are the caller's to put into the hidden states.  ``forward`` takes the new tokens of a batch of
 sequences -- whole prompts, chunks of prompts and single tokens mixed -- and only launches kernels on the current
-stream.  ``Pages`` keeps the host's side of the cache: which pages a sequence owns.
+stream; ``check`` says afterwards whether all of them have done their work.  ``Pages`` keeps the host's side of the cache: which pages a sequence owns.
 
     python -m paper_1905_13389_b200.decoder          # a small model: two prompts, then eight tokens each
 """
@@ -94,6 +94,7 @@ class EncodedDecoder:
             layer.update({name: w[name].float().contiguous() for name in ("up_bias", "norm1", "norm2")})
             layer["cache"] = mpq.level_cache(pages, config.kv_heads, page_size, config.dim, config.cache_bits, device)
             self.layers.append(layer)
+        self.given_up = mpq.wait_failures()
 
     def forward(self, x: torch.Tensor, batch: Batch) -> torch.Tensor:
         """Hidden states [tokens][width] (float16 or bfloat16) of the batch's new tokens -> hidden states after the last
@@ -112,6 +113,15 @@ class EncodedDecoder:
             h = mpq.linear_levels(h, w["up"], bias=w["up_bias"], act="gelu_tanh", dtype=dtype)
             x = mpq.linear_levels(mpq.encode_levels(h, c.act_bits), w["down"], residual=x, dtype=dtype)
         return x
+
+
+    def check(self):
+        """Raises if a kernel has given up a wait since the model was made or last checked.  What it left is NaN, but an encoder
+        behind it takes a NaN for a zero, so the hidden states need not show it.  Waits for the stream: for a place where the
+        caller waits for a result anyway."""
+        before, self.given_up = self.given_up, mpq.wait_failures()
+        if self.given_up != before:
+            raise RuntimeError("%d CTAs gave up a wait: the results since the last check are not valid" % (self.given_up - before))
 
 
 def random_weights(config: Config, device, seed: int = 0) -> List[Dict[str, torch.Tensor]]:
@@ -142,6 +152,7 @@ def main():
         x = model.forward(x, batch)[batch.q_starts[1:].long() - 1]                             # each sequence's last token
         logits = mpq.linear_levels(mpq.rmsnorm_levels(x, None, config.eps), words)
         nxt = logits.argmax(1).cpu()
+        model.check()
         tokens = {s: nxt[i:i + 1] for i, s in enumerate(tokens)}
         for i, s in enumerate(said):
             said[s].append(int(nxt[i]))

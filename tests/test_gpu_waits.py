@@ -63,6 +63,33 @@ def test_a_wait_that_runs_out_leaves_nan_and_a_healthy_device(mpq, cuda, what):
     assert r.returncode == 0 and "waits ran out" in r.stdout, r.stdout[-2000:] + r.stderr[-4000:]
 
 
+DECODER = """
+import torch
+from paper_1905_13389_b200 import binding as mpq, decoder
+
+cuda = torch.device("cuda:0")
+config = decoder.Config(layers=1, width=256, heads=8, kv_heads=2, dim=64, inner=768)
+model, pages = decoder.EncodedDecoder(config, decoder.random_weights(config, cuda), pages=32, page_size=16), decoder.Pages(32, 16)
+x = torch.randn((70, config.width), device=cuda).to(torch.bfloat16)
+model.forward(x, pages.extend({0: 70}, cuda))
+model.check()
+mpq.wait_limit(0)
+model.forward(x, pages.extend({1: 70}, cuda))
+mpq.wait_limit()
+try:
+    model.check()
+except RuntimeError as e:
+    print("noticed:", e)
+model.forward(x, pages.extend({2: 70}, cuda))
+model.check()
+"""
+
+
+def test_the_decoder_notices_a_wait_that_ran_out(mpq, cuda):
+    r = subprocess.run([sys.executable, "-c", DECODER], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "noticed:" in r.stdout, r.stdout[-2000:] + r.stderr[-4000:]
+
+
 def test_no_wait_runs_out_in_ordinary_calls(mpq, cuda):
     """One call of each tensor-core form, in this process and with the ordinary limit."""
     import torch
