@@ -24,32 +24,35 @@ struct RowArgs {
 // a third of the kernel's instructions, and it is bound by issuing them (0.78 of the issue slots).
 // Under the norm the largest magnitude keeps NaNs: an infinite element gives r = 0, and its product with a gain of 0 or
 // with r is the NaN that the row's range has to be.  Without the norm a NaN takes no part in the range.
-// A finite row whose sum of squares overflows fp32 gives r = 0 as well.  Every thread sees that, the row is read again
-// and (2^-80 h)^2 is summed (`scaled`), so it keeps its range.  residual_out, which may lie over the inputs, is therefore
-// stored after the statistics (29.6 -> 30.4 us at 4096 x 4096; a second sum beside the ordinary one: 31.4).
-constexpr float kDown = 8.271806125530277e-25f;                          // 2^-80: 2^23 squares of 2^48 fit
+// A finite row whose sum of squares overflows fp32 gives r = 0 as well.  Every thread sees that, the row is read again and
+// its squares are summed 2^160 times smaller (large_row_scalars), so it keeps its range; residual_out, which may lie over
+// the inputs, is therefore stored after the statistics.  (4096 x 4096: 28.2 us before, 28.9 so; with a sum of its own for large
+// squares beside the ordinary one some 30.)
 struct RowScalars { float r, s, inv, alpha; };
 template <bool NORM> __device__ __forceinline__ float larger(float a, float b) { return NORM ? max_nan(a, b) : fmaxf(a, b); }
 template <bool NORM>
-__device__ __forceinline__ RowScalars row_scalars(float ss, float mx, const RowArgs& g, bool scaled) {
+__device__ __forceinline__ RowScalars row_scalars(float r, float mx, int L) {
     RowScalars c;
-    const float eps = scaled ? g.eps * kDown * kDown : g.eps;
-    c.r = NORM ? __fdiv_rn(scaled ? kDown : 1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)g.k), eps))) : 1.0f;
-    if (scaled && !ordinary(ss)) mx = __int_as_float(0x7fffffff);        // NaN: an element is infinite
-    c.s = NORM ? mx * c.r : mx;
+    c.r = r;
+    c.s = NORM ? mx * r : mx;
     c.inv = inverse_scale(c.s);
-    c.alpha = __fdiv_rn(c.s, (float)g.rule.L);
+    c.alpha = __fdiv_rn(c.s, (float)L);
     return c;
 }
 template <bool NORM>
-__device__ __forceinline__ RowScalars block_scalars(float ss, float mx, const RowArgs& g, float2* sh, RowScalars* sh_scalars, bool scaled = false) {
+__device__ __forceinline__ float row_factor(float ss, const RowArgs& g) {
+    return NORM ? __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)g.k), g.eps))) : 1.0f;
+}
+// The row's constants in every thread.  (sh keeps the warps' maxima, and the lanes of a single warp the row's in mx.)
+template <bool NORM>
+__device__ __forceinline__ RowScalars block_scalars(float ss, float& mx, const RowArgs& g, float2* sh, RowScalars* sh_scalars) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         if (NORM) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         mx = larger<NORM>(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     }
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    if (warps == 1) return row_scalars<NORM>(ss, mx, g, scaled);
+    if (warps == 1) return row_scalars<NORM>(row_factor<NORM>(ss, g), mx, g.rule.L);
     if (lane == 0) sh[threadIdx.x >> 5] = make_float2(ss, mx);
     __syncthreads();
     if (threadIdx.x < 32) {
@@ -60,23 +63,35 @@ __device__ __forceinline__ RowScalars block_scalars(float ss, float mx, const Ro
             if (NORM) ss += __shfl_xor_sync(0xffffffffu, ss, o);
             mx = larger<NORM>(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         }
-        const RowScalars c = row_scalars<NORM>(ss, mx, g, scaled);
+        const RowScalars c = row_scalars<NORM>(row_factor<NORM>(ss, g), mx, g.rule.L);
         if (lane == 0) *sh_scalars = c;
     }
     __syncthreads();
     return *sh_scalars;
 }
-// This thread's share of the row's squares in that scale.  Not inlined: inside the kernel the loop, which hardly any call
-// reaches, cost 5 us of 30.
+// The constants of a row whose squares overflow, in every thread; sh holds the warps' maxima of the first round.  Not inlined:
+// hardly any call comes here.
 template <typename T>
-__device__ __noinline__ float small_squares(const T* x, const T* res, int k) {
+__device__ __noinline__ RowScalars large_row_scalars(const T* x, const T* res, int k, float eps, int L, float mx, float2* sh) {
+    constexpr float kDown = 8.271806125530277e-25f;                      // 2^-80: 2^23 squares of 2^48 fit
     float ss = 0.0f;
 #pragma unroll 1
     for (int i = threadIdx.x; i < k; i += blockDim.x) {
         const float v = (to_f32(x[i]) + (res ? to_f32(res[i]) : 0.0f)) * kDown;
         ss = fmaf(v, v, ss);
     }
-    return ss;
+#pragma unroll 1
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    const int warps = blockDim.x >> 5;
+    if (warps > 1) {
+        if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5].x = ss;
+        __syncthreads();
+        ss = mx = 0.0f;
+#pragma unroll 1
+        for (int w = 0; w < warps; ++w) { ss += sh[w].x; mx = max_nan(mx, sh[w].y); }
+    }
+    const float r = __fdiv_rn(kDown, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)k), eps * kDown * kDown)));
+    return row_scalars<true>(ordinary(ss) ? r : kNaN, mx, L);            // an element is infinite: NaN
 }
 __device__ __forceinline__ void block_level_sum(int u, int32_t* dst, int* sh) {
     u = __reduce_add_sync(0xffffffffu, u);
@@ -151,7 +166,7 @@ __device__ __forceinline__ void store_values(const RowArgs& g, int64_t row, int6
 // One CTA per row; the row stays in registers between the statistics and the quantizer (NV vectors of
 // VEC elements per thread), so memory is read once and written once.
 template <typename T, int VEC, int NV, bool VECTOR, bool NORM, int ACT>
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(1024, NV == 1 ? 2 : 1)           // 32 registers where a vector is all a thread has: every thread of the device
 level_rows_kernel(const RowArgs g) {
     __shared__ float2 sh_stats[32];
     __shared__ RowScalars sh_scalars;
@@ -211,7 +226,7 @@ level_rows_kernel(const RowArgs g) {
         }
     }
     RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
-    if (NORM && c.r == 0.0f) c = block_scalars<NORM>(small_squares(x, res, k), mx, g, sh_stats, &sh_scalars, true);
+    if (NORM && c.r == 0.0f) c = large_row_scalars(x, res, k, g.eps, g.rule.L, mx, sh_stats);
     const float r = c.r, s = c.s, inv = c.inv, alpha = c.alpha;
     // (a NaN range, after a NaN or an infinity under the norm, has the reciprocal 0 and is not ordinary)
     const bool plain = ordinary(s) && ordinary(inv);
@@ -260,7 +275,7 @@ level_wide_rows_kernel(const RowArgs g) {
         mx = larger<NORM>(mx, ACT == MPQ_ACT_HRELU ? h : fabsf(h));
     }
     RowScalars c = block_scalars<NORM>(ss, mx, g, sh_stats, &sh_scalars);
-    if (NORM && c.r == 0.0f) c = block_scalars<NORM>(small_squares(x, res, (int)g.k), mx, g, sh_stats, &sh_scalars, true);
+    if (NORM && c.r == 0.0f) c = large_row_scalars(x, res, (int)g.k, g.eps, g.rule.L, mx, sh_stats);
     const float r = c.r, s = c.s, inv = c.inv, alpha = c.alpha;
     uint8_t* out = g.levels + row * g.row_bytes;
     int total = 0;
