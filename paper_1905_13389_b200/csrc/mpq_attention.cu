@@ -9,7 +9,7 @@
 // query rows the other one, so a single token of a few heads wastes little.  The element order inside a dot product is free, so the 16 level bytes that a lane reads ARE its operand
 // fragment, for the keys (lane = token, bytes along dim) and for the values (lane = 16 dims of a token pair);
 // only W^T changes hands, by one 8 x 8 register transpose per 8 tokens.  With so few rows the work is bound by
-// reading the cache, not by the matrix pipe, which is why the 128-row tcgen05 tile, mostly empty here, is not used.
+// reading the cache, not by the matrix pipe, which is why the 256-row tcgen05 tile, mostly empty here, is not used.
 #include "mpq_attention.cuh"
 
 namespace mpq {

@@ -11,8 +11,9 @@
 // has outgrown it by 2^3; the weights are then made again and its part of O_h is rescaled.
 //
 // What bounds it (dim 128, 8 bits; cycles per step of 128 tokens and both tiles, of 5800 measured): shared memory
-// some 4700 at 128 bytes a cycle (the products' operands 2000 -- those 64 wide read Q again for every half step -- the
-// softmax's constants, which all 16 warps read, 1500, the levels' stores 600), the issue slots 3100, the tensor cores
+// some 4900 at 128 bytes a cycle (the products' operands 2000 -- those 64 wide read Q again for every half step -- and 2900
+// wavefronts of loads and stores as counted, a launch's beginning and end among them: the softmax's constants, which all
+// 16 warps read, are 1500 of these, the levels' stores 500 without their conflicts), the issue slots 3200, the tensor cores
 // 2000 at their full rate, the exponentials 2048 of the special-function units.  None is full, each phase waits for
 // another one's.  2048 tokens over 10240, 32 heads on 8: 503 us, 615 TFLOP/s.  On the way: 1181 us with row-per-thread
 // softmax and loads as they were needed, 715 with everything loaded a step ahead, 690 with constants shared by four

@@ -21,7 +21,7 @@ struct RowArgs {
 // y = (h gain) r with one r > 0 per row, and a rounded product by r is monotone, so
 // max |y| = r max |h gain| to the last bit: both statistics come out of ONE pass.
 // The row's constants follow from them in the first warp alone: a root and four exact divisions in every thread were
-// a third of the kernel's instructions, and it is bound by issuing them (0.78 of the issue slots).
+// a third of the kernel's instructions, and it is bound by issuing them (0.74 of the issue slots).
 // Under the norm the largest magnitude keeps NaNs: an infinite element gives r = 0, and its product with a gain of 0 or
 // with r is the NaN that the row's range has to be.  Without the norm a NaN takes no part in the range.
 // A finite row whose sum of squares overflows fp32 gives r = 0 as well.  Every thread sees that, the row is read again and

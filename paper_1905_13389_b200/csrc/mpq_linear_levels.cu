@@ -62,7 +62,9 @@ __device__ __forceinline__ float gelu(float f) {
     const float below = q * t * fast_exp2(f * f * -0.72134752f);         // Phi(-|f|); log2(e) / 2
     return f * (f >= 0.0f ? 1.0f - below : below);
 }
-// The activation of N values at once: one (uniform) branch for all of them, so their chains overlap.
+// The activation of N values at once: one (uniform) branch for all of them, so their chains overlap.  SiLU and the tanh form
+// use the fast exponential and quotient also for fp32 results: between -8 and -3 they are off by 0.4e-6 and 3.3e-6 of the
+// result (measured), more of it from the rounded exponent than from the fast forms.
 template <int N>
 __device__ __forceinline__ void glue_values(float (&f)[N], int glue) {
     if (glue == MPQ_GLUE_RELU) {
@@ -287,7 +289,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 // row pieces whatever the row stride is.  Sixteen warps store (eight: 60.2 us for 57.7 at 4096^3, 45.9 for 41.5 at
 // 777 x 5001 x 4100 with an unaligned residual and output).
 // What bounds it: the operands' way from L2, 24 KB per CTA and 128 bytes of k, some 45 bytes a cycle and multiprocessor;
-// 4096^3 with bias and GELU takes 57.7 us, 2.38 POP/s.  256 x 256 tiles read a quarter less but leave the last of their
+// 4096^3 with bias and GELU (tanh form) takes 57.3 us, 2.40 POP/s.  256 x 256 tiles read a quarter less but leave the last of their
 // 3.5 rounds half empty (62 us for 61 with eight storing warps; 1024 x 4096 x 4096 23.5 for 22.0).
 constexpr int kPairStoreWarps = 16;                       // four per quarter of the TMEM lanes: two for each half of the columns
 constexpr int kPairThreads = 64 + 32 * kPairStoreWarps;
