@@ -64,7 +64,7 @@ __device__ __forceinline__ float gelu(float f) {
 }
 // The activation of N values at once: one (uniform) branch for all of them, so their chains overlap.  SiLU and the tanh form
 // use the fast exponential and quotient also for fp32 results: between -8 and -3 they are off by 0.4e-6 and 3.3e-6 of the
-// result (measured), more of it from the rounded exponent than from the fast forms.
+// result (measured).
 template <int N>
 __device__ __forceinline__ void glue_values(float (&f)[N], int glue) {
     if (glue == MPQ_GLUE_RELU) {

@@ -10,8 +10,9 @@
 
 namespace mpq {
 
-// Polls that each last 4 us at most: 4 s.  The longest wait is that for a whole tile of a product, a third of a microsecond
-// per 128 bytes of k: 1 s for a single row of 2^31 elements in four parts, less for any other operands that memory holds.
+// Polls that each last 4 us at most: 4 s.  The longest wait is that for a whole tile of a product, under half a microsecond
+// per 128 bytes of k (64 x 4096 x 9216): 2 s for a single row of 2^31 elements in four parts, less for any other operands that
+// memory holds.
 constexpr uint32_t kSpinLimit = 1u << 20;
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
