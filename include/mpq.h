@@ -407,6 +407,80 @@ int mpq_cache_attention(const void* q, int64_t q_token_stride, int64_t q_head_st
                         void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
                         void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ==== A server's step over many requests ======================================================
+ * What lies around the block when many requests are served at once: their pages and slots, made
+ * on the device, so that a captured step can be replayed while the requests grow; adapters that
+ * differ from request to request beside the shared weights; and the drawing of their tokens.
+ *
+ * State of a paged cache on the device: table [sequences][per_sequence] (the pages that each
+ * sequence owns, in the order of its tokens), lens [sequences] (its tokens), free_pages [pages] (a
+ * stack of the pages that nobody owns: the first count[0] entries, the last of which is taken
+ * next) and count [2] (count[1] is 0 between calls).  One state serves all layers' caches.  Calls
+ * on one state follow one another: two that overlap on the GPU race.
+ *
+ * mpq_pages_extend makes room for the new tokens of a batch and describes it in the form that
+ * mpq_cache_write and mpq_cache_attention take.  Entry b asks for new_tokens[b] tokens of sequence
+ * seqs[b] (seqs NULL: sequence b); an entry whose sequence lies outside the state (-1 by
+ * convention) or that asks for a negative number is padding.  Sequences of one call are distinct.
+ *   need_b = ceil((lens + new) / page_size) - ceil(lens / page_size) pages, taken off the stack
+ *   entry by entry;  q_starts[b] = new tokens before entry b [batch + 1];  kv_lens[b] = lens + new;
+ *   slots[t], t < tokens: where new token t goes, -1 from q_starts[batch] on;
+ *   batch_table [batch][per_sequence]: the entry's pages, 0 behind the last.  Padding: no tokens, no context.
+ * All or nothing: missing[0] is 0, or the number of pages that the stack lacks, or -1 (a sequence
+ * would outgrow its row of the table) or -2 (more new tokens than `tokens`); in these cases the
+ * state stays as it was, all slots are -1 and q_starts, kv_lens and batch_table are 0.
+ *
+ * mpq_pages_trim shortens sequences to keep[b] tokens (those that have fewer, and entries with a
+ * negative keep, stay) and puts the pages behind them back on the stack -- 0 drops a sequence.  A
+ * trim to the lengths before an extend, with the same seqs, undoes it to the last entry of the stack.
+ * batch is at most 8192; pages, tokens and per_sequence * page_size are below 2^31. */
+int mpq_pages_extend(int32_t* table, int64_t per_sequence, int32_t* lens, int sequences,
+                     int32_t* free_pages, int64_t pages, int32_t* count, int page_size,
+                     const int32_t* seqs, const int32_t* new_tokens, int batch, int64_t tokens,
+                     int64_t* slots, int32_t* q_starts, int32_t* kv_lens, int32_t* batch_table, int32_t* missing,
+                     void* stream);
+int mpq_pages_trim(int32_t* table, int64_t per_sequence, int32_t* lens, int sequences,
+                   int32_t* free_pages, int64_t pages, int32_t* count, int page_size,
+                   const int32_t* seqs, const int32_t* keep, int batch, void* stream);
+
+/* mpq_linear_levels with a low-rank adapter per request beside the shared weights:
+ *   z[r][i] = factor[id] (a_scale[r] / L_a) sum_t q_a[r][t] down[id][i][t]            (fp32)
+ *   f = float(acc) * (...) + bias[c] + sum_i z[r][i] up[id][c][i];  f = glue(f);  ... as there.
+ * Row r of the activations belongs to sequence b with q_starts[b] <= r < q_starts[b+1] (q_starts
+ * [batch + 1] ascends) and takes adapter id = ids[b]; rows of no sequence, and those whose id lies
+ * outside 0 .. adapters-1 (-1 by convention), take none.
+ * down [adapters][rank][mpq_level_row_bytes(k)] (0 behind element k-1) and up [adapters][n][rank],
+ * of adapter_dtype (MPQ_F16 or MPQ_BF16), 16-byte aligned; rank a multiple of 16, at most 128
+ * (smaller adapters are padded with zeros).  factor [adapters] may be NULL (ones).
+ * workspace: mpq_linear_adapted_workspace(m, rank) bytes, 16-byte aligned, used by this call alone. */
+int64_t mpq_linear_adapted_workspace(int64_t m, int rank);
+int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const int32_t* a_sums, int a_bits,
+                       const uint8_t* w, const float* w_scale, const int32_t* w_sums, int w_bits,
+                       int64_t m, int64_t n, int64_t k,
+                       const void* down, const void* up, int adapter_dtype, const float* factor, int adapters, int rank,
+                       const int32_t* q_starts, const int32_t* ids, int batch,
+                       const float* bias, int glue, const void* residual, int64_t ldr,
+                       void* out, int dtype, int64_t ldo,
+                       void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Draws one token a row from logits [rows x vocab] of dtype, row stride ld.  Per row, with the
+ * tokens ordered by logit (largest first, the lower index first among equals):
+ *   w_i = exp((x_i - max x) / temperature);  top_k: the first top_k of the order stay;
+ *   top_p: of these the shortest beginning whose weights sum to top_p of theirs or more;
+ *   min_p: of these the ones with w_i >= min_p; the first of the order always stays;
+ *   token = the lowest index among those left at which the sum of the weights up to it (in the order of the
+ *   indices) exceeds uniform * (the sum of all of them).
+ * temperature <= 0 takes the first of the order.  top_k <= 0 or >= vocab, top_p >= 1 and min_p <= 0
+ * leave their rule out, as does a NULL array (temperature NULL: 1).  uniform lies in [0, 1) and is
+ * clamped to it.  Weights are held to 2^-44 of the largest; a logit of -infinity is never drawn.
+ * logprob (optional): log of the token's share in sum_i exp(x_i), whatever the rules are.
+ * tokens -1 and logprob NaN: a row with a NaN, with nothing over -infinity, with +infinity at a
+ * temperature over 0, or with a NaN among its own numbers.
+ * vocab is at most 393216 (MPQ_F32) or 786432 (MPQ_F16, MPQ_BF16).  rows = 0 does nothing. */
+int mpq_sample(const void* logits, int64_t ld, int dtype, int64_t rows, int64_t vocab,
+               const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+               const float* uniform, int64_t* tokens, float* logprob, void* stream);
+
 /* How many CTAs of the tensor-core kernels (mpq_linear_levels, mpq_cache_attention) have given up a wait since
  * the library was loaded on the current device: 0 unless the device or the driver misbehaves.  The results that
  * such a CTA would have stored are NaN.  Synchronizes the stream. */

@@ -101,11 +101,18 @@ def lib() -> ctypes.CDLL:
         L.mpq_cache_attention_workspace.restype = i64
         L.mpq_cache_attention.argtypes = [P, i64, i64, i32, P, P, P, i64, i64, i32, i32, i32, i32, i64, i64, P, P, P, P,
                                           i32, i64, i32, i32, i64, f32, P, i64, i64, P, P, i64, P]
+        L.mpq_pages_extend.argtypes = [P, i64, P, i32, P, i64, P, i32, P, P, i32, i64, P, P, P, P, P, P]
+        L.mpq_pages_trim.argtypes = [P, i64, P, i32, P, i64, P, i32, P, P, i32, P]
+        L.mpq_linear_adapted_workspace.argtypes = [i64, i32]
+        L.mpq_linear_adapted_workspace.restype = i64
+        L.mpq_linear_adapted.argtypes = [P, P, P, i32, P, P, P, i32, i64, i64, i64, P, P, i32, P, i32, i32, P, P, i32, P, i32, P, i64, P, i32, i64,
+                                         P, i64, P]
+        L.mpq_sample.argtypes = [P, i64, i32, i64, i64, P, P, P, P, P, P, P, P]
         L.mpq_wait_failures.argtypes = [ctypes.POINTER(ctypes.c_uint), P]
         L.mpq_wait_limit.argtypes = [i32]
         L.mpq_wait_limit.restype = None
         for name in ("mpq_wait_failures", "mpq_rmsnorm_levels", "mpq_encode_levels", "mpq_linear_levels", "mpq_cache_write", "mpq_cache_read",
-                     "mpq_cache_attention"):
+                     "mpq_cache_attention", "mpq_pages_extend", "mpq_pages_trim", "mpq_linear_adapted", "mpq_sample"):
             getattr(L, name).restype = i32
         for name in ("mpq_absmax", "mpq_encode", "mpq_encode_nchw", "mpq_encode_oihw", "mpq_gemm", "mpq_conv",
                      "mpq_add_relu", "mpq_stem_conv7x7", "mpq_maxpool3x3s2", "mpq_conv_fused", "mpq_zero", "mpq_linear", "mpq_linear_static", "mpq_linear_host", "mpq_measure_popc_peak",
@@ -712,6 +719,151 @@ def cache_attention(q: torch.Tensor, cache: LevelCache, q_starts: torch.Tensor, 
         None if lse is None else _vector(lse, tokens * heads, torch.float32, dev), ws, ws_bytes, _raw_stream(dev))
     if st:
         raise MpqError(st, "mpq_cache_attention")
+    return out
+
+
+class PageState(NamedTuple):
+    """Who owns the pages of a paged cache, on the device: table int32 [sequences][pages per sequence], lens int32 [sequences],
+    free int32 [pages] (a stack), count int32 [2] (how many of them are free; 0), page_size."""
+    table: torch.Tensor
+    lens: torch.Tensor
+    free: torch.Tensor
+    count: torch.Tensor
+    page_size: int
+
+
+class PagePlan(NamedTuple):
+    """A batch's new tokens as the cache calls take them (slots int64 [tokens], the others int32), and what the cache lacked."""
+    slots: torch.Tensor
+    q_starts: torch.Tensor
+    kv_lens: torch.Tensor
+    table: torch.Tensor
+    missing: torch.Tensor
+
+
+class Adapters(NamedTuple):
+    """Low-rank adapters as a product takes them: down [adapters][rank][level_row_bytes(k)] and up [adapters][n][rank] of
+    float16 or bfloat16, rank a multiple of 16, scale float32 [adapters] or None.  See :func:`adapters`."""
+    down: torch.Tensor
+    up: torch.Tensor
+    scale: Optional[torch.Tensor]
+    k: int
+
+
+def page_state(sequences: int, per_sequence: int, pages: int, page_size: int, device="cuda") -> PageState:
+    """The state of a cache of which every page is free; page 0 is taken first."""
+    ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)                 # noqa: E731
+    return PageState(ints(sequences, per_sequence), ints(sequences), torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device),
+                     torch.tensor([pages, 0], dtype=torch.int32, device=device), page_size)
+
+
+def _pages(s: PageState, seqs: Optional[torch.Tensor], amount: torch.Tensor):
+    """Device and the arguments that both calls on a state begin with."""
+    table, lens, free, count, page_size = s
+    dev = _device(table)
+    sequences, per = table.shape
+    batch, pages = amount.numel(), free.numel()
+    return dev, per, batch, (_vector(table, sequences * per, torch.int32, dev), per, _vector(lens, sequences, torch.int32, dev), sequences,
+                             _vector(free, pages, torch.int32, dev), pages, _vector(count, 2, torch.int32, dev), page_size,
+                             None if seqs is None else _vector(seqs, batch, torch.int32, dev), _vector(amount, batch, torch.int32, dev), batch)
+
+
+def pages_extend(state: PageState, seqs: Optional[torch.Tensor], new: torch.Tensor, tokens: int, out: Optional[PagePlan] = None) -> PagePlan:
+    """Takes pages for ``new`` tokens (int32 [batch]) of the sequences ``seqs`` (int32 [batch], -1: padding; None: 0, 1, ..)
+    and describes the batch, its slots padded to ``tokens`` with -1.  All or nothing: missing says what did not fit."""
+    dev, per, batch, args = _pages(state, seqs, new)
+    if out is None:
+        ints = torch.empty_strided((2 * batch + 2,), (1,), dtype=torch.int32, device=new.device)
+        out = PagePlan(torch.empty_strided((tokens,), (1,), dtype=torch.int64, device=new.device), ints[:batch + 1], ints[batch + 1:2 * batch + 1],
+                       torch.empty_strided((batch, per), (per, 1), dtype=torch.int32, device=new.device), ints[2 * batch + 1:])
+    slots, starts, lens, table, missing = out
+    st = (_lib or lib()).mpq_pages_extend(
+        *args, tokens, _vector(slots, tokens, torch.int64, dev), _vector(starts, batch + 1, torch.int32, dev), _vector(lens, batch, torch.int32, dev),
+        _vector(table, batch * per, torch.int32, dev), _vector(missing, 1, torch.int32, dev), _raw_stream(dev))
+    if st:
+        raise MpqError(st, "mpq_pages_extend")
+    return out
+
+
+def pages_trim(state: PageState, seqs: Optional[torch.Tensor], keep: torch.Tensor) -> PageState:
+    """Shortens the sequences ``seqs`` to ``keep`` tokens (int32 [batch]; 0 drops one, a negative number leaves it) and gives
+    the pages behind them back."""
+    dev, _, _, args = _pages(state, seqs, keep)
+    st = (_lib or lib()).mpq_pages_trim(*args, _raw_stream(dev))
+    if st:
+        raise MpqError(st, "mpq_pages_trim")
+    return state
+
+
+def adapters(down: torch.Tensor, up: torch.Tensor, scale: Optional[torch.Tensor] = None) -> Adapters:
+    """Lays adapters out once: down [adapters][rank][k] and up [adapters][n][rank] (float16 or bfloat16) padded with zeros to
+    whole 16s of rank and k."""
+    count, rank, k = down.shape
+    if up.shape[0] != count or up.shape[2] != rank or up.dtype != down.dtype or (scale is not None and scale.shape != (count,)):
+        raise ValueError("expected down [adapters][rank][k], up [adapters][n][rank] of one type and scale [adapters], got %s %s, %s %s" % (
+            down.dtype, tuple(down.shape), up.dtype, tuple(up.shape)))
+    pad = torch.nn.functional.pad
+    return Adapters(pad(down, (0, -k % 16, 0, -rank % 16)).contiguous(), pad(up, (0, -rank % 16)).contiguous(),
+                    None if scale is None else scale.float().contiguous(), k)
+
+
+def linear_adapted_workspace(m: int, rank: int) -> int:
+    return int(lib().mpq_linear_adapted_workspace(m, rank))
+
+
+def linear_adapted(a: Levels, w: Levels, low: Adapters, q_starts: torch.Tensor, ids: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                   act: str = "none", residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   dtype: torch.dtype = torch.float32, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """:func:`linear_levels` with the adapter ids[b] (int32; -1: none) beside the weights for the rows q_starts[b] ..
+    q_starts[b + 1] - 1 (int32 [batch + 1]) of the activations, inside the activation."""
+    m, n, k = a.bytes.shape[0], w.bytes.shape[0], a.k
+    if act not in GLUE:
+        raise ValueError("unknown activation %r: expected one of %s" % (act, ", ".join(GLUE)))
+    dev = _device(a.bytes)
+    pa, pw = _held(a, m, k, dev), _held(w, n, k, dev)
+    down, up, factor, low_k = low
+    count, rank, _ = down.shape
+    if low_k != k:
+        raise ValueError("the adapters are for k = %d, the product has k = %d" % (low_k, k))
+    batch, wtype = ids.numel(), down.dtype
+    row = (k + 15) // 16 * 16
+    if out is None:
+        out = torch.empty_strided((m, n), (n, 1), dtype=dtype, device=a.bytes.device)
+    else:
+        dtype = out.dtype
+    po, ldo = _rows(out, m, n, dtype, dev)
+    if workspace is None:
+        need = (m * (rank + 1) * 4 + 15) // 16 * 16       # = linear_adapted_workspace(m, rank)
+        workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=a.bytes.device)
+    st = (_lib or lib()).mpq_linear_adapted(
+        *pa, a.bits, *pw, w.bits, m, n, k, _vector(down, count * rank * row, wtype, dev), _vector(up, count * n * rank, wtype, dev), _dtype(wtype),
+        None if factor is None else _vector(factor, count, torch.float32, dev), count, rank,
+        _vector(q_starts, batch + 1, torch.int32, dev), _vector(ids, batch, torch.int32, dev), batch,
+        None if bias is None else _vector(bias, n, torch.float32, dev), GLUE[act],
+        *(_NO_ROWS if residual is None else _rows(residual, m, n, dtype, dev)), po, _dtype(dtype), ldo, *_workspace(workspace, dev), _raw_stream(dev))
+    if st:
+        raise MpqError(st, "mpq_linear_adapted")
+    return out
+
+
+def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+           logprob: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Draws a token (int64) from each row of logits [rows x vocab] with the random numbers ``uniform`` (float32 [rows], in
+    [0, 1)) and the rows' own rules (float32, top_k int32; None: not used).  logprob receives the tokens' log probabilities."""
+    rows, vocab = logits.shape
+    dev = _device(logits)
+    if out is None:
+        out = torch.empty_strided((rows,), (1,), dtype=torch.int64, device=logits.device)
+    f32 = torch.float32
+    st = (_lib or lib()).mpq_sample(
+        *_rows(logits, rows, vocab, logits.dtype, dev), _dtype(logits.dtype), rows, vocab,
+        None if temperature is None else _vector(temperature, rows, f32, dev), None if top_k is None else _vector(top_k, rows, torch.int32, dev),
+        None if top_p is None else _vector(top_p, rows, f32, dev), None if min_p is None else _vector(min_p, rows, f32, dev),
+        _vector(uniform, rows, f32, dev), _vector(out, rows, torch.int64, dev), None if logprob is None else _vector(logprob, rows, f32, dev),
+        _raw_stream(dev))
+    if st:
+        raise MpqError(st, "mpq_sample")
     return out
 
 

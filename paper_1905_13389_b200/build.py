@@ -21,10 +21,12 @@ FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-I", INCLUDE,
 # IEEE arithmetic is part of the contract (bit-exact codes): never --use_fast_math / -ftz.
 
 PLAIN = ["mpq_api.cu", "mpq_encode.cu", "mpq_encode_trig.cu", "mpq_gemm.cu", "mpq_glue.cu", "mpq_probe.cu",
-         "mpq_levels.cu", "mpq_linear_levels.cu", "mpq_cache.cu", "mpq_attention.cu", "mpq_attention_tiles.cu"]
+         "mpq_levels.cu", "mpq_linear_levels.cu", "mpq_cache.cu", "mpq_attention.cu", "mpq_attention_tiles.cu",
+         "mpq_pages.cu", "mpq_adapters.cu", "mpq_sample.cu"]
 # headers of the decoder-block operators only: the other sources are not rebuilt for them
-BLOCK_HEADERS = ["mpq_levels.cuh", "mpq_attention.cuh", "mpq_tensor.cuh"]
-BLOCK_SOURCES = {"mpq_levels.cu", "mpq_linear_levels.cu", "mpq_cache.cu", "mpq_attention.cu", "mpq_attention_tiles.cu"}
+BLOCK_HEADERS = ["mpq_levels.cuh", "mpq_attention.cuh", "mpq_tensor.cuh", "mpq_adapters.cuh"]
+BLOCK_SOURCES = {"mpq_levels.cu", "mpq_linear_levels.cu", "mpq_cache.cu", "mpq_attention.cu", "mpq_attention_tiles.cu",
+                 "mpq_adapters.cu", "mpq_sample.cu"}
 HEADERS = ["mpq_common.cuh", "mpq_branch_kernel.cuh", "mpq_branch_launch.cuh", "mpq_pointwise_kernel.cuh", os.path.join(INCLUDE, "mpq.h")]
 
 

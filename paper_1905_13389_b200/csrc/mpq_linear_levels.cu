@@ -4,6 +4,7 @@
 //   sum q_a q_w = 4 sum u_a u_w - 2 L_w sum u_a - 2 L_a sum u_w + k L_a L_w,
 // so the inner loop multiplies unsigned bytes and the level sums that lie beside the operands do the rest.
 // The result fits int32 (checked on the host), hence the terms may be combined modulo 2^32.
+#include "mpq_adapters.cuh"
 #include "mpq_attention.cuh"
 #include "mpq_tensor.cuh"
 
@@ -22,7 +23,29 @@ struct LinearArgs {
     const void* res; int64_t ldr;
     void* out; int64_t ldo;
     uint32_t polls;                                       // limit of a wait
+    const void* up = nullptr; int rank = 0;               // adapters: [..][n][rank]
+    const float* z = nullptr; const int32_t* chosen = nullptr;    // per token: what its adapter has made of it [rank], which one (-1: none)
 };
+
+// What the adapter of token r adds to column c; W: the type of its elements, void for a product without adapters.
+template <typename W>
+__device__ __forceinline__ float low_rank(const LinearArgs& g, int64_t r, int64_t c) {
+    if constexpr (std::is_void_v<W>) {
+        return 0.0f;
+    } else {
+        const int id = __ldg(g.chosen + r);
+        if (id < 0) return 0.0f;
+        const W* up = static_cast<const W*>(g.up) + ((int64_t)id * g.n + c) * g.rank;
+        float sum = 0.0f;
+        for (int i = 0; i < g.rank; i += 8) {
+            float u[8];
+            load_vec<W, 8>(up + i, u);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(u[j], __ldg(g.z + r * g.rank + i + j), sum);
+        }
+        return sum;
+    }
+}
 
 // acc (levels u, unsigned) -> one output, in the header's order of operations
 struct RowTerm { float scale; uint32_t term; };          // a_scale / L_a;  k L_a L_w - 2 L_w sums_a
@@ -122,7 +145,7 @@ __device__ __forceinline__ void store_column(const LinearArgs& g, float (&f)[N],
     for (int j = 0; j < N; ++j) if (j < count) out[j * g.ldo] = from_f32<T>(f[j]);
 }
 
-template <typename T, int BN>
+template <typename T, typename W, int BN>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const LinearArgs g,
                     int tiles_w, int splits) {
@@ -233,6 +256,10 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                     float f[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) f[j] = linear_value(g, v[j], RowTerm{row_scale[r0 + j], row_terms[r0 + j]}, ct);
+                    if constexpr (!std::is_void_v<W>) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) if (c < g.n && m0 + r0 + j < g.m) f[j] += low_rank<W>(g, m0 + r0 + j, c);
+                    }
                     glue_values(f, g.glue);
                     store_column<T, 16>(g, f, (int64_t)m0 + r0, c, (int)min((int64_t)16, g.m - m0 - r0));
                 } else {
@@ -265,6 +292,10 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                         uint32_t acc = 0;
                         for (int s = 0; s < splits; ++s) acc += exchange_ptr[(s * own + j0 + j) * 128 + col];
                         f[j] = linear_value(g, acc, RowTerm{row_scale[rr + j], row_terms[rr + j]}, ct);
+                    }
+                    if constexpr (!std::is_void_v<W>) {
+#pragma unroll
+                        for (int j = 0; j < N; ++j) if (m0 + rr + j < g.m) f[j] += low_rank<W>(g, m0 + rr + j, c);
                     }
                     glue_values(f, g.glue);
                     store_column<T, N>(g, f, (int64_t)m0 + rr, c, (int)min((int64_t)N, g.m - m0 - rr));
@@ -302,7 +333,7 @@ struct PairShape {
     static constexpr int smem = stages * stage_bytes + transpose_bytes + 1024;
 };
 
-template <typename T>
+template <typename T, typename W>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const LinearArgs g,
                    int tiles_m, int tiles) {
@@ -481,6 +512,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         f[2 * j] = linear_value(g, v.x, rt, ct[0]);
                         f[2 * j + 1] = linear_value(g, v.y, rt, ct[1]);
                     }
+                    if constexpr (!std::is_void_v<W>) {
+#pragma unroll
+                        for (int j = 0; j < kRowsAtOnce; ++j) {
+                            if (r0 + j < rows && in_x) f[2 * j] += low_rank<W>(g, row0 + r0 + j, cx);
+                            if (r0 + j < rows && in_y) f[2 * j + 1] += low_rank<W>(g, row0 + r0 + j, cy);
+                        }
+                    }
                     glue_values(f, g.glue);
                     if (res) {
 #pragma unroll
@@ -530,11 +568,11 @@ inline int small_splits(int64_t tiles, int64_t blocks, int bn, int64_t sms) {
     return splits;
 }
 
-template <typename T, int BN>
+template <typename T, typename W, int BN>
 int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
     using Shape = SmallShape<BN>;
     static PerDeviceOnce once;
-    auto* kernel = linear_small_kernel<T, BN>;
+    auto* kernel = linear_small_kernel<T, W, BN>;
     int rc = once.raise_smem_limit(kernel, Shape::smem);
     if (rc != MPQ_OK) return rc;
     CUtensorMap map_w, map_a;
@@ -561,12 +599,12 @@ int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
     return launch_status();
 }
 
-template <typename T>
+template <typename T, typename W>
 int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     using Shape = PairShape;
     constexpr int BN = kPairCols;
     static PerDeviceOnce once;
-    auto* kernel = linear_pair_kernel<T>;
+    auto* kernel = linear_pair_kernel<T, W>;
     int rc = once.raise_smem_limit(kernel, Shape::smem);
     if (rc != MPQ_OK) return rc;
     CUtensorMap map_w, map_a;
@@ -585,23 +623,23 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
 //   64 tiles: 128 x 4096 x 4096 11.8 / 15.2;  128: 200 x 4096 x 4096 12.5 / 15.2;  142: 100 x 9000 x 1000 9.4 / 11.9;
 //   144: 128 x 9216 x 4096 14.3 / 17.1, 2300 x 512 x 9216 19.5 / 22.4;  150: 128 x 9600 x 4096 23.7 / 22.4;
 //   213: 130 x 9000 x 1000 16.6 / 12.6;  256: 1000 x 2000 x 2000 19.8 / 13.1.
-template <typename T>
+template <typename T, typename W = void>
 int launch_linear_levels(const LinearArgs& g, cudaStream_t st) {
-    if (g.m <= 16) return launch_linear_small<T, 16>(g, st);
-    if (g.m <= 32) return launch_linear_small<T, 32>(g, st);
-    if (g.m <= 64 || ceil_div(g.m, 64) * ceil_div(g.n, 128) <= sm_count()) return launch_linear_small<T, 64>(g, st);
-    return launch_linear_pair<T>(g, st);
+    if (g.m <= 16) return launch_linear_small<T, W, 16>(g, st);
+    if (g.m <= 32) return launch_linear_small<T, W, 32>(g, st);
+    if (g.m <= 64 || ceil_div(g.m, 64) * ceil_div(g.n, 128) <= sm_count()) return launch_linear_small<T, W, 64>(g, st);
+    return launch_linear_pair<T, W>(g, st);
 }
 
 }  // namespace mpq
 
 using namespace mpq;
 
-extern "C" int mpq_linear_levels(const uint8_t* a, const float* a_scale, const int32_t* a_sums, int a_bits,
-                                 const uint8_t* w, const float* w_scale, const int32_t* w_sums, int w_bits,
-                                 int64_t m, int64_t n, int64_t k,
-                                 const float* bias, int glue, const void* residual, int64_t ldr,
-                                 void* out, int dtype, int64_t ldo, void* stream) {
+namespace {
+// What both calls look at; `g` is filled in where they are right.
+int linear_args(LinearArgs& g, const uint8_t* a, const float* a_scale, const int32_t* a_sums, int a_bits,
+                const uint8_t* w, const float* w_scale, const int32_t* w_sums, int w_bits, int64_t m, int64_t n, int64_t k,
+                const float* bias, int glue, const void* residual, int64_t ldr, void* out, int dtype, int64_t ldo) {
     if (m != 0 && (!a || !a_scale || !a_sums || !w || !w_scale || !w_sums || !out)) return MPQ_ERR_NULL;
     if (m < 0 || n <= 0 || k <= 0 || m > 0x7fffffff || n > 0x7fffffff || (m > 1 && (ldo < n || (residual && ldr < n)))) return MPQ_ERR_BAD_SHAPE;
     if (!bits_ok(a_bits) || !bits_ok(w_bits) || !dtype_ok(dtype) || glue < MPQ_GLUE_NONE || glue > MPQ_GLUE_SILU) return MPQ_ERR_UNSUPPORTED;
@@ -610,12 +648,57 @@ extern "C" int mpq_linear_levels(const uint8_t* a, const float* a_scale, const i
     const int e = dtype_size(dtype);
     if (!aligned16(a) || !aligned16(w) || !aligned_to(a_scale, 4) || !aligned_to(a_sums, 4) || !aligned_to(w_scale, 4) || !aligned_to(w_sums, 4) ||
         !aligned_to(bias, 4) || !aligned_to(residual, e) || !aligned_to(out, e)) return MPQ_ERR_ALIGN;
+    g = LinearArgs{a, a_scale, a_sums, w, w_scale, w_sums, m, n, k, level_row_bytes(k), (int)La, (int)Lw, bias, glue, residual, ldr, out, ldo, wait_limit()};
+    return MPQ_OK;
+}
+template <typename W>
+int launch_linear_typed(const LinearArgs& g, int dtype, cudaStream_t st) {
+    if (dtype == MPQ_F32) return launch_linear_levels<float, W>(g, st);
+    if (dtype == MPQ_F16) return launch_linear_levels<__half, W>(g, st);
+    return launch_linear_levels<__nv_bfloat16, W>(g, st);
+}
+}  // namespace
+
+extern "C" int mpq_linear_levels(const uint8_t* a, const float* a_scale, const int32_t* a_sums, int a_bits,
+                                 const uint8_t* w, const float* w_scale, const int32_t* w_sums, int w_bits,
+                                 int64_t m, int64_t n, int64_t k,
+                                 const float* bias, int glue, const void* residual, int64_t ldr,
+                                 void* out, int dtype, int64_t ldo, void* stream) {
+    LinearArgs g;
+    const int rc = linear_args(g, a, a_scale, a_sums, a_bits, w, w_scale, w_sums, w_bits, m, n, k, bias, glue, residual, ldr, out, dtype, ldo);
+    return rc != MPQ_OK || m == 0 ? rc : launch_linear_typed<void>(g, dtype, (cudaStream_t)stream);
+}
+
+extern "C" int64_t mpq_linear_adapted_workspace(int64_t m, int rank) {
+    return m <= 0 || rank <= 0 ? 0 : (m * (rank + 1) * 4 + 15) / 16 * 16;
+}
+
+extern "C" int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const int32_t* a_sums, int a_bits,
+                                  const uint8_t* w, const float* w_scale, const int32_t* w_sums, int w_bits,
+                                  int64_t m, int64_t n, int64_t k,
+                                  const void* down, const void* up, int adapter_dtype, const float* factor, int adapters, int rank,
+                                  const int32_t* q_starts, const int32_t* ids, int batch,
+                                  const float* bias, int glue, const void* residual, int64_t ldr,
+                                  void* out, int dtype, int64_t ldo, void* workspace, int64_t workspace_bytes, void* stream) {
+    LinearArgs g;
+    int rc = linear_args(g, a, a_scale, a_sums, a_bits, w, w_scale, w_sums, w_bits, m, n, k, bias, glue, residual, ldr, out, dtype, ldo);
+    if (rc != MPQ_OK) return rc;
+    if (m != 0 && (!down || !up || !q_starts || (batch != 0 && !ids) || !workspace)) return MPQ_ERR_NULL;
+    if (adapters <= 0 || rank <= 0 || batch < 0) return MPQ_ERR_BAD_SHAPE;
+    if ((adapter_dtype != MPQ_F16 && adapter_dtype != MPQ_BF16) || rank % 16 || rank > 128) return MPQ_ERR_UNSUPPORTED;
+    if (!aligned16(down) || !aligned16(up) || !aligned16(workspace) || !aligned_to(factor, 4) || !aligned_to(q_starts, 4) || !aligned_to(ids, 4)) return MPQ_ERR_ALIGN;
     if (m == 0) return MPQ_OK;
-    const LinearArgs g = {a, a_scale, a_sums, w, w_scale, w_sums, m, n, k, level_row_bytes(k), (int)La, (int)Lw, bias, glue, residual, ldr, out, ldo,
-                          wait_limit()};
-    if (dtype == MPQ_F32) return launch_linear_levels<float>(g, (cudaStream_t)stream);
-    if (dtype == MPQ_F16) return launch_linear_levels<__half>(g, (cudaStream_t)stream);
-    return launch_linear_levels<__nv_bfloat16>(g, (cudaStream_t)stream);
+    if (workspace_bytes < mpq_linear_adapted_workspace(m, rank)) return MPQ_ERR_WORKSPACE;
+    g.up = up;
+    g.rank = rank;
+    float* z = static_cast<float*>(workspace);
+    int32_t* chosen = reinterpret_cast<int32_t*>(z + m * rank);
+    g.z = z;
+    g.chosen = chosen;
+    const AdapterArgs d = {a, a_scale, g.La, m, k, g.row_bytes, down, factor, adapters, rank, q_starts, ids, batch, z, chosen};
+    rc = adapter_down(d, adapter_dtype, (cudaStream_t)stream);
+    if (rc != MPQ_OK) return rc;
+    return adapter_dtype == MPQ_F16 ? launch_linear_typed<__half>(g, dtype, (cudaStream_t)stream) : launch_linear_typed<__nv_bfloat16>(g, dtype, (cudaStream_t)stream);
 }
 
 namespace {
