@@ -2,20 +2,33 @@
 //
 // Which token is drawn hangs on where a running sum passes a border, so weights are 64-bit fixed-point numbers
 // (whole multiples of 2^-shift of the largest weight, made from 64-bit exponentials): their sums are exact whatever the
-// order, and a border lies within 2^-44 or so of where real numbers would have it.
-#include "mpq_levels.cuh"
+// order, borders are exact products with the row's own numbers, and the sums lie within some 2^-45 of real numbers'.
+// (With 32-bit weights a tail token of a flat row of 131,072 is another one in some percent of the draws.)
+//
+// A row belongs to a thread-block cluster, whose CTAs hold a share of it each in shared memory: the logits are read once,
+// and every further look at them is at the shares.  Nothing is sorted.  The end of top-k and of top-p is a key (the
+// logit's bits in their order) and a place among its equals: two passes count, by 11 bits of the key each, where the
+// border lies -- exactly for top-k, with rounded weights for top-p --, and a third one takes the exact sum of all that
+// lies above the 2^10 keys found and counts their members; equals have equal weights, so count times weight is exact.
+// Where rounding had led astray the search goes on from there, on the right side.
+#include "mpq_attention.cuh"
+#include "mpq_tensor.cuh"
 
 namespace mpq {
 
+typedef unsigned long long u64;
+
 struct SampleArgs {
     const void* logits; int64_t ld;
-    int64_t rows; int vocab;
+    int vocab;
     const float *temperature; const int32_t* top_k; const float *top_p, *min_p, *uniform;
     int64_t* tokens; float* logprob;
     int shift;                                            // weights are multiples of 2^-shift: vocab 2^shift <= 2^62
+    int ctas, warp_chunks;                                // CTAs of a row; 16-byte chunks that a warp holds
 };
 
-constexpr int kSampleThreads = 1024;
+constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
+constexpr int kSampleBins = 2048, kLowBits = 10;          // 11 + 11 + 10 bits of a key
 
 // Whole numbers in the order of the logits; -0 and 0 are the same number.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -24,98 +37,488 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-template <typename V, typename Op>
-__device__ V block_reduce(V v, Op op, V* sh) {
-    for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = sh[threadIdx.x & 31];
-    for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+// f s for 0 <= f < 1, rounded down or up to a whole number, exactly.
+__device__ __forceinline__ u64 share_of(u64 s, float f, bool up) {
+    const uint32_t b = __float_as_uint(f), e = b >> 23;
+    const u64 m = e ? (b & 0x7fffffu) | 0x800000u : b;
+    const int shift = 150 - (int)(e ? e : 1);             // f = m 2^-shift, shift >= 24
+    const u64 lo = m * s, hi = __umul64hi(m, s);
+    if (m == 0) return 0;
+    u64 q, rest;
+    if (shift < 64) { q = hi << (64 - shift) | lo >> shift; rest = lo << (64 - shift); }
+    else if (shift == 64) { q = hi; rest = lo; }
+    else if (shift < 128) { q = hi >> (shift - 64); rest = lo | hi << (128 - shift); }
+    else { q = 0; rest = 1; }
+    return q + (up && rest ? 1 : 0);
+}
+
+__device__ __forceinline__ u64 ld_cluster64(uint32_t addr) {
+    u64 v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_cluster32(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint2 ld_cluster32x2(uint32_t addr) {
+    uint2 v;
+    asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
     return v;
 }
 
+// What passes between a row's CTAs, two of each: one is written while others may still read the one before.
+struct SampleShared {
+    u64 parts[2][kSampleWarps];
+    uint32_t bins[2][kSampleBins];
+    u64 scan[kSampleWarps];
+    double powers[16];                                    // 2^(i / 16): sixteen, so that lanes never ask one bank for two of them
+    int found[2];
+    uint32_t digit, digit_before;
+    u64 above;
+};
+
 template <typename T>
-__global__ void __launch_bounds__(kSampleThreads) sample_kernel(const SampleArgs g) {
-    typedef unsigned long long u64;
-    __shared__ u64 sh[32];
-    __shared__ double shd[32];
-    chain_entry();
-    const int64_t row = blockIdx.x;
-    const T* x = static_cast<const T*>(g.logits) + row * g.ld;
-    const float warm = g.temperature ? g.temperature[row] : 1.0f;
-    const bool greedy = warm <= 0.0f;
-    auto sum = [&](auto f) {
-        u64 s = 0;
-        for (int i = threadIdx.x; i < g.vocab; i += kSampleThreads) s += f(i, to_f32(x[i]) + 0.0f);
-        return block_reduce(s, [](u64 a, u64 b) { return a + b; }, sh);
-    };
-    // the first of the order: largest value, lowest index
-    u64 best = 0;
-    bool bad = false;
-    for (int i = threadIdx.x; i < g.vocab; i += kSampleThreads) {
-        const float v = to_f32(x[i]);
-        bad |= v != v;
-        best = max(best, (u64)order_key(v) << 32 | (uint32_t)~i);
+struct SampleRow {
+    static constexpr int E = 16 / (int)sizeof(T);         // elements of a chunk
+    SampleShared& sh;
+    uint4* data;
+    const int ctas, rank, warp, lane, warp_chunks;
+    const int v0;                                         // place of this warp's first element; places count from the 16-byte boundary before the row
+    int turn = 0;                                         // which of the two exchange buffers comes next
+
+    __device__ SampleRow(SampleShared& s, uint4* d, const SampleArgs& g)
+        : sh(s), data(d), ctas(g.ctas), rank(g.ctas > 1 ? (int)cluster_rank() : 0), warp(__shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0)), lane(threadIdx.x & 31),
+          warp_chunks(g.warp_chunks), v0((rank * kSampleWarps + warp) * g.warp_chunks * E) {}
+
+    __device__ __forceinline__ void sync() {
+        if (ctas > 1) cluster_sync_all();
+        else __syncthreads();
     }
-    best = block_reduce(best, [](u64 a, u64 b) { return a > b ? a : b; }, sh);
-    bad = __syncthreads_or(bad);
-    const float top = key_value((uint32_t)(best >> 32));
-    const int first = (int)~(uint32_t)best;
-    const float p = g.top_p ? g.top_p[row] : 1.0f, least = g.min_p ? g.min_p[row] : 0.0f, u = greedy ? 0.0f : g.uniform[row];
-    bad |= top == -INFINITY || warm != warm || (!greedy && (top == INFINITY || p != p || least != least || u != u));
-    int token = first;
-    if (!bad && !greedy) {
-        const double cool = 1.0 / (double)warm, unit = (double)(1ull << g.shift);
-        auto exact = [&](float v) { return exp(((double)v - (double)top) * cool); };
-        auto weight = [&](float v) { return v == -INFINITY ? 0ull : max(1ull, (u64)__double2ll_rn(exact(v) * unit)); };
-        // kept: keys over `edge`, and those equal to it up to index `cut`
-        uint32_t edge = 0;
-        int cut = 0x7fffffff;
-        auto kept = [&](int i, float v) { const uint32_t k = order_key(v); return k > edge || (k == edge && i <= cut); };
-        // the largest edge whose keys and those over it have f's sum at `goal` or more, then the place among its equals
-        auto narrow = [&](u64 goal, auto f) {
-            uint32_t e = 0;
-            for (int bit = 31; bit >= 0; --bit) {
-                const uint32_t next = e | 1u << bit;
-                if (sum([&](int i, float v) { return kept(i, v) && order_key(v) >= next ? f(v) : 0ull; }) >= goal) e = next;
+    __device__ __forceinline__ uint32_t peer(const void* p, int cta) const { return ctas > 1 ? map_to_cta(smem_addr(p), (uint32_t)cta) : smem_addr(p); }
+
+    static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[E]) {
+        const T* e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = to_f32(e[i]);
+    }
+    // f(place, value) for this lane's elements, in whole warps: places of a warp ascend with the step, then the lane.
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        for (int c0 = 0; c0 < warp_chunks; c0 += 32) {
+            const int c = c0 + lane;
+            if (c < warp_chunks) {
+                float x[E];
+                unpack(data[warp * warp_chunks + c], x);
+#pragma unroll
+                for (int i = 0; i < E; ++i) f(v0 + c * E + i, x[i]);
             }
-            const u64 over = sum([&](int i, float v) { return kept(i, v) && order_key(v) > e ? f(v) : 0ull; });
-            const u64 each = f(key_value(e));
-            const u64 equals = goal > over && each ? (goal - over + each - 1) / each : 0;
-            int c = -1;                                    // the largest cut with fewer than `equals` equals before it, plus one
-            for (int bit = 30; bit >= 0; --bit) {
-                const int next = c + (1 << bit);
-                if (next < g.vocab && sum([&](int i, float v) { return (u64)(kept(i, v) && order_key(v) == e && i <= next); }) < equals) c = next;
+        }
+    }
+
+    // Every warp's number -> all numbers of the row's warps, four to a lane, the same in all warps of all CTAs.
+    __device__ __forceinline__ void gather(u64 mine, u64 (&v)[4]) {
+        u64* part = sh.parts[turn];
+        if (lane == 0) part[warp] = mine;
+        sync();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = lane * 4 + i;
+            v[i] = n < ctas * kSampleWarps ? ld_cluster64(peer(part + n % kSampleWarps, n / kSampleWarps)) : 0;
+        }
+        turn ^= 1;
+    }
+    static __device__ __forceinline__ u64 warp_sum(u64 s) {
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        return s;
+    }
+    template <typename F>
+    __device__ __forceinline__ u64 total(F f) {
+        u64 s = 0, v[4];
+        each([&](int place, float x) { s += f(place, x); });
+        gather(warp_sum(s), v);
+        return warp_sum(v[0] + v[1] + v[2] + v[3]);
+    }
+
+    // The lowest place at which the running sum of f exceeds goal(sum of all), in the one thread that finds it (-1 elsewhere).
+    template <typename F, typename Goal>
+    __device__ __forceinline__ int running(F f, Goal goal_of) {
+        u64 s = 0, v[4];
+        each([&](int place, float x) { s += f(place, x); });
+        gather(warp_sum(s), v);
+        auto scan = [&](u64 x) {
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 below = __shfl_up_sync(0xffffffffu, x, o);
+                if (lane >= o) x += below;
+            }
+            return x;
+        };
+        const u64 here = v[0] + v[1] + v[2] + v[3], upto = scan(here), all = __shfl_sync(0xffffffffu, upto, 31), goal = goal_of(all);
+        const int in = __ffs(__ballot_sync(0xffffffffu, upto > goal)) - 1;      // the lane that holds the warp in question
+        if (in < 0) return -1;
+        u64 before = upto - here;
+        int which = lane * 4;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (which == lane * 4 + i && before + v[i] <= goal) { before += v[i]; ++which; }
+        which = __shfl_sync(0xffffffffu, which, in);
+        before = __shfl_sync(0xffffffffu, before, in);
+        if (which != rank * kSampleWarps + warp) return -1;
+        for (int c0 = 0; c0 < warp_chunks; c0 += 32) {
+            const int c = c0 + lane;
+            float x[E];
+            u64 w[E], mine = 0;
+            if (c < warp_chunks) unpack(data[warp * warp_chunks + c], x);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                w[i] = c < warp_chunks ? f(v0 + c * E + i, x[i]) : 0;
+                mine += w[i];
+            }
+            const u64 to = before + scan(mine);
+            const int hit = __ffs(__ballot_sync(0xffffffffu, to > goal)) - 1;
+            if (hit >= 0) {
+                if (lane != hit) return -1;
+                u64 sum = to - mine;
+                for (int i = 0; i < E; ++i) {
+                    sum += w[i];
+                    if (sum > goal) return v0 + c * E + i;
+                }
+            }
+            before = __shfl_sync(0xffffffffu, to, 31);
+        }
+        return -1;
+    }
+
+    // Adds up what the CTAs have counted by `bins` and finds, from the highest bin down, the one in which the sum reaches goal
+    // (the lowest that has anything, if none does); `above` is the sum before it.
+    __device__ __forceinline__ void border(u64 goal, uint32_t& digit, u64& above) {
+        sync();
+        constexpr int kPer = kSampleBins / kSampleThreads;
+        const int hi = kSampleBins - 1 - (int)threadIdx.x * kPer;          // this thread's bins: hi, hi - 1, ..
+        u64 n[kPer] = {};
+#pragma unroll
+        for (int i = 0; i < kPer; i += 2)
+            for (int c = 0; c < ctas; ++c) {
+                const uint2 two = ld_cluster32x2(peer(&sh.bins[turn][hi - i - 1], c));
+                n[i] += two.y;
+                n[i + 1] += two.x;
+            }
+        u64 mine = 0, over_lowest = 0;
+        uint32_t lowest = kSampleBins;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (n[i]) { lowest = hi - i; over_lowest = mine; }
+            mine += n[i];
+        }
+        const u64 upto = block_scan(mine);
+        if (threadIdx.x == 0) { sh.digit = kSampleBins; sh.digit_before = kSampleBins; }
+        __syncthreads();
+        if (lowest < kSampleBins) atomicMin(&sh.digit_before, lowest);
+        u64 before = upto - mine;
+        over_lowest += before;
+        if (before < goal && upto >= goal) {
+            bool open = true;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (open && before + n[i] >= goal) { sh.digit = hi - i; sh.above = before; open = false; }
+                before += n[i];
+            }
+        }
+        __syncthreads();
+        if (sh.digit == kSampleBins && lowest == sh.digit_before && lowest < kSampleBins) sh.above = over_lowest;
+        __syncthreads();
+        digit = sh.digit == kSampleBins ? sh.digit_before : sh.digit;
+        above = sh.above;
+        turn ^= 1;
+    }
+    __device__ __forceinline__ u64 block_scan(u64 x) {
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 below = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += below;
+        }
+        if (lane == 31) sh.scan[warp] = x;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) x += sh.scan[w];
+        __syncthreads();
+        return x;
+    }
+    __device__ __forceinline__ uint32_t* clear_bins() {
+        uint32_t* bins = sh.bins[turn];
+        for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) bins[i] = 0;
+        __syncthreads();
+        return bins;
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleArgs g) {
+    extern __shared__ uint4 held[];
+    __shared__ SampleShared sh;
+    constexpr int E = SampleRow<T>::E;
+    SampleRow<T> r(sh, held, g);
+    const int warp = r.warp, lane = r.lane;
+    if (threadIdx.x < 16) sh.powers[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+    chain_entry();
+    const int64_t row = blockIdx.x / g.ctas;
+    const T* x0 = static_cast<const T*>(g.logits) + row * g.ld;
+    const int skew = (int)(reinterpret_cast<uintptr_t>(x0) & 15) / (int)sizeof(T);        // the row's first place
+    const float warm = g.temperature ? g.temperature[row] : 1.0f;
+    const int k = g.top_k ? g.top_k[row] : 0;
+    const float p = g.top_p ? g.top_p[row] : 1.0f, least = g.min_p ? g.min_p[row] : 0.0f, u = g.uniform[row];
+
+    // the row into shared memory, -infinity before and behind it; the first of its order, and NaNs
+    float best = -INFINITY;
+    int best_chunk = 0;
+    bool nan = false;
+    constexpr int kLoads = 4;
+    for (int c0 = 0; c0 < g.warp_chunks; c0 += 32 * kLoads) {
+        uint4 in[kLoads];
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int c = c0 + 32 * j + lane;
+            const int64_t i = (int64_t)r.v0 + c * E - skew;
+            if (c < g.warp_chunks && i >= 0 && i + E <= g.vocab) {
+                in[j] = __ldg(reinterpret_cast<const uint4*>(x0 + i));
+            } else {
+                T* e = reinterpret_cast<T*>(&in[j]);
+#pragma unroll
+                for (int q = 0; q < E; ++q) e[q] = c < g.warp_chunks && i + q >= 0 && i + q < g.vocab ? x0[i + q] : from_f32<T>(-INFINITY);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int c = c0 + 32 * j + lane;
+            if (c < g.warp_chunks) held[warp * g.warp_chunks + c] = in[j];
+            float x[E], top = -INFINITY;
+            SampleRow<T>::unpack(in[j], x);
+#pragma unroll
+            for (int q = 0; q < E; ++q) { nan |= x[q] != x[q]; top = fmaxf(top, x[q]); }
+            if (top > best) { best = top; best_chunk = c; }
+        }
+    }
+    u64 code = 0;                                         // 0: nothing over -infinity; all ones: a NaN
+    if (best > -INFINITY) {
+        float x[E];
+        SampleRow<T>::unpack(held[warp * g.warp_chunks + best_chunk], x);
+        int at = E - 1;
+#pragma unroll
+        for (int q = E - 1; q >= 0; --q) if (x[q] == best) at = q;
+        code = (u64)order_key(best) << 32 | (uint32_t)~(r.v0 + best_chunk * E + at);
+    }
+    if (nan) code = ~0ull;
+    {
+        u64 v[4];
+        for (int o = 16; o > 0; o >>= 1) code = max(code, __shfl_xor_sync(0xffffffffu, code, o));
+        r.gather(code, v);
+        code = max(max(v[0], v[1]), max(v[2], v[3]));
+        for (int o = 16; o > 0; o >>= 1) code = max(code, __shfl_xor_sync(0xffffffffu, code, o));
+    }
+    const float top = key_value((uint32_t)(code >> 32));
+    const int first = (int)~(uint32_t)code;
+    const bool greedy = warm <= 0.0f;
+    const bool bad = code == 0 || code == ~0ull || warm != warm || (!greedy && (top == INFINITY || p != p || least != least || u != u));
+    if (bad) {
+        if (r.rank == 0 && threadIdx.x == 0) {
+            g.tokens[row] = -1;
+            if (g.logprob) g.logprob[row] = kNaN;
+        }
+        if (g.ctas > 1) cluster_sync_all();               // nobody leaves while others read its numbers
+        return;
+    }
+
+    // What the others weigh together, the first one's weight being 1: where it has nearly all of the probability its
+    // logarithm is -log(1 + rest).  32 bits: a term is off by
+    // (2 |d| + 4) 2^-24 of itself at most, d its distance from the first.
+    double rest = 0.0;
+    if (g.logprob) {
+        float some = 0.0f;
+        r.each([&](int v, float x) {
+            const float e = fast_exp2((x - top) * 1.4426950408889634f);
+            some += v != first ? e : 0.0f;
+        });
+        rest = some;
+        for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+        u64 v[4];
+        r.gather((u64)__double_as_longlong(rest), v);
+        rest = (__longlong_as_double(v[0]) + __longlong_as_double(v[1])) + (__longlong_as_double(v[2]) + __longlong_as_double(v[3]));
+        for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+    }
+    auto finish = [&](int v, float x) {                   // by one thread of the row
+        g.tokens[row] = v - skew;
+        if (g.logprob) g.logprob[row] = (float)(((double)x - (double)top) - log1p(rest));
+    };
+    if (greedy) {
+        if (r.rank == 0 && threadIdx.x == 0) finish(first, top);
+        if (g.ctas > 1) cluster_sync_all();
+        return;
+    }
+
+    // exp((x - top) / warm) 2^shift, rounded: 2^(t / 16) with t = n + f is 2^(n / 16) from the table and shifts, times the
+    // series of 2^(f / 16), |f| <= 1/2, off by 2^-42 of itself.  What is less than one multiple weighs one, so that
+    // every token over -infinity can be drawn.
+    const double cool = 16.0 * 1.4426950408889634073599 / (double)warm;
+    const float coolf = 1.0f / warm, gone = -0.69314718f * (float)g.shift;
+    const double dtop = (double)top;
+    constexpr double kMagic = 6755399441055744.0;         // 1.5 2^52: its low bits are whole numbers
+    auto weight = [&](float x) -> u64 {
+        u64 w = 1;
+        if (!((x - top) * coolf < gone)) {
+            const double t = ((double)x - dtop) * cool, m = t + kMagic, f = t - (m - kMagic);
+            const int n = __double2loint(m);
+            const double a = sh.powers[n & 15];
+            constexpr double kLog = 0.69314718055994530942 / 16;
+            double q = fma(f, kLog * kLog * kLog * kLog * kLog / 120, kLog * kLog * kLog * kLog / 24);
+            q = fma(f, q, kLog * kLog * kLog / 6);
+            q = fma(f, q, kLog * kLog / 2);
+            q = fma(f, q, kLog);
+            const double scaled = __hiloint2double(__double2hiint(a) + (((n >> 4) + g.shift) << 20), __double2loint(a));
+            // below 2^51: on top of 2^52 its low bits are the rounded number
+            w = (u64)__double_as_longlong(fma(scaled * f, q, scaled) + 4503599627370496.0) & ((1ull << 52) - 1);
+        }
+        return x > -INFINITY ? w : 0ull;
+    };
+    // kept: keys over `edge`, and those equal to it up to place `cut`
+    uint32_t edge = 0;
+    int cut = 0x7fffffff;
+    auto kept = [&](int v, float x) { const uint32_t key = order_key(x); return key > edge || (key == edge && v <= cut); };
+    // The keys, and the place among the equals of the last one, at which the sum of f from the top reaches `goal`: edge and cut.
+    // guess: f, or something near it in 32 bits of which the whole row's sum fits 32 bits, in units of `unit` of f's.
+    auto narrow = [&](u64 goal, auto f, auto guess, float unit) {
+        uint32_t over = 1u << (32 - kLowBits), under = 0xffffffffu;        // the border lies below `over` and above `under` (key >> kLowBits)
+        u64 base = 0;                                     // f's sum from `over` on
+        uint32_t e;
+        u64 before, each_one, members;
+        int64_t bias = 0;                                 // by how much the guesses above `under` fall short
+        for (;;) {                                        // (each turn takes at least one occupied key off the open ones)
+            auto open = [&](uint32_t key) { const uint32_t high = key >> kLowBits; return high < over && (under == 0xffffffffu || high > under); };
+            u64 above1, above2;
+            const u64 want = (u64)max((int64_t)((double)(goal - base) / (double)unit) - bias, (int64_t)1);
+            uint32_t high, low;
+            uint32_t* bins = r.clear_bins();
+            r.each([&](int v, float x) {
+                const uint32_t key = order_key(x);
+                if (open(key) && kept(v, x)) { const uint32_t n = guess(x); if (n) atomicAdd(bins + (key >> 21), n); }
+            });
+            r.border(want, high, above1);
+            bins = r.clear_bins();
+            r.each([&](int v, float x) {
+                const uint32_t key = order_key(x);
+                if (key >> 21 == high && open(key) && kept(v, x)) { const uint32_t n = guess(x); if (n) atomicAdd(bins + (key >> kLowBits & 2047), n); }
+            });
+            r.border(want > above1 ? want - above1 : 1, low, above2);
+            high = min(high << 11 | low, (1u << (32 - kLowBits)) - 1);
+            // exactly: what lies above, and how many have each of the keys found
+            bins = r.clear_bins();
+            u64 s = 0;
+            r.each([&](int v, float x) {
+                const uint32_t key = order_key(x);
+                if (key >> kLowBits >= high && kept(v, x)) {
+                    if (key >> kLowBits == high) atomicAdd(bins + (key & 1023), 1u);
+                    else s += f(x);
+                }
+            });
+            u64 v[4];
+            const int turn = r.turn;
+            r.gather(SampleRow<T>::warp_sum(s), v);
+            const u64 sum = SampleRow<T>::warp_sum(v[0] + v[1] + v[2] + v[3]);
+            const int lo = 1023 - 2 * (int)threadIdx.x;   // this thread's keys: lo, lo - 1
+            u64 n[2] = {0, 0}, w[2];
+            for (int c = 0; c < g.ctas; ++c) {
+                const uint2 two = ld_cluster32x2(r.peer(&sh.bins[turn][lo - 1], c));
+                n[0] += two.y;
+                n[1] += two.x;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w[i] = n[i] ? f(key_value(high << kLowBits | (uint32_t)(lo - i))) : 0;
+            const u64 mine = n[0] * w[0] + n[1] * w[1], upto = sum + r.block_scan(mine);
+            if (threadIdx.x == kSampleThreads - 1) sh.above = upto;
+            if (threadIdx.x == 0) sh.digit = kSampleBins;
+            __syncthreads();
+            const u64 down_to = sh.above;                 // f's sum from the lowest of these keys on
+            __syncthreads();
+            if (sum >= goal) { under = high; bias = (int64_t)((double)(sum - base) / (double)unit) - (int64_t)(above1 + above2); continue; }
+            if (down_to < goal) { over = high; base = down_to; bias = 0; continue; }
+            if (upto >= goal && upto - mine < goal) {
+                const int i = upto - n[1] * w[1] >= goal ? 0 : 1;
+                sh.digit = (uint32_t)(lo - i);
+                sh.above = upto - n[1] * w[1] - (i ? 0 : n[0] * w[0]);
+                sh.scan[0] = w[i];
+                sh.scan[1] = n[i];
+            }
+            __syncthreads();
+            e = high << kLowBits | sh.digit;
+            before = sh.above;
+            each_one = sh.scan[0];
+            members = sh.scan[1];
+            __syncthreads();
+            const u64 wanted = (goal - before + each_one - 1) / each_one;
+            int c = cut;
+            if (e != edge) c = 0x7fffffff;
+            if (wanted < members) {                       // the place of the last one wanted
+                const int place = r.running([&](int v, float x) { return (u64)(order_key(x) == e && kept(v, x)); }, [&](u64) { return wanted - 1; });
+                if (place >= 0)
+                    for (int q = 0; q < g.ctas; ++q) st_cluster(r.peer(&sh.found[r.turn], q), (uint32_t)place);
+                const int turn_now = r.turn;
+                r.sync();
+                c = sh.found[turn_now];
+                r.turn ^= 1;
             }
             edge = e;
-            cut = c + 1;
-        };
-        const int k = g.top_k ? g.top_k[row] : 0;
-        if (k > 0 && k < g.vocab) narrow(k, [](float) { return 1ull; });
-        if (p < 1.0f) {
-            const u64 all = sum([&](int i, float v) { return kept(i, v) ? weight(v) : 0ull; });
-            narrow(max(1ull, (u64)ceil((double)fmaxf(p, 0.0f) * (double)all)), weight);
+            cut = c;
+            break;
         }
-        auto stays = [&](int i, float v) { return kept(i, v) && (i == first || exact(v) >= (double)least); };
-        const u64 all = sum([&](int i, float v) { return stays(i, v) ? weight(v) : 0ull; });
-        const u64 goal = min((u64)((double)fminf(fmaxf(u, 0.0f), 1.0f) * (double)all), all - 1);
-        int c = -1;                                        // the largest index up to which no more than `goal` has come together
-        for (int bit = 30; bit >= 0; --bit) {
-            const int next = c + (1 << bit);
-            if (next < g.vocab && sum([&](int i, float v) { return i <= next && stays(i, v) ? weight(v) : 0ull; }) <= goal) c = next;
-        }
-        token = c + 1;
+    };
+    if (k > 0 && k < g.vocab) narrow((u64)k, [](float) { return 1ull; }, [](float) { return 1u; }, 1.0f);
+    if (p < 1.0f) {
+        const u64 all = r.total([&](int v, float x) { return kept(v, x) ? weight(x) : 0ull; });
+        const float units = 4.2e9f / ((float)all * 1.0001f), per = units * exp2f((float)g.shift);
+        narrow(max(p > 0.0f ? share_of(all, p, true) : 0ull, 1ull), weight,
+               [&](float x) { return x > -INFINITY ? max(1u, __float2uint_rn(fast_exp2((x - top) * coolf * 1.4426950408889634f) * per)) : 0u; }, 1.0f / units);
     }
-    if (threadIdx.x == 0) g.tokens[row] = bad ? -1 : token;
-    if (g.logprob) {
-        // The first of the order is left out of the sum: where it has nearly all of the probability, its logarithm is that of 1 + the rest.
-        double rest = 0.0;
-        for (int i = threadIdx.x; !bad && i < g.vocab; i += kSampleThreads)
-            if (i != first) rest += exp((double)to_f32(x[i]) - (double)top);
-        rest = block_reduce(rest, [](double a, double b) { return a + b; }, shd);
-        if (threadIdx.x == 0) g.logprob[row] = bad ? kNaN : (float)(((double)to_f32(x[token]) - (double)top) - log1p(rest));
-    }
+    const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
+    const int place = r.running(
+        [&](int v, float x) {
+            if (!kept(v, x)) return 0ull;
+            const u64 w = weight(x);
+            return w >= floor_w || v == first ? w : 0ull;
+        },
+        [&](u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(all, u, false) : 0ull; });
+    if (place >= 0) finish(place, to_f32(reinterpret_cast<const T*>(held)[place - r.rank * kSampleWarps * g.warp_chunks * E]));
+    if (g.ctas > 1) cluster_sync_all();
+}
+
+constexpr int kSampleMost = 196608;                       // bytes of a row that a CTA can hold
+
+template <typename T>
+int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
+    constexpr int E = 16 / (int)sizeof(T);
+    static PerDeviceOnce once;
+    const int rc = once.raise_smem_limit(sample_kernel<T>, kSampleMost + 16 * kSampleWarps);
+    if (rc != MPQ_OK) return rc;
+    const int sms = sm_count();
+    if (sms == 0) return MPQ_ERR_CUDA;
+    // As many CTAs to a row as let two share a multiprocessor, more while the device has room and a CTA 8192 elements.
+    const int64_t chunks = ceil_div((int64_t)g.vocab + E - 1, E);
+    g.ctas = 1;
+    while (g.ctas < 8 && (ceil_div(chunks, g.ctas) * 16 > 96000 || (rows * g.ctas * 2 <= sms && g.vocab / g.ctas >= 8192))) g.ctas *= 2;
+    g.warp_chunks = (int)ceil_div(chunks, g.ctas * kSampleWarps);
+    if (rows * g.ctas > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * g.ctas), 1, 1);
+    cfg.blockDim = dim3(kSampleThreads, 1, 1);
+    cfg.dynamicSmemBytes = (size_t)g.warp_chunks * kSampleWarps * 16;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)g.ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, sample_kernel<T>, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
+    return launch_status();
 }
 
 }  // namespace mpq
@@ -127,13 +530,14 @@ extern "C" int mpq_sample(const void* logits, int64_t ld, int dtype, int64_t row
                           int64_t* tokens, float* logprob, void* stream) {
     if (rows != 0 && (!logits || !uniform || !tokens)) return MPQ_ERR_NULL;
     if (rows < 0 || rows > 0x7fffffff || vocab <= 0 || (rows > 1 && ld < vocab)) return MPQ_ERR_BAD_SHAPE;
-    if (!dtype_ok(dtype) || vocab > 8 * (196608 / dtype_size(dtype))) return MPQ_ERR_UNSUPPORTED;
+    if (!dtype_ok(dtype) || vocab > 8 * (kSampleMost / dtype_size(dtype))) return MPQ_ERR_UNSUPPORTED;
     if (!aligned_to(logits, dtype_size(dtype)) || !aligned_to(temperature, 4) || !aligned_to(top_k, 4) || !aligned_to(top_p, 4) || !aligned_to(min_p, 4) ||
         !aligned_to(uniform, 4) || !aligned_to(tokens, 8) || !aligned_to(logprob, 4)) return MPQ_ERR_ALIGN;
     if (rows == 0) return MPQ_OK;
     int bits = 0;
     while ((int64_t)1 << bits < vocab) ++bits;
-    const SampleArgs g = {logits, ld, rows, (int)vocab, temperature, top_k, top_p, min_p, uniform, tokens, logprob, 62 - bits > 50 ? 50 : 62 - bits};
-    auto* kernel = dtype == MPQ_F32 ? sample_kernel<float> : dtype == MPQ_F16 ? sample_kernel<__half> : sample_kernel<__nv_bfloat16>;
-    return launch_chained_as(true, kernel, (unsigned)rows, kSampleThreads, 0, (cudaStream_t)stream, g);
+    const SampleArgs g = {logits, ld, (int)vocab, temperature, top_k, top_p, min_p, uniform, tokens, logprob, 62 - bits > 50 ? 50 : 62 - bits, 1, 0};
+    if (dtype == MPQ_F32) return launch_sample<float>(g, rows, (cudaStream_t)stream);
+    if (dtype == MPQ_F16) return launch_sample<__half>(g, rows, (cudaStream_t)stream);
+    return launch_sample<__nv_bfloat16>(g, rows, (cudaStream_t)stream);
 }
