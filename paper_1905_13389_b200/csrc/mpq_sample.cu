@@ -6,11 +6,13 @@
 // (With 32-bit weights a tail token of a flat row of 131,072 is another one in some percent of the draws.)
 //
 // A row belongs to a thread-block cluster, whose CTAs hold a share of it each in shared memory: the logits are read once,
-// and every further look at them is at the shares.  Nothing is sorted.  The end of top-k and of top-p is a key (the
-// logit's bits in their order) and a place among its equals: two passes count, by 11 bits of the key each, where the
-// border lies -- exactly for top-k, with rounded weights for top-p --, and a third one takes the exact sum of all that
-// lies above the 2^10 keys found and counts their members; equals have equal weights, so count times weight is exact.
-// Where rounding had led astray the search goes on from there, on the right side.
+// and every further look at them is at the shares.  Nothing is sorted.  Where top-k or top-p ends is found in two steps.
+// Counts by distance from the largest logit, in 2048 steps of 1/64, say how far the kept ones can reach at most; those
+// that lie there are noted in a list, and the rest is not looked at again.  The end itself is a key (the logit's bits in
+// their order) and a place among its equals: two passes count by 11 bits of the key each -- exactly for top-k, with rounded
+// weights for top-p --, and a third takes the exact sum of all above the 2^10 keys found and counts their
+// members; equals have equal weights, so count times weight is exact.  Where rounding had led astray the search goes on from
+// there, on the right side.  What the list cannot hold is searched in the shares themselves, the same way.
 #include "mpq_attention.cuh"
 #include "mpq_tensor.cuh"
 
@@ -29,6 +31,7 @@ struct SampleArgs {
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleBins = 2048, kLowBits = 10;          // 11 + 11 + 10 bits of a key
+constexpr int kSampleList = 512;                          // elements of a warp's share that its list holds
 
 // Whole numbers in the order of the logits; -0 and 0 are the same number.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -73,24 +76,74 @@ struct SampleShared {
     u64 parts[2][kSampleWarps];
     uint32_t bins[2][kSampleBins];
     u64 scan[kSampleWarps];
-    double powers[16];                                    // 2^(i / 16): sixteen, so that lanes never ask one bank for two of them
+    double powers[16];                                    // 2^(i / 16 + shift): sixteen, so that lanes never ask one bank for two of them
     int found[2];
     uint32_t digit, digit_before;
-    u64 above;
+    u64 above, weight, members;
+    uint16_t list[kSampleWarps][kSampleList];             // places in a warp's share, ascending
+};
+
+// The largest element of a chunk, NaN if one is.
+__device__ __forceinline__ float chunk_max(const uint4& r, const float*) {
+    return max_nan(max_nan(__uint_as_float(r.x), __uint_as_float(r.y)), max_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
+}
+template <typename T, typename Two>
+__device__ __forceinline__ float chunk_max_pairs(const uint4& r) {
+    const Two* e = reinterpret_cast<const Two*>(&r);
+    const Two m = __hmax2_nan(__hmax2_nan(e[0], e[1]), __hmax2_nan(e[2], e[3]));
+    return max_nan(to_f32(m.x), to_f32(m.y));
+}
+__device__ __forceinline__ float chunk_max(const uint4& r, const __half*) { return chunk_max_pairs<__half, __half2>(r); }
+__device__ __forceinline__ float chunk_max(const uint4& r, const __nv_bfloat16*) { return chunk_max_pairs<__nv_bfloat16, __nv_bfloat162>(r); }
+
+// exp((x - top) / warm) 2^shift, rounded: 2^(t / 16) with t = n + f is 2^(n / 16) from the table and the exponent, times
+// the series of 2^(f / 16), |f| <= 1/2, off by 2^-42 of itself at most.
+struct SampleWeight {
+    float top, coolf, gone;                               // gone: where a weight is less than one multiple
+    double dtop, cool;
+    const double* powers;
+    static constexpr u64 kBias = 0x433ull << 52;          // 2^52: on top of it, the low bits of a number are its whole part
+
+    __device__ SampleWeight(float largest, float warm, int shift, const double* table)
+        : top(largest), coolf(1.0f / warm), gone(-0.69314718f * (float)shift), dtop(largest), cool(16.0 * 1.4426950408889634073599 / (double)warm), powers(table) {}
+    __device__ __forceinline__ u64 biased(float x) const {
+        constexpr double kMagic = 6755399441055744.0;     // 1.5 2^52: on top of it, the low bits are the nearest whole number
+        constexpr double kLog = 0.69314718055994530942 / 16;
+        const double d = (double)x - dtop, m = fma(d, cool, kMagic), f = fma(d, cool, -(m - kMagic));
+        const int n = __double2loint(m);
+        const double a = powers[n & 15];
+        double q = fma(f, kLog * kLog * kLog * kLog * kLog / 120, kLog * kLog * kLog * kLog / 24);
+        q = fma(f, q, kLog * kLog * kLog / 6);
+        q = fma(f, q, kLog * kLog / 2);
+        q = fma(f, q, kLog);
+        const double scaled = __hiloint2double(__double2hiint(a) + (n & ~15) * 65536, __double2loint(a));
+        return (u64)__double_as_longlong(fma(scaled * f, q, scaled) + 4503599627370496.0);
+    }
+    __device__ __forceinline__ bool small(float x) const { return (x - top) * coolf < gone; }
+    // What is less than one multiple weighs one, so that every token over -infinity can be drawn.
+    __device__ __forceinline__ u64 operator()(float x) const {
+        u64 w = 1;
+        if (!small(x)) w = biased(x) - kBias;
+        return x > -INFINITY ? w : 0ull;
+    }
 };
 
 template <typename T>
 struct SampleRow {
     static constexpr int E = 16 / (int)sizeof(T);         // elements of a chunk
     SampleShared& sh;
-    uint4* data;
+    uint4* chunks;                                        // this warp's share
     const int ctas, rank, warp, lane, warp_chunks;
-    const int v0;                                         // place of this warp's first element; places count from the 16-byte boundary before the row
+    const int v0;                                         // place of its first element; places count from the 16-byte boundary before the row
     int turn = 0;                                         // which of the two exchange buffers comes next
+    bool listed = false;                                  // whether the list has all that can still be kept, and how much that is
+    int count;
 
-    __device__ SampleRow(SampleShared& s, uint4* d, const SampleArgs& g)
-        : sh(s), data(d), ctas(g.ctas), rank(g.ctas > 1 ? (int)cluster_rank() : 0), warp(__shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0)), lane(threadIdx.x & 31),
-          warp_chunks(g.warp_chunks), v0((rank * kSampleWarps + warp) * g.warp_chunks * E) {}
+    __device__ SampleRow(SampleShared& s, uint4* data, const SampleArgs& g)
+        : sh(s), ctas(g.ctas), rank(g.ctas > 1 ? (int)cluster_rank() : 0), warp(__shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0)), lane(threadIdx.x & 31),
+          warp_chunks(g.warp_chunks), v0((rank * kSampleWarps + warp) * g.warp_chunks * E), count(g.warp_chunks * E) {
+        chunks = data + warp * warp_chunks;
+    }
 
     __device__ __forceinline__ void sync() {
         if (ctas > 1) cluster_sync_all();
@@ -103,17 +156,31 @@ struct SampleRow {
 #pragma unroll
         for (int i = 0; i < E; ++i) x[i] = to_f32(e[i]);
     }
-    // f(place, value) for this lane's elements, in whole warps: places of a warp ascend with the step, then the lane.
+    // f(place of the first, values) for this lane's chunks of the whole share.
+    template <typename F>
+    __device__ __forceinline__ void each_chunk(F f) const {
+#pragma unroll 1
+        for (int c = lane; c < warp_chunks; c += 32) {
+            float x[E];
+            unpack(chunks[c], x);
+            f(v0 + c * E, x);
+        }
+    }
+    // Element i of what is still looked at in the share of warp w of this CTA.
+    __device__ __forceinline__ void element(int w, int i, int& place, float& x) const {
+        const int at = listed ? sh.list[w][i] : i;
+        place = v0 + (w - warp) * warp_chunks * E + at;
+        x = to_f32(reinterpret_cast<const T*>(chunks + (w - warp) * warp_chunks)[at]);
+    }
+    // f(place, value) for what is still looked at, in ascending places of the warp.
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        for (int c0 = 0; c0 < warp_chunks; c0 += 32) {
-            const int c = c0 + lane;
-            if (c < warp_chunks) {
-                float x[E];
-                unpack(data[warp * warp_chunks + c], x);
-#pragma unroll
-                for (int i = 0; i < E; ++i) f(v0 + c * E + i, x[i]);
-            }
+#pragma unroll 1
+        for (int i = lane; i < count; i += 32) {
+            int place;
+            float x;
+            element(warp, i, place, x);
+            f(place, x);
         }
     }
 
@@ -133,28 +200,65 @@ struct SampleRow {
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         return s;
     }
-    template <typename F>
-    __device__ __forceinline__ u64 total(F f) {
-        u64 s = 0, v[4];
-        each([&](int place, float x) { s += f(place, x); });
+    __device__ __forceinline__ u64 warp_scan(u64 x) const {
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 below = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += below;
+        }
+        return x;
+    }
+    __device__ __forceinline__ u64 block_scan(u64 x) {
+        x = warp_scan(x);
+        if (lane == 31) sh.scan[warp] = x;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) x += sh.scan[w];
+        __syncthreads();
+        return x;
+    }
+    __device__ __forceinline__ u64 row_sum(u64 s) {
+        u64 v[4];
         gather(warp_sum(s), v);
         return warp_sum(v[0] + v[1] + v[2] + v[3]);
     }
+    // Sum of f over what is still looked at.
+    template <typename F>
+    __device__ __forceinline__ u64 sum(F f) const {
+        u64 s = 0;
+        each([&](int place, float x) { s += f(place, x); });
+        return s;
+    }
+    // Sum of the weights of the whole share.
+    __device__ __forceinline__ u64 sum_all(const SampleWeight& weight) const {
+        u64 s = 0;
+        each_chunk([&](int, const float (&x)[E]) {
+            float low = x[0];
+#pragma unroll
+            for (int i = 1; i < E; ++i) low = fminf(low, x[i]);
+            if (!weight.small(low) && low > -INFINITY) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) s += weight.biased(x[i]);
+                s -= E * SampleWeight::kBias;             // (modulo 2^64)
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < E; ++i) {
+                    float one = x[0];
+#pragma unroll
+                    for (int j = 1; j < E; ++j) one = i == j ? x[j] : one;
+                    s += weight(one);
+                }
+            }
+        });
+        return s;
+    }
 
     // The lowest place at which the running sum of f exceeds goal(sum of all), in the one thread that finds it (-1 elsewhere).
+    // `s`: this thread's part of the sum of f over its warp.  The warp in whose share it lies is found first, then that
+    // share is gone through by all warps of its CTA, a sixteenth each, then a sixteenth by one warp.
     template <typename F, typename Goal>
-    __device__ __forceinline__ int running(F f, Goal goal_of) {
-        u64 s = 0, v[4];
-        each([&](int place, float x) { s += f(place, x); });
+    __device__ __forceinline__ int running(u64 s, F f, Goal goal_of) {
+        u64 v[4];
         gather(warp_sum(s), v);
-        auto scan = [&](u64 x) {
-            for (int o = 1; o < 32; o <<= 1) {
-                const u64 below = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += below;
-            }
-            return x;
-        };
-        const u64 here = v[0] + v[1] + v[2] + v[3], upto = scan(here), all = __shfl_sync(0xffffffffu, upto, 31), goal = goal_of(all);
+        const u64 here = v[0] + v[1] + v[2] + v[3], upto = warp_scan(here), all = __shfl_sync(0xffffffffu, upto, 31), goal = goal_of(all);
         const int in = __ffs(__ballot_sync(0xffffffffu, upto > goal)) - 1;      // the lane that holds the warp in question
         if (in < 0) return -1;
         u64 before = upto - here;
@@ -164,35 +268,51 @@ struct SampleRow {
             if (which == lane * 4 + i && before + v[i] <= goal) { before += v[i]; ++which; }
         which = __shfl_sync(0xffffffffu, which, in);
         before = __shfl_sync(0xffffffffu, before, in);
-        if (which != rank * kSampleWarps + warp) return -1;
-        for (int c0 = 0; c0 < warp_chunks; c0 += 32) {
-            const int c = c0 + lane;
-            float x[E];
-            u64 w[E], mine = 0;
-            if (c < warp_chunks) unpack(data[warp * warp_chunks + c], x);
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                w[i] = c < warp_chunks ? f(v0 + c * E + i, x[i]) : 0;
-                mine += w[i];
+        if (which / kSampleWarps != rank) return -1;
+        which %= kSampleWarps;
+        if (lane == 0 && warp == which) sh.found[0] = count;
+        __syncthreads();
+        const int n = sh.found[0], per = ((n + kSampleWarps - 1) / kSampleWarps + 31) / 32 * 32, from = min(n, warp * per), to = min(n, from + per);
+        u64 part = 0;
+#pragma unroll 1
+        for (int i = from + lane; i < to; i += 32) {
+            int place;
+            float x;
+            element(which, i, place, x);
+            part += f(place, x);
+        }
+        part = warp_sum(part);
+        if (lane == 0) sh.scan[warp] = part;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) before += sh.scan[w];
+        if (before > goal || before + part <= goal) return -1;
+#pragma unroll 1
+        for (int i0 = from; i0 < to; i0 += 32) {
+            int place = 0;
+            float x = 0.0f;
+            u64 w = 0;
+            if (i0 + lane < to) {
+                element(which, i0 + lane, place, x);
+                w = f(place, x);
             }
-            const u64 to = before + scan(mine);
-            const int hit = __ffs(__ballot_sync(0xffffffffu, to > goal)) - 1;
-            if (hit >= 0) {
-                if (lane != hit) return -1;
-                u64 sum = to - mine;
-                for (int i = 0; i < E; ++i) {
-                    sum += w[i];
-                    if (sum > goal) return v0 + c * E + i;
-                }
-            }
-            before = __shfl_sync(0xffffffffu, to, 31);
+            const u64 sum_to = before + warp_scan(w);
+            const uint32_t over = __ballot_sync(0xffffffffu, sum_to > goal);
+            if (over) return lane == __ffs(over) - 1 ? place : -1;
+            before = __shfl_sync(0xffffffffu, sum_to, 31);
         }
         return -1;
     }
 
-    // Adds up what the CTAs have counted by `bins` and finds, from the highest bin down, the one in which the sum reaches goal
-    // (the lowest that has anything, if none does); `above` is the sum before it.
-    __device__ __forceinline__ void border(u64 goal, uint32_t& digit, u64& above) {
+    __device__ __forceinline__ uint32_t* clear_bins() {
+        uint32_t* bins = sh.bins[turn];
+        for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) bins[i] = 0;
+        __syncthreads();
+        return bins;
+    }
+    // Adds up what the CTAs have counted by `bins`, worth(bin, count), and finds, from the highest bin down, the one in which the
+    // sum reaches goal (the lowest that has anything, if none does); `above` is the sum before it.
+    template <typename Worth>
+    __device__ __forceinline__ void border(u64 goal, Worth worth, uint32_t& digit, u64& above) {
         sync();
         constexpr int kPer = kSampleBins / kSampleThreads;
         const int hi = kSampleBins - 1 - (int)threadIdx.x * kPer;          // this thread's bins: hi, hi - 1, ..
@@ -209,6 +329,7 @@ struct SampleRow {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             if (n[i]) { lowest = hi - i; over_lowest = mine; }
+            n[i] = worth(hi - i, n[i]);
             mine += n[i];
         }
         const u64 upto = block_scan(mine);
@@ -232,22 +353,54 @@ struct SampleRow {
         above = sh.above;
         turn ^= 1;
     }
-    __device__ __forceinline__ u64 block_scan(u64 x) {
-        for (int o = 1; o < 32; o <<= 1) {
-            const u64 below = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += below;
+
+    // Notes in the lists what can lie among the first of the order whose worth(bin, count) comes to goal: bins of 1 / steps by the
+    // distance from `top`, the last one for all beyond.  False: a list cannot hold it.
+    template <typename Worth>
+    __device__ __forceinline__ bool shorten(float top, float steps, u64 goal, Worth worth) {
+        auto bin = [&](float x) { return kSampleBins - 1 - (__float_as_uint(fminf((top - x) * steps, (float)(kSampleBins - 1)) + 8388608.0f) & (kSampleBins - 1)); };
+        uint32_t* bins = clear_bins();
+        each_chunk([&](int, const float (&x)[E]) {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (x[i] > -INFINITY) atomicAdd(bins + bin(x[i]), 1u);
+        });
+        uint32_t digit;
+        u64 above;
+        border(goal, worth, digit, above);
+        int have = 0;
+#pragma unroll 1
+        for (int c0 = 0; c0 < warp_chunks; c0 += 32) {
+            const int c = c0 + lane;
+            uint32_t in = 0;
+            if (c < warp_chunks) {
+                float x[E];
+                unpack(chunks[c], x);
+#pragma unroll
+                for (int i = 0; i < E; ++i) if (x[i] > -INFINITY && bin(x[i]) >= digit) in |= 1u << i;
+            }
+            if (!__any_sync(0xffffffffu, in)) continue;
+            int at = __popc(in);
+            for (int o = 1; o < 32; o <<= 1) {
+                const int below = __shfl_up_sync(0xffffffffu, at, o);
+                if (lane >= o) at += below;
+            }
+            const int more = __shfl_sync(0xffffffffu, at, 31);
+            at += have - __popc(in);
+            for (; in && at < kSampleList; in &= in - 1) sh.list[warp][at++] = (uint16_t)(c * E + __ffs(in) - 1);
+            have += more;
         }
-        if (lane == 31) sh.scan[warp] = x;
-        __syncthreads();
-        for (int w = 0; w < warp; ++w) x += sh.scan[w];
-        __syncthreads();
-        return x;
+        __syncwarp();
+        u64 v[4];
+        gather(have > kSampleList, v);
+        if (__any_sync(0xffffffffu, (v[0] | v[1] | v[2] | v[3]) != 0)) return false;
+        listed = true;
+        count = have;
+        return true;
     }
-    __device__ __forceinline__ uint32_t* clear_bins() {
-        uint32_t* bins = sh.bins[turn];
-        for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) bins[i] = 0;
-        __syncthreads();
-        return bins;
+    __device__ __forceinline__ void forget_list() {
+        listed = false;
+        count = warp_chunks * E;
     }
 };
 
@@ -257,8 +410,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     __shared__ SampleShared sh;
     constexpr int E = SampleRow<T>::E;
     SampleRow<T> r(sh, held, g);
-    const int warp = r.warp, lane = r.lane;
-    if (threadIdx.x < 16) sh.powers[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+    const int lane = r.lane;
+    if (threadIdx.x < 16) sh.powers[threadIdx.x] = exp2((double)threadIdx.x / 16.0 + (double)g.shift);
     chain_entry();
     const int64_t row = blockIdx.x / g.ctas;
     const T* x0 = static_cast<const T*>(g.logits) + row * g.ld;
@@ -272,12 +425,12 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     int best_chunk = 0;
     bool nan = false;
     constexpr int kLoads = 4;
+#pragma unroll 1
     for (int c0 = 0; c0 < g.warp_chunks; c0 += 32 * kLoads) {
         uint4 in[kLoads];
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int c = c0 + 32 * j + lane;
-            const int64_t i = (int64_t)r.v0 + c * E - skew;
+            const int c = c0 + 32 * j + lane, i = r.v0 + c * E - skew;
             if (c < g.warp_chunks && i >= 0 && i + E <= g.vocab) {
                 in[j] = __ldg(reinterpret_cast<const uint4*>(x0 + i));
             } else {
@@ -289,18 +442,19 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int c = c0 + 32 * j + lane;
-            if (c < g.warp_chunks) held[warp * g.warp_chunks + c] = in[j];
-            float x[E], top = -INFINITY;
-            SampleRow<T>::unpack(in[j], x);
-#pragma unroll
-            for (int q = 0; q < E; ++q) { nan |= x[q] != x[q]; top = fmaxf(top, x[q]); }
-            if (top > best) { best = top; best_chunk = c; }
+            if (c < g.warp_chunks) r.chunks[c] = in[j];
+            const float top = chunk_max(in[j], static_cast<const T*>(nullptr));
+            if (!(top <= best)) {
+                nan |= top != top;
+                best = top;
+                best_chunk = c;
+            }
         }
     }
     u64 code = 0;                                         // 0: nothing over -infinity; all ones: a NaN
     if (best > -INFINITY) {
         float x[E];
-        SampleRow<T>::unpack(held[warp * g.warp_chunks + best_chunk], x);
+        SampleRow<T>::unpack(r.chunks[best_chunk], x);
         int at = E - 1;
 #pragma unroll
         for (int q = E - 1; q >= 0; --q) if (x[q] == best) at = q;
@@ -328,14 +482,20 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     }
 
     // What the others weigh together, the first one's weight being 1: where it has nearly all of the probability its
-    // logarithm is -log(1 + rest).  32 bits: a term is off by
-    // (2 |d| + 4) 2^-24 of itself at most, d its distance from the first.
+    // logarithm is -log(1 + rest).  32 bits: a term is off by (2.5 |d| + 4) 2^-24 of itself at most, d its distance from the first.
     double rest = 0.0;
     if (g.logprob) {
         float some = 0.0f;
-        r.each([&](int v, float x) {
-            const float e = fast_exp2((x - top) * 1.4426950408889634f);
-            some += v != first ? e : 0.0f;
+        r.each_chunk([&](int v, const float (&x)[E]) {
+            float e[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) e[i] = fast_exp2((x[i] - top) * 1.4426950408889634f);
+            if ((unsigned)(first - v) < (unsigned)E) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) if (v + i == first) e[i] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) some += e[i];
         });
         rest = some;
         for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
@@ -354,75 +514,52 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         return;
     }
 
-    // exp((x - top) / warm) 2^shift, rounded: 2^(t / 16) with t = n + f is 2^(n / 16) from the table and shifts, times the
-    // series of 2^(f / 16), |f| <= 1/2, off by 2^-42 of itself.  What is less than one multiple weighs one, so that
-    // every token over -infinity can be drawn.
-    const double cool = 16.0 * 1.4426950408889634073599 / (double)warm;
-    const float coolf = 1.0f / warm, gone = -0.69314718f * (float)g.shift;
-    const double dtop = (double)top;
-    constexpr double kMagic = 6755399441055744.0;         // 1.5 2^52: its low bits are whole numbers
-    auto weight = [&](float x) -> u64 {
-        u64 w = 1;
-        if (!((x - top) * coolf < gone)) {
-            const double t = ((double)x - dtop) * cool, m = t + kMagic, f = t - (m - kMagic);
-            const int n = __double2loint(m);
-            const double a = sh.powers[n & 15];
-            constexpr double kLog = 0.69314718055994530942 / 16;
-            double q = fma(f, kLog * kLog * kLog * kLog * kLog / 120, kLog * kLog * kLog * kLog / 24);
-            q = fma(f, q, kLog * kLog * kLog / 6);
-            q = fma(f, q, kLog * kLog / 2);
-            q = fma(f, q, kLog);
-            const double scaled = __hiloint2double(__double2hiint(a) + (((n >> 4) + g.shift) << 20), __double2loint(a));
-            // below 2^51: on top of 2^52 its low bits are the rounded number
-            w = (u64)__double_as_longlong(fma(scaled * f, q, scaled) + 4503599627370496.0) & ((1ull << 52) - 1);
-        }
-        return x > -INFINITY ? w : 0ull;
-    };
+    const SampleWeight weight(top, warm, g.shift, sh.powers);
     // kept: keys over `edge`, and those equal to it up to place `cut`
     uint32_t edge = 0;
     int cut = 0x7fffffff;
     auto kept = [&](int v, float x) { const uint32_t key = order_key(x); return key > edge || (key == edge && v <= cut); };
-    // The keys, and the place among the equals of the last one, at which the sum of f from the top reaches `goal`: edge and cut.
-    // guess: f, or something near it in 32 bits of which the whole row's sum fits 32 bits, in units of `unit` of f's.
+    // The key, and the place among the equals of it, at which the sum of f from the top reaches `goal`: edge and cut.
+    // guess: f, or something near it in 32 bits, one at least, of which the whole row's sum fits 32 bits, in units of `unit` of f's.
     auto narrow = [&](u64 goal, auto f, auto guess, float unit) {
         uint32_t over = 1u << (32 - kLowBits), under = 0xffffffffu;        // the border lies below `over` and above `under` (key >> kLowBits)
         u64 base = 0;                                     // f's sum from `over` on
-        uint32_t e;
-        u64 before, each_one, members;
         int64_t bias = 0;                                 // by how much the guesses above `under` fall short
+        auto as_counted = [](uint32_t, u64 n) { return n; };
         for (;;) {                                        // (each turn takes at least one occupied key off the open ones)
             auto open = [&](uint32_t key) { const uint32_t high = key >> kLowBits; return high < over && (under == 0xffffffffu || high > under); };
-            u64 above1, above2;
             const u64 want = (u64)max((int64_t)((double)(goal - base) / (double)unit) - bias, (int64_t)1);
-            uint32_t high, low;
-            uint32_t* bins = r.clear_bins();
-            r.each([&](int v, float x) {
-                const uint32_t key = order_key(x);
-                if (open(key) && kept(v, x)) { const uint32_t n = guess(x); if (n) atomicAdd(bins + (key >> 21), n); }
-            });
-            r.border(want, high, above1);
-            bins = r.clear_bins();
-            r.each([&](int v, float x) {
-                const uint32_t key = order_key(x);
-                if (key >> 21 == high && open(key) && kept(v, x)) { const uint32_t n = guess(x); if (n) atomicAdd(bins + (key >> kLowBits & 2047), n); }
-            });
-            r.border(want > above1 ? want - above1 : 1, low, above2);
-            high = min(high << 11 | low, (1u << (32 - kLowBits)) - 1);
+            u64 above1 = 0, above2 = 0;
+            uint32_t high = 0;
+#pragma unroll 1
+            for (int level = 0; level < 2; ++level) {
+                uint32_t* bins = r.clear_bins();
+                r.each([&](int v, float x) {
+                    const uint32_t key = order_key(x);
+                    if ((level == 0 || key >> 21 == high) && open(key) && kept(v, x)) {
+                        const uint32_t n = guess(x);
+                        if (n) atomicAdd(bins + (level ? key >> kLowBits & (kSampleBins - 1) : key >> 21), n);
+                    }
+                });
+                uint32_t digit;
+                above1 += above2;
+                r.border(want > above1 ? want - above1 : 1, as_counted, digit, above2);
+                high = level ? high << 11 | digit : digit;
+            }
+            high = min(high, (1u << (32 - kLowBits)) - 1);
             // exactly: what lies above, and how many have each of the keys found
-            bins = r.clear_bins();
+            uint32_t* bins = r.clear_bins();
             u64 s = 0;
             r.each([&](int v, float x) {
                 const uint32_t key = order_key(x);
                 if (key >> kLowBits >= high && kept(v, x)) {
-                    if (key >> kLowBits == high) atomicAdd(bins + (key & 1023), 1u);
+                    if (key >> kLowBits == high) atomicAdd(bins + (key & ((1 << kLowBits) - 1)), 1u);
                     else s += f(x);
                 }
             });
-            u64 v[4];
             const int turn = r.turn;
-            r.gather(SampleRow<T>::warp_sum(s), v);
-            const u64 sum = SampleRow<T>::warp_sum(v[0] + v[1] + v[2] + v[3]);
-            const int lo = 1023 - 2 * (int)threadIdx.x;   // this thread's keys: lo, lo - 1
+            const u64 sum = r.row_sum(s);
+            const int lo = (1 << kLowBits) - 1 - 2 * (int)threadIdx.x;     // this thread's keys: lo, lo - 1
             u64 n[2] = {0, 0}, w[2];
             for (int c = 0; c < g.ctas; ++c) {
                 const uint2 two = ld_cluster32x2(r.peer(&sh.bins[turn][lo - 1], c));
@@ -433,7 +570,6 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             for (int i = 0; i < 2; ++i) w[i] = n[i] ? f(key_value(high << kLowBits | (uint32_t)(lo - i))) : 0;
             const u64 mine = n[0] * w[0] + n[1] * w[1], upto = sum + r.block_scan(mine);
             if (threadIdx.x == kSampleThreads - 1) sh.above = upto;
-            if (threadIdx.x == 0) sh.digit = kSampleBins;
             __syncthreads();
             const u64 down_to = sh.above;                 // f's sum from the lowest of these keys on
             __syncthreads();
@@ -443,47 +579,58 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                 const int i = upto - n[1] * w[1] >= goal ? 0 : 1;
                 sh.digit = (uint32_t)(lo - i);
                 sh.above = upto - n[1] * w[1] - (i ? 0 : n[0] * w[0]);
-                sh.scan[0] = w[i];
-                sh.scan[1] = n[i];
+                sh.weight = w[i];
+                sh.members = n[i];
             }
             __syncthreads();
-            e = high << kLowBits | sh.digit;
-            before = sh.above;
-            each_one = sh.scan[0];
-            members = sh.scan[1];
-            __syncthreads();
-            const u64 wanted = (goal - before + each_one - 1) / each_one;
-            int c = cut;
-            if (e != edge) c = 0x7fffffff;
-            if (wanted < members) {                       // the place of the last one wanted
-                const int place = r.running([&](int v, float x) { return (u64)(order_key(x) == e && kept(v, x)); }, [&](u64) { return wanted - 1; });
+            const uint32_t e = high << kLowBits | sh.digit;
+            const u64 wanted = (goal - sh.above + sh.weight - 1) / sh.weight;
+            int c = e == edge ? cut : 0x7fffffff;
+            if (wanted < sh.members) {                    // the place of the last one wanted
+                auto equal = [&](int v, float x) { return (u64)(order_key(x) == e && kept(v, x)); };
+                const int place = r.running(r.sum(equal), equal, [&](u64) { return wanted - 1; });
                 if (place >= 0)
-                    for (int q = 0; q < g.ctas; ++q) st_cluster(r.peer(&sh.found[r.turn], q), (uint32_t)place);
-                const int turn_now = r.turn;
+                    for (int q = 0; q < g.ctas; ++q) st_cluster(r.peer(&sh.found[1], q), (uint32_t)place);
                 r.sync();
-                c = sh.found[turn_now];
+                c = sh.found[1];
                 r.turn ^= 1;
             }
             edge = e;
             cut = c;
+            __syncthreads();
             break;
         }
     };
-    if (k > 0 && k < g.vocab) narrow((u64)k, [](float) { return 1ull; }, [](float) { return 1u; }, 1.0f);
+    auto one = [](float) { return 1ull; };
+    const bool some = k > 0 && k < g.vocab;
+    if (some) {
+        const u64 goal = (u64)k;
+        bool all_of_them = false;
+        if (r.shorten(top, 64.0f, goal, [](uint32_t, u64 n) { return n; })) all_of_them = r.row_sum(r.sum([](int, float) { return 1ull; })) <= goal;
+        if (!all_of_them) narrow(goal, one, [](float) { return 1u; }, 1.0f);
+    }
     if (p < 1.0f) {
-        const u64 all = r.total([&](int v, float x) { return kept(v, x) ? weight(x) : 0ull; });
+        const u64 all = r.row_sum(some ? r.sum([&](int v, float x) { return kept(v, x) ? weight(x) : 0ull; }) : r.sum_all(weight));
+        const u64 goal = max(p > 0.0f ? share_of(all, p, true) : 0ull, 1ull);
+        if (!some) {                                      // a thousandth more than the goal, since the bins' weights are those of their middles
+            const float unit = exp2f((float)g.shift);
+            auto worth = [&](uint32_t bin, u64 n) { return bin == 0 ? 0ull : (u64)((float)n * (fast_exp2(((float)bin - (float)(kSampleBins - 1)) * (1.4426950408889634f / 64.0f)) * unit)); };
+            if (r.shorten(top, fminf(weight.coolf, 1e30f) * 64.0f, goal + (all >> 10), worth) &&
+                r.row_sum(r.sum([&](int, float x) { return weight(x); })) < goal) r.forget_list();
+        }
         const float units = 4.2e9f / ((float)all * 1.0001f), per = units * exp2f((float)g.shift);
-        narrow(max(p > 0.0f ? share_of(all, p, true) : 0ull, 1ull), weight,
-               [&](float x) { return x > -INFINITY ? max(1u, __float2uint_rn(fast_exp2((x - top) * coolf * 1.4426950408889634f) * per)) : 0u; }, 1.0f / units);
+        narrow(goal, weight,
+               [&](float x) { return x > -INFINITY ? max(1u, __float2uint_rn(fast_exp2((x - top) * weight.coolf * 1.4426950408889634f) * per)) : 0u; }, 1.0f / units);
     }
     const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
-    const int place = r.running(
-        [&](int v, float x) {
-            if (!kept(v, x)) return 0ull;
-            const u64 w = weight(x);
-            return w >= floor_w || v == first ? w : 0ull;
-        },
-        [&](u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(all, u, false) : 0ull; });
+    auto stays = [&](int v, float x) {
+        if (!kept(v, x)) return 0ull;
+        const u64 w = weight(x);
+        return w >= floor_w || v == first ? w : 0ull;
+    };
+    const bool all_stay = !some && !(p < 1.0f) && floor_w <= 1;
+    const int place = r.running(all_stay ? r.sum_all(weight) : r.sum(stays), stays,
+                                [&](u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(all, u, false) : 0ull; });
     if (place >= 0) finish(place, to_f32(reinterpret_cast<const T*>(held)[place - r.rank * kSampleWarps * g.warp_chunks * E]));
     if (g.ctas > 1) cluster_sync_all();
 }
@@ -501,7 +648,7 @@ int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
     // As many CTAs to a row as let two share a multiprocessor, more while the device has room and a CTA 8192 elements.
     const int64_t chunks = ceil_div((int64_t)g.vocab + E - 1, E);
     g.ctas = 1;
-    while (g.ctas < 8 && (ceil_div(chunks, g.ctas) * 16 > 96000 || (rows * g.ctas * 2 <= sms && g.vocab / g.ctas >= 8192))) g.ctas *= 2;
+    while (g.ctas < 8 && (ceil_div(chunks, g.ctas) * 16 > 80000 || (rows * g.ctas * 2 <= sms && g.vocab / g.ctas >= 8192))) g.ctas *= 2;
     g.warp_chunks = (int)ceil_div(chunks, g.ctas * kSampleWarps);
     if (rows * g.ctas > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
     cudaLaunchConfig_t cfg = {};
