@@ -31,7 +31,9 @@ struct SampleArgs {
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleBins = 2048, kLowBits = 10;          // 11 + 11 + 10 bits of a key
-constexpr int kSampleList = 512;                          // elements of a warp's share that its list holds
+constexpr int kSampleGroups = kSampleBins / 32;
+constexpr int kSampleOwn = 4, kSampleMembers = 1024;      // members that a thread holds, and a CTA hands out
+constexpr int kSampleList = 480;                          // elements of a warp's share that its list holds
 
 // Whole numbers in the order of the logits; -0 and 0 are the same number.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -79,7 +81,13 @@ struct SampleShared {
     double powers[16];                                    // 2^(i / 16 + shift): sixteen, so that lanes never ask one bank for two of them
     int found[2];
     uint32_t digit, digit_before;
-    u64 above, weight, members;
+    u64 above, above_to, weight, members;
+    u64 coarse[2][2][kSampleGroups];                      // what groups of 32 bins are worth, and their counts
+    uint32_t counts[2];                                   // of the bins down to a border, and of its own bin
+    int noted[2], longest;                                // members a CTA hands out; elements of the longest list
+    double rest[kSampleWarps];
+    u64 sums[2][3][kSampleWarps];
+    uint32_t differ[2];
     uint16_t list[kSampleWarps][kSampleList];             // places in a warp's share, ascending
 };
 
@@ -310,64 +318,67 @@ struct SampleRow {
         return bins;
     }
     // Adds up what the CTAs have counted by `bins`, worth(bin, count), and finds, from the highest bin down, the one in which the
-    // sum reaches goal (the lowest that has anything, if none does); `above` is the sum before it.
-    template <typename Worth>
-    __device__ __forceinline__ void border(u64 goal, Worth worth, uint32_t& digit, u64& above) {
+    // sum reaches goal() (the lowest that has anything, if none does); `above` is the sum before it.  Groups of 32 bins are
+    // summed by each CTA and looked at first, so that little passes between the CTAs.
+    template <typename Worth, typename Goal>
+    __device__ __forceinline__ void border(Goal goal_of, Worth worth, uint32_t& digit, u64& above) {
+        __syncthreads();
+        for (int i = warp; i < kSampleGroups; i += kSampleWarps) {
+            const u64 n = sh.bins[turn][i * 32 + lane], value = warp_sum(worth(i * 32 + lane, n)), all = warp_sum(n);
+            if (lane == 0) { sh.coarse[turn][0][i] = value; sh.coarse[turn][1][i] = all; }
+        }
         sync();
-        constexpr int kPer = kSampleBins / kSampleThreads;
-        const int hi = kSampleBins - 1 - (int)threadIdx.x * kPer;          // this thread's bins: hi, hi - 1, ..
-        u64 n[kPer] = {};
+        const u64 goal = goal_of();
+        if (warp == 0) {
+            // two groups a lane, the highest first
+            u64 value[2] = {}, n[2] = {};
+            for (int c = 0; c < ctas; ++c)
 #pragma unroll
-        for (int i = 0; i < kPer; i += 2)
-            for (int c = 0; c < ctas; ++c) {
-                const uint2 two = ld_cluster32x2(peer(&sh.bins[turn][hi - i - 1], c));
-                n[i] += two.y;
-                n[i + 1] += two.x;
+                for (int i = 0; i < 2; ++i) {
+                    const int group = kSampleGroups - 1 - 2 * lane - i;
+                    value[i] += ld_cluster64(peer(&sh.coarse[turn][0][group], c));
+                    n[i] += ld_cluster64(peer(&sh.coarse[turn][1][group], c));
+                }
+            const u64 to = warp_scan(value[0] + value[1]), n_to = warp_scan(n[0] + n[1]);
+            const uint32_t reach = __ballot_sync(0xffffffffu, to >= goal), any = __ballot_sync(0xffffffffu, (n[0] | n[1]) != 0);
+            const int in = reach ? __ffs(reach) - 1 : 31 - __clz(any);      // something has been counted
+            const bool second = reach ? to - value[1] < goal : n[1] != 0;
+            const int group = __shfl_sync(0xffffffffu, kSampleGroups - 1 - 2 * lane - (second ? 1 : 0), in);
+            const u64 before = __shfl_sync(0xffffffffu, to - value[1] - (second ? 0 : value[0]), in);
+            const u64 n_before = __shfl_sync(0xffffffffu, n_to - n[1] - (second ? 0 : n[0]), in);
+            const int bin = group * 32 + 31 - lane;
+            u64 here = 0;
+            for (int c = 0; c < ctas; ++c) here += ld_cluster32(peer(&sh.bins[turn][bin], c));
+            const u64 w = worth(bin, here), upto = before + warp_scan(w), n_upto = n_before + warp_scan(here);
+            const uint32_t reaches = __ballot_sync(0xffffffffu, upto >= goal), anything = __ballot_sync(0xffffffffu, here != 0);
+            if (lane == (reaches ? __ffs(reaches) - 1 : 31 - __clz(anything))) {
+                sh.digit = (uint32_t)bin;
+                sh.above = upto - w;
+                sh.above_to = upto;
+                sh.counts[0] = (uint32_t)n_upto;
+                sh.counts[1] = (uint32_t)here;
             }
-        u64 mine = 0, over_lowest = 0;
-        uint32_t lowest = kSampleBins;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (n[i]) { lowest = hi - i; over_lowest = mine; }
-            n[i] = worth(hi - i, n[i]);
-            mine += n[i];
-        }
-        const u64 upto = block_scan(mine);
-        if (threadIdx.x == 0) { sh.digit = kSampleBins; sh.digit_before = kSampleBins; }
-        __syncthreads();
-        if (lowest < kSampleBins) atomicMin(&sh.digit_before, lowest);
-        u64 before = upto - mine;
-        over_lowest += before;
-        if (before < goal && upto >= goal) {
-            bool open = true;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                if (open && before + n[i] >= goal) { sh.digit = hi - i; sh.above = before; open = false; }
-                before += n[i];
-            }
         }
         __syncthreads();
-        if (sh.digit == kSampleBins && lowest == sh.digit_before && lowest < kSampleBins) sh.above = over_lowest;
-        __syncthreads();
-        digit = sh.digit == kSampleBins ? sh.digit_before : sh.digit;
+        digit = sh.digit;
         above = sh.above;
         turn ^= 1;
     }
 
-    // Notes in the lists what can lie among the first of the order whose worth(bin, count) comes to goal: bins of 1 / steps by the
-    // distance from `top`, the last one for all beyond.  False: a list cannot hold it.
-    template <typename Worth>
-    __device__ __forceinline__ bool shorten(float top, float steps, u64 goal, Worth worth) {
-        auto bin = [&](float x) { return kSampleBins - 1 - (__float_as_uint(fminf((top - x) * steps, (float)(kSampleBins - 1)) + 8388608.0f) & (kSampleBins - 1)); };
+    // Counts live elements by their distance from `top`, in steps of 1 / steps, the last bin for all beyond.
+    __device__ __forceinline__ uint32_t bin_of(float x, float top, float steps) const {
+        return kSampleBins - 1 - (__float_as_uint(fminf((top - x) * steps, (float)(kSampleBins - 1)) + 8388608.0f) & (kSampleBins - 1));
+    }
+    __device__ __forceinline__ void count_distances(float top, float steps) {
         uint32_t* bins = clear_bins();
         each_chunk([&](int, const float (&x)[E]) {
 #pragma unroll
             for (int i = 0; i < E; ++i)
-                if (x[i] > -INFINITY) atomicAdd(bins + bin(x[i]), 1u);
+                if (x[i] > -INFINITY) atomicAdd(bins + bin_of(x[i], top, steps), 1u);
         });
-        uint32_t digit;
-        u64 above;
-        border(goal, worth, digit, above);
+    }
+    // Notes in the list what lies in bin `digit` or above; false where a list of this CTA cannot hold it.
+    __device__ __forceinline__ bool make_list(float top, float steps, uint32_t digit) {
         int have = 0;
 #pragma unroll 1
         for (int c0 = 0; c0 < warp_chunks; c0 += 32) {
@@ -377,7 +388,7 @@ struct SampleRow {
                 float x[E];
                 unpack(chunks[c], x);
 #pragma unroll
-                for (int i = 0; i < E; ++i) if (x[i] > -INFINITY && bin(x[i]) >= digit) in |= 1u << i;
+                for (int i = 0; i < E; ++i) if (x[i] > -INFINITY && bin_of(x[i], top, steps) >= digit) in |= 1u << i;
             }
             if (!__any_sync(0xffffffffu, in)) continue;
             int at = __popc(in);
@@ -390,13 +401,75 @@ struct SampleRow {
             for (; in && at < kSampleList; in &= in - 1) sh.list[warp][at++] = (uint16_t)(c * E + __ffs(in) - 1);
             have += more;
         }
-        __syncwarp();
-        u64 v[4];
-        gather(have > kSampleList, v);
-        if (__any_sync(0xffffffffu, (v[0] | v[1] | v[2] | v[3]) != 0)) return false;
+        if (threadIdx.x == 0) sh.longest = 0;
+        __syncthreads();
+        if (lane == 0) atomicMax(&sh.longest, have);
         listed = true;
-        count = have;
-        return true;
+        count = min(have, kSampleList);
+        __syncthreads();
+        return sh.longest <= kSampleList;
+    }
+    // An element's place in the order, the larger the earlier.
+    static __device__ __forceinline__ u64 code_of(int place, float x) { return (u64)order_key(x) << 32 | (uint32_t)~place; }
+
+    // Sums of N numbers over the CTA's threads, the same in all of them.
+    template <int N>
+    __device__ __forceinline__ void block_sums(u64 (&v)[N], int& phase) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sh.sums[phase][i][warp] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = sh.sums[phase][i][lane % kSampleWarps];
+            for (int o = kSampleWarps / 2; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+        }
+        phase ^= 1;
+    }
+    // The largest code at which the sum of f over the codes from it on reaches goal, where that of all does.
+    __device__ __forceinline__ u64 resolve(const u64 (&code)[kSampleOwn], const u64 (&f)[kSampleOwn], u64 goal, int& phase) {
+        if (threadIdx.x == 0) sh.differ[0] = sh.differ[1] = 0;
+        __syncthreads();
+        u64 ref = code[0];                                // thread 0's first member exists
+        if (threadIdx.x == 0) sh.weight = ref;
+        __syncthreads();
+        ref = sh.weight;
+        u64 other = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleOwn; ++i) if (code[i]) other |= code[i] ^ ref;
+        const uint32_t hi = __reduce_or_sync(0xffffffffu, (uint32_t)(other >> 32)), lo = __reduce_or_sync(0xffffffffu, (uint32_t)other);
+        if (lane == 0) {
+            if (hi) atomicOr(&sh.differ[0], hi);
+            if (lo) atomicOr(&sh.differ[1], lo);
+        }
+        __syncthreads();
+        const u64 differ = (u64)sh.differ[0] << 32 | sh.differ[1];
+        int bits = 64 - __clzll((long long)differ);       // all codes agree above
+        bits += bits & 1;
+        u64 e = bits >= 64 ? 0 : ref >> bits << bits;
+        for (int at = bits - 2; at >= 0; at -= 2) {       // two bits at a time
+            if (((differ >> at) & 3) == 0) { e |= ref & 3ull << at; continue; }
+            u64 s[3] = {};
+#pragma unroll
+            for (int i = 0; i < kSampleOwn; ++i)
+#pragma unroll
+                for (int q = 0; q < 3; ++q) s[q] += code[i] >= (e | (u64)(q + 1) << at) ? f[i] : 0ull;
+            block_sums(s, phase);
+            e |= (u64)(s[2] >= goal ? 3 : s[1] >= goal ? 2 : s[0] >= goal ? 1 : 0) << at;
+        }
+        return e;
+    }
+    // Takes the members that the CTAs have noted, thread by thread in their order; 0 behind the last.
+    __device__ __forceinline__ void take_members(int noted_turn, u64 (&code)[kSampleOwn]) {
+        int end = 0, c = -1, n = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleOwn; ++i) {
+            const int at = (int)threadIdx.x * kSampleOwn + i;
+            while (at >= end && c + 1 < ctas) { n = (int)ld_cluster32(peer(&sh.noted[noted_turn], ++c)); end += n; }
+            code[i] = at < end ? ld_cluster64(peer(reinterpret_cast<u64*>(sh.bins[noted_turn]) + (at - (end - n)), c)) : 0;
+        }
     }
     __device__ __forceinline__ void forget_list() {
         listed = false;
@@ -483,7 +556,6 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
 
     // What the others weigh together, the first one's weight being 1: where it has nearly all of the probability its
     // logarithm is -log(1 + rest).  32 bits: a term is off by (2.5 |d| + 4) 2^-24 of itself at most, d its distance from the first.
-    double rest = 0.0;
     if (g.logprob) {
         float some = 0.0f;
         r.each_chunk([&](int v, const float (&x)[E]) {
@@ -497,18 +569,22 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
 #pragma unroll
             for (int i = 0; i < E; ++i) some += e[i];
         });
-        rest = some;
+        double rest = some;
         for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
-        u64 v[4];
-        r.gather((u64)__double_as_longlong(rest), v);
-        rest = (__longlong_as_double(v[0]) + __longlong_as_double(v[1])) + (__longlong_as_double(v[2]) + __longlong_as_double(v[3]));
-        for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+        if (lane == 0) sh.rest[r.warp] = rest;
     }
-    auto finish = [&](int v, float x) {                   // by one thread of the row
+    // by one thread of the row, after an exchange between its CTAs
+    auto finish = [&](int v, float x) {
         g.tokens[row] = v - skew;
-        if (g.logprob) g.logprob[row] = (float)(((double)x - (double)top) - log1p(rest));
+        if (!g.logprob) return;
+        double rest = 0.0;
+        for (int c = 0; c < g.ctas; ++c)
+#pragma unroll
+            for (int w = 0; w < kSampleWarps; ++w) rest += __longlong_as_double((long long)ld_cluster64(r.peer(&sh.rest[w], c)));
+        g.logprob[row] = (float)(((double)x - (double)top) - log1p(rest));
     };
     if (greedy) {
+        r.sync();
         if (r.rank == 0 && threadIdx.x == 0) finish(first, top);
         if (g.ctas > 1) cluster_sync_all();
         return;
@@ -543,7 +619,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                 });
                 uint32_t digit;
                 above1 += above2;
-                r.border(want > above1 ? want - above1 : 1, as_counted, digit, above2);
+                const u64 left = want > above1 ? want - above1 : 1;
+                r.border([&] { return left; }, as_counted, digit, above2);
                 high = level ? high << 11 | digit : digit;
             }
             high = min(high, (1u << (32 - kLowBits)) - 1);
@@ -601,36 +678,166 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             break;
         }
     };
-    auto one = [](float) { return 1ull; };
-    const bool some = k > 0 && k < g.vocab;
-    if (some) {
-        const u64 goal = (u64)k;
-        bool all_of_them = false;
-        if (r.shorten(top, 64.0f, goal, [](uint32_t, u64 n) { return n; })) all_of_them = r.row_sum(r.sum([](int, float) { return 1ull; })) <= goal;
-        if (!all_of_them) narrow(goal, one, [](float) { return 1u; }, 1.0f);
-    }
-    if (p < 1.0f) {
-        const u64 all = r.row_sum(some ? r.sum([&](int v, float x) { return kept(v, x) ? weight(x) : 0ull; }) : r.sum_all(weight));
-        const u64 goal = max(p > 0.0f ? share_of(all, p, true) : 0ull, 1ull);
-        if (!some) {                                      // a thousandth more than the goal, since the bins' weights are those of their middles
-            const float unit = exp2f((float)g.shift);
-            auto worth = [&](uint32_t bin, u64 n) { return bin == 0 ? 0ull : (u64)((float)n * (fast_exp2(((float)bin - (float)(kSampleBins - 1)) * (1.4426950408889634f / 64.0f)) * unit)); };
-            if (r.shorten(top, fminf(weight.coolf, 1e30f) * 64.0f, goal + (all >> 10), worth) &&
-                r.row_sum(r.sum([&](int, float x) { return weight(x); })) < goal) r.forget_list();
+    const bool some = k > 0 && k < g.vocab, top_p = p < 1.0f;
+    const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
+    auto drawn = [&](u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(all, u, false) : 0ull; };
+    auto share = [&](u64 all) { return max(p > 0.0f ? share_of(all, p, true) : 0ull, 1ull); };
+    u64 all = 0;                                          // top-p without top-k: what the row weighs
+    bool open = some || top_p;                            // whether the first end is still to be found
+    int64_t bias = 0;
+    int phase = 0;
+    const float steps = 64.0f * (some ? 1.0f : fminf(weight.coolf, 1e30f)), unit = exp2f((float)g.shift);
+#pragma unroll 1
+    for (int tries = 0; open && tries < 3; ++tries) {
+        // How far the first of the order reach: for top-k by counts, for top-p by counts times the weight in the middle of a bin.
+        // Where that is too far off, the sums show it, and the next try takes the difference into account.
+        auto worth = [&](uint32_t bin, u64 n) -> u64 {
+            if (some) return n;
+            return bin == 0 ? 0ull : (u64)((float)n * (fast_exp2(((float)bin - (float)(kSampleBins - 1)) * (1.4426950408889634f / 64.0f)) * unit));
+        };
+        r.forget_list();
+        r.count_distances(top, steps);
+        const int turn = r.turn;
+        if (!some && tries == 0) {
+            const u64 mine = SampleRow<T>::warp_sum(r.sum_all(weight));
+            if (lane == 0) sh.parts[turn][r.warp] = mine;
         }
-        const float units = 4.2e9f / ((float)all * 1.0001f), per = units * exp2f((float)g.shift);
-        narrow(goal, weight,
+        u64 goal = 0, above;
+        uint32_t digit;
+        r.border(
+            [&] {
+                if (!some && tries == 0) {
+                    for (int i = 0; i < 4; ++i) {
+                        const int n = lane * 4 + i;
+                        if (n < g.ctas * kSampleWarps) all += ld_cluster64(r.peer(&sh.parts[turn][n % kSampleWarps], n / kSampleWarps));
+                    }
+                    all = SampleRow<T>::warp_sum(all);
+                }
+                goal = some ? (u64)k : share(all);
+                return (u64)max((int64_t)goal + bias, (int64_t)1);
+            },
+            worth, digit, above);
+        const u64 above_to = sh.above_to;
+        const uint32_t listed = sh.counts[0], within = sh.counts[1], most = (uint32_t)min(kSampleThreads * kSampleOwn, kSampleMembers * g.ctas);
+        // Few: every CTA gets all of them and goes on alone.  Many: the border's bin; the others' sum is taken here.
+        const bool few = listed <= most;
+        const bool fits = r.make_list(top, steps, digit);
+        if (!fits) r.forget_list();
+        if (!few && within > most) break;
+        int at = 0;
+        if (few) {                                        // noted in ascending places
+            if (lane == 0) sh.scan[r.warp] = fits ? (u64)r.count : 0ull;
+            __syncthreads();
+            int end = 0;
+            for (int w = 0; w < kSampleWarps; ++w) {
+                if (w == r.warp) at = end;
+                end += (int)sh.scan[w];
+            }
+            if (threadIdx.x == 0) sh.noted[r.turn] = fits ? end : kSampleMembers + 1;
+            at += lane;
+        } else if (threadIdx.x == 0) {
+            sh.noted[r.turn] = 0;
+        }
+        __syncthreads();
+        u64* members = reinterpret_cast<u64*>(sh.bins[r.turn]);
+        u64 s = 0;
+        if (few ? fits : true) {
+            r.each([&](int v, float x) {
+                const uint32_t bin = r.bin_of(x, top, steps);
+                if (few || (bin == digit && x > -INFINITY)) {
+                    const int i = few ? at : atomicAdd(&sh.noted[r.turn], 1);
+                    if (i < kSampleMembers) members[i] = SampleRow<T>::code_of(v, x);
+                    at += 32;
+                } else if (bin > digit) {
+                    s += some ? 1ull : weight(x);
+                }
+            });
+        }
+        __syncthreads();
+        const int noted_turn = r.turn;
+        const bool too_many = sh.noted[noted_turn] > kSampleMembers;
+        u64 v[4];
+        r.gather(SampleRow<T>::warp_sum(s) | (too_many ? 1ull << 63 : 0ull), v);
+        if (__any_sync(0xffffffffu, (int64_t)(v[0] | v[1] | v[2] | v[3]) < 0)) break;
+        const u64 sum = SampleRow<T>::warp_sum(v[0] + v[1] + v[2] + v[3]);
+        u64 code[kSampleOwn], w[kSampleOwn], f[kSampleOwn], whole[1] = {0};
+        r.take_members(noted_turn, code);
+#pragma unroll
+        for (int i = 0; i < kSampleOwn; ++i) {
+            w[i] = code[i] ? weight(key_value((uint32_t)(code[i] >> 32))) : 0;
+            f[i] = some ? (u64)(code[i] != 0) : w[i];
+            whole[0] += f[i];
+        }
+        r.block_sums(whole, phase);
+        u64 e = 0;
+        if (sum + whole[0] < goal) {                      // fewer over -infinity than top-k lets stay, or too short a guess
+            if (!some) { bias += (int64_t)(above_to - (sum + whole[0])); continue; }
+        } else if (sum >= goal) {
+            bias += (int64_t)(above - sum);
+            continue;
+        } else {
+            e = r.resolve(code, f, goal - sum, phase);
+        }
+        open = false;
+        if (!few) {
+            edge = (uint32_t)(e >> 32);
+            cut = (int)~(uint32_t)e;
+            break;
+        }
+        if (some && top_p) {
+            u64 kept_sum[1] = {0};
+#pragma unroll
+            for (int i = 0; i < kSampleOwn; ++i) {
+                f[i] = code[i] >= e ? w[i] : 0;
+                kept_sum[0] += f[i];
+            }
+            r.block_sums(kept_sum, phase);
+            e = max(e, r.resolve(code, f, share(kept_sum[0]), phase));
+        }
+        u64 mine = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleOwn; ++i) {
+            f[i] = code[i] >= e && (w[i] >= floor_w || (int)~(uint32_t)code[i] == first) ? w[i] : 0;
+            mine += f[i];
+        }
+        const u64 upto = r.block_scan(mine);
+        if (threadIdx.x == kSampleThreads - 1) sh.above = upto;
+        __syncthreads();
+        const u64 point = drawn(sh.above);
+        u64 before = upto - mine;
+        if (r.rank == 0 && before <= point && upto > point) {
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < kSampleOwn; ++i) {
+                before += f[i];
+                if (!found && before > point) {
+                    finish((int)~(uint32_t)code[i], key_value((uint32_t)(code[i] >> 32)));
+                    found = true;
+                }
+            }
+        }
+        if (g.ctas > 1) cluster_sync_all();
+        return;
+    }
+    if (open && some) narrow((u64)k, [](float) { return 1ull; }, [](float) { return 1u; }, 1.0f);
+    if (top_p && (some || open)) {
+        if (!some) r.forget_list();
+        const u64 left = r.row_sum(r.sum([&](int v, float x) { return kept(v, x) ? weight(x) : 0ull; }));
+        const float units = 4.2e9f / ((float)left * 1.0001f), per = units * unit;
+        narrow(share(left), weight,
                [&](float x) { return x > -INFINITY ? max(1u, __float2uint_rn(fast_exp2((x - top) * weight.coolf * 1.4426950408889634f) * per)) : 0u; }, 1.0f / units);
     }
-    const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
+    const bool all_stay = !some && !top_p && floor_w <= 1;
+    if (!some && !top_p && !all_stay) {                   // min-p alone: two bins below its border at most
+        const uint32_t far = (uint32_t)fminf(-64.0f * logf(least) + 2.0f, (float)(kSampleBins - 1));
+        if (!(least < 1.0f) || !r.make_list(top, steps, kSampleBins - 1 - far)) r.forget_list();
+    }
     auto stays = [&](int v, float x) {
         if (!kept(v, x)) return 0ull;
         const u64 w = weight(x);
         return w >= floor_w || v == first ? w : 0ull;
     };
-    const bool all_stay = !some && !(p < 1.0f) && floor_w <= 1;
-    const int place = r.running(all_stay ? r.sum_all(weight) : r.sum(stays), stays,
-                                [&](u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(all, u, false) : 0ull; });
+    const int place = r.running(all_stay ? r.sum_all(weight) : r.sum(stays), stays, drawn);
     if (place >= 0) finish(place, to_f32(reinterpret_cast<const T*>(held)[place - r.rank * kSampleWarps * g.warp_chunks * E]));
     if (g.ctas > 1) cluster_sync_all();
 }
