@@ -5,14 +5,16 @@
 // order, borders are exact products with the row's own numbers, and the sums lie within some 2^-45 of real numbers'.
 // (With 32-bit weights a tail token of a flat row of 131,072 is another one in some percent of the draws.)
 //
-// A row belongs to a thread-block cluster, whose CTAs hold a share of it each in shared memory: the logits are read once,
-// and every further look at them is at the shares.  Nothing is sorted.  Where top-k or top-p ends is found in two steps.
-// Counts by distance from the largest logit, in 2048 steps of 1/64, say how far the kept ones can reach at most; those
-// that lie there are noted in a list, and the rest is not looked at again.  The end itself is a key (the logit's bits in
-// their order) and a place among its equals: two passes count by 11 bits of the key each -- exactly for top-k, with rounded
-// weights for top-p --, and a third takes the exact sum of all above the 2^10 keys found and counts their
-// members; equals have equal weights, so count times weight is exact.  Where rounding had led astray the search goes on from
-// there, on the right side.  What the list cannot hold is searched in the shares themselves, the same way.
+// A row belongs to one CTA, or where there are few rows to a cluster of up to eight.  Shares that are small enough stay in shared
+// memory; of larger ones only the first look goes to memory, the later ones find the row in L2.  Nothing is sorted.  Where
+// top-k or top-p ends is found in two steps.  Counts by distance from the largest logit, in 2048 steps of 1/64, say in which
+// step the end lies; what lies above is kept, and what lies in it is handed to every CTA of the row, which counts
+// it by the bits of a code, key (the logit's bits in their order) before place -- no two elements have the same one.
+// Where few are kept all of them are handed round, and the rest of the work needs no more exchange.
+// Where that fails (more than 2048 equals, say) the row is searched by the bits of its keys: two passes count by 11 bits each --
+// exactly for top-k, with rounded weights for top-p --, and a third takes the exact sum of all above the 2^10 keys found
+// and counts their members; equals have equal weights, so count times weight is exact.  Where rounding had led astray the
+// search goes on from there, on the right side.
 #include "mpq_attention.cuh"
 #include "mpq_tensor.cuh"
 
@@ -26,14 +28,14 @@ struct SampleArgs {
     const float *temperature; const int32_t* top_k; const float *top_p, *min_p, *uniform;
     int64_t* tokens; float* logprob;
     int shift;                                            // weights are multiples of 2^-shift: vocab 2^shift <= 2^62
-    int ctas, warp_chunks;                                // CTAs of a row; 16-byte chunks that a warp holds
+    int ctas, warp_chunks;                                // CTAs of a row; 16-byte chunks that are a warp's share
+    int cached, list;                                     // whether shares stay in shared memory; elements that a warp's list holds
 };
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleBins = 2048, kLowBits = 10;          // 11 + 11 + 10 bits of a key
 constexpr int kSampleGroups = kSampleBins / 32;
 constexpr int kSampleOwn = 4, kSampleMembers = 1024;      // members that a thread holds, and a CTA hands out
-constexpr int kSampleList = 480;                          // elements of a warp's share that its list holds
 
 // Whole numbers in the order of the logits; -0 and 0 are the same number.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -88,7 +90,7 @@ struct SampleShared {
     double rest[kSampleWarps];
     u64 sums[2][3][kSampleWarps];
     uint32_t differ[2];
-    uint16_t list[kSampleWarps][kSampleList];             // places in a warp's share, ascending
+    u64 member;
 };
 
 // The largest element of a chunk, NaN if one is.
@@ -140,17 +142,24 @@ template <typename T>
 struct SampleRow {
     static constexpr int E = 16 / (int)sizeof(T);         // elements of a chunk
     SampleShared& sh;
-    uint4* chunks;                                        // this warp's share
-    const int ctas, rank, warp, lane, warp_chunks;
-    const int v0;                                         // place of its first element; places count from the 16-byte boundary before the row
+    const T* x0;                                          // the row
+    const int vocab, skew;                                // skew: place of its first element; places count from the 16-byte boundary before it
+    uint4* chunks;                                        // this warp's share, where it is cached
+    uint16_t* list;                                       // elements of the share that can still be kept, ascending
+    const bool cached;
+    const int ctas, rank, warp, lane, warp_chunks, list_size;
+    const int v0;                                         // place of the share's first element
     int turn = 0;                                         // which of the two exchange buffers comes next
     bool listed = false;                                  // whether the list has all that can still be kept, and how much that is
     int count;
 
     __device__ SampleRow(SampleShared& s, uint4* data, const SampleArgs& g)
-        : sh(s), ctas(g.ctas), rank(g.ctas > 1 ? (int)cluster_rank() : 0), warp(__shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0)), lane(threadIdx.x & 31),
-          warp_chunks(g.warp_chunks), v0((rank * kSampleWarps + warp) * g.warp_chunks * E), count(g.warp_chunks * E) {
+        : sh(s), x0(static_cast<const T*>(g.logits) + (int64_t)(blockIdx.x / (unsigned)g.ctas) * g.ld), vocab(g.vocab),
+          skew((int)(reinterpret_cast<uintptr_t>(x0) & 15) / (int)sizeof(T)), cached(g.cached != 0), ctas(g.ctas), rank(g.ctas > 1 ? (int)cluster_rank() : 0),
+          warp(__shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0)), lane(threadIdx.x & 31), warp_chunks(g.warp_chunks), list_size(g.list),
+          v0((rank * kSampleWarps + warp) * g.warp_chunks * E), count(g.warp_chunks * E) {
         chunks = data + warp * warp_chunks;
+        list = reinterpret_cast<uint16_t*>(data + (g.cached ? kSampleWarps * warp_chunks : 0)) + warp * list_size;
     }
 
     __device__ __forceinline__ void sync() {
@@ -164,31 +173,73 @@ struct SampleRow {
 #pragma unroll
         for (int i = 0; i < E; ++i) x[i] = to_f32(e[i]);
     }
+    // Chunk c of the share from memory, -infinity where the row is not.
+    __device__ __forceinline__ uint4 read_chunk(int c) const {
+        const int i = v0 + c * E - skew;
+        if (i >= 0 && i + E <= vocab) return __ldg(reinterpret_cast<const uint4*>(x0 + i));
+        uint4 r;
+        T* e = reinterpret_cast<T*>(&r);
+#pragma unroll
+        for (int q = 0; q < E; ++q) e[q] = i + q >= 0 && i + q < vocab ? x0[i + q] : from_f32<T>(-INFINITY);
+        return r;
+    }
+    // Chunks c, c + 32, .. of the share (the last one in place of those behind it), asked for together.
+    template <int N>
+    __device__ __forceinline__ void read_chunks(int c, uint4 (&in)[N], bool from_memory) const {
+        if (!from_memory) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) in[j] = chunks[min(c + 32 * j, warp_chunks - 1)];
+        } else if (v0 >= skew && v0 + warp_chunks * E - skew <= vocab) {         // every share but a row's first and last one
+            const uint4* from = reinterpret_cast<const uint4*>(x0 + (v0 - skew));
+#pragma unroll
+            for (int j = 0; j < N; ++j) in[j] = __ldg(from + min(c + 32 * j, warp_chunks - 1));
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) in[j] = read_chunk(min(c + 32 * j, warp_chunks - 1));
+        }
+    }
     // f(place of the first, values) for this lane's chunks of the whole share.
     template <typename F>
     __device__ __forceinline__ void each_chunk(F f) const {
+        constexpr int kAtOnce = 2;
 #pragma unroll 1
-        for (int c = lane; c < warp_chunks; c += 32) {
-            float x[E];
-            unpack(chunks[c], x);
-            f(v0 + c * E, x);
+        for (int c = lane; c < warp_chunks; c += 32 * kAtOnce) {
+            uint4 in[kAtOnce];
+            read_chunks(c, in, !cached);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                float x[E];
+                unpack(in[j], x);
+                if (c + 32 * j < warp_chunks) f(v0 + (c + 32 * j) * E, x);
+            }
         }
     }
     // Element i of what is still looked at in the share of warp w of this CTA.
     __device__ __forceinline__ void element(int w, int i, int& place, float& x) const {
-        const int at = listed ? sh.list[w][i] : i;
+        const int at = listed ? list[(w - warp) * list_size + i] : i;
         place = v0 + (w - warp) * warp_chunks * E + at;
-        x = to_f32(reinterpret_cast<const T*>(chunks + (w - warp) * warp_chunks)[at]);
+        if (cached) x = to_f32(reinterpret_cast<const T*>(chunks + (w - warp) * warp_chunks)[at]);
+        else x = place >= skew && place - skew < vocab ? to_f32(x0[place - skew]) : -INFINITY;
     }
-    // f(place, value) for what is still looked at, in ascending places of the warp.
+    // f(place, value) for what is still looked at; a list's in ascending places of the warp.
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
+        if (listed) {
+            constexpr int kAtOnce = 4;
 #pragma unroll 1
-        for (int i = lane; i < count; i += 32) {
-            int place;
-            float x;
-            element(warp, i, place, x);
-            f(place, x);
+            for (int i = lane; i < count; i += 32 * kAtOnce) {
+                int place[kAtOnce];
+                float x[kAtOnce];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) element(warp, min(i + 32 * j, count - 1), place[j], x[j]);
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) if (i + 32 * j < count) f(place[j], x[j]);
+            }
+        } else {
+            each_chunk([&](int v, const float (&x)[E]) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) f(v + i, x[i]);
+            });
         }
     }
 
@@ -235,27 +286,24 @@ struct SampleRow {
         each([&](int place, float x) { s += f(place, x); });
         return s;
     }
-    // Sum of the weights of the whole share.
-    __device__ __forceinline__ u64 sum_all(const SampleWeight& weight) const {
+    // Sum of a chunk's weights.
+    static __device__ __forceinline__ u64 chunk_sum(const SampleWeight& weight, const float (&x)[E]) {
         u64 s = 0;
-        each_chunk([&](int, const float (&x)[E]) {
-            float low = x[0];
+        float low = x[0];
 #pragma unroll
-            for (int i = 1; i < E; ++i) low = fminf(low, x[i]);
-            if (!weight.small(low) && low > -INFINITY) {
+        for (int i = 1; i < E; ++i) low = fminf(low, x[i]);
+        if (!weight.small(low) && low > -INFINITY) {
 #pragma unroll
-                for (int i = 0; i < E; ++i) s += weight.biased(x[i]);
-                s -= E * SampleWeight::kBias;             // (modulo 2^64)
-            } else {
+            for (int i = 0; i < E; ++i) s += weight.biased(x[i]);
+            return s - E * SampleWeight::kBias;           // (modulo 2^64)
+        }
 #pragma unroll 1
-                for (int i = 0; i < E; ++i) {
-                    float one = x[0];
+        for (int i = 0; i < E; ++i) {
+            float one = x[0];
 #pragma unroll
-                    for (int j = 1; j < E; ++j) one = i == j ? x[j] : one;
-                    s += weight(one);
-                }
-            }
-        });
+            for (int j = 1; j < E; ++j) one = i == j ? x[j] : one;
+            s += weight(one);
+        }
         return s;
     }
 
@@ -365,49 +413,48 @@ struct SampleRow {
         turn ^= 1;
     }
 
-    // Counts live elements by their distance from `top`, in steps of 1 / steps, the last bin for all beyond.
+    // Bin of an element by its distance from `top`, in steps of 1 / steps, the lowest one for all beyond.
     __device__ __forceinline__ uint32_t bin_of(float x, float top, float steps) const {
         return kSampleBins - 1 - (__float_as_uint(fminf((top - x) * steps, (float)(kSampleBins - 1)) + 8388608.0f) & (kSampleBins - 1));
     }
-    __device__ __forceinline__ void count_distances(float top, float steps) {
-        uint32_t* bins = clear_bins();
-        each_chunk([&](int, const float (&x)[E]) {
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (x[i] > -INFINITY) atomicAdd(bins + bin_of(x[i], top, steps), 1u);
-        });
-    }
-    // Notes in the list what lies in bin `digit` or above; false where a list of this CTA cannot hold it.
+    // Notes in the list what lies in bin `digit` or above; false, and no list, where this CTA's cannot hold it.
     __device__ __forceinline__ bool make_list(float top, float steps, uint32_t digit) {
+        constexpr int kAtOnce = 4;
         int have = 0;
 #pragma unroll 1
-        for (int c0 = 0; c0 < warp_chunks; c0 += 32) {
-            const int c = c0 + lane;
-            uint32_t in = 0;
-            if (c < warp_chunks) {
-                float x[E];
-                unpack(chunks[c], x);
+        for (int c0 = lane; c0 - lane < warp_chunks; c0 += 32 * kAtOnce) {
+            uint4 in[kAtOnce];
+            read_chunks(min(c0, warp_chunks - 1), in, !cached);
 #pragma unroll
-                for (int i = 0; i < E; ++i) if (x[i] > -INFINITY && bin_of(x[i], top, steps) >= digit) in |= 1u << i;
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int c = c0 + 32 * j;
+                float x[E];
+                unpack(in[j], x);
+                uint32_t mine = 0;
+#pragma unroll
+                for (int i = 0; i < E; ++i) mine |= x[i] > -INFINITY && bin_of(x[i], top, steps) >= digit ? 1u << i : 0u;
+                if (c >= warp_chunks) mine = 0;
+                if (!__any_sync(0xffffffffu, mine)) continue;
+                int at = __popc(mine);
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int below = __shfl_up_sync(0xffffffffu, at, o);
+                    if (lane >= o) at += below;
+                }
+                const int more = __shfl_sync(0xffffffffu, at, 31);
+                at += have - __popc(mine);
+                for (; mine && at < list_size; mine &= mine - 1) list[at++] = (uint16_t)(c * E + __ffs(mine) - 1);
+                have += more;
             }
-            if (!__any_sync(0xffffffffu, in)) continue;
-            int at = __popc(in);
-            for (int o = 1; o < 32; o <<= 1) {
-                const int below = __shfl_up_sync(0xffffffffu, at, o);
-                if (lane >= o) at += below;
-            }
-            const int more = __shfl_sync(0xffffffffu, at, 31);
-            at += have - __popc(in);
-            for (; in && at < kSampleList; in &= in - 1) sh.list[warp][at++] = (uint16_t)(c * E + __ffs(in) - 1);
-            have += more;
         }
         if (threadIdx.x == 0) sh.longest = 0;
         __syncthreads();
         if (lane == 0) atomicMax(&sh.longest, have);
-        listed = true;
-        count = min(have, kSampleList);
         __syncthreads();
-        return sh.longest <= kSampleList;
+        if (sh.longest > list_size) return false;
+        listed = true;
+        count = have;
+        return true;
     }
     // An element's place in the order, the larger the earlier.
     static __device__ __forceinline__ u64 code_of(int place, float x) { return (u64)order_key(x) << 32 | (uint32_t)~place; }
@@ -428,14 +475,17 @@ struct SampleRow {
         }
         phase ^= 1;
     }
-    // The largest code at which the sum of f over the codes from it on reaches goal, where that of all does.
-    __device__ __forceinline__ u64 resolve(const u64 (&code)[kSampleOwn], const u64 (&f)[kSampleOwn], u64 goal, int& phase) {
-        if (threadIdx.x == 0) sh.differ[0] = sh.differ[1] = 0;
+    // The largest code at which the sum of f over the codes from it on reaches goal, where that of all does: ten bits at a
+    // time, from the highest one in which they differ, until one is left.
+    __device__ __forceinline__ u64 resolve(const u64 (&code)[kSampleOwn], const u64 (&f)[kSampleOwn], u64 goal) {
+        constexpr int kBits = 10, kPer = (1 << kBits) / kSampleThreads;
+        u64* bins = reinterpret_cast<u64*>(sh.bins[turn]);
+        if (threadIdx.x == 0) {
+            sh.differ[0] = sh.differ[1] = 0;
+            sh.member = code[0];                          // thread 0's first member exists
+        }
         __syncthreads();
-        u64 ref = code[0];                                // thread 0's first member exists
-        if (threadIdx.x == 0) sh.weight = ref;
-        __syncthreads();
-        ref = sh.weight;
+        const u64 ref = sh.member;
         u64 other = 0;
 #pragma unroll
         for (int i = 0; i < kSampleOwn; ++i) if (code[i]) other |= code[i] ^ ref;
@@ -445,21 +495,42 @@ struct SampleRow {
             if (lo) atomicOr(&sh.differ[1], lo);
         }
         __syncthreads();
-        const u64 differ = (u64)sh.differ[0] << 32 | sh.differ[1];
-        int bits = 64 - __clzll((long long)differ);       // all codes agree above
-        bits += bits & 1;
-        u64 e = bits >= 64 ? 0 : ref >> bits << bits;
-        for (int at = bits - 2; at >= 0; at -= 2) {       // two bits at a time
-            if (((differ >> at) & 3) == 0) { e |= ref & 3ull << at; continue; }
-            u64 s[3] = {};
+        int at = 64 - __clzll((long long)((u64)sh.differ[0] << 32 | sh.differ[1]));        // all codes agree from this bit up
+        if (at == 0) return ref;
+        u64 prefix = at < 64 ? ref >> at : 0;
+        for (;;) {
+            const int shift = max(at - kBits, 0), width = at - shift;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) bins[threadIdx.x + i * kSampleThreads] = 0;
+            __syncthreads();
 #pragma unroll
             for (int i = 0; i < kSampleOwn; ++i)
+                if (f[i] && (at == 64 || code[i] >> at == prefix)) atomicAdd(bins + (code[i] >> shift & ((1u << width) - 1)), f[i]);
+            __syncthreads();
+            u64 n[kPer], mine = 0;
+            const int first = (1 << kBits) - 1 - (int)threadIdx.x * kPer;
 #pragma unroll
-                for (int q = 0; q < 3; ++q) s[q] += code[i] >= (e | (u64)(q + 1) << at) ? f[i] : 0ull;
-            block_sums(s, phase);
-            e |= (u64)(s[2] >= goal ? 3 : s[1] >= goal ? 2 : s[0] >= goal ? 1 : 0) << at;
+            for (int i = 0; i < kPer; ++i) { n[i] = bins[first - i]; mine += n[i]; }
+            u64 before = block_scan(mine) - mine;
+            if (before < goal && before + mine >= goal) {
+                bool open = true;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    if (open && before + n[i] >= goal) { sh.digit = (uint32_t)(first - i); sh.above = before; open = false; }
+                    before += n[i];
+                }
+            }
+            __syncthreads();
+            prefix = prefix << width | sh.digit;
+            goal -= sh.above;
+            at = shift;
+            int left = 0;
+#pragma unroll
+            for (int i = 0; i < kSampleOwn; ++i)
+                if (f[i] && code[i] >> at == prefix) { ++left; sh.member = code[i]; }
+            const bool one = __syncthreads_or(left > 1) == 0 && __syncthreads_count(left == 1) == 1;
+            if (one || at == 0) return sh.member;
         }
-        return e;
     }
     // Takes the members that the CTAs have noted, thread by thread in their order; 0 behind the last.
     __device__ __forceinline__ void take_members(int noted_turn, u64 (&code)[kSampleOwn]) {
@@ -483,39 +554,27 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     __shared__ SampleShared sh;
     constexpr int E = SampleRow<T>::E;
     SampleRow<T> r(sh, held, g);
-    const int lane = r.lane;
+    const int lane = r.lane, skew = r.skew;
     if (threadIdx.x < 16) sh.powers[threadIdx.x] = exp2((double)threadIdx.x / 16.0 + (double)g.shift);
     chain_entry();
     const int64_t row = blockIdx.x / g.ctas;
-    const T* x0 = static_cast<const T*>(g.logits) + row * g.ld;
-    const int skew = (int)(reinterpret_cast<uintptr_t>(x0) & 15) / (int)sizeof(T);        // the row's first place
     const float warm = g.temperature ? g.temperature[row] : 1.0f;
     const int k = g.top_k ? g.top_k[row] : 0;
     const float p = g.top_p ? g.top_p[row] : 1.0f, least = g.min_p ? g.min_p[row] : 0.0f, u = g.uniform[row];
 
-    // the row into shared memory, -infinity before and behind it; the first of its order, and NaNs
+    // the first of the row's order, and NaNs
     float best = -INFINITY;
     int best_chunk = 0;
     bool nan = false;
-    constexpr int kLoads = 4;
+    constexpr int kLoads = 8;
 #pragma unroll 1
-    for (int c0 = 0; c0 < g.warp_chunks; c0 += 32 * kLoads) {
+    for (int c0 = lane; c0 < g.warp_chunks; c0 += 32 * kLoads) {
         uint4 in[kLoads];
+        r.read_chunks(c0, in, true);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int c = c0 + 32 * j + lane, i = r.v0 + c * E - skew;
-            if (c < g.warp_chunks && i >= 0 && i + E <= g.vocab) {
-                in[j] = __ldg(reinterpret_cast<const uint4*>(x0 + i));
-            } else {
-                T* e = reinterpret_cast<T*>(&in[j]);
-#pragma unroll
-                for (int q = 0; q < E; ++q) e[q] = c < g.warp_chunks && i + q >= 0 && i + q < g.vocab ? x0[i + q] : from_f32<T>(-INFINITY);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int c = c0 + 32 * j + lane;
-            if (c < g.warp_chunks) r.chunks[c] = in[j];
+            const int c = min(c0 + 32 * j, g.warp_chunks - 1);
+            if (r.cached) r.chunks[c] = in[j];
             const float top = chunk_max(in[j], static_cast<const T*>(nullptr));
             if (!(top <= best)) {
                 nan |= top != top;
@@ -527,7 +586,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     u64 code = 0;                                         // 0: nothing over -infinity; all ones: a NaN
     if (best > -INFINITY) {
         float x[E];
-        SampleRow<T>::unpack(r.chunks[best_chunk], x);
+        SampleRow<T>::unpack(r.cached ? r.chunks[best_chunk] : r.read_chunk(best_chunk), x);
         int at = E - 1;
 #pragma unroll
         for (int q = E - 1; q >= 0; --q) if (x[q] == best) at = q;
@@ -554,25 +613,45 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         return;
     }
 
-    // What the others weigh together, the first one's weight being 1: where it has nearly all of the probability its
-    // logarithm is -log(1 + rest).  32 bits: a term is off by (2.5 |d| + 4) 2^-24 of itself at most, d its distance from the first.
-    if (g.logprob) {
-        float some = 0.0f;
+    const bool some = k > 0 && k < g.vocab, top_p = p < 1.0f, cut_off = !greedy && (some || top_p);
+    const SampleWeight weight(top, warm, g.shift, sh.powers);
+    const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
+    const bool all_stay = !some && !top_p && floor_w <= 1;
+    const float steps = 64.0f * (some ? 1.0f : fminf(weight.coolf, 1e30f));
+    // A second look at all of it, for whatever is wanted: counts of distances; the sum of all weights; and what the others weigh
+    // together at temperature 1, the first one's weight being 1 -- where it has nearly all of the probability its logarithm is
+    // -log(1 + rest).  That one in 32 bits: a term is off by (2.5 |d| + 4) 2^-24 of itself at most, d its distance from the first.
+    u64 weights = 0;
+    auto look = [&](bool distances, bool sums, bool others) {
+        if (!distances && !sums && !others) return;
+        uint32_t* bins = distances ? r.clear_bins() : nullptr;
+        float rest = 0.0f;
         r.each_chunk([&](int v, const float (&x)[E]) {
-            float e[E];
+            if (distances) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) e[i] = fast_exp2((x[i] - top) * 1.4426950408889634f);
-            if ((unsigned)(first - v) < (unsigned)E) {
-#pragma unroll
-                for (int i = 0; i < E; ++i) if (v + i == first) e[i] = 0.0f;
+                for (int i = 0; i < E; ++i)
+                    if (x[i] > -INFINITY) atomicAdd(bins + r.bin_of(x[i], top, steps), 1u);
             }
+            if (sums) weights += SampleRow<T>::chunk_sum(weight, x);
+            if (others) {
+                float e[E];
 #pragma unroll
-            for (int i = 0; i < E; ++i) some += e[i];
+                for (int i = 0; i < E; ++i) e[i] = fast_exp2((x[i] - top) * 1.4426950408889634f);
+                if ((unsigned)(first - v) < (unsigned)E) {
+#pragma unroll
+                    for (int i = 0; i < E; ++i) if (v + i == first) e[i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < E; ++i) rest += e[i];
+            }
         });
-        double rest = some;
-        for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
-        if (lane == 0) sh.rest[r.warp] = rest;
-    }
+        if (others) {
+            double sum = rest;
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0) sh.rest[r.warp] = sum;
+        }
+    };
+    look(cut_off, !greedy && (all_stay || (top_p && !some)), g.logprob != nullptr);
     // by one thread of the row, after an exchange between its CTAs
     auto finish = [&](int v, float x) {
         g.tokens[row] = v - skew;
@@ -590,7 +669,6 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         return;
     }
 
-    const SampleWeight weight(top, warm, g.shift, sh.powers);
     // kept: keys over `edge`, and those equal to it up to place `cut`
     uint32_t edge = 0;
     int cut = 0x7fffffff;
@@ -678,15 +756,13 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             break;
         }
     };
-    const bool some = k > 0 && k < g.vocab, top_p = p < 1.0f;
-    const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
     auto drawn = [&](u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(all, u, false) : 0ull; };
     auto share = [&](u64 all) { return max(p > 0.0f ? share_of(all, p, true) : 0ull, 1ull); };
     u64 all = 0;                                          // top-p without top-k: what the row weighs
     bool open = some || top_p;                            // whether the first end is still to be found
     int64_t bias = 0;
     int phase = 0;
-    const float steps = 64.0f * (some ? 1.0f : fminf(weight.coolf, 1e30f)), unit = exp2f((float)g.shift);
+    const float unit = exp2f((float)g.shift);
 #pragma unroll 1
     for (int tries = 0; open && tries < 3; ++tries) {
         // How far the first of the order reach: for top-k by counts, for top-p by counts times the weight in the middle of a bin.
@@ -696,10 +772,10 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             return bin == 0 ? 0ull : (u64)((float)n * (fast_exp2(((float)bin - (float)(kSampleBins - 1)) * (1.4426950408889634f / 64.0f)) * unit));
         };
         r.forget_list();
-        r.count_distances(top, steps);
+        if (tries > 0) look(true, false, false);
         const int turn = r.turn;
         if (!some && tries == 0) {
-            const u64 mine = SampleRow<T>::warp_sum(r.sum_all(weight));
+            const u64 mine = SampleRow<T>::warp_sum(weights);
             if (lane == 0) sh.parts[turn][r.warp] = mine;
         }
         u64 goal = 0, above;
@@ -722,7 +798,6 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         // Few: every CTA gets all of them and goes on alone.  Many: the border's bin; the others' sum is taken here.
         const bool few = listed <= most;
         const bool fits = r.make_list(top, steps, digit);
-        if (!fits) r.forget_list();
         if (!few && within > most) break;
         int at = 0;
         if (few) {                                        // noted in ascending places
@@ -776,7 +851,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             bias += (int64_t)(above - sum);
             continue;
         } else {
-            e = r.resolve(code, f, goal - sum, phase);
+            e = r.resolve(code, f, goal - sum);
         }
         open = false;
         if (!few) {
@@ -792,7 +867,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                 kept_sum[0] += f[i];
             }
             r.block_sums(kept_sum, phase);
-            e = max(e, r.resolve(code, f, share(kept_sum[0]), phase));
+            e = max(e, r.resolve(code, f, share(kept_sum[0])));
         }
         u64 mine = 0;
 #pragma unroll
@@ -827,41 +902,45 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         narrow(share(left), weight,
                [&](float x) { return x > -INFINITY ? max(1u, __float2uint_rn(fast_exp2((x - top) * weight.coolf * 1.4426950408889634f) * per)) : 0u; }, 1.0f / units);
     }
-    const bool all_stay = !some && !top_p && floor_w <= 1;
     if (!some && !top_p && !all_stay) {                   // min-p alone: two bins below its border at most
         const uint32_t far = (uint32_t)fminf(-64.0f * logf(least) + 2.0f, (float)(kSampleBins - 1));
-        if (!(least < 1.0f) || !r.make_list(top, steps, kSampleBins - 1 - far)) r.forget_list();
+        if (least < 1.0f) r.make_list(top, steps, kSampleBins - 1 - far);
     }
     auto stays = [&](int v, float x) {
         if (!kept(v, x)) return 0ull;
         const u64 w = weight(x);
         return w >= floor_w || v == first ? w : 0ull;
     };
-    const int place = r.running(all_stay ? r.sum_all(weight) : r.sum(stays), stays, drawn);
-    if (place >= 0) finish(place, to_f32(reinterpret_cast<const T*>(held)[place - r.rank * kSampleWarps * g.warp_chunks * E]));
+    const int place = r.running(all_stay ? weights : r.sum(stays), stays, drawn);
+    if (place >= 0) finish(place, to_f32(r.x0[place - skew]));
     if (g.ctas > 1) cluster_sync_all();
 }
 
-constexpr int kSampleMost = 196608;                       // bytes of a row that a CTA can hold
+constexpr int kSampleMost = 786432;                       // elements of a row: a place in a warp's share has 16 bits
+constexpr int kSampleHeld = 88 * 1024;                    // bytes of shares and lists with which two CTAs fit a multiprocessor
 
 template <typename T>
 int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
     constexpr int E = 16 / (int)sizeof(T);
     static PerDeviceOnce once;
-    const int rc = once.raise_smem_limit(sample_kernel<T>, kSampleMost + 16 * kSampleWarps);
+    const int rc = once.raise_smem_limit(sample_kernel<T>, kSampleHeld);
     if (rc != MPQ_OK) return rc;
     const int sms = sm_count();
     if (sms == 0) return MPQ_ERR_CUDA;
-    // As many CTAs to a row as let two share a multiprocessor, more while the device has room and a CTA 8192 elements.
+    // more CTAs to a row while the device has room for all rows' at once and a CTA 8192 elements
     const int64_t chunks = ceil_div((int64_t)g.vocab + E - 1, E);
     g.ctas = 1;
-    while (g.ctas < 8 && (ceil_div(chunks, g.ctas) * 16 > 80000 || (rows * g.ctas * 2 <= sms && g.vocab / g.ctas >= 8192))) g.ctas *= 2;
+    while (g.ctas < 8 && rows * g.ctas <= sms && g.vocab / g.ctas >= 8192) g.ctas *= 2;
     g.warp_chunks = (int)ceil_div(chunks, g.ctas * kSampleWarps);
+    const int share = g.warp_chunks * kSampleWarps * 16;
+    g.list = 512;
+    g.cached = share + g.list * kSampleWarps * 2 <= kSampleHeld;
+    if (!g.cached) g.list = kSampleHeld / (kSampleWarps * 2);
     if (rows * g.ctas > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * g.ctas), 1, 1);
     cfg.blockDim = dim3(kSampleThreads, 1, 1);
-    cfg.dynamicSmemBytes = (size_t)g.warp_chunks * kSampleWarps * 16;
+    cfg.dynamicSmemBytes = (size_t)(g.cached ? share : 0) + (size_t)g.list * kSampleWarps * 2;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -884,13 +963,13 @@ extern "C" int mpq_sample(const void* logits, int64_t ld, int dtype, int64_t row
                           int64_t* tokens, float* logprob, void* stream) {
     if (rows != 0 && (!logits || !uniform || !tokens)) return MPQ_ERR_NULL;
     if (rows < 0 || rows > 0x7fffffff || vocab <= 0 || (rows > 1 && ld < vocab)) return MPQ_ERR_BAD_SHAPE;
-    if (!dtype_ok(dtype) || vocab > 8 * (kSampleMost / dtype_size(dtype))) return MPQ_ERR_UNSUPPORTED;
+    if (!dtype_ok(dtype) || vocab > kSampleMost / (dtype == MPQ_F32 ? 2 : 1)) return MPQ_ERR_UNSUPPORTED;
     if (!aligned_to(logits, dtype_size(dtype)) || !aligned_to(temperature, 4) || !aligned_to(top_k, 4) || !aligned_to(top_p, 4) || !aligned_to(min_p, 4) ||
         !aligned_to(uniform, 4) || !aligned_to(tokens, 8) || !aligned_to(logprob, 4)) return MPQ_ERR_ALIGN;
     if (rows == 0) return MPQ_OK;
     int bits = 0;
     while ((int64_t)1 << bits < vocab) ++bits;
-    const SampleArgs g = {logits, ld, (int)vocab, temperature, top_k, top_p, min_p, uniform, tokens, logprob, 62 - bits > 50 ? 50 : 62 - bits, 1, 0};
+    const SampleArgs g = {logits, ld, (int)vocab, temperature, top_k, top_p, min_p, uniform, tokens, logprob, 62 - bits > 50 ? 50 : 62 - bits, 1, 0, 0, 0};
     if (dtype == MPQ_F32) return launch_sample<float>(g, rows, (cudaStream_t)stream);
     if (dtype == MPQ_F16) return launch_sample<__half>(g, rows, (cudaStream_t)stream);
     return launch_sample<__nv_bfloat16>(g, rows, (cudaStream_t)stream);
