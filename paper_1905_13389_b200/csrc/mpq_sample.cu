@@ -201,11 +201,15 @@ struct SampleRow {
     // f(place of the first, values) for this lane's chunks of the whole share.
     template <typename F>
     __device__ __forceinline__ void each_chunk(F f) const {
-        constexpr int kAtOnce = 2;
+        constexpr int kAtOnce = 8 / E;
+        uint4 next[kAtOnce];
+        read_chunks(min(lane, warp_chunks - 1), next, !cached);
 #pragma unroll 1
         for (int c = lane; c < warp_chunks; c += 32 * kAtOnce) {
             uint4 in[kAtOnce];
-            read_chunks(c, in, !cached);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) in[j] = next[j];
+            read_chunks(min(c + 32 * kAtOnce, warp_chunks - 1), next, !cached);
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
                 float x[E];
@@ -413,38 +417,79 @@ struct SampleRow {
         turn ^= 1;
     }
 
-    // Bin of an element by its distance from `top`, in steps of 1 / steps, the lowest one for all beyond.
-    __device__ __forceinline__ uint32_t bin_of(float x, float top, float steps) const {
-        return kSampleBins - 1 - (__float_as_uint(fminf((top - x) * steps, (float)(kSampleBins - 1)) + 8388608.0f) & (kSampleBins - 1));
+    // Distance of an element from `top` in steps, rounded the same way for equals and never against the order (NaN only for what
+    // is not over -infinity), and its bin, the lowest one for all beyond.
+    static __device__ __forceinline__ float distance(float x, float top, float steps) { return (top - x) * steps; }
+    static __device__ __forceinline__ uint32_t bin_of(float away) {
+        return kSampleBins - 1 - (__float_as_uint(__fadd_rd(fminf(away, (float)(kSampleBins - 1)), 8388608.0f)) & (kSampleBins - 1));
     }
-    // Notes in the list what lies in bin `digit` or above; false, and no list, where this CTA's cannot hold it.
-    __device__ __forceinline__ bool make_list(float top, float steps, uint32_t digit) {
-        constexpr int kAtOnce = 4;
+    // The smallest number whose distance is below `limit` (1 or more), by a warp: distances never grow with the number.
+    __device__ __forceinline__ float nearest_below(float top, float steps, float limit) const {
+        uint32_t lo = 0x00800000u, hi = order_key(top);   // from the lowest finite number on; hi's distance is 0
+        for (int turn = 0; lo < hi && turn < 16; ++turn) {                 // (eight turns at most)
+            const uint32_t step = (hi - lo) / 32 + 1, at = min(lo + lane * step, hi);
+            const uint32_t yes = __ballot_sync(0xffffffffu, at == hi || distance(key_value(at), top, steps) < limit);
+            if (yes == 0) {
+                lo += 31 * step + 1;
+            } else {
+                const uint32_t f = (uint32_t)__ffs(yes) - 1;
+                hi = min(lo + f * step, hi);
+                lo = f == 0 ? hi : min(hi, lo + (f - 1) * step + 1);
+            }
+        }
+        return key_value(hi);
+    }
+    // What lies in bins from `digit` up is this number or more.
+    __device__ __forceinline__ float least_of(float top, float steps, uint32_t digit) const {
+        return digit == 0 ? key_value(0x00800000u) : digit >= kSampleBins ? INFINITY : nearest_below(top, steps, (float)(kSampleBins - (int)digit));
+    }
+    // Notes in the list what is `from_on` or more; false, and no list, where this CTA's cannot hold it.  Four bytes a lane at a time,
+    // so that the places of a warp's vote ascend.
+    __device__ __forceinline__ bool make_list(float from_on) {
+        constexpr int kAtOnce = 8, W = 4 / (int)sizeof(T);
+        const int words = warp_chunks * 4;
+        const bool inside = v0 >= skew && v0 + warp_chunks * E - skew <= vocab;
+        const uint32_t* from = cached ? reinterpret_cast<const uint32_t*>(chunks) : reinterpret_cast<const uint32_t*>(x0 + (v0 - skew));
+        const uint32_t lower = (1u << lane) - 1;
         int have = 0;
 #pragma unroll 1
-        for (int c0 = lane; c0 - lane < warp_chunks; c0 += 32 * kAtOnce) {
-            uint4 in[kAtOnce];
-            read_chunks(min(c0, warp_chunks - 1), in, !cached);
+        for (int c0 = 0; c0 < words; c0 += 32 * kAtOnce) {
+            uint32_t in[kAtOnce];
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
-                const int c = c0 + 32 * j;
-                float x[E];
-                unpack(in[j], x);
-                uint32_t mine = 0;
+                const int c = min(c0 + 32 * j + lane, words - 1);
+                if (cached || inside) {
+                    in[j] = from[c];
+                } else {
+                    T* e = reinterpret_cast<T*>(&in[j]);
 #pragma unroll
-                for (int i = 0; i < E; ++i) mine |= x[i] > -INFINITY && bin_of(x[i], top, steps) >= digit ? 1u << i : 0u;
-                if (c >= warp_chunks) mine = 0;
-                if (!__any_sync(0xffffffffu, mine)) continue;
-                int at = __popc(mine);
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int below = __shfl_up_sync(0xffffffffu, at, o);
-                    if (lane >= o) at += below;
+                    for (int q = 0; q < W; ++q) {
+                        const int i = v0 + c * W + q - skew;
+                        e[q] = i >= 0 && i < vocab ? x0[i] : from_f32<T>(-INFINITY);
+                    }
                 }
-                const int more = __shfl_sync(0xffffffffu, at, 31);
-                at += have - __popc(mine);
-                for (; mine && at < list_size; mine &= mine - 1) list[at++] = (uint16_t)(c * E + __ffs(mine) - 1);
-                have += more;
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int c = c0 + 32 * j + lane;
+                const T* e = reinterpret_cast<const T*>(&in[j]);
+                bool mine[W];
+                uint32_t votes[W], any = 0;
+#pragma unroll
+                for (int q = 0; q < W; ++q) {
+                    mine[q] = c < words && to_f32(e[q]) >= from_on;
+                    votes[q] = __ballot_sync(0xffffffffu, mine[q]);
+                    any |= votes[q];
+                }
+                if (!any) continue;
+                int at = have;
+#pragma unroll
+                for (int q = 0; q < W; ++q) { at += __popc(votes[q] & lower); have += __popc(votes[q]); }
+#pragma unroll
+                for (int q = 0; q < W; ++q) {
+                    if (mine[q] && at < list_size) list[at] = (uint16_t)(c * W + q);
+                    at += mine[q];
+                }
             }
         }
         if (threadIdx.x == 0) sh.longest = 0;
@@ -630,7 +675,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             if (distances) {
 #pragma unroll
                 for (int i = 0; i < E; ++i)
-                    if (x[i] > -INFINITY) atomicAdd(bins + r.bin_of(x[i], top, steps), 1u);
+                    if (x[i] > -INFINITY) atomicAdd(bins + r.bin_of(r.distance(x[i], top, steps)), 1u);
             }
             if (sums) weights += SampleRow<T>::chunk_sum(weight, x);
             if (others) {
@@ -676,11 +721,12 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     // The key, and the place among the equals of it, at which the sum of f from the top reaches `goal`: edge and cut.
     // guess: f, or something near it in 32 bits, one at least, of which the whole row's sum fits 32 bits, in units of `unit` of f's.
     auto narrow = [&](u64 goal, auto f, auto guess, float unit) {
+        if (r.row_sum(r.sum([&](int v, float x) { return kept(v, x) ? f(x) : 0ull; })) <= goal) return;       // all of it stays
         uint32_t over = 1u << (32 - kLowBits), under = 0xffffffffu;        // the border lies below `over` and above `under` (key >> kLowBits)
         u64 base = 0;                                     // f's sum from `over` on
         int64_t bias = 0;                                 // by how much the guesses above `under` fall short
         auto as_counted = [](uint32_t, u64 n) { return n; };
-        for (;;) {                                        // (each turn takes at least one occupied key off the open ones)
+        for (int turns = 0; turns < 1 << 16; ++turns) {   // (each one takes at least one occupied key off the open ones)
             auto open = [&](uint32_t key) { const uint32_t high = key >> kLowBits; return high < over && (under == 0xffffffffu || high > under); };
             const u64 want = (u64)max((int64_t)((double)(goal - base) / (double)unit) - bias, (int64_t)1);
             u64 above1 = 0, above2 = 0;
@@ -760,6 +806,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     auto share = [&](u64 all) { return max(p > 0.0f ? share_of(all, p, true) : 0ull, 1ull); };
     u64 all = 0;                                          // top-p without top-k: what the row weighs
     bool open = some || top_p;                            // whether the first end is still to be found
+    bool summed = all_stay;                               // whether `weights` has what is kept
     int64_t bias = 0;
     int phase = 0;
     const float unit = exp2f((float)g.shift);
@@ -769,7 +816,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         // Where that is too far off, the sums show it, and the next try takes the difference into account.
         auto worth = [&](uint32_t bin, u64 n) -> u64 {
             if (some) return n;
-            return bin == 0 ? 0ull : (u64)((float)n * (fast_exp2(((float)bin - (float)(kSampleBins - 1)) * (1.4426950408889634f / 64.0f)) * unit));
+            return bin == 0 ? 0ull : (u64)((float)n * (fast_exp2(((float)bin - (float)(kSampleBins - 1) - 0.5f) * (1.4426950408889634f / 64.0f)) * unit));
         };
         r.forget_list();
         if (tries > 0) look(true, false, false);
@@ -797,7 +844,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         const uint32_t listed = sh.counts[0], within = sh.counts[1], most = (uint32_t)min(kSampleThreads * kSampleOwn, kSampleMembers * g.ctas);
         // Few: every CTA gets all of them and goes on alone.  Many: the border's bin; the others' sum is taken here.
         const bool few = listed <= most;
-        const bool fits = r.make_list(top, steps, digit);
+        const float outer = r.least_of(top, steps, digit), inner = r.least_of(top, steps, digit + 1);
+        const bool fits = r.make_list(outer);
         if (!few && within > most) break;
         int at = 0;
         if (few) {                                        // noted in ascending places
@@ -818,12 +866,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         u64 s = 0;
         if (few ? fits : true) {
             r.each([&](int v, float x) {
-                const uint32_t bin = r.bin_of(x, top, steps);
-                if (few || (bin == digit && x > -INFINITY)) {
+                if (few || (x >= outer && x < inner)) {
                     const int i = few ? at : atomicAdd(&sh.noted[r.turn], 1);
                     if (i < kSampleMembers) members[i] = SampleRow<T>::code_of(v, x);
                     at += 32;
-                } else if (bin > digit) {
+                } else if (x >= inner) {
                     s += some ? 1ull : weight(x);
                 }
             });
@@ -857,6 +904,18 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         if (!few) {
             edge = (uint32_t)(e >> 32);
             cut = (int)~(uint32_t)e;
+            if (!some && floor_w <= 1) {                  // the sums of what is kept: what lies above, and the kept ones of the border's bin
+                if (threadIdx.x < kSampleWarps) sh.sums[0][0][threadIdx.x] = 0;
+                __syncthreads();
+                for (int i = threadIdx.x; i < sh.noted[noted_turn]; i += kSampleThreads) {
+                    const u64 one = members[i];
+                    if (one >= e) atomicAdd(&sh.sums[0][0][((int)~(uint32_t)one - r.rank * kSampleWarps * g.warp_chunks * E) / (g.warp_chunks * E)],
+                                            weight(key_value((uint32_t)(one >> 32))));
+                }
+                __syncthreads();
+                weights = s + (lane == 0 ? sh.sums[0][0][r.warp] : 0ull);
+                summed = true;
+            }
             break;
         }
         if (some && top_p) {
@@ -902,16 +961,16 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         narrow(share(left), weight,
                [&](float x) { return x > -INFINITY ? max(1u, __float2uint_rn(fast_exp2((x - top) * weight.coolf * 1.4426950408889634f) * per)) : 0u; }, 1.0f / units);
     }
-    if (!some && !top_p && !all_stay) {                   // min-p alone: two bins below its border at most
-        const uint32_t far = (uint32_t)fminf(-64.0f * logf(least) + 2.0f, (float)(kSampleBins - 1));
-        if (least < 1.0f) r.make_list(top, steps, kSampleBins - 1 - far);
+    if (!some && !top_p && !all_stay && least < 1.0f) {   // min-p alone: two steps below its border at most
+        const float far = -64.0f * logf(least) + 2.0f;
+        if (far < 4e6f) r.make_list(r.nearest_below(top, steps, far));
     }
     auto stays = [&](int v, float x) {
         if (!kept(v, x)) return 0ull;
         const u64 w = weight(x);
         return w >= floor_w || v == first ? w : 0ull;
     };
-    const int place = r.running(all_stay ? weights : r.sum(stays), stays, drawn);
+    const int place = r.running(summed ? weights : r.sum(stays), stays, drawn);
     if (place >= 0) finish(place, to_f32(r.x0[place - skew]));
     if (g.ctas > 1) cluster_sync_all();
 }
