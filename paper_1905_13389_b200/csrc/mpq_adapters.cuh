@@ -1,5 +1,7 @@
 // Low-rank adapters of a product of level bytes: what its two kernels share.
 #pragma once
+#include <type_traits>
+
 #include "mpq_levels.cuh"
 
 namespace mpq {

@@ -27,26 +27,6 @@ struct LinearArgs {
     const float* z = nullptr; const int32_t* chosen = nullptr;    // per token: what its adapter has made of it [rank], which one (-1: none)
 };
 
-// What the adapter of token r adds to column c; W: the type of its elements, void for a product without adapters.
-template <typename W>
-__device__ __forceinline__ float low_rank(const LinearArgs& g, int64_t r, int64_t c) {
-    if constexpr (std::is_void_v<W>) {
-        return 0.0f;
-    } else {
-        const int id = __ldg(g.chosen + r);
-        if (id < 0) return 0.0f;
-        const W* up = static_cast<const W*>(g.up) + ((int64_t)id * g.n + c) * g.rank;
-        float sum = 0.0f;
-        for (int i = 0; i < g.rank; i += 8) {
-            float u[8];
-            load_vec<W, 8>(up + i, u);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(u[j], __ldg(g.z + r * g.rank + i + j), sum);
-        }
-        return sum;
-    }
-}
-
 // acc (levels u, unsigned) -> one output, in the header's order of operations
 struct RowTerm { float scale; uint32_t term; };          // a_scale / L_a;  k L_a L_w - 2 L_w sums_a
 struct ColTerm { float scale; uint32_t term; float bias; };   // w_scale / L_w;  2 L_a sums_w;  bias
@@ -125,7 +105,55 @@ template <int BN> struct SmallShape {
     static constexpr int stage_bytes = (128 + BN) * kBlock;
     static constexpr int exchange_bytes = BN * 128 * 4;   // [S source CTAs][BN / S rows][128 columns] int32
     static constexpr int smem = stages * stage_bytes + exchange_bytes + 1024;
+    static constexpr int low_bytes = BN * 128 * 4;        // [BN rows][128 columns] fp32: what the adapters add
 };
+
+// What the adapters of rows row0 + first .. + count add to column c, to low[row][..] of this thread's own column: each row's z
+// (the same address in all lanes) times the column's row of `up`, in fp32.  Four rows at once, so that as many reads of `up` are
+// under way; it runs beside the products.
+template <typename W>
+__device__ __forceinline__ void low_rank_rows(const LinearArgs& g, int64_t row0, int first, int count, int64_t c, float* low) {
+    constexpr int kRows = 4;
+    const W* up = static_cast<const W*>(g.up) + min(c, g.n - 1) * g.rank;
+#pragma unroll 1
+    for (int r = first; r < first + count; r += kRows) {
+        int id[kRows];
+        float sum[kRows] = {};
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+            id[j] = r + j < first + count && row0 + r + j < g.m ? __ldg(g.chosen + row0 + r + j) : -1;
+            any |= id[j] >= 0;
+        }
+        if (any)
+#pragma unroll 1
+            for (int i = 0; i < g.rank; i += 16) {
+                uint4 u[kRows][2];
+#pragma unroll
+                for (int j = 0; j < kRows; ++j) {
+                    const uint4* from = reinterpret_cast<const uint4*>(up + (int64_t)max(id[j], 0) * g.n * g.rank + i);
+                    u[j][0] = __ldg(from);
+                    u[j][1] = __ldg(from + 1);
+                }
+#pragma unroll
+                for (int j = 0; j < kRows; ++j)
+                    if (id[j] >= 0) {
+                        const float4* z = reinterpret_cast<const float4*>(g.z + (row0 + r + j) * g.rank + i);
+                        const W* e = reinterpret_cast<const W*>(u[j]);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const float4 v = __ldg(z + q);
+                            sum[j] = fmaf(to_f32(e[4 * q]), v.x, sum[j]);
+                            sum[j] = fmaf(to_f32(e[4 * q + 1]), v.y, sum[j]);
+                            sum[j] = fmaf(to_f32(e[4 * q + 2]), v.z, sum[j]);
+                            sum[j] = fmaf(to_f32(e[4 * q + 3]), v.w, sum[j]);
+                        }
+                    }
+            }
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) if (r + j < first + count) low[(r + j) * 128] = sum[j];
+    }
+}
 
 // `count` of N results of one column, rows r .. : the residuals are all read before the first result is written
 // (they may be the same tensor, so the compiler cannot move a load over a store).
@@ -161,6 +189,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     const uint32_t ring = (smem_addr(smem_raw) + 1023u) & ~1023u;
     const uint32_t exchange = ring + kStages * Shape::stage_bytes;
     uint32_t* exchange_ptr = reinterpret_cast<uint32_t*>(smem_raw + (exchange - smem_addr(smem_raw)));
+    [[maybe_unused]] float* low = reinterpret_cast<float*>(exchange_ptr) + Shape::exchange_bytes / 4;        // [BN][128]: what the adapters add
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     auto full = [&](int s) { return smem_addr(&bars[s]); };
     auto empty = [&](int s) { return smem_addr(&bars[kStages + s]); };
@@ -236,6 +265,8 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         const int64_t c = (int64_t)n0 + col;
         ColTerm ct = {0.0f, 0u, 0.0f};
         if (c < g.n) ct = col_term(g, c);
+        const int own = BN / splits;
+        if constexpr (!std::is_void_v<W>) low_rank_rows<W>(g, m0, split * own, own, c, low + col);
         bool ok = mbar_wait_warp(done, 0, &failed, g.polls);
         if (!ok) mbar_wait(done, 0);                      // what has been issued must end before TMEM is freed
         ok = ok && !__any_sync(0xffffffffu, has_failed());
@@ -244,7 +275,6 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             if (splits > 1 && lane < splits) st_cluster(map_to_cta(smem_addr(&peer_failed), (uint32_t)lane), 1u);
         }
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-        const int own = BN / splits;
         {
             tmem_fence_after();
 #pragma unroll 1
@@ -258,7 +288,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                     for (int j = 0; j < 16; ++j) f[j] = linear_value(g, v[j], RowTerm{row_scale[r0 + j], row_terms[r0 + j]}, ct);
                     if constexpr (!std::is_void_v<W>) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) if (c < g.n && m0 + r0 + j < g.m) f[j] += low_rank<W>(g, m0 + r0 + j, c);
+                        for (int j = 0; j < 16; ++j) f[j] += low[(r0 + j) * 128 + col];
                     }
                     glue_values(f, g.glue);
                     store_column<T, 16>(g, f, (int64_t)m0 + r0, c, (int)min((int64_t)16, g.m - m0 - r0));
@@ -295,7 +325,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                     }
                     if constexpr (!std::is_void_v<W>) {
 #pragma unroll
-                        for (int j = 0; j < N; ++j) if (m0 + rr + j < g.m) f[j] += low_rank<W>(g, m0 + rr + j, c);
+                        for (int j = 0; j < N; ++j) f[j] += low[(rr + j) * 128 + col];
                     }
                     glue_values(f, g.glue);
                     store_column<T, N>(g, f, (int64_t)m0 + rr, c, (int)min((int64_t)N, g.m - m0 - rr));
@@ -331,7 +361,83 @@ struct PairShape {
     static constexpr int row_words = 64;                            // column pair p of row r lies at pair p ^ r: no bank conflicts either way
     static constexpr int transpose_bytes = kPairStoreWarps / 2 * 32 * row_words * 4;
     static constexpr int smem = stages * stage_bytes + transpose_bytes + 1024;
+    static constexpr int term_bytes = kPairStoreWarps / 2 * 64 * 16;     // with adapters: the columns' constants
 };
+
+// What the adapters of 16 rows add to 64 columns, into TMEM lanes and columns from `at` on: z times the columns' rows of `up` as
+// 16 x 8 x 8 matrix instructions on tf32, which holds 16-bit types whole; z, in two such parts, to 2^-22 of itself whatever its
+// size.  A lane owns four adjacent ranks of 16, in both operands alike.  One adapter after the other of those that the rows
+// have: a row takes its own one's sums alone, so that nothing of another's reaches it.
+// (fp32 multiply-adds instead would take 2 rank / 32 instructions an output for 0.6 rank / 16 here: rank 64 then costs more
+// than the product that it runs beside.)
+__device__ __forceinline__ uint32_t as_tf32(float v) {
+    uint32_t r;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ void mma_16x8x8(uint32_t* d, const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    float* f = reinterpret_cast<float*>(d);
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <typename W>
+__device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0, int64_t c0, uint32_t at, int lane) {
+    const int row = lane >> 2, quad = lane & 3;
+    const int id = lane < 16 && row0 + lane < g.m ? __ldg(g.chosen + row0 + lane) : -1;
+    uint32_t left = __ballot_sync(0xffffffffu, id >= 0);
+    bool begun = false;
+    do {
+        uint32_t acc[32] = {};                             // as the instruction leaves them and TMEM takes them: 4 j + 2 h + e is row + 8 h, column 8 j + 2 quad + e
+        uint32_t rows = 0xffffu;
+        if (left) {
+            const int which = __shfl_sync(0xffffffffu, id, __ffs(left) - 1);
+            rows = __ballot_sync(0xffffffffu, id == which);
+            left &= ~rows;
+            const W* up = static_cast<const W*>(g.up) + (int64_t)which * g.n * g.rank + 4 * quad;
+#pragma unroll 1
+            for (int i = 0; i < g.rank; i += 16) {
+                uint2 u[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) u[j] = __ldg(reinterpret_cast<const uint2*>(up + min(c0 + 8 * j + row, g.n - 1) * g.rank + i));
+                uint32_t part[2][2][4];                    // [leading and trailing part][first and second 8 ranks]
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float4 v = __ldg(reinterpret_cast<const float4*>(g.z + min(row0 + row + 8 * h, g.m - 1) * g.rank + 4 * quad + i));
+                    const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {          // element q: instruction q / 2, its k of lane `quad` or of quad + 4
+                        const uint32_t lead = as_tf32(e[q]);
+                        const float rest = e[q] - __uint_as_float(lead);
+                        part[0][q >> 1][h + 2 * (q & 1)] = lead;
+                        part[1][q >> 1][h + 2 * (q & 1)] = as_tf32(ordinary(rest) ? rest : 0.0f);      // of an infinity nothing is left
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const W* e = reinterpret_cast<const W*>(&u[j]);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const uint32_t b0 = __float_as_uint(to_f32(e[2 * s])), b1 = __float_as_uint(to_f32(e[2 * s + 1]));
+                        mma_16x8x8(acc + 4 * j, part[1][s], b0, b1);
+                        mma_16x8x8(acc + 4 * j, part[0][s], b0, b1);
+                    }
+                }
+            }
+        }
+        if (rows != 0xffffu) {
+            uint32_t before[32] = {};
+            if (begun) {
+                tmem_load_frag(at, before);
+                tmem_wait_ld();
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[i] = rows >> (row + 8 * ((i >> 1) & 1)) & 1 ? acc[i] : before[i];
+        }
+        tmem_store_frag(at, acc);
+        tmem_wait_st();
+        begun = true;
+    } while (left);
+}
 
 template <typename T, typename W>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
@@ -363,7 +469,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         tma_prefetch(&map_a);
         tma_prefetch(&map_w);
     }
-    if (warp == 0) tmem_alloc<2>(&tmem_holder, kAccs * BN);
+    constexpr uint32_t kTmemCols = kAccs * BN * (std::is_void_v<W> ? 1 : 2);       // what the adapters add lies behind the accumulators
+    if (warp == 0) tmem_alloc<2>(&tmem_holder, kTmemCols);
     tmem_fence_before();
     cluster_sync_all();                                    // both CTAs' barriers exist
     tmem_fence_after();
@@ -454,27 +561,51 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             const int rows = (int)min((int64_t)32, g.m - row0);                    // 0 or less: none of them exists
             RowTerm mine = {0.0f, 0u};                                             // lane's row; handed round by shuffles
             if (lane < rows) mine = row_term(g, row0 + lane);
+            const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+            [[maybe_unused]] float4* terms = reinterpret_cast<float4*>(transpose + kPairStoreWarps / 2 * 32 * Shape::row_words) + block * 64;
+            if constexpr (!std::is_void_v<W>) {
+                // What the adapters add, while the tile is multiplied.  Their sums lie by rows, so the columns' constants are needed
+                // by rows too: this warp's 32 columns of them.
+                const int64_t c = (int64_t)n0 + c0 + part * 32 + lane;
+                const ColTerm t = c < g.n ? col_term(g, c) : ColTerm{0.0f, 0u, 0.0f};
+                terms[part * 32 + lane] = make_float4(t.scale, __uint_as_float(t.term), t.bias, 0.0f);
+                tmem_fence_after();                        // (the block has read what the tile before had there)
+                low_rank_tile<W>(g, row0 + part * 16, (int64_t)n0 + c0, lanes + ((uint32_t)(part * 16) << 16) + (uint32_t)(kAccs * BN + c0), lane);
+                tmem_fence_before();
+                block_sync();
+                tmem_fence_after();
+            }
             ok = ok && mbar_wait_warp(acc_full(acc), (i >> 1) & 1, &failed, g.polls) && !__any_sync(0xffffffffu, has_failed());
             const int64_t cx = (int64_t)n0 + c0 + ca, cy = (int64_t)n0 + c0 + cb;
             const bool in_x = cx < g.n, in_y = cy < g.n;
             ColTerm ct[2] = {{0.0f, 0u, 0.0f}, {0.0f, 0u, 0.0f}};
-            if (in_x) ct[0] = col_term(g, cx);
-            if (in_y) ct[1] = col_term(g, cy);
+            if (std::is_void_v<W> && in_x) ct[0] = col_term(g, cx);
+            if (std::is_void_v<W> && in_y) ct[1] = col_term(g, cy);
             const bool fast = twos && n0 + c0 + 64 <= g.n;
             if (ok) {
                 tmem_fence_after();
                 uint32_t v[32];
-                tmem_load32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + c0 + part * 32), v);
+                tmem_load32(lanes + (uint32_t)(acc * BN + c0 + part * 32), v);
+                [[maybe_unused]] uint32_t low[32];
+                if constexpr (!std::is_void_v<W>) tmem_load32(lanes + (uint32_t)(kAccs * BN + c0 + part * 32), low);
                 tmem_wait_ld();
                 tmem_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(acc), 0));       // this warp's part of the accumulator is read
+                if constexpr (!std::is_void_v<W>) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const float4 t = terms[part * 32 + j];
+                        v[j] = __float_as_uint(linear_value(g, v[j], mine, ColTerm{t.x, __float_as_uint(t.y), t.z}) + __uint_as_float(low[j]));
+                    }
+                }
 #pragma unroll
                 for (int j = 0; j < 32; j += 2)
                     *reinterpret_cast<uint2*>(sh + lane * Shape::row_words + 2 * ((part * 16 + j / 2) ^ lane)) = make_uint2(v[j], v[j + 1]);
             }
             // (the other warp of the block may have given up: half of the columns are missing then)
-            if (!block_all(ok)) ct[0].scale = ct[1].scale = kNaN;
+            const bool all_ok = block_all(ok);
+            if (!all_ok) ct[0].scale = ct[1].scale = kNaN;
             {
                 // kRowsAtOnce rows at a time.  All residuals of a group are requested before any is used or any result is
                 // written: they may lie in the result's own tensor, so the compiler could not move a load up by itself, and
@@ -508,15 +639,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                             v.x = sh[r * Shape::row_words + 2 * ((ca >> 1) ^ r) + (ca & 1)];
                             v.y = sh[r * Shape::row_words + 2 * ((cb >> 1) ^ r) + (cb & 1)];
                         }
-                        const RowTerm rt = {__shfl_sync(0xffffffffu, mine.scale, r), __shfl_sync(0xffffffffu, mine.term, r)};
-                        f[2 * j] = linear_value(g, v.x, rt, ct[0]);
-                        f[2 * j + 1] = linear_value(g, v.y, rt, ct[1]);
-                    }
-                    if constexpr (!std::is_void_v<W>) {
-#pragma unroll
-                        for (int j = 0; j < kRowsAtOnce; ++j) {
-                            if (r0 + j < rows && in_x) f[2 * j] += low_rank<W>(g, row0 + r0 + j, cx);
-                            if (r0 + j < rows && in_y) f[2 * j + 1] += low_rank<W>(g, row0 + r0 + j, cy);
+                        if constexpr (std::is_void_v<W>) {
+                            const RowTerm rt = {__shfl_sync(0xffffffffu, mine.scale, r), __shfl_sync(0xffffffffu, mine.term, r)};
+                            f[2 * j] = linear_value(g, v.x, rt, ct[0]);
+                            f[2 * j + 1] = linear_value(g, v.y, rt, ct[1]);
+                        } else {
+                            f[2 * j] = all_ok ? __uint_as_float(v.x) : kNaN;
+                            f[2 * j + 1] = all_ok ? __uint_as_float(v.y) : kNaN;
                         }
                     }
                     glue_values(f, g.glue);
@@ -557,7 +686,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         cluster_sync_all();
         tmem_fence_after();
     }
-    if (warp == 0) tmem_free<2>(tmem, kAccs * BN);
+    if (warp == 0) tmem_free<2>(tmem, kTmemCols);
     if (threadIdx.x == 0 && failed) atomicAdd(&g_wait_failures, 1u);
 }
 
@@ -573,7 +702,8 @@ int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
     using Shape = SmallShape<BN>;
     static PerDeviceOnce once;
     auto* kernel = linear_small_kernel<T, W, BN>;
-    int rc = once.raise_smem_limit(kernel, Shape::smem);
+    constexpr int smem = Shape::smem + (std::is_void_v<W> ? 0 : Shape::low_bytes);
+    int rc = once.raise_smem_limit(kernel, smem);
     if (rc != MPQ_OK) return rc;
     CUtensorMap map_w, map_a;
     if (!byte_tensor_map(&map_w, g.w, g.n, g.row_bytes, 128) || !byte_tensor_map(&map_a, g.a, g.m, g.row_bytes, BN)) return MPQ_ERR_CUDA;
@@ -585,7 +715,7 @@ int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * splits), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = Shape::smem;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -605,7 +735,8 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     constexpr int BN = kPairCols;
     static PerDeviceOnce once;
     auto* kernel = linear_pair_kernel<T, W>;
-    int rc = once.raise_smem_limit(kernel, Shape::smem);
+    constexpr int smem = Shape::smem + (std::is_void_v<W> ? 0 : Shape::term_bytes);
+    int rc = once.raise_smem_limit(kernel, smem);
     if (rc != MPQ_OK) return rc;
     CUtensorMap map_w, map_a;
     if (!byte_tensor_map(&map_w, g.w, g.n, g.row_bytes, BN / 2) || !byte_tensor_map(&map_a, g.a, g.m, g.row_bytes, 128)) return MPQ_ERR_CUDA;
@@ -614,7 +745,7 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     const int64_t tiles_m = ceil_div(g.m, 256), tiles = tiles_m * ceil_div(g.n, BN);
     if (tiles > (1 << 28)) return MPQ_ERR_BAD_SHAPE;
     const unsigned ctas = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
-    return launch_chained_as(true, kernel, ctas, (unsigned)kPairThreads, Shape::smem, st, map_a, map_w, g, (int)tiles_m, (int)tiles);
+    return launch_chained_as(true, kernel, ctas, (unsigned)kPairThreads, smem, st, map_a, map_w, g, (int)tiles_m, (int)tiles);
 }
 
 // Which form.  Up to 64 rows the weights' own traffic decides: the small form, its tile just wide enough.  Above, the
