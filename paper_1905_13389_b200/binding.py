@@ -833,7 +833,7 @@ def linear_adapted(a: Levels, w: Levels, low: Adapters, q_starts: torch.Tensor, 
         dtype = out.dtype
     po, ldo = _rows(out, m, n, dtype, dev)
     if workspace is None:
-        need = (m * (rank + 1) * 4 + 15) // 16 * 16       # = linear_adapted_workspace(m, rank)
+        need = (m * (10 * rank + 8) + 15) // 16 * 16      # = linear_adapted_workspace(m, rank)
         workspace = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=a.bytes.device)
     st = (_lib or lib()).mpq_linear_adapted(
         *pa, a.bits, *pw, w.bits, m, n, k, _vector(down, count * rank * row, wtype, dev), _vector(up, count * n * rank, wtype, dev), _dtype(wtype),

@@ -24,7 +24,8 @@ struct LinearArgs {
     void* out; int64_t ldo;
     uint32_t polls;                                       // limit of a wait
     const void* up = nullptr; int rank = 0;               // adapters: [..][n][rank]
-    const float* z = nullptr; const int32_t* chosen = nullptr;    // per token: what its adapter has made of it [rank], which one (-1: none)
+    int adapters = 0;
+    LowWorkspace low = {};                                // what the adapters have made of the tokens
 };
 
 // acc (levels u, unsigned) -> one output, in the header's order of operations
@@ -122,7 +123,8 @@ __device__ __forceinline__ void low_rank_rows(const LinearArgs& g, int64_t row0,
         bool any = false;
 #pragma unroll
         for (int j = 0; j < kRows; ++j) {
-            id[j] = r + j < first + count && row0 + r + j < g.m ? __ldg(g.chosen + row0 + r + j) : -1;
+            id[j] = r + j < first + count && row0 + r + j < g.m ? __ldg(g.low.chosen + row0 + r + j) : -1;
+            if (id[j] >= g.adapters) id[j] = -1;
             any |= id[j] >= 0;
         }
         if (any)
@@ -138,7 +140,7 @@ __device__ __forceinline__ void low_rank_rows(const LinearArgs& g, int64_t row0,
 #pragma unroll
                 for (int j = 0; j < kRows; ++j)
                     if (id[j] >= 0) {
-                        const float4* z = reinterpret_cast<const float4*>(g.z + (row0 + r + j) * g.rank + i);
+                        const float4* z = reinterpret_cast<const float4*>(g.low.z + (row0 + r + j) * g.rank + i);
                         const W* e = reinterpret_cast<const W*>(u[j]);
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
@@ -209,7 +211,14 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     else __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = tmem_holder;
-    chain_entry();
+    // With adapters the kernel before has made z, and was let in only when those before it had ended: the operands are there, and
+    // only the storing warps wait.
+    if constexpr (std::is_void_v<W>) {
+        chain_entry();
+    } else {
+        chain_next();
+        if (warp >= 2) chain_wait();
+    }
 
     const int split = splits > 1 ? (int)cluster_rank() : 0;
     const int tile = (int)blockIdx.x / splits;
@@ -364,66 +373,51 @@ struct PairShape {
     static constexpr int term_bytes = kPairStoreWarps / 2 * 64 * 16;     // with adapters: the columns' constants
 };
 
-// What the adapters of 16 rows add to 64 columns, into TMEM lanes and columns from `at` on: z times the columns' rows of `up` as
-// 16 x 8 x 8 matrix instructions on tf32, which holds 16-bit types whole; z, in two such parts, to 2^-22 of itself whatever its
-// size.  A lane owns four adjacent ranks of 16, in both operands alike.  One adapter after the other of those that the rows
-// have: a row takes its own one's sums alone, so that nothing of another's reaches it.
-// (fp32 multiply-adds instead would take 2 rank / 32 instructions an output for 0.6 rank / 16 here: rank 64 then costs more
-// than the product that it runs beside.)
-__device__ __forceinline__ uint32_t as_tf32(float v) {
-    uint32_t r;
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(v));
-    return r;
-}
-__device__ __forceinline__ void mma_16x8x8(uint32_t* d, const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    float* f = reinterpret_cast<float*>(d);
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-template <typename W>
+// What the adapters of 16 rows add to 64 columns, into TMEM lanes and columns from `at` on: the parts of z times the columns'
+// rows of `up` as 16 x 8 x 16 matrix instructions.  A lane owns four adjacent ranks of 16, in both operands alike.  One
+// adapter after the other of those that the rows have: a row takes its own one's sums alone, so that nothing of another's
+// reaches it.  PARTS: 16-bit results need two parts of z (2^-16 of it, 2^-22 in float16), 32-bit ones all.
+// (fp32 multiply-adds instead would take 2 rank / 32 instructions an output for some rank / 250 here; products on tf32, whose
+// range needs no parts' exponent, took twice the time of these and kept the tensor cores from the product itself.)
+template <typename W, int PARTS>
 __device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0, int64_t c0, uint32_t at, int lane) {
     const int row = lane >> 2, quad = lane & 3;
-    const int id = lane < 16 && row0 + lane < g.m ? __ldg(g.chosen + row0 + lane) : -1;
+    int id = lane < 16 && row0 + lane < g.m ? __ldg(g.low.chosen + row0 + lane) : -1;
+    if (id >= g.adapters) id = -1;
     uint32_t left = __ballot_sync(0xffffffffu, id >= 0);
+    const int64_t z0 = min(row0 + row, g.m - 1), z1 = min(row0 + row + 8, g.m - 1);
     bool begun = false;
     do {
-        uint32_t acc[32] = {};                             // as the instruction leaves them and TMEM takes them: 4 j + 2 h + e is row + 8 h, column 8 j + 2 quad + e
+        float acc[32] = {};                                // as the instruction leaves them and TMEM takes them: 4 j + 2 h + e is row + 8 h, column 8 j + 2 quad + e
         uint32_t rows = 0xffffu;
         if (left) {
             const int which = __shfl_sync(0xffffffffu, id, __ffs(left) - 1);
             rows = __ballot_sync(0xffffffffu, id == which);
             left &= ~rows;
             const W* up = static_cast<const W*>(g.up) + (int64_t)which * g.n * g.rank + 4 * quad;
+            const W* z = reinterpret_cast<const W*>(g.low.parts) + 4 * quad;
 #pragma unroll 1
             for (int i = 0; i < g.rank; i += 16) {
-                uint2 u[8];
+                uint2 u[8], a[PARTS][2];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) u[j] = __ldg(reinterpret_cast<const uint2*>(up + min(c0 + 8 * j + row, g.n - 1) * g.rank + i));
-                uint32_t part[2][2][4];                    // [leading and trailing part][first and second 8 ranks]
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float4 v = __ldg(reinterpret_cast<const float4*>(g.z + min(row0 + row + 8 * h, g.m - 1) * g.rank + 4 * quad + i));
-                    const float e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {          // element q: instruction q / 2, its k of lane `quad` or of quad + 4
-                        const uint32_t lead = as_tf32(e[q]);
-                        const float rest = e[q] - __uint_as_float(lead);
-                        part[0][q >> 1][h + 2 * (q & 1)] = lead;
-                        part[1][q >> 1][h + 2 * (q & 1)] = as_tf32(ordinary(rest) ? rest : 0.0f);      // of an infinity nothing is left
-                    }
+                for (int q = 0; q < PARTS; ++q) {
+                    a[q][0] = __ldg(reinterpret_cast<const uint2*>(z + (q * g.m + z0) * g.rank + i));
+                    a[q][1] = __ldg(reinterpret_cast<const uint2*>(z + (q * g.m + z1) * g.rank + i));
                 }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const W* e = reinterpret_cast<const W*>(&u[j]);
+                for (int q = PARTS - 1; q >= 0; --q)
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const uint32_t b0 = __float_as_uint(to_f32(e[2 * s])), b1 = __float_as_uint(to_f32(e[2 * s + 1]));
-                        mma_16x8x8(acc + 4 * j, part[1][s], b0, b1);
-                        mma_16x8x8(acc + 4 * j, part[0][s], b0, b1);
-                    }
-                }
+                    for (int j = 0; j < 8; ++j) mma_16x8x16<W>(acc + 4 * j, a[q][0].x, a[q][1].x, a[q][0].y, a[q][1].y, u[j].x, u[j].y);
             }
+            const float s0 = __ldg(g.low.scale + z0), s1 = __ldg(g.low.scale + z1);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[i] *= (i >> 1) & 1 ? s1 : s0;
         }
+        uint32_t sums[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sums[i] = __float_as_uint(acc[i]);
         if (rows != 0xffffu) {
             uint32_t before[32] = {};
             if (begun) {
@@ -431,9 +425,9 @@ __device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0,
                 tmem_wait_ld();
             }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) acc[i] = rows >> (row + 8 * ((i >> 1) & 1)) & 1 ? acc[i] : before[i];
+            for (int i = 0; i < 32; ++i) sums[i] = rows >> (row + 8 * ((i >> 1) & 1)) & 1 ? sums[i] : before[i];
         }
-        tmem_store_frag(at, acc);
+        tmem_store_frag(at, sums);
         tmem_wait_st();
         begun = true;
     } while (left);
@@ -475,7 +469,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     cluster_sync_all();                                    // both CTAs' barriers exist
     tmem_fence_after();
     const uint32_t tmem = tmem_holder;
-    chain_entry();
+    if constexpr (std::is_void_v<W>) {
+        chain_entry();
+    } else {                                               // (see linear_small_kernel)
+        chain_next();
+        if (warp >= 2) chain_wait();
+    }
 
     const int pair = (int)blockIdx.x / 2, pairs = (int)gridDim.x / 2;
     const int my_tiles = tiles > pair ? (tiles - pair + pairs - 1) / pairs : 0;
@@ -570,7 +569,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 const ColTerm t = c < g.n ? col_term(g, c) : ColTerm{0.0f, 0u, 0.0f};
                 terms[part * 32 + lane] = make_float4(t.scale, __uint_as_float(t.term), t.bias, 0.0f);
                 tmem_fence_after();                        // (the block has read what the tile before had there)
-                low_rank_tile<W>(g, row0 + part * 16, (int64_t)n0 + c0, lanes + ((uint32_t)(part * 16) << 16) + (uint32_t)(kAccs * BN + c0), lane);
+                low_rank_tile<W, std::is_same_v<W, __nv_bfloat16> && std::is_same_v<T, float> ? kLowParts : 2>(g, row0 + part * 16, (int64_t)n0 + c0, lanes + ((uint32_t)(part * 16) << 16) + (uint32_t)(kAccs * BN + c0), lane);
                 tmem_fence_before();
                 block_sync();
                 tmem_fence_after();
@@ -801,7 +800,7 @@ extern "C" int mpq_linear_levels(const uint8_t* a, const float* a_scale, const i
 }
 
 extern "C" int64_t mpq_linear_adapted_workspace(int64_t m, int rank) {
-    return m <= 0 || rank <= 0 ? 0 : (m * (rank + 1) * 4 + 15) / 16 * 16;
+    return m <= 0 || rank <= 0 ? 0 : LowWorkspace::bytes(m, rank);
 }
 
 extern "C" int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const int32_t* a_sums, int a_bits,
@@ -822,11 +821,9 @@ extern "C" int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const 
     if (workspace_bytes < mpq_linear_adapted_workspace(m, rank)) return MPQ_ERR_WORKSPACE;
     g.up = up;
     g.rank = rank;
-    float* z = static_cast<float*>(workspace);
-    int32_t* chosen = reinterpret_cast<int32_t*>(z + m * rank);
-    g.z = z;
-    g.chosen = chosen;
-    const AdapterArgs d = {a, a_scale, g.La, m, k, g.row_bytes, down, factor, adapters, rank, q_starts, ids, batch, z, chosen};
+    g.adapters = adapters;
+    g.low = LowWorkspace(workspace, m, rank);
+    const AdapterArgs d = {a, a_scale, g.La, m, g.row_bytes, down, factor, adapters, rank, q_starts, ids, batch, g.low};
     rc = adapter_down(d, adapter_dtype, (cudaStream_t)stream);
     if (rc != MPQ_OK) return rc;
     return adapter_dtype == MPQ_F16 ? launch_linear_typed<__half>(g, dtype, (cudaStream_t)stream) : launch_linear_typed<__nv_bfloat16>(g, dtype, (cudaStream_t)stream);
