@@ -743,7 +743,7 @@ class PagePlan(NamedTuple):
 
 class Adapters(NamedTuple):
     """Low-rank adapters as a product takes them: down [adapters][rank][level_row_bytes(k)] and up [adapters][n][rank] of
-    float16 or bfloat16, rank a multiple of 16, scale float32 [adapters] or None.  See :func:`adapters`."""
+    float16 or bfloat16, rank 16, 32, 64 or 128, scale float32 [adapters] or None.  See :func:`adapters`."""
     down: torch.Tensor
     up: torch.Tensor
     scale: Optional[torch.Tensor]
@@ -797,13 +797,13 @@ def pages_trim(state: PageState, seqs: Optional[torch.Tensor], keep: torch.Tenso
 
 def adapters(down: torch.Tensor, up: torch.Tensor, scale: Optional[torch.Tensor] = None) -> Adapters:
     """Lays adapters out once: down [adapters][rank][k] and up [adapters][n][rank] (float16 or bfloat16) padded with zeros to
-    whole 16s of rank and k."""
+    a rank of 16, 32, 64 or 128 and to whole 16s of k."""
     count, rank, k = down.shape
     if up.shape[0] != count or up.shape[2] != rank or up.dtype != down.dtype or (scale is not None and scale.shape != (count,)):
         raise ValueError("expected down [adapters][rank][k], up [adapters][n][rank] of one type and scale [adapters], got %s %s, %s %s" % (
             down.dtype, tuple(down.shape), up.dtype, tuple(up.shape)))
-    pad = torch.nn.functional.pad
-    return Adapters(pad(down, (0, -k % 16, 0, -rank % 16)).contiguous(), pad(up, (0, -rank % 16)).contiguous(),
+    pad, wide = torch.nn.functional.pad, max(16, 1 << (rank - 1).bit_length())
+    return Adapters(pad(down, (0, -k % 16, 0, wide - rank)).contiguous(), pad(up, (0, wide - rank)).contiguous(),
                     None if scale is None else scale.float().contiguous(), k)
 
 

@@ -76,13 +76,13 @@ __global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const Adapte
     const int64_t kb0 = blocks * split / splits, kb1 = blocks * (split + 1) / splits;
     const float L = (float)g.La;
     float acc[MT][NT][4] = {};
-    for (int64_t kb = kb0 + part; kb < kb1; kb += parts) {
+    struct Block { uint4 a[MT][2][2], u[NT]; };
+    auto ask = [&](int64_t kb, Block& x) {
         const int64_t at = kb * 64 + quad * 16;
-        const bool in = at < g.row_bytes;
-        uint4 a[MT][2][2], u[NT];
+        const bool in = kb < kb1 && at < g.row_bytes;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-            u[j] = in ? __ldg(reinterpret_cast<const uint4*>(levels + min(j * 8 + row, count - 1) * g.row_bytes + at)) : make_uint4(0, 0, 0, 0);
+            x.u[j] = in ? __ldg(reinterpret_cast<const uint4*>(levels + min(j * 8 + row, count - 1) * g.row_bytes + at)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -90,18 +90,36 @@ __global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const Adapte
                 const int r = r0 + i * 16 + h * 8 + row;
                 const uint4* from = reinterpret_cast<const uint4*>(down + (int64_t)r * g.row_bytes + at);
 #pragma unroll
-                for (int q = 0; q < 2; ++q) a[i][h][q] = in && r < g.rank ? __ldg(from + q) : make_uint4(0, 0, 0, 0);
+                for (int q = 0; q < 2; ++q) x.a[i][h][q] = in && r < g.rank ? __ldg(from + q) : make_uint4(0, 0, 0, 0);
             }
+    };
+    auto multiply = [&](const Block& x) {
 #pragma unroll
         for (int s = 0; s < 4; ++s)                       // four of the sixteen k at a time
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const uint32_t x0 = odd_pair<W>(word_of(u[j], s), 0, L), x1 = odd_pair<W>(word_of(u[j], s), 2, L);
+                const uint32_t x0 = odd_pair<W>(word_of(x.u[j], s), 0, L), x1 = odd_pair<W>(word_of(x.u[j], s), 2, L);
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
-                    mma_16x8x16<W>(acc[i][j], word_of(a[i][0][s >> 1], 2 * (s & 1)), word_of(a[i][1][s >> 1], 2 * (s & 1)),
-                                   word_of(a[i][0][s >> 1], 2 * (s & 1) + 1), word_of(a[i][1][s >> 1], 2 * (s & 1) + 1), x0, x1);
+                    mma_16x8x16<W>(acc[i][j], word_of(x.a[i][0][s >> 1], 2 * (s & 1)), word_of(x.a[i][1][s >> 1], 2 * (s & 1)),
+                                   word_of(x.a[i][0][s >> 1], 2 * (s & 1) + 1), word_of(x.a[i][1][s >> 1], 2 * (s & 1) + 1), x0, x1);
             }
+    };
+    if constexpr (NT == 1) {                              // several blocks on their way: these pieces are bound by latency
+        constexpr int kAhead = MT == 1 ? 4 : 2;
+        for (int64_t kb = kb0 + part; kb < kb1; kb += kAhead * parts) {
+            Block x[kAhead];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) ask(kb + q * parts, x[q]);
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) multiply(x[q]);
+        }
+    } else {
+        for (int64_t kb = kb0 + part; kb < kb1; kb += parts) {
+            Block x;
+            ask(kb, x);
+            multiply(x);
+        }
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i)

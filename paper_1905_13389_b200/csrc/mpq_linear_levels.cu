@@ -109,52 +109,84 @@ template <int BN> struct SmallShape {
     static constexpr int low_bytes = BN * 128 * 4;        // [BN rows][128 columns] fp32: what the adapters add
 };
 
-// What the adapters of rows row0 + first .. + count add to column c, to low[row][..] of this thread's own column: each row's z
-// (the same address in all lanes) times the column's row of `up`, in fp32.  Four rows at once, so that as many reads of `up` are
-// under way; it runs beside the products.
-template <typename W>
-__device__ __forceinline__ void low_rank_rows(const LinearArgs& g, int64_t row0, int first, int count, int64_t c, float* low) {
-    constexpr int kRows = 4;
-    const W* up = static_cast<const W*>(g.up) + min(c, g.n - 1) * g.rank;
-#pragma unroll 1
-    for (int r = first; r < first + count; r += kRows) {
-        int id[kRows];
-        float sum[kRows] = {};
-        bool any = false;
+// What the adapters of rows row0 + first .. + count (64 at most) add to a warp's 32 columns c0 .., to low[row][..]: each row's z times
+// the columns' rows of `up`, in fp32.  The 32 rows of `up` are 64 RANK adjacent bytes, read as whole lines: a lane owns
+// the same eight ranks of RANK / 8 columns, and the sums of the lanes that share a column are exchanged so that each lane
+// is left with one column.  It is the latency of these reads that bounds it: eight to sixteen are on their way while as many are summed.
+template <typename W, int RANK>
+__device__ __forceinline__ void low_rank_rows_of(const LinearArgs& g, int64_t row0, int first, int count, int64_t c0, float* low, int lane) {
+    constexpr int kReads = RANK / 8, kRows = RANK <= 32 ? 4 : 128 / RANK;  // reads of a row, rows at once
+    constexpr int kStep = 32 / kReads;                     // columns of a read
+    const int sub = lane % kReads;
+    auto adapter = [&](int r) {
+        const int id = r < count && row0 + first + r < g.m ? __ldg(g.low.chosen + row0 + first + r) : -1;
+        return id < g.adapters ? id : -1;
+    };
+    const int ids[2] = {adapter(lane), adapter(lane + 32)};
+    auto id_of = [&](int r) { return __shfl_sync(0xffffffffu, r < 32 ? ids[0] : ids[1], r & 31); };
+    const bool any = __any_sync(0xffffffffu, ids[0] >= 0 || ids[1] >= 0);
+    uint4 next[kRows][kReads];
+    float4 next_z[kRows][2];
+    auto ask = [&](int r0) {
 #pragma unroll
         for (int j = 0; j < kRows; ++j) {
-            id[j] = r + j < first + count && row0 + r + j < g.m ? __ldg(g.low.chosen + row0 + r + j) : -1;
-            if (id[j] >= g.adapters) id[j] = -1;
-            any |= id[j] >= 0;
-        }
-        if (any)
-#pragma unroll 1
-            for (int i = 0; i < g.rank; i += 16) {
-                uint4 u[kRows][2];
+            const int r = min(r0 + j, count - 1);
+            const int64_t id = max(id_of(r), 0);
 #pragma unroll
-                for (int j = 0; j < kRows; ++j) {
-                    const uint4* from = reinterpret_cast<const uint4*>(up + (int64_t)max(id[j], 0) * g.n * g.rank + i);
-                    u[j][0] = __ldg(from);
-                    u[j][1] = __ldg(from + 1);
+            for (int q = 0; q < kReads; ++q) {
+                const int64_t c = min(c0 + q * kStep + lane / kReads, g.n - 1);
+                next[j][q] = __ldg(reinterpret_cast<const uint4*>(static_cast<const W*>(g.up) + (id * g.n + c) * RANK + sub * 8));
+            }
+            const float4* z = reinterpret_cast<const float4*>(g.low.z + min(row0 + first + r, g.m - 1) * RANK + sub * 8);
+            next_z[j][0] = __ldg(z);
+            next_z[j][1] = __ldg(z + 1);
+        }
+    };
+    if (any) ask(0);
+#pragma unroll 1
+    for (int r0 = 0; r0 < count; r0 += kRows) {
+        uint4 u[kRows][kReads];
+        float4 z[kRows][2];
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+#pragma unroll
+            for (int q = 0; q < kReads; ++q) u[j][q] = next[j][q];
+            z[j][0] = next_z[j][0];
+            z[j][1] = next_z[j][1];
+        }
+        if (any && r0 + kRows < count) ask(r0 + kRows);
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+            if (r0 + j >= count) break;
+            float sum[kReads] = {};
+            if (id_of(r0 + j) >= 0) {                      // (the same for all lanes)
+                const float v[8] = {z[j][0].x, z[j][0].y, z[j][0].z, z[j][0].w, z[j][1].x, z[j][1].y, z[j][1].z, z[j][1].w};
+#pragma unroll
+                for (int q = 0; q < kReads; ++q) {
+                    const W* e = reinterpret_cast<const W*>(&u[j][q]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[q] = fmaf(to_f32(e[i]), v[i], sum[q]);
                 }
 #pragma unroll
-                for (int j = 0; j < kRows; ++j)
-                    if (id[j] >= 0) {
-                        const float4* z = reinterpret_cast<const float4*>(g.low.z + (row0 + r + j) * g.rank + i);
-                        const W* e = reinterpret_cast<const W*>(u[j]);
+                for (int o = kReads / 2; o > 0; o >>= 1)   // a lane keeps the half of the reads that its bit `o` names
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const float4 v = __ldg(z + q);
-                            sum[j] = fmaf(to_f32(e[4 * q]), v.x, sum[j]);
-                            sum[j] = fmaf(to_f32(e[4 * q + 1]), v.y, sum[j]);
-                            sum[j] = fmaf(to_f32(e[4 * q + 2]), v.z, sum[j]);
-                            sum[j] = fmaf(to_f32(e[4 * q + 3]), v.w, sum[j]);
-                        }
+                    for (int q = 0; q < o; ++q) {
+                        const bool upper = (sub & o) != 0;
+                        const float give = upper ? sum[q] : sum[q + o], keep = upper ? sum[q + o] : sum[q];
+                        sum[q] = keep + __shfl_xor_sync(0xffffffffu, give, o);
                     }
             }
-#pragma unroll
-        for (int j = 0; j < kRows; ++j) if (r + j < first + count) low[(r + j) * 128] = sum[j];
+            low[(first + r0 + j) * 128 + sub * kStep + lane / kReads] = sum[0];        // read number `sub` is this lane's
+        }
     }
+    __syncwarp();
+}
+template <typename W>
+__device__ __forceinline__ void low_rank_rows(const LinearArgs& g, int64_t row0, int first, int count, int64_t c0, float* low, int lane) {
+    if (g.rank == 16) low_rank_rows_of<W, 16>(g, row0, first, count, c0, low, lane);
+    else if (g.rank == 32) low_rank_rows_of<W, 32>(g, row0, first, count, c0, low, lane);
+    else if (g.rank == 64) low_rank_rows_of<W, 64>(g, row0, first, count, c0, low, lane);
+    else low_rank_rows_of<W, 128>(g, row0, first, count, c0, low, lane);
 }
 
 // `count` of N results of one column, rows r .. : the residuals are all read before the first result is written
@@ -275,7 +307,7 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
         ColTerm ct = {0.0f, 0u, 0.0f};
         if (c < g.n) ct = col_term(g, c);
         const int own = BN / splits;
-        if constexpr (!std::is_void_v<W>) low_rank_rows<W>(g, m0, split * own, own, c, low + col);
+        if constexpr (!std::is_void_v<W>) low_rank_rows<W>(g, m0, split * own, own, (int64_t)n0 + quarter * 32, low + quarter * 32, lane);
         bool ok = mbar_wait_warp(done, 0, &failed, g.polls);
         if (!ok) mbar_wait(done, 0);                      // what has been issued must end before TMEM is freed
         ok = ok && !__any_sync(0xffffffffu, has_failed());
@@ -364,13 +396,15 @@ linear_small_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
 constexpr int kPairStoreWarps = 16;                       // four per quarter of the TMEM lanes: two for each half of the columns
 constexpr int kPairThreads = 64 + 32 * kPairStoreWarps;
 constexpr int kPairCols = 128;
+template <bool ADAPTED>
 struct PairShape {
     static constexpr int stage_bytes = (128 + kPairCols / 2) * kBlock;   // per CTA
-    static constexpr int stages = 6;
+    // with adapters fewer: what they read by all storing warps then stays in L1
+    static constexpr int stages = ADAPTED ? 4 : 6;
     static constexpr int row_words = 64;                            // column pair p of row r lies at pair p ^ r: no bank conflicts either way
     static constexpr int transpose_bytes = kPairStoreWarps / 2 * 32 * row_words * 4;
-    static constexpr int smem = stages * stage_bytes + transpose_bytes + 1024;
-    static constexpr int term_bytes = kPairStoreWarps / 2 * 64 * 16;     // with adapters: the columns' constants
+    static constexpr int term_bytes = ADAPTED ? kPairStoreWarps / 2 * 64 * 16 : 0;      // the columns' constants
+    static constexpr int smem = stages * stage_bytes + transpose_bytes + term_bytes + 1024;
 };
 
 // What the adapters of 16 rows add to 64 columns, into TMEM lanes and columns from `at` on: the parts of z times the columns'
@@ -380,7 +414,7 @@ struct PairShape {
 // (fp32 multiply-adds instead would take 2 rank / 32 instructions an output for some rank / 250 here; products on tf32, whose
 // range needs no parts' exponent, took twice the time of these and kept the tensor cores from the product itself.)
 template <typename W, int PARTS>
-__device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0, int64_t c0, uint32_t at, int lane) {
+__device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0, int64_t c0, uint32_t at, int lane, int turn) {
     const int row = lane >> 2, quad = lane & 3;
     int id = lane < 16 && row0 + lane < g.m ? __ldg(g.low.chosen + row0 + lane) : -1;
     if (id >= g.adapters) id = -1;
@@ -396,8 +430,9 @@ __device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0,
             left &= ~rows;
             const W* up = static_cast<const W*>(g.up) + (int64_t)which * g.n * g.rank + 4 * quad;
             const W* z = reinterpret_cast<const W*>(g.low.parts) + 4 * quad;
+            int i = turn * 16 % g.rank;                    // warps begin with different ranks: each is fetched once and is in L1 for the others
 #pragma unroll 1
-            for (int i = 0; i < g.rank; i += 16) {
+            for (int n = 0; n < g.rank; n += 16, i = i + 16 < g.rank ? i + 16 : 0) {
                 uint2 u[8], a[PARTS][2];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) u[j] = __ldg(reinterpret_cast<const uint2*>(up + min(c0 + 8 * j + row, g.n - 1) * g.rank + i));
@@ -437,7 +472,7 @@ template <typename T, typename W>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const LinearArgs g,
                    int tiles_m, int tiles) {
-    using Shape = PairShape;
+    using Shape = PairShape<!std::is_void_v<W>>;
     constexpr int BN = kPairCols, kStages = Shape::stages, kAccs = 2;
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kAccs + 1];
@@ -569,7 +604,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 const ColTerm t = c < g.n ? col_term(g, c) : ColTerm{0.0f, 0u, 0.0f};
                 terms[part * 32 + lane] = make_float4(t.scale, __uint_as_float(t.term), t.bias, 0.0f);
                 tmem_fence_after();                        // (the block has read what the tile before had there)
-                low_rank_tile<W, std::is_same_v<W, __nv_bfloat16> && std::is_same_v<T, float> ? kLowParts : 2>(g, row0 + part * 16, (int64_t)n0 + c0, lanes + ((uint32_t)(part * 16) << 16) + (uint32_t)(kAccs * BN + c0), lane);
+                low_rank_tile<W, std::is_same_v<W, __nv_bfloat16> && std::is_same_v<T, float> ? kLowParts : 2>(g, row0 + part * 16, (int64_t)n0 + c0, lanes + ((uint32_t)(part * 16) << 16) + (uint32_t)(kAccs * BN + c0), lane, quarter * 2 + part);
                 tmem_fence_before();
                 block_sync();
                 tmem_fence_after();
@@ -730,11 +765,11 @@ int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
 
 template <typename T, typename W>
 int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
-    using Shape = PairShape;
+    using Shape = PairShape<!std::is_void_v<W>>;
     constexpr int BN = kPairCols;
     static PerDeviceOnce once;
     auto* kernel = linear_pair_kernel<T, W>;
-    constexpr int smem = Shape::smem + (std::is_void_v<W> ? 0 : Shape::term_bytes);
+    constexpr int smem = Shape::smem;
     int rc = once.raise_smem_limit(kernel, smem);
     if (rc != MPQ_OK) return rc;
     CUtensorMap map_w, map_a;
@@ -815,7 +850,7 @@ extern "C" int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const 
     if (rc != MPQ_OK) return rc;
     if (m != 0 && (!down || !up || !q_starts || (batch != 0 && !ids) || !workspace)) return MPQ_ERR_NULL;
     if (adapters <= 0 || rank <= 0 || batch < 0) return MPQ_ERR_BAD_SHAPE;
-    if ((adapter_dtype != MPQ_F16 && adapter_dtype != MPQ_BF16) || rank % 16 || rank > 128) return MPQ_ERR_UNSUPPORTED;
+    if ((adapter_dtype != MPQ_F16 && adapter_dtype != MPQ_BF16) || (rank != 16 && rank != 32 && rank != 64 && rank != 128)) return MPQ_ERR_UNSUPPORTED;
     if (!aligned16(down) || !aligned16(up) || !aligned16(workspace) || !aligned_to(factor, 4) || !aligned_to(q_starts, 4) || !aligned_to(ids, 4)) return MPQ_ERR_ALIGN;
     if (m == 0) return MPQ_OK;
     if (workspace_bytes < mpq_linear_adapted_workspace(m, rank)) return MPQ_ERR_WORKSPACE;
