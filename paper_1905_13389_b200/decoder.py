@@ -13,13 +13,16 @@ A block is the usual one of a decoder-only transformer, with every product on le
 Weights are encoded once, at construction, with one range per output channel; activations get one range per
 token.  Positions are the caller's to put into the hidden states.  ``forward`` takes the new tokens of a batch of
 sequences -- whole prompts, chunks of prompts and single tokens mixed -- and only launches kernels on the current
-stream; ``check`` says afterwards whether all of them have done their work.  ``Pages`` keeps the host's side of the cache: which pages a sequence owns.
+stream; ``check`` says afterwards whether all of them have done their work.  Any product can have low-rank adapters beside its
+weights, another one for each sequence of a batch (linear_adapted).  Which pages of the cache a sequence owns is kept by
+``Pages`` on the host, or by ``DevicePages`` on the device (pages_extend, pages_trim): a whole step, from the
+lengths to the tokens that ``sample`` draws, can then be captured once and replayed while the sequences grow.
 
     python -m paper_1905_13389_b200.decoder          # a small model: two prompts, then eight tokens each
 """
 from __future__ import annotations
 
-from typing import Dict, List, NamedTuple
+from typing import Dict, List, NamedTuple, Optional
 
 import torch
 
@@ -82,12 +85,43 @@ class Pages:
         self.length.pop(sequence, None)
 
 
+class DevicePages:
+    """Which pages of a cache each of ``sequences`` sequences owns, ``per_sequence`` at most, kept on the device: nothing is copied
+    or waited for, so that calls can be captured.  Numbers of sequences and tokens are int32 tensors on the device."""
+
+    def __init__(self, pages: int, page_size: int, sequences: int, per_sequence: int, device):
+        self.state = mpq.page_state(sequences, per_sequence, pages, page_size, device)
+        self.missing = torch.zeros((1,), dtype=torch.int32, device=device)
+
+    def extend(self, sequences: Optional[torch.Tensor], new: torch.Tensor, tokens: int, max_q: int, max_kv: int,
+               out: Optional[mpq.PagePlan] = None) -> Batch:
+        """Makes room for ``new`` tokens of each of ``sequences`` (None: all, in their order; -1: padding) and describes the batch,
+        padded to ``tokens``; max_q and max_kv bound a sequence's new tokens and its context."""
+        plan = mpq.pages_extend(self.state, sequences, new, tokens, out)
+        self.missing = plan.missing
+        return Batch(plan.slots, plan.q_starts, plan.kv_lens, plan.table, max_q, max_kv)
+
+    def trim(self, sequences: Optional[torch.Tensor], keep: torch.Tensor):
+        """Gives back what lies behind the first ``keep`` tokens of each of ``sequences`` (0 drops one)."""
+        mpq.pages_trim(self.state, sequences, keep)
+
+    def check(self):
+        """Raises if the last batch did not fit (nothing was taken for it then).  Waits for the stream."""
+        missing = int(self.missing)
+        if missing:
+            raise MemoryError("a sequence outgrows its row of the table" if missing == -1 else "the batch has more tokens than slots" if missing == -2
+                              else "the cache is full: %d pages are missing" % missing)
+
+
 class EncodedDecoder:
     """``weights``: per layer a dict of float tensors qkv [(heads + 2 kv_heads) dim x width], o [width x heads dim],
-    up [inner x width], up_bias [inner], down [width x inner], norm1, norm2 [width]."""
+    up [inner x width], up_bias [inner], down [width x inner], norm1, norm2 [width].  ``adapters``: per layer a dict of
+    mpq.Adapters beside any of qkv, o, up and down."""
 
-    def __init__(self, config: Config, weights: List[Dict[str, torch.Tensor]], pages: int, page_size: int):
+    def __init__(self, config: Config, weights: List[Dict[str, torch.Tensor]], pages: int, page_size: int,
+                 adapters: Optional[List[Dict[str, mpq.Adapters]]] = None):
         self.config, device = config, weights[0]["qkv"].device
+        self.adapters = adapters or [{}] * len(weights)
         self.layers = []
         for w in weights:
             layer = {name: mpq.encode_levels(w[name], config.weight_bits) for name in ("qkv", "o", "up", "down")}
@@ -96,24 +130,28 @@ class EncodedDecoder:
             self.layers.append(layer)
         self.given_up = mpq.wait_failures()
 
-    def forward(self, x: torch.Tensor, batch: Batch) -> torch.Tensor:
+    def forward(self, x: torch.Tensor, batch: Batch, ids: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Hidden states [tokens][width] (float16 or bfloat16) of the batch's new tokens -> hidden states after the last
-        block; the tokens' keys and values are in the cache afterwards."""
+        block; the tokens' keys and values are in the cache afterwards.  ``ids`` (int32): the adapter of each sequence of the
+        batch, -1 for none."""
         c, dtype = self.config, x.dtype
         tokens = x.shape[0]
-        for w in self.layers:
+        for w, low in zip(self.layers, self.adapters):
+            def product(a, name, **kw):
+                if ids is None or name not in low:
+                    return mpq.linear_levels(a, w[name], dtype=dtype, **kw)
+                return mpq.linear_adapted(a, w[name], low[name], batch.q_starts, ids, dtype=dtype, **kw)
             h = mpq.rmsnorm_levels(x, w["norm1"], c.eps, c.act_bits)
-            qkv = mpq.linear_levels(h, w["qkv"], dtype=dtype).view(tokens, c.heads + 2 * c.kv_heads, c.dim)
+            qkv = product(h, "qkv").view(tokens, c.heads + 2 * c.kv_heads, c.dim)
             q, k, v = qkv.split((c.heads, c.kv_heads, c.kv_heads), dim=1)
             mpq.cache_write(w["cache"], k, v, batch.slots)
             a = mpq.cache_attention(q, w["cache"], batch.q_starts, batch.kv_lens, batch.table, batch.max_q, batch.max_kv)
             a = mpq.encode_levels(a.view(tokens, c.heads * c.dim), c.act_bits)
-            x = mpq.linear_levels(a, w["o"], residual=x, dtype=dtype)
+            x = product(a, "o", residual=x)
             h = mpq.rmsnorm_levels(x, w["norm2"], c.eps, c.act_bits)
-            h = mpq.linear_levels(h, w["up"], bias=w["up_bias"], act="gelu_tanh", dtype=dtype)
-            x = mpq.linear_levels(mpq.encode_levels(h, c.act_bits), w["down"], residual=x, dtype=dtype)
+            h = product(h, "up", bias=w["up_bias"], act="gelu_tanh")
+            x = product(mpq.encode_levels(h, c.act_bits), "down", residual=x)
         return x
-
 
     def check(self):
         """Raises if a kernel has given up a wait since the model was made or last checked.  What it left is NaN, but an encoder
@@ -137,28 +175,38 @@ def random_weights(config: Config, device, seed: int = 0) -> List[Dict[str, torc
     return out
 
 
+def random_adapters(config: Config, count: int, rank: int, device, seed: int = 0) -> List[Dict[str, mpq.Adapters]]:
+    """Adapters beside all four products, some tenth of the weights' size each."""
+    g = torch.Generator().manual_seed(seed)
+    shapes = {"qkv": ((config.heads + 2 * config.kv_heads) * config.dim, config.width), "o": (config.width, config.heads * config.dim),
+              "up": (config.inner, config.width), "down": (config.width, config.inner)}
+    normal = lambda *shape, size: (torch.randn(shape, generator=g) * size).to(device).to(torch.bfloat16)      # noqa: E731
+    return [{name: mpq.adapters(normal(count, rank, k, size=k ** -0.5), normal(count, n, rank, size=rank ** -0.5),
+                                torch.full((count,), 0.1, device=device)) for name, (n, k) in shapes.items()} for _ in range(config.layers)]
+
+
 def main():
     device = torch.device("cuda:0")
     config = Config(layers=4, width=1024, heads=16, kv_heads=4, dim=64, inner=4096)
-    model = EncodedDecoder(config, random_weights(config, device), pages=64, page_size=16)
-    pages, g = Pages(64, 16), torch.Generator().manual_seed(1)
+    model = EncodedDecoder(config, random_weights(config, device), pages=64, page_size=16, adapters=random_adapters(config, 2, 8, device))
+    pages, g = DevicePages(64, 16, sequences=2, per_sequence=16, device=device), torch.Generator().manual_seed(1)
     vocabulary = torch.randn((500, config.width), generator=g).to(device)
     words = mpq.encode_levels(vocabulary, 8)                 # the last product is on levels as well
-    tokens = {0: torch.randint(0, 500, (37,), generator=g), 1: torch.randint(0, 500, (5,), generator=g)}
-    said = {s: [] for s in tokens}
-    for _ in range(8):
-        batch = pages.extend({s: len(t) for s, t in tokens.items()}, device)
-        x = vocabulary[torch.cat(list(tokens.values())).to(device)].to(torch.bfloat16)
-        x = model.forward(x, batch)[batch.q_starts[1:].long() - 1]                             # each sequence's last token
+    prompts = [torch.randint(0, 500, (37,), generator=g), torch.randint(0, 500, (5,), generator=g)]
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device=device)                        # noqa: E731
+    ids, warm, top_p = ints(1, -1), torch.tensor([0.0, 0.8], device=device), torch.tensor([1.0, 0.9], device=device)
+    tokens, new, said = torch.cat(prompts).to(device), ints(37, 5), []
+    for step in range(8):
+        batch = pages.extend(None, new, len(tokens), max_q=37 if step == 0 else 1, max_kv=64)
+        x = model.forward(vocabulary[tokens].to(torch.bfloat16), batch, ids)[batch.q_starts[1:].long() - 1]     # each sequence's last token
         logits = mpq.linear_levels(mpq.rmsnorm_levels(x, None, config.eps), words)
-        nxt = logits.argmax(1).cpu()
-        model.check()
-        tokens = {s: nxt[i:i + 1] for i, s in enumerate(tokens)}
-        for i, s in enumerate(said):
-            said[s].append(int(nxt[i]))
-    for s, t in said.items():
-        print("sequence %d, %d tokens in the cache: %s" % (s, pages.length[s], t))
-        pages.drop(s)
+        tokens, new = mpq.sample(logits, torch.rand(2, generator=g).to(device), warm, top_p=top_p), ints(1, 1)
+        said.append(tokens)
+    pages.check()
+    model.check()
+    for s, (n, t) in enumerate(zip(pages.state.lens.tolist(), torch.stack(said, 1).tolist())):
+        print("sequence %d, %d tokens in the cache: %s" % (s, n, t))
+    pages.trim(None, ints(0, 0))
 
 
 if __name__ == "__main__":
