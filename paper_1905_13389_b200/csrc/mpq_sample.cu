@@ -7,10 +7,12 @@
 //
 // A row belongs to one CTA, or where there are few rows to a cluster of up to eight.  Shares that are small enough stay in shared
 // memory; of larger ones only the first look goes to memory, the later ones find the row in L2.  Nothing is sorted.  Where
-// top-k or top-p ends is found in two steps.  Counts by distance from the largest logit, in 2048 steps of 1/64, say in which
-// step the end lies; what lies above is kept, and what lies in it is handed to every CTA of the row, which counts
-// it by the bits of a code, key (the logit's bits in their order) before place -- no two elements have the same one.
-// Where few are kept all of them are handed round, and the rest of the work needs no more exchange.
+// top-k or top-p ends is found in three looks.  The first finds the largest logit.  The second counts elements by their distance
+// from it, in 2048 steps of 1/64, which says in which steps the end lies: exactly for top-k, by counts times weights for top-p.
+// The third adds up the weights -- of all, and of what lies above those steps -- and hands what lies in them (where few
+// are kept: all that are kept) to every CTA of the row.  There it is counted by the bits of a code, key (the logit's bits in
+// their order) before place, which no two elements share.  Where the second look was too far off the sums show it, and
+// it is looked at again with the difference known.
 // Where that fails (more than 2048 equals, say) the row is searched by the bits of its keys: two passes count by 11 bits each --
 // exactly for top-k, with rounded weights for top-p --, and a third takes the exact sum of all above the 2^10 keys found
 // and counts their members; equals have equal weights, so count times weight is exact.  Where rounding had led astray the
@@ -29,13 +31,13 @@ struct SampleArgs {
     int64_t* tokens; float* logprob;
     int shift;                                            // weights are multiples of 2^-shift: vocab 2^shift <= 2^62
     int ctas, warp_chunks;                                // CTAs of a row; 16-byte chunks that are a warp's share
-    int cached, list;                                     // whether shares stay in shared memory; elements that a warp's list holds
+    int cached;                                           // whether shares stay in shared memory
 };
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleBins = 2048, kLowBits = 10;          // 11 + 11 + 10 bits of a key
 constexpr int kSampleGroups = kSampleBins / 32;
-constexpr int kSampleOwn = 4, kSampleMembers = 1024;      // members that a thread holds, and a CTA hands out
+constexpr int kSampleOwn = 4, kSampleMembers = 1024;      // members that a thread holds, and one of several CTAs hands out
 
 // Whole numbers in the order of the logits; -0 and 0 are the same number.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -75,22 +77,24 @@ __device__ __forceinline__ uint2 ld_cluster32x2(uint32_t addr) {
     return v;
 }
 
+struct SampleBorder {                                      // the bin in which a sum is reached: the sums before and with it, the counts
+    u64 above, above_to;
+    uint32_t digit, count, count_to;
+};
 // What passes between a row's CTAs, two of each: one is written while others may still read the one before.
 struct SampleShared {
-    u64 parts[2][kSampleWarps];
+    u64 parts[2][2][kSampleWarps];
     uint32_t bins[2][kSampleBins];
-    u64 scan[kSampleWarps];
-    double powers[16];                                    // 2^(i / 16 + shift): sixteen, so that lanes never ask one bank for two of them
-    int found[2];
-    uint32_t digit, digit_before;
-    u64 above, above_to, weight, members;
+    uint32_t offsets[kSampleBins];                        // sums of 1/256 of a step by which a bin's members lie behind its beginning
     u64 coarse[2][2][kSampleGroups];                      // what groups of 32 bins are worth, and their counts
-    uint32_t counts[2];                                   // of the bins down to a border, and of its own bin
-    int noted[2], longest;                                // members a CTA hands out; elements of the longest list
+    int noted[2], found[2];                               // members a CTA hands out; a place
     double rest[kSampleWarps];
-    u64 sums[2][3][kSampleWarps];
-    uint32_t differ[2];
-    u64 member;
+    // within a CTA
+    SampleBorder border[2];
+    u64 scan[kSampleWarps], sums[2][kSampleWarps];
+    double powers[16];                                    // 2^(i / 16 + shift): sixteen, so that lanes never ask one bank for two of them
+    uint32_t digit, differ[2];
+    u64 above, weight, members, member, all;
 };
 
 // The largest element of a chunk, NaN if one is.
@@ -145,21 +149,17 @@ struct SampleRow {
     const T* x0;                                          // the row
     const int vocab, skew;                                // skew: place of its first element; places count from the 16-byte boundary before it
     uint4* chunks;                                        // this warp's share, where it is cached
-    uint16_t* list;                                       // elements of the share that can still be kept, ascending
     const bool cached;
-    const int ctas, rank, warp, lane, warp_chunks, list_size;
+    const int ctas, rank, warp, lane, warp_chunks;
     const int v0;                                         // place of the share's first element
     int turn = 0;                                         // which of the two exchange buffers comes next
-    bool listed = false;                                  // whether the list has all that can still be kept, and how much that is
-    int count;
 
     __device__ SampleRow(SampleShared& s, uint4* data, const SampleArgs& g)
         : sh(s), x0(static_cast<const T*>(g.logits) + (int64_t)(blockIdx.x / (unsigned)g.ctas) * g.ld), vocab(g.vocab),
           skew((int)(reinterpret_cast<uintptr_t>(x0) & 15) / (int)sizeof(T)), cached(g.cached != 0), ctas(g.ctas), rank(g.ctas > 1 ? (int)cluster_rank() : 0),
-          warp(__shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0)), lane(threadIdx.x & 31), warp_chunks(g.warp_chunks), list_size(g.list),
-          v0((rank * kSampleWarps + warp) * g.warp_chunks * E), count(g.warp_chunks * E) {
+          warp(__shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0)), lane(threadIdx.x & 31), warp_chunks(g.warp_chunks),
+          v0((rank * kSampleWarps + warp) * g.warp_chunks * E) {
         chunks = data + warp * warp_chunks;
-        list = reinterpret_cast<uint16_t*>(data + (g.cached ? kSampleWarps * warp_chunks : 0)) + warp * list_size;
     }
 
     __device__ __forceinline__ void sync() {
@@ -198,65 +198,62 @@ struct SampleRow {
             for (int j = 0; j < N; ++j) in[j] = read_chunk(min(c + 32 * j, warp_chunks - 1));
         }
     }
-    // f(place of the first, values) for this lane's chunks of the whole share.
-    template <typename F>
-    __device__ __forceinline__ void each_chunk(F f) const {
-        constexpr int kAtOnce = 8 / E;
-        uint4 next[kAtOnce];
+    // f(v, values) for this lane's elements of the share, eight at a time (-infinity behind the share's last), N such groups under
+    // way; place_of(v, i) is where the i-th of them lies.
+    static constexpr int kParts = 8 / E;
+    static __device__ __forceinline__ int place_of(int v, int i) { return v + i % E + i / E * 32 * E; }
+    template <int N, typename F>
+    __device__ __forceinline__ void each_group(F f) const {
+        uint4 next[N * kParts];
         read_chunks(min(lane, warp_chunks - 1), next, !cached);
 #pragma unroll 1
-        for (int c = lane; c < warp_chunks; c += 32 * kAtOnce) {
-            uint4 in[kAtOnce];
+        for (int c = lane; c < warp_chunks; c += 32 * N * kParts) {
+            uint4 in[N * kParts];
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) in[j] = next[j];
-            read_chunks(min(c + 32 * kAtOnce, warp_chunks - 1), next, !cached);
+            for (int j = 0; j < N * kParts; ++j) in[j] = next[j];
+            read_chunks(min(c + 32 * N * kParts, warp_chunks - 1), next, !cached);
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                float x[E];
-                unpack(in[j], x);
-                if (c + 32 * j < warp_chunks) f(v0 + (c + 32 * j) * E, x);
+            for (int n = 0; n < N; ++n) {
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < kParts; ++j) {
+                    float e[E];
+                    unpack(in[n * kParts + j], e);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) x[j * E + i] = c + 32 * (n * kParts + j) < warp_chunks ? e[i] : -INFINITY;
+                }
+                if (c + 32 * n * kParts < warp_chunks) f(v0 + (c + 32 * n * kParts) * E, x);
             }
         }
     }
-    // Element i of what is still looked at in the share of warp w of this CTA.
+    // Element i of the share of warp w of this CTA.
     __device__ __forceinline__ void element(int w, int i, int& place, float& x) const {
-        const int at = listed ? list[(w - warp) * list_size + i] : i;
-        place = v0 + (w - warp) * warp_chunks * E + at;
-        if (cached) x = to_f32(reinterpret_cast<const T*>(chunks + (w - warp) * warp_chunks)[at]);
+        place = v0 + (w - warp) * warp_chunks * E + i;
+        if (cached) x = to_f32(reinterpret_cast<const T*>(chunks + (w - warp) * warp_chunks)[i]);
         else x = place >= skew && place - skew < vocab ? to_f32(x0[place - skew]) : -INFINITY;
     }
-    // f(place, value) for what is still looked at; a list's in ascending places of the warp.
+    // f(place, value) for all elements of the share.
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        if (listed) {
-            constexpr int kAtOnce = 4;
-#pragma unroll 1
-            for (int i = lane; i < count; i += 32 * kAtOnce) {
-                int place[kAtOnce];
-                float x[kAtOnce];
+        each_group<1>([&](int v, const float (&x)[8]) {
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) element(warp, min(i + 32 * j, count - 1), place[j], x[j]);
-#pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) if (i + 32 * j < count) f(place[j], x[j]);
-            }
-        } else {
-            each_chunk([&](int v, const float (&x)[E]) {
-#pragma unroll
-                for (int i = 0; i < E; ++i) f(v + i, x[i]);
-            });
-        }
+            for (int i = 0; i < 8; ++i) if (x[i] > -INFINITY) f(place_of(v, i), x[i]);
+        });
     }
 
-    // Every warp's number -> all numbers of the row's warps, four to a lane, the same in all warps of all CTAs.
-    __device__ __forceinline__ void gather(u64 mine, u64 (&v)[4]) {
-        u64* part = sh.parts[turn];
-        if (lane == 0) part[warp] = mine;
-        sync();
+    // Every warp's numbers -> all of the row's warps, four to a lane, the same in all warps of all CTAs.
+    __device__ __forceinline__ void collect(int which, int of_turn, u64 (&v)[4]) const {
+        const u64* part = sh.parts[of_turn][which];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int n = lane * 4 + i;
             v[i] = n < ctas * kSampleWarps ? ld_cluster64(peer(part + n % kSampleWarps, n / kSampleWarps)) : 0;
         }
+    }
+    __device__ __forceinline__ void gather(u64 mine, u64 (&v)[4]) {
+        if (lane == 0) sh.parts[turn][0][warp] = mine;
+        sync();
+        collect(0, turn, v);
         turn ^= 1;
     }
     static __device__ __forceinline__ u64 warp_sum(u64 s) {
@@ -283,32 +280,26 @@ struct SampleRow {
         gather(warp_sum(s), v);
         return warp_sum(v[0] + v[1] + v[2] + v[3]);
     }
-    // Sum of f over what is still looked at.
+    // Sum of f over the share.
     template <typename F>
     __device__ __forceinline__ u64 sum(F f) const {
         u64 s = 0;
         each([&](int place, float x) { s += f(place, x); });
         return s;
     }
-    // Sum of a chunk's weights.
-    static __device__ __forceinline__ u64 chunk_sum(const SampleWeight& weight, const float (&x)[E]) {
-        u64 s = 0;
+    // A group's weights, f(i, weight) each.
+    template <typename F>
+    static __device__ __forceinline__ void weigh(const SampleWeight& weight, const float (&x)[8], F f) {
         float low = x[0];
 #pragma unroll
-        for (int i = 1; i < E; ++i) low = fminf(low, x[i]);
-        if (!weight.small(low) && low > -INFINITY) {
+        for (int i = 1; i < 8; ++i) low = fminf(low, x[i]);
+        if (!weight.small(low) && low > -INFINITY) {      // (without a branch between them they are made side by side)
 #pragma unroll
-            for (int i = 0; i < E; ++i) s += weight.biased(x[i]);
-            return s - E * SampleWeight::kBias;           // (modulo 2^64)
-        }
-#pragma unroll 1
-        for (int i = 0; i < E; ++i) {
-            float one = x[0];
+            for (int i = 0; i < 8; ++i) f(i, weight.biased(x[i]) - SampleWeight::kBias);
+        } else {
 #pragma unroll
-            for (int j = 1; j < E; ++j) one = i == j ? x[j] : one;
-            s += weight(one);
+            for (int i = 0; i < 8; ++i) f(i, weight(x[i]));
         }
-        return s;
     }
 
     // The lowest place at which the running sum of f exceeds goal(sum of all), in the one thread that finds it (-1 elsewhere).
@@ -330,9 +321,7 @@ struct SampleRow {
         before = __shfl_sync(0xffffffffu, before, in);
         if (which / kSampleWarps != rank) return -1;
         which %= kSampleWarps;
-        if (lane == 0 && warp == which) sh.found[0] = count;
-        __syncthreads();
-        const int n = sh.found[0], per = ((n + kSampleWarps - 1) / kSampleWarps + 31) / 32 * 32, from = min(n, warp * per), to = min(n, from + per);
+        const int n = warp_chunks * E, per = ((n + kSampleWarps - 1) / kSampleWarps + 31) / 32 * 32, from = min(n, warp * per), to = min(n, from + per);
         u64 part = 0;
 #pragma unroll 1
         for (int i = from + lane; i < to; i += 32) {
@@ -369,18 +358,18 @@ struct SampleRow {
         __syncthreads();
         return bins;
     }
-    // Adds up what the CTAs have counted by `bins`, worth(bin, count), and finds, from the highest bin down, the one in which the
-    // sum reaches goal() (the lowest that has anything, if none does); `above` is the sum before it.  Groups of 32 bins are
-    // summed by each CTA and looked at first, so that little passes between the CTAs.
-    template <typename Worth, typename Goal>
-    __device__ __forceinline__ void border(Goal goal_of, Worth worth, uint32_t& digit, u64& above) {
+    // Adds up what the CTAs have counted by bins, worth(bin, count, offsets) of each, and finds, from the highest bin down, those in
+    // which the sum reaches goals(sum of all, ..) (the lowest that has anything, if none does): sh.border, N of them.  Groups of
+    // 32 bins are summed by each CTA and looked at first, so that little passes between the CTAs.
+    template <int N, typename Worth, typename Goals>
+    __device__ __forceinline__ void find_borders(Worth worth, Goals goals) {
         __syncthreads();
         for (int i = warp; i < kSampleGroups; i += kSampleWarps) {
-            const u64 n = sh.bins[turn][i * 32 + lane], value = warp_sum(worth(i * 32 + lane, n)), all = warp_sum(n);
+            const int bin = i * 32 + lane;
+            const u64 n = sh.bins[turn][bin], value = warp_sum(worth(bin, (uint32_t)n, sh.offsets[bin])), all = warp_sum(n);
             if (lane == 0) { sh.coarse[turn][0][i] = value; sh.coarse[turn][1][i] = all; }
         }
         sync();
-        const u64 goal = goal_of();
         if (warp == 0) {
             // two groups a lane, the highest first
             u64 value[2] = {}, n[2] = {};
@@ -392,37 +381,38 @@ struct SampleRow {
                     n[i] += ld_cluster64(peer(&sh.coarse[turn][1][group], c));
                 }
             const u64 to = warp_scan(value[0] + value[1]), n_to = warp_scan(n[0] + n[1]);
-            const uint32_t reach = __ballot_sync(0xffffffffu, to >= goal), any = __ballot_sync(0xffffffffu, (n[0] | n[1]) != 0);
-            const int in = reach ? __ffs(reach) - 1 : 31 - __clz(any);      // something has been counted
-            const bool second = reach ? to - value[1] < goal : n[1] != 0;
-            const int group = __shfl_sync(0xffffffffu, kSampleGroups - 1 - 2 * lane - (second ? 1 : 0), in);
-            const u64 before = __shfl_sync(0xffffffffu, to - value[1] - (second ? 0 : value[0]), in);
-            const u64 n_before = __shfl_sync(0xffffffffu, n_to - n[1] - (second ? 0 : n[0]), in);
-            const int bin = group * 32 + 31 - lane;
-            u64 here = 0;
-            for (int c = 0; c < ctas; ++c) here += ld_cluster32(peer(&sh.bins[turn][bin], c));
-            const u64 w = worth(bin, here), upto = before + warp_scan(w), n_upto = n_before + warp_scan(here);
-            const uint32_t reaches = __ballot_sync(0xffffffffu, upto >= goal), anything = __ballot_sync(0xffffffffu, here != 0);
-            if (lane == (reaches ? __ffs(reaches) - 1 : 31 - __clz(anything))) {
-                sh.digit = (uint32_t)bin;
-                sh.above = upto - w;
-                sh.above_to = upto;
-                sh.counts[0] = (uint32_t)n_upto;
-                sh.counts[1] = (uint32_t)here;
+            u64 goal[N];
+            goals(__shfl_sync(0xffffffffu, to, 31), goal);
+            const uint32_t any = __ballot_sync(0xffffffffu, (n[0] | n[1]) != 0);
+#pragma unroll 1
+            for (int k = 0; k < N; ++k) {
+                const u64 here_goal = k == 0 ? goal[0] : goal[N - 1];
+                const uint32_t reach = __ballot_sync(0xffffffffu, to >= here_goal);
+                const int in = reach ? __ffs(reach) - 1 : 31 - __clz(any);      // something has been counted
+                const bool second = reach ? to - value[1] < here_goal : n[1] != 0;
+                const int group = __shfl_sync(0xffffffffu, kSampleGroups - 1 - 2 * lane - (second ? 1 : 0), in);
+                const u64 before = __shfl_sync(0xffffffffu, to - value[1] - (second ? 0 : value[0]), in);
+                const u64 n_before = __shfl_sync(0xffffffffu, n_to - n[1] - (second ? 0 : n[0]), in);
+                const int bin = group * 32 + 31 - lane;
+                u64 here = 0, w = 0;
+                for (int c = 0; c < ctas; ++c) {
+                    const uint32_t one = ld_cluster32(peer(&sh.bins[turn][bin], c));
+                    here += one;
+                    w += worth(bin, one, ld_cluster32(peer(&sh.offsets[bin], c)));
+                }
+                const u64 upto = before + warp_scan(w), n_upto = n_before + warp_scan(here);
+                const uint32_t reaches = __ballot_sync(0xffffffffu, upto >= here_goal), anything = __ballot_sync(0xffffffffu, here != 0);
+                if (lane == (reaches ? __ffs(reaches) - 1 : 31 - __clz(anything)))
+                    sh.border[k] = SampleBorder{upto - w, upto, (uint32_t)bin, (uint32_t)here, (uint32_t)n_upto};
             }
         }
         __syncthreads();
-        digit = sh.digit;
-        above = sh.above;
         turn ^= 1;
     }
 
     // Distance of an element from `top` in steps, rounded the same way for equals and never against the order (NaN only for what
-    // is not over -infinity), and its bin, the lowest one for all beyond.
+    // is not over -infinity).  Bins count the steps down from the highest, the lowest one for all beyond.
     static __device__ __forceinline__ float distance(float x, float top, float steps) { return (top - x) * steps; }
-    static __device__ __forceinline__ uint32_t bin_of(float away) {
-        return kSampleBins - 1 - (__float_as_uint(__fadd_rd(fminf(away, (float)(kSampleBins - 1)), 8388608.0f)) & (kSampleBins - 1));
-    }
     // The smallest number whose distance is below `limit` (1 or more), by a warp: distances never grow with the number.
     __device__ __forceinline__ float nearest_below(float top, float steps, float limit) const {
         uint32_t lo = 0x00800000u, hi = order_key(top);   // from the lowest finite number on; hi's distance is 0
@@ -443,97 +433,48 @@ struct SampleRow {
     __device__ __forceinline__ float least_of(float top, float steps, uint32_t digit) const {
         return digit == 0 ? key_value(0x00800000u) : digit >= kSampleBins ? INFINITY : nearest_below(top, steps, (float)(kSampleBins - (int)digit));
     }
-    // Notes in the list what is `from_on` or more; false, and no list, where this CTA's cannot hold it.  Four bytes a lane at a time,
-    // so that the places of a warp's vote ascend.
-    __device__ __forceinline__ bool make_list(float from_on) {
-        constexpr int kAtOnce = 8, W = 4 / (int)sizeof(T);
-        const int words = warp_chunks * 4;
-        const bool inside = v0 >= skew && v0 + warp_chunks * E - skew <= vocab;
-        const uint32_t* from = cached ? reinterpret_cast<const uint32_t*>(chunks) : reinterpret_cast<const uint32_t*>(x0 + (v0 - skew));
-        const uint32_t lower = (1u << lane) - 1;
-        int have = 0;
-#pragma unroll 1
-        for (int c0 = 0; c0 < words; c0 += 32 * kAtOnce) {
-            uint32_t in[kAtOnce];
+    // Where members are handed out: in the exchange's bins, both of them where there is no exchange.
+    __device__ __forceinline__ u64* members_of(int of_turn) const { return reinterpret_cast<u64*>(sh.bins[ctas > 1 ? of_turn : 0]); }
+    __device__ __forceinline__ int most_members() const { return ctas > 1 ? kSampleMembers : 2 * kSampleMembers; }
+    // Hands out those of a group that `mask` names.
+    __device__ __forceinline__ void note(uint32_t mask, int v, const float (&x)[8]) {
+        u64* members = members_of(turn);
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                const int c = min(c0 + 32 * j + lane, words - 1);
-                if (cached || inside) {
-                    in[j] = from[c];
-                } else {
-                    T* e = reinterpret_cast<T*>(&in[j]);
-#pragma unroll
-                    for (int q = 0; q < W; ++q) {
-                        const int i = v0 + c * W + q - skew;
-                        e[q] = i >= 0 && i < vocab ? x0[i] : from_f32<T>(-INFINITY);
-                    }
-                }
+        for (int i = 0; i < 8; ++i)
+            if (mask >> i & 1) {
+                const int at = atomicAdd(&sh.noted[turn], 1);
+                if (at < most_members()) members[at] = code_of(place_of(v, i), x[i]);
             }
-#pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                const int c = c0 + 32 * j + lane;
-                const T* e = reinterpret_cast<const T*>(&in[j]);
-                bool mine[W];
-                uint32_t votes[W], any = 0;
-#pragma unroll
-                for (int q = 0; q < W; ++q) {
-                    mine[q] = c < words && to_f32(e[q]) >= from_on;
-                    votes[q] = __ballot_sync(0xffffffffu, mine[q]);
-                    any |= votes[q];
-                }
-                if (!any) continue;
-                int at = have;
-#pragma unroll
-                for (int q = 0; q < W; ++q) { at += __popc(votes[q] & lower); have += __popc(votes[q]); }
-#pragma unroll
-                for (int q = 0; q < W; ++q) {
-                    if (mine[q] && at < list_size) list[at] = (uint16_t)(c * W + q);
-                    at += mine[q];
-                }
-            }
-        }
-        if (threadIdx.x == 0) sh.longest = 0;
-        __syncthreads();
-        if (lane == 0) atomicMax(&sh.longest, have);
-        __syncthreads();
-        if (sh.longest > list_size) return false;
-        listed = true;
-        count = have;
-        return true;
     }
     // An element's place in the order, the larger the earlier.
     static __device__ __forceinline__ u64 code_of(int place, float x) { return (u64)order_key(x) << 32 | (uint32_t)~place; }
 
-    // Sums of N numbers over the CTA's threads, the same in all of them.
-    template <int N>
-    __device__ __forceinline__ void block_sums(u64 (&v)[N], int& phase) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-        if (lane == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i) sh.sums[phase][i][warp] = v[i];
+    // Sum of a number over the CTA's threads, the same in all of them.
+    __device__ __forceinline__ u64 block_sum(u64 v, int& phase) {
+        v = warp_sum(v);
+        if (lane == 0) sh.sums[phase][warp] = v;
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = sh.sums[phase][i][lane % kSampleWarps];
-            for (int o = kSampleWarps / 2; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-        }
+        v = sh.sums[phase][lane % kSampleWarps];
+        for (int o = kSampleWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         phase ^= 1;
+        return v;
     }
     // The largest code at which the sum of f over the codes from it on reaches goal, where that of all does: ten bits at a
-    // time, from the highest one in which they differ, until one is left.
+    // time, from the highest one in which those with f differ, until one is left.
     __device__ __forceinline__ u64 resolve(const u64 (&code)[kSampleOwn], const u64 (&f)[kSampleOwn], u64 goal) {
         constexpr int kBits = 10, kPer = (1 << kBits) / kSampleThreads;
         u64* bins = reinterpret_cast<u64*>(sh.bins[turn]);
         if (threadIdx.x == 0) {
             sh.differ[0] = sh.differ[1] = 0;
-            sh.member = code[0];                          // thread 0's first member exists
         }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kSampleOwn; ++i) if (f[i]) sh.member = code[i];            // any one
         __syncthreads();
         const u64 ref = sh.member;
         u64 other = 0;
 #pragma unroll
-        for (int i = 0; i < kSampleOwn; ++i) if (code[i]) other |= code[i] ^ ref;
+        for (int i = 0; i < kSampleOwn; ++i) if (f[i]) other |= code[i] ^ ref;
         const uint32_t hi = __reduce_or_sync(0xffffffffu, (uint32_t)(other >> 32)), lo = __reduce_or_sync(0xffffffffu, (uint32_t)other);
         if (lane == 0) {
             if (hi) atomicOr(&sh.differ[0], hi);
@@ -584,12 +525,8 @@ struct SampleRow {
         for (int i = 0; i < kSampleOwn; ++i) {
             const int at = (int)threadIdx.x * kSampleOwn + i;
             while (at >= end && c + 1 < ctas) { n = (int)ld_cluster32(peer(&sh.noted[noted_turn], ++c)); end += n; }
-            code[i] = at < end ? ld_cluster64(peer(reinterpret_cast<u64*>(sh.bins[noted_turn]) + (at - (end - n)), c)) : 0;
+            code[i] = at < end ? ld_cluster64(peer(members_of(noted_turn) + (at - (end - n)), c)) : 0;
         }
-    }
-    __device__ __forceinline__ void forget_list() {
-        listed = false;
-        count = warp_chunks * E;
     }
 };
 
@@ -611,11 +548,15 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     float best = -INFINITY;
     int best_chunk = 0;
     bool nan = false;
-    constexpr int kLoads = 8;
+    constexpr int kLoads = 4;
+    uint4 next[kLoads];
+    r.read_chunks(min(lane, g.warp_chunks - 1), next, true);
 #pragma unroll 1
     for (int c0 = lane; c0 < g.warp_chunks; c0 += 32 * kLoads) {
         uint4 in[kLoads];
-        r.read_chunks(c0, in, true);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) in[j] = next[j];
+        r.read_chunks(min(c0 + 32 * kLoads, g.warp_chunks - 1), next, true);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int c = min(c0 + 32 * j, g.warp_chunks - 1);
@@ -663,40 +604,50 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
     const bool all_stay = !some && !top_p && floor_w <= 1;
     const float steps = 64.0f * (some ? 1.0f : fminf(weight.coolf, 1e30f));
-    // A second look at all of it, for whatever is wanted: counts of distances; the sum of all weights; and what the others weigh
-    // together at temperature 1, the first one's weight being 1 -- where it has nearly all of the probability its logarithm is
+    // The second look, for whatever is wanted: counts of distances; the sum of all weights; and what the others weigh together at
+    // temperature 1, the first one's weight being 1 -- where it has nearly all of the probability its logarithm is
     // -log(1 + rest).  That one in 32 bits: a term is off by (2.5 |d| + 4) 2^-24 of itself at most, d its distance from the first.
     u64 weights = 0;
     auto look = [&](bool distances, bool sums, bool others) {
-        if (!distances && !sums && !others) return;
-        uint32_t* bins = distances ? r.clear_bins() : nullptr;
+        uint32_t* bins = sh.bins[r.turn];
+        if (distances) {
+            for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) bins[i] = sh.offsets[i] = 0;
+            __syncthreads();
+        }
         float rest = 0.0f;
-        r.each_chunk([&](int v, const float (&x)[E]) {
+        auto one = [&](int v, const float (&x)[8]) {
             if (distances) {
 #pragma unroll
-                for (int i = 0; i < E; ++i)
-                    if (x[i] > -INFINITY) atomicAdd(bins + r.bin_of(r.distance(x[i], top, steps)), 1u);
+                for (int i = 0; i < 8; ++i)
+                    if (x[i] > -INFINITY) {
+                        // in 1/256 of a step, rounded down: on top of 2^23 the low bits are whole numbers
+                        const uint32_t away = __float_as_uint(__fadd_rd(fminf(r.distance(x[i], top, steps), (float)kSampleBins - 0.25f) * 256.0f, 8388608.0f)) - 0x4b000000u;
+                        const uint32_t bin = kSampleBins - 1 - (away >> 8);
+                        atomicAdd(bins + bin, 1u);
+                        if (!some) atomicAdd(sh.offsets + bin, away & 255u);
+                    }
             }
-            if (sums) weights += SampleRow<T>::chunk_sum(weight, x);
+            if (sums) r.weigh(weight, x, [&](int, u64 w) { weights += w; });
             if (others) {
-                float e[E];
+                float e[8];
 #pragma unroll
-                for (int i = 0; i < E; ++i) e[i] = fast_exp2((x[i] - top) * 1.4426950408889634f);
-                if ((unsigned)(first - v) < (unsigned)E) {
+                for (int i = 0; i < 8; ++i) e[i] = fast_exp2((x[i] - top) * 1.4426950408889634f);
+                if (first >= v && first <= r.place_of(v, 7)) {
 #pragma unroll
-                    for (int i = 0; i < E; ++i) if (v + i == first) e[i] = 0.0f;
+                    for (int i = 0; i < 8; ++i) if (r.place_of(v, i) == first) e[i] = 0.0f;
                 }
 #pragma unroll
-                for (int i = 0; i < E; ++i) rest += e[i];
+                for (int i = 0; i < 8; ++i) rest += e[i];
             }
-        });
+        };
+        if (distances || sums || others) r.template each_group<1>(one);
         if (others) {
             double sum = rest;
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             if (lane == 0) sh.rest[r.warp] = sum;
         }
     };
-    look(cut_off, !greedy && (all_stay || (top_p && !some)), g.logprob != nullptr);
+    look(cut_off, !greedy && all_stay, g.logprob != nullptr);
     // by one thread of the row, after an exchange between its CTAs
     auto finish = [&](int v, float x) {
         g.tokens[row] = v - skew;
@@ -725,7 +676,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         uint32_t over = 1u << (32 - kLowBits), under = 0xffffffffu;        // the border lies below `over` and above `under` (key >> kLowBits)
         u64 base = 0;                                     // f's sum from `over` on
         int64_t bias = 0;                                 // by how much the guesses above `under` fall short
-        auto as_counted = [](uint32_t, u64 n) { return n; };
+        auto as_counted = [](uint32_t, uint32_t n, uint32_t) { return (u64)n; };
         for (int turns = 0; turns < 1 << 16; ++turns) {   // (each one takes at least one occupied key off the open ones)
             auto open = [&](uint32_t key) { const uint32_t high = key >> kLowBits; return high < over && (under == 0xffffffffu || high > under); };
             const u64 want = (u64)max((int64_t)((double)(goal - base) / (double)unit) - bias, (int64_t)1);
@@ -741,11 +692,11 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                         if (n) atomicAdd(bins + (level ? key >> kLowBits & (kSampleBins - 1) : key >> 21), n);
                     }
                 });
-                uint32_t digit;
                 above1 += above2;
                 const u64 left = want > above1 ? want - above1 : 1;
-                r.border([&] { return left; }, as_counted, digit, above2);
-                high = level ? high << 11 | digit : digit;
+                r.template find_borders<1>(as_counted, [&](u64, u64 (&goal)[1]) { goal[0] = left; });
+                above2 = sh.border[0].above;
+                high = level ? high << 11 | sh.border[0].digit : sh.border[0].digit;
             }
             high = min(high, (1u << (32 - kLowBits)) - 1);
             // exactly: what lies above, and how many have each of the keys found
@@ -804,166 +755,161 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     };
     auto drawn = [&](u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(all, u, false) : 0ull; };
     auto share = [&](u64 all) { return max(p > 0.0f ? share_of(all, p, true) : 0ull, 1ull); };
-    u64 all = 0;                                          // top-p without top-k: what the row weighs
-    bool open = some || top_p;                            // whether the first end is still to be found
-    bool summed = all_stay;                               // whether `weights` has what is kept
+    u64 all = 0;                                          // top-p without top-k: what the row weighs, once it is known
+    bool open = !all_stay;                                // whether it is still to be found what stays
+    bool summed = all_stay;                               // whether `weights` is the sum of what stays
+    const float unit = exp2f((float)g.shift);
     int64_t bias = 0;
     int phase = 0;
-    const float unit = exp2f((float)g.shift);
+    if (!some && !top_p && open) {                        // min-p alone: two steps below its border at most
+        open = least >= 1.0f || -64.0f * logf(least) + 2.0f < 4e6f;
+        if (!open) summed = false;
+    }
+    const bool least_only = !some && !top_p;
 #pragma unroll 1
     for (int tries = 0; open && tries < 3; ++tries) {
-        // How far the first of the order reach: for top-k by counts, for top-p by counts times the weight in the middle of a bin.
-        // Where that is too far off, the sums show it, and the next try takes the difference into account.
-        auto worth = [&](uint32_t bin, u64 n) -> u64 {
-            if (some) return n;
-            return bin == 0 ? 0ull : (u64)((float)n * (fast_exp2(((float)bin - (float)(kSampleBins - 1) - 0.5f) * (1.4426950408889634f / 64.0f)) * unit));
-        };
-        r.forget_list();
-        if (tries > 0) look(true, false, false);
-        const int turn = r.turn;
-        if (!some && tries == 0) {
-            const u64 mine = SampleRow<T>::warp_sum(weights);
-            if (lane == 0) sh.parts[turn][r.warp] = mine;
-        }
-        u64 goal = 0, above;
-        uint32_t digit;
-        r.border(
-            [&] {
-                if (!some && tries == 0) {
-                    for (int i = 0; i < 4; ++i) {
-                        const int n = lane * 4 + i;
-                        if (n < g.ctas * kSampleWarps) all += ld_cluster64(r.peer(&sh.parts[turn][n % kSampleWarps], n / kSampleWarps));
-                    }
-                    all = SampleRow<T>::warp_sum(all);
-                }
-                goal = some ? (u64)k : share(all);
-                return (u64)max((int64_t)goal + bias, (int64_t)1);
-            },
-            worth, digit, above);
-        const u64 above_to = sh.above_to;
-        const uint32_t listed = sh.counts[0], within = sh.counts[1], most = (uint32_t)min(kSampleThreads * kSampleOwn, kSampleMembers * g.ctas);
-        // Few: every CTA gets all of them and goes on alone.  Many: the border's bin; the others' sum is taken here.
-        const bool few = listed <= most;
-        const float outer = r.least_of(top, steps, digit), inner = r.least_of(top, steps, digit + 1);
-        const bool fits = r.make_list(outer);
-        if (!few && within > most) break;
-        int at = 0;
-        if (few) {                                        // noted in ascending places
-            if (lane == 0) sh.scan[r.warp] = fits ? (u64)r.count : 0ull;
-            __syncthreads();
-            int end = 0;
-            for (int w = 0; w < kSampleWarps; ++w) {
-                if (w == r.warp) at = end;
-                end += (int)sh.scan[w];
-            }
-            if (threadIdx.x == 0) sh.noted[r.turn] = fits ? end : kSampleMembers + 1;
-            at += lane;
-        } else if (threadIdx.x == 0) {
-            sh.noted[r.turn] = 0;
-        }
-        __syncthreads();
-        u64* members = reinterpret_cast<u64*>(sh.bins[r.turn]);
-        u64 s = 0;
-        if (few ? fits : true) {
-            r.each([&](int v, float x) {
-                if (few || (x >= outer && x < inner)) {
-                    const int i = few ? at : atomicAdd(&sh.noted[r.turn], 1);
-                    if (i < kSampleMembers) members[i] = SampleRow<T>::code_of(v, x);
-                    at += 32;
-                } else if (x >= inner) {
-                    s += some ? 1ull : weight(x);
-                }
+        float outer, inner = INFINITY;                    // what is handed out is `outer` or more and below `inner`
+        bool few = true;                                  // ... is all that can stay
+        u64 above = 0, above_to = 0;
+        if (least_only) {
+            outer = r.nearest_below(top, steps, least >= 1.0f ? 3.0f : -64.0f * logf(least) + 2.0f);
+        } else {
+            if (tries > 0) look(true, false, false);
+            // the weight of a bin's members is that of their mean distance, off by some 2^-15 of itself; 2^-12 on both sides
+            auto worth = [&](uint32_t bin, uint32_t n, uint32_t offsets) -> u64 {
+                if (some) return n;
+                if (bin == 0 || n == 0) return 0ull;
+                const float away = (float)(kSampleBins - 1 - bin) + ((float)offsets / (float)n + 0.5f) * (1.0f / 256.0f);
+                return (u64)((float)n * (fast_exp2(away * (-1.4426950408889634f / 64.0f)) * unit));
+            };
+            r.template find_borders<2>(worth, [&](u64 guessed, u64 (&goal)[2]) {
+                if (some) { goal[0] = goal[1] = (u64)k; return; }
+                const int64_t margin = (int64_t)(guessed >> 12), aim = (int64_t)(tries == 0 ? share(guessed) : share(all)) + bias;
+                goal[0] = (u64)max(aim - margin, (int64_t)1);
+                goal[1] = (u64)max(aim + margin, (int64_t)1);
             });
+            const SampleBorder hi = sh.border[0], lo = sh.border[1];
+            above = hi.above;
+            above_to = lo.above_to;
+            const uint32_t most = (uint32_t)(kSampleThreads * kSampleOwn);
+            few = lo.count_to <= most;
+            outer = r.least_of(top, steps, lo.digit);
+            if (!few) {
+                inner = r.least_of(top, steps, hi.digit + 1);
+                if (lo.count_to - (hi.count_to - hi.count) > most) break;
+            }
+        }
+        // The third look.
+        const int turn = r.turn;
+        if (threadIdx.x == 0) sh.noted[turn] = 0;
+        __syncthreads();
+        u64 s = 0, total = 0;                             // of what lies above `inner`, of all
+        const bool sums = top_p && !some;
+        if (sums) {
+            r.template each_group<1>([&](int v, const float (&x)[8]) {
+                uint32_t mask = 0;
+                r.weigh(weight, x, [&](int i, u64 w) {
+                    total += w;
+                    if (x[i] >= inner) s += w;
+                    mask |= x[i] >= outer && x[i] < inner ? 1u << i : 0u;
+                });
+                if (mask) r.note(mask, v, x);
+            });
+        } else {
+            uint32_t n = 0;
+            r.template each_group<1>([&](int v, const float (&x)[8]) {
+                uint32_t mask = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    n += x[i] >= inner;
+                    mask |= x[i] >= outer && x[i] < inner ? 1u << i : 0u;
+                }
+                if (mask) r.note(mask, v, x);
+            });
+            s = n;
         }
         __syncthreads();
-        const int noted_turn = r.turn;
-        const bool too_many = sh.noted[noted_turn] > kSampleMembers;
+        const bool too_many = sh.noted[turn] > r.most_members();
+        const u64 mine = SampleRow<T>::warp_sum(s);
+        total = SampleRow<T>::warp_sum(total);
+        if (lane == 0) sh.parts[turn][1][r.warp] = total;
         u64 v[4];
-        r.gather(SampleRow<T>::warp_sum(s) | (too_many ? 1ull << 63 : 0ull), v);
+        r.gather(mine | (too_many ? 1ull << 63 : 0ull), v);
         if (__any_sync(0xffffffffu, (int64_t)(v[0] | v[1] | v[2] | v[3]) < 0)) break;
         const u64 sum = SampleRow<T>::warp_sum(v[0] + v[1] + v[2] + v[3]);
-        u64 code[kSampleOwn], w[kSampleOwn], f[kSampleOwn], whole[1] = {0};
-        r.take_members(noted_turn, code);
+        if (sums && tries == 0) {
+            r.collect(1, turn, v);
+            all = SampleRow<T>::warp_sum(v[0] + v[1] + v[2] + v[3]);
+        }
+        u64 code[kSampleOwn], w[kSampleOwn], f[kSampleOwn], whole = 0;
+        r.take_members(turn, code);
 #pragma unroll
         for (int i = 0; i < kSampleOwn; ++i) {
             w[i] = code[i] ? weight(key_value((uint32_t)(code[i] >> 32))) : 0;
             f[i] = some ? (u64)(code[i] != 0) : w[i];
-            whole[0] += f[i];
+            whole += f[i];
         }
-        r.block_sums(whole, phase);
+        whole = r.block_sum(whole, phase);
         u64 e = 0;
-        if (sum + whole[0] < goal) {                      // fewer over -infinity than top-k lets stay, or too short a guess
-            if (!some) { bias += (int64_t)(above_to - (sum + whole[0])); continue; }
-        } else if (sum >= goal) {
-            bias += (int64_t)(above - sum);
-            continue;
-        } else {
-            e = r.resolve(code, f, goal - sum);
+        if (!least_only) {
+            const u64 goal = some ? (u64)k : share(all);
+            if (sum + whole < goal) {                     // fewer over -infinity than top-k lets stay, or too short a guess
+                if (!some) { bias += (int64_t)(above_to - (sum + whole)); continue; }
+            } else if (sum >= goal) {
+                bias += (int64_t)(above - sum);
+                continue;
+            } else {
+                e = r.resolve(code, f, goal - sum);
+            }
         }
         open = false;
         if (!few) {
             edge = (uint32_t)(e >> 32);
             cut = (int)~(uint32_t)e;
-            if (!some && floor_w <= 1) {                  // the sums of what is kept: what lies above, and the kept ones of the border's bin
-                if (threadIdx.x < kSampleWarps) sh.sums[0][0][threadIdx.x] = 0;
+            if (sums && floor_w <= 1) {                   // what lies above, and the kept ones of what was handed out
+                if (threadIdx.x < kSampleWarps) sh.sums[0][threadIdx.x] = 0;
                 __syncthreads();
-                for (int i = threadIdx.x; i < sh.noted[noted_turn]; i += kSampleThreads) {
-                    const u64 one = members[i];
-                    if (one >= e) atomicAdd(&sh.sums[0][0][((int)~(uint32_t)one - r.rank * kSampleWarps * g.warp_chunks * E) / (g.warp_chunks * E)],
-                                            weight(key_value((uint32_t)(one >> 32))));
+#pragma unroll
+                for (int i = 0; i < kSampleOwn; ++i) {
+                    const int owner = (int)~(uint32_t)code[i] / (g.warp_chunks * E) - r.rank * kSampleWarps;
+                    if (code[i] >= e && code[i] && owner >= 0 && owner < kSampleWarps) atomicAdd(&sh.sums[0][owner], w[i]);
                 }
                 __syncthreads();
-                weights = s + (lane == 0 ? sh.sums[0][0][r.warp] : 0ull);
+                weights = s + (lane == 0 ? sh.sums[0][r.warp] : 0ull);
                 summed = true;
             }
             break;
         }
         if (some && top_p) {
-            u64 kept_sum[1] = {0};
+            u64 left = 0;
 #pragma unroll
             for (int i = 0; i < kSampleOwn; ++i) {
                 f[i] = code[i] >= e ? w[i] : 0;
-                kept_sum[0] += f[i];
+                left += f[i];
             }
-            r.block_sums(kept_sum, phase);
-            e = max(e, r.resolve(code, f, share(kept_sum[0])));
+            left = r.block_sum(left, phase);
+            e = max(e, r.resolve(code, f, share(left)));
         }
-        u64 mine = 0;
+        u64 left = 0;
 #pragma unroll
         for (int i = 0; i < kSampleOwn; ++i) {
             f[i] = code[i] >= e && (w[i] >= floor_w || (int)~(uint32_t)code[i] == first) ? w[i] : 0;
-            mine += f[i];
+            left += f[i];
+            if (!f[i]) code[i] = 0;
+            code[i] &= 0xffffffffull;                     // in the order of the places from here on
         }
-        const u64 upto = r.block_scan(mine);
-        if (threadIdx.x == kSampleThreads - 1) sh.above = upto;
-        __syncthreads();
-        const u64 point = drawn(sh.above);
-        u64 before = upto - mine;
-        if (r.rank == 0 && before <= point && upto > point) {
-            bool found = false;
-#pragma unroll
-            for (int i = 0; i < kSampleOwn; ++i) {
-                before += f[i];
-                if (!found && before > point) {
-                    finish((int)~(uint32_t)code[i], key_value((uint32_t)(code[i] >> 32)));
-                    found = true;
-                }
-            }
-        }
+        left = r.block_sum(left, phase);
+        const int place = (int)~(uint32_t)r.resolve(code, f, drawn(left) + 1);
+        if (r.rank == 0 && threadIdx.x == 0) finish(place, to_f32(r.x0[place - skew]));
         if (g.ctas > 1) cluster_sync_all();
         return;
     }
     if (open && some) narrow((u64)k, [](float) { return 1ull; }, [](float) { return 1u; }, 1.0f);
     if (top_p && (some || open)) {
-        if (!some) r.forget_list();
         const u64 left = r.row_sum(r.sum([&](int v, float x) { return kept(v, x) ? weight(x) : 0ull; }));
         const float units = 4.2e9f / ((float)left * 1.0001f), per = units * unit;
         narrow(share(left), weight,
                [&](float x) { return x > -INFINITY ? max(1u, __float2uint_rn(fast_exp2((x - top) * weight.coolf * 1.4426950408889634f) * per)) : 0u; }, 1.0f / units);
-    }
-    if (!some && !top_p && !all_stay && least < 1.0f) {   // min-p alone: two steps below its border at most
-        const float far = -64.0f * logf(least) + 2.0f;
-        if (far < 4e6f) r.make_list(r.nearest_below(top, steps, far));
     }
     auto stays = [&](int v, float x) {
         if (!kept(v, x)) return 0ull;
@@ -975,8 +921,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     if (g.ctas > 1) cluster_sync_all();
 }
 
-constexpr int kSampleMost = 786432;                       // elements of a row: a place in a warp's share has 16 bits
-constexpr int kSampleHeld = 88 * 1024;                    // bytes of shares and lists with which two CTAs fit a multiprocessor
+constexpr int kSampleMost = 786432;                       // elements of a row (half of that in 32 bits)
+constexpr int kSampleHeld = 80 * 1024;                    // bytes of shares with which two CTAs fit a multiprocessor
 
 template <typename T>
 int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
@@ -992,14 +938,12 @@ int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
     while (g.ctas < 8 && rows * g.ctas <= sms && g.vocab / g.ctas >= 8192) g.ctas *= 2;
     g.warp_chunks = (int)ceil_div(chunks, g.ctas * kSampleWarps);
     const int share = g.warp_chunks * kSampleWarps * 16;
-    g.list = 512;
-    g.cached = share + g.list * kSampleWarps * 2 <= kSampleHeld;
-    if (!g.cached) g.list = kSampleHeld / (kSampleWarps * 2);
+    g.cached = share <= kSampleHeld;
     if (rows * g.ctas > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * g.ctas), 1, 1);
     cfg.blockDim = dim3(kSampleThreads, 1, 1);
-    cfg.dynamicSmemBytes = (size_t)(g.cached ? share : 0) + (size_t)g.list * kSampleWarps * 2;
+    cfg.dynamicSmemBytes = (size_t)(g.cached ? share : 0);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1028,7 +972,7 @@ extern "C" int mpq_sample(const void* logits, int64_t ld, int dtype, int64_t row
     if (rows == 0) return MPQ_OK;
     int bits = 0;
     while ((int64_t)1 << bits < vocab) ++bits;
-    const SampleArgs g = {logits, ld, (int)vocab, temperature, top_k, top_p, min_p, uniform, tokens, logprob, 62 - bits > 50 ? 50 : 62 - bits, 1, 0, 0, 0};
+    const SampleArgs g = {logits, ld, (int)vocab, temperature, top_k, top_p, min_p, uniform, tokens, logprob, 62 - bits > 50 ? 50 : 62 - bits, 1, 0, 0};
     if (dtype == MPQ_F32) return launch_sample<float>(g, rows, (cudaStream_t)stream);
     if (dtype == MPQ_F16) return launch_sample<__half>(g, rows, (cudaStream_t)stream);
     return launch_sample<__nv_bfloat16>(g, rows, (cudaStream_t)stream);
