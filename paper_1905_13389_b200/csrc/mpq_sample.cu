@@ -183,47 +183,41 @@ struct SampleRow {
         for (int q = 0; q < E; ++q) e[q] = i + q >= 0 && i + q < vocab ? x0[i + q] : from_f32<T>(-INFINITY);
         return r;
     }
-    // Chunks c, c + 32, .. of the share (the last one in place of those behind it), asked for together.
+    // Chunks c, c + 32, .. of the share, asked for together.
     template <int N>
     __device__ __forceinline__ void read_chunks(int c, uint4 (&in)[N], bool from_memory) const {
         if (!from_memory) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) in[j] = chunks[min(c + 32 * j, warp_chunks - 1)];
-        } else if (v0 >= skew && v0 + warp_chunks * E - skew <= vocab) {         // every share but a row's first and last one
-            const uint4* from = reinterpret_cast<const uint4*>(x0 + (v0 - skew));
+            for (int j = 0; j < N; ++j) in[j] = chunks[c + 32 * j];
+        } else if (v0 >= skew && v0 + warp_chunks * E - skew <= vocab) {         // every share but a row's first and last ones
+            const uint4* from = reinterpret_cast<const uint4*>(x0 + (v0 - skew)) + c;
 #pragma unroll
-            for (int j = 0; j < N; ++j) in[j] = __ldg(from + min(c + 32 * j, warp_chunks - 1));
+            for (int j = 0; j < N; ++j) in[j] = __ldg(from + 32 * j);
         } else {
 #pragma unroll
-            for (int j = 0; j < N; ++j) in[j] = read_chunk(min(c + 32 * j, warp_chunks - 1));
+            for (int j = 0; j < N; ++j) in[j] = read_chunk(c + 32 * j);
         }
     }
-    // f(v, values) for this lane's elements of the share, eight at a time (-infinity behind the share's last), N such groups under
-    // way; place_of(v, i) is where the i-th of them lies.
-    static constexpr int kParts = 8 / E;
+    // f(v, values) for this lane's elements of the share, eight at a time (a share is whole groups of them), the next eight on
+    // their way; place_of(v, i) is where the i-th of them lies.
+    static constexpr int kParts = 8 / E, kGroup = 32 * kParts;             // chunks of a warp's step
     static __device__ __forceinline__ int place_of(int v, int i) { return v + i % E + i / E * 32 * E; }
-    template <int N, typename F>
+    template <typename F>
     __device__ __forceinline__ void each_group(F f) const {
-        uint4 next[N * kParts];
-        read_chunks(min(lane, warp_chunks - 1), next, !cached);
+        uint4 next[kParts];
+        read_chunks(lane, next, !cached);
 #pragma unroll 1
-        for (int c = lane; c < warp_chunks; c += 32 * N * kParts) {
-            uint4 in[N * kParts];
+        for (int c = lane; c < warp_chunks; c += kGroup) {
+            float x[8];
 #pragma unroll
-            for (int j = 0; j < N * kParts; ++j) in[j] = next[j];
-            read_chunks(min(c + 32 * N * kParts, warp_chunks - 1), next, !cached);
+            for (int j = 0; j < kParts; ++j) {
+                float e[E];
+                unpack(next[j], e);
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                float x[8];
-#pragma unroll
-                for (int j = 0; j < kParts; ++j) {
-                    float e[E];
-                    unpack(in[n * kParts + j], e);
-#pragma unroll
-                    for (int i = 0; i < E; ++i) x[j * E + i] = c + 32 * (n * kParts + j) < warp_chunks ? e[i] : -INFINITY;
-                }
-                if (c + 32 * n * kParts < warp_chunks) f(v0 + (c + 32 * n * kParts) * E, x);
+                for (int i = 0; i < E; ++i) x[j * E + i] = e[i];
             }
+            read_chunks(c + kGroup < warp_chunks ? c + kGroup : lane, next, !cached);
+            f(v0 + c * E, x);
         }
     }
     // Element i of the share of warp w of this CTA.
@@ -235,7 +229,7 @@ struct SampleRow {
     // f(place, value) for all elements of the share.
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        each_group<1>([&](int v, const float (&x)[8]) {
+        each_group([&](int v, const float (&x)[8]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) if (x[i] > -INFINITY) f(place_of(v, i), x[i]);
         });
@@ -287,7 +281,7 @@ struct SampleRow {
         each([&](int place, float x) { s += f(place, x); });
         return s;
     }
-    // A group's weights, f(i, weight) each.
+    // A group's weights, f(i, weight + kBias) each: sums of them are corrected once, modulo 2^64.
     template <typename F>
     static __device__ __forceinline__ void weigh(const SampleWeight& weight, const float (&x)[8], F f) {
         float low = x[0];
@@ -295,10 +289,10 @@ struct SampleRow {
         for (int i = 1; i < 8; ++i) low = fminf(low, x[i]);
         if (!weight.small(low) && low > -INFINITY) {      // (without a branch between them they are made side by side)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f(i, weight.biased(x[i]) - SampleWeight::kBias);
+            for (int i = 0; i < 8; ++i) f(i, weight.biased(x[i]));
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f(i, weight(x[i]));
+            for (int i = 0; i < 8; ++i) f(i, weight(x[i]) + SampleWeight::kBias);
         }
     }
 
@@ -518,6 +512,11 @@ struct SampleRow {
             if (one || at == 0) return sh.member;
         }
     }
+    // Whether no CTA has been given more than it can hand out, nor all together more than one can take.
+    __device__ __forceinline__ bool can_take(int noted_turn) const {
+        const uint32_t n = lane < ctas ? ld_cluster32(peer(&sh.noted[noted_turn], lane)) : 0;
+        return __all_sync(0xffffffffu, n <= (uint32_t)most_members()) && __reduce_add_sync(0xffffffffu, min(n, 4096u)) <= kSampleThreads * kSampleOwn;
+    }
     // Takes the members that the CTAs have noted, thread by thread in their order; 0 behind the last.
     __device__ __forceinline__ void take_members(int noted_turn, u64 (&code)[kSampleOwn]) {
         int end = 0, c = -1, n = 0;
@@ -549,17 +548,27 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     int best_chunk = 0;
     bool nan = false;
     constexpr int kLoads = 4;
+    auto ask = [&](int c0, uint4 (&in)[kLoads]) {         // (what is not there is asked for twice instead)
+#pragma unroll
+        for (int j = 0; j < kLoads; j += SampleRow<T>::kParts) {
+            uint4 some[SampleRow<T>::kParts];
+            r.read_chunks(c0 + 32 * j < g.warp_chunks ? c0 + 32 * j : lane, some, true);
+#pragma unroll
+            for (int i = 0; i < SampleRow<T>::kParts; ++i) in[j + i] = some[i];
+        }
+    };
     uint4 next[kLoads];
-    r.read_chunks(min(lane, g.warp_chunks - 1), next, true);
+    ask(lane, next);
 #pragma unroll 1
     for (int c0 = lane; c0 < g.warp_chunks; c0 += 32 * kLoads) {
         uint4 in[kLoads];
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) in[j] = next[j];
-        r.read_chunks(min(c0 + 32 * kLoads, g.warp_chunks - 1), next, true);
+        ask(c0 + 32 * kLoads, next);
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int c = min(c0 + 32 * j, g.warp_chunks - 1);
+            const int c = c0 + 32 * j;
+            if (c >= g.warp_chunks) break;
             if (r.cached) r.chunks[c] = in[j];
             const float top = chunk_max(in[j], static_cast<const T*>(nullptr));
             if (!(top <= best)) {
@@ -599,7 +608,10 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         return;
     }
 
-    const bool some = k > 0 && k < g.vocab, top_p = p < 1.0f, cut_off = !greedy && (some || top_p);
+    const bool some = k > 0 && k < g.vocab, top_p = p < 1.0f;
+    // Small k: as many of the threads' own largest elements as k say how far the first k can reach at most.
+    const bool by_threads = some && k <= kSampleThreads * g.ctas / 2;
+    const bool cut_off = !greedy && ((some && !by_threads) || (top_p && !some));
     const SampleWeight weight(top, warm, g.shift, sh.powers);
     const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
     const bool all_stay = !some && !top_p && floor_w <= 1;
@@ -607,6 +619,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     // The second look, for whatever is wanted: counts of distances; the sum of all weights; and what the others weigh together at
     // temperature 1, the first one's weight being 1 -- where it has nearly all of the probability its logarithm is
     // -log(1 + rest).  That one in 32 bits: a term is off by (2.5 |d| + 4) 2^-24 of itself at most, d its distance from the first.
+    constexpr uint32_t kNear = 512 << 8;                   // eight steps of a factor e
     u64 weights = 0;
     auto look = [&](bool distances, bool sums, bool others) {
         uint32_t* bins = sh.bins[r.turn];
@@ -624,10 +637,14 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                         const uint32_t away = __float_as_uint(__fadd_rd(fminf(r.distance(x[i], top, steps), (float)kSampleBins - 0.25f) * 256.0f, 8388608.0f)) - 0x4b000000u;
                         const uint32_t bin = kSampleBins - 1 - (away >> 8);
                         atomicAdd(bins + bin, 1u);
-                        if (!some) atomicAdd(sh.offsets + bin, away & 255u);
+                        // 32-bit logits that many share a bin lie anywhere in it
+                        if (!some && (sizeof(T) == 2 || away < kNear)) atomicAdd(sh.offsets + bin, away & 255u);
                     }
             }
-            if (sums) r.weigh(weight, x, [&](int, u64 w) { weights += w; });
+            if (sums) {
+                r.weigh(weight, x, [&](int, u64 w) { weights += w; });
+                weights -= 8 * SampleWeight::kBias;
+            }
             if (others) {
                 float e[8];
 #pragma unroll
@@ -640,7 +657,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                 for (int i = 0; i < 8; ++i) rest += e[i];
             }
         };
-        if (distances || sums || others) r.template each_group<1>(one);
+        if (distances || sums || others) r.each_group(one);
         if (others) {
             double sum = rest;
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -766,12 +783,30 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         if (!open) summed = false;
     }
     const bool least_only = !some && !top_p;
+    bool by_reach = by_threads;
+    float reach = -INFINITY;
+    if (by_threads) {
+        // each CTA's share of k (by its share of the row) among its threads, and the least of what the CTAs find: k elements at
+        // least are no smaller
+        const u64 code[kSampleOwn] = {best > -INFINITY ? (u64)order_key(best) << 32 | (threadIdx.x + 1) : 0ull};
+        const u64 one[kSampleOwn] = {code[0] ? 1ull : 0ull};
+        const int64_t span = (int64_t)kSampleWarps * g.warp_chunks * E, from = max(r.rank * span - skew, (int64_t)0), to = min((r.rank + 1) * span - skew, (int64_t)g.vocab);
+        const u64 goal = (u64)((max(to - from, (int64_t)0) * k + g.vocab - 1) / g.vocab), have = r.block_sum(one[0], phase);
+        u64 v[4];
+        r.gather(~(goal == 0 ? ~0ull : have < goal ? 0ull : r.resolve(code, one, goal) >> 32), v);
+        u64 lowest = max(max(v[0], v[1]), max(v[2], v[3]));
+        for (int o = 16; o > 0; o >>= 1) lowest = max(lowest, __shfl_xor_sync(0xffffffffu, lowest, o));
+        lowest = ~lowest;
+        reach = lowest ? key_value((uint32_t)lowest) : key_value(0x00800000u);
+    }
 #pragma unroll 1
-    for (int tries = 0; open && tries < 3; ++tries) {
+    for (int tries = 0; open && tries < 4; ++tries) {
         float outer, inner = INFINITY;                    // what is handed out is `outer` or more and below `inner`
         bool few = true;                                  // ... is all that can stay
         u64 above = 0, above_to = 0;
-        if (least_only) {
+        if (by_reach) {
+            outer = reach;
+        } else if (least_only) {
             outer = r.nearest_below(top, steps, least >= 1.0f ? 3.0f : -64.0f * logf(least) + 2.0f);
         } else {
             if (tries > 0) look(true, false, false);
@@ -779,7 +814,8 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             auto worth = [&](uint32_t bin, uint32_t n, uint32_t offsets) -> u64 {
                 if (some) return n;
                 if (bin == 0 || n == 0) return 0ull;
-                const float away = (float)(kSampleBins - 1 - bin) + ((float)offsets / (float)n + 0.5f) * (1.0f / 256.0f);
+                const bool exact = sizeof(T) == 2 || kSampleBins - 1 - bin < (kNear >> 8);
+                const float away = (float)(kSampleBins - 1 - bin) + (exact ? ((float)offsets / (float)n + 0.5f) * (1.0f / 256.0f) : 0.5f);
                 return (u64)((float)n * (fast_exp2(away * (-1.4426950408889634f / 64.0f)) * unit));
             };
             r.template find_borders<2>(worth, [&](u64 guessed, u64 (&goal)[2]) {
@@ -806,18 +842,21 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         u64 s = 0, total = 0;                             // of what lies above `inner`, of all
         const bool sums = top_p && !some;
         if (sums) {
-            r.template each_group<1>([&](int v, const float (&x)[8]) {
+            r.each_group([&](int v, const float (&x)[8]) {
                 uint32_t mask = 0;
+                uint32_t over = 0;
                 r.weigh(weight, x, [&](int i, u64 w) {
                     total += w;
-                    if (x[i] >= inner) s += w;
+                    if (x[i] >= inner) { s += w; ++over; }
                     mask |= x[i] >= outer && x[i] < inner ? 1u << i : 0u;
                 });
+                total -= 8 * SampleWeight::kBias;
+                s -= over * SampleWeight::kBias;
                 if (mask) r.note(mask, v, x);
             });
         } else {
             uint32_t n = 0;
-            r.template each_group<1>([&](int v, const float (&x)[8]) {
+            r.each_group([&](int v, const float (&x)[8]) {
                 uint32_t mask = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -829,13 +868,16 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             s = n;
         }
         __syncthreads();
-        const bool too_many = sh.noted[turn] > r.most_members();
         const u64 mine = SampleRow<T>::warp_sum(s);
         total = SampleRow<T>::warp_sum(total);
         if (lane == 0) sh.parts[turn][1][r.warp] = total;
         u64 v[4];
-        r.gather(mine | (too_many ? 1ull << 63 : 0ull), v);
-        if (__any_sync(0xffffffffu, (int64_t)(v[0] | v[1] | v[2] | v[3]) < 0)) break;
+        r.gather(mine, v);
+        if (!r.can_take(turn)) {
+            if (!by_reach) break;
+            by_reach = false;                             // the largest ones lie with few threads: they are counted after all
+            continue;
+        }
         const u64 sum = SampleRow<T>::warp_sum(v[0] + v[1] + v[2] + v[3]);
         if (sums && tries == 0) {
             r.collect(1, turn, v);
@@ -933,10 +975,12 @@ int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
     const int sms = sm_count();
     if (sms == 0) return MPQ_ERR_CUDA;
     // more CTAs to a row while the device has room for all rows' at once and a CTA 8192 elements
-    const int64_t chunks = ceil_div((int64_t)g.vocab + E - 1, E);
+    const bool aligned = aligned16(g.logits) && (rows == 1 || g.ld % E == 0);
+    const int64_t chunks = ceil_div((int64_t)g.vocab + (aligned ? 0 : E - 1), E);
     g.ctas = 1;
     while (g.ctas < 8 && rows * g.ctas <= sms && g.vocab / g.ctas >= 8192) g.ctas *= 2;
-    g.warp_chunks = (int)ceil_div(chunks, g.ctas * kSampleWarps);
+    constexpr int kGroup = SampleRow<T>::kGroup;
+    g.warp_chunks = (int)ceil_div(chunks, g.ctas * kSampleWarps * kGroup) * kGroup;
     const int share = g.warp_chunks * kSampleWarps * 16;
     g.cached = share <= kSampleHeld;
     if (rows * g.ctas > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;

@@ -191,6 +191,35 @@ def test_flat_and_steep_rows(mpq, cuda, spread):
         check(mpq, cuda, x + 11, u, None, [0, 100, 0, 20000], [1.0, 1.0, 0.6, 0.5], [0.0, 0.0, 0.0, 1e-9], dtype=dtype)
 
 
+@pytest.mark.parametrize("rows,vocab", [(1, 131072), (1, 66001), (37, 20001), (300, 9001), (1, 3000)])
+def test_however_many_stay(mpq, cuda, rows, vocab):
+    """Numbers of kept tokens around what a block notes (1024 or 2048) and all blocks take (2048); ends of rows in any block."""
+    x, u, _ = bell(rows, vocab, vocab, 1.0)
+    for dtype in ("f32", "bf16"):
+        for n in (900, 1000, 1024, 1100, 2000, 2048, 2100, 4000, 7000, 12000):
+            if n < vocab:
+                check(mpq, cuda, x[:9], u[:9], k=[n] * len(x[:9]), dtype=dtype)
+                threshold = torch.exp(x.to(TYPES[dtype]).float().sort(1, descending=True).values[:, n] - x.to(TYPES[dtype]).float().max(1).values)
+                check(mpq, cuda, x[:9], u[:9], least=threshold[:9] * 1.0001, dtype=dtype)
+                w = torch.softmax(x[:9].to(TYPES[dtype]).double(), 1).sort(1, descending=True).values
+                check(mpq, cuda, x[:9], u[:9], p=w[:, :n].sum(1), dtype=dtype)
+    if rows > 9:                                              # ... with as many blocks to a row as there are for so many rows
+        for n in (1024, 2048, 7000):
+            check(mpq, cuda, x, u, k=[min(n, vocab - 1)] * rows)
+            check(mpq, cuda, x, u, p=torch.softmax(x.double(), 1).sort(1, descending=True).values[:, :n].sum(1))
+
+
+def test_ordered_rows(mpq, cuda):
+    """The largest logits side by side, with few threads of one block."""
+    for vocab in (9000, 131072):
+        x, u, _ = bell(4, vocab, 2)
+        x = x.sort(1).values
+        for y in (x, x.flip(1)):
+            for k in (40, 700, 1500):
+                check(mpq, cuda, y, u, [0.8] * 4, [k] * 4, [1.0, 0.9, 1.0, 0.5], [0.0, 0.0, 0.05, 0.0])
+            check(mpq, cuda, y, u, p=[0.3, 0.9, 0.99, 0.9999])
+
+
 def test_strides_outputs_and_odd_addresses(mpq, cuda):
     for vocab in (4096, 4099):
         for dtype in TYPES.values():
