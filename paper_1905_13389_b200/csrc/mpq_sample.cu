@@ -88,13 +88,14 @@ struct SampleShared {
     uint32_t offsets[kSampleBins];                        // sums of 1/256 of a step by which a bin's members lie behind its beginning
     u64 coarse[2][2][kSampleGroups];                      // what groups of 32 bins are worth, and their counts
     int noted[2], found[2];                               // members a CTA hands out; a place
-    double rest[kSampleWarps];
+    double rest[kSampleWarps], rest_all;                  // (the latter of a CTA, for the others)
     // within a CTA
     SampleBorder border[2];
     u64 scan[kSampleWarps], sums[2][kSampleWarps];
     double powers[16];                                    // 2^(i / 16 + shift): sixteen, so that lanes never ask one bank for two of them
     uint32_t digit, differ[2];
-    u64 above, weight, members, member, all;
+    u64 above, weight, members, member;
+    u64 codes[kSampleThreads], ordered[kSampleThreads];   // few members, one to a thread: their codes, their weights in the codes' order
 };
 
 // The largest element of a chunk, NaN if one is.
@@ -265,9 +266,9 @@ struct SampleRow {
         x = warp_scan(x);
         if (lane == 31) sh.scan[warp] = x;
         __syncthreads();
-        for (int w = 0; w < warp; ++w) x += sh.scan[w];
+        const u64 before = warp_sum(lane < warp ? sh.scan[lane] : 0);
         __syncthreads();
-        return x;
+        return x + before;
     }
     __device__ __forceinline__ u64 row_sum(u64 s) {
         u64 v[4];
@@ -327,7 +328,7 @@ struct SampleRow {
         part = warp_sum(part);
         if (lane == 0) sh.scan[warp] = part;
         __syncthreads();
-        for (int w = 0; w < warp; ++w) before += sh.scan[w];
+        before += warp_sum(lane < warp ? sh.scan[lane] : 0);
         if (before > goal || before + part <= goal) return -1;
 #pragma unroll 1
         for (int i0 = from; i0 < to; i0 += 32) {
@@ -430,14 +431,24 @@ struct SampleRow {
     // Where members are handed out: in the exchange's bins, both of them where there is no exchange.
     __device__ __forceinline__ u64* members_of(int of_turn) const { return reinterpret_cast<u64*>(sh.bins[ctas > 1 ? of_turn : 0]); }
     __device__ __forceinline__ int most_members() const { return ctas > 1 ? kSampleMembers : 2 * kSampleMembers; }
-    // Hands out those of a group that `mask` names.
+    // Hands out those of a group that `mask` names (called by whole warps: one of them is asked for room).
     __device__ __forceinline__ void note(uint32_t mask, int v, const float (&x)[8]) {
+        if (!__any_sync(0xffffffffu, mask)) return;
+        const int mine = __popc(mask);
+        int at = mine;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int below = __shfl_up_sync(0xffffffffu, at, o);
+            if (lane >= o) at += below;
+        }
+        int from = 0;
+        if (lane == 31) from = atomicAdd(&sh.noted[turn], at);
+        at += __shfl_sync(0xffffffffu, from, 31) - mine;
         u64* members = members_of(turn);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (mask >> i & 1) {
-                const int at = atomicAdd(&sh.noted[turn], 1);
                 if (at < most_members()) members[at] = code_of(place_of(v, i), x[i]);
+                ++at;
             }
     }
     // An element's place in the order, the larger the earlier.
@@ -475,8 +486,9 @@ struct SampleRow {
             if (lo) atomicOr(&sh.differ[1], lo);
         }
         __syncthreads();
-        int at = 64 - __clzll((long long)((u64)sh.differ[0] << 32 | sh.differ[1]));        // all codes agree from this bit up
-        if (at == 0) return ref;
+        const u64 differ = (u64)sh.differ[0] << 32 | sh.differ[1];
+        if (differ == 0) return ref;
+        int at = 64 - __clzll((long long)differ);         // all codes agree from this bit up
         u64 prefix = at < 64 ? ref >> at : 0;
         for (;;) {
             const int shift = max(at - kBits, 0), width = at - shift;
@@ -504,12 +516,16 @@ struct SampleRow {
             prefix = prefix << width | sh.digit;
             goal -= sh.above;
             at = shift;
+            const u64 below = differ & (((u64)1 << at) - 1);
+            const int next = 64 - __clzll((long long)below);                // bits that none differ in are passed over
             int left = 0;
 #pragma unroll
             for (int i = 0; i < kSampleOwn; ++i)
                 if (f[i] && code[i] >> at == prefix) { ++left; sh.member = code[i]; }
             const bool one = __syncthreads_or(left > 1) == 0 && __syncthreads_count(left == 1) == 1;
-            if (one || at == 0) return sh.member;
+            if (one || below == 0) return sh.member;
+            prefix = prefix << (at - next) | (ref >> next & (((u64)1 << (at - next)) - 1));
+            at = next;
         }
     }
     // Whether no CTA has been given more than it can hand out, nor all together more than one can take.
@@ -517,12 +533,18 @@ struct SampleRow {
         const uint32_t n = lane < ctas ? ld_cluster32(peer(&sh.noted[noted_turn], lane)) : 0;
         return __all_sync(0xffffffffu, n <= (uint32_t)most_members()) && __reduce_add_sync(0xffffffffu, min(n, 4096u)) <= kSampleThreads * kSampleOwn;
     }
-    // Takes the members that the CTAs have noted, thread by thread in their order; 0 behind the last.
-    __device__ __forceinline__ void take_members(int noted_turn, u64 (&code)[kSampleOwn]) {
+    __device__ __forceinline__ int handed(int noted_turn) const {
+        int n = 0;
+        for (int c = 0; c < ctas; ++c) n += (int)ld_cluster32(peer(&sh.noted[noted_turn], c));
+        return n;
+    }
+    // Takes the members that the CTAs have noted, OWN to a thread in their order; 0 behind the last.
+    template <int OWN>
+    __device__ __forceinline__ void take_members(int noted_turn, u64 (&code)[OWN]) {
         int end = 0, c = -1, n = 0;
 #pragma unroll
-        for (int i = 0; i < kSampleOwn; ++i) {
-            const int at = (int)threadIdx.x * kSampleOwn + i;
+        for (int i = 0; i < OWN; ++i) {
+            const int at = (int)threadIdx.x * OWN + i;
             while (at >= end && c + 1 < ctas) { n = (int)ld_cluster32(peer(&sh.noted[noted_turn], ++c)); end += n; }
             code[i] = at < end ? ld_cluster64(peer(members_of(noted_turn) + (at - (end - n)), c)) : 0;
         }
@@ -662,6 +684,10 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             double sum = rest;
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             if (lane == 0) sh.rest[r.warp] = sum;
+            __syncthreads();
+            sum = sh.rest[lane % kSampleWarps];
+            for (int o = kSampleWarps / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (threadIdx.x == 0) sh.rest_all = sum;
         }
     };
     look(cut_off, !greedy && all_stay, g.logprob != nullptr);
@@ -670,9 +696,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         g.tokens[row] = v - skew;
         if (!g.logprob) return;
         double rest = 0.0;
-        for (int c = 0; c < g.ctas; ++c)
-#pragma unroll
-            for (int w = 0; w < kSampleWarps; ++w) rest += __longlong_as_double((long long)ld_cluster64(r.peer(&sh.rest[w], c)));
+        for (int c = 0; c < g.ctas; ++c) rest += __longlong_as_double((long long)ld_cluster64(r.peer(&sh.rest_all, c)));
         g.logprob[row] = (float)(((double)x - (double)top) - log1p(rest));
     };
     if (greedy) {
@@ -852,7 +876,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                 });
                 total -= 8 * SampleWeight::kBias;
                 s -= over * SampleWeight::kBias;
-                if (mask) r.note(mask, v, x);
+                r.note(mask, v, x);
             });
         } else {
             uint32_t n = 0;
@@ -863,7 +887,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                     n += x[i] >= inner;
                     mask |= x[i] >= outer && x[i] < inner ? 1u << i : 0u;
                 }
-                if (mask) r.note(mask, v, x);
+                r.note(mask, v, x);
             });
             s = n;
         }
@@ -882,6 +906,50 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         if (sums && tries == 0) {
             r.collect(1, turn, v);
             all = SampleRow<T>::warp_sum(v[0] + v[1] + v[2] + v[3]);
+        }
+        const int handed = r.handed(turn);
+        if (few && handed <= kSampleThreads) {
+            // A member a thread.  Its rank among the codes orders the weights, sums over that order say where top-k and top-p end,
+            // and sums over the smaller places which one is drawn.
+            u64 own[1];
+            r.take_members(turn, own);
+            const u64 mine = own[0], w = mine ? weight(key_value((uint32_t)(mine >> 32))) : 0;
+            sh.codes[threadIdx.x] = mine;
+            __syncthreads();
+            int rank = 0;
+            if (r.warp * 32 < handed)
+#pragma unroll 4
+                for (int i = 0; i < handed; ++i) rank += sh.codes[i] > mine;
+            const int kept = some ? min(k, handed) : handed;
+            sh.ordered[threadIdx.x] = 0;
+            __syncthreads();
+            if (mine && rank < kept) sh.ordered[rank] = w;
+            __syncthreads();
+            const u64 at_rank = sh.ordered[threadIdx.x];
+            const u64 upto = r.block_scan(at_rank);
+            if (threadIdx.x == kSampleThreads - 1) sh.above = upto;
+            if (threadIdx.x == 0) sh.digit = (uint32_t)kept;
+            __syncthreads();
+            if (top_p) {
+                const u64 whole = sh.above, goal = share(some ? whole : all);
+                if (whole < goal) { bias += (int64_t)(above_to - whole); continue; }       // (top-p alone: too short a guess)
+                if (at_rank && upto >= goal && upto - at_rank < goal) sh.digit = threadIdx.x + 1;
+                __syncthreads();
+            }
+            const bool stays = mine && rank < (int)sh.digit && (w >= floor_w || rank == 0);
+            sh.ordered[threadIdx.x] = stays ? w : 0;       // (now beside the codes; nobody reads the ranks' any more)
+            __syncthreads();
+            u64 before = 0;                                // what stays at smaller places
+            if (r.warp * 32 < handed)
+#pragma unroll 4
+                for (int i = 0; i < handed; ++i) before += (uint32_t)sh.codes[i] > (uint32_t)mine ? sh.ordered[i] : 0ull;
+            const u64 point = drawn(r.block_sum(stays ? w : 0, phase));
+            if (r.rank == 0 && stays && before <= point && before + w > point) {
+                const int place = (int)~(uint32_t)mine;
+                finish(place, to_f32(r.x0[place - skew]));
+            }
+            if (g.ctas > 1) cluster_sync_all();
+            return;
         }
         u64 code[kSampleOwn], w[kSampleOwn], f[kSampleOwn], whole = 0;
         r.take_members(turn, code);
@@ -964,7 +1032,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
 }
 
 constexpr int kSampleMost = 786432;                       // elements of a row (half of that in 32 bits)
-constexpr int kSampleHeld = 80 * 1024;                    // bytes of shares with which two CTAs fit a multiprocessor
+constexpr int kSampleHeld = 76 * 1024;                    // bytes of shares with which two CTAs fit a multiprocessor
 
 template <typename T>
 int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
