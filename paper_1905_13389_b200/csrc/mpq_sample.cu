@@ -80,6 +80,7 @@ __device__ __forceinline__ uint2 ld_cluster32x2(uint32_t addr) {
 struct SampleBorder {                                      // the bin in which a sum is reached: the sums before and with it, the counts
     u64 above, above_to;
     uint32_t digit, count, count_to;
+    float edge;                                           // the smallest number in it, or over it
 };
 // What passes between a row's CTAs, two of each: one is written while others may still read the one before.
 struct SampleShared {
@@ -316,33 +317,45 @@ struct SampleRow {
         before = __shfl_sync(0xffffffffu, before, in);
         if (which / kSampleWarps != rank) return -1;
         which %= kSampleWarps;
-        const int n = warp_chunks * E, per = ((n + kSampleWarps - 1) / kSampleWarps + 31) / 32 * 32, from = min(n, warp * per), to = min(n, from + per);
+        // a sixteenth by each warp, several reads under way
+        const int n = warp_chunks * E, per = (n + kSampleWarps - 1) / kSampleWarps, from = min(n, warp * per), to = min(n, from + per);
         u64 part = 0;
+        constexpr int kAtOnce = 8;
 #pragma unroll 1
-        for (int i = from + lane; i < to; i += 32) {
-            int place;
-            float x;
-            element(which, i, place, x);
-            part += f(place, x);
+        for (int i = from + lane; i < to; i += 32 * kAtOnce) {
+            int place[kAtOnce];
+            float x[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) element(which, min(i + 32 * j, to - 1), place[j], x[j]);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) part += i + 32 * j < to ? f(place[j], x[j]) : 0;
         }
         part = warp_sum(part);
         if (lane == 0) sh.scan[warp] = part;
         __syncthreads();
-        before += warp_sum(lane < warp ? sh.scan[lane] : 0);
-        if (before > goal || before + part <= goal) return -1;
+        const u64 sums_to = warp_scan(lane < kSampleWarps ? sh.scan[lane] : 0) + before;
+        const int sixteenth = __ffs(__ballot_sync(0xffffffffu, sums_to > goal)) - 1;
+        if (sixteenth < 0) return -1;
+        if (sixteenth > 0) before = __shfl_sync(0xffffffffu, sums_to, sixteenth - 1);
+        __syncthreads();
+        // ... and that one by all threads, in their order
+        const int last = min(n, (sixteenth + 1) * per);
 #pragma unroll 1
-        for (int i0 = from; i0 < to; i0 += 32) {
+        for (int i0 = sixteenth * per; i0 < last; i0 += kSampleThreads) {
+            const int i = i0 + (int)threadIdx.x;
             int place = 0;
             float x = 0.0f;
             u64 w = 0;
-            if (i0 + lane < to) {
-                element(which, i0 + lane, place, x);
+            if (i < last) {
+                element(which, i, place, x);
                 w = f(place, x);
             }
-            const u64 sum_to = before + warp_scan(w);
-            const uint32_t over = __ballot_sync(0xffffffffu, sum_to > goal);
-            if (over) return lane == __ffs(over) - 1 ? place : -1;
-            before = __shfl_sync(0xffffffffu, sum_to, 31);
+            const u64 upto_here = before + block_scan(w);
+            if (threadIdx.x == kSampleThreads - 1) sh.above = upto_here;
+            __syncthreads();
+            before = sh.above;
+            if (before > goal) return upto_here > goal && upto_here - w <= goal ? place : -1;
+            __syncthreads();
         }
         return -1;
     }
@@ -356,8 +369,8 @@ struct SampleRow {
     // Adds up what the CTAs have counted by bins, worth(bin, count, offsets) of each, and finds, from the highest bin down, those in
     // which the sum reaches goals(sum of all, ..) (the lowest that has anything, if none does): sh.border, N of them.  Groups of
     // 32 bins are summed by each CTA and looked at first, so that little passes between the CTAs.
-    template <int N, typename Worth, typename Goals>
-    __device__ __forceinline__ void find_borders(Worth worth, Goals goals) {
+    template <int N, typename Worth, typename Goals, typename Edge>
+    __device__ __forceinline__ void find_borders(Worth worth, Goals goals, Edge edge) {
         __syncthreads();
         for (int i = warp; i < kSampleGroups; i += kSampleWarps) {
             const int bin = i * 32 + lane;
@@ -365,7 +378,7 @@ struct SampleRow {
             if (lane == 0) { sh.coarse[turn][0][i] = value; sh.coarse[turn][1][i] = all; }
         }
         sync();
-        if (warp == 0) {
+        if (warp < N) {                                   // a warp for each
             // two groups a lane, the highest first
             u64 value[2] = {}, n[2] = {};
             for (int c = 0; c < ctas; ++c)
@@ -379,27 +392,25 @@ struct SampleRow {
             u64 goal[N];
             goals(__shfl_sync(0xffffffffu, to, 31), goal);
             const uint32_t any = __ballot_sync(0xffffffffu, (n[0] | n[1]) != 0);
-#pragma unroll 1
-            for (int k = 0; k < N; ++k) {
-                const u64 here_goal = k == 0 ? goal[0] : goal[N - 1];
-                const uint32_t reach = __ballot_sync(0xffffffffu, to >= here_goal);
-                const int in = reach ? __ffs(reach) - 1 : 31 - __clz(any);      // something has been counted
-                const bool second = reach ? to - value[1] < here_goal : n[1] != 0;
-                const int group = __shfl_sync(0xffffffffu, kSampleGroups - 1 - 2 * lane - (second ? 1 : 0), in);
-                const u64 before = __shfl_sync(0xffffffffu, to - value[1] - (second ? 0 : value[0]), in);
-                const u64 n_before = __shfl_sync(0xffffffffu, n_to - n[1] - (second ? 0 : n[0]), in);
-                const int bin = group * 32 + 31 - lane;
-                u64 here = 0, w = 0;
-                for (int c = 0; c < ctas; ++c) {
-                    const uint32_t one = ld_cluster32(peer(&sh.bins[turn][bin], c));
-                    here += one;
-                    w += worth(bin, one, ld_cluster32(peer(&sh.offsets[bin], c)));
-                }
-                const u64 upto = before + warp_scan(w), n_upto = n_before + warp_scan(here);
-                const uint32_t reaches = __ballot_sync(0xffffffffu, upto >= here_goal), anything = __ballot_sync(0xffffffffu, here != 0);
-                if (lane == (reaches ? __ffs(reaches) - 1 : 31 - __clz(anything)))
-                    sh.border[k] = SampleBorder{upto - w, upto, (uint32_t)bin, (uint32_t)here, (uint32_t)n_upto};
+            const u64 here_goal = warp == 0 ? goal[0] : goal[N - 1];
+            const uint32_t reach = __ballot_sync(0xffffffffu, to >= here_goal);
+            const int in = reach ? __ffs(reach) - 1 : 31 - __clz(any);          // something has been counted
+            const bool second = reach ? to - value[1] < here_goal : n[1] != 0;
+            const int group = __shfl_sync(0xffffffffu, kSampleGroups - 1 - 2 * lane - (second ? 1 : 0), in);
+            const u64 before = __shfl_sync(0xffffffffu, to - value[1] - (second ? 0 : value[0]), in);
+            const u64 n_before = __shfl_sync(0xffffffffu, n_to - n[1] - (second ? 0 : n[0]), in);
+            const int bin = group * 32 + 31 - lane;
+            u64 here = 0, w = 0;
+            for (int c = 0; c < ctas; ++c) {
+                const uint32_t one = ld_cluster32(peer(&sh.bins[turn][bin], c));
+                here += one;
+                w += worth(bin, one, ld_cluster32(peer(&sh.offsets[bin], c)));
             }
+            const u64 upto = before + warp_scan(w), n_upto = n_before + warp_scan(here);
+            const uint32_t reaches = __ballot_sync(0xffffffffu, upto >= here_goal), anything = __ballot_sync(0xffffffffu, here != 0);
+            const int at = reaches ? __ffs(reaches) - 1 : 31 - __clz(anything);
+            const float number = edge(warp, (uint32_t)__shfl_sync(0xffffffffu, bin, at));
+            if (lane == at) sh.border[warp] = SampleBorder{upto - w, upto, (uint32_t)bin, (uint32_t)here, (uint32_t)n_upto, number};
         }
         __syncthreads();
         turn ^= 1;
@@ -600,6 +611,26 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             }
         }
     }
+    // Small k: where m warps have j elements each that are no smaller than some number, and m j is k or more, the first k are no
+    // smaller either.  The number is the m-th largest of the warps' j-th largest among their threads' own largest elements;
+    // with m three quarters of the warps it leaves some two or three times k.
+    const bool some = k > 0 && k < g.vocab;
+    const int warps = min((int)(((int64_t)g.vocab + skew + g.warp_chunks * E - 1) / (g.warp_chunks * E)), g.ctas * kSampleWarps);      // that have elements
+    const int per_warp = (int)min((4 * (int64_t)k + 3 * warps - 1) / (3 * warps), (int64_t)64);
+    const bool by_threads = some && per_warp <= 24;
+    u64 last = 0;                                         // the key of that element
+    if (by_threads) {
+        uint32_t key = order_key(best);
+#pragma unroll
+        for (int size = 2; size <= 32; size *= 2)         // sorted by the warp, the largest first
+#pragma unroll
+            for (int o = size / 2; o > 0; o >>= 1) {
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, key, o);
+                const bool falling = (lane & size) == 0 || size == 32;
+                key = ((lane & o) == 0) == falling ? max(key, other) : min(key, other);
+            }
+        last = __shfl_sync(0xffffffffu, key, per_warp - 1);
+    }
     u64 code = 0;                                         // 0: nothing over -infinity; all ones: a NaN
     if (best > -INFINITY) {
         float x[E];
@@ -610,12 +641,31 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         code = (u64)order_key(best) << 32 | (uint32_t)~(r.v0 + best_chunk * E + at);
     }
     if (nan) code = ~0ull;
+    float reach = -INFINITY;
     {
         u64 v[4];
         for (int o = 16; o > 0; o >>= 1) code = max(code, __shfl_xor_sync(0xffffffffu, code, o));
+        if (lane == 0) sh.parts[r.turn][1][r.warp] = last;
+        const int turn = r.turn;
         r.gather(code, v);
         code = max(max(v[0], v[1]), max(v[2], v[3]));
         for (int o = 16; o > 0; o >>= 1) code = max(code, __shfl_xor_sync(0xffffffffu, code, o));
+        if (by_threads) {
+            r.collect(1, turn, v);
+            const int m = (k + per_warp - 1) / per_warp;
+            int over[4] = {}, from[4] = {};                // how many are larger, and no smaller
+            for (int l = 0; l < g.ctas * kSampleWarps / 4; ++l)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t other = __shfl_sync(0xffffffffu, (uint32_t)v[i], l);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) { over[q] += other > (uint32_t)v[q]; from[q] += other >= (uint32_t)v[q]; }
+                }
+            uint32_t mth = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) if (over[q] < m && from[q] >= m) mth = (uint32_t)v[q];
+            reach = key_value(max(__reduce_max_sync(0xffffffffu, mth), 0x00800000u));      // (finite, where there are fewer than k)
+        }
     }
     const float top = key_value((uint32_t)(code >> 32));
     const int first = (int)~(uint32_t)code;
@@ -630,9 +680,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
         return;
     }
 
-    const bool some = k > 0 && k < g.vocab, top_p = p < 1.0f;
-    // Small k: as many of the threads' own largest elements as k say how far the first k can reach at most.
-    const bool by_threads = some && k <= kSampleThreads * g.ctas / 2;
+    const bool top_p = p < 1.0f;
     const bool cut_off = !greedy && ((some && !by_threads) || (top_p && !some));
     const SampleWeight weight(top, warm, g.shift, sh.powers);
     const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
@@ -735,7 +783,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                 });
                 above1 += above2;
                 const u64 left = want > above1 ? want - above1 : 1;
-                r.template find_borders<1>(as_counted, [&](u64, u64 (&goal)[1]) { goal[0] = left; });
+                r.template find_borders<1>(as_counted, [&](u64, u64 (&goal)[1]) { goal[0] = left; }, [](int, uint32_t) { return 0.0f; });
                 above2 = sh.border[0].above;
                 high = level ? high << 11 | sh.border[0].digit : sh.border[0].digit;
             }
@@ -808,21 +856,6 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
     }
     const bool least_only = !some && !top_p;
     bool by_reach = by_threads;
-    float reach = -INFINITY;
-    if (by_threads) {
-        // each CTA's share of k (by its share of the row) among its threads, and the least of what the CTAs find: k elements at
-        // least are no smaller
-        const u64 code[kSampleOwn] = {best > -INFINITY ? (u64)order_key(best) << 32 | (threadIdx.x + 1) : 0ull};
-        const u64 one[kSampleOwn] = {code[0] ? 1ull : 0ull};
-        const int64_t span = (int64_t)kSampleWarps * g.warp_chunks * E, from = max(r.rank * span - skew, (int64_t)0), to = min((r.rank + 1) * span - skew, (int64_t)g.vocab);
-        const u64 goal = (u64)((max(to - from, (int64_t)0) * k + g.vocab - 1) / g.vocab), have = r.block_sum(one[0], phase);
-        u64 v[4];
-        r.gather(~(goal == 0 ? ~0ull : have < goal ? 0ull : r.resolve(code, one, goal) >> 32), v);
-        u64 lowest = max(max(v[0], v[1]), max(v[2], v[3]));
-        for (int o = 16; o > 0; o >>= 1) lowest = max(lowest, __shfl_xor_sync(0xffffffffu, lowest, o));
-        lowest = ~lowest;
-        reach = lowest ? key_value((uint32_t)lowest) : key_value(0x00800000u);
-    }
 #pragma unroll 1
     for (int tries = 0; open && tries < 4; ++tries) {
         float outer, inner = INFINITY;                    // what is handed out is `outer` or more and below `inner`
@@ -847,15 +880,15 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                 const int64_t margin = (int64_t)(guessed >> 12), aim = (int64_t)(tries == 0 ? share(guessed) : share(all)) + bias;
                 goal[0] = (u64)max(aim - margin, (int64_t)1);
                 goal[1] = (u64)max(aim + margin, (int64_t)1);
-            });
+            }, [&](int which, uint32_t digit) { return r.least_of(top, steps, which == 0 ? digit + 1 : digit); });
             const SampleBorder hi = sh.border[0], lo = sh.border[1];
             above = hi.above;
             above_to = lo.above_to;
             const uint32_t most = (uint32_t)(kSampleThreads * kSampleOwn);
             few = lo.count_to <= most;
-            outer = r.least_of(top, steps, lo.digit);
+            outer = lo.edge;
             if (!few) {
-                inner = r.least_of(top, steps, hi.digit + 1);
+                inner = hi.edge;
                 if (lo.count_to - (hi.count_to - hi.count) > most) break;
             }
         }
