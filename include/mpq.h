@@ -451,7 +451,7 @@ int mpq_pages_trim(int32_t* table, int64_t per_sequence, int32_t* lens, int sequ
  * outside 0 .. adapters-1 (-1 by convention), take none.
  * down [adapters][rank][mpq_level_row_bytes(k)] (0 behind element k-1) and up [adapters][n][rank],
  * of adapter_dtype (MPQ_F16 or MPQ_BF16), 16-byte aligned; rank is 16, 32, 64 or 128 (others
- * are padded with zeros).  factor [adapters] may be NULL (ones).
+ * are padded with zeros).  factor [adapters] may be NULL (ones).  adapters n and 3 m are below 2^31.
  * workspace: mpq_linear_adapted_workspace(m, rank) bytes, 16-byte aligned, used by this call alone. */
 int64_t mpq_linear_adapted_workspace(int64_t m, int rank);
 int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const int32_t* a_sums, int a_bits,

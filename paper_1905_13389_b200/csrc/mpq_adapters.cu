@@ -19,12 +19,17 @@ constexpr int kDownThreads = 256, kDownWarps = kDownThreads / 32;
 // Two levels (bytes `at` and `at` + 1 of a word) as the odd numbers 2u - L, in a pair of W.
 template <typename W>
 __device__ __forceinline__ uint32_t odd_pair(uint32_t word, int at, float L) {
+    if constexpr (std::is_same_v<W, __half>) {            // 2^10 + u, twice, in the low bits of a pair
+        const uint32_t raised = __byte_perm(word, 0x64646464u, at == 0 ? 0x4140 : 0x4342);
+        const __half2 u = __hsub2(*reinterpret_cast<const __half2*>(&raised), __float2half2_rn(1024.0f));
+        const __half2 x = __hfma2(u, __float2half2_rn(2.0f), __float2half2_rn(-L));
+        return *reinterpret_cast<const uint32_t*>(&x);
+    }
     const float a = __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7650u + (uint32_t)at)) - 8388608.0f;
     const float b = __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7651u + (uint32_t)at)) - 8388608.0f;
     const float x = fmaf(2.0f, a, -L), y = fmaf(2.0f, b, -L);
     uint32_t r;
-    if constexpr (std::is_same_v<W, __half>) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
-    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
     return r;
 }
 __device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
@@ -114,10 +119,18 @@ __global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const Adapte
 #pragma unroll
             for (int q = 0; q < kAhead; ++q) multiply(x[q]);
         }
-    } else {
+    } else if constexpr (MT == 2) {                       // (a second block would not fit beside the first)
         for (int64_t kb = kb0 + part; kb < kb1; kb += parts) {
             Block x;
             ask(kb, x);
+            multiply(x);
+        }
+    } else {
+        Block next;
+        ask(kb0 + part, next);
+        for (int64_t kb = kb0 + part; kb < kb1; kb += parts) {
+            const Block x = next;
+            ask(kb + parts, next);
             multiply(x);
         }
     }
@@ -211,10 +224,10 @@ int launch_down(const AdapterArgs& g, int groups, cudaStream_t st) {
 
 template <typename W>
 int adapter_down_typed(const AdapterArgs& g, cudaStream_t st) {
-    const int tiles = g.rank / 16, groups = tiles <= 2 ? 1 : tiles <= 4 ? 2 : 4;         // two m-tiles to a warp
+    const int tiles = g.rank / 16;
     if (g.m <= 8 * (int64_t)(g.batch > 0 ? g.batch : 1))  // pieces of up to 8 tokens on average
-        return tiles == 1 ? launch_down<W, 1, 1>(g, 1, st) : launch_down<W, 1, 2>(g, groups, st);
-    return tiles == 1 ? launch_down<W, 4, 1>(g, 1, st) : launch_down<W, 4, 2>(g, groups, st);
+        return tiles == 1 ? launch_down<W, 1, 1>(g, 1, st) : launch_down<W, 1, 2>(g, tiles / 2, st);
+    return tiles == 1 ? launch_down<W, 4, 1>(g, 1, st) : launch_down<W, 4, 2>(g, tiles / 2, st);
 }
 
 int adapter_down(const AdapterArgs& g, int dtype, cudaStream_t st) {

@@ -399,20 +399,26 @@ constexpr int kPairCols = 128;
 template <bool ADAPTED>
 struct PairShape {
     static constexpr int stage_bytes = (128 + kPairCols / 2) * kBlock;   // per CTA
-    // with adapters fewer: what they read by all storing warps then stays in L1
-    static constexpr int stages = ADAPTED ? 4 : 6;
+    static constexpr int stages = ADAPTED ? 5 : 6;        // with adapters L1 keeps what their reads share
     static constexpr int row_words = 64;                            // column pair p of row r lies at pair p ^ r: no bank conflicts either way
     static constexpr int transpose_bytes = kPairStoreWarps / 2 * 32 * row_words * 4;
     static constexpr int term_bytes = ADAPTED ? kPairStoreWarps / 2 * 64 * 16 : 0;      // the columns' constants
     static constexpr int smem = stages * stage_bytes + transpose_bytes + term_bytes + 1024;
 };
 
-// What the adapters of 16 rows add to 64 columns, into TMEM lanes and columns from `at` on: the parts of z times the columns'
-// rows of `up` as 16 x 8 x 16 matrix instructions.  A lane owns four adjacent ranks of 16, in both operands alike.  One
-// adapter after the other of those that the rows have: a row takes its own one's sums alone, so that nothing of another's
-// reaches it.  PARTS: 16-bit results need two parts of z (2^-16 of it, 2^-22 in float16), 32-bit ones all.
-// (fp32 multiply-adds instead would take 2 rank / 32 instructions an output for some rank / 250 here; products on tf32, whose
-// range needs no parts' exponent, took twice the time of these and kept the tensor cores from the product itself.)
+__device__ __forceinline__ void umma_f16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// What adapters add in the pair form.  Where one adapter has all 256 rows of a tile, the parts of z times its rows of `up` are more
+// blocks of the tile's product, on the 5th-generation tensor cores, into accumulators of their own (kind::f16; 64 ranks
+// of a part are a block, ranks that are not there are read as zeros).  Other tiles, with ends of sequences in them, have it
+// from low_rank_tile: 16 rows and 64 columns by 16 x 8 x 16 matrix instructions of the storing warps, a lane owning four adjacent
+// ranks of 16 in both operands alike, one adapter after the other of those that the rows have: a row takes its own one's
+// sums alone, so that nothing of another's reaches it.  PARTS: 16-bit results need two parts of z (2^-16 of it, 2^-22 in
+// float16), 32-bit ones all.
 template <typename W, int PARTS>
 __device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0, int64_t c0, uint32_t at, int lane, int turn) {
     const int row = lane >> 2, quad = lane & 3;
@@ -468,10 +474,22 @@ __device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0,
     } while (left);
 }
 
+// The adapter that all of a tile's rows have (those behind the last row have any), or -1; by a warp, after chain_wait().
+__device__ __forceinline__ int tile_adapter(const LinearArgs& g, int64_t m0, int lane) {
+    const int64_t last = g.m - 1;
+    const int first = __ldg(g.low.chosen + m0);
+    bool same = first >= 0 && first < g.adapters;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) same = same && __ldg(g.low.chosen + min(m0 + i * 32 + lane, last)) == first;
+    return __all_sync(0xffffffffu, same) ? first : -1;
+}
+constexpr int kBlockRanks = 64;                            // of a block, which is 128 bytes wide
+
 template <typename T, typename W>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const LinearArgs g,
-                   int tiles_m, int tiles) {
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w,
+                   const __grid_constant__ CUtensorMap map_z, const __grid_constant__ CUtensorMap map_up, const LinearArgs g, int tiles_m, int tiles) {
+    constexpr int kZParts = std::is_same_v<W, __nv_bfloat16> && std::is_same_v<T, float> ? kLowParts : 2;
     using Shape = PairShape<!std::is_void_v<W>>;
     constexpr int BN = kPairCols, kStages = Shape::stages, kAccs = 2;
     extern __shared__ unsigned char smem_raw[];
@@ -498,7 +516,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         tma_prefetch(&map_a);
         tma_prefetch(&map_w);
     }
-    constexpr uint32_t kTmemCols = kAccs * BN * (std::is_void_v<W> ? 1 : 2);       // what the adapters add lies behind the accumulators
+    constexpr uint32_t kTmemCols = kAccs * BN * (std::is_void_v<W> ? 1 : 2);       // what the adapters add lies behind the accumulators, as many
     if (warp == 0) tmem_alloc<2>(&tmem_holder, kTmemCols);
     tmem_fence_before();
     cluster_sync_all();                                    // both CTAs' barriers exist
@@ -510,6 +528,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         chain_next();
         if (warp >= 2) chain_wait();
     }
+    [[maybe_unused]] bool waited = false;                  // of the other warps: once they need what the kernel before has made
+    [[maybe_unused]] const int low_blocks = std::is_void_v<W> ? 0 : kZParts * ((g.rank + kBlockRanks - 1) / kBlockRanks);
 
     const int pair = (int)blockIdx.x / 2, pairs = (int)gridDim.x / 2;
     const int my_tiles = tiles > pair ? (tiles - pair + pairs - 1) / pairs : 0;
@@ -538,6 +558,21 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     tma_load_2d_pair(dst + 128 * kBlock, &map_w, kb * kBlock, n0 + (int)rank * (BN / 2), bar);
                 }
             }
+            if constexpr (!std::is_void_v<W>) {
+                if (!waited) chain_wait();
+                waited = true;
+                const int id = tile_adapter(g, m0, lane);
+                for (int e = 0; ok && id >= 0 && e < low_blocks; ++e, ++issued) {
+                    const int s = issued % kStages, part = e % kZParts, r0 = e / kZParts * kBlockRanks;
+                    if (issued >= kStages && !mbar_wait_warp(empty(s), (issued / kStages - 1) & 1, &failed, g.polls)) { ok = false; break; }
+                    if (leader) {
+                        const uint32_t dst = ring + s * Shape::stage_bytes, bar = map_to_cta(full(s), 0);
+                        if (rank == 0) mbar_expect_tx(full(s), 2 * Shape::stage_bytes);
+                        tma_load_2d_pair(dst, &map_z, r0, (int)(part * g.m) + m0 + (int)rank * 128, bar);
+                        tma_load_2d_pair(dst + 128 * kBlock, &map_up, r0, (int)(id * g.n) + n0 + (int)rank * (BN / 2), bar);
+                    }
+                }
+            }
         }
     } else if (warp == 1) {
         if (rank == 0) {
@@ -561,6 +596,26 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 #pragma unroll
                         for (int j = 0; j < kBlock / 32; ++j) umma_u8<2>(d, da + 2 * j, db + 2 * j, idesc, kb > 0 || j > 0);
                         umma_commit<2>(empty(s));
+                    }
+                }
+                if constexpr (!std::is_void_v<W>) {
+                    if (!waited) chain_wait();
+                    waited = true;
+                    int m0, n0;
+                    origin(i, m0, n0);
+                    const int id = tile_adapter(g, m0, lane);
+                    constexpr uint32_t idesc_low = umma_idesc_f16(256, BN) | (std::is_same_v<W, __nv_bfloat16> ? 1u << 7 | 1u << 10 : 0u);
+                    for (int e = 0; ok && id >= 0 && e < low_blocks; ++e, ++consumed) {
+                        const int s = consumed % kStages, r0 = e / kZParts * kBlockRanks;
+                        if (!mbar_wait_warp(full(s), (consumed / kStages) & 1, &failed, g.polls)) { ok = false; break; }
+                        tmem_fence_after();
+                        const uint32_t at = ring + s * Shape::stage_bytes;
+                        if (leader) {
+                            const uint64_t da = umma_desc(at), db = umma_desc(at + 128 * kBlock);
+                            for (int j = 0; j < kBlockRanks / 16 && r0 + 16 * j < g.rank; ++j)
+                                umma_f16_pair(d + kAccs * BN, da + 2 * j, db + 2 * j, idesc_low, e > 0 || j > 0);
+                            umma_commit<2>(empty(s));
+                        }
                     }
                 }
                 if (leader && ok) umma_commit<2>(acc_full(acc));        // a sum that is not complete is never handed over
@@ -596,16 +651,20 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             RowTerm mine = {0.0f, 0u};                                             // lane's row; handed round by shuffles
             if (lane < rows) mine = row_term(g, row0 + lane);
             const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+            [[maybe_unused]] bool whole_tile = false;
             [[maybe_unused]] float4* terms = reinterpret_cast<float4*>(transpose + kPairStoreWarps / 2 * 32 * Shape::row_words) + block * 64;
             if constexpr (!std::is_void_v<W>) {
-                // What the adapters add, while the tile is multiplied.  Their sums lie by rows, so the columns' constants are needed
-                // by rows too: this warp's 32 columns of them.
+                // Sums of what the adapters add lie by rows, so the columns' constants are needed by rows too: this warp's 32
+                // columns of them.  Where the storing warps make those sums they do it while the tile is multiplied.
                 const int64_t c = (int64_t)n0 + c0 + part * 32 + lane;
                 const ColTerm t = c < g.n ? col_term(g, c) : ColTerm{0.0f, 0u, 0.0f};
                 terms[part * 32 + lane] = make_float4(t.scale, __uint_as_float(t.term), t.bias, 0.0f);
-                tmem_fence_after();                        // (the block has read what the tile before had there)
-                low_rank_tile<W, std::is_same_v<W, __nv_bfloat16> && std::is_same_v<T, float> ? kLowParts : 2>(g, row0 + part * 16, (int64_t)n0 + c0, lanes + ((uint32_t)(part * 16) << 16) + (uint32_t)(kAccs * BN + c0), lane, quarter * 2 + part);
-                tmem_fence_before();
+                whole_tile = tile_adapter(g, m0, lane) >= 0;
+                if (!whole_tile) {
+                    tmem_fence_after();                    // (the block has read what an earlier tile had there)
+                    low_rank_tile<W, kZParts>(g, row0 + part * 16, (int64_t)n0 + c0, lanes + ((uint32_t)(part * 16) << 16) + (uint32_t)((kAccs + acc) * BN + c0), lane, quarter * 2 + part);
+                    tmem_fence_before();
+                }
                 block_sync();
                 tmem_fence_after();
             }
@@ -621,16 +680,17 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 uint32_t v[32];
                 tmem_load32(lanes + (uint32_t)(acc * BN + c0 + part * 32), v);
                 [[maybe_unused]] uint32_t low[32];
-                if constexpr (!std::is_void_v<W>) tmem_load32(lanes + (uint32_t)(kAccs * BN + c0 + part * 32), low);
+                if constexpr (!std::is_void_v<W>) tmem_load32(lanes + (uint32_t)((kAccs + acc) * BN + c0 + part * 32), low);
                 tmem_wait_ld();
                 tmem_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(acc), 0));       // this warp's part of the accumulator is read
                 if constexpr (!std::is_void_v<W>) {
+                    const float scale = whole_tile ? __ldg(g.low.scale + min(row0 + lane, g.m - 1)) : 1.0f;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
                         const float4 t = terms[part * 32 + j];
-                        v[j] = __float_as_uint(linear_value(g, v[j], mine, ColTerm{t.x, __float_as_uint(t.y), t.z}) + __uint_as_float(low[j]));
+                        v[j] = __float_as_uint(linear_value(g, v[j], mine, ColTerm{t.x, __float_as_uint(t.y), t.z}) + scale * __uint_as_float(low[j]));
                     }
                 }
 #pragma unroll
@@ -763,6 +823,18 @@ int launch_linear_small(const LinearArgs& g, cudaStream_t st) {
     return launch_status();
 }
 
+// [rows][ranks] pairs of bytes; boxes of box_rows rows x 64 ranks, 128-byte swizzle; what lies outside reads as 0.
+inline bool pair_tensor_map(CUtensorMap* map, const void* base, int64_t rows, int64_t ranks, int box_rows) {
+    const TensorMapEncodeFn encode = tensor_map_encoder();
+    const cuuint64_t dims[2] = {(cuuint64_t)ranks, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ranks * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)kBlockRanks, (cuuint32_t)box_rows};
+    const cuuint32_t elem[2] = {1, 1};
+    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(base), dims, strides, box, elem,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, typename W>
 int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     using Shape = PairShape<!std::is_void_v<W>>;
@@ -774,12 +846,17 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
     if (rc != MPQ_OK) return rc;
     CUtensorMap map_w, map_a;
     if (!byte_tensor_map(&map_w, g.w, g.n, g.row_bytes, BN / 2) || !byte_tensor_map(&map_a, g.a, g.m, g.row_bytes, 128)) return MPQ_ERR_CUDA;
+    CUtensorMap map_z = map_a, map_up = map_w;
+    if constexpr (!std::is_void_v<W>) {
+        if (!pair_tensor_map(&map_z, g.low.parts, (int64_t)kLowParts * g.m, g.rank, 128) ||
+            !pair_tensor_map(&map_up, g.up, (int64_t)g.adapters * g.n, g.rank, BN / 2)) return MPQ_ERR_CUDA;
+    }
     const int pairs = sm_count() / 2;
     if (pairs == 0) return MPQ_ERR_CUDA;
     const int64_t tiles_m = ceil_div(g.m, 256), tiles = tiles_m * ceil_div(g.n, BN);
     if (tiles > (1 << 28)) return MPQ_ERR_BAD_SHAPE;
     const unsigned ctas = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
-    return launch_chained_as(true, kernel, ctas, (unsigned)kPairThreads, smem, st, map_a, map_w, g, (int)tiles_m, (int)tiles);
+    return launch_chained_as(true, kernel, ctas, (unsigned)kPairThreads, smem, st, map_a, map_w, map_z, map_up, g, (int)tiles_m, (int)tiles);
 }
 
 // Which form.  Up to 64 rows the weights' own traffic decides: the small form, its tile just wide enough.  Above, the
@@ -849,7 +926,7 @@ extern "C" int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const 
     int rc = linear_args(g, a, a_scale, a_sums, a_bits, w, w_scale, w_sums, w_bits, m, n, k, bias, glue, residual, ldr, out, dtype, ldo);
     if (rc != MPQ_OK) return rc;
     if (m != 0 && (!down || !up || !q_starts || (batch != 0 && !ids) || !workspace)) return MPQ_ERR_NULL;
-    if (adapters <= 0 || rank <= 0 || batch < 0) return MPQ_ERR_BAD_SHAPE;
+    if (adapters <= 0 || rank <= 0 || batch < 0 || kLowParts * m > 0x7fffffff || adapters * n > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
     if ((adapter_dtype != MPQ_F16 && adapter_dtype != MPQ_BF16) || (rank != 16 && rank != 32 && rank != 64 && rank != 128)) return MPQ_ERR_UNSUPPORTED;
     if (!aligned16(down) || !aligned16(up) || !aligned16(workspace) || !aligned_to(factor, 4) || !aligned_to(q_starts, 4) || !aligned_to(ids, 4)) return MPQ_ERR_ALIGN;
     if (m == 0) return MPQ_OK;

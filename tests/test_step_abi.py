@@ -51,6 +51,7 @@ def test_linear_adapted(mpq, mem):
         assert lin(**{name: N}) == NULL_, name
     assert lin(m=-1) == SHAPE and lin(n=0) == SHAPE and lin(k=0) == SHAPE and lin(ldo=7) == SHAPE and lin(res=p, ldr=7) == SHAPE
     assert lin(adapters=0) == SHAPE and lin(rank=0) == SHAPE and lin(rank=-16) == SHAPE and lin(batch=-1) == SHAPE
+    assert lin(adapters=1 << 29) == SHAPE and lin(m=1 << 30, ldo=8) == SHAPE
     assert lin(ab=0) == UNSUP and lin(wb=9) == UNSUP and lin(dtype=3) == UNSUP and lin(glue=5) == UNSUP
     assert lin(at=0) == UNSUP and lin(at=3) == UNSUP and lin(rank=8) == UNSUP and lin(rank=24) == UNSUP and lin(rank=144) == UNSUP
     assert lin(k=33026) == OVER
