@@ -539,6 +539,30 @@ struct SampleRow {
             at = next;
         }
     }
+    // How many of the members, one to a thread, have a larger code.
+    __device__ __forceinline__ int rank_of(u64 code, int members) {
+        sh.codes[threadIdx.x] = code;
+        __syncthreads();
+        int rank = 0;
+        if (warp * 32 < members)
+#pragma unroll 4
+            for (int i = 0; i < members; ++i) rank += sh.codes[i] > code;
+        return rank;
+    }
+    // resolve() of as many members as threads, one to a thread: by their ranks.
+    __device__ __forceinline__ u64 resolve_few(u64 code, u64 f, int members, u64 goal) {
+        const int rank = rank_of(code, members);
+        sh.ordered[threadIdx.x] = 0;
+        __syncthreads();
+        if (code) sh.ordered[rank] = f;
+        __syncthreads();
+        const u64 here = sh.ordered[threadIdx.x], upto = block_scan(here);
+        if (upto >= goal && upto - here < goal) sh.digit = threadIdx.x;
+        __syncthreads();
+        if (code && rank == (int)sh.digit) sh.member = code;
+        __syncthreads();
+        return sh.member;
+    }
     // Whether no CTA has been given more than it can hand out, nor all together more than one can take.
     __device__ __forceinline__ bool can_take(int noted_turn) const {
         const uint32_t n = lane < ctas ? ld_cluster32(peer(&sh.noted[noted_turn], lane)) : 0;
@@ -947,12 +971,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             u64 own[1];
             r.take_members(turn, own);
             const u64 mine = own[0], w = mine ? weight(key_value((uint32_t)(mine >> 32))) : 0;
-            sh.codes[threadIdx.x] = mine;
-            __syncthreads();
-            int rank = 0;
-            if (r.warp * 32 < handed)
-#pragma unroll 4
-                for (int i = 0; i < handed; ++i) rank += sh.codes[i] > mine;
+            const int rank = r.rank_of(mine, handed);
             const int kept = some ? min(k, handed) : handed;
             sh.ordered[threadIdx.x] = 0;
             __syncthreads();
@@ -985,7 +1004,14 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
             return;
         }
         u64 code[kSampleOwn], w[kSampleOwn], f[kSampleOwn], whole = 0;
-        r.take_members(turn, code);
+        if (handed <= kSampleThreads) {
+            u64 own[1];
+            r.take_members(turn, own);
+#pragma unroll
+            for (int i = 0; i < kSampleOwn; ++i) code[i] = i == 0 ? own[0] : 0ull;
+        } else {
+            r.take_members(turn, code);
+        }
 #pragma unroll
         for (int i = 0; i < kSampleOwn; ++i) {
             w[i] = code[i] ? weight(key_value((uint32_t)(code[i] >> 32))) : 0;
@@ -1002,7 +1028,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleA
                 bias += (int64_t)(above - sum);
                 continue;
             } else {
-                e = r.resolve(code, f, goal - sum);
+                e = handed <= kSampleThreads ? r.resolve_few(code[0], f[0], handed, goal - sum) : r.resolve(code, f, goal - sum);
             }
         }
         open = false;
@@ -1075,11 +1101,13 @@ int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
     if (rc != MPQ_OK) return rc;
     const int sms = sm_count();
     if (sms == 0) return MPQ_ERR_CUDA;
-    // more CTAs to a row while the device has room for all rows' at once and a CTA 8192 elements
+    // More CTAs to a row, up to four, while the device has room for all rows' at once and a CTA 8192 elements.  Many CTAs that wait for one another
+    // cost more than they bring: us with 1 / 2 / 4 / 8 of them, 1 x 131072 in 32 bits 47 / 36 / 32 / 39, 7 x 50021 72 / 52 / 45 / 48,
+    // 64 x 131072 in 16 bits 203 / 134 / 106 / 141, 256 x 151000 205 / 216 / 278 / 519.
     const bool aligned = aligned16(g.logits) && (rows == 1 || g.ld % E == 0);
     const int64_t chunks = ceil_div((int64_t)g.vocab + (aligned ? 0 : E - 1), E);
     g.ctas = 1;
-    while (g.ctas < 8 && rows * g.ctas <= sms && g.vocab / g.ctas >= 8192) g.ctas *= 2;
+    while (g.ctas < 4 && rows * g.ctas <= sms && g.vocab / g.ctas >= 8192) g.ctas *= 2;
     constexpr int kGroup = SampleRow<T>::kGroup;
     g.warp_chunks = (int)ceil_div(chunks, g.ctas * kSampleWarps * kGroup) * kGroup;
     const int share = g.warp_chunks * kSampleWarps * 16;
