@@ -292,6 +292,20 @@ struct SampleRow {
         if (!weight.small(low) && low > -INFINITY) {      // (without a branch between them they are made side by side)
 #pragma unroll
             for (int i = 0; i < 8; ++i) f(i, weight.biased(x[i]));
+            return;
+        }
+        float live[8], least = weight.top;                 // forbidden tokens among ordinary ones: the same beside a choice
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            live[i] = x[i] > -INFINITY ? x[i] : weight.top;
+            least = fminf(least, live[i]);
+        }
+        if (!weight.small(least)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const u64 w = weight.biased(live[i]);
+                f(i, x[i] > -INFINITY ? w : SampleWeight::kBias);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) f(i, weight(x[i]) + SampleWeight::kBias);
@@ -586,8 +600,9 @@ struct SampleRow {
     }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const SampleArgs g) {
+// PER_SM: CTAs to a multiprocessor, one where there are no more (some of what it holds does not fit the registers of half of one).
+template <typename T, int PER_SM>
+__global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const SampleArgs g) {
     extern __shared__ uint4 held[];
     __shared__ SampleShared sh;
     constexpr int E = SampleRow<T>::E;
@@ -1096,9 +1111,6 @@ constexpr int kSampleHeld = 76 * 1024;                    // bytes of shares wit
 template <typename T>
 int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
     constexpr int E = 16 / (int)sizeof(T);
-    static PerDeviceOnce once;
-    const int rc = once.raise_smem_limit(sample_kernel<T>, kSampleHeld);
-    if (rc != MPQ_OK) return rc;
     const int sms = sm_count();
     if (sms == 0) return MPQ_ERR_CUDA;
     // More CTAs to a row, up to four, while the device has room for all rows' at once and a CTA 8192 elements.  Many CTAs that wait for one another
@@ -1113,6 +1125,11 @@ int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
     const int share = g.warp_chunks * kSampleWarps * 16;
     g.cached = share <= kSampleHeld;
     if (rows * g.ctas > 0x7fffffff) return MPQ_ERR_BAD_SHAPE;
+    static PerDeviceOnce once[2];
+    const bool alone = rows * g.ctas <= sms;
+    auto* kernel = alone ? sample_kernel<T, 1> : sample_kernel<T, 2>;
+    const int rc = once[alone].raise_smem_limit(kernel, kSampleHeld);
+    if (rc != MPQ_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * g.ctas), 1, 1);
     cfg.blockDim = dim3(kSampleThreads, 1, 1);
@@ -1126,7 +1143,7 @@ int launch_sample(SampleArgs g, int64_t rows, cudaStream_t st) {
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, sample_kernel<T>, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, kernel, g) != cudaSuccess) { cudaGetLastError(); return MPQ_ERR_CUDA; }
     return launch_status();
 }
 
