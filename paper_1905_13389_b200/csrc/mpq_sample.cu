@@ -798,16 +798,20 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
     int cut = 0x7fffffff;
     auto kept = [&](int v, float x) { const uint32_t key = order_key(x); return key > edge || (key == edge && v <= cut); };
     // The key, and the place among the equals of it, at which the sum of f from the top reaches `goal`: edge and cut.
-    // guess: f, or something near it in 32 bits, one at least, of which the whole row's sum fits 32 bits, in units of `unit` of f's.
-    auto narrow = [&](u64 goal, auto f, auto guess, float unit) {
-        if (r.row_sum(r.sum([&](int v, float x) { return kept(v, x) ? f(x) : 0ull; })) <= goal) return;       // all of it stays
+    // f: one, or (weights) the weight -- that is guessed at first, one at least, in 32 bits that hold the sum of what is open.
+    const float unit = exp2f((float)g.shift);
+    auto narrow = [&](u64 goal, auto f, bool weights) {
+        const u64 total = r.row_sum(r.sum([&](int v, float x) { return kept(v, x) ? f(x) : 0ull; }));
+        if (total <= goal) return;                        // all of it stays
         uint32_t over = 1u << (32 - kLowBits), under = 0xffffffffu;        // the border lies below `over` and above `under` (key >> kLowBits)
         u64 base = 0;                                     // f's sum from `over` on
         int64_t bias = 0;                                 // by how much the guesses above `under` fall short
         auto as_counted = [](uint32_t, uint32_t n, uint32_t) { return (u64)n; };
         for (int turns = 0; turns < 1 << 16; ++turns) {   // (each one takes at least one occupied key off the open ones)
             auto open = [&](uint32_t key) { const uint32_t high = key >> kLowBits; return high < over && (under == 0xffffffffu || high > under); };
-            const u64 want = (u64)max((int64_t)((double)(goal - base) / (double)unit) - bias, (int64_t)1);
+            const float scale = weights ? 4.2e9f / ((float)(total - base) * 1.0001f) : 1.0f, per = scale * unit;
+            auto guess = [&](float x) { return weights ? max(1u, __float2uint_rn(fast_exp2((x - top) * weight.coolf * 1.4426950408889634f) * per)) : 1u; };
+            const u64 want = (u64)max((int64_t)((double)(goal - base) * (double)scale) - bias, (int64_t)1);
             u64 above1 = 0, above2 = 0;
             uint32_t high = 0;
 #pragma unroll 1
@@ -816,8 +820,7 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
                 r.each([&](int v, float x) {
                     const uint32_t key = order_key(x);
                     if ((level == 0 || key >> 21 == high) && open(key) && kept(v, x)) {
-                        const uint32_t n = guess(x);
-                        if (n) atomicAdd(bins + (level ? key >> kLowBits & (kSampleBins - 1) : key >> 21), n);
+                        atomicAdd(bins + (level ? key >> kLowBits & (kSampleBins - 1) : key >> 21), guess(x));
                     }
                 });
                 above1 += above2;
@@ -853,7 +856,7 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
             __syncthreads();
             const u64 down_to = sh.above;                 // f's sum from the lowest of these keys on
             __syncthreads();
-            if (sum >= goal) { under = high; bias = (int64_t)((double)(sum - base) / (double)unit) - (int64_t)(above1 + above2); continue; }
+            if (sum >= goal) { under = high; bias = (int64_t)((double)(sum - base) * (double)scale) - (int64_t)(above1 + above2); continue; }
             if (down_to < goal) { over = high; base = down_to; bias = 0; continue; }
             if (upto >= goal && upto - mine < goal) {
                 const int i = upto - n[1] * w[1] >= goal ? 0 : 1;
@@ -886,7 +889,6 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
     u64 all = 0;                                          // top-p without top-k: what the row weighs, once it is known
     bool open = !all_stay;                                // whether it is still to be found what stays
     bool summed = all_stay;                               // whether `weights` is the sum of what stays
-    const float unit = exp2f((float)g.shift);
     int64_t bias = 0;
     int phase = 0;
     if (!some && !top_p && open) {                        // min-p alone: two steps below its border at most
@@ -1088,12 +1090,10 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
         if (g.ctas > 1) cluster_sync_all();
         return;
     }
-    if (open && some) narrow((u64)k, [](float) { return 1ull; }, [](float) { return 1u; }, 1.0f);
+    if (open && some) narrow((u64)k, [](float) { return 1ull; }, false);
     if (top_p && (some || open)) {
         const u64 left = r.row_sum(r.sum([&](int v, float x) { return kept(v, x) ? weight(x) : 0ull; }));
-        const float units = 4.2e9f / ((float)left * 1.0001f), per = units * unit;
-        narrow(share(left), weight,
-               [&](float x) { return x > -INFINITY ? max(1u, __float2uint_rn(fast_exp2((x - top) * weight.coolf * 1.4426950408889634f) * per)) : 0u; }, 1.0f / units);
+        narrow(share(left), weight, true);
     }
     auto stays = [&](int v, float x) {
         if (!kept(v, x)) return 0ull;

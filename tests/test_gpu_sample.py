@@ -37,7 +37,7 @@ def draw(x, warm, k, p, least, u):
     return order[at][min(len(at) - 1, int((upto <= goal).sum()))], near
 
 
-def check(mpq, cuda, x, u, warm=None, k=None, p=None, least=None, dtype="f32"):
+def check(mpq, cuda, x, u, warm=None, k=None, p=None, least=None, dtype="f32", open_ends=None):
     rows = x.shape[0]
     logits = x.to(TYPES[dtype]).to(cuda)
     to = lambda v, t=torch.float32: None if v is None else torch.as_tensor(v).to(t).to(cuda)      # noqa: E731
@@ -52,15 +52,15 @@ def check(mpq, cuda, x, u, warm=None, k=None, p=None, least=None, dtype="f32"):
         assert got[i].item() == ref or near, (i, got[i].item(), ref)
         # The share of the first of the order is exact, the others' sum is made of 32-bit terms.  With d a term's distance from the
         # first: d is rounded (d 2^-24 of the term), its product with log2 e too (d 2^-24; the constant is off by less than d 2^-25 of
-        # it), and the fast exponential is off by 2^-22; a thread adds at most 97 terms (196,608 bytes over 512 threads), each
-        # addition off by 2^-24 of the sum.  Of the logarithm of 1 + rest that is the error over 1 + rest, and one rounding at the end.
+        # it), and the fast exponential is off by 2^-22; a thread adds at most eight terms more than its share of the row (512 threads
+        # or more), each addition off by 2^-24 of the sum.  Of the logarithm of 1 + rest that is the error over 1 + rest, and one rounding at the end.
         d = xs[i] - xs[i].max()
         terms = np.exp(d)
         terms[np.argmax(xs[i])] = 0.0
-        off = (terms[terms > 0] * (2.5 * -d[terms > 0] + 4 + 97)).sum() * 2.0 ** -24 / (1 + terms.sum())
+        off = (terms[terms > 0] * (2.5 * -d[terms > 0] + 4 + 8 + len(d) / 512)).sum() * 2.0 ** -24 / (1 + terms.sum())
         want = d[got[i].item()] - math.log1p(terms.sum())
         assert abs(logprob[i].item() - want) <= 2.0 ** -24 * abs(want) + off + 1e-15, (i, logprob[i].item(), want)
-    assert ambiguous <= 1 + rows // 8
+    assert ambiguous <= (1 + rows // 8 if open_ends is None else open_ends)
     return got
 
 
@@ -207,6 +207,21 @@ def test_however_many_stay(mpq, cuda, rows, vocab):
         for n in (1024, 2048, 7000):
             check(mpq, cuda, x, u, k=[min(n, vocab - 1)] * rows)
             check(mpq, cuda, x, u, p=torch.softmax(x.double(), 1).sort(1, descending=True).values[:, :n].sum(1))
+
+
+@pytest.mark.parametrize("vocab", [300, 9001, 131072])
+def test_rules_at_the_ends_of_their_range(mpq, cuda, vocab):
+    """top-p a step below 1 and a step above 0, temperatures from the smallest number to the largest, min-p of next to nothing."""
+    x, u, _ = bell(5, vocab, vocab + 3)
+    for dtype in ("f32", "f16"):
+        for spread in (0.01, 1.0, 4.0):
+            y = x * spread
+            # (at the end of a steep row tokens weigh less than the 1e-10 of the sum by which a border counts as near: the first four rows)
+            check(mpq, cuda, y, u, p=[1 - 2.0 ** -24, 1 - 2.0 ** -20, 0.9999, 0.99999, 1e-30], dtype=dtype, open_ends=4)
+            check(mpq, cuda, y, u, [0.5] * 5, [vocab - 1] * 5, [1 - 2.0 ** -24, 0.99999, 0.5, 0.999, 2.0 ** -24], dtype=dtype, open_ends=4)
+            check(mpq, cuda, y, u, p=[0.999] * 5, least=[1e-30, 1e-9, 1e-12, 1e-4, 2.0 ** -24], dtype=dtype)
+            check(mpq, cuda, y, u, [1e4, 3e38, 100.0, 1e-30, 1e-3], dtype=dtype)
+            check(mpq, cuda, y, u, [1e4, 3e38, 100.0, 1e-30, 1e-3], [40, 50, vocab // 2, 3, 9], [0.9, 0.5, 0.99, 0.9, 0.9], [0.0, 0.9, 0.5, 0.1, 1e-9], dtype=dtype)
 
 
 def test_ordered_rows(mpq, cuda):
