@@ -481,7 +481,7 @@ int mpq_sample(const void* logits, int64_t ld, int dtype, int64_t rows, int64_t 
                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                const float* uniform, int64_t* tokens, float* logprob, void* stream);
 
-/* How many CTAs of the tensor-core kernels (mpq_linear_levels, mpq_cache_attention) have given up a wait since
+/* How many CTAs of the tensor-core kernels (mpq_linear_levels, mpq_linear_adapted, mpq_cache_attention) have given up a wait since
  * the library was loaded on the current device: 0 unless the device or the driver misbehaves.  The results that
  * such a CTA would have stored are NaN.  Synchronizes the stream. */
 int mpq_wait_failures(unsigned int* count_host, void* stream);
