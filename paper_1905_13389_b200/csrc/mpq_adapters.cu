@@ -9,7 +9,7 @@
 // that loads are 16 bytes and nothing is staged.  The k range is split over the CTA's warps too; the parts meet in shared
 // memory in a fixed order.  Pieces of single tokens: tiles of 8, bound by the latency of the loads (a token with rank 16
 // reads 32 k bytes): 64 tokens over 9216 with 48 adapters of rank 16 take 10 us in a graph.  Longer pieces: tiles of 32; 4096
-// tokens over 4096 with rank 64 take 28 us, bound by L1 lookups (eight lines a load) and by making the odd numbers, seven
+// tokens over 4096 with rank 64 take 28 us, bound by L1 lookups (eight lines a load) and by making the odd numbers, five
 // instructions a pair in bfloat16 and three in float16.  (One m-tile a warp, with the next block under way: 31 us; a CTA that
 // takes all sequences of its tile in turn: 72.)
 #include "mpq_adapters.cuh"
@@ -28,9 +28,10 @@ __device__ __forceinline__ uint32_t odd_pair(uint32_t word, int at, float L) {
         const __half2 x = __hfma2(u, __float2half2_rn(2.0f), __float2half2_rn(-L));
         return *reinterpret_cast<const uint32_t*>(&x);
     }
-    const float a = __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7650u + (uint32_t)at)) - 8388608.0f;
-    const float b = __uint_as_float(__byte_perm(word, 0x4b000000u, 0x7651u + (uint32_t)at)) - 8388608.0f;
-    const float x = fmaf(2.0f, a, -L), y = fmaf(2.0f, b, -L);
+    // 1 + 2^-15 u, so that one multiply-add makes the number
+    const float a = __uint_as_float(__byte_perm(word, 0x3f800000u, 0x7604u | (uint32_t)at << 4));
+    const float b = __uint_as_float(__byte_perm(word, 0x3f800000u, 0x7604u | (uint32_t)(at + 1) << 4));
+    const float x = fmaf(65536.0f, a, -65536.0f - L), y = fmaf(65536.0f, b, -65536.0f - L);
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
     return r;
