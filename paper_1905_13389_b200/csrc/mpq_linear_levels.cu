@@ -24,7 +24,7 @@ struct LinearArgs {
     void* out; int64_t ldo;
     uint32_t polls;                                       // limit of a wait
     const void* up = nullptr; int rank = 0;               // adapters: [..][n][rank]
-    int adapters = 0;
+    int adapters = 0, sequences = 0;
     LowWorkspace low = {};                                // what the adapters have made of the tokens
 };
 
@@ -866,8 +866,15 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
 //   64 tiles: 128 x 4096 x 4096 11.8 / 15.2;  128: 200 x 4096 x 4096 12.5 / 15.2;  142: 100 x 9000 x 1000 9.4 / 11.9;
 //   144: 128 x 9216 x 4096 14.3 / 17.1, 2300 x 512 x 9216 19.5 / 22.4;  150: 128 x 9600 x 4096 23.7 / 22.4;
 //   213: 130 x 9000 x 1000 16.6 / 12.6;  256: 1000 x 2000 x 2000 19.8 / 13.1.
+// With adapters the small form's sums take longer the more rows and ranks there are, the pairs' the more sequences a tile
+// has: pairs from sequences of 12 tokens on average.  us for m x n x k, rank, sequences, small / pairs --
+//   33 x 4096 x 4096, 16, 1 16.4 / 14.1, 64, 1 25.8 / 18.0;  60 x 4096 x 4096, 64, 1 25.9 / 18.5, 5 26.7 / 30.1, 25 21.7 / 41.7;
+//   140 x 4096 x 4096, 64, 9 41.2 / 33.7, 17 40.4 / 36.8, 35 36.2 / 46.6;  256 x 4096 x 1024, 16, 16 21.2 / 17.9, 64 21.6 / 21.8;
+//   512 x 2048 x 2048, 64, 1 43.6 / 23.5, 25 40.6 / 32.2, 50 39.9 / 40.0, 200 39.2 / 48.7;  20 x 4096 x 4096, 64, 1 21.1 / 21.3.
 template <typename T, typename W = void>
 int launch_linear_levels(const LinearArgs& g, cudaStream_t st) {
+    if constexpr (!std::is_void_v<W>)
+        if (g.m > 32 && g.m > 12 * (int64_t)g.sequences) return launch_linear_pair<T, W>(g, st);
     if (g.m <= 16) return launch_linear_small<T, W, 16>(g, st);
     if (g.m <= 32) return launch_linear_small<T, W, 32>(g, st);
     if (g.m <= 64 || ceil_div(g.m, 64) * ceil_div(g.n, 128) <= sm_count()) return launch_linear_small<T, W, 64>(g, st);
@@ -935,6 +942,7 @@ extern "C" int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const 
     g.up = up;
     g.rank = rank;
     g.adapters = adapters;
+    g.sequences = batch;
     g.low = LowWorkspace(workspace, m, rank);
     const AdapterArgs d = {a, a_scale, g.La, m, g.row_bytes, down, factor, adapters, rank, q_starts, ids, batch, g.low};
     rc = adapter_down(d, adapter_dtype, (cudaStream_t)stream);
