@@ -11,7 +11,8 @@
 // reads 32 k bytes): 64 tokens over 9216 with 48 adapters of rank 16 take 10 us in a graph.  Longer pieces: tiles of 32; 4096
 // tokens over 4096 with rank 64 take 28 us, bound by L1 lookups (eight lines a load) and by making the odd numbers, five
 // instructions a pair in bfloat16 and three in float16.  (One m-tile a warp, with the next block under way: 31 us; a CTA that
-// takes all sequences of its tile in turn: 72.)
+// takes all sequences of its tile in turn: 72.  Tiles of 64 staged by cp.async, one CTA a multiprocessor: 11.5 us for k = 1024, as
+// long as two CTAs here take for 32 tokens and k = 2048 each.)
 #include "mpq_adapters.cuh"
 #include "mpq_tensor.cuh"
 

@@ -7,7 +7,7 @@
 // Bound by issuing: some 30 instructions an element for a weight, 11 of them FP64.  256 x 131072 in bfloat16 by temperature take
 // 94 us (memory would take 10), top-p over 256 x 151000 in 32 bits 204; a row alone is bound by latency, 30 us with every rule.
 //
-// A row belongs to one CTA, or where there are few rows to a cluster of up to eight.  Shares that are small enough stay in shared
+// A row belongs to one CTA, or where there are few rows to a cluster of up to four.  Shares that are small enough stay in shared
 // memory; of larger ones only the first look goes to memory, the later ones find the row in L2.  Nothing is sorted.  Where
 // top-k or top-p ends is found in three looks.  The first finds the largest logit.  The second counts elements by their distance
 // from it, in 2048 steps of 1/64, which says in which steps the end lies: exactly for top-k, by counts times weights for top-p.
@@ -90,7 +90,7 @@ struct SampleShared {
     uint32_t bins[2][kSampleBins];
     uint32_t offsets[kSampleBins];                        // sums of 1/256 of a step by which a bin's members lie behind its beginning
     u64 coarse[2][2][kSampleGroups];                      // what groups of 32 bins are worth, and their counts
-    int noted[2], found[2];                               // members a CTA hands out; a place
+    int noted[2], found;                                  // members a CTA hands out; a place
     double rest[kSampleWarps], rest_all;                  // (the latter of a CTA, for the others)
     // within a CTA
     SampleBorder border[2];
@@ -875,9 +875,9 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
                 auto equal = [&](int v, float x) { return (u64)(order_key(x) == e && kept(v, x)); };
                 const int place = r.running(r.sum(equal), equal, [&](u64) { return wanted - 1; });
                 if (place >= 0)
-                    for (int q = 0; q < g.ctas; ++q) st_cluster(r.peer(&sh.found[1], q), (uint32_t)place);
+                    for (int q = 0; q < g.ctas; ++q) st_cluster(r.peer(&sh.found, q), (uint32_t)place);
                 r.sync();
-                c = sh.found[1];
+                c = sh.found;
                 r.turn ^= 1;
             }
             edge = e;
