@@ -871,10 +871,13 @@ int launch_linear_pair(const LinearArgs& g, cudaStream_t st) {
 //   33 x 4096 x 4096, 16, 1 16.4 / 14.1, 64, 1 25.8 / 18.0;  60 x 4096 x 4096, 64, 1 25.9 / 18.5, 5 26.7 / 30.1, 25 21.7 / 41.7;
 //   140 x 4096 x 4096, 64, 9 41.2 / 33.7, 17 40.4 / 36.8, 35 36.2 / 46.6;  256 x 4096 x 1024, 16, 16 21.2 / 17.9, 64 21.6 / 21.8;
 //   512 x 2048 x 2048, 64, 1 43.6 / 23.5, 25 40.6 / 32.2, 50 39.9 / 40.0, 200 39.2 / 48.7;  20 x 4096 x 4096, 64, 1 21.1 / 21.3.
+// A long k is another matter, since the small form splits it: the more rows and ranks, the longer it may be.  One sequence --
+//   64 x 128 x 30000, 16 19.3 / 57.7, 64 33.8 / 58.2;  64 x 1024 x 9216, 16 16.6 / 18.4, 64 24.8 / 20.9;  64 x 4096 x 16384, 16 21.8 / 28.4,
+//   64 34.7 / 30.6;  100 x 2048 x 9216, 16 18.8 / 18.5, 64 33.6 / 21.4;  200 x 512 x 9216, 16 24.4 / 18.5;  256 x 4096 x 9216, 16 27.5 / 19.3.
 template <typename T, typename W = void>
 int launch_linear_levels(const LinearArgs& g, cudaStream_t st) {
     if constexpr (!std::is_void_v<W>)
-        if (g.m > 32 && g.m > 12 * (int64_t)g.sequences) return launch_linear_pair<T, W>(g, st);
+        if (g.m > 32 && g.m > 12 * (int64_t)g.sequences && g.k <= 4096 + 4 * (g.m < 256 ? g.m : 256) * g.rank) return launch_linear_pair<T, W>(g, st);
     if (g.m <= 16) return launch_linear_small<T, W, 16>(g, st);
     if (g.m <= 32) return launch_linear_small<T, W, 32>(g, st);
     if (g.m <= 64 || ceil_div(g.m, 64) * ceil_div(g.n, 128) <= sm_count()) return launch_linear_small<T, W, 64>(g, st);

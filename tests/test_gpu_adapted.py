@@ -100,7 +100,7 @@ def test_many_rows(mpq, cuda, lens, ids, tail, n, k, rank, dtype):
 # both sides of the rule that chooses the form: rows, and tokens of a sequence on average
 @pytest.mark.parametrize("lens,n,k,rank", [([32], 130, 70, 16), ([33], 130, 70, 16), ([12] * 3, 300, 512, 32), ([12, 12, 13], 300, 512, 32), ([5] * 30, 700, 96, 64),
                                            ([12] * 11, 257, 1040, 128), ([13] * 11, 257, 1040, 128), ([64], 3, 5, 16), ([0] * 50 + [200], 520, 260, 48),
-                                           ([256], 128, 128, 128), ([40, 0, 0, 1], 9001, 17, 16)])
+                                           ([256], 128, 128, 128), ([40, 0, 0, 1], 9001, 17, 16), ([38], 150, 6656, 16), ([38], 150, 6657, 16), ([66], 70, 20000, 16)])
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_few_rows_of_long_and_short_sequences(mpq, cuda, lens, n, k, rank, dtype):
     c = Case(mpq, cuda, lens, [(i + 1) % 5 - 1 for i in range(len(lens))], n, k, rank, dtype, tail=2, seed=n + k)
