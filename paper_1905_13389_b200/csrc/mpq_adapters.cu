@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const Adapte
         const bool in = kb < kb1 && at < g.row_bytes;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-            x.u[j] = in ? __ldg(reinterpret_cast<const uint4*>(levels + min(j * 8 + row, count - 1) * g.row_bytes + at)) : make_uint4(0, 0, 0, 0);
+            x.u[j] = in ? load16(levels + min(j * 8 + row, count - 1) * g.row_bytes + at) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kDownThreads) adapter_down_kernel(const Adapte
                 const int r = r0 + i * 16 + h * 8 + row;
                 const uint4* from = reinterpret_cast<const uint4*>(down + (int64_t)r * g.row_bytes + at);
 #pragma unroll
-                for (int q = 0; q < 2; ++q) x.a[i][h][q] = in && r < g.rank ? __ldg(from + q) : make_uint4(0, 0, 0, 0);
+                for (int q = 0; q < 2; ++q) x.a[i][h][q] = in && r < g.rank ? load16(from + q) : make_uint4(0, 0, 0, 0);
             }
     };
     auto multiply = [&](const Block& x) {

@@ -47,8 +47,17 @@ __device__ __forceinline__ void mma_16x8x16(float* d, uint32_t a0, uint32_t a1, 
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The two halves of a chain's launch (chain_entry): let the next kernel's blocks come, and wait for the kernel before.
+// The two halves of a chain's launch (chain_entry): let the next kernel's blocks come, and wait for the kernel before.  That one may
+// be writing while this one already runs, so what it makes is read by ordinary loads, which the wait orders: the read-only path
+// (__ldg) is for memory that nobody writes as long as the kernel runs -- `up`, which the product multiplies z with: the kernel before
+// lets the product in only when all earlier ones have ended.
 __device__ __forceinline__ void chain_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// An ordinary load that keeps its place behind the wait, but not behind stores: several can be on their way.
+__device__ __forceinline__ uint4 load16(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
 
 }  // namespace mpq

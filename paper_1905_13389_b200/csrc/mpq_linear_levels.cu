@@ -33,15 +33,15 @@ struct RowTerm { float scale; uint32_t term; };          // a_scale / L_a;  k L_
 struct ColTerm { float scale; uint32_t term; float bias; };   // w_scale / L_w;  2 L_a sums_w;  bias
 __device__ __forceinline__ RowTerm row_term(const LinearArgs& g, int64_t r) {
     RowTerm t;
-    t.scale = __fdiv_rn(__ldg(g.a_scale + r), (float)g.La);
-    t.term = (uint32_t)g.k * (uint32_t)g.La * (uint32_t)g.Lw - 2u * (uint32_t)g.Lw * (uint32_t)__ldg(g.a_sums + r);
+    t.scale = __fdiv_rn(g.a_scale[r], (float)g.La);
+    t.term = (uint32_t)g.k * (uint32_t)g.La * (uint32_t)g.Lw - 2u * (uint32_t)g.Lw * (uint32_t)g.a_sums[r];
     return t;
 }
 __device__ __forceinline__ ColTerm col_term(const LinearArgs& g, int64_t c) {
     ColTerm t;
-    t.scale = __fdiv_rn(__ldg(g.w_scale + c), (float)g.Lw);
-    t.term = 2u * (uint32_t)g.La * (uint32_t)__ldg(g.w_sums + c);
-    t.bias = g.bias ? __ldg(g.bias + c) : 0.0f;
+    t.scale = __fdiv_rn(g.w_scale[c], (float)g.Lw);
+    t.term = 2u * (uint32_t)g.La * (uint32_t)g.w_sums[c];
+    t.bias = g.bias ? g.bias[c] : 0.0f;
     return t;
 }
 __device__ __forceinline__ float linear_value(const LinearArgs& g, uint32_t acc, const RowTerm& r, const ColTerm& c) {
@@ -119,7 +119,7 @@ __device__ __forceinline__ void low_rank_rows_of(const LinearArgs& g, int64_t ro
     constexpr int kStep = 32 / kReads;                     // columns of a read
     const int sub = lane % kReads;
     auto adapter = [&](int r) {
-        const int id = r < count && row0 + first + r < g.m ? __ldg(g.low.chosen + row0 + first + r) : -1;
+        const int id = r < count && row0 + first + r < g.m ? g.low.chosen[row0 + first + r] : -1;
         return id < g.adapters ? id : -1;
     };
     const int ids[2] = {adapter(lane), adapter(lane + 32)};
@@ -138,8 +138,8 @@ __device__ __forceinline__ void low_rank_rows_of(const LinearArgs& g, int64_t ro
                 next[j][q] = __ldg(reinterpret_cast<const uint4*>(static_cast<const W*>(g.up) + (id * g.n + c) * RANK + sub * 8));
             }
             const float4* z = reinterpret_cast<const float4*>(g.low.z + min(row0 + first + r, g.m - 1) * RANK + sub * 8);
-            next_z[j][0] = __ldg(z);
-            next_z[j][1] = __ldg(z + 1);
+            next_z[j][0] = z[0];
+            next_z[j][1] = z[1];
         }
     };
     if (any) ask(0);
@@ -423,7 +423,7 @@ __device__ __forceinline__ void umma_f16_pair(uint32_t d, uint64_t a, uint64_t b
 template <typename W, int PARTS>
 __device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0, int64_t c0, uint32_t at, int lane, int turn) {
     const int row = lane >> 2, quad = lane & 3;
-    int id = lane < 16 && row0 + lane < g.m ? __ldg(g.low.chosen + row0 + lane) : -1;
+    int id = lane < 16 && row0 + lane < g.m ? g.low.chosen[row0 + lane] : -1;
     if (id >= g.adapters) id = -1;
     uint32_t left = __ballot_sync(0xffffffffu, id >= 0);
     const int64_t z0 = min(row0 + row, g.m - 1), z1 = min(row0 + row + 8, g.m - 1);
@@ -445,15 +445,15 @@ __device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0,
                 for (int j = 0; j < 8; ++j) u[j] = __ldg(reinterpret_cast<const uint2*>(up + min(c0 + 8 * j + row, g.n - 1) * g.rank + i));
 #pragma unroll
                 for (int q = 0; q < PARTS; ++q) {
-                    a[q][0] = __ldg(reinterpret_cast<const uint2*>(z + (q * g.m + z0) * g.rank + i));
-                    a[q][1] = __ldg(reinterpret_cast<const uint2*>(z + (q * g.m + z1) * g.rank + i));
+                    a[q][0] = *reinterpret_cast<const uint2*>(z + (q * g.m + z0) * g.rank + i);
+                    a[q][1] = *reinterpret_cast<const uint2*>(z + (q * g.m + z1) * g.rank + i);
                 }
 #pragma unroll
                 for (int q = PARTS - 1; q >= 0; --q)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) mma_16x8x16<W>(acc + 4 * j, a[q][0].x, a[q][1].x, a[q][0].y, a[q][1].y, u[j].x, u[j].y);
             }
-            const float s0 = __ldg(g.low.scale + z0), s1 = __ldg(g.low.scale + z1);
+            const float s0 = g.low.scale[z0], s1 = g.low.scale[z1];
 #pragma unroll
             for (int i = 0; i < 32; ++i) acc[i] *= (i >> 1) & 1 ? s1 : s0;
         }
@@ -478,10 +478,10 @@ __device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0,
 // The adapter that all of a tile's rows have (those behind the last row have any), or -1; by a warp, after chain_wait().
 __device__ __forceinline__ int tile_adapter(const LinearArgs& g, int64_t m0, int lane) {
     const int64_t last = g.m - 1;
-    const int first = __ldg(g.low.chosen + m0);
+    const int first = g.low.chosen[m0];
     bool same = first >= 0 && first < g.adapters;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) same = same && __ldg(g.low.chosen + min(m0 + i * 32 + lane, last)) == first;
+    for (int i = 0; i < 8; ++i) same &= g.low.chosen[min(m0 + i * 32 + lane, last)] == first;
     return __all_sync(0xffffffffu, same) ? first : -1;
 }
 constexpr int kBlockRanks = 64;                            // of a block, which is 128 bytes wide
@@ -687,7 +687,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(acc), 0));       // this warp's part of the accumulator is read
                 if constexpr (!std::is_void_v<W>) {
-                    const float scale = whole_tile ? __ldg(g.low.scale + min(row0 + lane, g.m - 1)) : 1.0f;
+                    const float scale = whole_tile ? g.low.scale[min(row0 + lane, g.m - 1)] : 1.0f;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
                         const float4 t = terms[part * 32 + j];

@@ -180,7 +180,7 @@ struct SampleRow {
     // Chunk c of the share from memory, -infinity where the row is not.
     __device__ __forceinline__ uint4 read_chunk(int c) const {
         const int i = v0 + c * E - skew;
-        if (i >= 0 && i + E <= vocab) return __ldg(reinterpret_cast<const uint4*>(x0 + i));
+        if (i >= 0 && i + E <= vocab) return *reinterpret_cast<const uint4*>(x0 + i);
         uint4 r;
         T* e = reinterpret_cast<T*>(&r);
 #pragma unroll
@@ -196,7 +196,7 @@ struct SampleRow {
         } else if (v0 >= skew && v0 + warp_chunks * E - skew <= vocab) {         // every share but a row's first and last ones
             const uint4* from = reinterpret_cast<const uint4*>(x0 + (v0 - skew)) + c;
 #pragma unroll
-            for (int j = 0; j < N; ++j) in[j] = __ldg(from + 32 * j);
+            for (int j = 0; j < N; ++j) in[j] = from[32 * j];
         } else {
 #pragma unroll
             for (int j = 0; j < N; ++j) in[j] = read_chunk(c + 32 * j);
