@@ -472,7 +472,9 @@ int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const int32_t* a_
  *   indices) exceeds uniform * (the sum of all of them).
  * temperature <= 0 takes the first of the order.  top_k <= 0 or >= vocab, top_p >= 1 and min_p <= 0
  * leave their rule out, as does a NULL array (temperature NULL: 1).  uniform lies in [0, 1) and is
- * clamped to it.  Weights are held to 2^-44 of the largest; a logit of -infinity is never drawn.
+ * clamped to it.  Weights are whole multiples of 2^-s of the largest, s = min(50, 62 - ceil(log2 vocab)) -- 45 for 131072 tokens, 42
+ * for 786432 --, the nearest to numbers that are off by 2^-42 of themselves at most, and summed exactly: a token that
+ * weighs less than half a multiple is never drawn (but for the first of the order), nor is a logit of -infinity.
  * logprob (optional): log of the token's share in sum_i exp(x_i), whatever the rules are.
  * tokens -1 and logprob NaN: a row with a NaN, with nothing over -infinity, with +infinity at a
  * temperature over 0, or with a NaN among its own numbers.

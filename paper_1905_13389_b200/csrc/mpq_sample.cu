@@ -1,8 +1,10 @@
 // Drawing one token a row from logits: temperature, top-k, top-p, min-p, given random numbers (mpq_sample).
 //
 // Which token is drawn hangs on where a running sum passes a border, so weights are 64-bit fixed-point numbers
-// (whole multiples of 2^-shift of the largest weight, made from 64-bit exponentials): their sums are exact whatever the
-// order, borders are exact products with the row's own numbers, and the sums lie within some 2^-45 of real numbers'.
+// (whole multiples of 2^-shift of the largest weight, the nearest ones, made from 64-bit exponentials): their sums are exact whatever
+// the order and borders are exact products with the row's own numbers.  shift is 62 less log2(vocab) rounded up, 50 at most, so
+// that a row's sum fits: 45 for 131,072 tokens, 42 for 786,432.  A weight is off by 2^-42 of itself and half a multiple, and by no more than
+// itself: what is less than half a multiple weighs nothing and is never drawn, however much of it there is.
 // (With 32-bit weights a tail token of a flat row of 131,072 is another one in some percent of the draws.)
 // Bound by issuing: some 30 instructions an element for a weight, 11 of them FP64.  256 x 131072 in bfloat16 by temperature take
 // 94 us (memory would take 10), top-p over 256 x 151000 in 32 bits 204; a row alone is bound by latency, 30 us with every rule.
@@ -117,13 +119,14 @@ __device__ __forceinline__ float chunk_max(const uint4& r, const __nv_bfloat16*)
 // exp((x - top) / warm) 2^shift, rounded: 2^(t / 16) with t = n + f is 2^(n / 16) from the table and the exponent, times
 // the series of 2^(f / 16), |f| <= 1/2, off by 2^-42 of itself at most.
 struct SampleWeight {
-    float top, coolf, gone;                               // gone: where a weight is less than one multiple
+    float top, coolf, lowest;                             // lowest: below it weights are less than a quarter of a multiple
     double dtop, cool;
     const double* powers;
     static constexpr u64 kBias = 0x433ull << 52;          // 2^52: on top of it, the low bits of a number are its whole part
 
     __device__ SampleWeight(float largest, float warm, int shift, const double* table)
-        : top(largest), coolf(1.0f / warm), gone(-0.69314718f * (float)shift), dtop(largest), cool(16.0 * 1.4426950408889634073599 / (double)warm), powers(table) {}
+        : top(largest), coolf(1.0f / warm), lowest((float)((double)largest - 0.69314718055994530942 * (double)(shift + 2) * (double)warm)), dtop(largest),
+          cool(16.0 * 1.4426950408889634073599 / (double)warm), powers(table) {}
     __device__ __forceinline__ u64 biased(float x) const {
         constexpr double kMagic = 6755399441055744.0;     // 1.5 2^52: on top of it, the low bits are the nearest whole number
         constexpr double kLog = 0.69314718055994530942 / 16;
@@ -137,10 +140,9 @@ struct SampleWeight {
         const double scaled = __hiloint2double(__double2hiint(a) + (n & ~15) * 65536, __double2loint(a));
         return (u64)__double_as_longlong(fma(scaled * f, q, scaled) + 4503599627370496.0);
     }
-    __device__ __forceinline__ bool small(float x) const { return (x - top) * coolf < gone; }
-    // What is less than one multiple weighs one, so that every token over -infinity can be drawn.
+    __device__ __forceinline__ bool small(float x) const { return x < lowest; }
     __device__ __forceinline__ u64 operator()(float x) const {
-        u64 w = 1;
+        u64 w = 0;
         if (!small(x)) w = biased(x) - kBias;
         return x > -INFINITY ? w : 0ull;
     }
