@@ -475,9 +475,10 @@ int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const int32_t* a_
  * clamped to it.  Weights are whole multiples of 2^-s of the largest, s = min(50, 62 - ceil(log2 vocab)) -- 45 for 131072 tokens, 42
  * for 786432 --, the nearest to numbers that are off by 2^-42 of themselves at most, and summed exactly: a token that
  * weighs less than half a multiple is never drawn (but for the first of the order), nor is a logit of -infinity.
- * logprob (optional): log of the token's share in sum_i exp(x_i), whatever the rules are.
+ * logprob (optional): log of the token's share in sum_i exp(x_i), whatever the rules are (NaN where the token's logit is
+ * +infinity).
  * tokens -1 and logprob NaN: a row with a NaN, with nothing over -infinity, with +infinity at a
- * temperature over 0, or with a NaN among its own numbers.
+ * temperature over 0, or with a NaN among its own numbers, whether its rules use them or not.
  * vocab is at most 393216 (MPQ_F32) or 786432 (MPQ_F16, MPQ_BF16).  rows = 0 does nothing. */
 int mpq_sample(const void* logits, int64_t ld, int dtype, int64_t rows, int64_t vocab,
                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,

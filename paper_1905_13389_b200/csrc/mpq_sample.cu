@@ -713,7 +713,7 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
     const float top = key_value((uint32_t)(code >> 32));
     const int first = (int)~(uint32_t)code;
     const bool greedy = warm <= 0.0f;
-    const bool bad = code == 0 || code == ~0ull || warm != warm || (!greedy && (top == INFINITY || p != p || least != least || u != u));
+    const bool bad = code == 0 || code == ~0ull || warm != warm || p != p || least != least || u != u || (!greedy && top == INFINITY);
     if (bad) {
         if (r.rank == 0 && threadIdx.x == 0) {
             g.tokens[row] = -1;
