@@ -119,14 +119,14 @@ __device__ __forceinline__ float chunk_max(const uint4& r, const __nv_bfloat16*)
 // exp((x - top) / warm) 2^shift, rounded: 2^(t / 16) with t = n + f is 2^(n / 16) from the table and the exponent, times
 // the series of 2^(f / 16), |f| <= 1/2, off by 2^-42 of itself at most.
 struct SampleWeight {
-    float top, coolf, lowest;                             // lowest: below it weights are less than a quarter of a multiple
+    float top, cool2, lowest;                             // 2 / temperature; below `lowest` weights are less than a quarter of a multiple
     double dtop, cool;
     const double* powers;
     static constexpr u64 kBias = 0x433ull << 52;          // 2^52: on top of it, the low bits of a number are its whole part
 
     __device__ SampleWeight(float largest, float warm, int shift, const double* table)
-        : top(largest), coolf(1.0f / warm), lowest((float)((double)largest - 0.69314718055994530942 * (double)(shift + 2) * (double)warm)), dtop(largest),
-          cool(16.0 * 1.4426950408889634073599 / (double)warm), powers(table) {}
+        : top(largest), cool2(fminf(2.0f / warm, 3e38f)), lowest((float)((double)largest - 0.69314718055994530942 * (double)(shift + 2) * (double)warm)),
+          dtop(largest), cool(16.0 * 1.4426950408889634073599 / (double)warm), powers(table) {}
     __device__ __forceinline__ u64 biased(float x) const {
         constexpr double kMagic = 6755399441055744.0;     // 1.5 2^52: on top of it, the low bits are the nearest whole number
         constexpr double kLog = 0.69314718055994530942 / 16;
@@ -141,6 +141,9 @@ struct SampleWeight {
         return (u64)__double_as_longlong(fma(scaled * f, q, scaled) + 4503599627370496.0);
     }
     __device__ __forceinline__ bool small(float x) const { return x < lowest; }
+    // In 32 bits, as a share of the largest; a guess (at temperatures below 2^-127 a poor one).  Two logits can lie farther apart than
+    // the largest number, half of that cannot.
+    __device__ __forceinline__ float guess(float x) const { return fast_exp2(fmaf(0.5f, x, -0.5f * top) * cool2 * 1.4426950408889634f); }
     __device__ __forceinline__ u64 operator()(float x) const {
         u64 w = 0;
         if (!small(x)) w = biased(x) - kBias;
@@ -434,15 +437,16 @@ struct SampleRow {
         turn ^= 1;
     }
 
-    // Distance of an element from `top` in steps, rounded the same way for equals and never against the order (NaN only for what
-    // is not over -infinity).  Bins count the steps down from the highest, the lowest one for all beyond.
-    static __device__ __forceinline__ float distance(float x, float top, float steps) { return (top - x) * steps; }
+    // Distance of an element from the largest in steps (of which `twice` are two logits), rounded the same way for equals and never
+    // against the order (NaN only for what is not over -infinity).  Bins count the steps down from the highest, the lowest one for
+    // all beyond.
+    static __device__ __forceinline__ float distance(float x, float top, float twice) { return fmaf(-0.5f, x, 0.5f * top) * twice; }
     // The smallest number whose distance is below `limit` (1 or more), by a warp: distances never grow with the number.
-    __device__ __forceinline__ float nearest_below(float top, float steps, float limit) const {
+    __device__ __forceinline__ float nearest_below(float top, float twice, float limit) const {
         uint32_t lo = 0x00800000u, hi = order_key(top);   // from the lowest finite number on; hi's distance is 0
         for (int turn = 0; lo < hi && turn < 16; ++turn) {                 // (eight turns at most)
             const uint32_t step = (hi - lo) / 32 + 1, at = min(lo + lane * step, hi);
-            const uint32_t yes = __ballot_sync(0xffffffffu, at == hi || distance(key_value(at), top, steps) < limit);
+            const uint32_t yes = __ballot_sync(0xffffffffu, at == hi || distance(key_value(at), top, twice) < limit);
             if (yes == 0) {
                 lo += 31 * step + 1;
             } else {
@@ -454,8 +458,8 @@ struct SampleRow {
         return key_value(hi);
     }
     // What lies in bins from `digit` up is this number or more.
-    __device__ __forceinline__ float least_of(float top, float steps, uint32_t digit) const {
-        return digit == 0 ? key_value(0x00800000u) : digit >= kSampleBins ? INFINITY : nearest_below(top, steps, (float)(kSampleBins - (int)digit));
+    __device__ __forceinline__ float least_of(float top, float twice, uint32_t digit) const {
+        return digit == 0 ? key_value(0x00800000u) : digit >= kSampleBins ? INFINITY : nearest_below(top, twice, (float)(kSampleBins - (int)digit));
     }
     // Where members are handed out: in the exchange's bins, both of them where there is no exchange.
     __device__ __forceinline__ u64* members_of(int of_turn) const { return reinterpret_cast<u64*>(sh.bins[ctas > 1 ? of_turn : 0]); }
@@ -728,7 +732,7 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
     const SampleWeight weight(top, warm, g.shift, sh.powers);
     const u64 floor_w = least > 0.0f ? (u64)ceil(fmin((double)least, 4.0) * exp2((double)g.shift)) : 0ull;
     const bool all_stay = !some && !top_p && floor_w <= 1;
-    const float steps = 64.0f * (some ? 1.0f : fminf(weight.coolf, 1e30f));
+    const float twice = some ? 128.0f : 64.0f * fminf(weight.cool2, 2e30f);
     // The second look, for whatever is wanted: counts of distances; the sum of all weights; and what the others weigh together at
     // temperature 1, the first one's weight being 1 -- where it has nearly all of the probability its logarithm is
     // -log(1 + rest).  That one in 32 bits: a term is off by (2.5 |d| + 4) 2^-24 of itself at most, d its distance from the first.
@@ -747,7 +751,7 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
                 for (int i = 0; i < 8; ++i)
                     if (x[i] > -INFINITY) {
                         // in 1/256 of a step, rounded down: on top of 2^23 the low bits are whole numbers
-                        const uint32_t away = __float_as_uint(__fadd_rd(fminf(r.distance(x[i], top, steps), (float)kSampleBins - 0.25f) * 256.0f, 8388608.0f)) - 0x4b000000u;
+                        const uint32_t away = __float_as_uint(__fadd_rd(fminf(r.distance(x[i], top, twice), (float)kSampleBins - 0.25f) * 256.0f, 8388608.0f)) - 0x4b000000u;
                         const uint32_t bin = kSampleBins - 1 - (away >> 8);
                         atomicAdd(bins + bin, 1u);
                         // 32-bit logits that many share a bin lie anywhere in it
@@ -814,7 +818,7 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
         for (int turns = 0; turns < 1 << 16; ++turns) {   // (each one takes at least one occupied key off the open ones)
             auto open = [&](uint32_t key) { const uint32_t high = key >> kLowBits; return high < over && (under == 0xffffffffu || high > under); };
             const float scale = weights ? 4.2e9f / ((float)(total - base) * 1.0001f) : 1.0f, per = scale * unit;
-            auto guess = [&](float x) { return weights ? max(1u, __float2uint_rn(fast_exp2((x - top) * weight.coolf * 1.4426950408889634f) * per)) : 1u; };
+            auto guess = [&](float x) { return weights ? max(1u, __float2uint_rn(weight.guess(x) * per)) : 1u; };
             const u64 want = (u64)max((int64_t)((double)(goal - base) * (double)scale) - bias, (int64_t)1);
             u64 above1 = 0, above2 = 0;
             uint32_t high = 0;
@@ -909,7 +913,7 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
         if (by_reach) {
             outer = reach;
         } else if (least_only) {
-            outer = r.nearest_below(top, steps, least >= 1.0f ? 3.0f : -64.0f * logf(least) + 2.0f);
+            outer = r.nearest_below(top, twice, least >= 1.0f ? 3.0f : -64.0f * logf(least) + 2.0f);
         } else {
             if (tries > 0) look(true, false, false);
             // the weight of a bin's members is that of their mean distance, off by some 2^-15 of itself; 2^-12 on both sides
@@ -925,7 +929,7 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
                 const int64_t margin = (int64_t)(guessed >> 12), aim = (int64_t)(tries == 0 ? share(guessed) : share(all)) + bias;
                 goal[0] = (u64)max(aim - margin, (int64_t)1);
                 goal[1] = (u64)max(aim + margin, (int64_t)1);
-            }, [&](int which, uint32_t digit) { return r.least_of(top, steps, which == 0 ? digit + 1 : digit); });
+            }, [&](int which, uint32_t digit) { return r.least_of(top, twice, which == 0 ? digit + 1 : digit); });
             const SampleBorder hi = sh.border[0], lo = sh.border[1];
             above = hi.above;
             above_to = lo.above_to;
