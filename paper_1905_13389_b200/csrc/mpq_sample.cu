@@ -899,11 +899,7 @@ __global__ void __launch_bounds__(kSampleThreads, PER_SM) sample_kernel(const Sa
     bool summed = all_stay;                               // whether `weights` is the sum of what stays
     int64_t bias = 0;
     int phase = 0;
-    if (!some && !top_p && open) {                        // min-p alone: two steps below its border at most
-        open = least >= 1.0f || -64.0f * logf(least) + 2.0f < 4e6f;
-        if (!open) summed = false;
-    }
-    const bool least_only = !some && !top_p;
+    const bool least_only = !some && !top_p;              // min-p alone: two steps below its border at most
     bool by_reach = by_threads;
 #pragma unroll 1
     for (int tries = 0; open && tries < 4; ++tries) {
