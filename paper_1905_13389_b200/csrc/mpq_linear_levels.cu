@@ -486,6 +486,15 @@ __device__ __forceinline__ int tile_adapter(const LinearArgs& g, int64_t m0, int
 }
 constexpr int kBlockRanks = 64;                            // of a block, which is 128 bytes wide
 
+// What an adapter adds to one result, term by term in fp32.  An infinity in `up` meets every part of z in the matrix instructions, and
+// parts may be zero or of the other sign (NaN, where z itself makes an infinity); sums that are not finite are made again from z.
+template <typename W>
+__device__ __noinline__ float low_rank_one(const W* up, const float* z, int rank) {
+    float s = 0.0f;
+    for (int i = 0; i < rank; ++i) s = fmaf(to_f32(up[i]), z[i], s);
+    return s;
+}
+
 template <typename T, typename W>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w,
@@ -688,10 +697,32 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty(acc), 0));       // this warp's part of the accumulator is read
                 if constexpr (!std::is_void_v<W>) {
                     const float scale = whole_tile ? g.low.scale[min(row0 + lane, g.m - 1)] : 1.0f;
+                    float none = 0.0f;                     // NaN if one of the sums is not finite
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const float4 t = terms[part * 32 + j];
-                        v[j] = __float_as_uint(linear_value(g, v[j], mine, ColTerm{t.x, __float_as_uint(t.y), t.z}) + scale * __uint_as_float(low[j]));
+                    for (int j = 0; j < 32; ++j) none = fmaf(__uint_as_float(low[j]), 0.0f, none);
+                    if (__any_sync(0xffffffffu, lane < rows && none != 0.0f)) {
+                        uint32_t* own = sh + lane * Shape::row_words;      // (this lane's and warp's part, in columns of pairs; see below)
+                        auto at = [&](int j) { return 2 * ((part * 16 + j / 2) ^ lane) + j % 2; };
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) own[at(j)] = __float_as_uint(scale * __uint_as_float(low[j]));
+                        const int id = lane < rows ? g.low.chosen[row0 + lane] : -1;
+#pragma unroll 1
+                        for (int j = 0; j < 32; ++j) {
+                            const int64_t c = (int64_t)n0 + c0 + part * 32 + j;
+                            if (id >= 0 && id < g.adapters && c < g.n && !ordinary(__uint_as_float(own[at(j)])))
+                                own[at(j)] = __float_as_uint(low_rank_one(static_cast<const W*>(g.up) + (id * g.n + c) * g.rank, g.low.z + (row0 + lane) * g.rank, g.rank));
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float4 t = terms[part * 32 + j];
+                            v[j] = __float_as_uint(linear_value(g, v[j], mine, ColTerm{t.x, __float_as_uint(t.y), t.z}) + __uint_as_float(own[at(j)]));
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            const float4 t = terms[part * 32 + j];
+                            v[j] = __float_as_uint(linear_value(g, v[j], mine, ColTerm{t.x, __float_as_uint(t.y), t.z}) + scale * __uint_as_float(low[j]));
+                        }
                     }
                 }
 #pragma unroll
