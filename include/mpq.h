@@ -446,6 +446,9 @@ int mpq_pages_trim(int32_t* table, int64_t per_sequence, int32_t* lens, int sequ
 /* mpq_linear_levels with a low-rank adapter per request beside the shared weights:
  *   z[r][i] = factor[id] (a_scale[r] / L_a) sum_t q_a[r][t] down[id][i][t]            (fp32)
  *   f = float(acc) * (...) + bias[c] + sum_i z[r][i] up[id][c][i];  f = glue(f);  ... as there.
+ * Sums are fp32.  Where there are many rows z meets up as two or three numbers of 16 bits: whole with bfloat16 adapters and MPQ_F32
+ * results, to 2^-16 of itself with bfloat16 adapters and 16-bit results, to 2^-22 of itself (or 2^-39 of its row's
+ * largest) with float16 adapters.  So the same row can come out different in its last bits beside more rows.
  * Row r of the activations belongs to sequence b with q_starts[b] <= r < q_starts[b+1] (q_starts
  * [batch + 1] ascends) and takes adapter id = ids[b]; rows of no sequence, and those whose id lies
  * outside 0 .. adapters-1 (-1 by convention), take none.
@@ -476,7 +479,8 @@ int mpq_linear_adapted(const uint8_t* a, const float* a_scale, const int32_t* a_
  * for 786432 --, the nearest to numbers that are off by 2^-42 of themselves at most, and summed exactly: a token that
  * weighs less than half a multiple is never drawn (but for the first of the order), nor is a logit of -infinity.
  * logprob (optional): log of the token's share in sum_i exp(x_i), whatever the rules are (NaN where the token's logit is
- * +infinity).
+ * +infinity).  The largest term is exact; the others are fp32, each off by (2.5 d + 12 + vocab / 512) 2^-24 of itself at
+ * most, their sums included, with d its distance from the largest.
  * tokens -1 and logprob NaN: a row with a NaN, with nothing over -infinity, with +infinity at a
  * temperature over 0, or with a NaN among its own numbers, whether its rules use them or not.
  * vocab is at most 393216 (MPQ_F32) or 786432 (MPQ_F16, MPQ_BF16).  rows = 0 does nothing. */

@@ -1,4 +1,4 @@
-"""Product of level bytes with adapters that hold infinities."""
+"""Product of level bytes with adapters: infinities in them, and what 16-bit parts keep of the inner sums."""
 import math
 
 import numpy as np
@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from tests.test_gpu_adapted import Case
+from tests.test_gpu_linear_levels import TYPES, UNIT, activate
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +44,37 @@ def test_inner_sums_past_the_parts_range(mpq, cuda, m):
         want = sum(c.sums()[:2])
     assert np.isinf(want).all()
     np.testing.assert_array_equal(c.run().double().cpu().numpy(), want)
+
+
+def check(c, act, out, bias=False, residual=False):
+    """As Case.check, with what z loses in 16-bit parts: two bfloat16 parts leave (2^-8)^2 of each z at most, and so 2^-16 of the sizes
+    that are added up; two float16 parts (2^-11)^2; an fp32 result has all of it.  Through the activation (slope at most 1.13)."""
+    g = torch.Generator().manual_seed(9)
+    b = torch.randn((c.n,), generator=g) if bias else None
+    r = torch.randn((c.m, c.n), generator=g).to(TYPES[out]) if residual else None
+    got = c.run(bias=None if b is None else b.to(c.cuda), act=act, residual=None if r is None else r.to(c.cuda), dtype=TYPES[out])
+    f, delta, size = c.sums()
+    whole = np.abs(f) + np.abs(delta)
+    f = f + delta
+    if bias:
+        f, whole = f + b.double().numpy(), whole + np.abs(b.double().numpy())
+    ref = activate(f, act) + (r.double().numpy() if residual else 0.0)
+    lost = 2.0 ** -22 if c.down.dtype is torch.float16 else 0.0 if out == "f32" else 2.0 ** -16
+    terms = 4 + math.sqrt(c.k + 128) / 4
+    tol = UNIT[out] * np.abs(ref) + 16 * 2.0 ** -24 * (whole + np.abs(ref)) + 1.2 * (terms * 2.0 ** -24 + lost) * size + (2.0 ** -25 if out == "f16" else 0)
+    err = np.abs(got.double().cpu().numpy() - ref)
+    assert got.dtype == TYPES[out] and np.all(err <= tol), (err - tol).max()
+
+
+@pytest.mark.parametrize("lens,n", [([9], 300), ([600], 1601), ([300, 17, 283], 1601)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_what_z_keeps(mpq, cuda, lens, n, dtype):
+    """Adapters whose terms cancel, beside a product of next to nothing: results of all types show no more than the parts of z lose."""
+    c = Case(mpq, cuda, lens, [2, 0, 1][:len(lens)], n, 320, 64, dtype, seed=5)
+    c.up[:, :, 32:] = -c.up[:, :, :32]
+    c.down[:, 32:] = (c.down[:, :32].float() * (1 + 2.0 ** -6)).to(c.down.dtype)
+    c.low = mpq.adapters(c.down.to(cuda), c.up.to(cuda), c.factor.to(cuda))
+    c.w.scale.mul_(1e-4)
+    c.sw = c.w.scale.double().cpu().numpy() / 255
+    for out in ("f32", "f16", "bf16"):
+        check(c, "none", out)
