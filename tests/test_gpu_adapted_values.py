@@ -1,4 +1,5 @@
-"""Product of level bytes with adapters: infinities in them, and what 16-bit parts keep of the inner sums."""
+"""Product of level bytes with adapters: infinities in them, and what 16-bit parts keep of the inner sums, and more
+tiles than every pair of CTAs has accumulators."""
 import math
 
 import numpy as np
@@ -78,3 +79,17 @@ def test_what_z_keeps(mpq, cuda, lens, n, dtype):
     c.sw = c.w.scale.double().cpu().numpy() / 255
     for out in ("f32", "f16", "bf16"):
         check(c, "none", out)
+
+
+# pairs of CTAs have some three tiles of 256 x 128 and more each, so that both accumulators, and what adapters add beside them, are used
+# again: tiles of one adapter, of several and of none one after the other
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("lens,ids,n,rank", [([1300, 1, 1299], [1, -1, 0], 4000, 128), ([1300, 1, 1299], [1, -1, 0], 9000, 16), ([2600], [2], 4001, 64),
+                                             ([256, 3, 509, 300, 700, 832], [0, 1, 2, -1, 3, 1], 5000, 16), ([100] * 26, [i % 5 - 1 for i in range(26)], 3900, 32),
+                                             ([512, 512, 512, 512, 512, 40], [0, -1, 1, -1, 2, 3], 4200, 80)])
+def test_more_tiles_than_accumulators(mpq, cuda, lens, ids, n, rank, dtype, out):
+    assert -(-sum(lens) // 256) * -(-n // 128) > 3 * 74
+    c = Case(mpq, cuda, lens, ids, n, 64, rank, dtype, seed=n)
+    check(c, "none", out)
+    check(c, "silu", out, True, True)
