@@ -113,6 +113,9 @@ class DevicePages:
                               else "the cache is full: %d pages are missing" % missing)
 
 
+PRODUCTS = ("qkv", "o", "up", "down")                      # of a layer, on levels
+
+
 class EncodedDecoder:
     """``weights``: per layer a dict of float tensors qkv [(heads + 2 kv_heads) dim x width], o [width x heads dim],
     up [inner x width], up_bias [inner], down [width x inner], norm1, norm2 [width].  ``adapters``: per layer a dict of
@@ -122,9 +125,17 @@ class EncodedDecoder:
                  adapters: Optional[List[Dict[str, mpq.Adapters]]] = None):
         self.config, device = config, weights[0]["qkv"].device
         self.adapters = adapters or [{}] * len(weights)
+        if len(self.adapters) != len(weights):
+            raise ValueError("expected adapters for %d layers (an empty dict where a layer has none), got %d" % (len(weights), len(self.adapters)))
+        for w, low in zip(weights, self.adapters):
+            for name, a in low.items():
+                if name not in PRODUCTS:
+                    raise ValueError("no product is called %r: expected adapters of %s" % (name, ", ".join(PRODUCTS)))
+                if (a.up.shape[1], a.k) != tuple(w[name].shape):
+                    raise ValueError("expected adapters of %s for [%d x %d] weights, got [%d x %d]" % (name, *w[name].shape, a.up.shape[1], a.k))
         self.layers = []
         for w in weights:
-            layer = {name: mpq.encode_levels(w[name], config.weight_bits) for name in ("qkv", "o", "up", "down")}
+            layer = {name: mpq.encode_levels(w[name], config.weight_bits) for name in PRODUCTS}
             layer.update({name: w[name].float().contiguous() for name in ("up_bias", "norm1", "norm2")})
             layer["cache"] = mpq.level_cache(pages, config.kv_heads, page_size, config.dim, config.cache_bits, device)
             self.layers.append(layer)
