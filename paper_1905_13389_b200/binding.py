@@ -822,11 +822,16 @@ def linear_adapted(a: Levels, w: Levels, low: Adapters, q_starts: torch.Tensor, 
     dev = _device(a.bytes)
     pa, pw = _held(a, m, k, dev), _held(w, n, k, dev)
     down, up, factor, low_k = low
+    if down.dim() != 3:
+        raise ValueError("expected down [adapters][rank][%d], got %s" % ((k + 15) // 16 * 16, tuple(down.shape)))
     count, rank, _ = down.shape
     if low_k != k:
         raise ValueError("the adapters are for k = %d, the product has k = %d" % (low_k, k))
     batch, wtype = ids.numel(), down.dtype
     row = (k + 15) // 16 * 16
+    if down.shape != (count, rank, row) or up.shape != (count, n, rank):
+        raise ValueError("expected down [%d][%d][%d] and up [%d][%d][%d], got %s and %s" % (
+            count, rank, row, count, n, rank, tuple(down.shape), tuple(up.shape)))
     if out is None:
         out = torch.empty_strided((m, n), (n, 1), dtype=dtype, device=a.bytes.device)
     else:
