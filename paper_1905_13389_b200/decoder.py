@@ -91,7 +91,7 @@ class DevicePages:
 
     def __init__(self, pages: int, page_size: int, sequences: int, per_sequence: int, device):
         self.state = mpq.page_state(sequences, per_sequence, pages, page_size, device)
-        self.missing = torch.zeros((1,), dtype=torch.int32, device=device)
+        self.missing, self.lost = (torch.zeros((1,), dtype=torch.int32, device=device) for _ in range(2))
 
     def extend(self, sequences: Optional[torch.Tensor], new: torch.Tensor, tokens: int, max_q: int, max_kv: int,
                out: Optional[mpq.PagePlan] = None) -> Batch:
@@ -99,6 +99,7 @@ class DevicePages:
         padded to ``tokens``; max_q and max_kv bound a sequence's new tokens and its context."""
         plan = mpq.pages_extend(self.state, sequences, new, tokens, out)
         self.missing = plan.missing
+        self.lost.bitwise_or_(plan.missing)
         return Batch(plan.slots, plan.q_starts, plan.kv_lens, plan.table, max_q, max_kv)
 
     def trim(self, sequences: Optional[torch.Tensor], keep: torch.Tensor):
@@ -106,11 +107,13 @@ class DevicePages:
         mpq.pages_trim(self.state, sequences, keep)
 
     def check(self):
-        """Raises if the last batch did not fit (nothing was taken for it then).  Waits for the stream."""
-        missing = int(self.missing)
-        if missing:
-            raise MemoryError("a sequence outgrows its row of the table" if missing == -1 else "the batch has more tokens than slots" if missing == -2
-                              else "the cache is full: %d pages are missing" % missing)
+        """Raises if a batch since the state was made or last checked did not fit: nothing was taken for it then, its tokens are in no
+        slot and what was drawn for it means nothing.  Waits for the stream."""
+        lost, missing = torch.cat([self.lost, self.missing]).tolist()
+        if lost:
+            self.lost.zero_()
+            raise MemoryError("an earlier batch did not fit" if missing == 0 else "a sequence outgrows its row of the table" if missing == -1
+                              else "the batch has more tokens than slots" if missing == -2 else "the cache is full: %d pages are missing" % missing)
 
 
 PRODUCTS = ("qkv", "o", "up", "down")                      # of a layer, on levels

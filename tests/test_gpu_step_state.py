@@ -2,11 +2,46 @@
 import pytest
 import torch
 
+from paper_1905_13389_b200 import decoder
+
 pytestmark = pytest.mark.gpu
 
 
 def ints(*v):
     return torch.tensor(v, dtype=torch.int32, device="cuda:0")
+
+
+def test_a_shortage_is_remembered_until_it_is_looked_for(mpq, cuda):
+    """A step that lacks pages between steps that do not, in eager calls and in a graph that is replayed."""
+    pages = decoder.DevicePages(4, 16, 3, 4, cuda)
+    first, one = ints(0), ints(16)
+    pages.extend(first, ints(0), 16, 16, 64)                  # (warms up)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pages.extend(first, one, 16, 16, 64)
+    pages.check()
+    for lost in (False, True):
+        for _ in range(4):
+            graph.replay()
+        if lost:
+            graph.replay()                                    # a fifth page
+        pages.trim(ints(0), ints(32))
+        graph.replay()                                        # ... and again one that fits
+        if lost:
+            with pytest.raises(MemoryError, match="earlier"):
+                pages.check()
+        pages.check()
+        pages.trim(ints(0), ints(0))
+    for _ in range(2):                                        # the same without a graph
+        pages.extend(ints(0, 1), ints(40, 40), 80, 40, 64)
+        pages.extend(ints(2), ints(3), 3, 3, 64)
+        with pytest.raises(MemoryError, match="earlier"):
+            pages.check()
+        pages.check()
+    pages.extend(ints(0, 1), ints(40, 40), 80, 40, 64)        # the last batch itself says what it lacked
+    with pytest.raises(MemoryError, match="pages are missing"):
+        pages.check()
+    pages.check()
 
 
 def test_adapters_in_another_order_are_refused(mpq, cuda):
