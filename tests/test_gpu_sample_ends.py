@@ -12,6 +12,10 @@ TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 LONG = np.longdouble
 
 
+def upto_of(w, n):
+    return w[:n].sum()
+
+
 def allowed(x, warm, k, p, least, u):
     """One row: the tokens that may be drawn.  A weight is a whole multiple of 2^-shift of the largest one, which is exact: the nearest to a
     number that is off by 2^-42 of itself at most.  So it is off by that and by half a multiple, or by itself where it comes out as
@@ -43,12 +47,14 @@ def allowed(x, warm, k, p, least, u):
         if least > 0:
             sure = max(1, int((w[:size] - off[:size] - unit >= least).sum()))
             maybe = max(1, int((w[:size] + off[:size] >= least).sum()))
-        for few in {sure, maybe}:
+        # (where weights differ by less than their errors any number of them may reach min-p: all numbers, or the ends as above)
+        wide_min = upto_of(w, maybe) - upto_of(w, sure) if maybe - sure > 64 else LONG(0)
+        for few in range(sure, maybe + 1) if maybe - sure <= 64 else (sure, maybe):
             at = np.argsort(order[:few])
             mine, err = w[:few][at], off[:few][at]
             upto, by = np.cumsum(mine), np.cumsum(err)
             share = LONG(min(max(u, 0.0), 1.0))
-            goal, wide = share * upto[-1], by + share * by[-1] + unit + spare
+            goal, wide = share * upto[-1], by + share * by[-1] + unit + spare + wide_min
             # (a token that may come out as nothing is not drawn for sure, one that must come out as nothing never)
             can = (upto - mine - wide <= goal) & (goal <= upto + wide) & (mine + err > unit / 2)
             if not can.any():                                 # u = 1: behind all sums
