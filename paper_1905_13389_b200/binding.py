@@ -769,8 +769,8 @@ def _pages(s: PageState, seqs: Optional[torch.Tensor], amount: torch.Tensor):
 
 
 def pages_extend(state: PageState, seqs: Optional[torch.Tensor], new: torch.Tensor, tokens: int, out: Optional[PagePlan] = None) -> PagePlan:
-    """Takes pages for ``new`` tokens (int32 [batch]) of the sequences ``seqs`` (int32 [batch], -1: padding; None: 0, 1, ..)
-    and describes the batch, its slots padded to ``tokens`` with -1.  All or nothing: missing says what did not fit."""
+    """Takes pages for ``new`` tokens (int32 [batch]) of the sequences ``seqs`` (int32 [batch], no number twice, -1: padding; None:
+    0, 1, ..) and describes the batch, its slots padded to ``tokens`` with -1.  All or nothing: missing says what did not fit."""
     dev, per, batch, args = _pages(state, seqs, new)
     if out is None:
         ints = torch.empty_strided((2 * batch + 2,), (1,), dtype=torch.int32, device=new.device)
@@ -786,8 +786,8 @@ def pages_extend(state: PageState, seqs: Optional[torch.Tensor], new: torch.Tens
 
 
 def pages_trim(state: PageState, seqs: Optional[torch.Tensor], keep: torch.Tensor) -> PageState:
-    """Shortens the sequences ``seqs`` to ``keep`` tokens (int32 [batch]; 0 drops one, a negative number leaves it) and gives
-    the pages behind them back."""
+    """Shortens the sequences ``seqs`` (no number twice) to ``keep`` tokens (int32 [batch]; 0 drops one, a negative number leaves it)
+    and gives the pages behind them back."""
     dev, _, _, args = _pages(state, seqs, keep)
     st = (_lib or lib()).mpq_pages_trim(*args, _raw_stream(dev))
     if st:

@@ -417,10 +417,10 @@ __device__ __forceinline__ void umma_f16_pair(uint32_t d, uint64_t a, uint64_t b
 // of a part are a block, ranks that are not there are read as zeros).  Other tiles, with ends of sequences in them, have it
 // from low_rank_tile: 16 rows and 64 columns by 16 x 8 x 16 matrix instructions of the storing warps, a lane owning four adjacent
 // ranks of 16 in both operands alike, one adapter after the other of those that the rows have: a row takes its own one's
-// sums alone, so that nothing of another's reaches it.  4096^3 with rank 64: 92 us where one sequence has all rows (28 of
-// them the first kernel's), 115 with six; all tiles the second way 120 to 127, bound by L1 lookups.  PARTS: of z, 32-bit results have all of it, 16-bit ones two parts,
-// 2^-16 of it in bfloat16 and 2^-22 in float16, a small part of their own last rounding unless the product and its adapter cancel
-// (a third part: six sequences 110 -> 117 us, 4096 x 4096 x 512 with rank 128 103 -> 114).
+// sums alone, so that nothing of another's reaches it.  4096^3 with rank 64: 88 us where one sequence has all rows (28 of
+// them the first kernel's), 110 with six; all tiles the second way 120 to 127, bound by L1 lookups.  PARTS: of z; 32-bit
+// results have all of it, 16-bit ones two parts, which lose 2^-16 of it in bfloat16 and 2^-22 in float16, little beside
+// their own last rounding unless the product and its adapter cancel (a third part: six sequences 110 -> 117 us, 4096 x 4096 x 512 with rank 128 103 -> 114).
 template <typename W, int PARTS>
 __device__ __forceinline__ void low_rank_tile(const LinearArgs& g, int64_t row0, int64_t c0, uint32_t at, int lane, int turn) {
     const int row = lane >> 2, quad = lane & 3;

@@ -7,7 +7,7 @@
 // itself: what is less than half a multiple weighs nothing and is never drawn, however much of it there is.
 // (With 32-bit weights a tail token of a flat row of 131,072 is another one in some percent of the draws.)
 // Bound by issuing: some 30 instructions an element for a weight, 11 of them FP64.  256 x 131072 in bfloat16 by temperature take
-// 94 us (memory would take 10), top-p over 256 x 151000 in 32 bits 204; a row alone is bound by latency, 30 us with every rule.
+// 87 us (memory would take 10), top-p over 256 x 151000 in 32 bits 204; a row alone is bound by latency, 30 us with every rule.
 //
 // A row belongs to one CTA, or where there are few rows to a cluster of up to four.  Shares that are small enough stay in shared
 // memory; of larger ones only the first look goes to memory, the later ones find the row in L2.  Nothing is sorted.  Where
